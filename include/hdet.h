@@ -302,6 +302,168 @@ const char* hdet_last_error(hdet_handle* h);
 /* Releases the control block and the handle.  hdet_destroy(NULL) is a no-op.                */
 int hdet_destroy(hdet_handle* h);
 
+/* ---------------------------------------------------------------------------------------
+ * Operators of language models
+ *
+ * What a program calls that forms its own forward and backward pass -- N replicas of a
+ * residual network with a root-mean-square norm, linear layers whose inputs and weights are
+ * held in 8 bits, and an output layer with its cross-entropy -- and hands the gradients to
+ * hdet_fanout_step.  No handle: every call enqueues its kernels on `stream` (hipStream_t or
+ * NULL), waits for nothing, allocates nothing and keeps nothing; scratch memory is the
+ * caller's.  Errors: HDET_EINVAL for what the argument checks refuse (nothing has been
+ * enqueued then), HDET_EHIP; the message is that of hdet_last_error(NULL).
+ *
+ * Matrices are hdet_rows: N replicas of a matrix of rows, columns next to each other.  Strides
+ * are in elements; any that keep rows and replicas apart (of an output: no two elements may
+ * share memory).  Rows of whole 16-byte pieces at 16-byte boundaries are the fastest, by a
+ * factor of two and more.  Outputs may not lie over inputs unless stated otherwise.  With no
+ * rows the sums over them (gradients of weights, mean losses) are written as 0.
+ *
+ * A matrix in 8 bits: codes -127 .. 127 and one fp32 scale a row; entry = code * scale.  The
+ * codes of a row start 16-byte aligned (row and replica strides are multiples of 16) and are
+ * followed by zeros up to the next multiple of 16 columns: hdet_rmsnorm and hdet_quantise_rows
+ * write them so.  Those two choose as scale the smallest power of two, from 2^-126 on, that
+ * takes the row's largest entry to 127 or less, and round to the nearest code, halves to even.  A
+ * power of two costs up to one of the eight bits and makes code * scale a bfloat16 number: the
+ * gradients below multiply the values themselves, with nothing rounded on the way.  A row with an
+ * entry that is not finite has scale NaN and codes 0.  (The type's largest numbers read back as
+ * infinity: the nearest code stands for 2^128.)
+ * ------------------------------------------------------------------------------------- */
+enum { HDET_TYPE_F32 = 0, HDET_TYPE_BF16 = 1 };               /* element type of a matrix    */
+#define HDET_MAX_NORM_WIDTH 32768                             /* a row is held in registers  */
+#define HDET_MAX_CODES_WIDTH 131056                           /* 32-bit sums of code products */
+
+typedef struct {
+  void*   dev;             /* element (replica r, row i, column j) at r * replica_stride +    */
+  int64_t row_stride;      /* i * row_stride + j; NULL: absent                               */
+  int64_t replica_stride;
+} hdet_rows;
+
+/* Root-mean-square norm of a residual sum:
+ *   u = x + resid (u = x without resid),  total = u,  rstd = 1 / sqrt(mean_j u_j^2 + eps),
+ *   y_j = u_j rstd gain_j,  codes and scale: y in 8 bits.
+ * Sums in fp32; the norm is that of u before it is rounded to `total`.  total, y, codes (with
+ * scale) and rstd are written where they are given.  total may be x or resid itself.          */
+typedef struct {
+  int32_t   n_replicas;
+  int32_t   dtype;         /* HDET_TYPE_* of x, resid, total and y                           */
+  int64_t   rows;          /* per replica, 0 allowed                                         */
+  int32_t   width;         /* 1 .. HDET_MAX_NORM_WIDTH                                       */
+  int32_t   reserved;
+  double    eps;           /* >= 0                                                           */
+  hdet_rows x, resid, total, y;
+  hdet_rows codes;         /* int8                                                           */
+  float*    scale_dev;     /* [N][rows]; with codes                                          */
+  float*    rstd_dev;      /* [N][rows]                                                      */
+  const float* gain_dev;   /* [width] per replica, gain_stride apart                         */
+  int64_t   gain_stride;
+} hdet_norm_args;
+int hdet_rmsnorm(const hdet_norm_args* args, void* stream);
+
+/* Backward pass: dy is the gradient at y (or at the values the codes stand for: rounding to 8
+ * bits counts as the identity), dtotal (optional) what arrives at `total` by the residual
+ * stream.  With h = total as stored and xh_j = h_j rstd:
+ *   dx_j = rstd (dy_j gain_j - xh_j mean_i(dy_i gain_i xh_i)) + dtotal_j     (of x and of resid)
+ *   dgain_j = sum over the rows of dy_j xh_j                       (in a fixed order; optional)
+ * dx may be dy or dtotal itself.  workspace: hdet_rmsnorm_backward_workspace bytes (needed for
+ * dgain only), 16-byte aligned.                                                             */
+typedef struct {
+  int32_t   n_replicas, dtype;                 /* HDET_TYPE_* of total, dy, dtotal and dx    */
+  int64_t   rows;
+  int32_t   width, reserved;
+  hdet_rows total, dy, dtotal, dx;
+  const float* rstd_dev;   /* [N][rows]                                                      */
+  const float* gain_dev;
+  int64_t   gain_stride;
+  float*    dgain_dev;     /* [width] per replica, dgain_stride apart, or NULL               */
+  int64_t   dgain_stride;
+  void*     workspace_dev;
+  size_t    workspace_bytes;
+} hdet_norm_grad_args;
+int hdet_rmsnorm_backward_workspace(int32_t n_replicas, int64_t rows, int32_t width, size_t* bytes);
+int hdet_rmsnorm_backward(const hdet_norm_grad_args* args, void* stream);
+
+/* Rows to 8 bits (weights for hdet_quantised_linear, activations kept for the backward pass)
+ * and back.  Reading back multiplies code and scale and rounds to dtype.                    */
+typedef struct {
+  int32_t   n_replicas, dtype;                 /* HDET_TYPE_* of values                      */
+  int64_t   rows;
+  int32_t   width, reserved;                   /* 1 .. HDET_MAX_NORM_WIDTH to quantise, ..   */
+  hdet_rows values, codes;                     /* .. HDET_MAX_CODES_WIDTH to restore         */
+  float*    scale_dev;                         /* [N][rows]                                  */
+} hdet_codes_args;
+int hdet_quantise_rows(const hdet_codes_args* args, void* stream);      /* reads values       */
+int hdet_restore_rows(const hdet_codes_args* args, void* stream);       /* writes values      */
+
+/* y = X W^T + bias with X [rows][d_in] and W [d_out][d_in] in 8 bits: whole-number sums of code
+ * products (exact in 32 bits), times both scales, plus bias, rounded once.  Scales may be any
+ * numbers here.                                                                             */
+typedef struct {
+  int32_t   n_replicas, y_dtype;               /* HDET_TYPE_* of y                           */
+  int64_t   rows;
+  int32_t   d_in, d_out;                       /* d_in up to HDET_MAX_CODES_WIDTH            */
+  hdet_rows codes, w_codes;
+  const float* scale_dev;                      /* [N][rows]                                  */
+  const float* w_scale_dev;                    /* [N][d_out]                                 */
+  const float* bias_dev;                       /* [d_out] per replica, bias_stride apart, or NULL */
+  int64_t   bias_stride;
+  hdet_rows y;
+} hdet_linear_args;
+int hdet_quantised_linear(const hdet_linear_args* args, void* stream);
+
+/* Gradients of that layer from the 8-bit copies and dy (bfloat16):
+ *   dx = dy W (bfloat16, optional),  dw = dy^T X (fp32, optional),  db = sum over the rows of dy (fp32, optional)
+ * in bfloat16 products with fp32 sums.  The values code * scale are read as bfloat16 numbers: exact for the
+ * scales that this library chooses, rounded for others.  X (for dw) and W (for dx) pass through the workspace in bfloat16:
+ * hdet_quantised_linear_backward_workspace bytes, 16-byte aligned.                          */
+typedef struct {
+  int32_t   n_replicas, reserved;
+  int64_t   rows;
+  int32_t   d_in, d_out;
+  hdet_rows dy, codes, w_codes;
+  const float* scale_dev;
+  const float* w_scale_dev;
+  hdet_rows dx, dw;
+  float*    db_dev;
+  int64_t   db_stride;
+  void*     workspace_dev;
+  size_t    workspace_bytes;
+} hdet_linear_grad_args;
+int hdet_quantised_linear_backward_workspace(int32_t n_replicas, int64_t rows, int32_t d_in, int32_t d_out, size_t* bytes);
+int hdet_quantised_linear_backward(const hdet_linear_grad_args* args, void* stream);
+
+/* Output layer with its softmax cross-entropy, in pieces of the vocabulary: neither the logits
+ * z = h W^T + bias nor their gradient are held for more than `piece` classes.  A row counts if its
+ * label is in 0 .. classes - 1; c = rows of the replica that count, at least 1.
+ *   row_loss = log sum_v exp(z_v) - z_label, 0 for rows that do not count
+ *   mean_loss = sum of row_loss / c
+ *   dz_v = (softmax(z)_v - [v = label]) / c, 0 for rows that do not count
+ *   dh = dz W,   dw = dz^T h,   db = sum over the rows of dz
+ * h, W and dh are bfloat16; sums are fp32.  dw is bfloat16 or fp32.  dh and a bfloat16 dw are
+ * formed from dz rounded to bfloat16, an fp32 dw from dz in three such parts (24 bits) and with two more
+ * products.  dh, dw and db are optional: without them only the losses are formed.  A bias of -inf takes a class out of the sum; a row that counts and has no class left is NaN.
+ * piece: classes at a time, or 0 for the library's choice.  The workspace depends on it
+ * (hdet_vocab_loss_workspace with the same arguments; without dw as for a bfloat16 one); 16-byte aligned. */
+typedef struct {
+  int32_t   n_replicas, dw_dtype;              /* HDET_TYPE_* of dw                          */
+  int64_t   rows;
+  int32_t   width, classes;
+  int32_t   piece, reserved;
+  hdet_rows h, w;                              /* bfloat16: [rows][width], [classes][width]  */
+  const float* bias_dev;                       /* [classes] per replica, bias_stride apart, or NULL */
+  int64_t   bias_stride;
+  const int32_t* labels_dev;                   /* [N][rows]                                  */
+  float*    row_loss_dev;                      /* [N][rows]                                  */
+  float*    mean_loss_dev;                     /* [N]                                        */
+  hdet_rows dh, dw;
+  float*    db_dev;                            /* or NULL                                    */
+  int64_t   db_stride;
+  void*     workspace_dev;
+  size_t    workspace_bytes;
+} hdet_vocab_args;
+int hdet_vocab_loss_workspace(int32_t n_replicas, int64_t rows, int32_t width, int32_t classes, int32_t dw_dtype, int32_t piece, size_t* bytes);
+int hdet_vocab_loss(const hdet_vocab_args* args, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

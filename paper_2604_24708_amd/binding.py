@@ -23,11 +23,16 @@ HDET_FP32, HDET_BF16_GEMM_FP32_MASTER = 0, 1
 HDET_FLAT, HDET_MLP, HDET_TRANSFORMER = 0, 1, 2
 HDET_CH_LR, HDET_CH_DROPOUT, HDET_CH_WD, HDET_CH_LABEL_SMOOTH, HDET_CH_ATTN_TEMP = 0, 1, 2, 3, 4
 HDET_FUSE_CONVERGE = 1
+HDET_TYPE_F32, HDET_TYPE_BF16 = 0, 1
+HDET_MAX_NORM_WIDTH, HDET_MAX_CODES_WIDTH = 32768, 131056
 
 EXPORTS = [
     "hdet_workspace_bytes", "hdet_create", "hdet_warm_init", "hdet_warm_init_noalloc", "hdet_forward_backward", "hdet_fanout_step", "hdet_train_step",
     "hdet_converge", "hdet_autolr_update", "hdet_get_state", "hdet_set_state",
     "hdet_set_launch_shape", "hdet_last_error", "hdet_destroy",
+    "hdet_rmsnorm", "hdet_rmsnorm_backward_workspace", "hdet_rmsnorm_backward", "hdet_quantise_rows", "hdet_restore_rows",
+    "hdet_quantised_linear", "hdet_quantised_linear_backward_workspace", "hdet_quantised_linear_backward",
+    "hdet_vocab_loss_workspace", "hdet_vocab_loss",
 ]
 
 
@@ -89,6 +94,49 @@ class hdet_state(C.Structure):
     ]
 
 
+class hdet_rows(C.Structure):
+    _fields_ = [("dev", C.c_void_p), ("row_stride", C.c_int64), ("replica_stride", C.c_int64)]
+
+
+class hdet_norm_args(C.Structure):
+    _fields_ = [("n_replicas", C.c_int32), ("dtype", C.c_int32), ("rows", C.c_int64), ("width", C.c_int32), ("reserved", C.c_int32),
+                ("eps", C.c_double), ("x", hdet_rows), ("resid", hdet_rows), ("total", hdet_rows), ("y", hdet_rows), ("codes", hdet_rows),
+                ("scale_dev", C.c_void_p), ("rstd_dev", C.c_void_p), ("gain_dev", C.c_void_p), ("gain_stride", C.c_int64)]
+
+
+class hdet_norm_grad_args(C.Structure):
+    _fields_ = [("n_replicas", C.c_int32), ("dtype", C.c_int32), ("rows", C.c_int64), ("width", C.c_int32), ("reserved", C.c_int32),
+                ("total", hdet_rows), ("dy", hdet_rows), ("dtotal", hdet_rows), ("dx", hdet_rows),
+                ("rstd_dev", C.c_void_p), ("gain_dev", C.c_void_p), ("gain_stride", C.c_int64), ("dgain_dev", C.c_void_p),
+                ("dgain_stride", C.c_int64), ("workspace_dev", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+class hdet_codes_args(C.Structure):
+    _fields_ = [("n_replicas", C.c_int32), ("dtype", C.c_int32), ("rows", C.c_int64), ("width", C.c_int32), ("reserved", C.c_int32),
+                ("values", hdet_rows), ("codes", hdet_rows), ("scale_dev", C.c_void_p)]
+
+
+class hdet_linear_args(C.Structure):
+    _fields_ = [("n_replicas", C.c_int32), ("y_dtype", C.c_int32), ("rows", C.c_int64), ("d_in", C.c_int32), ("d_out", C.c_int32),
+                ("codes", hdet_rows), ("w_codes", hdet_rows), ("scale_dev", C.c_void_p), ("w_scale_dev", C.c_void_p),
+                ("bias_dev", C.c_void_p), ("bias_stride", C.c_int64), ("y", hdet_rows)]
+
+
+class hdet_linear_grad_args(C.Structure):
+    _fields_ = [("n_replicas", C.c_int32), ("reserved", C.c_int32), ("rows", C.c_int64), ("d_in", C.c_int32), ("d_out", C.c_int32),
+                ("dy", hdet_rows), ("codes", hdet_rows), ("w_codes", hdet_rows), ("scale_dev", C.c_void_p), ("w_scale_dev", C.c_void_p),
+                ("dx", hdet_rows), ("dw", hdet_rows), ("db_dev", C.c_void_p), ("db_stride", C.c_int64),
+                ("workspace_dev", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+class hdet_vocab_args(C.Structure):
+    _fields_ = [("n_replicas", C.c_int32), ("dw_dtype", C.c_int32), ("rows", C.c_int64), ("width", C.c_int32), ("classes", C.c_int32),
+                ("piece", C.c_int32), ("reserved", C.c_int32), ("h", hdet_rows), ("w", hdet_rows), ("bias_dev", C.c_void_p),
+                ("bias_stride", C.c_int64), ("labels_dev", C.c_void_p), ("row_loss_dev", C.c_void_p), ("mean_loss_dev", C.c_void_p),
+                ("dh", hdet_rows), ("dw", hdet_rows), ("db_dev", C.c_void_p), ("db_stride", C.c_int64),
+                ("workspace_dev", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libhdet.so")
 _lib = None
 
@@ -130,6 +178,14 @@ def load_library(path: Optional[str] = None):
     lib.hdet_last_error.argtypes = [vp]
     lib.hdet_last_error.restype = C.c_char_p
     lib.hdet_destroy.argtypes = [vp]
+    for name, args in (("hdet_rmsnorm", hdet_norm_args), ("hdet_rmsnorm_backward", hdet_norm_grad_args), ("hdet_quantise_rows", hdet_codes_args),
+                       ("hdet_restore_rows", hdet_codes_args), ("hdet_quantised_linear", hdet_linear_args),
+                       ("hdet_quantised_linear_backward", hdet_linear_grad_args), ("hdet_vocab_loss", hdet_vocab_args)):
+        getattr(lib, name).argtypes = [C.POINTER(args), vp]
+    size = C.POINTER(C.c_size_t)
+    lib.hdet_rmsnorm_backward_workspace.argtypes = [C.c_int32, C.c_int64, C.c_int32, size]
+    lib.hdet_quantised_linear_backward_workspace.argtypes = [C.c_int32, C.c_int64, C.c_int32, C.c_int32, size]
+    lib.hdet_vocab_loss_workspace.argtypes = [C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32, size]
     for name in EXPORTS:
         if name != "hdet_last_error":
             getattr(lib, name).restype = C.c_int
@@ -279,3 +335,192 @@ def hdet_last_error(h=None) -> str:
 
 def hdet_destroy(h):
     _check(load_library().hdet_destroy(h))
+
+
+# ---------------------------------------------------------------------------------------
+# Operators of language models.  Matrices are device tensors [N, rows, columns] whose columns are next to each other (any strides
+# between rows and replicas); vectors a replica are [N, columns]; row scalars [N, rows] are contiguous.  `stream`: a hipStream_t as
+# an integer, None for the default stream.  Tensors are borrowed until the work on that stream is done.
+# ---------------------------------------------------------------------------------------
+def _dtype_code(t) -> int:
+    import torch
+    if t.dtype == torch.float32:
+        return HDET_TYPE_F32
+    if t.dtype == torch.bfloat16:
+        return HDET_TYPE_BF16
+    raise ValueError(f"dtype {t.dtype}: float32 or bfloat16 is wanted")
+
+
+def _need(name, t, shape, dtype, contiguous=False):
+    """The tensor t, refused unless it has this shape and type, lies on a GPU, and has its last dimension's elements next to each other."""
+    if tuple(t.shape) != tuple(shape):
+        raise ValueError(f"{name} has shape {tuple(t.shape)}, {tuple(shape)} is wanted")
+    if t.dtype != dtype:
+        raise ValueError(f"{name} is {t.dtype}, {dtype} is wanted")
+    if t.device.type != "cuda":
+        raise ValueError(f"{name} is on {t.device}: device memory is wanted")
+    if contiguous and not t.is_contiguous():
+        raise ValueError(f"{name} must be contiguous")
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError(f"{name}: the last dimension's elements must be next to each other")
+    return t
+
+
+def _rows_of(name, t, shape, dtype) -> hdet_rows:
+    if t is None:
+        return hdet_rows()
+    _need(name, t, shape, dtype)
+    return hdet_rows(t.data_ptr(), t.stride(1), t.stride(0))
+
+
+def _codes_of(name, t, shape) -> hdet_rows:
+    """int8 codes; the strides of dimensions of size 1 say nothing and are made to fit."""
+    import torch
+    if t is None:
+        return hdet_rows()
+    _need(name, t, shape, torch.int8)
+    wide = (shape[2] + 15) // 16 * 16
+    row = t.stride(1) if shape[1] > 1 else max(wide, t.stride(1) // 16 * 16)
+    rep = t.stride(0) if shape[0] > 1 else row * max(shape[1], 1)
+    end = t.storage_offset() + (shape[0] - 1) * rep + (shape[1] - 1) * t.stride(1) + wide
+    if shape[0] and shape[1] and end > t.untyped_storage().nbytes():
+        raise ValueError(f"{name}: rows of codes end with zeros up to a multiple of 16 columns, which this tensor's memory does not hold")
+    return hdet_rows(t.data_ptr(), row, rep)
+
+
+def _vector(name, t, shape):
+    """(pointer, stride) of fp32 vectors [N, columns]"""
+    import torch
+    if t is None:
+        return None, 0
+    _need(name, t, shape, torch.float32)
+    return t.data_ptr(), t.stride(0) if shape[0] > 1 else max(t.stride(0), shape[1])
+
+
+def _scalars(name, t, shape, dtype=None):
+    """pointer of contiguous row scalars"""
+    import torch
+    return None if t is None else _need(name, t, shape, dtype or torch.float32, contiguous=True).data_ptr()
+
+
+def _call(name, args, stream):
+    _check(getattr(load_library(), name)(C.byref(args), stream))
+
+
+def _workspace(args, t):
+    if t is not None:
+        args.workspace_dev, args.workspace_bytes = t.data_ptr(), t.numel() * t.element_size()
+
+
+def _size_of(name, *args) -> int:
+    n = C.c_size_t()
+    _check(getattr(load_library(), name)(*args, C.byref(n)))
+    return n.value
+
+
+def hdet_codes_empty(n_replicas: int, rows: int, width: int, device="cuda"):
+    """int8 codes [N, rows, width] in memory whose rows are padded with zeros to a multiple of 16 columns."""
+    import torch
+    return torch.zeros(n_replicas, rows, (width + 15) // 16 * 16, dtype=torch.int8, device=device)[..., :width]
+
+
+def hdet_rmsnorm(x, gain, resid=None, total=None, y=None, codes=None, scale=None, rstd=None, eps: float = 1e-5, stream: Optional[int] = None):
+    """total = x + resid; y = total / rms(total) * gain; codes and scale: y in 8 bits; rstd = 1 / rms.  Writes those of the four that are given."""
+    n, rows, width = x.shape
+    a = hdet_norm_args(n_replicas=n, dtype=_dtype_code(x), rows=rows, width=width, eps=eps)
+    a.x, a.resid = _rows_of("x", x, x.shape, x.dtype), _rows_of("resid", resid, x.shape, x.dtype)
+    a.total, a.y, a.codes = _rows_of("total", total, x.shape, x.dtype), _rows_of("y", y, x.shape, x.dtype), _codes_of("codes", codes, x.shape)
+    a.scale_dev, a.rstd_dev = _scalars("scale", scale, (n, rows)), _scalars("rstd", rstd, (n, rows))
+    a.gain_dev, a.gain_stride = _vector("gain", gain, (n, width))
+    _call("hdet_rmsnorm", a, stream)
+
+
+def hdet_rmsnorm_backward_workspace(n_replicas: int, rows: int, width: int) -> int:
+    return _size_of("hdet_rmsnorm_backward_workspace", n_replicas, rows, width)
+
+
+def hdet_rmsnorm_backward(total, gain, rstd, dy, dx, dtotal=None, dgain=None, workspace=None, stream: Optional[int] = None):
+    """dx (of x and of resid) and dgain from the gradients at y (dy) and at total (dtotal)."""
+    n, rows, width = total.shape
+    a = hdet_norm_grad_args(n_replicas=n, dtype=_dtype_code(total), rows=rows, width=width)
+    a.total, a.dy = _rows_of("total", total, total.shape, total.dtype), _rows_of("dy", dy, total.shape, total.dtype)
+    a.dtotal, a.dx = _rows_of("dtotal", dtotal, total.shape, total.dtype), _rows_of("dx", dx, total.shape, total.dtype)
+    a.rstd_dev = _scalars("rstd", rstd, (n, rows))
+    a.gain_dev, a.gain_stride = _vector("gain", gain, (n, width))
+    a.dgain_dev, a.dgain_stride = _vector("dgain", dgain, (n, width))
+    _workspace(a, workspace)
+    _call("hdet_rmsnorm_backward", a, stream)
+
+
+def _codes_call(name, values, codes, scale, stream):
+    n, rows, width = values.shape
+    a = hdet_codes_args(n_replicas=n, dtype=_dtype_code(values), rows=rows, width=width, scale_dev=_scalars("scale", scale, (n, rows)))
+    a.values, a.codes = _rows_of("values", values, values.shape, values.dtype), _codes_of("codes", codes, values.shape)
+    _call(name, a, stream)
+
+
+def hdet_quantise_rows(values, codes, scale, stream: Optional[int] = None):
+    """codes, scale <- values, a power of two as each row's scale."""
+    _codes_call("hdet_quantise_rows", values, codes, scale, stream)
+
+
+def hdet_restore_rows(codes, scale, values, stream: Optional[int] = None):
+    """values <- codes * scale."""
+    _codes_call("hdet_restore_rows", values, codes, scale, stream)
+
+
+def hdet_quantised_linear(codes, scale, w_codes, w_scale, y, bias=None, stream: Optional[int] = None):
+    """y [N, rows, d_out] <- (codes * scale) (w_codes * w_scale)^T + bias."""
+    n, rows, d_in = codes.shape
+    d_out = w_codes.shape[1]
+    a = hdet_linear_args(n_replicas=n, y_dtype=_dtype_code(y), rows=rows, d_in=d_in, d_out=d_out)
+    a.codes, a.w_codes = _codes_of("codes", codes, codes.shape), _codes_of("w_codes", w_codes, (n, d_out, d_in))
+    a.scale_dev, a.w_scale_dev = _scalars("scale", scale, (n, rows)), _scalars("w_scale", w_scale, (n, d_out))
+    a.bias_dev, a.bias_stride = _vector("bias", bias, (n, d_out))
+    a.y = _rows_of("y", y, (n, rows, d_out), y.dtype)
+    _call("hdet_quantised_linear", a, stream)
+
+
+def hdet_quantised_linear_backward_workspace(n_replicas: int, rows: int, d_in: int, d_out: int) -> int:
+    return _size_of("hdet_quantised_linear_backward_workspace", n_replicas, rows, d_in, d_out)
+
+
+def hdet_quantised_linear_backward(dy, codes, scale, w_codes, w_scale, dx=None, dw=None, db=None, workspace=None, stream: Optional[int] = None):
+    """dx = dy W (bfloat16), dw = dy^T X (fp32), db = the rows' sum of dy (fp32), from the 8-bit copies; those that are given."""
+    import torch
+    n, rows, d_out = dy.shape
+    d_in = codes.shape[2]
+    a = hdet_linear_grad_args(n_replicas=n, rows=rows, d_in=d_in, d_out=d_out)
+    a.dy = _rows_of("dy", dy, dy.shape, torch.bfloat16)
+    a.codes, a.w_codes = _codes_of("codes", codes, (n, rows, d_in)), _codes_of("w_codes", w_codes, (n, d_out, d_in))
+    a.scale_dev, a.w_scale_dev = _scalars("scale", scale, (n, rows)), _scalars("w_scale", w_scale, (n, d_out))
+    a.dx, a.dw = _rows_of("dx", dx, (n, rows, d_in), torch.bfloat16), _rows_of("dw", dw, (n, d_out, d_in), torch.float32)
+    a.db_dev, a.db_stride = _vector("db", db, (n, d_out))
+    _workspace(a, workspace)
+    _call("hdet_quantised_linear_backward", a, stream)
+
+
+def hdet_vocab_loss_workspace(n_replicas: int, rows: int, width: int, classes: int, dw=None, piece: int = 0) -> int:
+    """`dw`: the dtype of the weight gradient (float32 if None)."""
+    import torch
+    return _size_of("hdet_vocab_loss_workspace", n_replicas, rows, width, classes, HDET_TYPE_BF16 if dw == torch.bfloat16 else HDET_TYPE_F32, piece)
+
+
+def hdet_vocab_loss(h, w, labels, row_loss, mean_loss, dh=None, dw=None, bias=None, db=None, piece: int = 0, workspace=None,
+                    stream: Optional[int] = None):
+    """Cross-entropy of softmax(h w^T + bias) at `labels` (int32 [N, rows]; rows whose label is no class do not count), and its gradients."""
+    import torch
+    n, rows, width = h.shape
+    classes = w.shape[1]
+    a = hdet_vocab_args(n_replicas=n, rows=rows, width=width, classes=classes, piece=piece)
+    a.h, a.w = _rows_of("h", h, h.shape, torch.bfloat16), _rows_of("w", w, (n, classes, width), torch.bfloat16)
+    a.bias_dev, a.bias_stride = _vector("bias", bias, (n, classes))
+    a.labels_dev = _scalars("labels", labels, (n, rows), torch.int32)
+    a.row_loss_dev, a.mean_loss_dev = _scalars("row_loss", row_loss, (n, rows)), _scalars("mean_loss", mean_loss, (n,))
+    a.dh = _rows_of("dh", dh, h.shape, torch.bfloat16)
+    if dw is not None:
+        a.dw_dtype = _dtype_code(dw)
+        a.dw = _rows_of("dw", dw, (n, classes, width), dw.dtype)
+    a.db_dev, a.db_stride = _vector("db", db, (n, classes))
+    _workspace(a, workspace)
+    _call("hdet_vocab_loss", a, stream)

@@ -229,6 +229,14 @@ __device__ __forceinline__ void put_element(const hdet_bgemm_args& g, int z, int
     reinterpret_cast<float*>(g.c)[off] = v;
     return;
   }
+  if (EPI == HDET_EPI_ACCUM_BF16) {
+    float* p = g.accum + (int64_t)z * g.accum_bs + (int64_t)row * g.accum_ld + col;
+    if (!g.accum_first) v += *p;
+    if (!g.accum_last) {
+      *p = v;
+      return;
+    }
+  }
   if (EPI == HDET_EPI_BIAS_RELU_BF16) v = v > 0.f ? v : 0.f;
   if (EPI == HDET_EPI_MASK_BF16)         // gradient through the ReLU of the layer below
     v = bf2f(g.mask[(int64_t)z * g.mask_bs + (int64_t)row * g.mask_ld + col]) > 0.f ? v : 0.f;
@@ -712,6 +720,7 @@ hipError_t hdet_launch_bgemm(const hdet_bgemm_args& g_in, bool a_kmajor, bool b_
   if (a_kmajor) {                        // dgrad
     if (epi == HDET_EPI_MASK_BF16) return launch_general<true, false, HDET_EPI_MASK_BF16>(g, batch, aligned, s);
     if (epi == HDET_EPI_BF16) return launch_general<true, false, HDET_EPI_BF16>(g, batch, aligned, s);
+    if (epi == HDET_EPI_ACCUM_BF16) return launch_general<true, false, HDET_EPI_ACCUM_BF16>(g, batch, aligned, s);
     return hipErrorInvalidValue;
   }
   if (!b_kmajor) {                       // wgrad

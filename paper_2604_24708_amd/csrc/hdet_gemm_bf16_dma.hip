@@ -332,7 +332,12 @@ __device__ __forceinline__ void store_tile(const hdet_bgemm_args& g, const typen
           const us4 o = {f2bf(hdet_gelu_tanh_fast(bf2f(pre[0]))), f2bf(hdet_gelu_tanh_fast(bf2f(pre[1]))),
                          f2bf(hdet_gelu_tanh_fast(bf2f(pre[2]))), f2bf(hdet_gelu_tanh_fast(bf2f(pre[3])))};
           put(reinterpret_cast<us4*>(reinterpret_cast<uint16_t*>(g.c2) + off), o);
+        } else if (EPI == HDET_EPI_ACCUM_BF16 && !g.accum_last) {
+          float* const p = g.accum + (int64_t)z * g.accum_bs + (int64_t)row * g.accum_ld + col;
+          *reinterpret_cast<f4*>(p) = g.accum_first ? v : v + *reinterpret_cast<const f4*>(p);
         } else {
+          if (EPI == HDET_EPI_ACCUM_BF16 && !g.accum_first)
+            v += *reinterpret_cast<const f4*>(g.accum + (int64_t)z * g.accum_bs + (int64_t)row * g.accum_ld + col);
           const us4 o = {f2bf(v[0]), f2bf(v[1]), f2bf(v[2]), f2bf(v[3])};
           put(reinterpret_cast<us4*>(reinterpret_cast<uint16_t*>(g.c) + off), o);
           if (kColsum) {
@@ -1067,7 +1072,7 @@ constexpr tile_shape kSmall = {128, 128, 2, 3.1f, 0.44f, 18.1f, 0.8f};         /
 constexpr tile_shape kDeep = {128, 128, 1, 0.f, 0.f, 0.f, 0.f};                // K step 64, four stages
 template <int EPI> constexpr float kEpiTime =
     EPI == HDET_EPI_ADAMW ? 80.f : EPI == HDET_EPI_GELUGRAD_BF16 || EPI == HDET_EPI_BIAS_DROP_RESID_BF16 ? 20.f
-    : EPI == HDET_EPI_MASK_BF16 || EPI == HDET_EPI_BIAS_RESID_BF16 || EPI == HDET_EPI_BIAS_GELU_BF16 ? 15.f
+    : EPI == HDET_EPI_MASK_BF16 || EPI == HDET_EPI_BIAS_RESID_BF16 || EPI == HDET_EPI_ACCUM_BF16 || EPI == HDET_EPI_BIAS_GELU_BF16 ? 15.f
     : EPI == HDET_EPI_F32 || EPI == HDET_EPI_BIAS_F32 ? 12.f : EPI == HDET_EPI_BIAS_RELU_BF16 ? 9.f : 8.f;
 
 // What hdet_bgemm_walk_kernel asks for beyond the LDS-direct kernels: whole groups of 8 columns, results and their rows 16-byte aligned, four K steps
@@ -1184,11 +1189,12 @@ bool hdet_bgemm_dma_eligible(const hdet_bgemm_args& g, bool a_kmajor, bool b_kma
        ((reinterpret_cast<uintptr_t>(g.upd.theta) | reinterpret_cast<uintptr_t>(g.upd.m) | reinterpret_cast<uintptr_t>(g.upd.v)) & 15) ||
        (reinterpret_cast<uintptr_t>(g.upd.shadow) & 7)))
     return false;
-  // instantiated combinations: what the MLP and the transformer use
+  if (epi == HDET_EPI_ACCUM_BF16 && (!g.accum || ((g.accum_ld | g.accum_bs) & 3) || (reinterpret_cast<uintptr_t>(g.accum) & 15) || g.n1 * g.n2 != 1)) return false;
+  // instantiated combinations: what the MLP, the transformer and the loss in pieces use
   if (a_kmajor && b_kmajor)
     return epi == HDET_EPI_BIAS_RELU_BF16 || epi == HDET_EPI_BIAS_F32 || epi == HDET_EPI_BIAS_BF16 || epi == HDET_EPI_F32 ||
            epi == HDET_EPI_BIAS_GELU_BF16 || epi == HDET_EPI_BIAS_RESID_BF16 || epi == HDET_EPI_BIAS_DROP_RESID_BF16;
-  if (a_kmajor && !b_kmajor) return epi == HDET_EPI_MASK_BF16 || epi == HDET_EPI_BF16 || epi == HDET_EPI_GELUGRAD_BF16;
+  if (a_kmajor && !b_kmajor) return epi == HDET_EPI_MASK_BF16 || epi == HDET_EPI_BF16 || epi == HDET_EPI_GELUGRAD_BF16 || epi == HDET_EPI_ACCUM_BF16;
   if (!a_kmajor && !b_kmajor) return epi == HDET_EPI_F32 || epi == HDET_EPI_BF16 || epi == HDET_EPI_ADAMW;
   return false;
 }
@@ -1213,6 +1219,7 @@ hipError_t hdet_launch_bgemm_dma(const hdet_bgemm_args& g_in, bool a_kmajor, boo
   if (a_kmajor) {                        // dgrad
     if (epi == HDET_EPI_MASK_BF16) return launch_shape<true, false, HDET_EPI_MASK_BF16>(g, batch, s);
     if (epi == HDET_EPI_GELUGRAD_BF16) return launch_shape<true, false, HDET_EPI_GELUGRAD_BF16>(g, batch, s);
+    if (epi == HDET_EPI_ACCUM_BF16) return launch_shape<true, false, HDET_EPI_ACCUM_BF16>(g, batch, s);
     return launch_shape<true, false, HDET_EPI_BF16>(g, batch, s);
   }
   if (epi == HDET_EPI_F32) return launch_shape<false, false, HDET_EPI_F32>(g, batch, s);   // wgrad

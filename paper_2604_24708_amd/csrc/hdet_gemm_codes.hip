@@ -1,0 +1,227 @@
+// Product of two matrices in 8 bits, N replicas:  y = s_m t_o sum_k q[m][k] w[o][k] + b_o,  on v_mfma_i32_16x16x64_i8.  The sums of code products
+// are whole numbers below 2^31 and exact; both scales and the bias come in as fp32 where a sum is complete.
+//
+//  * Tiles (hdet_codes_gemm_kernel): both operands are contiguous along k and their rows start at 16-byte boundaries, with zeros behind the last
+//    column up to the next one, so every shape is made of whole 16-byte chunks.  Chunks go from global memory straight into LDS, a K step of 128 bytes a row,
+//    NST steps in flight; a row's chunks are permuted by row / 2 so that the 128-bit fragment reads are free of bank conflicts.  Rows past the matrix and
+//    chunks past k lie outside the buffer descriptor and arrive as zeros: no edge cases in the loop.
+//  * Few rows (hdet_codes_rows_kernel): the weights' stream is all there is; see there.
+
+#include "hdet_ops.h"
+#include "hdet_elem.h"
+#include "hdet_lds.h"
+
+namespace {
+
+typedef int i4v __attribute__((ext_vector_type(4)));
+typedef float f4 __attribute__((ext_vector_type(4)));
+typedef unsigned short us4 __attribute__((ext_vector_type(4)));
+
+constexpr uint32_t kAbsent = 0x80000000u;   // offset beyond every extent
+
+struct codes_args {
+  const int8_t *x, *w;
+  const float *x_scale, *w_scale, *bias;
+  void* y;
+  int64_t x_z, w_z, bias_z, y_z, x_ld, w_ld, y_ld;
+  int m, n, kbytes;          // kbytes: k rounded up to whole chunks
+};
+
+// extent of the rows from `row0` on, as a descriptor takes it (offsets inside a tile stay below 2^31)
+__device__ __forceinline__ uint32_t extent(int rows, int row0, int64_t ld, int kbytes) {
+  const int64_t e = (int64_t)(rows - row0 - 1) * ld + kbytes;
+  return e > 0x7fffffff ? 0x7fffffffu : (uint32_t)e;
+}
+__device__ __forceinline__ int swz(int r) { return (r >> 1) & 7; }
+
+// Four consecutive results of one row.  V4: rows of y are whole groups of four, 16 (8) bytes aligned.
+template <typename OUT, bool V4>
+__device__ __forceinline__ void put4(OUT* y, int col, int n, f4 v) {
+  if constexpr (V4) {
+    if (col < n) {
+      if constexpr (sizeof(OUT) == 4) *reinterpret_cast<f4*>(y + col) = v;
+      else *reinterpret_cast<hdet_u2v*>(y + col) = hdet_u2v{hdet_bf16_pack(v[0], v[1]), hdet_bf16_pack(v[2], v[3])};
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (col + e < n) hdet_st(y + col + e, v[e]);
+  }
+}
+
+}  // namespace
+
+template <typename OUT, bool V4, int TM, int TN, int WGM, int WGN, int NST>
+__global__ __launch_bounds__(64 * WGM * WGN, 160 * 1024 / (NST * (TM + TN) * 128) * (WGM * WGN / 4))
+void hdet_codes_gemm_kernel(const codes_args g) {
+  constexpr int THREADS = 64 * WGM * WGN, MB = TM / WGM / 16, NB = TN / WGN / 16;
+  constexpr int STAGE = (TM + TN) * 128, NA = TM * 128 / (THREADS * 16), NBL = TN * 128 / (THREADS * 16), LPT = NA + NBL;
+  __shared__ __attribute__((aligned(1024))) uint16_t S[NST * STAGE / 2];
+  const int z = blockIdx.z, m0 = blockIdx.y * TM, n0 = blockIdx.x * TN;
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wm = (wave / WGN) * (TM / WGM), wn = (wave % WGN) * (TN / WGN);
+  const hdet_rsrc ra = make_rsrc(g.x + z * g.x_z + (int64_t)m0 * g.x_ld, extent(g.m, m0, g.x_ld, g.kbytes));
+  const hdet_rsrc rb = make_rsrc(g.w + z * g.w_z + (int64_t)n0 * g.w_ld, extent(g.n, n0, g.w_ld, g.kbytes));
+  const uint32_t s_addr = lds_addr_of(S);
+  // chunk slot c = tid + i THREADS of a tile: row c / 8, chunk (c mod 8) ^ swz(row); THREADS / 8 rows apart the permutation is the same
+  const int ck = ((tid & 7) ^ swz(tid >> 3)) * 16;
+  const uint32_t off_a = (uint32_t)((tid >> 3) * g.x_ld + ck), off_b = (uint32_t)((tid >> 3) * g.w_ld + ck);
+  auto issue = [&](int i, int s, int kt) {
+    const bool ok = ck + kt * 128 < g.kbytes;
+    if (i < NA) lds_load16(ra, s_addr + s * STAGE + (i * THREADS + wave * 64) * 16, ok ? off_a + (uint32_t)(kt * 128 + i * (THREADS / 8) * g.x_ld) : kAbsent);
+    else lds_load16(rb, s_addr + s * STAGE + TM * 128 + ((i - NA) * THREADS + wave * 64) * 16, ok ? off_b + (uint32_t)(kt * 128 + (i - NA) * (THREADS / 8) * g.w_ld) : kAbsent);
+  };
+  static_assert(THREADS / 8 % 16 == 0, "the chunk permutation repeats every 16 rows");
+  i4v acc[MB][NB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i)
+#pragma unroll
+    for (int j = 0; j < NB; ++j) acc[i][j] = i4v{0, 0, 0, 0};
+  const int nk = (g.kbytes + 127) / 128;
+#pragma unroll
+  for (int s = 0; s < NST; ++s)
+#pragma unroll
+    for (int i = 0; i < LPT; ++i) issue(i, s, s);
+  wait_and_barrier<(NST - 1) * LPT>();
+  const int8_t* const base = reinterpret_cast<const int8_t*>(S);
+  i4v fa[2][MB], fb[2][NB];
+  auto read_frag = [&](int set, int s, int ss, int idx) {
+    const int r = lane & 15, ch = ((ss * 4 + (lane >> 4)) ^ swz(r)) * 16;
+    if (idx < NB) fb[set][idx] = *reinterpret_cast<const i4v*>(base + s * STAGE + TM * 128 + (wn + idx * 16 + r) * 128 + ch);
+    else if (idx < NB + MB) fa[set][idx - NB] = *reinterpret_cast<const i4v*>(base + s * STAGE + (wm + (idx - NB) * 16 + r) * 128 + ch);
+  };
+  constexpr int NM = MB * NB, NR = MB + NB, IPA = (NR + NM - 1) / NM, IPB = (NR + LPT + NM - 1) / NM;
+  auto multiply = [&](int set, int q) { acc[q / NB][q % NB] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[set][q % NB], fa[set][q / NB], acc[q / NB][q % NB], 0, 0, 0); };
+#pragma unroll
+  for (int idx = 0; idx < NR; ++idx) read_frag(0, 0, 0, idx);
+  for (int kt0 = 0; kt0 < nk; kt0 += NST) {
+#pragma unroll
+    for (int s = 0; s < NST; ++s) {
+      const int kt = kt0 + s;
+      if (kt >= nk) break;
+#pragma unroll
+      for (int q = 0; q < NM; ++q) {
+        multiply(0, q);
+#pragma unroll
+        for (int u = 0; u < IPA; ++u) read_frag(1, s, 1, q * IPA + u);
+        __builtin_amdgcn_sched_barrier(0);
+      }
+      // every wavefront has read all of this stage; the next one has landed
+      wait_and_barrier<(NST - 2) * LPT>();
+#pragma unroll
+      for (int q = 0; q < NM; ++q) {
+        multiply(1, q);
+#pragma unroll
+        for (int u = 0; u < IPB; ++u) {
+          const int it = q * IPB + u;
+          if (it < LPT) issue(it, s, kt + NST);
+          else read_frag(0, (s + 1) % NST, 0, it - LPT);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+      }
+    }
+  }
+  wait_and_barrier<0>();           // loads past the end have drained before the block gives its LDS up
+  // accumulator element e of lane l: row l mod 16, column 4 (l / 16) + e of its block
+  float sx[MB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i) {
+    const int row = m0 + wm + i * 16 + (lane & 15);
+    sx[i] = row < g.m ? g.x_scale[(int64_t)z * g.m + row] : 0.f;
+  }
+#pragma unroll
+  for (int j = 0; j < NB; ++j) {
+    const int col = n0 + wn + j * 16 + (lane >> 4) * 4;
+    f4 sw, b;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool ok = col + e < g.n;
+      sw[e] = ok ? g.w_scale[(int64_t)z * g.n + col + e] : 0.f;
+      b[e] = ok && g.bias ? g.bias[z * g.bias_z + col + e] : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < MB; ++i) {
+      const int row = m0 + wm + i * 16 + (lane & 15);
+      f4 v;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf((float)acc[i][j][e], sx[i] * sw[e], b[e]);
+      if (row < g.m) put4<OUT, V4>((OUT*)g.y + z * g.y_z + (int64_t)row * g.y_ld, col, g.n, v);
+    }
+  }
+}
+
+// Up to 64 rows: MB blocks of 16.  The weights' stream is the work: a block takes 16 columns of y, its four wavefronts a quarter of k each, with fragments
+// straight from global memory (16 rows of the weights, 64 bytes of each, an instruction) and no barrier in the loop; whole-number partial sums are added through LDS.
+template <typename OUT, int MB>
+__global__ __launch_bounds__(256) void hdet_codes_rows_kernel(const codes_args g) {
+  __shared__ i4v part[4][MB][64];
+  const int z = blockIdx.z, n0 = blockIdx.x * 16, m0 = blockIdx.y * (16 * MB), lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const hdet_rsrc unused = {0, 0, 0, 0};
+  (void)unused;
+  const auto ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(g.x + z * g.x_z + (int64_t)m0 * g.x_ld), 0, (int)extent(g.m, m0, g.x_ld, g.kbytes), 0x00020000);
+  const auto rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(g.w + z * g.w_z + (int64_t)n0 * g.w_ld), 0, (int)extent(g.n, n0, g.w_ld, g.kbytes), 0x00020000);
+  const int nk = (g.kbytes + 63) / 64, k0 = wave * nk / 4, k1 = (wave + 1) * nk / 4;
+  const int r = lane & 15, kc = (lane >> 4) * 16;
+  i4v acc[MB];
+#pragma unroll
+  for (int i = 0; i < MB; ++i) acc[i] = i4v{0, 0, 0, 0};
+#pragma unroll 4
+  for (int k = k0; k < k1; ++k) {
+    const int at = k * 64 + kc;
+    const bool ok = at < g.kbytes;
+    const i4v b = __builtin_bit_cast(i4v, __builtin_amdgcn_raw_buffer_load_b128(rb, ok ? (int)(r * g.w_ld) + at : (int)kAbsent, 0, 0));
+#pragma unroll
+    for (int i = 0; i < MB; ++i) {
+      const i4v a = __builtin_bit_cast(i4v, __builtin_amdgcn_raw_buffer_load_b128(ra, ok ? (int)((i * 16 + r) * g.x_ld) + at : (int)kAbsent, 0, 0));
+      acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b, a, acc[i], 0, 0, 0);
+    }
+  }
+#pragma unroll
+  for (int i = 0; i < MB; ++i) part[wave][i][lane] = acc[i];
+  __syncthreads();
+  const int col = n0 + (lane >> 4) * 4;
+  for (int i = wave; i < MB; i += 4) {
+    const int row = m0 + i * 16 + r;
+    if (row >= g.m) continue;
+    const i4v s = part[0][i][lane] + part[1][i][lane] + part[2][i][lane] + part[3][i][lane];
+    const float sx = g.x_scale[(int64_t)z * g.m + row];
+    f4 v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const bool ok = col + e < g.n;
+      v[e] = __builtin_fmaf((float)s[e], ok ? sx * g.w_scale[(int64_t)z * g.n + col + e] : 0.f, ok && g.bias ? g.bias[z * g.bias_z + col + e] : 0.f);
+    }
+    put4<OUT, false>((OUT*)g.y + z * g.y_z + (int64_t)row * g.y_ld, col, g.n, v);
+  }
+}
+
+namespace {
+
+template <typename OUT>
+hipError_t launch_typed(const codes_args& g, int n_replicas, hipStream_t s) {
+  const int size = sizeof(OUT);
+  const bool v4 = (reinterpret_cast<uintptr_t>(g.y) & (4 * size - 1)) == 0 && ((g.n | g.y_ld | g.y_z) & 3) == 0;
+  if (g.m <= 64) {
+    const dim3 grid((g.n + 15) / 16, 1, n_replicas);
+    if (g.m <= 16) hipLaunchKernelGGL((hdet_codes_rows_kernel<OUT, 1>), grid, dim3(256), 0, s, g);
+    else if (g.m <= 32) hipLaunchKernelGGL((hdet_codes_rows_kernel<OUT, 2>), grid, dim3(256), 0, s, g);
+    else hipLaunchKernelGGL((hdet_codes_rows_kernel<OUT, 4>), grid, dim3(256), 0, s, g);
+    return hipGetLastError();
+  }
+  const dim3 grid((g.n + 127) / 128, (g.m + 127) / 128, n_replicas);
+  if (v4) hipLaunchKernelGGL((hdet_codes_gemm_kernel<OUT, true, 128, 128, 2, 2, 2>), grid, dim3(256), 0, s, g);
+  else hipLaunchKernelGGL((hdet_codes_gemm_kernel<OUT, false, 128, 128, 2, 2, 2>), grid, dim3(256), 0, s, g);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+hipError_t hdet_launch_codes_gemm(const hdet_linear_args& a, hipStream_t s) {
+  if (a.rows == 0) return hipSuccess;
+  const codes_args g = {(const int8_t*)a.codes.dev, (const int8_t*)a.w_codes.dev, a.scale_dev, a.w_scale_dev, a.bias_dev, a.y.dev,
+                        a.codes.replica_stride, a.w_codes.replica_stride, a.bias_stride, a.y.replica_stride,
+                        a.codes.row_stride, a.w_codes.row_stride, a.y.row_stride, (int)a.rows, a.d_out, (a.d_in + 15) & ~15};
+  return a.y_dtype == HDET_TYPE_BF16 ? launch_typed<uint16_t>(g, a.n_replicas, s) : launch_typed<float>(g, a.n_replicas, s);
+}

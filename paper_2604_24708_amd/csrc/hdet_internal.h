@@ -168,7 +168,9 @@ enum { HDET_EPI_F32 = 0, HDET_EPI_BIAS_F32 = 1, HDET_EPI_BIAS_RELU_BF16 = 2, HDE
        HDET_EPI_ADAMW = 10,           // weight gradient that is applied at once: the AdamW update of `upd` on the tile (c is not written)
        // output layer whose logits z = acc + bias stay on the chip (hdet_launch_head_loss only):
        HDET_EPI_XENT_STAT = 11,       // reference and sum of a tile's rows (hdet_xent_epi; c is not written)
-       HDET_EPI_XENT_GRAD = 12 };     // c = bf16 gradient of the mean cross-entropy at z, from the whole rows' reference and sum; row losses, column sums
+       HDET_EPI_XENT_GRAD = 12,
+       // a product in pieces of its contraction, input-gradient order: the sum so far is in fp32 at `accum`, the last piece's is rounded to c
+       HDET_EPI_ACCUM_BF16 = 13 };     // c = bf16 gradient of the mean cross-entropy at z, from the whole rows' reference and sum; row losses, column sums
 
 // Cross-entropy inside the output layer's product: what its two passes and the merge between them exchange.  Row scalars are [replica][row].
 struct hdet_xent_epi {
@@ -203,6 +205,8 @@ struct hdet_bgemm_args {
   // rounded (where logits go through memory, xent_row_kernel adds what it stores)
   float* colsum;
   hdet_xent_epi xent;      // HDET_EPI_XENT_*
+  float* accum; int64_t accum_ld, accum_bs;   // HDET_EPI_ACCUM_BF16: accum[z0*accum_bs + m*accum_ld + n]; the first piece does not read it,
+  bool accum_first, accum_last;               // the last writes c instead
   float* rowsum; int64_t rowsum_bs;     // general kernels, weight gradients: rowsum[z0*rowsum_bs + m] = sum_k A(m,k), or null
   int tile_group;          // LDS-direct kernel: consecutive blocks walk groups of this many tile rows column by column (0, 1: row by row)
   // HDET_EPI_ADAMW (n1 = n2 = 1, batch item = replica): the product is the replica's gradient of a weight matrix;

@@ -1,0 +1,24 @@
+// Launchers of the language-model operators (hdet_ops.hip checks arguments and calls them).
+#pragma once
+
+#include "hdet_internal.h"
+
+// hdet_norm.hip
+hipError_t hdet_launch_norm(const hdet_norm_args& a, hipStream_t s);
+hipError_t hdet_launch_norm_backward(const hdet_norm_grad_args& a, hipStream_t s);
+size_t hdet_norm_backward_bytes(int n_replicas, int64_t rows, int width);
+hipError_t hdet_launch_quantise(const hdet_codes_args& a, hipStream_t s);
+hipError_t hdet_launch_restore(const hdet_codes_args& a, hipStream_t s);
+// Sums over the rows of a bfloat16 matrix, [width] per replica, in a fixed order; scratch: hdet_row_sum_bytes bytes.
+size_t hdet_row_sum_bytes(int n_replicas, int64_t rows, int width);
+hipError_t hdet_launch_row_sum(const hdet_rows& x, int n_replicas, int64_t rows, int width, float* out, int64_t out_stride, void* scratch, hipStream_t s);
+// The second half of such a sum: out[z][j] = sum_p partial[z][p][j]
+hipError_t hdet_launch_partial_sum(const float* partial, int n_replicas, int parts, int width, int64_t pitch, float* out, int64_t out_stride, hipStream_t s);
+
+// hdet_gemm_codes.hip
+hipError_t hdet_launch_codes_gemm(const hdet_linear_args& a, hipStream_t s);
+
+// hdet_vocab.hip
+hipError_t hdet_launch_zero_rows(const hdet_rows& m, int n_replicas, int64_t rows, int width, int dtype, hipStream_t s);
+size_t hdet_vocab_bytes(int n_replicas, int64_t rows, int width, int classes, int dw_dtype, int piece);
+hipError_t hdet_launch_vocab_loss(const hdet_vocab_args& a, hipStream_t s);

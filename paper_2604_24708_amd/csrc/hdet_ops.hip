@@ -1,0 +1,284 @@
+// C entry points of the language-model operators: argument checks, and the order of the launches.
+
+#include "hdet_ops.h"
+
+#include <limits.h>
+
+namespace {
+
+// rows a replica: what the launches' grids and 32-bit row numbers hold
+constexpr int64_t kMaxRows = (int64_t)1 << 21;
+
+struct checker {
+  std::string why;
+  bool ok() const { return why.empty(); }
+  void need(bool cond, const char* msg) { if (why.empty() && !cond) why = msg; }
+  void common(int n, int64_t rows) {
+    need(n >= 1 && n <= HDET_MAX_REPLICAS, "n_replicas out of range");
+    need(rows >= 0 && rows <= kMaxRows, "rows must be in 0 .. 2^21 per replica");
+  }
+  void type(int dtype, const char* msg) { need(dtype == HDET_TYPE_F32 || dtype == HDET_TYPE_BF16, msg); }
+  // a matrix of rows x width elements of `size` bytes; `out`: no two elements share memory
+  void matrix(const char* name, const hdet_rows& m, int n, int64_t rows, int64_t width, int size, bool required, bool out) {
+    if (!ok()) return;
+    const std::string s(name);
+    if (!m.dev) {
+      if (required && rows > 0) why = s + " is required";
+      return;
+    }
+    if (reinterpret_cast<uintptr_t>(m.dev) % size) why = s + " is not aligned to its elements";
+    else if (m.row_stride < 0 || m.replica_stride < 0 || m.row_stride > (int64_t)1 << 32 || m.replica_stride > (int64_t)1 << 44) why = s + ": strides out of range";
+    else if (rows > 1 && m.row_stride < width) why = s + ": row_stride is less than a row";
+    else if (out && n > 1 && m.replica_stride < (rows - 1) * m.row_stride + width) {
+      // replicas may also lie between each other's rows
+      if (rows > 1 && !(m.replica_stride >= width && m.row_stride >= (n - 1) * m.replica_stride + width)) why = s + ": replicas overlap";
+      else if (rows <= 1 && m.replica_stride < width) why = s + ": replicas overlap";
+    }
+  }
+  void codes(const char* name, const hdet_rows& m, int n, int64_t rows, int64_t width, bool required, bool out) {
+    matrix(name, m, n, rows, (width + 15) / 16 * 16, 1, required, out);
+    if (!ok() || !m.dev) return;
+    const std::string s(name);
+    if (reinterpret_cast<uintptr_t>(m.dev) & 15 || (m.row_stride | m.replica_stride) & 15) why = s + ": rows must start 16-byte aligned (strides multiples of 16)";
+    else if (m.row_stride >= (int64_t)1 << 22) why = s + ": row_stride must be less than 2^22";
+  }
+  // [count] fp32 a replica, `stride` apart
+  void vector(const char* name, const void* p, int n, int64_t count, int64_t stride, bool required, bool out) {
+    if (!ok()) return;
+    const std::string s(name);
+    if (!p) {
+      if (required && count > 0) why = s + " is required";
+    } else if (reinterpret_cast<uintptr_t>(p) & 3) why = s + " is not aligned to its elements";
+    else if (stride < 0 || (out && n > 1 && stride < count)) why = s + ": stride is less than a vector";
+  }
+  void workspace(const void* p, size_t have, size_t want) {
+    if (!ok() || !want) return;
+    if (!p || have < want) why = "workspace is too small: " + std::to_string(want) + " bytes are needed";
+    else if (reinterpret_cast<uintptr_t>(p) & 15) why = "workspace must be 16-byte aligned";
+  }
+};
+
+// Runs one entry: f(checker) checks, g() launches.  Nothing thrown leaves it.
+template <typename F, typename G>
+int entry(const char* name, F check, G launch) {
+  try {
+    checker c;
+    check(c);
+    if (!c.ok()) {
+      hdet_set_global_error(std::string(name) + ": " + c.why);
+      return HDET_EINVAL;
+    }
+    const hipError_t e = launch();
+    if (e == hipSuccess) return HDET_OK;
+    hdet_set_global_error(std::string(name) + ": " + hipGetErrorString(e));
+    return HDET_EHIP;
+  } catch (...) {
+    return HDET_EINVAL;        // out of host memory while a message was made
+  }
+}
+
+int element(int dtype) { return dtype == HDET_TYPE_BF16 ? 2 : 4; }
+
+size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+// workspace of the linear layer's gradients: X and W in bfloat16 (rows of whole 16-byte pieces), partial sums of dy
+struct linear_layout { int64_t pitch; size_t x, w, sum, total; };
+linear_layout linear_layout_of(int n, int64_t rows, int d_in, int d_out) {
+  linear_layout l;
+  l.pitch = (d_in + 7) & ~7;
+  l.x = 0;
+  l.w = l.x + up256((size_t)n * rows * l.pitch * 2);
+  l.sum = l.w + up256((size_t)n * d_out * l.pitch * 2);
+  l.total = l.sum + up256(hdet_row_sum_bytes(n, rows, d_out));
+  return l;
+}
+void linear_sizes(checker& c, int n, int64_t rows, int d_in, int d_out) {
+  c.common(n, rows);
+  c.need(d_in >= 1 && d_in <= HDET_MAX_CODES_WIDTH, "d_in must be in 1 .. HDET_MAX_CODES_WIDTH");
+  c.need(d_out >= 1 && d_out <= kMaxRows, "d_out must be in 1 .. 2^21");
+}
+void vocab_sizes(checker& c, int n, int64_t rows, int width, int classes, int dw_dtype, int piece) {
+  c.common(n, rows);
+  c.need(width >= 1 && width <= HDET_MAX_CODES_WIDTH, "width must be in 1 .. HDET_MAX_CODES_WIDTH");
+  c.need(classes >= 1 && classes <= kMaxRows, "classes must be in 1 .. 2^21");
+  c.type(dw_dtype, "dw_dtype must be HDET_TYPE_F32 or HDET_TYPE_BF16");
+  c.need(piece >= 0, "piece must be 0 or a number of classes");
+}
+
+}  // namespace
+
+extern "C" int hdet_rmsnorm(const hdet_norm_args* a, void* stream) {
+  return entry("hdet_rmsnorm", [&](checker& c) {
+    c.need(a != nullptr, "args is null");
+    if (!c.ok()) return;
+    const int n = a->n_replicas;
+    c.common(n, a->rows);
+    c.need(a->width >= 1 && a->width <= HDET_MAX_NORM_WIDTH, "width must be in 1 .. HDET_MAX_NORM_WIDTH");
+    c.type(a->dtype, "dtype must be HDET_TYPE_F32 or HDET_TYPE_BF16");
+    c.need(a->eps >= 0.0 && a->eps < 1e30, "eps must be a number from 0 on");
+    if (!c.ok()) return;
+    const int size = element(a->dtype);
+    c.matrix("x", a->x, n, a->rows, a->width, size, true, false);
+    c.matrix("resid", a->resid, n, a->rows, a->width, size, false, false);
+    c.matrix("total", a->total, n, a->rows, a->width, size, false, true);
+    c.matrix("y", a->y, n, a->rows, a->width, size, false, true);
+    c.codes("codes", a->codes, n, a->rows, a->width, false, true);
+    c.vector("scale_dev", a->scale_dev, n, a->rows, a->rows, a->codes.dev != nullptr, true);
+    c.vector("rstd_dev", a->rstd_dev, n, a->rows, a->rows, false, true);
+    c.vector("gain_dev", a->gain_dev, n, a->width, a->gain_stride, true, false);
+  }, [&] { return hdet_launch_norm(*a, (hipStream_t)stream); });
+}
+
+extern "C" int hdet_rmsnorm_backward_workspace(int32_t n_replicas, int64_t rows, int32_t width, size_t* bytes) {
+  return entry("hdet_rmsnorm_backward_workspace", [&](checker& c) {
+    c.common(n_replicas, rows);
+    c.need(width >= 1 && width <= HDET_MAX_NORM_WIDTH, "width must be in 1 .. HDET_MAX_NORM_WIDTH");
+    c.need(bytes != nullptr, "bytes is null");
+  }, [&] { *bytes = hdet_norm_backward_bytes(n_replicas, rows, width); return hipSuccess; });
+}
+
+extern "C" int hdet_rmsnorm_backward(const hdet_norm_grad_args* a, void* stream) {
+  return entry("hdet_rmsnorm_backward", [&](checker& c) {
+    c.need(a != nullptr, "args is null");
+    if (!c.ok()) return;
+    const int n = a->n_replicas;
+    c.common(n, a->rows);
+    c.need(a->width >= 1 && a->width <= HDET_MAX_NORM_WIDTH, "width must be in 1 .. HDET_MAX_NORM_WIDTH");
+    c.type(a->dtype, "dtype must be HDET_TYPE_F32 or HDET_TYPE_BF16");
+    if (!c.ok()) return;
+    const int size = element(a->dtype);
+    c.matrix("total", a->total, n, a->rows, a->width, size, true, false);
+    c.matrix("dy", a->dy, n, a->rows, a->width, size, true, false);
+    c.matrix("dtotal", a->dtotal, n, a->rows, a->width, size, false, false);
+    c.matrix("dx", a->dx, n, a->rows, a->width, size, true, true);
+    c.vector("rstd_dev", a->rstd_dev, n, a->rows, a->rows, true, false);
+    c.vector("gain_dev", a->gain_dev, n, a->width, a->gain_stride, true, false);
+    c.vector("dgain_dev", a->dgain_dev, n, a->width, a->dgain_stride, false, true);
+    if (c.ok() && a->dgain_dev) c.workspace(a->workspace_dev, a->workspace_bytes, hdet_norm_backward_bytes(n, a->rows, a->width));
+  }, [&] { return hdet_launch_norm_backward(*a, (hipStream_t)stream); });
+}
+
+static int codes_entry(const char* name, const hdet_codes_args* a, void* stream, bool restore) {
+  return entry(name, [&](checker& c) {
+    c.need(a != nullptr, "args is null");
+    if (!c.ok()) return;
+    const int n = a->n_replicas;
+    c.common(n, a->rows);
+    const int most = restore ? HDET_MAX_CODES_WIDTH : HDET_MAX_NORM_WIDTH;
+    c.need(a->width >= 1 && a->width <= most, restore ? "width must be in 1 .. HDET_MAX_CODES_WIDTH" : "width must be in 1 .. HDET_MAX_NORM_WIDTH");
+    c.type(a->dtype, "dtype must be HDET_TYPE_F32 or HDET_TYPE_BF16");
+    if (!c.ok()) return;
+    c.matrix("values", a->values, n, a->rows, a->width, element(a->dtype), true, restore);
+    c.codes("codes", a->codes, n, a->rows, a->width, true, !restore);
+    c.vector("scale_dev", a->scale_dev, n, a->rows, a->rows, true, !restore);
+  }, [&] { return restore ? hdet_launch_restore(*a, (hipStream_t)stream) : hdet_launch_quantise(*a, (hipStream_t)stream); });
+}
+extern "C" int hdet_quantise_rows(const hdet_codes_args* a, void* stream) { return codes_entry("hdet_quantise_rows", a, stream, false); }
+extern "C" int hdet_restore_rows(const hdet_codes_args* a, void* stream) { return codes_entry("hdet_restore_rows", a, stream, true); }
+
+extern "C" int hdet_quantised_linear(const hdet_linear_args* a, void* stream) {
+  return entry("hdet_quantised_linear", [&](checker& c) {
+    c.need(a != nullptr, "args is null");
+    if (!c.ok()) return;
+    const int n = a->n_replicas;
+    linear_sizes(c, n, a->rows, a->d_in, a->d_out);
+    c.type(a->y_dtype, "y_dtype must be HDET_TYPE_F32 or HDET_TYPE_BF16");
+    if (!c.ok()) return;
+    c.codes("codes", a->codes, n, a->rows, a->d_in, true, false);
+    c.codes("w_codes", a->w_codes, n, a->d_out, a->d_in, true, false);
+    c.vector("scale_dev", a->scale_dev, n, a->rows, a->rows, true, false);
+    c.vector("w_scale_dev", a->w_scale_dev, n, a->d_out, a->d_out, true, false);
+    c.vector("bias_dev", a->bias_dev, n, a->d_out, a->bias_stride, false, false);
+    c.matrix("y", a->y, n, a->rows, a->d_out, element(a->y_dtype), true, true);
+  }, [&] { return hdet_launch_codes_gemm(*a, (hipStream_t)stream); });
+}
+
+extern "C" int hdet_quantised_linear_backward_workspace(int32_t n_replicas, int64_t rows, int32_t d_in, int32_t d_out, size_t* bytes) {
+  return entry("hdet_quantised_linear_backward_workspace", [&](checker& c) {
+    linear_sizes(c, n_replicas, rows, d_in, d_out);
+    c.need(bytes != nullptr, "bytes is null");
+  }, [&] { *bytes = linear_layout_of(n_replicas, rows, d_in, d_out).total; return hipSuccess; });
+}
+
+extern "C" int hdet_quantised_linear_backward(const hdet_linear_grad_args* a, void* stream) {
+  return entry("hdet_quantised_linear_backward", [&](checker& c) {
+    c.need(a != nullptr, "args is null");
+    if (!c.ok()) return;
+    const int n = a->n_replicas;
+    linear_sizes(c, n, a->rows, a->d_in, a->d_out);
+    if (!c.ok()) return;
+    c.matrix("dy", a->dy, n, a->rows, a->d_out, 2, true, false);
+    c.codes("codes", a->codes, n, a->rows, a->d_in, a->dw.dev != nullptr, false);
+    c.codes("w_codes", a->w_codes, n, a->d_out, a->d_in, a->dx.dev != nullptr, false);
+    c.vector("scale_dev", a->scale_dev, n, a->rows, a->rows, a->dw.dev != nullptr, false);
+    c.vector("w_scale_dev", a->w_scale_dev, n, a->d_out, a->d_out, a->dx.dev != nullptr, false);
+    c.matrix("dx", a->dx, n, a->rows, a->d_in, 2, false, true);
+    c.matrix("dw", a->dw, n, a->d_out, a->d_in, 4, false, true);
+    c.vector("db_dev", a->db_dev, n, a->d_out, a->db_stride, false, true);
+    if (c.ok()) c.workspace(a->workspace_dev, a->workspace_bytes, linear_layout_of(n, a->rows, a->d_in, a->d_out).total);
+  }, [&]() -> hipError_t {
+    const hipStream_t s = (hipStream_t)stream;
+    const int n = a->n_replicas;
+    const int64_t M = a->rows;
+    const linear_layout l = linear_layout_of(n, M, a->d_in, a->d_out);
+    char* const ws = (char*)a->workspace_dev;
+    hipError_t e;
+    if (M == 0) {
+      if (a->dw.dev && (e = hdet_launch_zero_rows(a->dw, n, a->d_out, a->d_in, HDET_TYPE_F32, s)) != hipSuccess) return e;
+      return a->db_dev ? hdet_launch_row_sum(a->dy, n, 0, a->d_out, a->db_dev, a->db_stride, nullptr, s) : hipSuccess;
+    }
+    auto restored = [&](const hdet_rows& codes, const float* scale, int64_t rows, size_t at) {
+      hdet_codes_args r = {};
+      r.n_replicas = n; r.dtype = HDET_TYPE_BF16; r.rows = rows; r.width = a->d_in;
+      r.values = {ws + at, l.pitch, rows * l.pitch};
+      r.codes = codes; r.scale_dev = const_cast<float*>(scale);
+      return hdet_launch_restore(r, s);
+    };
+    if (a->db_dev && (e = hdet_launch_row_sum(a->dy, n, M, a->d_out, a->db_dev, a->db_stride, ws + l.sum, s)) != hipSuccess) return e;
+    if (a->dx.dev) {
+      if ((e = restored(a->w_codes, a->w_scale_dev, a->d_out, l.w)) != hipSuccess) return e;
+      hdet_bgemm_args g = {};
+      g.a = (const uint16_t*)a->dy.dev; g.lda = a->dy.row_stride; g.a_s[0] = a->dy.replica_stride;
+      g.b = (const uint16_t*)(ws + l.w); g.ldb = l.pitch; g.b_s[0] = a->d_out * l.pitch;
+      g.c = a->dx.dev; g.ldc = a->dx.row_stride; g.c_s[0] = a->dx.replica_stride;
+      g.m = (int)M; g.n = a->d_in; g.k = a->d_out;
+      if ((e = hdet_launch_bgemm(g, true, false, HDET_EPI_BF16, n, s)) != hipSuccess) return e;
+    }
+    if (a->dw.dev) {
+      if ((e = restored(a->codes, a->scale_dev, M, l.x)) != hipSuccess) return e;
+      hdet_bgemm_args g = {};
+      g.a = (const uint16_t*)a->dy.dev; g.lda = a->dy.row_stride; g.a_s[0] = a->dy.replica_stride;
+      g.b = (const uint16_t*)(ws + l.x); g.ldb = l.pitch; g.b_s[0] = M * l.pitch;
+      g.c = a->dw.dev; g.ldc = a->dw.row_stride; g.c_s[0] = a->dw.replica_stride;
+      g.m = a->d_out; g.n = a->d_in; g.k = (int)M;
+      if ((e = hdet_launch_bgemm(g, false, false, HDET_EPI_F32, n, s)) != hipSuccess) return e;
+    }
+    return hipSuccess;
+  });
+}
+
+extern "C" int hdet_vocab_loss_workspace(int32_t n_replicas, int64_t rows, int32_t width, int32_t classes, int32_t dw_dtype, int32_t piece, size_t* bytes) {
+  return entry("hdet_vocab_loss_workspace", [&](checker& c) {
+    vocab_sizes(c, n_replicas, rows, width, classes, dw_dtype, piece);
+    c.need(bytes != nullptr, "bytes is null");
+  }, [&] { *bytes = hdet_vocab_bytes(n_replicas, rows, width, classes, dw_dtype, piece); return hipSuccess; });
+}
+
+extern "C" int hdet_vocab_loss(const hdet_vocab_args* a, void* stream) {
+  return entry("hdet_vocab_loss", [&](checker& c) {
+    c.need(a != nullptr, "args is null");
+    if (!c.ok()) return;
+    const int n = a->n_replicas;
+    vocab_sizes(c, n, a->rows, a->width, a->classes, a->dw_dtype, a->piece);
+    if (!c.ok()) return;
+    c.matrix("h", a->h, n, a->rows, a->width, 2, true, false);
+    c.matrix("w", a->w, n, a->classes, a->width, 2, true, false);
+    c.vector("bias_dev", a->bias_dev, n, a->classes, a->bias_stride, false, false);
+    c.vector("labels_dev", a->labels_dev, n, a->rows, a->rows, true, false);
+    c.vector("row_loss_dev", a->row_loss_dev, n, a->rows, a->rows, true, true);
+    c.vector("mean_loss_dev", a->mean_loss_dev, n, 1, 1, true, true);
+    c.matrix("dh", a->dh, n, a->rows, a->width, 2, false, true);
+    c.matrix("dw", a->dw, n, a->classes, a->width, element(a->dw_dtype), false, true);
+    c.vector("db_dev", a->db_dev, n, a->classes, a->db_stride, false, true);
+    if (c.ok()) c.workspace(a->workspace_dev, a->workspace_bytes, hdet_vocab_bytes(n, a->rows, a->width, a->classes, a->dw.dev ? a->dw_dtype : HDET_TYPE_BF16, a->piece));
+  }, [&] { return hdet_launch_vocab_loss(*a, (hipStream_t)stream); });
+}

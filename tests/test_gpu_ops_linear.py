@@ -1,0 +1,173 @@
+"""The linear layer on 8-bit matrices and its gradients against 64 bits."""
+import pytest
+import torch
+
+import ops_reference as R
+import paper_2604_24708_amd as H
+
+pytestmark = pytest.mark.gpu
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def codes_of(v):
+    """8-bit copy of v [N, rows, cols] (made here, not by the library), in rows padded with zeros."""
+    q, s = R.rows8(v.double())
+    c = H.hdet_codes_empty(*v.shape)
+    c.copy_(q.to(torch.int8))
+    return c, s[..., 0].float().contiguous()
+
+
+def make(n, rows, d_in, d_out, seed):
+    g = torch.Generator(device=R.DEV).manual_seed(seed)
+    rnd = lambda *s: torch.randn(*s, generator=g, device=R.DEV)  # noqa: E731
+    x, xs = codes_of(rnd(n, rows, d_in) * torch.exp(rnd(n, rows, 1)))
+    w, ws = codes_of(rnd(n, d_out, d_in) * d_in ** -0.5)
+    return x, xs, w, ws, rnd(n, d_out), rnd(n, rows, d_out).to(BF)
+
+
+def values(c, s):
+    return c.double() * s.double()[..., None]
+
+
+def check_y(y, x, xs, w, ws, bias):
+    plain = torch.matmul(values(x, xs), values(w, ws).transpose(1, 2).contiguous())
+    want = plain + (0 if bias is None else bias.double()[:, None])
+    # the sum is exact; its conversion, the product of the scales and the fused addition round once each
+    bound = 3 * R.U * (plain.abs() + want.abs()) + R.half_ulp(y.dtype) * want.abs()
+    assert torch.all((y.double() - want).abs() <= bound + 1e-38)
+
+
+SHAPES = [(1, 1, 1, 1), (2, 1, 16, 5), (3, 2, 17, 33), (1, 5, 200, 64), (8, 1, 512, 300), (2, 16, 1000, 48), (2, 17, 128, 100), (1, 33, 640, 130), (2, 64, 257, 127),
+          (2, 65, 96, 65), (1, 128, 128, 128), (3, 129, 300, 131), (1, 200, 2050, 72), (2, 300, 64, 520), (2, 257, 384, 1024), (1, 1000, 144, 1003), (2, 513, 1024, 768),
+          (1, 700, 130, 2304), (4, 1024, 512, 1024), (1, 3, 9000, 40), (1, 2100, 776, 1500), (2, 4096, 256, 640)]
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("n,rows,d_in,d_out", SHAPES)
+def test_forward(n, rows, d_in, d_out, dtype):
+    x, xs, w, ws, bias, _ = make(n, rows, d_in, d_out, d_in + rows)
+    y = torch.full((n, rows, d_out), float("nan"), dtype=dtype, device=R.DEV)
+    H.hdet_quantised_linear(x, xs, w, ws, y, bias=bias)
+    check_y(y, x, xs, w, ws, bias)
+    H.hdet_quantised_linear(x, xs, w, ws, y)
+    check_y(y, x, xs, w, ws, None)
+
+
+@pytest.mark.parametrize("rows", [1, 20, 300])
+def test_largest_codes_and_other_scales(rows):
+    """Sums of products of +-127 over the longest row, -128 as a code, and scales that are no powers of two."""
+    d_in, d_out = H.HDET_MAX_CODES_WIDTH if rows == 1 else 30000, 33
+    x, w = H.hdet_codes_empty(1, rows, d_in), H.hdet_codes_empty(1, d_out, d_in)
+    x.fill_(-127)
+    w.fill_(127)
+    w[0, 1] = -128
+    x[0, 0] = -128
+    xs = torch.rand(1, rows, device=R.DEV) + 0.1
+    ws = torch.rand(1, d_out, device=R.DEV) + 0.1
+    y = torch.empty(1, rows, d_out, device=R.DEV)
+    H.hdet_quantised_linear(x, xs, w, ws, y)
+    check_y(y, x, xs, w, ws, None)
+
+
+@pytest.mark.parametrize("dtype", [BF, F32])
+@pytest.mark.parametrize("rows", [3, 40, 150])
+def test_strides(rows, dtype):
+    n, d_in, d_out = 3, 100, 70
+    x, xs, w, ws, bias, _ = make(n, rows, d_in, d_out, 4)
+    wide = torch.zeros(n, rows, 160, dtype=torch.int8, device=R.DEV)
+    wide[..., :d_in] = x
+    wide[..., 112:] = 55                                  # behind the padding: belongs to somebody else
+    wide_w = torch.zeros(d_out, n, 112, dtype=torch.int8, device=R.DEV)     # replicas between each other's rows
+    wide_w[..., :d_in] = w.transpose(0, 1)
+    for row_pad, rep_pad, offset in [(0, 0, 0), (2, 4, 4), (3, 1, 1), (1, 0, 0)]:
+        y = R.strided(torch.zeros(n, rows, d_out, dtype=dtype, device=R.DEV), row_pad, rep_pad, offset)
+        H.hdet_quantised_linear(wide[..., :d_in], xs, wide_w.transpose(0, 1)[..., :d_in], ws, y, bias=bias[:1].expand(n, d_out))
+        check_y(y, x, xs, w, ws, bias[:1].expand(n, d_out))
+        gaps = torch.as_strided(y, (n, rows, d_out + row_pad), y.stride(), y.storage_offset())[:, : rows - 1, d_out:]
+        assert torch.all(torch.isnan(gaps))
+    # one set of codes for all replicas
+    y = torch.empty(n, rows, d_out, dtype=dtype, device=R.DEV)
+    H.hdet_quantised_linear(wide[:1, :, :d_in].expand(n, rows, d_in), xs, w, ws, y, bias=bias)
+    check_y(y, x[:1].expand(n, rows, d_in), xs, w, ws, bias)
+
+
+@pytest.mark.parametrize("n,rows,d_in,d_out", [(1, 1, 1, 1), (2, 1, 40, 7), (3, 2, 17, 33), (2, 17, 128, 100), (1, 128, 128, 128), (3, 129, 300, 131), (2, 300, 64, 520),
+                                               (2, 257, 384, 1024), (1, 1000, 144, 1003), (2, 513, 1024, 768), (8, 256, 512, 512), (2, 4096, 256, 640)])
+def test_backward(n, rows, d_in, d_out):
+    x, xs, w, ws, _, dy = make(n, rows, d_in, d_out, rows)
+    dx = torch.full((n, rows, d_in), float("nan"), dtype=BF, device=R.DEV)
+    dw, db = torch.full((n, d_out, d_in), float("nan"), device=R.DEV), torch.full((n, d_out), float("nan"), device=R.DEV)
+    work = torch.empty(H.hdet_quantised_linear_backward_workspace(n, rows, d_in, d_out), dtype=torch.uint8, device=R.DEV)
+    H.hdet_quantised_linear_backward(dy, x, xs, w, ws, dx=dx, dw=dw, db=db, workspace=work)
+    vx, vw, d = values(x, xs), values(w, ws), dy.double()
+    want_x, want_w = torch.matmul(d, vw), torch.matmul(d.transpose(1, 2).contiguous(), vx)
+    # products are exact in fp32, sums of at most K of them in any order
+    size_x, size_w = torch.matmul(d.abs(), vw.abs()), torch.matmul(d.abs().transpose(1, 2).contiguous(), vx.abs())
+    assert torch.all((dx.double() - want_x).abs() <= R.half_ulp(BF) * want_x.abs() + (d_out + 2) * R.U * size_x)
+    assert torch.all((dw.double() - want_w).abs() <= (rows + 2) * R.U * size_w)
+    assert R.rel(dw, want_w) <= 8 * R.U * max(1.0, rows ** 0.5)
+    assert torch.all((db.double() - d.sum(1)).abs() <= (rows + 2) * R.U * d.abs().sum(1))
+    one = torch.empty_like(dw)
+    H.hdet_quantised_linear_backward(dy, x, xs, w, ws, dw=one, workspace=work)
+    assert torch.equal(one, dw)                            # each by itself, and the same bits again
+    other, db2 = torch.empty_like(dx), torch.empty_like(db)
+    H.hdet_quantised_linear_backward(dy, x, xs, w, ws, dx=other, db=db2, workspace=work)
+    assert torch.equal(other, dx) and torch.equal(db2, db)
+
+
+def test_backward_strides_and_no_rows():
+    n, rows, d_in, d_out = 2, 70, 72, 40
+    x, xs, w, ws, _, dy = make(n, rows, d_in, d_out, 8)
+    plane = torch.full((n, d_out * d_in + 60), float("nan"), device=R.DEV)       # gradients inside a parameter plane
+    dw = torch.as_strided(plane, (n, d_out, d_in), (plane.stride(0), d_in, 1), 20)
+    dyp, dxp = R.strided(dy, 3, 5, 1), R.strided(torch.zeros(n, rows, d_in, dtype=BF, device=R.DEV), 8, 0, 0)
+    work = torch.empty(H.hdet_quantised_linear_backward_workspace(n, rows, d_in, d_out), dtype=torch.uint8, device=R.DEV)
+    H.hdet_quantised_linear_backward(dyp, x, xs, w, ws, dx=dxp, dw=dw, workspace=work)
+    want_w = torch.matmul(dy.double().transpose(1, 2).contiguous(), values(x, xs))
+    want_x = torch.matmul(dy.double(), values(w, ws))
+    assert R.rel(dw, want_w) <= 8 * R.U * rows ** 0.5
+    assert R.rel(dxp, want_x) <= R.half_ulp(BF)
+    assert torch.all(torch.isnan(plane[:, :20])) and torch.all(torch.isnan(plane[:, 20 + d_in * d_out:]))
+    none = torch.empty(n, 0, d_out, dtype=BF, device=R.DEV)
+    db = torch.ones(n, d_out, device=R.DEV)
+    dw0 = torch.ones(n, d_out, d_in, device=R.DEV)
+    H.hdet_quantised_linear_backward(none, x[:, :0], xs[:, :0].contiguous(), w, ws, dw=dw0, db=db, workspace=work)
+    assert torch.all(db == 0) and torch.all(dw0 == 0)
+    H.hdet_quantised_linear(x[:, :0], xs[:, :0].contiguous(), w, ws, torch.empty(n, 0, d_out, device=R.DEV))
+
+
+def test_not_finite_rows_stay_in_their_row():
+    x, xs, w, ws, bias, _ = make(1, 100, 64, 48, 3)
+    xs[0, 7] = float("nan")
+    y = torch.empty(1, 100, 48, device=R.DEV)
+    H.hdet_quantised_linear(x, xs, w, ws, y, bias=bias)
+    bad = torch.isnan(y[0]).any(-1)
+    assert bool(torch.isnan(y[0, 7]).all()) and int(bad.sum()) == 1
+
+
+def test_gradient_against_differences():
+    """y is linear in x and in w: the differences of L = sum(dy y) are exact but for the fp32 roundings of y."""
+    n, rows, d_in, d_out = 1, 60, 48, 40
+    x, xs, w, ws, bias, dy = make(n, rows, d_in, d_out, 21)
+    dx = torch.empty(n, rows, d_in, dtype=BF, device=R.DEV)
+    dw = torch.empty(n, d_out, d_in, device=R.DEV)
+    work = torch.empty(H.hdet_quantised_linear_backward_workspace(n, rows, d_in, d_out), dtype=torch.uint8, device=R.DEV)
+    H.hdet_quantised_linear_backward(dy, x, xs, w, ws, dx=dx, dw=dw, workspace=work)
+
+    def value(x, w):
+        y = torch.empty(n, rows, d_out, device=R.DEV)
+        H.hdet_quantised_linear(x, xs, w, ws, y, bias=bias)
+        return float((dy.double() * y.double()).sum()), float((dy.double() * y.double()).abs().sum())
+
+    base, size = value(x, w)
+    g = torch.Generator(device=R.DEV).manual_seed(2)
+    for which in ("x", "w"):
+        c, s, grad = (x, xs, dx) if which == "x" else (w, ws, dw)
+        d = torch.randint(-3, 4, c.shape, generator=g, device=R.DEV, dtype=torch.int8)
+        moved = H.hdet_codes_empty(*c.shape)
+        moved.copy_((c.to(torch.int32) + d).clamp(-127, 127).to(torch.int8))
+        step = (moved.double() - c.double()) * s.double()[..., None]
+        got = (value(moved, w) if which == "x" else value(x, moved))[0] - base
+        want = float((grad.double() * step).sum())
+        half = R.half_ulp(grad.dtype) + 8 * R.U * max(rows, d_out)
+        assert abs(got - want) <= 8 * R.U * size + half * float((grad.double() * step).abs().sum())

@@ -255,6 +255,8 @@ __device__ __forceinline__ void store_tile(const hdet_bgemm_args& g, const typen
       }
     }
   };
+  constexpr bool kScaled = EPI == HDET_EPI_SCALED_F32 || EPI == HDET_EPI_SCALED_BF16 || EPI == HDET_EPI_ACCUM_BF16;
+  const float out_scale = kScaled ? g.out_scale[z] : 1.f;
   // column sums of the stored result over the rows this lane stores, for its 4 columns
   constexpr bool kColsum = EPI == HDET_EPI_GELUGRAD_BF16 || EPI == HDET_EPI_MASK_BF16;
   f4 csum = {0.f, 0.f, 0.f, 0.f};
@@ -282,6 +284,7 @@ __device__ __forceinline__ void store_tile(const hdet_bgemm_args& g, const typen
       if (row < g.m && col_ok) {
         const int64_t off = c_base + (int64_t)row * g.ldc + col;
         if (kBias) v += bias;
+        if (EPI == HDET_EPI_SCALED_F32 || EPI == HDET_EPI_SCALED_BF16) v *= out_scale;
         if (EPI == HDET_EPI_BIAS_RELU_BF16) {
 #pragma unroll
           for (int q = 0; q < 4; ++q) v[q] = v[q] > 0.f ? v[q] : 0.f;
@@ -324,7 +327,7 @@ __device__ __forceinline__ void store_tile(const hdet_bgemm_args& g, const typen
             const us4 o = {hdet_um::to_bf16(th[0]), hdet_um::to_bf16(th[1]), hdet_um::to_bf16(th[2]), hdet_um::to_bf16(th[3])};
             __builtin_nontemporal_store(o, reinterpret_cast<us4*>(g.upd.shadow + off));
           }
-        } else if (EPI == HDET_EPI_F32 || EPI == HDET_EPI_BIAS_F32) {
+        } else if (EPI == HDET_EPI_F32 || EPI == HDET_EPI_BIAS_F32 || EPI == HDET_EPI_SCALED_F32) {
           put(reinterpret_cast<f4*>(reinterpret_cast<float*>(g.c) + off), v);
         } else if (EPI == HDET_EPI_BIAS_GELU_BF16) {
           const us4 pre = {f2bf(v[0]), f2bf(v[1]), f2bf(v[2]), f2bf(v[3])};
@@ -338,6 +341,7 @@ __device__ __forceinline__ void store_tile(const hdet_bgemm_args& g, const typen
         } else {
           if (EPI == HDET_EPI_ACCUM_BF16 && !g.accum_first)
             v += *reinterpret_cast<const f4*>(g.accum + (int64_t)z * g.accum_bs + (int64_t)row * g.accum_ld + col);
+          if (EPI == HDET_EPI_ACCUM_BF16) v *= out_scale;
           const us4 o = {f2bf(v[0]), f2bf(v[1]), f2bf(v[2]), f2bf(v[3])};
           put(reinterpret_cast<us4*>(reinterpret_cast<uint16_t*>(g.c) + off), o);
           if (kColsum) {
@@ -405,8 +409,8 @@ void hdet_bgemm_dma_kernel(const hdet_bgemm_args g) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = (wave / WGN) * (32 * WMT), wn = (wave % WGN) * (32 * WNT);
 
-  // byte extent of each operand for this batch item: the bound that turns absent chunks into zeros
-  const uint32_t a_bytes = (uint32_t)(((int64_t)((A_KMAJOR ? g.m : g.k) - 1) * g.lda + (A_KMAJOR ? g.k : g.m)) * 2);
+  // byte extent of each operand for this batch item: the bound that turns absent chunks into zeros (A in whole chunks: hdet_bgemm_args::padded)
+  const uint32_t a_bytes = (uint32_t)(((int64_t)((A_KMAJOR ? g.m : g.k) - 1) * g.lda + (((A_KMAJOR ? g.k : g.m) + 7) & ~7)) * 2);
   const uint32_t b_bytes = (uint32_t)(((int64_t)((B_KMAJOR ? g.n : g.k) - 1) * g.ldb + (B_KMAJOR ? g.k : g.n)) * 2);
   const i4 ra = make_rsrc(A, a_bytes), rb = make_rsrc(B, b_bytes);
   const uint32_t s_addr = lds_addr_of(S);
@@ -553,7 +557,7 @@ __global__ __launch_bounds__(512, 2) void hdet_bgemm_alt_kernel(const hdet_bgemm
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wn = (wave % WGN) * 64, hr = (wave / WGN) * 64;
-  const uint32_t a_bytes = (uint32_t)(((int64_t)((A_KMAJOR ? g.m : g.k) - 1) * g.lda + (A_KMAJOR ? g.k : g.m)) * 2);
+  const uint32_t a_bytes = (uint32_t)(((int64_t)((A_KMAJOR ? g.m : g.k) - 1) * g.lda + (((A_KMAJOR ? g.k : g.m) + 7) & ~7)) * 2);
   const uint32_t b_bytes = (uint32_t)(((int64_t)((B_KMAJOR ? g.n : g.k) - 1) * g.ldb + (B_KMAJOR ? g.k : g.n)) * 2);
   const i4 ra = make_rsrc(A, a_bytes), rb = make_rsrc(B, b_bytes);
   const uint32_t s_addr = lds_addr_of(S);
@@ -664,8 +668,9 @@ __global__ __launch_bounds__(512, 2) void hdet_bgemm_alt_kernel(const hdet_bgemm
 template <int EPI>
 __global__ __launch_bounds__(512, 2) void hdet_bgemm_walk_kernel(const hdet_bgemm_args g, unsigned gx, unsigned gy, unsigned total) {
   constexpr int TM = 256, TN = 256, TK = 64, HALF = 128 * TK;
-  constexpr bool kStat = EPI == HDET_EPI_XENT_STAT, kGrad = EPI == HDET_EPI_XENT_GRAD;
-  constexpr int kStores = kStat ? 0 : 16;
+  constexpr int kParts = EPI == HDET_EPI_XENT_PARTS ? 3 : 1;
+  constexpr bool kStat = EPI == HDET_EPI_XENT_STAT, kGrad = EPI == HDET_EPI_XENT_GRAD || EPI == HDET_EPI_XENT_PARTS;
+  constexpr int kStores = kStat ? 0 : 16 * kParts;
   constexpr int kBiasAt = 8 * HALF * 2, kRowsAt = kBiasAt + 2 * TN * 4;           // bytes: bias [2][TN], then what the epilogue needs
   constexpr int kExtra = 2 * TN * 4 + (kStat ? 4 * TM * 8 : kGrad ? 3 * TM * 4 : 0);
   __shared__ __attribute__((aligned(1024))) uint16_t S[8 * HALF + kExtra / 2];
@@ -682,7 +687,8 @@ __global__ __launch_bounds__(512, 2) void hdet_bgemm_walk_kernel(const hdet_bgem
   const uint32_t s_addr = lds_addr_of(S);
   float* const s_bias = reinterpret_cast<float*>(S) + kBiasAt / 4;
   float* const s_rows = reinterpret_cast<float*>(S) + kRowsAt / 4;
-  const int nk = ((g.k + TK - 1) / TK + 1) & ~1;                 // K steps of a tile, an even number (steps beyond K are zeros)
+  int nk = ((g.k + TK - 1) / TK + 1) & ~1;                       // K steps of a tile, an even number from 4 on (steps beyond K are zeros)
+  nk = nk < 4 ? 4 : nk;
 
   struct tile { int m0, n0, bx, z; i4 ra, rb, rbias; };
   auto tile_at = [&](unsigned t) {
@@ -692,7 +698,7 @@ __global__ __launch_bounds__(512, 2) void hdet_bgemm_walk_kernel(const hdet_bgem
     const bool ok = t < total;
     r.ra = make_rsrc(g.a + id.bz * g.a_s[0] + (int64_t)r.m0 * g.lda, ok ? (uint32_t)(((int64_t)(g.m - r.m0 - 1) * g.lda + g.k) * 2) : 0u);
     r.rb = make_rsrc(g.b + id.bz * g.b_s[0] + (int64_t)r.n0 * g.ldb, ok ? (uint32_t)(((int64_t)(g.n - r.n0 - 1) * g.ldb + g.k) * 2) : 0u);
-    r.rbias = make_rsrc(g.bias + id.bz * g.bias_bs + r.n0, ok ? (uint32_t)(g.n - r.n0) * 4u : 0u);
+    r.rbias = make_rsrc(g.bias + id.bz * g.bias_bs + r.n0, ok ? (uint32_t)((g.n - r.n0 + 7) & ~7) * 4u : 0u);
     return r;
   };
   const int ck = ((tid & 7) ^ ta::swz(tid >> 3)) * 8;            // k of this thread's chunks inside a K step
@@ -828,7 +834,8 @@ __global__ __launch_bounds__(512, 2) void hdet_bgemm_walk_kernel(const hdet_bgem
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
           const int tr = wm + i * 16 + lr;
-          rref[i] = s_rows[tr]; ra[i] = s_rows[TM + tr]; rlab[i] = __float_as_int(s_rows[2 * TM + tr]);
+          rref[i] = s_rows[tr]; ra[i] = s_rows[TM + tr]; rlab[i] = __float_as_int(s_rows[2 * TM + tr]) - g.xent.label0;
+          rlab[i] = (unsigned)rlab[i] < (unsigned)g.n ? rlab[i] : -1;
         }
       }
 #pragma unroll
@@ -838,11 +845,15 @@ __global__ __launch_bounds__(512, 2) void hdet_bgemm_walk_kernel(const hdet_bgem
         f4 v[4];
         if constexpr (kGrad) {
           const float ref = row_ok ? rref[i] : INFINITY, a = ra[i];
-          const int yc = row_ok ? rlab[i] - (t.n0 + wn + cg * 4) : -1;
+          const int yc = row_ok && rlab[i] >= 0 ? rlab[i] - (t.n0 + wn + cg * 4) : -1;
 #pragma unroll
           for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int e = 0; e < 4; ++e) v[j][e] = __builtin_amdgcn_exp2f(__builtin_fmaf(acc[i][j][e], kLog2e, -ref)) * a;
+          if (__builtin_expect(a == 0.f, 0)) {                   // a row that does not count: 0 whatever its logits are
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = f4{0.f, 0.f, 0.f, 0.f};
+          }
           if (__builtin_expect((unsigned)yc < 64u && (yc & 12) == 0, 0)) {      // the row's label is among this lane's columns
             float zy = 0.f;
 #pragma unroll
@@ -860,17 +871,27 @@ __global__ __launch_bounds__(512, 2) void hdet_bgemm_walk_kernel(const hdet_bgem
 #pragma unroll
           for (int j = 0; j < 4; ++j) v[j] = acc[i][j];
         }
-        unsigned d[4][2];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) { d[j][0] = hdet_bf16_pack(v[j][0], v[j][1]); d[j][1] = hdet_bf16_pack(v[j][2], v[j][3]); }
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          swap32(d[0][w], d[2][w]); swap32(d[1][w], d[3][w]);
-          swap16(d[0][w], d[1][w]); swap16(d[2][w], d[3][w]);
-        }
         const uint32_t at = (uint32_t)((tr * (int)g.ldc + col) * 2);
-        __builtin_amdgcn_raw_buffer_store_b128(hdet_u4v{d[0][0], d[0][1], d[1][0], d[1][1]}, rc, row_ok && ok0 ? at : kAbsent, 0, 0);
-        __builtin_amdgcn_raw_buffer_store_b128(hdet_u4v{d[2][0], d[2][1], d[3][0], d[3][1]}, rc, row_ok && ok1 ? at + 16 : kAbsent, 0, 0);
+#pragma unroll
+        for (int part = 0; part < kParts; ++part) {
+          unsigned d[4][2];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) { d[j][0] = hdet_bf16_pack(v[j][0], v[j][1]); d[j][1] = hdet_bf16_pack(v[j][2], v[j][3]); }
+          if (part + 1 < kParts) {                               // what is left for the next part, exactly
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+              v[j] -= f4{__uint_as_float(d[j][0] << 16), __uint_as_float(d[j][0] & 0xffff0000u), __uint_as_float(d[j][1] << 16), __uint_as_float(d[j][1] & 0xffff0000u)};
+          }
+#pragma unroll
+          for (int w = 0; w < 2; ++w) {
+            swap32(d[0][w], d[2][w]); swap32(d[1][w], d[3][w]);
+            swap16(d[0][w], d[1][w]); swap16(d[2][w], d[3][w]);
+          }
+          const auto to = part == 0 ? rc : __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<uint16_t*>(g.c) + t.z * g.c_s[0] + ((int64_t)part * g.m + t.m0) * g.ldc + t.n0, 0,
+                                                                            0x7fffffff, 0x00020000);
+          __builtin_amdgcn_raw_buffer_store_b128(hdet_u4v{d[0][0], d[0][1], d[1][0], d[1][1]}, to, row_ok && ok0 ? at : kAbsent, 0, 0);
+          __builtin_amdgcn_raw_buffer_store_b128(hdet_u4v{d[2][0], d[2][1], d[3][0], d[3][1]}, to, row_ok && ok1 ? at + 16 : kAbsent, 0, 0);
+        }
       }
       if (kGrad && g.colsum) {                                   // a wavefront's 128 rows are one chunk of the column sums
         f4 out = {0.f, 0.f, 0.f, 0.f};
@@ -886,7 +907,8 @@ __global__ __launch_bounds__(512, 2) void hdet_bgemm_walk_kernel(const hdet_bgem
             if (lr == j) out[e] = x;
           }
         const int nchunks = (g.m + 127) / 128, chunk = (t.m0 + wm) / 128, c = t.n0 + wn + lr * 16 + cg * 4;
-        if (lr < 4 && chunk < nchunks && c < g.n) *reinterpret_cast<f4*>(g.colsum + ((int64_t)t.z * nchunks + chunk) * g.n + c) = out;
+        const int pitch = (g.n + 3) & ~3;
+        if (lr < 4 && chunk < nchunks && c < g.n) *reinterpret_cast<f4*>(g.colsum + ((int64_t)t.z * nchunks + chunk) * pitch + c) = out;
       }
     }
   };
@@ -1033,6 +1055,8 @@ namespace {
 // (the update epilogue writes no result)
 template <int EPI> constexpr bool kAlwaysStream = EPI == HDET_EPI_ADAMW || EPI == HDET_EPI_GELUGRAD_BF16;
 bool stream_result(const hdet_bgemm_args& g, int epi, int batch) {
+  if (epi == HDET_EPI_SCALED_F32) epi = HDET_EPI_F32;
+  if (epi == HDET_EPI_SCALED_BF16) epi = HDET_EPI_BF16;
   const int64_t size = epi == HDET_EPI_F32 || epi == HDET_EPI_BIAS_F32 ? 4 : 2;
   const uint64_t part = (reinterpret_cast<uintptr_t>(g.c) | (uint64_t)((g.ldc | g.c_s[0] | g.c_s[1] | g.c_s[2]) * size)) & 127;
   if (part == 0) return true;
@@ -1073,11 +1097,11 @@ constexpr tile_shape kDeep = {128, 128, 1, 0.f, 0.f, 0.f, 0.f};                /
 template <int EPI> constexpr float kEpiTime =
     EPI == HDET_EPI_ADAMW ? 80.f : EPI == HDET_EPI_GELUGRAD_BF16 || EPI == HDET_EPI_BIAS_DROP_RESID_BF16 ? 20.f
     : EPI == HDET_EPI_MASK_BF16 || EPI == HDET_EPI_BIAS_RESID_BF16 || EPI == HDET_EPI_ACCUM_BF16 || EPI == HDET_EPI_BIAS_GELU_BF16 ? 15.f
-    : EPI == HDET_EPI_F32 || EPI == HDET_EPI_BIAS_F32 ? 12.f : EPI == HDET_EPI_BIAS_RELU_BF16 ? 9.f : 8.f;
+    : EPI == HDET_EPI_F32 || EPI == HDET_EPI_BIAS_F32 || EPI == HDET_EPI_SCALED_F32 ? 12.f : EPI == HDET_EPI_BIAS_RELU_BF16 ? 9.f : 8.f;
 
 // What hdet_bgemm_walk_kernel asks for beyond the LDS-direct kernels: whole groups of 8 columns, results and their rows 16-byte aligned, four K steps
 bool walkable(const hdet_bgemm_args& g) {
-  return g.n1 * g.n2 == 1 && g.k >= 192 && (g.n & 7) == 0 && ((g.ldc | g.c_s[0]) & 7) == 0 &&
+  return g.n1 * g.n2 == 1 && (g.padded || (g.k >= 192 && (g.n & 7) == 0)) && ((g.ldc | g.c_s[0]) & 7) == 0 &&
          (reinterpret_cast<uintptr_t>(g.c) & 15) == 0 && g.ldc < 1 << 22 && g.m < 1 << 28 &&
          ((int64_t)g.m + 256) * g.lda * 2 < (int64_t)1 << 31 && ((int64_t)g.n + 256) * g.ldb * 2 < (int64_t)1 << 31;
 }
@@ -1161,12 +1185,12 @@ hipError_t launch_shape(const hdet_bgemm_args& g, int batch, hipStream_t s) {
 }  // namespace
 
 bool hdet_bgemm_dma_eligible(const hdet_bgemm_args& g, bool a_kmajor, bool b_kmajor, int epi) {
-  const bool f32_out = epi == HDET_EPI_F32 || epi == HDET_EPI_BIAS_F32;
+  const bool f32_out = epi == HDET_EPI_F32 || epi == HDET_EPI_BIAS_F32 || epi == HDET_EPI_SCALED_F32;
   const bool has_bias = epi == HDET_EPI_BIAS_F32 || epi == HDET_EPI_BIAS_BF16 || epi == HDET_EPI_BIAS_RELU_BF16 ||
                         epi == HDET_EPI_BIAS_GELU_BF16 || epi == HDET_EPI_BIAS_RESID_BF16 || epi == HDET_EPI_BIAS_DROP_RESID_BF16;
   if (g.m < 1 || g.n < 1 || g.k < 1) return false;
   // a chunk is 8 elements along the operand's contiguous axis: k if k-major, else the row axis
-  if (!chunk_regular(g.a, g.lda, g.a_s, a_kmajor ? g.k : g.m)) return false;
+  if (!chunk_regular(g.a, g.lda, g.a_s, g.padded ? 0 : a_kmajor ? g.k : g.m)) return false;
   if (!chunk_regular(g.b, g.ldb, g.b_s, b_kmajor ? g.k : g.n)) return false;
   // operand extents of one batch item as 32-bit byte offsets below the "absent" mark
   const int64_t a_bytes = ((int64_t)((a_kmajor ? g.m : g.k) - 1) * g.lda + (a_kmajor ? g.k : g.m)) * 2;
@@ -1195,7 +1219,8 @@ bool hdet_bgemm_dma_eligible(const hdet_bgemm_args& g, bool a_kmajor, bool b_kma
     return epi == HDET_EPI_BIAS_RELU_BF16 || epi == HDET_EPI_BIAS_F32 || epi == HDET_EPI_BIAS_BF16 || epi == HDET_EPI_F32 ||
            epi == HDET_EPI_BIAS_GELU_BF16 || epi == HDET_EPI_BIAS_RESID_BF16 || epi == HDET_EPI_BIAS_DROP_RESID_BF16;
   if (a_kmajor && !b_kmajor) return epi == HDET_EPI_MASK_BF16 || epi == HDET_EPI_BF16 || epi == HDET_EPI_GELUGRAD_BF16 || epi == HDET_EPI_ACCUM_BF16;
-  if (!a_kmajor && !b_kmajor) return epi == HDET_EPI_F32 || epi == HDET_EPI_BF16 || epi == HDET_EPI_ADAMW;
+  if (!a_kmajor && !b_kmajor)
+    return epi == HDET_EPI_F32 || epi == HDET_EPI_BF16 || epi == HDET_EPI_ADAMW || epi == HDET_EPI_SCALED_F32 || epi == HDET_EPI_SCALED_BF16;
   return false;
 }
 
@@ -1224,11 +1249,30 @@ hipError_t hdet_launch_bgemm_dma(const hdet_bgemm_args& g_in, bool a_kmajor, boo
   }
   if (epi == HDET_EPI_F32) return launch_shape<false, false, HDET_EPI_F32>(g, batch, s);   // wgrad
   if (epi == HDET_EPI_ADAMW) return launch_shape<false, false, HDET_EPI_ADAMW>(g, batch, s);
+  if (epi == HDET_EPI_SCALED_F32) return launch_shape<false, false, HDET_EPI_SCALED_F32>(g, batch, s);
+  if (epi == HDET_EPI_SCALED_BF16) return launch_shape<false, false, HDET_EPI_SCALED_BF16>(g, batch, s);
   return launch_shape<false, false, HDET_EPI_BF16>(g, batch, s);
 }
 
 bool hdet_head_loss_eligible(const hdet_bgemm_args& g, int batch) {
   return walkable(g) && hdet_bgemm_dma_eligible(g, true, true, HDET_EPI_BIAS_BF16);
+}
+
+bool hdet_vocab_tiles_eligible(const hdet_bgemm_args& g) {
+  if (g.m < 1 || g.n < 1 || g.k < 1 || !g.padded || !g.bias) return false;
+  return walkable(g) && chunk_regular(g.a, g.lda, g.a_s, g.k) && chunk_regular(g.b, g.ldb, g.b_s, g.k) && (g.bias_bs & 3) == 0 &&
+         (reinterpret_cast<uintptr_t>(g.bias) & 15) == 0;
+}
+
+hipError_t hdet_launch_vocab_stat(const hdet_bgemm_args& g, int batch, hipStream_t s) {
+  launch_walk<HDET_EPI_XENT_STAT>(g, batch, s);
+  return hipGetLastError();
+}
+
+hipError_t hdet_launch_vocab_grad(const hdet_bgemm_args& g, int parts, int batch, hipStream_t s) {
+  if (parts == 3) launch_walk<HDET_EPI_XENT_PARTS>(g, batch, s);
+  else launch_walk<HDET_EPI_XENT_GRAD>(g, batch, s);
+  return hipGetLastError();
 }
 
 size_t hdet_head_loss_scratch(int m, int n, int batch) {

@@ -169,8 +169,10 @@ enum { HDET_EPI_F32 = 0, HDET_EPI_BIAS_F32 = 1, HDET_EPI_BIAS_RELU_BF16 = 2, HDE
        // output layer whose logits z = acc + bias stay on the chip (hdet_launch_head_loss only):
        HDET_EPI_XENT_STAT = 11,       // reference and sum of a tile's rows (hdet_xent_epi; c is not written)
        HDET_EPI_XENT_GRAD = 12,
-       // a product in pieces of its contraction, input-gradient order: the sum so far is in fp32 at `accum`, the last piece's is rounded to c
-       HDET_EPI_ACCUM_BF16 = 13 };     // c = bf16 gradient of the mean cross-entropy at z, from the whole rows' reference and sum; row losses, column sums
+       // a product in pieces of its contraction, input-gradient order: the sum so far is in fp32 at `accum`, the last piece's is times out_scale and
+       // rounded to c; weight gradients times out_scale
+       HDET_EPI_ACCUM_BF16 = 13, HDET_EPI_SCALED_F32 = 14, HDET_EPI_SCALED_BF16 = 15,
+       HDET_EPI_XENT_PARTS = 16 };    // HDET_EPI_XENT_GRAD in three bf16 parts (hdet_launch_vocab_grad only)     // c = bf16 gradient of the mean cross-entropy at z, from the whole rows' reference and sum; row losses, column sums
 
 // Cross-entropy inside the output layer's product: what its two passes and the merge between them exchange.  Row scalars are [replica][row].
 struct hdet_xent_epi {
@@ -181,6 +183,7 @@ struct hdet_xent_epi {
   const int32_t* labels;
   float* row_loss;
   float invb;              // 1 / rows
+  int label0;              // class of column 0
 };
 
 struct hdet_bgemm_args {
@@ -207,6 +210,10 @@ struct hdet_bgemm_args {
   hdet_xent_epi xent;      // HDET_EPI_XENT_*
   float* accum; int64_t accum_ld, accum_bs;   // HDET_EPI_ACCUM_BF16: accum[z0*accum_bs + m*accum_ld + n]; the first piece does not read it,
   bool accum_first, accum_last;               // the last writes c instead
+  const float* out_scale;                     // [z0]
+  // An axis that is no multiple of 8 lies in rows that go on to one: A with zeros (its chunks are read whole), and for HDET_EPI_XENT_* bias with -inf and c
+  // with columns that may be written
+  bool padded;
   float* rowsum; int64_t rowsum_bs;     // general kernels, weight gradients: rowsum[z0*rowsum_bs + m] = sum_k A(m,k), or null
   int tile_group;          // LDS-direct kernel: consecutive blocks walk groups of this many tile rows column by column (0, 1: row by row)
   // HDET_EPI_ADAMW (n1 = n2 = 1, batch item = replica): the product is the replica's gradient of a weight matrix;
@@ -256,6 +263,11 @@ bool hdet_bgemm_dma_eligible(const hdet_bgemm_args& g, bool a_kmajor, bool b_kma
 bool hdet_head_loss_eligible(const hdet_bgemm_args& g, int batch);
 size_t hdet_head_loss_scratch(int m, int n, int batch);
 hipError_t hdet_launch_head_loss(const hdet_bgemm_args& g, int batch, void* scratch, hipStream_t stream);
+// The two passes of that product by themselves, over the columns of a piece of the classes (g: operands, bias, padded; c, colsum, xent as each pass needs
+// them).  parts = 3: the gradient in three bf16 parts whose sum it is to 24 bits, each [rows][ldc], one behind the other.
+bool hdet_vocab_tiles_eligible(const hdet_bgemm_args& g);
+hipError_t hdet_launch_vocab_stat(const hdet_bgemm_args& g, int batch, hipStream_t stream);
+hipError_t hdet_launch_vocab_grad(const hdet_bgemm_args& g, int parts, int batch, hipStream_t stream);
 int hdet_compute_units();     // compute units of the current device (queried once per device; 256 on MI355X)
 hipError_t hdet_launch_bgemm_dma(const hdet_bgemm_args& g, bool a_kmajor, bool b_kmajor, int epi, int batch,
                                  hipStream_t stream);

@@ -2,12 +2,16 @@
 //
 //   z = h W^T + b,  loss = log sum exp z - z_label,  dz = (softmax(z) - onehot) / c,  dh = dz W,  dW = dz^T h,  db = sum_rows dz
 //
-// No more than `piece` classes of z and dz exist at a time.  A first round over the pieces forms each row's reference and sum of exponentials, a second
-// forms z again, dz from it, and with dz the piece's share of dh (added up in fp32) and its rows of dW and db.  With one piece z is formed once.
+// No more than `piece` classes of z and dz exist at a time: a first round forms each row's reference and sum of exponentials, a second forms z again,
+// dz from it, and with dz the piece's share of dh (added up in fp32) and its rows of dW and db.
 //
-// Exponentials are exp2(z log2(e) - r) with r the whole number next to max log2(e): pieces refer to each other by exact powers of two.
-// dz leaves as bfloat16 -- what the matrix cores multiply -- for dh and a bfloat16 dW, whose own rounding is as coarse.  An fp32 dW takes dz in three bfloat16 parts,
-// 24 bits: they stand below each other as rows, beside three copies of h, and make one product of three times the rows.
+//  * Where h and W are made of whole 16-byte chunks z never leaves the matrix cores' registers: one product leaves reference and sum of each tile's part of a row,
+//    a second dz (hdet_bgemm_walk_kernel).  Other operands take z through memory in fp32, by pieces that are smaller by as much.
+//  * Exponentials are exp2(z log2(e) - r) with r the whole number next to max log2(e): tiles and pieces refer to each other by exact powers of two.
+//  * dz is held as c dz = softmax - onehot and the products' results are divided by c: at a label it is next to -1, which a bfloat16 holds to 2^-9 of itself, where
+//    (softmax - onehot) / c lies anywhere between two powers of two (dh against 64 bits: 2.9e-3 of its norm with the division before the rounding).
+//  * dz leaves as bfloat16 -- what the matrix cores multiply -- for dh and a bfloat16 dW, whose own rounding is as coarse.  An fp32 dW takes dz in three bfloat16
+//    parts, 24 bits: they stand below each other as rows, beside three copies of h, and make one product of three times the rows.
 
 #include <type_traits>
 
@@ -17,66 +21,114 @@
 namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
-constexpr double kLn2 = 0.6931471805599453;
-constexpr int kRowChunk = 128;      // rows of a block's column sums
+constexpr double kLn2 = 0.6931471805599453, kLog2eD = 1.4426950408889634;
+constexpr int kRowChunk = 128;                          // rows of a block's column sums
+constexpr size_t kPieceBytes = (size_t)256 << 20;       // dz of a piece, where the caller does not say
 
 // Memory of a call, in the order it is carved.  What a member names: [replica][...].
 struct vocab_layout {
-  int piece;                // classes at a time
-  int pieces;
+  int piece, pieces;        // classes at a time where z stays in registers
+  int small_piece;          // ... where it goes through memory
   int planes;               // bfloat16 parts of dz
-  int64_t pitch;            // columns of z and dz as they lie in memory
-  size_t count, ref, a, sum, zy, z, dz, h3, acc, part, total;
+  int64_t bias_pitch;
+  size_t inv, labels, ref, a, sum, zy, bias, dz, h3, acc, part, total;
 };
 size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
+int64_t up8(int64_t x) { return (x + 7) & ~(int64_t)7; }
 
 vocab_layout layout_of(int n, int64_t rows, int width, int classes, int dw_dtype, int piece) {
   vocab_layout l;
   l.planes = dw_dtype == HDET_TYPE_F32 ? 3 : 1;
-  const size_t all = (size_t)n * rows;
-  if (piece <= 0) {
-    // z and dz of a piece in a few hundred megabytes, at least 1024 classes
-    const size_t a_class = all * (4 + 2 * l.planes);
-    size_t p = a_class ? ((size_t)512 << 20) / a_class : (size_t)classes;
-    p = p / 256 * 256;
-    piece = p < 1024 ? 1024 : p > (size_t)classes ? classes : (int)p;
+  const size_t all = (size_t)n * (rows > 0 ? rows : 1);
+  size_t most = piece > 0 ? (size_t)piece : kPieceBytes / (all * 2 * l.planes);
+  if (piece <= 0 && most < 1024) most = 1024;
+  if (most > (size_t)classes) most = classes;
+  l.pieces = (int)((classes + most - 1) / most);
+  l.piece = (int)most;
+  if (l.pieces > 1) {
+    // pieces of one size, whole tiles of 256 classes, or whole groups of 8 where the caller wants fewer
+    if (piece <= 0) l.piece = (classes + l.pieces - 1) / l.pieces;
+    l.piece = piece <= 0 ? (l.piece + 255) / 256 * 256 : l.piece >= 256 ? l.piece / 256 * 256 : l.piece >= 8 ? l.piece / 8 * 8 : 8;
+    l.pieces = (classes + l.piece - 1) / l.piece;
   }
-  if (piece > classes) piece = classes;
-  l.piece = piece;
-  l.pieces = (classes + piece - 1) / piece;
-  l.pitch = (piece + 7) & ~7;
+  size_t room = all * up8(l.piece) * 2 * l.planes;                                  // dz
+  const size_t a_class = all * (4 + 2 * l.planes), small = (size_t)64 << 20;        // z and dz
+  const size_t whole = a_class * up8(l.piece);
+  if (room < (whole < small ? whole : small)) room = whole < small ? whole : small;
+  if (room < a_class * 8) room = a_class * 8;
+  const size_t stats = all * 8 * ((size_t)(classes + 255) / 256);                   // the first round's, before there is a dz
+  if (room < stats) room = stats;
+  size_t fit = room / a_class / 8 * 8;
+  l.small_piece = fit < (size_t)l.piece ? (int)fit : l.piece;
+  l.bias_pitch = up8(classes);
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t here = at; at += up(bytes); return here; };
-  l.count = take((size_t)n * 4);
+  l.inv = take((size_t)n * 4);
+  l.labels = take(all * 4);
   l.ref = take(all * 4);
   l.a = take(all * 4);
   l.sum = take(all * 8);
   l.zy = take(all * 4);
-  l.z = take(all * l.pitch * 4);
-  l.dz = take(all * l.pitch * 2 * l.planes);
+  l.bias = take((size_t)n * l.bias_pitch * 4);
+  l.dz = take(room);
   l.h3 = take(l.planes == 3 ? all * 3 * width * 2 : 0);
-  l.acc = take(l.pieces > 1 ? all * width * 4 : 0);
-  l.part = take((size_t)n * ((rows + kRowChunk - 1) / kRowChunk) * l.pitch * 4);
+  l.acc = take(l.pieces > 1 || l.small_piece < l.piece ? all * width * 4 : 0);
+  l.part = take((size_t)n * ((rows + kRowChunk - 1) / kRowChunk) * up8(l.piece) * 4);
   l.total = at;
   return l;
 }
 
+struct prep_args {
+  const int32_t* labels; int32_t* labels_out;
+  const float* bias; int64_t bias_z; float* bias_out; int64_t bias_pitch;
+  const uint16_t* h; int64_t h_s, h_z; uint16_t* h3;
+  float *inv, *mean, *row_loss;
+  int64_t rows;
+  int classes, width;
+};
+
 }  // namespace
 
-// 1 / rows that count, and the losses of a replica without rows.  One block a replica.
-__global__ __launch_bounds__(256) void hdet_vocab_count_kernel(const int32_t* labels, int64_t rows, int classes, float* inv, float* mean) {
-  __shared__ int part[4];
-  const int z = blockIdx.x;
+// What a call starts with, [replica] on blockIdx.y: labels that name no class become -1; 1 / rows that count; bias in rows padded with -inf; three copies of h.
+__global__ __launch_bounds__(1024) void hdet_vocab_prep_kernel(const prep_args a) {
+  const int z = blockIdx.y;
+  const int64_t t = (int64_t)blockIdx.x * 1024 + threadIdx.x, step = (int64_t)gridDim.x * 1024;
+  const int32_t* lab = a.labels + z * a.rows;
+  for (int64_t i = t; i < a.rows; i += step) a.labels_out[z * a.rows + i] = (unsigned)lab[i] < (unsigned)a.classes ? lab[i] : -1;
+  if (a.bias_out)
+    for (int64_t i = t; i < a.bias_pitch; i += step) a.bias_out[z * a.bias_pitch + i] = i >= a.classes ? -INFINITY : a.bias ? a.bias[z * a.bias_z + i] : 0.f;
+  if (a.h3) {
+    uint16_t* out = a.h3 + z * 3 * a.rows * a.width;
+    if (((a.width | a.h_s | a.h_z) & 7) == 0 && (reinterpret_cast<uintptr_t>(a.h) & 15) == 0) {
+      const int64_t pieces = a.width / 8, all = a.rows * pieces;
+      for (int64_t i = t; i < all; i += step) {
+        const hdet_u4v v = *reinterpret_cast<const hdet_u4v*>(a.h + z * a.h_z + i / pieces * a.h_s + i % pieces * 8);
+#pragma unroll
+        for (int q = 0; q < 3; ++q) reinterpret_cast<hdet_u4v*>(out)[q * all + i] = v;
+      }
+    } else {
+      const int64_t all = a.rows * a.width;
+      for (int64_t i = t; i < all; i += step) {
+        const uint16_t v = a.h[z * a.h_z + i / a.width * a.h_s + i % a.width];
+#pragma unroll
+        for (int q = 0; q < 3; ++q) out[q * all + i] = v;
+      }
+    }
+  }
+  if (blockIdx.x != 0) return;
+  __shared__ int part[16];
   int n = 0;
-  for (int64_t i = threadIdx.x; i < rows; i += 256) n += (unsigned)labels[z * rows + i] < (unsigned)classes ? 1 : 0;
+  for (int64_t i = threadIdx.x; i < a.rows; i += 1024) n += (unsigned)lab[i] < (unsigned)a.classes ? 1 : 0;
 #pragma unroll
   for (int o = 1; o < 64; o <<= 1) n += __shfl_xor(n, o);
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = n;
   __syncthreads();
   if (threadIdx.x == 0) {
-    n = part[0] + part[1] + part[2] + part[3];
-    inv[z] = 1.f / (float)(n > 1 ? n : 1);
-    if (rows == 0) mean[z] = 0.f;
+    n = 0;
+#pragma unroll
+    for (int w = 0; w < 16; ++w) n += part[w];
+    a.inv[z] = 1.f / (float)(n > 1 ? n : 1);
+    if (a.rows == 0) a.mean[z] = 0.f;
   }
 }
 
@@ -118,44 +170,89 @@ __global__ __launch_bounds__(256) void hdet_vocab_stat_kernel(const float* z, in
 }
 
 // A row's loss and the factor of its exponentials in dz
-__global__ __launch_bounds__(256) void hdet_vocab_rows_kernel(const float* ref, const double* sum, const float* zy, const int32_t* labels, const float* inv, int64_t rows,
-                                                              int classes, float* a, float* row_loss) {
-  const int64_t row = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int z = blockIdx.y;
+__global__ __launch_bounds__(256) void hdet_vocab_rows_kernel(const float* ref, const double* sum, const float* zy, const int32_t* labels, int64_t rows, float* a, float* row_loss) {
+  const int64_t row = (int64_t)blockIdx.x * 256 + threadIdx.x, at = blockIdx.y * rows + row;
   if (row >= rows) return;
-  const int64_t at = z * rows + row;
-  const bool counts = (unsigned)labels[at] < (unsigned)classes;
-  a[at] = counts ? (float)((double)inv[z] / sum[at]) : 0.f;
-  row_loss[at] = counts ? (float)(((double)ref[at] + log2(sum[at]) - (double)zy[at] * 1.4426950408889634) * kLn2) : 0.f;
+  const bool counts = labels[at] >= 0;
+  a[at] = counts ? (float)(1.0 / sum[at]) : 0.f;
+  row_loss[at] = counts ? (float)(((double)ref[at] + log2(sum[at]) - (double)zy[at] * kLog2eD) * kLn2) : 0.f;
 }
 
-__global__ __launch_bounds__(256) void hdet_vocab_mean_kernel(const float* row_loss, const float* inv, int64_t rows, float* mean) {
-  __shared__ double part[4];
-  const int z = blockIdx.x;
+// The same from the column tiles' references and sums ([replica][tile][row]); lse: log2 of the sum of exp2(z log2(e)).  Rows that do not count: loss and factor 0.
+// Block = 64 rows x 4 phases; phase q takes tiles q, q + 4, ..., the phases are added in their order, in 64 bits.
+__global__ __launch_bounds__(256) void hdet_vocab_merge_kernel(const float2* part, int tiles, int64_t rows, const int32_t* labels, float* ref, float* a, double* lse, float* row_loss) {
+  __shared__ float refs[4][64];
+  __shared__ double sums[4][64];
+  const int lane = threadIdx.x & 63, q = threadIdx.x >> 6;
+  const int64_t row = (int64_t)blockIdx.x * 64 + lane, at = blockIdx.y * rows + row;
+  float mx = -INFINITY;
   double s = 0.0;
-  for (int64_t i = threadIdx.x; i < rows; i += 256) s += (double)row_loss[z * rows + i];
-#pragma unroll
-  for (int o = 1; o < 64; o <<= 1) s += __shfl_xor(s, o);
-  if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
+  if (row < rows) {
+    const float2* p = part + (int64_t)blockIdx.y * tiles * rows + row;
+#pragma unroll 8
+    for (int t = q; t < tiles; t += 4) {
+      const float2 v = p[(int64_t)t * rows];
+      const float mn = fmaxf(mx, v.x);
+      if (v.x != -INFINITY) s = s * (double)__builtin_amdgcn_exp2f(mx - mn) + (double)(v.y * __builtin_amdgcn_exp2f(v.x - mn));
+      else s += v.y;
+      mx = mn;
+    }
+  }
+  refs[q][lane] = mx;
+  sums[q][lane] = s;
   __syncthreads();
-  if (threadIdx.x == 0) mean[z] = (float)((part[0] + part[1] + part[2] + part[3]) * (double)inv[z]);
+  if (q != 0 || row >= rows) return;
+  float r[4];
+  double p[4];
+#pragma unroll
+  for (int w = 0; w < 4; ++w) { r[w] = refs[w][lane]; p[w] = sums[w][lane]; }
+  const float top = fmaxf(fmaxf(r[0], r[1]), fmaxf(r[2], r[3]));
+  double sum = 0.0;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) sum += r[w] == -INFINITY && p[w] == 0.0 && top != -INFINITY ? 0.0 : p[w] * (double)__builtin_amdgcn_exp2f(r[w] - top);
+  const bool counts = labels[at] >= 0;
+  ref[at] = top;
+  a[at] = counts ? (float)(1.0 / sum) : 0.f;
+  lse[at] = (double)top + log2(sum);
+  if (!counts) row_loss[at] = 0.f;
 }
 
-// dz of a piece from z, in PLANES bfloat16 parts, and its sums over 128 rows.  Thread = a column; grid (ceil(pitch / 256), row chunks, replicas).
+// Row losses where no gradients are wanted: the label's logit by itself.  A wavefront a row; grid (ceil(rows / 4), replicas).
+__global__ __launch_bounds__(256) void hdet_vocab_label_kernel(const uint16_t* h, int64_t h_s, int64_t h_z, const uint16_t* w, int64_t w_s, int64_t w_z, const float* bias,
+                                                               int64_t bias_pitch, const int32_t* labels, const double* lse, int64_t rows, int width, float* row_loss) {
+  const int64_t row = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6), at = blockIdx.y * rows + row;
+  const int lane = threadIdx.x & 63;
+  if (row >= rows) return;
+  const int y = labels[at];
+  if (y < 0) return;
+  const uint16_t *p = h + blockIdx.y * h_z + row * h_s, *q = w + blockIdx.y * w_z + y * w_s;
+  float s = 0.f;
+  for (int c = lane * 8; c < width; c += 512) {
+    const hdet_f8 u = hdet_ld8(p + c), v = hdet_ld8(q + c);
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s = __builtin_fmaf(u.v[e], v.v[e], s);
+  }
+  s = hdet_wave_sum(s) + bias[blockIdx.y * bias_pitch + y];
+  if (lane == 0) row_loss[at] = (float)((lse[at] - (double)s * kLog2eD) * kLn2);
+}
+
+// c dz of a piece from z, in PLANES bfloat16 parts, and its sums over 128 rows.  Thread = a column; grid (ceil(pitch / 256), row chunks, replicas).
 template <int PLANES>
-__global__ __launch_bounds__(256) void hdet_vocab_grad_kernel(const float* z, int64_t pitch, int64_t rows, int cols, int v0, int classes, const int32_t* labels, const float* ref,
-                                                              const float* a, const float* inv, uint16_t* dz, float* part) {
+__global__ __launch_bounds__(256) void hdet_vocab_grad_kernel(const float* z, int64_t pitch, int64_t rows, int cols, int v0, const int32_t* labels, const float* ref,
+                                                              const float* a, uint16_t* dz, float* part, int64_t part_pitch) {
   const int c = blockIdx.x * 256 + threadIdx.x, zr = blockIdx.z;
   if (c >= pitch) return;
   const int64_t r0 = (int64_t)blockIdx.y * kRowChunk, r1 = r0 + kRowChunk < rows ? r0 + kRowChunk : rows;
-  const float invc = inv[zr];
   float sum = 0.f;
+#pragma unroll 4
   for (int64_t r = r0; r < r1; ++r) {
     const int64_t at = zr * rows + r;
-    const int y = labels[at] - v0;
     float v = 0.f;
-    if (c < cols && a[at] != 0.f) v = __builtin_amdgcn_exp2f(__builtin_fmaf(z[at * pitch + c], kLog2e, -ref[at])) * a[at];
-    if (c < cols && c == y) v -= invc;
+    if (c < cols) {
+      const float x = z[at * pitch + c], f = a[at];
+      if (f != 0.f) v = __builtin_amdgcn_exp2f(__builtin_fmaf(x, kLog2e, -ref[at])) * f;
+      if (c == labels[at] - v0) v -= 1.f;
+    }
     sum += v;
     uint16_t* p = dz + ((int64_t)zr * PLANES * rows + r) * pitch + c;
 #pragma unroll
@@ -165,16 +262,35 @@ __global__ __launch_bounds__(256) void hdet_vocab_grad_kernel(const float* z, in
       v -= __uint_as_float(b << 16);
     }
   }
-  if (part) part[((int64_t)zr * gridDim.y + blockIdx.y) * pitch + c] = sum;
+  if (part && c < part_pitch) part[((int64_t)zr * gridDim.y + blockIdx.y) * part_pitch + c] = sum;
 }
 
-// three copies of h below each other: [replica][3][rows][width]
-__global__ __launch_bounds__(256) void hdet_vocab_copy_kernel(const uint16_t* h, int64_t h_s, int64_t h_z, int64_t rows, int width, uint16_t* out) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x, all = rows * width;
-  if (i >= all) return;
-  const uint16_t v = h[blockIdx.y * h_z + i / width * h_s + i % width];
-  uint16_t* p = out + blockIdx.y * 3 * all + i;
-  p[0] = v; p[all] = v; p[2 * all] = v;
+// db of a piece from its column sums, 64 columns x 4 phases a block; the last block column, where row_loss is given: the mean loss.  Grid (blocks, replicas).
+__global__ __launch_bounds__(256) void hdet_vocab_sums_kernel(const float* part, int parts, int cols, int64_t pitch, float* db, int64_t db_z, const float* inv, const float* row_loss,
+                                                              int64_t rows, float* mean) {
+  __shared__ double sum[4];
+  __shared__ float s[4][64];
+  const int z = blockIdx.y, lane = threadIdx.x & 63, ph = threadIdx.x >> 6;
+  if (row_loss && blockIdx.x + 1 == gridDim.x) {
+    double x = 0.0;
+    for (int64_t i = threadIdx.x; i < rows; i += 256) x += (double)row_loss[z * rows + i];
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) x += __shfl_xor(x, o);
+    if (lane == 0) sum[ph] = x;
+    __syncthreads();
+    if (threadIdx.x == 0) mean[z] = (float)((sum[0] + sum[1] + sum[2] + sum[3]) * (double)inv[z]);
+    return;
+  }
+  const int col = blockIdx.x * 64 + lane;
+  float x = 0.f;
+  if (col < cols) {
+    const float* p = part + (int64_t)z * parts * pitch + col;
+#pragma unroll 4
+    for (int i = ph; i < parts; i += 4) x += p[i * pitch];
+  }
+  s[ph][lane] = x;
+  __syncthreads();
+  if (ph == 0 && col < cols) db[z * db_z + col] = ((s[0][lane] + s[1][lane]) + (s[2][lane] + s[3][lane])) * inv[z];
 }
 
 // zeros in a matrix of `size`-byte elements (2 or 4)
@@ -201,69 +317,124 @@ hipError_t hdet_launch_vocab_loss(const hdet_vocab_args& a, hipStream_t s) {
   const int64_t M = a.rows;
   const vocab_layout l = layout_of(n, M, d, V, a.dw.dev ? a.dw_dtype : HDET_TYPE_BF16, a.piece);
   char* const ws = (char*)a.workspace_dev;
-  float* const inv = (float*)(ws + l.count);
-  hipLaunchKernelGGL(hdet_vocab_count_kernel, dim3(n), dim3(256), 0, s, a.labels_dev, M, V, inv, a.mean_loss_dev);
-  hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return e;
+  float *const inv = (float*)(ws + l.inv), *const ref = (float*)(ws + l.ref), *const ra = (float*)(ws + l.a), *const zy = (float*)(ws + l.zy), *const part = (float*)(ws + l.part);
+  float* const bias = (float*)(ws + l.bias);
+  int32_t* const labels = (int32_t*)(ws + l.labels);
+  double* const sum = (double*)(ws + l.sum);
+  uint16_t* const h3 = (uint16_t*)(ws + l.h3);
+  const uint16_t *h = (const uint16_t*)a.h.dev, *w = (const uint16_t*)a.w.dev;
+  const bool grads = a.dh.dev || a.dw.dev || a.db_dev;
+  const int chunks = (int)((M + kRowChunk - 1) / kRowChunk);
+  hipError_t e;
+
+  // z = h W^T + bias of the classes from v0 on; in tiles: bias padded
+  auto product = [&](int v0, int cols, bool tiles) {
+    hdet_bgemm_args g = {};
+    g.a = h; g.lda = a.h.row_stride; g.a_s[0] = a.h.replica_stride;
+    g.b = w + v0 * a.w.row_stride; g.ldb = a.w.row_stride; g.b_s[0] = a.w.replica_stride;
+    g.m = (int)M; g.n = cols; g.k = d; g.n1 = g.n2 = 1;
+    g.bias = tiles ? bias + v0 : a.bias_dev ? a.bias_dev + v0 : nullptr;
+    g.bias_bs = tiles ? l.bias_pitch : a.bias_stride;
+    g.padded = tiles;
+    g.xent.labels = labels; g.xent.row_loss = a.row_loss_dev; g.xent.row_ref = ref; g.xent.row_a = ra; g.xent.row_lse = sum;
+    g.xent.invb = 1.f; g.xent.label0 = v0;
+    return g;
+  };
+  const bool tiles = M > 0 && hdet_vocab_tiles_eligible(product(0, V, true));
+  const int piece = tiles ? l.piece : l.small_piece, pieces = (V + piece - 1) / piece;
+  const int64_t pitch = up8(piece);
+
+  {
+    prep_args p = {a.labels_dev, labels, a.bias_dev, a.bias_stride, tiles ? bias : nullptr, l.bias_pitch, h, a.h.row_stride, a.h.replica_stride,
+                   l.planes == 3 && M > 0 ? h3 : nullptr, inv, a.mean_loss_dev, a.row_loss_dev, M, V, d};
+    int64_t work = M > l.bias_pitch ? M : l.bias_pitch;
+    if (p.h3 && M * d / 8 > work) work = M * d / 8;
+    int64_t blocks = (work + 1023) / 1024;
+    if (blocks > 1024) blocks = 1024;
+    hipLaunchKernelGGL(hdet_vocab_prep_kernel, dim3((unsigned)blocks, n), dim3(1024), 0, s, p);
+    if ((e = hipGetLastError()) != hipSuccess) return e;
+  }
   if (M == 0) {
     if (a.dw.dev && (e = hdet_launch_zero_rows(a.dw, n, V, d, a.dw_dtype, s)) != hipSuccess) return e;
     return a.db_dev ? hdet_launch_partial_sum(nullptr, n, 0, V, 0, a.db_dev, a.db_stride, s) : hipSuccess;
   }
-  float *const ref = (float*)(ws + l.ref), *const ra = (float*)(ws + l.a), *const zy = (float*)(ws + l.zy), *const z = (float*)(ws + l.z);
-  double* const sum = (double*)(ws + l.sum);
-  uint16_t *const dz = (uint16_t*)(ws + l.dz), *const h3 = (uint16_t*)(ws + l.h3);
-  float* const part = (float*)(ws + l.part);
-  const bool grads = a.dh.dev || a.dw.dev || a.db_dev;
-  const uint16_t *h = (const uint16_t*)a.h.dev, *w = (const uint16_t*)a.w.dev;
-  const int chunks = (int)((M + kRowChunk - 1) / kRowChunk);
-
+  float* const z = (float*)(ws + l.dz);
+  uint16_t* const dz = (uint16_t*)(ws + l.dz + (tiles ? 0 : (size_t)n * M * pitch * 4));
   auto logits = [&](int v0, int cols) {
-    hdet_bgemm_args g = {};
-    g.a = h; g.lda = a.h.row_stride; g.a_s[0] = a.h.replica_stride;
-    g.b = w + v0 * a.w.row_stride; g.ldb = a.w.row_stride; g.b_s[0] = a.w.replica_stride;
-    g.c = z; g.ldc = l.pitch; g.c_s[0] = M * l.pitch;
-    g.m = (int)M; g.n = cols; g.k = d;
-    if (a.bias_dev) { g.bias = a.bias_dev + v0; g.bias_bs = a.bias_stride; }
+    hdet_bgemm_args g = product(v0, cols, false);
+    g.c = z; g.ldc = pitch; g.c_s[0] = M * pitch;
     return hdet_launch_bgemm(g, true, true, a.bias_dev ? HDET_EPI_BIAS_F32 : HDET_EPI_F32, n, s);
   };
-  for (int p = 0; p < l.pieces; ++p) {
-    const int v0 = p * l.piece, cols = V - v0 < l.piece ? V - v0 : l.piece;
-    if ((e = logits(v0, cols)) != hipSuccess) return e;
-    hipLaunchKernelGGL(hdet_vocab_stat_kernel, dim3((unsigned)M, n), dim3(256), 0, s, z, l.pitch, M, cols, v0, a.labels_dev, ref, sum, zy);
+
+  // first round: every row's reference and sum
+  if (tiles) {
+    hdet_bgemm_args g = product(0, V, true);
+    float2* const stats = (float2*)(ws + l.dz);
+    g.xent.part = stats;
+    if ((e = hdet_launch_vocab_stat(g, n, s)) != hipSuccess) return e;
+    hipLaunchKernelGGL(hdet_vocab_merge_kernel, dim3((unsigned)((M + 63) / 64), n), dim3(256), 0, s, stats, (V + 255) / 256, M, labels, ref, ra, sum, a.row_loss_dev);
+    if (!grads)
+      hipLaunchKernelGGL(hdet_vocab_label_kernel, dim3((unsigned)((M + 3) / 4), n), dim3(256), 0, s, h, a.h.row_stride, a.h.replica_stride, w, a.w.row_stride, a.w.replica_stride,
+                         bias, l.bias_pitch, labels, sum, M, d, a.row_loss_dev);
+  } else {
+    for (int p = 0; p < pieces; ++p) {
+      const int v0 = p * piece, cols = V - v0 < piece ? V - v0 : piece;
+      if ((e = logits(v0, cols)) != hipSuccess) return e;
+      hipLaunchKernelGGL(hdet_vocab_stat_kernel, dim3((unsigned)M, n), dim3(256), 0, s, z, pitch, M, cols, v0, labels, ref, sum, zy);
+    }
+    hipLaunchKernelGGL(hdet_vocab_rows_kernel, dim3((unsigned)((M + 255) / 256), n), dim3(256), 0, s, ref, sum, zy, labels, M, ra, a.row_loss_dev);
   }
-  hipLaunchKernelGGL(hdet_vocab_rows_kernel, dim3((unsigned)((M + 255) / 256), n), dim3(256), 0, s, ref, sum, zy, a.labels_dev, inv, M, V, ra, a.row_loss_dev);
-  hipLaunchKernelGGL(hdet_vocab_mean_kernel, dim3(n), dim3(256), 0, s, a.row_loss_dev, inv, M, a.mean_loss_dev);
-  if ((e = hipGetLastError()) != hipSuccess || !grads) return e;
-  if (l.planes == 3 && a.dw.dev)
-    hipLaunchKernelGGL(hdet_vocab_copy_kernel, dim3((unsigned)((M * d + 255) / 256), n), dim3(256), 0, s, h, a.h.row_stride, a.h.replica_stride, M, d, h3);
-  for (int p = 0; p < l.pieces; ++p) {
-    const int v0 = p * l.piece, cols = V - v0 < l.piece ? V - v0 : l.piece;
-    if (l.pieces > 1 && (e = logits(v0, cols)) != hipSuccess) return e;
-    const dim3 grid((unsigned)((l.pitch + 255) / 256), chunks, n);
-    float* const to = a.db_dev ? part : nullptr;
-    if (l.planes == 3) hipLaunchKernelGGL(hdet_vocab_grad_kernel<3>, grid, dim3(256), 0, s, z, l.pitch, M, cols, v0, V, a.labels_dev, ref, ra, inv, dz, to);
-    else hipLaunchKernelGGL(hdet_vocab_grad_kernel<1>, grid, dim3(256), 0, s, z, l.pitch, M, cols, v0, V, a.labels_dev, ref, ra, inv, dz, to);
-    if ((e = hipGetLastError()) != hipSuccess) return e;
-    if (a.db_dev && (e = hdet_launch_partial_sum(part, n, chunks, cols, l.pitch, a.db_dev + v0, a.db_stride, s)) != hipSuccess) return e;
+  if ((e = hipGetLastError()) != hipSuccess) return e;
+
+  // second round: dz of a piece and what comes of it
+  for (int p = 0; p < pieces && grads; ++p) {
+    const int v0 = p * piece, cols = V - v0 < piece ? V - v0 : piece;
+    const int64_t part_pitch = (cols + 3) & ~3;
+    if (tiles) {
+      hdet_bgemm_args g = product(v0, cols, true);
+      g.c = dz; g.ldc = pitch; g.c_s[0] = l.planes * M * pitch;
+      g.colsum = a.db_dev ? part : nullptr;
+      if ((e = hdet_launch_vocab_grad(g, l.planes, n, s)) != hipSuccess) return e;
+    } else {
+      if (pieces > 1 && (e = logits(v0, cols)) != hipSuccess) return e;
+      const dim3 grid((unsigned)((pitch + 255) / 256), chunks, n);
+      float* const to = a.db_dev ? part : nullptr;
+      if (l.planes == 3) hipLaunchKernelGGL(hdet_vocab_grad_kernel<3>, grid, dim3(256), 0, s, z, pitch, M, cols, v0, labels, ref, ra, dz, to, part_pitch);
+      else hipLaunchKernelGGL(hdet_vocab_grad_kernel<1>, grid, dim3(256), 0, s, z, pitch, M, cols, v0, labels, ref, ra, dz, to, part_pitch);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
+    const bool last = p + 1 == pieces;
+    if (a.db_dev || last) {
+      const unsigned blocks = (a.db_dev ? (cols + 63) / 64 : 0) + (last ? 1 : 0);
+      hipLaunchKernelGGL(hdet_vocab_sums_kernel, dim3(blocks, n), dim3(256), 0, s, part, chunks, cols, part_pitch, a.db_dev + v0, a.db_stride, inv,
+                         last ? a.row_loss_dev : nullptr, M, a.mean_loss_dev);
+      if ((e = hipGetLastError()) != hipSuccess) return e;
+    }
     if (a.dh.dev) {
       hdet_bgemm_args g = {};
-      g.a = dz; g.lda = l.pitch; g.a_s[0] = l.planes * M * l.pitch;
+      g.a = dz; g.lda = pitch; g.a_s[0] = l.planes * M * pitch;
       g.b = w + v0 * a.w.row_stride; g.ldb = a.w.row_stride; g.b_s[0] = a.w.replica_stride;
       g.c = a.dh.dev; g.ldc = a.dh.row_stride; g.c_s[0] = a.dh.replica_stride;
       g.m = (int)M; g.n = d; g.k = cols;
       g.accum = (float*)(ws + l.acc); g.accum_ld = d; g.accum_bs = M * d;
-      g.accum_first = p == 0; g.accum_last = p + 1 == l.pieces;
-      if ((e = hdet_launch_bgemm(g, true, false, l.pieces > 1 ? HDET_EPI_ACCUM_BF16 : HDET_EPI_BF16, n, s)) != hipSuccess) return e;
+      g.accum_first = p == 0; g.accum_last = last; g.out_scale = inv;
+      g.padded = true;
+      if ((e = hdet_launch_bgemm(g, true, false, HDET_EPI_ACCUM_BF16, n, s)) != hipSuccess) return e;
     }
     if (a.dw.dev) {
       const bool f32 = l.planes == 3;
       hdet_bgemm_args g = {};
-      g.a = dz; g.lda = l.pitch; g.a_s[0] = l.planes * M * l.pitch;
+      g.a = dz; g.lda = pitch; g.a_s[0] = l.planes * M * pitch;
       g.b = f32 ? h3 : h; g.ldb = f32 ? d : a.h.row_stride; g.b_s[0] = f32 ? 3 * M * d : a.h.replica_stride;
       g.c = (char*)a.dw.dev + v0 * a.dw.row_stride * (f32 ? 4 : 2); g.ldc = a.dw.row_stride; g.c_s[0] = a.dw.replica_stride;
-      g.m = cols; g.n = d; g.k = (int)(l.planes * M);
-      if ((e = hdet_launch_bgemm(g, false, false, f32 ? HDET_EPI_F32 : HDET_EPI_BF16, n, s)) != hipSuccess) return e;
+      g.m = cols; g.n = d; g.k = (int)(l.planes * M); g.out_scale = inv;
+      g.padded = true;
+      if ((e = hdet_launch_bgemm(g, false, false, f32 ? HDET_EPI_SCALED_F32 : HDET_EPI_SCALED_BF16, n, s)) != hipSuccess) return e;
     }
+  }
+  if (!grads) {
+    hipLaunchKernelGGL(hdet_vocab_sums_kernel, dim3(1, n), dim3(256), 0, s, part, 0, 0, 0, a.db_dev, 0, inv, a.row_loss_dev, M, a.mean_loss_dev);
+    return hipGetLastError();
   }
   return hipSuccess;
 }

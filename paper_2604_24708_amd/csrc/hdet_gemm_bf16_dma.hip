@@ -41,6 +41,7 @@
 #include "hdet_internal.h"
 #include "hdet_elem.h"
 #include "hdet_lds.h"
+#include "hdet_tiles.h"
 #include "hdet_update_math.h"
 
 namespace {
@@ -52,8 +53,6 @@ typedef short s4 __attribute__((ext_vector_type(4)));
 typedef short s8 __attribute__((ext_vector_type(8)));
 typedef hdet_rsrc i4;
 typedef unsigned short us4 __attribute__((ext_vector_type(4)));
-
-constexpr uint32_t kAbsent = 0x80000000u;   // offset beyond every extent the host lets through
 
 __device__ __forceinline__ unsigned short f2bf(float x) {      // round to nearest even
   return __builtin_bit_cast(unsigned short, (__bf16)x);
@@ -137,16 +136,6 @@ struct lds_tile {
   }
 };
 
-// What lanes 32 .. 63 of a hold for what lanes 0 .. 31 of b hold; odd rows of 16 lanes of a for even rows of b
-__device__ __forceinline__ void swap32(unsigned& a, unsigned& b) {
-  const auto r = __builtin_amdgcn_permlane32_swap(a, b, false, false);
-  a = r[0]; b = r[1];
-}
-__device__ __forceinline__ void swap16(unsigned& a, unsigned& b) {
-  const auto r = __builtin_amdgcn_permlane16_swap(a, b, false, false);
-  a = r[0]; b = r[1];
-}
-
 // a reduction over the four groups of 16 lanes, the same value in each
 template <typename F>
 __device__ __forceinline__ float over_groups(float x, F op) {
@@ -158,28 +147,6 @@ __device__ __forceinline__ float over_groups(float x, F op) {
   return op(__uint_as_float(a), __uint_as_float(b));
 }
 
-// Launch order -> tile: each XCD (own L2; blocks are dealt to the XCDs round-robin) works through a contiguous
-// range of tiles, and inside a batch item consecutive tiles walk groups of tile_group tile rows column by column,
-// so that the blocks an XCD runs at one time share operand tiles of both kinds in its L2.
-struct tile_id { int bx, by, bz; };
-__device__ __forceinline__ tile_id tile_of_index(unsigned t, unsigned gx, unsigned gy, unsigned total, int tile_group) {
-  {   // XCD x = launch index mod 8 takes the x-th of eight contiguous ranges (the first total mod 8 ranges one tile longer)
-    const unsigned x = t & 7u, rem = total & 7u;
-    t = x * (total >> 3) + (x < rem ? x : rem) + (t >> 3);
-  }
-  tile_id id;
-  const unsigned per = gx * gy;
-  id.bz = t / per;
-  const unsigned r = t - id.bz * per;
-  const unsigned gm = tile_group > 1 ? (unsigned)tile_group : 1u;
-  const unsigned gsz = gm * gx;
-  const unsigned grp = r / gsz, first = grp * gm;
-  const unsigned rows = gy - first < gm ? gy - first : gm;
-  const unsigned q = r - grp * gsz;
-  id.by = first + q % rows;
-  id.bx = q / rows;
-  return id;
-}
 __device__ __forceinline__ tile_id tile_of_block(int tile_group) {
   return tile_of_index(blockIdx.x + gridDim.x * (blockIdx.y + gridDim.y * blockIdx.z), gridDim.x, gridDim.y, gridDim.x * gridDim.y * gridDim.z, tile_group);
 }
@@ -1105,7 +1072,6 @@ bool walkable(const hdet_bgemm_args& g) {
          (reinterpret_cast<uintptr_t>(g.c) & 15) == 0 && g.ldc < 1 << 22 && g.m < 1 << 28 &&
          ((int64_t)g.m + 256) * g.lda * 2 < (int64_t)1 << 31 && ((int64_t)g.n + 256) * g.ldb * 2 < (int64_t)1 << 31;
 }
-int tile_group_of(unsigned columns) { return columns >= 64 ? 4 : columns >= 12 ? 2 : 1; }
 template <int EPI>
 void launch_walk(hdet_bgemm_args g, int batch, hipStream_t s) {
   const unsigned gx = (g.n + 255) / 256, gy = (g.m + 255) / 256, total = gx * gy * (unsigned)batch, cus = (unsigned)compute_units();

@@ -10,14 +10,13 @@
 #include "hdet_ops.h"
 #include "hdet_elem.h"
 #include "hdet_lds.h"
+#include "hdet_tiles.h"
 
 namespace {
 
 typedef int i4v __attribute__((ext_vector_type(4)));
 typedef float f4 __attribute__((ext_vector_type(4)));
 typedef unsigned short us4 __attribute__((ext_vector_type(4)));
-
-constexpr uint32_t kAbsent = 0x80000000u;   // offset beyond every extent
 
 struct codes_args {
   const int8_t *x, *w;
@@ -151,6 +150,213 @@ void hdet_codes_gemm_kernel(const codes_args g) {
   }
 }
 
+// Large products: blocks that walk over tiles of 256 x 256, so that a tile's end -- y is written there, as many bytes as the products of a K of 500 take to form -- lies under the
+// next tile's loads.
+//  * Eight wavefronts of 128 x 64 in two groups of four, one of each on every SIMD: while one group multiplies (32 instructions, 512 cycles), the other reads its next
+//    fragments and requests a later K step; the block's barriers hand the matrix cores over.  A K step of 128 bytes is two such turns: rows 0-63 of the wavefront, then rows
+//    64-127 with the column fragments still in registers.  Two stages of 64 KiB; each turn waits for all but the newest eight of its loads.
+//  * The next tile's first two K steps are requested in the last two of the tile before; its scales and bias come into LDS a tile ahead.
+//  * Results leave from the registers.  Stores are always issued -- what does not exist lies outside the descriptor -- and the next tile's first K step waits for the loads before
+//    them, not for them.
+//  * Rows and columns past the matrices are zeros in the loop, and their results are not stored.
+template <typename OUT>
+__global__ __launch_bounds__(512, 2) void hdet_codes_walk_kernel(const codes_args g, unsigned gx, unsigned gy, unsigned total, int tile_group) {
+  constexpr int TM = 256, TN = 256, HALF = 128 * 128;             // bytes of half an operand tile
+  constexpr int kStores = sizeof(OUT) == 4 ? 32 : 16;
+  constexpr int kSideAt = 8 * HALF;                               // bias, column scales, row scales: [2][3][256]
+  __shared__ __attribute__((aligned(1024))) uint16_t S[(8 * HALF + 2 * 3 * 256 * 4) / 2];
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wn = (wave % 4) * 64, hr = (wave / 4) * 64, wm = (wave / 4) * 128;
+  // the lane's number outside the K loop, computed where it is used: kept over the tiles it would spill
+  auto lane_now = [] {
+    int x;
+    asm volatile("v_mbcnt_lo_u32_b32 %0, -1, 0\n\tv_mbcnt_hi_u32_b32 %0, -1, %0" : "=v"(x));
+    return x;
+  };
+  const uint32_t s_addr = lds_addr_of(S);
+  const int8_t* const base = reinterpret_cast<const int8_t*>(S);
+  const float* const side = reinterpret_cast<const float*>(base + kSideAt);
+  // A fragment is rows order(i) + row_in(0 .. 15) of the wavefront's 64, so a lane of group cg = lane / 16 accumulates columns order(j) + cg * kGroup + (0 .. 3), j = 0 .. 3, of
+  // y.  For bfloat16 results the order gives it 8 neighbours twice, so that one store of 16 bytes a lane covers 64 bytes of each row; four fp32 results are 16 bytes as they are.
+  constexpr bool kPlain = sizeof(OUT) == 4;
+  constexpr int kGroup = kPlain ? 4 : 8;
+  auto order = [](int j) { return kPlain ? j * 16 : (j >> 1) * 32 + (j & 1) * 4; };
+  auto row_in = [](int r) { return kPlain ? r : ((r & 12) << 1) + (r & 3); };
+  // the chunk permutation: by the bits in which a fragment's rows differ, but the lowest
+  auto perm = [](int r) { return kPlain ? swz(r) : ((r >> 2) & 6) | ((r >> 1) & 1); };
+  int nk = ((g.kbytes + 127) / 128 + 1) & ~1;                     // K steps of a tile, an even number from 4 on (steps beyond k are zeros)
+  nk = nk < 4 ? 4 : nk;
+
+  struct tile { int m0, n0, z; hdet_rsrc ra, rb; bool ok; };
+  auto tile_at = [&](unsigned t) {
+    tile r;
+    const tile_id id = tile_of_index(t < total ? t : total - 1, gx, gy, total, tile_group);
+    r.m0 = id.by * TM; r.n0 = id.bx * TN; r.z = id.bz;
+    r.ok = t < total;
+    r.ra = make_rsrc(g.x + r.z * g.x_z + (int64_t)r.m0 * g.x_ld, r.ok ? extent(g.m, r.m0, g.x_ld, g.kbytes) : 0u);
+    r.rb = make_rsrc(g.w + r.z * g.w_z + (int64_t)r.n0 * g.w_ld, r.ok ? extent(g.n, r.n0, g.w_ld, g.kbytes) : 0u);
+    return r;
+  };
+  const int ck = ((tid & 7) ^ perm(tid >> 3)) * 16;
+  uint32_t off_a = (uint32_t)((tid >> 3) * g.x_ld + ck), off_b = (uint32_t)((tid >> 3) * g.w_ld + ck);
+  // LDS, in units of 128 rows x 128 bytes: half h of A of stage s at 2 h + s (its rows 64 .. 127 are the tile's 128 .. 191 of that half), B at 4 + 2 s
+  auto load_a = [&](const hdet_rsrc& r, int h, int s, int kt) {
+    const uint32_t at = s_addr + (2 * h + s) * HALF;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+      lds_load16(r, at + (i * 512 + wave * 64) * 16, ck + kt * 128 < g.kbytes ? off_a + (uint32_t)(kt * 128 + (64 * h + 128 * i) * g.x_ld) : kAbsent);
+  };
+  auto load_b = [&](const hdet_rsrc& r, int s, int kt) {
+    const uint32_t at = s_addr + (4 + 2 * s) * HALF;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      lds_load16(r, at + (i * 512 + wave * 64) * 16, ck + kt * 128 < g.kbytes ? off_b + (uint32_t)(kt * 128 + 64 * i * g.w_ld) : kAbsent);
+  };
+  auto load_side = [&](const tile& t, int slot) {
+    const int ln = lane_now();
+#pragma unroll
+    for (int u = 0; u < 2; ++u) {
+      const int q = wave + 8 * u, at = (q & 3) * 64 + ln;
+      if (q < 12) {
+        const float* src = q < 4 ? (g.bias ? g.bias + t.z * g.bias_z + t.n0 : nullptr) : q < 8 ? g.w_scale + (int64_t)t.z * g.n + t.n0 : g.x_scale + (int64_t)t.z * g.m + t.m0;
+        const int count = q < 8 ? g.n - t.n0 : g.m - t.m0;
+        lds_load4(make_rsrc(src, t.ok && src ? (uint32_t)count * 4u : 0u), s_addr + kSideAt + (slot * 3 * 256 + q * 64) * 4, (uint32_t)at * 4u);
+      }
+    }
+  };
+  i4v acc[8][4];
+  i4v fa[2][4], fb[2][4];
+  // fragment i of sub-step ss is order(i) rows behind fragment 0, whose chunk permutation it shares: two addresses an operand
+  const int8_t *pa[2], *pb[2];
+#pragma unroll
+  for (int ss = 0; ss < 2; ++ss) {
+    const int r = row_in(lane & 15), at = r * 128 + (((ss * 4 + (lane >> 4)) ^ perm(r)) << 4);
+    pa[ss] = base + hr * 128 + at;
+    pb[ss] = base + 4 * HALF + wn * 128 + at;
+  }
+  auto read_a = [&](int h, int s) {
+#pragma unroll
+    for (int ss = 0; ss < 2; ++ss)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) fa[ss][i] = *reinterpret_cast<const i4v*>(pa[ss] + (2 * h + s) * HALF + order(i) * 128);
+  };
+  auto read_b = [&](int s) {
+#pragma unroll
+    for (int ss = 0; ss < 2; ++ss)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) fb[ss][j] = *reinterpret_cast<const i4v*>(pb[ss] + 2 * s * HALF + order(j) * 128);
+  };
+  auto multiply = [&](int h, bool first) {
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int ss = 0; ss < 2; ++ss)
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          acc[4 * h + i][j] = __builtin_amdgcn_mfma_i32_16x16x64_i8(fb[ss][j], fa[ss][i], first && ss == 0 ? i4v{0, 0, 0, 0} : acc[4 * h + i][j], 0, 0, 0);
+    __builtin_amdgcn_s_setprio(0);
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto meet = [] {
+    __builtin_amdgcn_sched_barrier(0);
+    asm volatile("s_barrier" ::: "memory");
+    __builtin_amdgcn_sched_barrier(0);
+  };
+  auto finish = [&](const tile& t, int slot) {
+    __builtin_amdgcn_sched_barrier(0);
+    const int ln = lane_now(), cg = ln >> 4, lr = row_in(ln & 15);
+    const float* sd = side + slot * 3 * 256;
+    f4 bias[4], sw[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      bias[j] = *reinterpret_cast<const f4*>(sd + wn + order(j) + cg * kGroup);
+      sw[j] = *reinterpret_cast<const f4*>(sd + 256 + wn + order(j) + cg * kGroup);
+    }
+    const auto rc = __builtin_amdgcn_make_buffer_rsrc(reinterpret_cast<OUT*>(g.y) + t.z * g.y_z + (int64_t)t.m0 * g.y_ld + t.n0, 0, 0x7fffffff, 0x00020000);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int tr = wm + (i >> 2) * 64 + order(i & 3) + lr;
+      const bool row_ok = t.m0 + tr < g.m;
+      const float sx = sd[512 + tr];
+      f4 v[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[j][e] = __builtin_fmaf((float)acc[i][j][e], sx * sw[j][e], bias[j][e]);
+      if constexpr (sizeof(OUT) == 4) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const int col = wn + j * 16 + cg * 4;
+          __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(hdet_u4v, v[j]), rc, row_ok && t.n0 + col < g.n ? (uint32_t)((tr * (int)g.y_ld + col) * 4) : kAbsent, 0, 0);
+        }
+      } else {
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+          const int col = wn + u * 32 + cg * 8;
+          const hdet_u4v o = {hdet_bf16_pack(v[2 * u][0], v[2 * u][1]), hdet_bf16_pack(v[2 * u][2], v[2 * u][3]),
+                              hdet_bf16_pack(v[2 * u + 1][0], v[2 * u + 1][1]), hdet_bf16_pack(v[2 * u + 1][2], v[2 * u + 1][3])};
+          __builtin_amdgcn_raw_buffer_store_b128(o, rc, row_ok && t.n0 + col < g.n ? (uint32_t)((tr * (int)g.y_ld + col) * 2) : kAbsent, 0, 0);
+        }
+      }
+    }
+  };
+
+  unsigned t = blockIdx.x;
+  tile cur = tile_at(t);
+  int slot = 0;
+  load_side(cur, 0);
+  load_a(cur.ra, 0, 0, 0); load_b(cur.rb, 0, 0); load_a(cur.ra, 1, 0, 0);
+  load_a(cur.ra, 0, 1, 1); load_b(cur.rb, 1, 1);
+  wait_and_barrier<8>();
+  if (wave >= 4) meet();
+  for (bool begun = false;; begun = true) {
+    tile nxt;
+    asm volatile("" : "+v"(off_a), "+v"(off_b));
+    auto pair = [&](int kt0, bool first) {
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        const int kt = kt0 + s;
+        const bool fs = first && s == 0;
+        auto wait = [&] {
+          if (fs && begun) wait_and_barrier<8 + kStores>();
+          else wait_and_barrier<8>();
+        };
+        read_a(0, s);
+        read_b(s);
+        if (first || kt + 1 < nk) load_a(cur.ra, 1, s ^ 1, kt + 1); else load_a(nxt.ra, 1, s ^ 1, 0);
+        wait();
+        multiply(0, fs);
+        meet();
+        read_a(1, s);
+        if (first || kt + 2 < nk) { load_a(cur.ra, 0, s, kt + 2); load_b(cur.rb, s, kt + 2); }
+        else { load_a(nxt.ra, 0, s, kt + 2 - nk); load_b(nxt.rb, s, kt + 2 - nk); }
+        if (first && s == 0) {
+          t += gridDim.x;
+          nxt = tile_at(t);
+        }
+        if (first && s == 1) load_side(nxt, slot ^ 1);
+        wait();
+        multiply(1, fs);
+        if (s == 0) meet();
+      }
+    };
+    pair(0, true);
+    for (int kt0 = 2; kt0 < nk; kt0 += 2) { meet(); pair(kt0, false); }
+    // the first group ends its tile under the second's last products, the second at once
+    if (wave < 4) meet();
+    finish(cur, slot);
+    if (wave >= 4) meet();
+    if (t >= total) break;
+    cur = nxt;
+    slot ^= 1;
+  }
+  if (wave < 4) meet();
+  wait_and_barrier<0>();
+}
+
 // Up to 64 rows: MB blocks of 16.  The weights' stream is the work: a block takes 16 columns of y, its four wavefronts a quarter of k each, with fragments
 // straight from global memory (16 rows of the weights, 64 bytes of each, an instruction) and no barrier in the loop; whole-number partial sums are added through LDS.
 template <typename OUT, int MB>
@@ -158,8 +364,6 @@ __global__ __launch_bounds__(256) void hdet_codes_rows_kernel(const codes_args g
   __shared__ i4v part[4][MB][64];
   const int z = blockIdx.z, n0 = blockIdx.x * 16, m0 = blockIdx.y * (16 * MB), lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const hdet_rsrc unused = {0, 0, 0, 0};
-  (void)unused;
   const auto ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(g.x + z * g.x_z + (int64_t)m0 * g.x_ld), 0, (int)extent(g.m, m0, g.x_ld, g.kbytes), 0x00020000);
   const auto rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(g.w + z * g.w_z + (int64_t)n0 * g.w_ld), 0, (int)extent(g.n, n0, g.w_ld, g.kbytes), 0x00020000);
   const int nk = (g.kbytes + 63) / 64, k0 = wave * nk / 4, k1 = (wave + 1) * nk / 4;
@@ -209,6 +413,14 @@ hipError_t launch_typed(const codes_args& g, int n_replicas, hipStream_t s) {
     else if (g.m <= 32) hipLaunchKernelGGL((hdet_codes_rows_kernel<OUT, 2>), grid, dim3(256), 0, s, g);
     else hipLaunchKernelGGL((hdet_codes_rows_kernel<OUT, 4>), grid, dim3(256), 0, s, g);
     return hipGetLastError();
+  }
+  const bool v8 = (reinterpret_cast<uintptr_t>(g.y) & 15) == 0 && ((g.n | g.y_ld | g.y_z) & (size == 2 ? 7 : 3)) == 0;
+  if (v8 && g.y_ld < (1 << 20)) {
+    const unsigned gx = (g.n + 255) / 256, gy = (g.m + 255) / 256, total = gx * gy * (unsigned)n_replicas, cus = (unsigned)hdet_compute_units();
+    if (total >= cus) {
+      hipLaunchKernelGGL(hdet_codes_walk_kernel<OUT>, dim3(total < cus ? total : cus), dim3(512), 0, s, g, gx, gy, total, tile_group_of(gx));
+      return hipGetLastError();
+    }
   }
   const dim3 grid((g.n + 127) / 128, (g.m + 127) / 128, n_replicas);
   if (v4) hipLaunchKernelGGL((hdet_codes_gemm_kernel<OUT, true, 128, 128, 2, 2, 2>), grid, dim3(256), 0, s, g);

@@ -23,7 +23,7 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr double kLn2 = 0.6931471805599453, kLog2eD = 1.4426950408889634;
 constexpr int kRowChunk = 128;                          // rows of a block's column sums
-constexpr size_t kPieceBytes = (size_t)256 << 20;       // dz of a piece, where the caller does not say
+constexpr size_t kPieceBytes = (size_t)1 << 30;         // most that dz of a piece takes where the caller does not say
 
 // Memory of a call, in the order it is carved.  What a member names: [replica][...].
 struct vocab_layout {
@@ -36,21 +36,40 @@ struct vocab_layout {
 size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
 int64_t up8(int64_t x) { return (x + 7) & ~(int64_t)7; }
 
+// Classes at a time.  A piece's dW is one product with the rows as its contraction: it wants whole rounds of 256 x 256 tiles over the compute units, and every piece costs
+// about a twelfth of a round in launches, first loads and passes over the sum of dh.  us, by classes a piece (rounds of each):
+//   8 x 4096 rows of 512, 32000 classes, bf16 dW: 1536 (3/8) 4876, 2048 (1/2) 4484, 4096 (1) 4161, 6400 (1.6) 4110, 8192 (2) 4028, 16384 (4) 3947, 32000 3860
+//   4 x 8192 rows of 1024, 32000 classes, fp32 dW: 2048 (1/2) 12739, 4096 (1) 10972, 6400 (1.6) 11420, 8192 (2) 10720, 32000 10439
+//   4096 rows of 1024, 50000 classes, bf16: 2048 (1/8) 2689, 4096 (1/4) 1883, 8192 (1/2) 1697, 16384 (1) 1550, 32000 (2) 1558, 50000 1684
+// Between the two stands kPieceBytes.
+int chosen_piece(int n, size_t class_bytes, int width, int classes) {
+  const int64_t tiles = (int64_t)((width + 255) / 256) * n, cus = hdet_compute_units(), columns = (classes + 255) / 256;
+  int64_t most = (int64_t)(kPieceBytes / class_bytes) / 256;      // columns of tiles that fit
+  if (most < 4) most = 4;
+  if (most >= columns) most = columns;
+  int64_t best = most;
+  double least = 1e30;
+  for (int64_t pieces = (columns + most - 1) / most; pieces <= columns && pieces <= 4 * ((columns + most - 1) / most) + 4; ++pieces) {
+    const int64_t c = (columns + pieces - 1) / pieces, count = (columns + c - 1) / c;
+    const double time = (double)count * ((double)((c * tiles + cus - 1) / cus) + 0.08);
+    if (time < least) { least = time; best = c; }
+  }
+  return best >= columns ? classes : (int)best * 256;
+}
+
 vocab_layout layout_of(int n, int64_t rows, int width, int classes, int dw_dtype, int piece) {
   vocab_layout l;
   l.planes = dw_dtype == HDET_TYPE_F32 ? 3 : 1;
   const size_t all = (size_t)n * (rows > 0 ? rows : 1);
-  size_t most = piece > 0 ? (size_t)piece : kPieceBytes / (all * 2 * l.planes);
-  if (piece <= 0 && most < 1024) most = 1024;
-  if (most > (size_t)classes) most = classes;
-  l.pieces = (int)((classes + most - 1) / most);
-  l.piece = (int)most;
-  if (l.pieces > 1) {
-    // pieces of one size, whole tiles of 256 classes, or whole groups of 8 where the caller wants fewer
-    if (piece <= 0) l.piece = (classes + l.pieces - 1) / l.pieces;
-    l.piece = piece <= 0 ? (l.piece + 255) / 256 * 256 : l.piece >= 256 ? l.piece / 256 * 256 : l.piece >= 8 ? l.piece / 8 * 8 : 8;
-    l.pieces = (classes + l.piece - 1) / l.piece;
+  if (piece <= 0) {
+    piece = chosen_piece(n, all * 2 * l.planes, width, classes);
+  } else {      // whole tiles of 256 classes, or whole groups of 8 where the caller wants fewer
+    if (piece > classes) piece = classes;
+    if (piece < classes) piece = piece >= 256 ? piece / 256 * 256 : piece >= 8 ? piece / 8 * 8 : 8;
+    if (piece > classes) piece = classes;
   }
+  l.piece = piece;
+  l.pieces = (classes + piece - 1) / piece;
   size_t room = all * up8(l.piece) * 2 * l.planes;                                  // dz
   const size_t a_class = all * (4 + 2 * l.planes), small = (size_t)64 << 20;        // z and dz
   const size_t whole = a_class * up8(l.piece);

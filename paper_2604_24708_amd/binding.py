@@ -159,7 +159,10 @@ def load_library(path: Optional[str] = None):
     # One HIP runtime per process: PyTorch ships its own libamdhip64 and must be the one that
     # libhdet.so binds to, or the library and the tensors it is handed would live in two
     # runtimes (the second one finds no device).  Importing torch first loads that copy.
-    import torch  # noqa: F401
+    import torch
+    global _F32, _BF16, _I8, _I32, _CODE
+    _F32, _BF16, _I8, _I32 = torch.float32, torch.bfloat16, torch.int8, torch.int32
+    _CODE = {_F32: HDET_TYPE_F32, _BF16: HDET_TYPE_BF16}
     lib = C.CDLL(p)
     vp = C.c_void_p
     lib.hdet_workspace_bytes.argtypes = [C.POINTER(hdet_config), C.c_int64, C.POINTER(C.c_size_t),
@@ -342,74 +345,79 @@ def hdet_destroy(h):
 # between rows and replicas); vectors a replica are [N, columns]; row scalars [N, rows] are contiguous.  `stream`: a hipStream_t as
 # an integer, None for the default stream.  Tensors are borrowed until the work on that stream is done.
 # ---------------------------------------------------------------------------------------
-def _dtype_code(t) -> int:
-    import torch
-    if t.dtype == torch.float32:
-        return HDET_TYPE_F32
-    if t.dtype == torch.bfloat16:
-        return HDET_TYPE_BF16
-    raise ValueError(f"dtype {t.dtype}: float32 or bfloat16 is wanted")
+_F32 = _BF16 = _I8 = _I32 = _CODE = None       # torch's types, from load_library on
 
 
-def _need(name, t, shape, dtype, contiguous=False):
-    """The tensor t, refused unless it has this shape and type, lies on a GPU, and has its last dimension's elements next to each other."""
+def _refuse(name, t, shape, dtype, contiguous=False):
+    """Says what is wrong with a tensor that is not of this shape and type, on a GPU, with the last dimension's elements next to each other."""
     if tuple(t.shape) != tuple(shape):
         raise ValueError(f"{name} has shape {tuple(t.shape)}, {tuple(shape)} is wanted")
     if t.dtype != dtype:
         raise ValueError(f"{name} is {t.dtype}, {dtype} is wanted")
-    if t.device.type != "cuda":
+    if not t.is_cuda:
         raise ValueError(f"{name} is on {t.device}: device memory is wanted")
-    if contiguous and not t.is_contiguous():
-        raise ValueError(f"{name} must be contiguous")
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
-        raise ValueError(f"{name}: the last dimension's elements must be next to each other")
-    return t
+    raise ValueError(f"{name} must be contiguous" if contiguous else f"{name}: the last dimension's elements must be next to each other")
 
 
-def _rows_of(name, t, shape, dtype) -> hdet_rows:
+def _dtype_code(name, t) -> int:
+    code = _CODE.get(t.dtype)
+    if code is None:
+        raise ValueError(f"{name} is {t.dtype}: float32 or bfloat16 is wanted")
+    return code
+
+
+# The helpers below return what a field of the C structures is made from: (pointer, row stride, replica stride) of a matrix, a pointer, or a
+# pointer and a stride.  (A call of a few microseconds notices every attribute that is asked twice.)
+_ABSENT = (None, 0, 0)
+
+
+def _rows_of(name, t, shape, dtype):
     if t is None:
-        return hdet_rows()
-    _need(name, t, shape, dtype)
-    return hdet_rows(t.data_ptr(), t.stride(1), t.stride(0))
+        return _ABSENT
+    s = t.stride()
+    if t.shape != shape or t.dtype is not dtype or not t.is_cuda or (s[2] != 1 and shape[2] > 1):
+        _refuse(name, t, shape, dtype)
+    return (t.data_ptr(), s[1], s[0])
 
 
-def _codes_of(name, t, shape) -> hdet_rows:
+def _codes_of(name, t, shape):
     """int8 codes; the strides of dimensions of size 1 say nothing and are made to fit."""
-    import torch
     if t is None:
-        return hdet_rows()
-    _need(name, t, shape, torch.int8)
-    wide = (shape[2] + 15) // 16 * 16
-    row = t.stride(1) if shape[1] > 1 else max(wide, t.stride(1) // 16 * 16)
-    rep = t.stride(0) if shape[0] > 1 else row * max(shape[1], 1)
-    end = t.storage_offset() + (shape[0] - 1) * rep + (shape[1] - 1) * t.stride(1) + wide
-    if shape[0] and shape[1] and end > t.untyped_storage().nbytes():
+        return _ABSENT
+    s = t.stride()
+    if t.shape != shape or t.dtype is not _I8 or not t.is_cuda or (s[2] != 1 and shape[2] > 1):
+        _refuse(name, t, shape, _I8)
+    n, rows, width = shape
+    wide = (width + 15) // 16 * 16
+    row = s[1] if rows > 1 else max(wide, s[1] // 16 * 16)
+    rep = s[0] if n > 1 else row * max(rows, 1)
+    if width % 16 and n and rows and t.storage_offset() + (n - 1) * rep + (rows - 1) * row + wide > t.untyped_storage().nbytes():
         raise ValueError(f"{name}: rows of codes end with zeros up to a multiple of 16 columns, which this tensor's memory does not hold")
-    return hdet_rows(t.data_ptr(), row, rep)
+    return (t.data_ptr(), row, rep)
 
 
 def _vector(name, t, shape):
-    """(pointer, stride) of fp32 vectors [N, columns]"""
-    import torch
+    """fp32 vectors [N, columns]"""
     if t is None:
         return None, 0
-    _need(name, t, shape, torch.float32)
-    return t.data_ptr(), t.stride(0) if shape[0] > 1 else max(t.stride(0), shape[1])
+    s = t.stride()
+    if t.shape != shape or t.dtype is not _F32 or not t.is_cuda or (s[1] != 1 and shape[1] > 1):
+        _refuse(name, t, shape, _F32)
+    return t.data_ptr(), s[0] if shape[0] > 1 else max(s[0], shape[1])
 
 
 def _scalars(name, t, shape, dtype=None):
-    """pointer of contiguous row scalars"""
-    import torch
-    return None if t is None else _need(name, t, shape, dtype or torch.float32, contiguous=True).data_ptr()
+    """contiguous row scalars"""
+    if t is None:
+        return None
+    dtype = dtype or _F32
+    if t.shape != shape or t.dtype is not dtype or not t.is_cuda or not t.is_contiguous():
+        _refuse(name, t, shape, dtype, contiguous=True)
+    return t.data_ptr()
 
 
-def _call(name, args, stream):
-    _check(getattr(load_library(), name)(C.byref(args), stream))
-
-
-def _workspace(args, t):
-    if t is not None:
-        args.workspace_dev, args.workspace_bytes = t.data_ptr(), t.numel() * t.element_size()
+def _work_of(t):
+    return (None, 0) if t is None else (t.data_ptr(), t.numel() * t.element_size())
 
 
 def _size_of(name, *args) -> int:
@@ -426,13 +434,15 @@ def hdet_codes_empty(n_replicas: int, rows: int, width: int, device="cuda"):
 
 def hdet_rmsnorm(x, gain, resid=None, total=None, y=None, codes=None, scale=None, rstd=None, eps: float = 1e-5, stream: Optional[int] = None):
     """total = x + resid; y = total / rms(total) * gain; codes and scale: y in 8 bits; rstd = 1 / rms.  Writes those of the four that are given."""
-    n, rows, width = x.shape
-    a = hdet_norm_args(n_replicas=n, dtype=_dtype_code(x), rows=rows, width=width, eps=eps)
-    a.x, a.resid = _rows_of("x", x, x.shape, x.dtype), _rows_of("resid", resid, x.shape, x.dtype)
-    a.total, a.y, a.codes = _rows_of("total", total, x.shape, x.dtype), _rows_of("y", y, x.shape, x.dtype), _codes_of("codes", codes, x.shape)
-    a.scale_dev, a.rstd_dev = _scalars("scale", scale, (n, rows)), _scalars("rstd", rstd, (n, rows))
-    a.gain_dev, a.gain_stride = _vector("gain", gain, (n, width))
-    _call("hdet_rmsnorm", a, stream)
+    lib = _lib or load_library()
+    shape, dt = x.shape, x.dtype
+    n, rows, width = shape
+    a = hdet_norm_args(n, _dtype_code("x", x), rows, width, 0, eps, _rows_of("x", x, shape, dt), _rows_of("resid", resid, shape, dt),
+                       _rows_of("total", total, shape, dt), _rows_of("y", y, shape, dt), _codes_of("codes", codes, shape),
+                       _scalars("scale", scale, (n, rows)), _scalars("rstd", rstd, (n, rows)), *_vector("gain", gain, (n, width)))
+    rc = lib.hdet_rmsnorm(C.byref(a), stream)
+    if rc:
+        _check(rc)
 
 
 def hdet_rmsnorm_backward_workspace(n_replicas: int, rows: int, width: int) -> int:
@@ -441,44 +451,52 @@ def hdet_rmsnorm_backward_workspace(n_replicas: int, rows: int, width: int) -> i
 
 def hdet_rmsnorm_backward(total, gain, rstd, dy, dx, dtotal=None, dgain=None, workspace=None, stream: Optional[int] = None):
     """dx (of x and of resid) and dgain from the gradients at y (dy) and at total (dtotal)."""
-    n, rows, width = total.shape
-    a = hdet_norm_grad_args(n_replicas=n, dtype=_dtype_code(total), rows=rows, width=width)
-    a.total, a.dy = _rows_of("total", total, total.shape, total.dtype), _rows_of("dy", dy, total.shape, total.dtype)
-    a.dtotal, a.dx = _rows_of("dtotal", dtotal, total.shape, total.dtype), _rows_of("dx", dx, total.shape, total.dtype)
-    a.rstd_dev = _scalars("rstd", rstd, (n, rows))
-    a.gain_dev, a.gain_stride = _vector("gain", gain, (n, width))
-    a.dgain_dev, a.dgain_stride = _vector("dgain", dgain, (n, width))
-    _workspace(a, workspace)
-    _call("hdet_rmsnorm_backward", a, stream)
+    lib = _lib or load_library()
+    shape, dt = total.shape, total.dtype
+    n, rows, width = shape
+    a = hdet_norm_grad_args(n, _dtype_code("total", total), rows, width, 0, _rows_of("total", total, shape, dt), _rows_of("dy", dy, shape, dt),
+                            _rows_of("dtotal", dtotal, shape, dt), _rows_of("dx", dx, shape, dt), _scalars("rstd", rstd, (n, rows)),
+                            *_vector("gain", gain, (n, width)), *_vector("dgain", dgain, (n, width)), *_work_of(workspace))
+    rc = lib.hdet_rmsnorm_backward(C.byref(a), stream)
+    if rc:
+        _check(rc)
 
 
-def _codes_call(name, values, codes, scale, stream):
-    n, rows, width = values.shape
-    a = hdet_codes_args(n_replicas=n, dtype=_dtype_code(values), rows=rows, width=width, scale_dev=_scalars("scale", scale, (n, rows)))
-    a.values, a.codes = _rows_of("values", values, values.shape, values.dtype), _codes_of("codes", codes, values.shape)
-    _call(name, a, stream)
+def _codes_args(values, codes, scale):
+    shape = values.shape
+    n, rows, width = shape
+    return C.byref(hdet_codes_args(n, _dtype_code("values", values), rows, width, 0, _rows_of("values", values, shape, values.dtype),
+                                   _codes_of("codes", codes, shape), _scalars("scale", scale, (n, rows))))
 
 
 def hdet_quantise_rows(values, codes, scale, stream: Optional[int] = None):
     """codes, scale <- values, a power of two as each row's scale."""
-    _codes_call("hdet_quantise_rows", values, codes, scale, stream)
+    lib = _lib or load_library()
+    rc = lib.hdet_quantise_rows(_codes_args(values, codes, scale), stream)
+    if rc:
+        _check(rc)
 
 
 def hdet_restore_rows(codes, scale, values, stream: Optional[int] = None):
     """values <- codes * scale."""
-    _codes_call("hdet_restore_rows", values, codes, scale, stream)
+    lib = _lib or load_library()
+    rc = lib.hdet_restore_rows(_codes_args(values, codes, scale), stream)
+    if rc:
+        _check(rc)
 
 
 def hdet_quantised_linear(codes, scale, w_codes, w_scale, y, bias=None, stream: Optional[int] = None):
     """y [N, rows, d_out] <- (codes * scale) (w_codes * w_scale)^T + bias."""
-    n, rows, d_in = codes.shape
+    lib = _lib or load_library()
+    shape = codes.shape
+    n, rows, d_in = shape
     d_out = w_codes.shape[1]
-    a = hdet_linear_args(n_replicas=n, y_dtype=_dtype_code(y), rows=rows, d_in=d_in, d_out=d_out)
-    a.codes, a.w_codes = _codes_of("codes", codes, codes.shape), _codes_of("w_codes", w_codes, (n, d_out, d_in))
-    a.scale_dev, a.w_scale_dev = _scalars("scale", scale, (n, rows)), _scalars("w_scale", w_scale, (n, d_out))
-    a.bias_dev, a.bias_stride = _vector("bias", bias, (n, d_out))
-    a.y = _rows_of("y", y, (n, rows, d_out), y.dtype)
-    _call("hdet_quantised_linear", a, stream)
+    a = hdet_linear_args(n, _dtype_code("y", y), rows, d_in, d_out, _codes_of("codes", codes, shape), _codes_of("w_codes", w_codes, (n, d_out, d_in)),
+                         _scalars("scale", scale, (n, rows)), _scalars("w_scale", w_scale, (n, d_out)), *_vector("bias", bias, (n, d_out)),
+                         _rows_of("y", y, (n, rows, d_out), y.dtype))
+    rc = lib.hdet_quantised_linear(C.byref(a), stream)
+    if rc:
+        _check(rc)
 
 
 def hdet_quantised_linear_backward_workspace(n_replicas: int, rows: int, d_in: int, d_out: int) -> int:
@@ -487,40 +505,37 @@ def hdet_quantised_linear_backward_workspace(n_replicas: int, rows: int, d_in: i
 
 def hdet_quantised_linear_backward(dy, codes, scale, w_codes, w_scale, dx=None, dw=None, db=None, workspace=None, stream: Optional[int] = None):
     """dx = dy W (bfloat16), dw = dy^T X (fp32), db = the rows' sum of dy (fp32), from the 8-bit copies; those that are given."""
-    import torch
-    n, rows, d_out = dy.shape
+    lib = _lib or load_library()
+    shape = dy.shape
+    n, rows, d_out = shape
     d_in = codes.shape[2]
-    a = hdet_linear_grad_args(n_replicas=n, rows=rows, d_in=d_in, d_out=d_out)
-    a.dy = _rows_of("dy", dy, dy.shape, torch.bfloat16)
-    a.codes, a.w_codes = _codes_of("codes", codes, (n, rows, d_in)), _codes_of("w_codes", w_codes, (n, d_out, d_in))
-    a.scale_dev, a.w_scale_dev = _scalars("scale", scale, (n, rows)), _scalars("w_scale", w_scale, (n, d_out))
-    a.dx, a.dw = _rows_of("dx", dx, (n, rows, d_in), torch.bfloat16), _rows_of("dw", dw, (n, d_out, d_in), torch.float32)
-    a.db_dev, a.db_stride = _vector("db", db, (n, d_out))
-    _workspace(a, workspace)
-    _call("hdet_quantised_linear_backward", a, stream)
+    a = hdet_linear_grad_args(n, 0, rows, d_in, d_out, _rows_of("dy", dy, shape, _BF16), _codes_of("codes", codes, (n, rows, d_in)),
+                              _codes_of("w_codes", w_codes, (n, d_out, d_in)), _scalars("scale", scale, (n, rows)), _scalars("w_scale", w_scale, (n, d_out)),
+                              _rows_of("dx", dx, (n, rows, d_in), _BF16), _rows_of("dw", dw, (n, d_out, d_in), _F32),
+                              *_vector("db", db, (n, d_out)), *_work_of(workspace))
+    rc = lib.hdet_quantised_linear_backward(C.byref(a), stream)
+    if rc:
+        _check(rc)
 
 
 def hdet_vocab_loss_workspace(n_replicas: int, rows: int, width: int, classes: int, dw=None, piece: int = 0) -> int:
     """`dw`: the dtype of the weight gradient (float32 if None)."""
-    import torch
-    return _size_of("hdet_vocab_loss_workspace", n_replicas, rows, width, classes, HDET_TYPE_BF16 if dw == torch.bfloat16 else HDET_TYPE_F32, piece)
+    load_library()
+    return _size_of("hdet_vocab_loss_workspace", n_replicas, rows, width, classes, HDET_TYPE_BF16 if dw == _BF16 else HDET_TYPE_F32, piece)
 
 
 def hdet_vocab_loss(h, w, labels, row_loss, mean_loss, dh=None, dw=None, bias=None, db=None, piece: int = 0, workspace=None,
                     stream: Optional[int] = None):
     """Cross-entropy of softmax(h w^T + bias) at `labels` (int32 [N, rows]; rows whose label is no class do not count), and its gradients."""
-    import torch
-    n, rows, width = h.shape
+    lib = _lib or load_library()
+    shape = h.shape
+    n, rows, width = shape
     classes = w.shape[1]
-    a = hdet_vocab_args(n_replicas=n, rows=rows, width=width, classes=classes, piece=piece)
-    a.h, a.w = _rows_of("h", h, h.shape, torch.bfloat16), _rows_of("w", w, (n, classes, width), torch.bfloat16)
-    a.bias_dev, a.bias_stride = _vector("bias", bias, (n, classes))
-    a.labels_dev = _scalars("labels", labels, (n, rows), torch.int32)
-    a.row_loss_dev, a.mean_loss_dev = _scalars("row_loss", row_loss, (n, rows)), _scalars("mean_loss", mean_loss, (n,))
-    a.dh = _rows_of("dh", dh, h.shape, torch.bfloat16)
-    if dw is not None:
-        a.dw_dtype = _dtype_code(dw)
-        a.dw = _rows_of("dw", dw, (n, classes, width), dw.dtype)
-    a.db_dev, a.db_stride = _vector("db", db, (n, classes))
-    _workspace(a, workspace)
-    _call("hdet_vocab_loss", a, stream)
+    wide = (n, classes, width)
+    a = hdet_vocab_args(n, 0 if dw is None else _dtype_code("dw", dw), rows, width, classes, piece, 0, _rows_of("h", h, shape, _BF16),
+                        _rows_of("w", w, wide, _BF16), *_vector("bias", bias, (n, classes)), _scalars("labels", labels, (n, rows), _I32),
+                        _scalars("row_loss", row_loss, (n, rows)), _scalars("mean_loss", mean_loss, (n,)), _rows_of("dh", dh, shape, _BF16),
+                        _ABSENT if dw is None else _rows_of("dw", dw, wide, dw.dtype), *_vector("db", db, (n, classes)), *_work_of(workspace))
+    rc = lib.hdet_vocab_loss(C.byref(a), stream)
+    if rc:
+        _check(rc)

@@ -33,14 +33,14 @@ __device__ __forceinline__ uint32_t extent(int rows, int row0, int64_t ld, int k
 }
 __device__ __forceinline__ int swz(int r) { return (r >> 1) & 7; }
 
-// Four consecutive results of one row.  V4: rows of y are whole groups of four, 16 (8) bytes aligned.
-template <typename OUT, bool V4>
+// Four consecutive results of one row, at any element
+typedef f4 f4_any __attribute__((aligned(4)));
+typedef hdet_u2v hdet_u2v_any __attribute__((aligned(2)));
+template <typename OUT>
 __device__ __forceinline__ void put4(OUT* y, int col, int n, f4 v) {
-  if constexpr (V4) {
-    if (col < n) {
-      if constexpr (sizeof(OUT) == 4) *reinterpret_cast<f4*>(y + col) = v;
-      else *reinterpret_cast<hdet_u2v*>(y + col) = hdet_u2v{hdet_bf16_pack(v[0], v[1]), hdet_bf16_pack(v[2], v[3])};
-    }
+  if (col + 4 <= n) {
+    if constexpr (sizeof(OUT) == 4) *reinterpret_cast<f4_any*>(y + col) = v;
+    else *reinterpret_cast<hdet_u2v_any*>(y + col) = hdet_u2v{hdet_bf16_pack(v[0], v[1]), hdet_bf16_pack(v[2], v[3])};
   } else {
 #pragma unroll
     for (int e = 0; e < 4; ++e)
@@ -50,7 +50,7 @@ __device__ __forceinline__ void put4(OUT* y, int col, int n, f4 v) {
 
 }  // namespace
 
-template <typename OUT, bool V4, int TM, int TN, int WGM, int WGN, int NST>
+template <typename OUT, int TM, int TN, int WGM, int WGN, int NST>
 __global__ __launch_bounds__(64 * WGM * WGN, 160 * 1024 / (NST * (TM + TN) * 128) * (WGM * WGN / 4))
 void hdet_codes_gemm_kernel(const codes_args g) {
   constexpr int THREADS = 64 * WGM * WGN, MB = TM / WGM / 16, NB = TN / WGN / 16;
@@ -145,7 +145,7 @@ void hdet_codes_gemm_kernel(const codes_args g) {
       f4 v;
 #pragma unroll
       for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf((float)acc[i][j][e], sx[i] * sw[e], b[e]);
-      if (row < g.m) put4<OUT, V4>((OUT*)g.y + z * g.y_z + (int64_t)row * g.y_ld, col, g.n, v);
+      if (row < g.m) put4<OUT>((OUT*)g.y + z * g.y_z + (int64_t)row * g.y_ld, col, g.n, v);
     }
   }
 }
@@ -357,48 +357,47 @@ __global__ __launch_bounds__(512, 2) void hdet_codes_walk_kernel(const codes_arg
   wait_and_barrier<0>();
 }
 
-// Up to 64 rows: MB blocks of 16.  The weights' stream is the work: a block takes 16 columns of y, its four wavefronts a quarter of k each, with fragments
-// straight from global memory (16 rows of the weights, 64 bytes of each, an instruction) and no barrier in the loop; whole-number partial sums are added through LDS.
-template <typename OUT, int MB>
+// Up to 16 rows.  The weights' stream is the work: a block takes 16 columns of y, its four wavefronts a quarter of k each, with fragments straight from global
+// memory (16 rows of the weights, 64 bytes of each, an instruction) and no barrier in the loop; whole-number partial sums are added through LDS.
+template <typename OUT>
 __global__ __launch_bounds__(256) void hdet_codes_rows_kernel(const codes_args g) {
-  __shared__ i4v part[4][MB][64];
-  const int z = blockIdx.z, n0 = blockIdx.x * 16, m0 = blockIdx.y * (16 * MB), lane = threadIdx.x & 63;
+  __shared__ i4v part[4][64];
+  const int z = blockIdx.z, n0 = blockIdx.x * 16, lane = threadIdx.x & 63;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const auto ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(g.x + z * g.x_z + (int64_t)m0 * g.x_ld), 0, (int)extent(g.m, m0, g.x_ld, g.kbytes), 0x00020000);
+  const auto ra = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(g.x + z * g.x_z), 0, (int)extent(g.m, 0, g.x_ld, g.kbytes), 0x00020000);
   const auto rb = __builtin_amdgcn_make_buffer_rsrc(const_cast<int8_t*>(g.w + z * g.w_z + (int64_t)n0 * g.w_ld), 0, (int)extent(g.n, n0, g.w_ld, g.kbytes), 0x00020000);
   const int nk = (g.kbytes + 63) / 64, k0 = wave * nk / 4, k1 = (wave + 1) * nk / 4;
   const int r = lane & 15, kc = (lane >> 4) * 16;
-  i4v acc[MB];
+  const int col = n0 + (lane >> 4) * 4;
+  // what the end needs is requested before the loop
+  float sx = 0.f;
+  f4 sw = {0.f, 0.f, 0.f, 0.f}, b = {0.f, 0.f, 0.f, 0.f};
+  if (wave == 0) {
+    if (r < g.m) sx = g.x_scale[(int64_t)z * g.m + r];
 #pragma unroll
-  for (int i = 0; i < MB; ++i) acc[i] = i4v{0, 0, 0, 0};
-#pragma unroll 4
+    for (int e = 0; e < 4; ++e)
+      if (col + e < g.n) {
+        sw[e] = g.w_scale[(int64_t)z * g.n + col + e];
+        if (g.bias) b[e] = g.bias[z * g.bias_z + col + e];
+      }
+  }
+  i4v acc = {0, 0, 0, 0};
+#pragma unroll 8
   for (int k = k0; k < k1; ++k) {
     const int at = k * 64 + kc;
     const bool ok = at < g.kbytes;
-    const i4v b = __builtin_bit_cast(i4v, __builtin_amdgcn_raw_buffer_load_b128(rb, ok ? (int)(r * g.w_ld) + at : (int)kAbsent, 0, 0));
-#pragma unroll
-    for (int i = 0; i < MB; ++i) {
-      const i4v a = __builtin_bit_cast(i4v, __builtin_amdgcn_raw_buffer_load_b128(ra, ok ? (int)((i * 16 + r) * g.x_ld) + at : (int)kAbsent, 0, 0));
-      acc[i] = __builtin_amdgcn_mfma_i32_16x16x64_i8(b, a, acc[i], 0, 0, 0);
-    }
+    const i4v w = __builtin_bit_cast(i4v, __builtin_amdgcn_raw_buffer_load_b128(rb, ok ? (int)(r * g.w_ld) + at : (int)kAbsent, 0, 0));
+    const i4v x = __builtin_bit_cast(i4v, __builtin_amdgcn_raw_buffer_load_b128(ra, ok ? (int)(r * g.x_ld) + at : (int)kAbsent, 0, 0));
+    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(w, x, acc, 0, 0, 0);
   }
-#pragma unroll
-  for (int i = 0; i < MB; ++i) part[wave][i][lane] = acc[i];
+  if (wave != 0) part[wave][lane] = acc;
   __syncthreads();
-  const int col = n0 + (lane >> 4) * 4;
-  for (int i = wave; i < MB; i += 4) {
-    const int row = m0 + i * 16 + r;
-    if (row >= g.m) continue;
-    const i4v s = part[0][i][lane] + part[1][i][lane] + part[2][i][lane] + part[3][i][lane];
-    const float sx = g.x_scale[(int64_t)z * g.m + row];
-    f4 v;
+  if (wave != 0 || r >= g.m) return;
+  acc += part[1][lane] + part[2][lane] + part[3][lane];
+  f4 v;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const bool ok = col + e < g.n;
-      v[e] = __builtin_fmaf((float)s[e], ok ? sx * g.w_scale[(int64_t)z * g.n + col + e] : 0.f, ok && g.bias ? g.bias[z * g.bias_z + col + e] : 0.f);
-    }
-    put4<OUT, false>((OUT*)g.y + z * g.y_z + (int64_t)row * g.y_ld, col, g.n, v);
-  }
+  for (int e = 0; e < 4; ++e) v[e] = __builtin_fmaf((float)acc[e], sx * sw[e], b[e]);
+  put4<OUT>((OUT*)g.y + z * g.y_z + (int64_t)r * g.y_ld, col, g.n, v);
 }
 
 namespace {
@@ -406,12 +405,9 @@ namespace {
 template <typename OUT>
 hipError_t launch_typed(const codes_args& g, int n_replicas, hipStream_t s) {
   const int size = sizeof(OUT);
-  const bool v4 = (reinterpret_cast<uintptr_t>(g.y) & (4 * size - 1)) == 0 && ((g.n | g.y_ld | g.y_z) & 3) == 0;
-  if (g.m <= 64) {
-    const dim3 grid((g.n + 15) / 16, 1, n_replicas);
-    if (g.m <= 16) hipLaunchKernelGGL((hdet_codes_rows_kernel<OUT, 1>), grid, dim3(256), 0, s, g);
-    else if (g.m <= 32) hipLaunchKernelGGL((hdet_codes_rows_kernel<OUT, 2>), grid, dim3(256), 0, s, g);
-    else hipLaunchKernelGGL((hdet_codes_rows_kernel<OUT, 4>), grid, dim3(256), 0, s, g);
+  // Up to 16 rows; beyond, the tiles' shorter chain counts for more than their empty rows (8 x 64 rows, 1024 -> 4096: 24 us in blocks of 16 columns, 13 in tiles)
+  if (g.m <= 16) {
+    hipLaunchKernelGGL(hdet_codes_rows_kernel<OUT>, dim3((g.n + 15) / 16, 1, n_replicas), dim3(256), 0, s, g);
     return hipGetLastError();
   }
   const bool v8 = (reinterpret_cast<uintptr_t>(g.y) & 15) == 0 && ((g.n | g.y_ld | g.y_z) & (size == 2 ? 7 : 3)) == 0;
@@ -423,8 +419,7 @@ hipError_t launch_typed(const codes_args& g, int n_replicas, hipStream_t s) {
     }
   }
   const dim3 grid((g.n + 127) / 128, (g.m + 127) / 128, n_replicas);
-  if (v4) hipLaunchKernelGGL((hdet_codes_gemm_kernel<OUT, true, 128, 128, 2, 2, 2>), grid, dim3(256), 0, s, g);
-  else hipLaunchKernelGGL((hdet_codes_gemm_kernel<OUT, false, 128, 128, 2, 2, 2>), grid, dim3(256), 0, s, g);
+  hipLaunchKernelGGL((hdet_codes_gemm_kernel<OUT, 128, 128, 2, 2, 2>), grid, dim3(256), 0, s, g);
   return hipGetLastError();
 }
 

@@ -5,8 +5,7 @@
 //
 // All of it is bound by memory: a row is read once, stays in registers between its sums and its results, and nothing but the results is
 // written.  L threads hold a row (8 .. 64: several rows to a wavefront or block, reductions by exchanges inside the wavefront; 256 and
-// 1024: a block to a row, one pass through LDS), each in C pieces of VEC elements: VEC = 8 where rows are whole 16-byte pieces at
-// 16-byte boundaries, else single elements.
+// 1024: a block to a row, one pass through LDS), each in C pieces of 8 elements.
 
 #include <type_traits>
 
@@ -15,28 +14,100 @@
 
 namespace {
 
-template <int VEC> struct piece_of { float v[VEC]; };
-template <int VEC, typename T>
-__device__ __forceinline__ piece_of<VEC> load_piece(const T* p) {
-  piece_of<VEC> r;
-  if constexpr (VEC == 8) {
-    const hdet_f8 x = hdet_ld8(p);
+// How a launch's rows lie: anywhere; in whole pieces of 8 elements at 16-byte boundaries; the same, and so much of it that what is written would push what is still to be read out of
+// the memory-side cache (256 MB): past the caches then.  us, through / past:  backward 8 x 8192 rows of 1024 119 / 101, 8 x 4096 of 512 26.5 / 29;  forward 84 / 78 and 22 / 26
+enum { kLoose = 0, kWhole = 1, kStream = 2 };
+
+// Eight neighbouring elements of a row of `width`, as they lie in memory; zeros behind the row's end.  Where rows are not whole pieces one lies at any
+// element, which the memory takes as it takes aligned ones but for the lines it crosses; the last piece of a row is loaded from 8 elements before the end and moved
+// into place, so that no lane waits for another's single elements (an odd row of 1001: 14.5 us of a launch that takes 9 so).
+typedef hdet_u4v hdet_u4v_any __attribute__((aligned(2)));
+typedef hdet_f4v hdet_f4v_any __attribute__((aligned(4)));
+template <typename T> struct piece;
+template <> struct piece<uint16_t> {
+  hdet_u4v w;
+  __device__ __forceinline__ void zero() { w = hdet_u4v{0u, 0u, 0u, 0u}; }
+  __device__ __forceinline__ float operator[](int e) const { return __uint_as_float(e & 1 ? w[e >> 1] & 0xffff0000u : w[e >> 1] << 16); }
+  template <int WHOLE> __device__ __forceinline__ void load(const uint16_t* p, int col, int width) {
+    if (WHOLE == kStream) {
+      w = __builtin_nontemporal_load(reinterpret_cast<const hdet_u4v*>(p + col));
+    } else if (WHOLE) {
+      w = *reinterpret_cast<const hdet_u4v*>(p + col);
+    } else if (width >= 8) {
+      const int back = col + 8 > width ? col + 8 - width : 0;
+      const hdet_u4v u = *reinterpret_cast<const hdet_u4v_any*>(p + col - back);
+      const int d = back >> 1;
+      unsigned x[5];
 #pragma unroll
-    for (int e = 0; e < 8; ++e) r.v[e] = x.v[e];
-  } else {
-    r.v[0] = hdet_ld(p);
+      for (int i = 0; i < 4; ++i) x[i] = d == 0 ? u[i] : d == 1 ? (i < 3 ? u[i + 1 & 3] : 0u) : d == 2 ? (i < 2 ? u[i + 2 & 3] : 0u) : (i < 1 ? u[3] : 0u);
+      x[4] = 0u;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) w[i] = back & 1 ? x[i] >> 16 | x[i + 1] << 16 : x[i];
+    } else {
+      zero();
+      for (int e = 0; e < width; ++e) w[e >> 1] |= (unsigned)p[e] << (16 * (e & 1));
+    }
   }
-  return r;
-}
-template <int VEC, typename T>
-__device__ __forceinline__ void store_piece(T* p, const float (&v)[VEC]) {
-  if constexpr (VEC == 8) {
-    hdet_f8 x;
+};
+template <> struct piece<float> {
+  hdet_f4v a, b;
+  __device__ __forceinline__ void zero() { a = b = hdet_f4v{0.f, 0.f, 0.f, 0.f}; }
+  __device__ __forceinline__ float operator[](int e) const { return e < 4 ? a[e & 3] : b[e & 3]; }
+  template <int WHOLE> __device__ __forceinline__ void load(const float* p, int col, int width) {
+    if (WHOLE == kStream) {
+      a = __builtin_nontemporal_load(reinterpret_cast<const hdet_f4v*>(p + col));
+      b = __builtin_nontemporal_load(reinterpret_cast<const hdet_f4v*>(p + col + 4));
+    } else if (WHOLE) {
+      a = *reinterpret_cast<const hdet_f4v*>(p + col);
+      b = *reinterpret_cast<const hdet_f4v*>(p + col + 4);
+    } else if (width >= 8) {
+      const int back = col + 8 > width ? col + 8 - width : 0;
+      const float* q = p + col - back;
+      const hdet_f4v u = *reinterpret_cast<const hdet_f4v_any*>(q), v = *reinterpret_cast<const hdet_f4v_any*>(q + 4);
+      float x[8] = {u[0], u[1], u[2], u[3], v[0], v[1], v[2], v[3]};
 #pragma unroll
-    for (int e = 0; e < 8; ++e) x.v[e] = v[e];
-    hdet_st8(p, x);
+      for (int h = 4; h > 0; h >>= 1)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] = back & h ? (e + h < 8 ? x[e + h < 8 ? e + h : 7] : 0.f) : x[e];
+      a = hdet_f4v{x[0], x[1], x[2], x[3]};
+      b = hdet_f4v{x[4], x[5], x[6], x[7]};
+    } else {
+      zero();
+#pragma unroll
+      for (int e = 0; e < 8; ++e)
+        if (e < width) (e < 4 ? a : b)[e & 3] = p[e];
+    }
+  }
+};
+template <int WHOLE>
+__device__ __forceinline__ void store_piece(uint16_t* p, const float (&v)[8], int left) {
+  if (WHOLE || left >= 8) {
+    hdet_u4v u;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) u[i] = hdet_bf16_pack(v[2 * i], v[2 * i + 1]);
+    if (WHOLE == kStream) __builtin_nontemporal_store(u, reinterpret_cast<hdet_u4v*>(p));
+    else if (WHOLE) *reinterpret_cast<hdet_u4v*>(p) = u;
+    else *reinterpret_cast<hdet_u4v_any*>(p) = u;
   } else {
-    hdet_st(p, v[0]);
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < left) hdet_st(p + e, v[e]);
+  }
+}
+template <int WHOLE>
+__device__ __forceinline__ void store_piece(float* p, const float (&v)[8], int left) {
+  if (WHOLE || left >= 8) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const hdet_f4v u = {v[4 * h], v[4 * h + 1], v[4 * h + 2], v[4 * h + 3]};
+      if (WHOLE == kStream) __builtin_nontemporal_store(u, reinterpret_cast<hdet_f4v*>(p + 4 * h));
+      else if (WHOLE) *reinterpret_cast<hdet_f4v*>(p + 4 * h) = u;
+      else *reinterpret_cast<hdet_f4v_any*>(p + 4 * h) = u;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e)
+      if (e < left) p[e] = v[e];
   }
 }
 
@@ -87,53 +158,52 @@ struct norm_kernel_args {
 
 // NORM: as above; otherwise y = x (rows to 8 bits).  Grid: (ceil(rows / rows a block), replicas).
 // (The row is in registers from its two loads to its two or three stores; what is left between the loads and the stores are the two reductions.)
-template <typename T, int VEC, int L, int C, bool NORM>
+template <typename T, int WHOLE, int L, int C, bool NORM>
 __global__ __launch_bounds__(L < 256 ? 256 : L) void hdet_norm_kernel(const norm_kernel_args a) {
   constexpr int THREADS = L < 256 ? 256 : L, RPB = THREADS / L;
   __shared__ unsigned buf[16];
   const int j = threadIdx.x % L, z = blockIdx.y;
   const int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / L;
   const bool here = row < a.rows;
-  float u[C][VEC];
+  float u[C][8];
   const T* x = (const T*)a.x + z * a.x_z + row * a.x_s;
   const T* r = (const T*)a.resid + z * a.r_z + row * a.r_s;
   float ss = 0.f;
+  piece<T> p[C], q[C];      // the two summands
+  piece<float> gain[C];
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    const int col = (c * L + j) * VEC;
+    const int col = (c * L + j) * 8;
+    p[c].zero();
+    q[c].zero();
     if (here && col < a.width) {
-      piece_of<VEC> p = load_piece<VEC>(x + col);
-      if (NORM && a.resid) {
-        const piece_of<VEC> q = load_piece<VEC>(r + col);
-#pragma unroll
-        for (int e = 0; e < VEC; ++e) p.v[e] += q.v[e];
-      }
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) u[c][e] = p.v[e];
-    } else {
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) u[c][e] = 0.f;
+      p[c].template load<WHOLE>(x, col, a.width);
+      if (NORM && a.resid) q[c].template load<WHOLE>(r, col, a.width);
+      if (NORM) gain[c].template load<kLoose>(a.gain + z * a.gain_z, col, a.width);
     }
   }
+#pragma unroll
+  for (int c = 0; c < C; ++c)
+#pragma unroll
+    for (int e = 0; e < 8; ++e) u[c][e] = NORM ? p[c][e] + q[c][e] : p[c][e];
   if constexpr (NORM) {
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) ss = __builtin_fmaf(u[c][e], u[c][e], ss);
+      for (int e = 0; e < 8; ++e) ss = __builtin_fmaf(u[c][e], u[c][e], ss);
     ss = row_sum_of<L>(ss, buf);
     const float rstd = 1.f / sqrtf(__builtin_fmaf(ss, a.inv_width, a.eps));
     if (a.rstd && here && j == 0) a.rstd[z * a.rows + row] = rstd;
     T* const total = (T*)a.total + z * a.t_z + row * a.t_s;
     T* const y = (T*)a.y + z * a.y_z + row * a.y_s;
-    const float* g = a.gain + z * a.gain_z;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const int col = (c * L + j) * VEC;
+      const int col = (c * L + j) * 8;
       if (here && col < a.width) {
-        if (a.total) store_piece<VEC>(total + col, u[c]);
+        if (a.total) store_piece<WHOLE>(total + col, u[c], a.width - col);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) u[c][e] = u[c][e] * rstd * g[col + e];
-        if (a.y) store_piece<VEC>(y + col, u[c]);
+        for (int e = 0; e < 8; ++e) u[c][e] = u[c][e] * rstd * gain[c][e];
+        if (a.y) store_piece<WHOLE>(y + col, u[c], a.width - col);
       }
     }
   }
@@ -142,23 +212,19 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void hdet_norm_kernel(const norm
 #pragma unroll
   for (int c = 0; c < C; ++c)
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) top = larger(top, __float_as_uint(u[c][e]) & 0x7fffffffu);
+    for (int e = 0; e < 8; ++e) top = larger(top, __float_as_uint(u[c][e]) & 0x7fffffffu);
   const row_scale sc = scale_of(over_row<L>(top, buf, larger));
   if (here && j == 0) a.scale[z * a.rows + row] = sc.scale;
-  int8_t* const q = a.codes + z * a.c_z + row * a.c_s;
+  int8_t* const to = a.codes + z * a.c_z + row * a.c_s;
   const int padded = (a.width + 15) & ~15;
 #pragma unroll
   for (int c = 0; c < C; ++c) {
-    const int col = (c * L + j) * VEC;
+    const int col = (c * L + j) * 8;
     if (here && col < padded) {                     // columns behind the last are 0 in u (a row of registers is a multiple of 16 long)
-      if constexpr (VEC == 8) {
-        unsigned w[2] = {0u, 0u};
+      unsigned w[2] = {0u, 0u};
 #pragma unroll
-        for (int e = 0; e < 8; ++e) w[e >> 2] |= ((unsigned)code_of(u[c][e], sc.inverse) & 255u) << (8 * (e & 3));
-        *reinterpret_cast<hdet_u2v*>(q + col) = hdet_u2v{w[0], w[1]};
-      } else {
-        q[col] = (int8_t)code_of(u[c][0], sc.inverse);
-      }
+      for (int e = 0; e < 8; ++e) w[e >> 2] |= ((unsigned)code_of(u[c][e], sc.inverse) & 255u) << (8 * (e & 3));
+      *reinterpret_cast<hdet_u2v*>(to + col) = hdet_u2v{w[0], w[1]};
     }
   }
 }
@@ -176,69 +242,82 @@ struct norm_grad_kernel_args {
 }  // namespace
 
 // Grid: (blocks, replicas); a block takes every gridDim.x-th group of rows and adds up its columns' dy xh on the way (the gain's gradient is then
-// `blocks` rows instead of all of them for a second launch).
-template <typename T, int VEC, int L, int C>
+// `blocks` rows instead of all of them for a second launch).  A row stays in registers as it lies in memory, and the next one's loads are in flight under it; the gain
+// is in LDS (in registers, with the row's products, there were four wavefronts a SIMD and no such loads: 8 x 8192 rows of 1024 119 us).
+template <typename T, int WHOLE, int L, int C>
 __global__ __launch_bounds__(L < 256 ? 256 : L) void hdet_norm_grad_kernel(const norm_grad_kernel_args a) {
-  constexpr int THREADS = L < 256 ? 256 : L, RPB = THREADS / L, COLS = L * VEC * C;
+  constexpr int THREADS = L < 256 ? 256 : L, RPB = THREADS / L, COLS = L * 8 * C;
+  constexpr bool kGainInLds = COLS <= 8192;
   __shared__ unsigned buf[16];
+  __shared__ __attribute__((aligned(16))) float s_gain[kGainInLds ? COLS : 1];
   __shared__ float sums[RPB > 1 ? RPB * COLS : 1];
   const int j = threadIdx.x % L, sub = threadIdx.x / L, z = blockIdx.y;
-  float g[C][VEC], acc[C][VEC];
+  const float* const gain = a.gain + z * a.gain_z;
+  float acc[C][8];
 #pragma unroll
   for (int c = 0; c < C; ++c)
 #pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-      const int col = (c * L + j) * VEC + e;
-      g[c][e] = col < a.width ? a.gain[z * a.gain_z + col] : 0.f;
-      acc[c][e] = 0.f;
-    }
-  for (int64_t base = (int64_t)blockIdx.x * RPB; base < a.rows; base += (int64_t)gridDim.x * RPB) {
-    const int64_t row = base + sub;
+    for (int e = 0; e < 8; ++e) acc[c][e] = 0.f;
+  const T *const h = (const T*)a.h + z * a.h_z, *const dy = (const T*)a.dy + z * a.dy_z, *const dt = (const T*)a.dt + z * a.dt_z;
+  auto gain_of = [&](int c, float (&g)[8]) {
+    const int col = (c * L + j) * 8;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) g[e] = kGainInLds ? s_gain[col + e] : col + e < a.width ? gain[col + e] : 0.f;
+  };
+  struct row_data { piece<T> h[C], dy[C], dt[C]; float rstd; };
+  auto fetch = [&](row_data& d, int64_t row) {
     const bool here = row < a.rows;
-    const T* h = (const T*)a.h + z * a.h_z + row * a.h_s;
-    const T* dy = (const T*)a.dy + z * a.dy_z + row * a.dy_s;
-    const T* dt = (const T*)a.dt + z * a.dt_z + row * a.dt_s;
-    const float rstd = here ? a.rstd[z * a.rows + row] : 0.f;
-    float xh[C][VEC], dn[C][VEC], add[C][VEC], dot = 0.f;
+    d.rstd = here ? a.rstd[z * a.rows + row] : 0.f;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const int col = (c * L + j) * VEC;
-      const bool ok = here && col < a.width;
-      piece_of<VEC> p, q, t;
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) p.v[e] = q.v[e] = t.v[e] = 0.f;
-      if (ok) {
-        p = load_piece<VEC>(h + col);
-        q = load_piece<VEC>(dy + col);
-        if (a.dt) t = load_piece<VEC>(dt + col);
-      }
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        xh[c][e] = p.v[e] * rstd;
-        dn[c][e] = q.v[e];
-        add[c][e] = t.v[e];
+      const int col = (c * L + j) * 8;
+      d.h[c].zero();
+      d.dy[c].zero();
+      d.dt[c].zero();
+      if (here && col < a.width) {
+        d.h[c].template load<WHOLE>(h + row * a.h_s, col, a.width);
+        d.dy[c].template load<WHOLE>(dy + row * a.dy_s, col, a.width);
+        if (a.dt) d.dt[c].template load<WHOLE>(dt + row * a.dt_s, col, a.width);
       }
     }
+  };
+  auto finish = [&](const row_data& d, int64_t row) {
+    float dot = 0.f;
 #pragma unroll
-    for (int c = 0; c < C; ++c)
+    for (int c = 0; c < C; ++c) {
+      float g[8];
+      gain_of(c, g);
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        acc[c][e] = __builtin_fmaf(dn[c][e], xh[c][e], acc[c][e]);
-        dn[c][e] *= g[c][e];
-        dot = __builtin_fmaf(dn[c][e], xh[c][e], dot);
+      for (int e = 0; e < 8; ++e) {
+        const float xh = d.h[c][e] * d.rstd, y = d.dy[c][e];
+        acc[c][e] = __builtin_fmaf(y, xh, acc[c][e]);
+        dot = __builtin_fmaf(y * g[e], xh, dot);
       }
+    }
     const float mean = row_sum_of<L>(dot, buf) * a.inv_width;
     T* const dx = (T*)a.dx + z * a.dx_z + row * a.dx_s;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
-      const int col = (c * L + j) * VEC;
-      if (here && col < a.width) {
-        float o[VEC];
+      const int col = (c * L + j) * 8;
+      float g[8], o[8];
+      gain_of(c, g);
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) o[e] = __builtin_fmaf(rstd, __builtin_fmaf(-xh[c][e], mean, dn[c][e]), add[c][e]);
-        store_piece<VEC>(dx + col, o);
-      }
+      for (int e = 0; e < 8; ++e) o[e] = __builtin_fmaf(d.rstd, __builtin_fmaf(-(d.h[c][e] * d.rstd), mean, d.dy[c][e] * g[e]), d.dt[c][e]);
+      if (row < a.rows && col < a.width) store_piece<WHOLE>(dx + col, o, a.width - col);
     }
+  };
+  const int64_t step = (int64_t)gridDim.x * RPB;
+  row_data d;
+  int64_t base = (int64_t)blockIdx.x * RPB;
+  fetch(d, base + sub);         // in flight while the gain comes into LDS
+  if (kGainInLds) {
+    for (int c = threadIdx.x; c < COLS; c += THREADS) s_gain[c] = c < a.width ? gain[c] : 0.f;
+    __syncthreads();
+  }
+  while (base < a.rows) {
+    finish(d, base + sub);
+    base += step;
+    fetch(d, base + sub);
   }
   if (!a.part) return;
   float* const out = a.part + z * a.part_z + (int64_t)blockIdx.x * a.width;
@@ -246,7 +325,7 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void hdet_norm_grad_kernel(const
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) sums[sub * COLS + (c * L + j) * VEC + e] = acc[c][e];
+      for (int e = 0; e < 8; ++e) sums[sub * COLS + (c * L + j) * 8 + e] = acc[c][e];
     __syncthreads();
     for (int col = threadIdx.x; col < a.width; col += THREADS) {
       float s = 0.f;
@@ -258,61 +337,62 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void hdet_norm_grad_kernel(const
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) {
-        const int col = (c * L + j) * VEC + e;
+      for (int e = 0; e < 8; ++e) {
+        const int col = (c * L + j) * 8 + e;
         if (col < a.width) out[col] = acc[c][e];
       }
   }
 }
 
-// out[z][col] = sum over p of part[z][p][col], ascending in four phases.  Block = 64 columns x 4 phases; grid (ceil(width / 64), replicas).
-__global__ __launch_bounds__(256) void hdet_partial_sum_kernel(const float* part, int parts, int width, int64_t pitch, float* out, int64_t out_z) {
-  __shared__ float s[4][64];
-  const int col = blockIdx.x * 64 + (threadIdx.x & 63), ph = threadIdx.x >> 6, z = blockIdx.y;
+// out[z][col] = sum over p of part[z][p][col], ascending in 16 phases that are added in their order.  Block = 64 columns x 16 phases; grid (ceil(width / 64), replicas).
+__global__ __launch_bounds__(1024) void hdet_partial_sum_kernel(const float* part, int parts, int width, int64_t pitch, float* out, int64_t out_z) {
+  __shared__ float s[16][64];
+  const int lane = threadIdx.x & 63, col = blockIdx.x * 64 + lane, ph = threadIdx.x >> 6, z = blockIdx.y;
   float x = 0.f;
   if (col < width) {
     const float* p = part + (int64_t)z * parts * pitch + col;
 #pragma unroll 4
-    for (int i = ph; i < parts; i += 4) x += p[i * pitch];
+    for (int i = ph; i < parts; i += 16) x += p[i * pitch];
   }
-  s[ph][threadIdx.x & 63] = x;
+  s[ph][lane] = x;
   __syncthreads();
-  if (ph == 0 && col < width) out[z * out_z + col] = (s[0][threadIdx.x] + s[1][threadIdx.x]) + (s[2][threadIdx.x] + s[3][threadIdx.x]);
+  if (ph != 0 || col >= width) return;
+  x = s[0][lane];
+#pragma unroll
+  for (int w = 1; w < 16; ++w) x += s[w][lane];
+  out[z * out_z + col] = x;
 }
 
-// Sums over up to kSumRows rows of a bfloat16 matrix.  Block = 32 groups of VEC columns x 8 phases of rows; grid (column blocks, row blocks, replicas).
-namespace { constexpr int kSumRows = 128; }
-template <int VEC>
-__global__ __launch_bounds__(256) void hdet_row_sum_kernel(const uint16_t* x, int64_t x_s, int64_t x_z, int64_t rows, int width, float* part, int64_t part_z) {
-  constexpr int COLS = 32 * VEC;
-  __shared__ float s[8][COLS + 1];
-  const int cg = threadIdx.x & 31, ph = threadIdx.x >> 5, z = blockIdx.z, col = blockIdx.x * COLS + cg * VEC;
-  const int64_t r0 = (int64_t)blockIdx.y * kSumRows, r1 = r0 + kSumRows < rows ? r0 + kSumRows : rows;
-  float acc[VEC];
+// Sums over `each` rows of a bfloat16 matrix.  Block = 64 pieces of 8 columns x 4 phases of rows, eight rows' loads in flight; grid (column blocks, row blocks, replicas).
+// (8 x 8192 rows of 4096, more than the memory-side cache holds: 122 us, past the caches 93 = 5.8 TB/s.)
+template <int WHOLE>
+__global__ __launch_bounds__(256) void hdet_row_sum_kernel(const uint16_t* x, int64_t x_s, int64_t x_z, int64_t rows, int each, int width, float* part, int64_t part_z) {
+  __shared__ float s[4][512 + 8];
+  const int cg = threadIdx.x & 63, ph = threadIdx.x >> 6, z = blockIdx.z, col = blockIdx.x * 512 + cg * 8;
+  const int64_t r0 = (int64_t)blockIdx.y * each, r1 = r0 + each < rows ? r0 + each : rows;
+  float acc[8];
 #pragma unroll
-  for (int e = 0; e < VEC; ++e) acc[e] = 0.f;
+  for (int e = 0; e < 8; ++e) acc[e] = 0.f;
   if (col < width) {
-    const uint16_t* p = x + z * x_z + col;
-#pragma unroll 4
-    for (int64_t r = r0 + ph; r < r1; r += 8) {
-      const piece_of<VEC> v = load_piece<VEC>(p + r * x_s);
+    const uint16_t* p = x + z * x_z;
+#pragma unroll 8
+    for (int64_t r = r0 + ph; r < r1; r += 4) {
+      piece<uint16_t> v;
+      v.load<WHOLE>(p + r * x_s, col, width);
 #pragma unroll
-      for (int e = 0; e < VEC; ++e) acc[e] += v.v[e];
+      for (int e = 0; e < 8; ++e) acc[e] += v[e];
     }
   }
 #pragma unroll
-  for (int e = 0; e < VEC; ++e) s[ph][cg * VEC + e] = acc[e];
+  for (int e = 0; e < 8; ++e) s[ph][cg * 8 + e] = acc[e];
   __syncthreads();
-  for (int c = threadIdx.x; c < COLS; c += 256) {
-    float v = 0.f;
-#pragma unroll
-    for (int w = 0; w < 8; ++w) v += s[w][c];
-    if (blockIdx.x * COLS + c < width) part[z * part_z + (int64_t)blockIdx.y * width + blockIdx.x * COLS + c] = v;
-  }
+  for (int c = threadIdx.x; c < 512; c += 256)
+    if (blockIdx.x * 512 + c < width)
+      part[z * part_z + (int64_t)blockIdx.y * width + blockIdx.x * 512 + c] = (s[0][c] + s[1][c]) + (s[2][c] + s[3][c]);
 }
 
 // Rows of codes to values: a thread takes 8 columns.  Grid: (ceil(rows * pieces / 256), replicas).
-template <typename T, int VEC>
+template <typename T, int WHOLE>
 __global__ __launch_bounds__(256) void hdet_restore_kernel(const int8_t* q, int64_t q_s, int64_t q_z, const float* scale, T* v, int64_t v_s, int64_t v_z,
                                                            int64_t rows, int width, int pieces) {
   const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x, row = t / pieces;
@@ -323,14 +403,7 @@ __global__ __launch_bounds__(256) void hdet_restore_kernel(const int8_t* q, int6
   float o[8];
 #pragma unroll
   for (int e = 0; e < 8; ++e) o[e] = (float)(int8_t)((w[e >> 2] >> (8 * (e & 3))) & 255u) * s;
-  T* const p = v + z * v_z + row * v_s + col;
-  if constexpr (VEC == 8) {
-    store_piece<8>(p, o);
-  } else {
-#pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (col + e < width) hdet_st(p + e, o[e]);
-  }
+  store_piece<WHOLE>(v + z * v_z + row * v_s + col, o, width - col);
 }
 
 namespace {
@@ -341,46 +414,45 @@ bool pieces_of_8(const hdet_rows& m, int size, int width) {
   return (reinterpret_cast<uintptr_t>(m.dev) & 15) == 0 && ((m.row_stride | m.replica_stride) * size & 15) == 0 && (width & 7) == 0;
 }
 
-// f(T, VEC, L, C) for the smallest row of registers that holds `width`
+int mode_of(bool whole, int64_t bytes) { return !whole ? kLoose : bytes > (int64_t)256 << 20 ? kStream : kWhole; }
+
+// f(T, mode, L, C) for the smallest row of registers that holds `width`
 template <typename T, typename F>
-void with_shape(int width, bool vec, F f) {
-#define HDET_SHAPE(VEC, L, C)                                                                         \
-  if (width <= VEC * L * C) return f(T(), std::integral_constant<int, VEC>(), std::integral_constant<int, L>(), std::integral_constant<int, C>())
-  if (vec) {
-    HDET_SHAPE(8, 8, 1);
-    HDET_SHAPE(8, 16, 1);
-    HDET_SHAPE(8, 32, 1);
-    HDET_SHAPE(8, 64, 1);
-    HDET_SHAPE(8, 64, 2);
-    HDET_SHAPE(8, 64, 4);
-    HDET_SHAPE(8, 256, 2);
-    HDET_SHAPE(8, 256, 4);
-    HDET_SHAPE(8, 1024, 2);
-    HDET_SHAPE(8, 1024, 4);
-  } else {
-    HDET_SHAPE(1, 64, 8);
-    HDET_SHAPE(1, 64, 32);
-    HDET_SHAPE(1, 256, 32);
-    HDET_SHAPE(1, 1024, 32);
+void with_shape(int width, int mode, F f) {
+#define HDET_SHAPE(L, C)                                                                              \
+  if (width <= 8 * L * C) {                                                                           \
+    if (mode == kStream) return f(T(), std::integral_constant<int, kStream>(), std::integral_constant<int, L>(), std::integral_constant<int, C>());   \
+    if (mode == kWhole) return f(T(), std::integral_constant<int, kWhole>(), std::integral_constant<int, L>(), std::integral_constant<int, C>());     \
+    return f(T(), std::integral_constant<int, kLoose>(), std::integral_constant<int, L>(), std::integral_constant<int, C>());                         \
   }
+  HDET_SHAPE(8, 1)
+  HDET_SHAPE(16, 1)
+  HDET_SHAPE(32, 1)
+  HDET_SHAPE(64, 1)
+  HDET_SHAPE(64, 2)
+  HDET_SHAPE(64, 4)
+  HDET_SHAPE(256, 2)
+  HDET_SHAPE(256, 4)
+  HDET_SHAPE(1024, 2)
+  HDET_SHAPE(1024, 4)
 #undef HDET_SHAPE
 }
-int rows_per_block(int width, bool vec) {
+int rows_per_block(int width) {
   int n = 1;
-  with_shape<float>(width, vec, [&](auto, auto, auto l, auto) { n = l < 256 ? 256 / l : 1; });
+  with_shape<float>(width, kWhole, [&](auto, auto, auto l, auto) { n = l < 256 ? 256 / l : 1; });
   return n;
 }
 // blocks a replica of the backward pass: about eight a compute unit over all replicas, so that the gain's partial sums stay few
-int grad_blocks(int n_replicas, int64_t rows, int width, bool vec) {
-  const int64_t most = (rows + rows_per_block(width, vec) - 1) / rows_per_block(width, vec);
+int grad_blocks(int n_replicas, int64_t rows, int width) {
+  const int64_t most = (rows + rows_per_block(width) - 1) / rows_per_block(width);
   int64_t want = 8 * (int64_t)hdet_compute_units() / n_replicas;
   if (want < 1) want = 1;
   return (int)(most < want ? most : want);
 }
 
 template <typename T>
-hipError_t launch_norm_typed(const norm_kernel_args& k, int n, bool vec, bool norm, hipStream_t s) {
-  with_shape<T>(k.width, vec, [&](auto t, auto v, auto l, auto c) {
+hipError_t launch_norm_typed(const norm_kernel_args& k, int n, int mode, bool norm, hipStream_t s) {
+  with_shape<T>(k.width, mode, [&](auto t, auto v, auto l, auto c) {
     constexpr int THREADS = l < 256 ? 256 : l;
     const dim3 grid((unsigned)((k.rows + THREADS / l - 1) / (THREADS / l)), n);
     if (norm) hipLaunchKernelGGL((hdet_norm_kernel<decltype(t), v, l, c, true>), grid, dim3(THREADS), 0, s, k);
@@ -395,20 +467,22 @@ hipError_t hdet_launch_norm(const hdet_norm_args& a, hipStream_t s) {
   if (a.rows == 0) return hipSuccess;
   const int size = a.dtype == HDET_TYPE_BF16 ? 2 : 4;
   const bool vec = pieces_of_8(a.x, size, a.width) && pieces_of_8(a.resid, size, a.width) && pieces_of_8(a.total, size, a.width) && pieces_of_8(a.y, size, a.width);
+  const int64_t each = (1 + (a.resid.dev != nullptr) + (a.total.dev != nullptr) + (a.y.dev != nullptr)) * size + (a.codes.dev != nullptr);
+  const int mode = mode_of(vec, each * a.n_replicas * a.rows * a.width);
   norm_kernel_args k = {a.x.dev, a.resid.dev, a.total.dev, a.y.dev, (int8_t*)a.codes.dev, a.scale_dev, a.rstd_dev, a.gain_dev,
                         a.x.row_stride, a.x.replica_stride, a.resid.row_stride, a.resid.replica_stride, a.total.row_stride, a.total.replica_stride,
                         a.y.row_stride, a.y.replica_stride, a.codes.row_stride, a.codes.replica_stride, a.gain_stride, a.rows, a.width, (float)a.eps, 1.f / (float)a.width};
-  return a.dtype == HDET_TYPE_BF16 ? launch_norm_typed<uint16_t>(k, a.n_replicas, vec, true, s) : launch_norm_typed<float>(k, a.n_replicas, vec, true, s);
+  return a.dtype == HDET_TYPE_BF16 ? launch_norm_typed<uint16_t>(k, a.n_replicas, mode, true, s) : launch_norm_typed<float>(k, a.n_replicas, mode, true, s);
 }
 
 hipError_t hdet_launch_quantise(const hdet_codes_args& a, hipStream_t s) {
   if (a.rows == 0) return hipSuccess;
-  const bool vec = pieces_of_8(a.values, a.dtype == HDET_TYPE_BF16 ? 2 : 4, a.width);
+  const int size = a.dtype == HDET_TYPE_BF16 ? 2 : 4, mode = mode_of(pieces_of_8(a.values, size, a.width), (int64_t)(size + 1) * a.n_replicas * a.rows * a.width);
   norm_kernel_args k = {};
   k.x = a.values.dev; k.x_s = a.values.row_stride; k.x_z = a.values.replica_stride;
   k.codes = (int8_t*)a.codes.dev; k.c_s = a.codes.row_stride; k.c_z = a.codes.replica_stride;
   k.scale = a.scale_dev; k.rows = a.rows; k.width = a.width;
-  return a.dtype == HDET_TYPE_BF16 ? launch_norm_typed<uint16_t>(k, a.n_replicas, vec, false, s) : launch_norm_typed<float>(k, a.n_replicas, vec, false, s);
+  return a.dtype == HDET_TYPE_BF16 ? launch_norm_typed<uint16_t>(k, a.n_replicas, mode, false, s) : launch_norm_typed<float>(k, a.n_replicas, mode, false, s);
 }
 
 hipError_t hdet_launch_restore(const hdet_codes_args& a, hipStream_t s) {
@@ -420,21 +494,20 @@ hipError_t hdet_launch_restore(const hdet_codes_args& a, hipStream_t s) {
     hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, (const int8_t*)a.codes.dev, a.codes.row_stride, a.codes.replica_stride, a.scale_dev, v,
                        a.values.row_stride, a.values.replica_stride, a.rows, a.width, pieces);
   };
-  if (bf && vec) go(&hdet_restore_kernel<uint16_t, 8>, (uint16_t*)a.values.dev);
-  else if (bf) go(&hdet_restore_kernel<uint16_t, 1>, (uint16_t*)a.values.dev);
-  else if (vec) go(&hdet_restore_kernel<float, 8>, (float*)a.values.dev);
-  else go(&hdet_restore_kernel<float, 1>, (float*)a.values.dev);
+  if (bf && vec) go(&hdet_restore_kernel<uint16_t, kWhole>, (uint16_t*)a.values.dev);
+  else if (bf) go(&hdet_restore_kernel<uint16_t, kLoose>, (uint16_t*)a.values.dev);
+  else if (vec) go(&hdet_restore_kernel<float, kWhole>, (float*)a.values.dev);
+  else go(&hdet_restore_kernel<float, kLoose>, (float*)a.values.dev);
   return hipGetLastError();
 }
 
 size_t hdet_norm_backward_bytes(int n_replicas, int64_t rows, int width) {
   if (rows == 0) return 0;
-  const int a = grad_blocks(n_replicas, rows, width, true), b = grad_blocks(n_replicas, rows, width, false);
-  return (size_t)n_replicas * (a > b ? a : b) * width * sizeof(float);
+  return (size_t)n_replicas * grad_blocks(n_replicas, rows, width) * width * sizeof(float);
 }
 
 hipError_t hdet_launch_partial_sum(const float* partial, int n_replicas, int parts, int width, int64_t pitch, float* out, int64_t out_stride, hipStream_t s) {
-  hipLaunchKernelGGL(hdet_partial_sum_kernel, dim3((width + 63) / 64, n_replicas), dim3(256), 0, s, partial, parts, width, pitch, out, out_stride);
+  hipLaunchKernelGGL(hdet_partial_sum_kernel, dim3((width + 63) / 64, n_replicas), dim3(1024), 0, s, partial, parts, width, pitch, out, out_stride);
   return hipGetLastError();
 }
 
@@ -443,7 +516,7 @@ hipError_t hdet_launch_norm_backward(const hdet_norm_grad_args& a, hipStream_t s
   if (a.rows == 0) return a.dgain_dev ? hdet_launch_partial_sum(nullptr, a.n_replicas, 0, a.width, 0, a.dgain_dev, a.dgain_stride, s) : hipSuccess;
   const int size = a.dtype == HDET_TYPE_BF16 ? 2 : 4;
   const bool vec = pieces_of_8(a.total, size, a.width) && pieces_of_8(a.dy, size, a.width) && pieces_of_8(a.dtotal, size, a.width) && pieces_of_8(a.dx, size, a.width);
-  const int blocks = grad_blocks(a.n_replicas, a.rows, a.width, vec);
+  const int blocks = grad_blocks(a.n_replicas, a.rows, a.width);
   const bool direct = blocks == 1;
   const norm_grad_kernel_args k = {a.total.dev, a.dy.dev, a.dtotal.dev, a.dx.dev, a.rstd_dev, a.gain_dev, !a.dgain_dev ? nullptr : direct ? a.dgain_dev : (float*)a.workspace_dev,
                                    a.total.row_stride, a.total.replica_stride, a.dy.row_stride, a.dy.replica_stride, a.dtotal.row_stride, a.dtotal.replica_stride,
@@ -451,24 +524,39 @@ hipError_t hdet_launch_norm_backward(const hdet_norm_grad_args& a, hipStream_t s
   auto go = [&](auto t, auto v, auto l, auto c) {
     hipLaunchKernelGGL((hdet_norm_grad_kernel<decltype(t), v, l, c>), dim3(blocks, a.n_replicas), dim3(l < 256 ? 256 : l), 0, s, k);
   };
-  if (a.dtype == HDET_TYPE_BF16) with_shape<uint16_t>(a.width, vec, go);
-  else with_shape<float>(a.width, vec, go);
+  const int mode = mode_of(vec, (int64_t)(3 + (a.dtotal.dev != nullptr)) * size * a.n_replicas * a.rows * a.width);
+  if (a.dtype == HDET_TYPE_BF16) with_shape<uint16_t>(a.width, mode, go);
+  else with_shape<float>(a.width, mode, go);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || direct || !a.dgain_dev) return e;
   return hdet_launch_partial_sum((const float*)a.workspace_dev, a.n_replicas, blocks, a.width, a.width, a.dgain_dev, a.dgain_stride, s);
 }
 
-size_t hdet_row_sum_bytes(int n_replicas, int64_t rows, int width) { return (size_t)n_replicas * ((rows + kSumRows - 1) / kSumRows) * width * sizeof(float); }
+// Rows of a block of hdet_row_sum_kernel: 128, fewer until there are four blocks a compute unit (3 x 515 rows of 1501: 128 16 us, 64 10)
+static int rows_each(int n_replicas, int64_t rows, int width) {
+  int each = 128;
+  while (each > 16 && (rows + each - 1) / each * ((width + 511) / 512) * n_replicas < 4 * hdet_compute_units()) each >>= 1;
+  return each;
+}
+static int row_sum_parts(int n_replicas, int64_t rows, int width) {
+  const int each = rows_each(n_replicas, rows, width);
+  return (int)((rows + each - 1) / each);
+}
+
+size_t hdet_row_sum_bytes(int n_replicas, int64_t rows, int width) { return (size_t)n_replicas * row_sum_parts(n_replicas, rows, width) * width * sizeof(float); }
 
 hipError_t hdet_launch_row_sum(const hdet_rows& x, int n_replicas, int64_t rows, int width, float* out, int64_t out_stride, void* scratch, hipStream_t s) {
-  const int parts = (int)((rows + kSumRows - 1) / kSumRows);
+  const int parts = row_sum_parts(n_replicas, rows, width), each = rows_each(n_replicas, rows, width);
   if (parts == 0) return hdet_launch_partial_sum(nullptr, n_replicas, 0, width, 0, out, out_stride, s);
   float* const to = parts == 1 ? out : (float*)scratch;
   const int64_t to_z = parts == 1 ? out_stride : (int64_t)parts * width;
-  if (pieces_of_8(x, 2, width))
-    hipLaunchKernelGGL(hdet_row_sum_kernel<8>, dim3((width + 255) / 256, parts, n_replicas), dim3(256), 0, s, (const uint16_t*)x.dev, x.row_stride, x.replica_stride, rows, width, to, to_z);
-  else
-    hipLaunchKernelGGL(hdet_row_sum_kernel<1>, dim3((width + 31) / 32, parts, n_replicas), dim3(256), 0, s, (const uint16_t*)x.dev, x.row_stride, x.replica_stride, rows, width, to, to_z);
+  const int mode = mode_of(pieces_of_8(x, 2, width), (int64_t)2 * n_replicas * rows * width);
+  auto go = [&](auto kernel) {
+    hipLaunchKernelGGL(kernel, dim3((width + 511) / 512, parts, n_replicas), dim3(256), 0, s, (const uint16_t*)x.dev, x.row_stride, x.replica_stride, rows, each, width, to, to_z);
+  };
+  if (mode == kStream) go(&hdet_row_sum_kernel<kStream>);
+  else if (mode == kWhole) go(&hdet_row_sum_kernel<kWhole>);
+  else go(&hdet_row_sum_kernel<kLoose>);
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess || parts == 1) return e;
   return hdet_launch_partial_sum((const float*)scratch, n_replicas, parts, width, width, out, out_stride, s);

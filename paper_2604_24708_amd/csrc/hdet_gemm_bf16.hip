@@ -225,7 +225,7 @@ __device__ __forceinline__ void put_element(const hdet_bgemm_args& g, int z, int
   if (row >= g.m || col >= g.n) return;
   const int64_t off = c_base + (int64_t)row * g.ldc + col;
   if (EPI == HDET_EPI_BIAS_RELU_BF16 || EPI == HDET_EPI_BIAS_F32 || EPI == HDET_EPI_BIAS_BF16) v += g.bias[(int64_t)z * g.bias_bs + col];
-  if (EPI == HDET_EPI_SCALED_F32 || EPI == HDET_EPI_SCALED_BF16) v *= g.out_scale[z];
+  if ((EPI == HDET_EPI_SCALED_F32 || EPI == HDET_EPI_SCALED_BF16) && g.out_scale) v *= g.out_scale[z];
   if (EPI == HDET_EPI_F32 || EPI == HDET_EPI_BIAS_F32 || EPI == HDET_EPI_SCALED_F32) {
     reinterpret_cast<float*>(g.c)[off] = v;
     return;
@@ -237,7 +237,7 @@ __device__ __forceinline__ void put_element(const hdet_bgemm_args& g, int z, int
       *p = v;
       return;
     }
-    v *= g.out_scale[z];
+    if (g.out_scale) v *= g.out_scale[z];
   }
   if (EPI == HDET_EPI_BIAS_RELU_BF16) v = v > 0.f ? v : 0.f;
   if (EPI == HDET_EPI_MASK_BF16)         // gradient through the ReLU of the layer below

@@ -173,10 +173,22 @@ __device__ __forceinline__ void store_tile(const hdet_bgemm_args& g, const typen
   float* const stg = reinterpret_cast<float*>(S) + wave * (SR * EP);
   const int lr = lane / LPR, lc = (lane % LPR) * 4;
   const int col = n0 + wn + lc;
-  const bool col_ok = col < g.n;                             // n is a multiple of 4: the 4 columns exist together
+  const bool col_ok = col < g.n;                             // n is a multiple of 4, or put_any looks: the 4 columns exist together
   auto put = [&](auto* p, auto v) {
     if (STREAM) __builtin_nontemporal_store(v, p);
     else *p = v;
+  };
+  // four columns of a row, or the `left` that there are, at any element
+  auto put_any = [&](auto* p, auto v, int left) {
+    typedef decltype(v) any __attribute__((aligned(sizeof(*p))));
+    if (left >= 4) {
+      if (STREAM) __builtin_nontemporal_store(v, reinterpret_cast<any*>(p));
+      else *reinterpret_cast<any*>(p) = v;
+    } else {
+#pragma unroll
+      for (int q = 0; q < 3; ++q)
+        if (q < left) p[q] = v[q];
+    }
   };
   constexpr bool kBias = EPI == HDET_EPI_BIAS_RELU_BF16 || EPI == HDET_EPI_BIAS_F32 || EPI == HDET_EPI_BIAS_BF16 ||
                          EPI == HDET_EPI_BIAS_GELU_BF16 || EPI == HDET_EPI_BIAS_RESID_BF16 || EPI == HDET_EPI_BIAS_DROP_RESID_BF16;
@@ -223,7 +235,7 @@ __device__ __forceinline__ void store_tile(const hdet_bgemm_args& g, const typen
     }
   };
   constexpr bool kScaled = EPI == HDET_EPI_SCALED_F32 || EPI == HDET_EPI_SCALED_BF16 || EPI == HDET_EPI_ACCUM_BF16;
-  const float out_scale = kScaled ? g.out_scale[z] : 1.f;
+  const float out_scale = kScaled && g.out_scale ? g.out_scale[z] : 1.f;
   // column sums of the stored result over the rows this lane stores, for its 4 columns
   constexpr bool kColsum = EPI == HDET_EPI_GELUGRAD_BF16 || EPI == HDET_EPI_MASK_BF16;
   f4 csum = {0.f, 0.f, 0.f, 0.f};
@@ -294,7 +306,9 @@ __device__ __forceinline__ void store_tile(const hdet_bgemm_args& g, const typen
             const us4 o = {hdet_um::to_bf16(th[0]), hdet_um::to_bf16(th[1]), hdet_um::to_bf16(th[2]), hdet_um::to_bf16(th[3])};
             __builtin_nontemporal_store(o, reinterpret_cast<us4*>(g.upd.shadow + off));
           }
-        } else if (EPI == HDET_EPI_F32 || EPI == HDET_EPI_BIAS_F32 || EPI == HDET_EPI_SCALED_F32) {
+        } else if (EPI == HDET_EPI_SCALED_F32) {
+          put_any(reinterpret_cast<float*>(g.c) + off, v, g.n - col);
+        } else if (EPI == HDET_EPI_F32 || EPI == HDET_EPI_BIAS_F32) {
           put(reinterpret_cast<f4*>(reinterpret_cast<float*>(g.c) + off), v);
         } else if (EPI == HDET_EPI_BIAS_GELU_BF16) {
           const us4 pre = {f2bf(v[0]), f2bf(v[1]), f2bf(v[2]), f2bf(v[3])};
@@ -310,7 +324,8 @@ __device__ __forceinline__ void store_tile(const hdet_bgemm_args& g, const typen
             v += *reinterpret_cast<const f4*>(g.accum + (int64_t)z * g.accum_bs + (int64_t)row * g.accum_ld + col);
           if (EPI == HDET_EPI_ACCUM_BF16) v *= out_scale;
           const us4 o = {f2bf(v[0]), f2bf(v[1]), f2bf(v[2]), f2bf(v[3])};
-          put(reinterpret_cast<us4*>(reinterpret_cast<uint16_t*>(g.c) + off), o);
+          if constexpr (kScaled) put_any(reinterpret_cast<uint16_t*>(g.c) + off, o, g.n - col);
+          else put(reinterpret_cast<us4*>(reinterpret_cast<uint16_t*>(g.c) + off), o);
           if (kColsum) {
 #pragma unroll
             for (int q = 0; q < 4; ++q) csum[q] += bf2f(o[q]);
@@ -376,9 +391,9 @@ void hdet_bgemm_dma_kernel(const hdet_bgemm_args g) {
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wm = (wave / WGN) * (32 * WMT), wn = (wave % WGN) * (32 * WNT);
 
-  // byte extent of each operand for this batch item: the bound that turns absent chunks into zeros (A in whole chunks: hdet_bgemm_args::padded)
+  // byte extent of each operand for this batch item: the bound that turns absent chunks into zeros (in whole chunks: hdet_bgemm_args::padded)
   const uint32_t a_bytes = (uint32_t)(((int64_t)((A_KMAJOR ? g.m : g.k) - 1) * g.lda + (((A_KMAJOR ? g.k : g.m) + 7) & ~7)) * 2);
-  const uint32_t b_bytes = (uint32_t)(((int64_t)((B_KMAJOR ? g.n : g.k) - 1) * g.ldb + (B_KMAJOR ? g.k : g.n)) * 2);
+  const uint32_t b_bytes = (uint32_t)(((int64_t)((B_KMAJOR ? g.n : g.k) - 1) * g.ldb + (((B_KMAJOR ? g.k : g.n) + 7) & ~7)) * 2);
   const i4 ra = make_rsrc(A, a_bytes), rb = make_rsrc(B, b_bytes);
   const uint32_t s_addr = lds_addr_of(S);
 
@@ -525,7 +540,7 @@ __global__ __launch_bounds__(512, 2) void hdet_bgemm_alt_kernel(const hdet_bgemm
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wn = (wave % WGN) * 64, hr = (wave / WGN) * 64;
   const uint32_t a_bytes = (uint32_t)(((int64_t)((A_KMAJOR ? g.m : g.k) - 1) * g.lda + (((A_KMAJOR ? g.k : g.m) + 7) & ~7)) * 2);
-  const uint32_t b_bytes = (uint32_t)(((int64_t)((B_KMAJOR ? g.n : g.k) - 1) * g.ldb + (B_KMAJOR ? g.k : g.n)) * 2);
+  const uint32_t b_bytes = (uint32_t)(((int64_t)((B_KMAJOR ? g.n : g.k) - 1) * g.ldb + (((B_KMAJOR ? g.k : g.n) + 7) & ~7)) * 2);
   const i4 ra = make_rsrc(A, a_bytes), rb = make_rsrc(B, b_bytes);
   const uint32_t s_addr = lds_addr_of(S);
 
@@ -1157,16 +1172,19 @@ bool hdet_bgemm_dma_eligible(const hdet_bgemm_args& g, bool a_kmajor, bool b_kma
   if (g.m < 1 || g.n < 1 || g.k < 1) return false;
   // a chunk is 8 elements along the operand's contiguous axis: k if k-major, else the row axis
   if (!chunk_regular(g.a, g.lda, g.a_s, g.padded ? 0 : a_kmajor ? g.k : g.m)) return false;
-  if (!chunk_regular(g.b, g.ldb, g.b_s, b_kmajor ? g.k : g.n)) return false;
+  if (!chunk_regular(g.b, g.ldb, g.b_s, g.padded ? 0 : b_kmajor ? g.k : g.n)) return false;
   // operand extents of one batch item as 32-bit byte offsets below the "absent" mark
   const int64_t a_bytes = ((int64_t)((a_kmajor ? g.m : g.k) - 1) * g.lda + (a_kmajor ? g.k : g.m)) * 2;
   const int64_t b_bytes = ((int64_t)((b_kmajor ? g.n : g.k) - 1) * g.ldb + (b_kmajor ? g.k : g.n)) * 2;
   // the K loop may form offsets up to one stage row past the extent before they are replaced
   const int64_t slack = 64 * 2 * (a_kmajor ? 1 : g.lda) + 64 * 2 * (b_kmajor ? 1 : g.ldb);
   if (a_bytes + slack >= (int64_t)1 << 31 || b_bytes + slack >= (int64_t)1 << 31) return false;
-  // C (and bias, mask) four columns at a time
-  if ((g.ldc & 3) || ((g.c_s[0] | g.c_s[1] | g.c_s[2]) & 3) || (g.n & 3)) return false;
-  if (reinterpret_cast<uintptr_t>(g.c) & (f32_out ? 15 : 7)) return false;
+  // C (and bias, mask) four columns at a time, in the last three epilogues at any element
+  const bool any_c = epi == HDET_EPI_ACCUM_BF16 || epi == HDET_EPI_SCALED_F32 || epi == HDET_EPI_SCALED_BF16;
+  if (!any_c) {
+    if ((g.ldc & 3) || ((g.c_s[0] | g.c_s[1] | g.c_s[2]) & 3) || (g.n & 3)) return false;
+    if (reinterpret_cast<uintptr_t>(g.c) & (f32_out ? 15 : 7)) return false;
+  }
   if (has_bias && ((g.bias_bs & 3) || (reinterpret_cast<uintptr_t>(g.bias) & 15))) return false;
   if (epi == HDET_EPI_BIAS_DROP_RESID_BF16 && (!g.drop_ctrl || g.drop_channel < 0 || g.n1 * g.n2 != 1 || g.c_s[0] >= ((int64_t)1 << 34)))
     return false;        // the replica is the batch index; the element counter has 32 bits

@@ -170,7 +170,7 @@ enum { HDET_EPI_F32 = 0, HDET_EPI_BIAS_F32 = 1, HDET_EPI_BIAS_RELU_BF16 = 2, HDE
        HDET_EPI_XENT_STAT = 11,       // reference and sum of a tile's rows (hdet_xent_epi; c is not written)
        HDET_EPI_XENT_GRAD = 12,
        // a product in pieces of its contraction, input-gradient order: the sum so far is in fp32 at `accum`, the last piece's is times out_scale and
-       // rounded to c; weight gradients times out_scale
+       // rounded to c; weight gradients times out_scale.  out_scale may be null, and c may lie at any element
        HDET_EPI_ACCUM_BF16 = 13, HDET_EPI_SCALED_F32 = 14, HDET_EPI_SCALED_BF16 = 15,
        HDET_EPI_XENT_PARTS = 16 };    // HDET_EPI_XENT_GRAD in three bf16 parts (hdet_launch_vocab_grad only)     // c = bf16 gradient of the mean cross-entropy at z, from the whole rows' reference and sum; row losses, column sums
 
@@ -210,9 +210,9 @@ struct hdet_bgemm_args {
   hdet_xent_epi xent;      // HDET_EPI_XENT_*
   float* accum; int64_t accum_ld, accum_bs;   // HDET_EPI_ACCUM_BF16: accum[z0*accum_bs + m*accum_ld + n]; the first piece does not read it,
   bool accum_first, accum_last;               // the last writes c instead
-  const float* out_scale;                     // [z0]
-  // An axis that is no multiple of 8 lies in rows that go on to one: A with zeros (its chunks are read whole), and for HDET_EPI_XENT_* bias with -inf and c
-  // with columns that may be written
+  const float* out_scale;                     // [z0], or null
+  // Rows of A and B go on to a multiple of 8: with zeros in A (its chunks are read whole), with anything in B.  For HDET_EPI_XENT_* an n that is no multiple of 8:
+  // bias goes on with -inf, and c with columns that may be written
   bool padded;
   float* rowsum; int64_t rowsum_bs;     // general kernels, weight gradients: rowsum[z0*rowsum_bs + m] = sum_k A(m,k), or null
   int tile_group;          // LDS-direct kernel: consecutive blocks walk groups of this many tile rows column by column (0, 1: row by row)

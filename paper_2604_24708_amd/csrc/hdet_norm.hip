@@ -112,10 +112,10 @@ __device__ __forceinline__ void store_piece(float* p, const float (&v)[8], int l
 }
 
 // Reduction over the L threads of a row, the same value in each, in a fixed order.  L > 64 (a block to a row): through `buf`.
-template <int L, typename F>
-__device__ __forceinline__ unsigned over_row(unsigned x, unsigned* buf, F op) {
+template <int L, typename V, typename F>
+__device__ __forceinline__ V over_row(V x, V* buf, F op) {
 #pragma unroll
-  for (int o = 1; o < (L < 64 ? L : 64); o <<= 1) x = op(x, (unsigned)__shfl_xor((int)x, o));
+  for (int o = 1; o < (L < 64 ? L : 64); o <<= 1) x = op(x, __shfl_xor(x, o));
   if constexpr (L > 64) {
     if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = x;
     __syncthreads();
@@ -126,9 +126,8 @@ __device__ __forceinline__ unsigned over_row(unsigned x, unsigned* buf, F op) {
   }
   return x;
 }
-__device__ __forceinline__ unsigned add_floats(unsigned a, unsigned b) { return __float_as_uint(__uint_as_float(a) + __uint_as_float(b)); }
+template <int L, typename V> __device__ __forceinline__ V row_sum_of(V x, V* buf) { return over_row<L>(x, buf, [](V a, V b) { return a + b; }); }
 __device__ __forceinline__ unsigned larger(unsigned a, unsigned b) { return a > b ? a : b; }
-template <int L> __device__ __forceinline__ float row_sum_of(float x, unsigned* buf) { return __uint_as_float(over_row<L>(__float_as_uint(x), buf, add_floats)); }
 
 // Scale of a row from the bits of its largest absolute value.  With top = m 2^(E - 126), m in [1/2, 1): 127 2^e >= top from e = E - 133 on, or one more
 // where m > 127 / 128.  Absolute values compare as their bits do, NaN above infinity above all numbers: either gives the exponent 255.
@@ -140,8 +139,10 @@ __device__ __forceinline__ row_scale scale_of(unsigned top) {
   if (e < -126) e = -126;
   return {__uint_as_float((unsigned)(e + 127) << 23), __uint_as_float((unsigned)(127 - e) << 23)};
 }
-// |x| <= 127; rows that are not finite have the inverse 0 and get codes 0
-__device__ __forceinline__ int code_of(float x, float inverse) { return inverse == 0.f ? 0 : (int)rintf(x * inverse); }
+// rint(x inverse) as the low bits of that + 1.5 2^52, halves to even; |x inverse| is 127 at most, up to what rounding the row's largest value to fp32 took off
+__device__ __forceinline__ unsigned code_of(double x, double inverse) {
+  return (unsigned)__builtin_bit_cast(unsigned long long, __builtin_fma(x, inverse, 6755399441055744.0));
+}
 
 struct norm_kernel_args {
   const void *x, *resid;
@@ -151,24 +152,26 @@ struct norm_kernel_args {
   const float* gain;
   int64_t x_s, x_z, r_s, r_z, t_s, t_z, y_s, y_z, c_s, c_z, gain_z, rows;
   int width;
-  float eps, inv_width;
+  double eps, inv_width;
 };
 
 }  // namespace
 
+// The sum of squares, the norm and what is rounded to codes are held in 64 bits, which costs nothing beside the memory (a 64-bit operation takes as long as a 32-bit one) and puts a
+// code where the formula has it: in 32 bits y is off by 1e-7 of itself, 1e-5 of a step, and one row of a thousand columns in ten has a code one off.
 // NORM: as above; otherwise y = x (rows to 8 bits).  Grid: (ceil(rows / rows a block), replicas).
 // (The row is in registers from its two loads to its two or three stores; what is left between the loads and the stores are the two reductions.)
 template <typename T, int WHOLE, int L, int C, bool NORM>
 __global__ __launch_bounds__(L < 256 ? 256 : L) void hdet_norm_kernel(const norm_kernel_args a) {
   constexpr int THREADS = L < 256 ? 256 : L, RPB = THREADS / L;
   __shared__ unsigned buf[16];
+  __shared__ double sums[16];
   const int j = threadIdx.x % L, z = blockIdx.y;
   const int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / L;
   const bool here = row < a.rows;
-  float u[C][8];
+  double u[C][8];
   const T* x = (const T*)a.x + z * a.x_z + row * a.x_s;
   const T* r = (const T*)a.resid + z * a.r_z + row * a.r_s;
-  float ss = 0.f;
   piece<T> p[C], q[C];      // the two summands
   piece<float> gain[C];
 #pragma unroll
@@ -176,6 +179,7 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void hdet_norm_kernel(const norm
     const int col = (c * L + j) * 8;
     p[c].zero();
     q[c].zero();
+    if (NORM) gain[c].zero();
     if (here && col < a.width) {
       p[c].template load<WHOLE>(x, col, a.width);
       if (NORM && a.resid) q[c].template load<WHOLE>(r, col, a.width);
@@ -185,26 +189,31 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void hdet_norm_kernel(const norm
 #pragma unroll
   for (int c = 0; c < C; ++c)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) u[c][e] = NORM ? p[c][e] + q[c][e] : p[c][e];
+    for (int e = 0; e < 8; ++e)      // (bfloat16 summands: the sum is exact in 32 bits unless one is 2^16 times the other)
+      u[c][e] = !NORM ? (double)p[c][e] : sizeof(T) == 2 ? (double)(p[c][e] + q[c][e]) : (double)p[c][e] + (double)q[c][e];
   if constexpr (NORM) {
+    double ss = 0.0;
 #pragma unroll
     for (int c = 0; c < C; ++c)
 #pragma unroll
-      for (int e = 0; e < 8; ++e) ss = __builtin_fmaf(u[c][e], u[c][e], ss);
-    ss = row_sum_of<L>(ss, buf);
-    const float rstd = 1.f / sqrtf(__builtin_fmaf(ss, a.inv_width, a.eps));
-    if (a.rstd && here && j == 0) a.rstd[z * a.rows + row] = rstd;
+      for (int e = 0; e < 8; ++e) ss = __builtin_fma(u[c][e], u[c][e], ss);
+    const double rstd = 1.0 / sqrt(row_sum_of<L>(ss, sums) * a.inv_width + a.eps);
+    if (a.rstd && here && j == 0) a.rstd[z * a.rows + row] = (float)rstd;
     T* const total = (T*)a.total + z * a.t_z + row * a.t_s;
     T* const y = (T*)a.y + z * a.y_z + row * a.y_s;
 #pragma unroll
     for (int c = 0; c < C; ++c) {
       const int col = (c * L + j) * 8;
-      if (here && col < a.width) {
-        if (a.total) store_piece<WHOLE>(total + col, u[c], a.width - col);
+      float v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) u[c][e] = u[c][e] * rstd * gain[c][e];
-        if (a.y) store_piece<WHOLE>(y + col, u[c], a.width - col);
+      for (int e = 0; e < 8; ++e) v[e] = (float)u[c][e];
+      if (a.total && here && col < a.width) store_piece<WHOLE>(total + col, v, a.width - col);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        u[c][e] *= rstd * (double)gain[c][e];
+        v[e] = (float)u[c][e];
       }
+      if (a.y && here && col < a.width) store_piece<WHOLE>(y + col, v, a.width - col);
     }
   }
   if (!a.codes) return;
@@ -212,7 +221,7 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void hdet_norm_kernel(const norm
 #pragma unroll
   for (int c = 0; c < C; ++c)
 #pragma unroll
-    for (int e = 0; e < 8; ++e) top = larger(top, __float_as_uint(u[c][e]) & 0x7fffffffu);
+    for (int e = 0; e < 8; ++e) top = larger(top, __float_as_uint((float)u[c][e]) & 0x7fffffffu);
   const row_scale sc = scale_of(over_row<L>(top, buf, larger));
   if (here && j == 0) a.scale[z * a.rows + row] = sc.scale;
   int8_t* const to = a.codes + z * a.c_z + row * a.c_s;
@@ -223,8 +232,8 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void hdet_norm_kernel(const norm
     if (here && col < padded) {                     // columns behind the last are 0 in u (a row of registers is a multiple of 16 long)
       unsigned w[2] = {0u, 0u};
 #pragma unroll
-      for (int e = 0; e < 8; ++e) w[e >> 2] |= ((unsigned)code_of(u[c][e], sc.inverse) & 255u) << (8 * (e & 3));
-      *reinterpret_cast<hdet_u2v*>(to + col) = hdet_u2v{w[0], w[1]};
+      for (int e = 0; e < 8; ++e) w[e >> 2] |= (code_of(u[c][e], sc.inverse) & 255u) << (8 * (e & 3));
+      *reinterpret_cast<hdet_u2v*>(to + col) = sc.inverse == 0.f ? hdet_u2v{0u, 0u} : hdet_u2v{w[0], w[1]};      // rows that are not finite: codes 0
     }
   }
 }
@@ -248,7 +257,7 @@ template <typename T, int WHOLE, int L, int C>
 __global__ __launch_bounds__(L < 256 ? 256 : L) void hdet_norm_grad_kernel(const norm_grad_kernel_args a) {
   constexpr int THREADS = L < 256 ? 256 : L, RPB = THREADS / L, COLS = L * 8 * C;
   constexpr bool kGainInLds = COLS <= 8192;
-  __shared__ unsigned buf[16];
+  __shared__ float buf[16];
   __shared__ __attribute__((aligned(16))) float s_gain[kGainInLds ? COLS : 1];
   __shared__ float sums[RPB > 1 ? RPB * COLS : 1];
   const int j = threadIdx.x % L, sub = threadIdx.x / L, z = blockIdx.y;
@@ -406,6 +415,19 @@ __global__ __launch_bounds__(256) void hdet_restore_kernel(const int8_t* q, int6
   store_piece<WHOLE>(v + z * v_z + row * v_s + col, o, width - col);
 }
 
+// Rows of a bfloat16 matrix in rows of `pitch`, `copies` times: a thread takes 8 columns.  Grid: (ceil(rows * pieces / 256), replicas).
+template <int WHOLE>
+__global__ __launch_bounds__(256) void hdet_pad_rows_kernel(const uint16_t* x, int64_t x_s, int64_t x_z, int64_t rows, int width, uint16_t* out, int64_t pitch, int copies) {
+  const int64_t pieces = pitch >> 3, t = (int64_t)blockIdx.x * 256 + threadIdx.x, row = t / pieces, all = rows * pieces;
+  const int col = (int)(t - row * pieces) * 8;
+  if (row >= rows) return;
+  piece<uint16_t> v;
+  v.zero();
+  if (col < width) v.load<WHOLE>(x + blockIdx.y * x_z + row * x_s, col, width);
+  hdet_u4v* const to = reinterpret_cast<hdet_u4v*>(out) + blockIdx.y * copies * all + t;
+  for (int c = 0; c < copies; ++c) to[c * all] = v.w;
+}
+
 namespace {
 
 // Whether rows are whole 16-byte pieces of `size`-byte elements (8 of them) at 16-byte boundaries, or the matrix is absent
@@ -471,7 +493,7 @@ hipError_t hdet_launch_norm(const hdet_norm_args& a, hipStream_t s) {
   const int mode = mode_of(vec, each * a.n_replicas * a.rows * a.width);
   norm_kernel_args k = {a.x.dev, a.resid.dev, a.total.dev, a.y.dev, (int8_t*)a.codes.dev, a.scale_dev, a.rstd_dev, a.gain_dev,
                         a.x.row_stride, a.x.replica_stride, a.resid.row_stride, a.resid.replica_stride, a.total.row_stride, a.total.replica_stride,
-                        a.y.row_stride, a.y.replica_stride, a.codes.row_stride, a.codes.replica_stride, a.gain_stride, a.rows, a.width, (float)a.eps, 1.f / (float)a.width};
+                        a.y.row_stride, a.y.replica_stride, a.codes.row_stride, a.codes.replica_stride, a.gain_stride, a.rows, a.width, a.eps, 1.0 / (double)a.width};
   return a.dtype == HDET_TYPE_BF16 ? launch_norm_typed<uint16_t>(k, a.n_replicas, mode, true, s) : launch_norm_typed<float>(k, a.n_replicas, mode, true, s);
 }
 
@@ -498,6 +520,14 @@ hipError_t hdet_launch_restore(const hdet_codes_args& a, hipStream_t s) {
   else if (bf) go(&hdet_restore_kernel<uint16_t, kLoose>, (uint16_t*)a.values.dev);
   else if (vec) go(&hdet_restore_kernel<float, kWhole>, (float*)a.values.dev);
   else go(&hdet_restore_kernel<float, kLoose>, (float*)a.values.dev);
+  return hipGetLastError();
+}
+
+hipError_t hdet_launch_pad_rows(const hdet_rows& x, int n_replicas, int64_t rows, int width, uint16_t* out, int64_t pitch, int copies, hipStream_t s) {
+  const dim3 grid((unsigned)((rows * (pitch >> 3) + 255) / 256), n_replicas);
+  const uint16_t* from = (const uint16_t*)x.dev;
+  if (pieces_of_8(x, 2, width)) hipLaunchKernelGGL(hdet_pad_rows_kernel<kWhole>, grid, dim3(256), 0, s, from, x.row_stride, x.replica_stride, rows, width, out, pitch, copies);
+  else hipLaunchKernelGGL(hdet_pad_rows_kernel<kLoose>, grid, dim3(256), 0, s, from, x.row_stride, x.replica_stride, rows, width, out, pitch, copies);
   return hipGetLastError();
 }
 

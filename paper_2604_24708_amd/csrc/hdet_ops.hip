@@ -80,14 +80,16 @@ int entry(const char* name, F check, G launch) {
 int element(int dtype) { return dtype == HDET_TYPE_BF16 ? 2 : 4; }
 
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
-// workspace of the linear layer's gradients: X and W in bfloat16 (rows of whole 16-byte pieces), partial sums of dy
-struct linear_layout { int64_t pitch; size_t x, w, sum, total; };
+// Workspace of the linear layer's gradients: X and W in bfloat16, and dy where its rows are no whole 16-byte pieces, in rows of whole pieces; partial sums of dy
+struct linear_layout { int64_t pitch, dy_pitch; size_t x, w, dy, sum, total; };
 linear_layout linear_layout_of(int n, int64_t rows, int d_in, int d_out) {
   linear_layout l;
   l.pitch = (d_in + 7) & ~7;
+  l.dy_pitch = (d_out + 7) & ~7;
   l.x = 0;
   l.w = l.x + up256((size_t)n * rows * l.pitch * 2);
-  l.sum = l.w + up256((size_t)n * d_out * l.pitch * 2);
+  l.dy = l.w + up256((size_t)n * d_out * l.pitch * 2);
+  l.sum = l.dy + (l.dy_pitch != d_out ? up256((size_t)n * rows * l.dy_pitch * 2) : 0);
   l.total = l.sum + up256(hdet_row_sum_bytes(n, rows, d_out));
   return l;
 }
@@ -228,29 +230,42 @@ extern "C" int hdet_quantised_linear_backward(const hdet_linear_grad_args* a, vo
     }
     auto restored = [&](const hdet_rows& codes, const float* scale, int64_t rows, size_t at) {
       hdet_codes_args r = {};
-      r.n_replicas = n; r.dtype = HDET_TYPE_BF16; r.rows = rows; r.width = a->d_in;
+      r.n_replicas = n; r.dtype = HDET_TYPE_BF16; r.rows = rows; r.width = (int32_t)l.pitch;      // with the zeros behind a row's codes
       r.values = {ws + at, l.pitch, rows * l.pitch};
       r.codes = codes; r.scale_dev = const_cast<float*>(scale);
       return hdet_launch_restore(r, s);
     };
     if (a->db_dev && (e = hdet_launch_row_sum(a->dy, n, M, a->d_out, a->db_dev, a->db_stride, ws + l.sum, s)) != hipSuccess) return e;
+    hdet_rows dy = a->dy;
+    if (l.dy_pitch != a->d_out && (a->dx.dev || a->dw.dev)) {
+      if ((e = hdet_launch_pad_rows(a->dy, n, M, a->d_out, (uint16_t*)(ws + l.dy), l.dy_pitch, 1, s)) != hipSuccess) return e;
+      dy = {ws + l.dy, l.dy_pitch, M * l.dy_pitch};
+    }
+    // a result of any alignment takes an epilogue that writes at any element where the operands allow the fast path
+    auto product = [&](hdet_bgemm_args& g, bool a_kmajor, int epi, int any_epi) {
+      g.padded = true;
+      g.accum = (float*)ws; g.accum_ld = 4; g.accum_first = g.accum_last = true;      // (one piece: never touched)
+      g.n1 = g.n2 = 1;
+      const bool any = !hdet_bgemm_dma_eligible(g, a_kmajor, false, epi) && hdet_bgemm_dma_eligible(g, a_kmajor, false, any_epi);
+      return hdet_launch_bgemm(g, a_kmajor, false, any ? any_epi : epi, n, s);
+    };
     if (a->dx.dev) {
       if ((e = restored(a->w_codes, a->w_scale_dev, a->d_out, l.w)) != hipSuccess) return e;
       hdet_bgemm_args g = {};
-      g.a = (const uint16_t*)a->dy.dev; g.lda = a->dy.row_stride; g.a_s[0] = a->dy.replica_stride;
+      g.a = (const uint16_t*)dy.dev; g.lda = dy.row_stride; g.a_s[0] = dy.replica_stride;
       g.b = (const uint16_t*)(ws + l.w); g.ldb = l.pitch; g.b_s[0] = a->d_out * l.pitch;
       g.c = a->dx.dev; g.ldc = a->dx.row_stride; g.c_s[0] = a->dx.replica_stride;
       g.m = (int)M; g.n = a->d_in; g.k = a->d_out;
-      if ((e = hdet_launch_bgemm(g, true, false, HDET_EPI_BF16, n, s)) != hipSuccess) return e;
+      if ((e = product(g, true, HDET_EPI_BF16, HDET_EPI_ACCUM_BF16)) != hipSuccess) return e;
     }
     if (a->dw.dev) {
       if ((e = restored(a->codes, a->scale_dev, M, l.x)) != hipSuccess) return e;
       hdet_bgemm_args g = {};
-      g.a = (const uint16_t*)a->dy.dev; g.lda = a->dy.row_stride; g.a_s[0] = a->dy.replica_stride;
+      g.a = (const uint16_t*)dy.dev; g.lda = dy.row_stride; g.a_s[0] = dy.replica_stride;
       g.b = (const uint16_t*)(ws + l.x); g.ldb = l.pitch; g.b_s[0] = M * l.pitch;
       g.c = a->dw.dev; g.ldc = a->dw.row_stride; g.c_s[0] = a->dw.replica_stride;
       g.m = a->d_out; g.n = a->d_in; g.k = (int)M;
-      if ((e = hdet_launch_bgemm(g, false, false, HDET_EPI_F32, n, s)) != hipSuccess) return e;
+      if ((e = product(g, false, HDET_EPI_F32, HDET_EPI_SCALED_F32)) != hipSuccess) return e;
     }
     return hipSuccess;
   });

@@ -5,8 +5,9 @@
 // No more than `piece` classes of z and dz exist at a time: a first round forms each row's reference and sum of exponentials, a second forms z again,
 // dz from it, and with dz the piece's share of dh (added up in fp32) and its rows of dW and db.
 //
-//  * Where h and W are made of whole 16-byte chunks z never leaves the matrix cores' registers: one product leaves reference and sum of each tile's part of a row,
-//    a second dz (hdet_bgemm_walk_kernel).  Other operands take z through memory in fp32, by pieces that are smaller by as much.
+//  * Where h and W are made of whole 16-byte chunks -- copies are made of rows that are not -- z never leaves the matrix cores' registers: one product leaves reference and sum of each tile's part of a row,
+//    a second dz (hdet_bgemm_walk_kernel).  Rows of whole chunks at other boundaries take z through memory in fp32, by pieces that are smaller
+//    by as much.
 //  * Exponentials are exp2(z log2(e) - r) with r the whole number next to max log2(e): tiles and pieces refer to each other by exact powers of two.
 //  * dz is held as c dz = softmax - onehot and the products' results are divided by c: at a label it is next to -1, which a bfloat16 holds to 2^-9 of itself, where
 //    (softmax - onehot) / c lies anywhere between two powers of two (dh against 64 bits: 2.9e-3 of its norm with the division before the rounding).
@@ -31,7 +32,9 @@ struct vocab_layout {
   int small_piece;          // ... where it goes through memory
   int planes;               // bfloat16 parts of dz
   int64_t bias_pitch;
-  size_t inv, labels, ref, a, sum, zy, bias, dz, h3, acc, part, total;
+  int64_t width8;           // a row of h and W in whole 16-byte pieces
+  int h_copies;             // copies of h in such rows: three below each other beside three parts of dz, one where its own rows are no whole pieces
+  size_t inv, labels, ref, a, sum, zy, bias, dz, h, w, acc, part, total;
 };
 size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
 int64_t up8(int64_t x) { return (x + 7) & ~(int64_t)7; }
@@ -80,6 +83,8 @@ vocab_layout layout_of(int n, int64_t rows, int width, int classes, int dw_dtype
   size_t fit = room / a_class / 8 * 8;
   l.small_piece = fit < (size_t)l.piece ? (int)fit : l.piece;
   l.bias_pitch = up8(classes);
+  l.width8 = up8(width);
+  l.h_copies = l.planes == 3 ? 3 : l.width8 != width ? 1 : 0;
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t here = at; at += up(bytes); return here; };
   l.inv = take((size_t)n * 4);
@@ -90,8 +95,9 @@ vocab_layout layout_of(int n, int64_t rows, int width, int classes, int dw_dtype
   l.zy = take(all * 4);
   l.bias = take((size_t)n * l.bias_pitch * 4);
   l.dz = take(room);
-  l.h3 = take(l.planes == 3 ? all * 3 * width * 2 : 0);
-  l.acc = take(l.pieces > 1 || l.small_piece < l.piece ? all * width * 4 : 0);
+  l.h = take(all * l.h_copies * l.width8 * 2);
+  l.w = take(l.width8 != width ? (size_t)n * classes * l.width8 * 2 : 0);
+  l.acc = take(l.pieces > 1 || l.small_piece < l.piece ? all * l.width8 * 4 : 0);
   l.part = take((size_t)n * ((rows + kRowChunk - 1) / kRowChunk) * up8(l.piece) * 4);
   l.total = at;
   return l;
@@ -100,15 +106,14 @@ vocab_layout layout_of(int n, int64_t rows, int width, int classes, int dw_dtype
 struct prep_args {
   const int32_t* labels; int32_t* labels_out;
   const float* bias; int64_t bias_z; float* bias_out; int64_t bias_pitch;
-  const uint16_t* h; int64_t h_s, h_z; uint16_t* h3;
-  float *inv, *mean, *row_loss;
+  float *inv, *mean;
   int64_t rows;
-  int classes, width;
+  int classes;
 };
 
 }  // namespace
 
-// What a call starts with, [replica] on blockIdx.y: labels that name no class become -1; 1 / rows that count; bias in rows padded with -inf; three copies of h.
+// What a call starts with, [replica] on blockIdx.y: labels that name no class become -1; 1 / rows that count; bias in rows padded with -inf.
 __global__ __launch_bounds__(1024) void hdet_vocab_prep_kernel(const prep_args a) {
   const int z = blockIdx.y;
   const int64_t t = (int64_t)blockIdx.x * 1024 + threadIdx.x, step = (int64_t)gridDim.x * 1024;
@@ -116,24 +121,6 @@ __global__ __launch_bounds__(1024) void hdet_vocab_prep_kernel(const prep_args a
   for (int64_t i = t; i < a.rows; i += step) a.labels_out[z * a.rows + i] = (unsigned)lab[i] < (unsigned)a.classes ? lab[i] : -1;
   if (a.bias_out)
     for (int64_t i = t; i < a.bias_pitch; i += step) a.bias_out[z * a.bias_pitch + i] = i >= a.classes ? -INFINITY : a.bias ? a.bias[z * a.bias_z + i] : 0.f;
-  if (a.h3) {
-    uint16_t* out = a.h3 + z * 3 * a.rows * a.width;
-    if (((a.width | a.h_s | a.h_z) & 7) == 0 && (reinterpret_cast<uintptr_t>(a.h) & 15) == 0) {
-      const int64_t pieces = a.width / 8, all = a.rows * pieces;
-      for (int64_t i = t; i < all; i += step) {
-        const hdet_u4v v = *reinterpret_cast<const hdet_u4v*>(a.h + z * a.h_z + i / pieces * a.h_s + i % pieces * 8);
-#pragma unroll
-        for (int q = 0; q < 3; ++q) reinterpret_cast<hdet_u4v*>(out)[q * all + i] = v;
-      }
-    } else {
-      const int64_t all = a.rows * a.width;
-      for (int64_t i = t; i < all; i += step) {
-        const uint16_t v = a.h[z * a.h_z + i / a.width * a.h_s + i % a.width];
-#pragma unroll
-        for (int q = 0; q < 3; ++q) out[q * all + i] = v;
-      }
-    }
-  }
   if (blockIdx.x != 0) return;
   __shared__ int part[16];
   int n = 0;
@@ -340,8 +327,14 @@ hipError_t hdet_launch_vocab_loss(const hdet_vocab_args& a, hipStream_t s) {
   float* const bias = (float*)(ws + l.bias);
   int32_t* const labels = (int32_t*)(ws + l.labels);
   double* const sum = (double*)(ws + l.sum);
-  uint16_t* const h3 = (uint16_t*)(ws + l.h3);
-  const uint16_t *h = (const uint16_t*)a.h.dev, *w = (const uint16_t*)a.w.dev;
+  // operands of the products: the caller's, or copies in rows of whole pieces
+  hdet_rows h = a.h, w = a.w, hk = a.h;              // hk: what stands beside all parts of dz
+  if (l.h_copies) hk = {ws + l.h, l.width8, l.h_copies * M * l.width8};
+  if (l.width8 != d) {
+    h = hk;
+    w = {ws + l.w, l.width8, V * l.width8};
+  }
+  const uint16_t *hp = (const uint16_t*)h.dev, *wp = (const uint16_t*)w.dev;
   const bool grads = a.dh.dev || a.dw.dev || a.db_dev;
   const int chunks = (int)((M + kRowChunk - 1) / kRowChunk);
   hipError_t e;
@@ -349,9 +342,9 @@ hipError_t hdet_launch_vocab_loss(const hdet_vocab_args& a, hipStream_t s) {
   // z = h W^T + bias of the classes from v0 on; in tiles: bias padded
   auto product = [&](int v0, int cols, bool tiles) {
     hdet_bgemm_args g = {};
-    g.a = h; g.lda = a.h.row_stride; g.a_s[0] = a.h.replica_stride;
-    g.b = w + v0 * a.w.row_stride; g.ldb = a.w.row_stride; g.b_s[0] = a.w.replica_stride;
-    g.m = (int)M; g.n = cols; g.k = d; g.n1 = g.n2 = 1;
+    g.a = hp; g.lda = h.row_stride; g.a_s[0] = h.replica_stride;
+    g.b = wp + v0 * w.row_stride; g.ldb = w.row_stride; g.b_s[0] = w.replica_stride;
+    g.m = (int)M; g.n = cols; g.k = l.width8 != d ? (int)l.width8 : d; g.n1 = g.n2 = 1;      // (zeros behind a copy's rows)
     g.bias = tiles ? bias + v0 : a.bias_dev ? a.bias_dev + v0 : nullptr;
     g.bias_bs = tiles ? l.bias_pitch : a.bias_stride;
     g.padded = tiles;
@@ -364,10 +357,8 @@ hipError_t hdet_launch_vocab_loss(const hdet_vocab_args& a, hipStream_t s) {
   const int64_t pitch = up8(piece);
 
   {
-    prep_args p = {a.labels_dev, labels, a.bias_dev, a.bias_stride, tiles ? bias : nullptr, l.bias_pitch, h, a.h.row_stride, a.h.replica_stride,
-                   l.planes == 3 && M > 0 ? h3 : nullptr, inv, a.mean_loss_dev, a.row_loss_dev, M, V, d};
-    int64_t work = M > l.bias_pitch ? M : l.bias_pitch;
-    if (p.h3 && M * d / 8 > work) work = M * d / 8;
+    prep_args p = {a.labels_dev, labels, a.bias_dev, a.bias_stride, tiles ? bias : nullptr, l.bias_pitch, inv, a.mean_loss_dev, M, V};
+    const int64_t work = M > l.bias_pitch ? M : l.bias_pitch;
     int64_t blocks = (work + 1023) / 1024;
     if (blocks > 1024) blocks = 1024;
     hipLaunchKernelGGL(hdet_vocab_prep_kernel, dim3((unsigned)blocks, n), dim3(1024), 0, s, p);
@@ -377,6 +368,8 @@ hipError_t hdet_launch_vocab_loss(const hdet_vocab_args& a, hipStream_t s) {
     if (a.dw.dev && (e = hdet_launch_zero_rows(a.dw, n, V, d, a.dw_dtype, s)) != hipSuccess) return e;
     return a.db_dev ? hdet_launch_partial_sum(nullptr, n, 0, V, 0, a.db_dev, a.db_stride, s) : hipSuccess;
   }
+  if (l.h_copies && (l.width8 != d || a.dw.dev) && (e = hdet_launch_pad_rows(a.h, n, M, d, (uint16_t*)(ws + l.h), l.width8, l.h_copies, s)) != hipSuccess) return e;
+  if (l.width8 != d && (e = hdet_launch_pad_rows(a.w, n, V, d, (uint16_t*)(ws + l.w), l.width8, 1, s)) != hipSuccess) return e;
   float* const z = (float*)(ws + l.dz);
   uint16_t* const dz = (uint16_t*)(ws + l.dz + (tiles ? 0 : (size_t)n * M * pitch * 4));
   auto logits = [&](int v0, int cols) {
@@ -393,8 +386,8 @@ hipError_t hdet_launch_vocab_loss(const hdet_vocab_args& a, hipStream_t s) {
     if ((e = hdet_launch_vocab_stat(g, n, s)) != hipSuccess) return e;
     hipLaunchKernelGGL(hdet_vocab_merge_kernel, dim3((unsigned)((M + 63) / 64), n), dim3(256), 0, s, stats, (V + 255) / 256, M, labels, ref, ra, sum, a.row_loss_dev);
     if (!grads)
-      hipLaunchKernelGGL(hdet_vocab_label_kernel, dim3((unsigned)((M + 3) / 4), n), dim3(256), 0, s, h, a.h.row_stride, a.h.replica_stride, w, a.w.row_stride, a.w.replica_stride,
-                         bias, l.bias_pitch, labels, sum, M, d, a.row_loss_dev);
+      hipLaunchKernelGGL(hdet_vocab_label_kernel, dim3((unsigned)((M + 3) / 4), n), dim3(256), 0, s, hp, h.row_stride, h.replica_stride, wp, w.row_stride, w.replica_stride,
+                         bias, l.bias_pitch, labels, sum, M, (int)l.width8, a.row_loss_dev);
   } else {
     for (int p = 0; p < pieces; ++p) {
       const int v0 = p * piece, cols = V - v0 < piece ? V - v0 : piece;
@@ -432,10 +425,10 @@ hipError_t hdet_launch_vocab_loss(const hdet_vocab_args& a, hipStream_t s) {
     if (a.dh.dev) {
       hdet_bgemm_args g = {};
       g.a = dz; g.lda = pitch; g.a_s[0] = l.planes * M * pitch;
-      g.b = w + v0 * a.w.row_stride; g.ldb = a.w.row_stride; g.b_s[0] = a.w.replica_stride;
+      g.b = wp + v0 * w.row_stride; g.ldb = w.row_stride; g.b_s[0] = w.replica_stride;
       g.c = a.dh.dev; g.ldc = a.dh.row_stride; g.c_s[0] = a.dh.replica_stride;
       g.m = (int)M; g.n = d; g.k = cols;
-      g.accum = (float*)(ws + l.acc); g.accum_ld = d; g.accum_bs = M * d;
+      g.accum = (float*)(ws + l.acc); g.accum_ld = l.width8; g.accum_bs = M * l.width8;
       g.accum_first = p == 0; g.accum_last = last; g.out_scale = inv;
       g.padded = true;
       if ((e = hdet_launch_bgemm(g, true, false, HDET_EPI_ACCUM_BF16, n, s)) != hipSuccess) return e;
@@ -444,7 +437,7 @@ hipError_t hdet_launch_vocab_loss(const hdet_vocab_args& a, hipStream_t s) {
       const bool f32 = l.planes == 3;
       hdet_bgemm_args g = {};
       g.a = dz; g.lda = pitch; g.a_s[0] = l.planes * M * pitch;
-      g.b = f32 ? h3 : h; g.ldb = f32 ? d : a.h.row_stride; g.b_s[0] = f32 ? 3 * M * d : a.h.replica_stride;
+      g.b = (const uint16_t*)hk.dev; g.ldb = hk.row_stride; g.b_s[0] = hk.replica_stride;
       g.c = (char*)a.dw.dev + v0 * a.dw.row_stride * (f32 ? 4 : 2); g.ldc = a.dw.row_stride; g.c_s[0] = a.dw.replica_stride;
       g.m = cols; g.n = d; g.k = (int)(l.planes * M); g.out_scale = inv;
       g.padded = true;

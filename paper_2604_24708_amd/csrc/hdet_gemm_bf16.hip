@@ -695,7 +695,7 @@ hipError_t hdet_launch_bgemm(const hdet_bgemm_args& g_in, bool a_kmajor, bool b_
   if (g.n2 < 1) g.n2 = 1;
   // The LDS-direct kernel where the operands allow it, except for products of few tiles in the epilogues that the general kernels
   // have.  Weight gradients stay: the update that the LDS-direct kernel can apply to them (HDET_EPI_ADAMW) has to see the same sums.
-  const bool plain = epi <= HDET_EPI_BIAS_BF16 && !g.colsum && a_kmajor;
+  const bool plain = (epi <= HDET_EPI_BIAS_BF16 || epi == HDET_EPI_ACCUM_BF16) && !g.colsum && a_kmajor;
   // Forward products of up to two 64 x 64 tiles a CU, of one row or column of tiles up to one: their time is the chain of one block, and four times
   // the blocks of 128 x 128 count for more than loads that pass the registers by.  us, this file's kernel / LDS-direct, operands cold:
   // 200 x 1000, K = 3000, 2 items 23.5 / 42.7;  96 x 704, K = 1504, 6 items 16.8 / 25.4;  96 x 1504, K = 784 16.0 / 19.0;  128 x 1024, K = 1024,
@@ -723,6 +723,7 @@ hipError_t hdet_launch_bgemm(const hdet_bgemm_args& g_in, bool a_kmajor, bool b_
     if (epi == HDET_EPI_MASK_BF16) return launch_general<true, false, HDET_EPI_MASK_BF16>(g, batch, aligned, s);
     if (epi == HDET_EPI_BF16) return launch_general<true, false, HDET_EPI_BF16>(g, batch, aligned, s);
     if (epi == HDET_EPI_ACCUM_BF16) return launch_general<true, false, HDET_EPI_ACCUM_BF16>(g, batch, aligned, s);
+    if (epi == HDET_EPI_SCALED_F32) return launch_general<true, false, HDET_EPI_SCALED_F32>(g, batch, aligned, s);
     return hipErrorInvalidValue;
   }
   if (!b_kmajor) {                       // wgrad

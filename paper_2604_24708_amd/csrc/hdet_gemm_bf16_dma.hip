@@ -151,6 +151,12 @@ __device__ __forceinline__ tile_id tile_of_block(int tile_group) {
   return tile_of_index(blockIdx.x + gridDim.x * (blockIdx.y + gridDim.y * blockIdx.z), gridDim.x, gridDim.y, gridDim.x * gridDim.y * gridDim.z, tile_group);
 }
 
+// the contraction of a batch item (hdet_bgemm_args::k_last)
+template <int EPI>
+__device__ __forceinline__ int contraction_of(const hdet_bgemm_args& g, const hdet_batch_index& bi) {
+  return EPI == HDET_EPI_SCALED_F32 && g.k_last && bi.z1 + 1 == g.n1 ? g.k_last : g.k;
+}
+
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr double kLn2 = 0.6931471805599453;
 
@@ -382,6 +388,7 @@ void hdet_bgemm_dma_kernel(const hdet_bgemm_args g) {
   const tile_id id = tile_of_block(g.tile_group);
   const int bx = id.bx, by = id.by, bz = id.bz;
   const hdet_batch_index bi = hdet_split_batch(bz, g.n1, g.n2);
+  const int gk = contraction_of<EPI>(g, bi);
   const int z = bi.z0;            // replica: bias and mask are per replica
   const uint16_t* A = g.a + hdet_batch_offset(bi, g.a_s);
   const uint16_t* B = g.b + hdet_batch_offset(bi, g.b_s);
@@ -392,8 +399,8 @@ void hdet_bgemm_dma_kernel(const hdet_bgemm_args g) {
   const int wm = (wave / WGN) * (32 * WMT), wn = (wave % WGN) * (32 * WNT);
 
   // byte extent of each operand for this batch item: the bound that turns absent chunks into zeros (in whole chunks: hdet_bgemm_args::padded)
-  const uint32_t a_bytes = (uint32_t)(((int64_t)((A_KMAJOR ? g.m : g.k) - 1) * g.lda + (((A_KMAJOR ? g.k : g.m) + 7) & ~7)) * 2);
-  const uint32_t b_bytes = (uint32_t)(((int64_t)((B_KMAJOR ? g.n : g.k) - 1) * g.ldb + (((B_KMAJOR ? g.k : g.n) + 7) & ~7)) * 2);
+  const uint32_t a_bytes = (uint32_t)(((int64_t)((A_KMAJOR ? g.m : gk) - 1) * g.lda + (((A_KMAJOR ? gk : g.m) + 7) & ~7)) * 2);
+  const uint32_t b_bytes = (uint32_t)(((int64_t)((B_KMAJOR ? g.n : gk) - 1) * g.ldb + (((B_KMAJOR ? gk : g.n) + 7) & ~7)) * 2);
   const i4 ra = make_rsrc(A, a_bytes), rb = make_rsrc(B, b_bytes);
   const uint32_t s_addr = lds_addr_of(S);
 
@@ -410,16 +417,16 @@ void hdet_bgemm_dma_kernel(const hdet_bgemm_args g) {
 #pragma unroll
       for (int e = 0; e < BLK * BLK / 64; ++e) acc[i][j][e] = 0.f;
 
-  const int nk = (g.k + TK - 1) / TK;
+  const int nk = (gk + TK - 1) / TK;
 #define STAGE_PTR(s) (S + (s) * STAGE)
 #define STAGE_ADDR(s) (s_addr + (s) * STAGE * 2)
   // K steps 0 .. NST-1 are requested up front; steps past the end load nothing (all chunks absent)
 #pragma unroll
   for (int s = 0; s < NST; ++s) {
 #pragma unroll
-    for (int i = 0; i < ta::NI; ++i) la.issue_one(i, ra, STAGE_ADDR(s), s, g.k, wave);
+    for (int i = 0; i < ta::NI; ++i) la.issue_one(i, ra, STAGE_ADDR(s), s, gk, wave);
 #pragma unroll
-    for (int i = 0; i < tb::NI; ++i) lb.issue_one(i, rb, STAGE_ADDR(s) + TM * TK * 2, s, g.k, wave);
+    for (int i = 0; i < tb::NI; ++i) lb.issue_one(i, rb, STAGE_ADDR(s) + TM * TK * 2, s, gk, wave);
   }
   wait_and_barrier<(NST - 1) * LPT>();
 
@@ -464,8 +471,8 @@ void hdet_bgemm_dma_kernel(const hdet_bgemm_args g) {
 #pragma unroll
         for (int u = 0; u < IPB; ++u) {
           const int it = q * IPB + u;
-          if (it < ta::NI) la.issue_one(it, ra, STAGE_ADDR(s), kt + NST, g.k, wave);
-          else if (it < LPT) lb.issue_one(it - ta::NI, rb, STAGE_ADDR(s) + TM * TK * 2, kt + NST, g.k, wave);
+          if (it < ta::NI) la.issue_one(it, ra, STAGE_ADDR(s), kt + NST, gk, wave);
+          else if (it < LPT) lb.issue_one(it - ta::NI, rb, STAGE_ADDR(s) + TM * TK * 2, kt + NST, gk, wave);
           else read_frag(fa[0], fb[0], nxt, 0, it - LPT);
         }
         __builtin_amdgcn_sched_barrier(0);
@@ -532,6 +539,7 @@ __global__ __launch_bounds__(512, 2) void hdet_bgemm_alt_kernel(const hdet_bgemm
   typedef half_tile<B_KMAJOR, TN, false> tb;
   const tile_id id = tile_of_block(g.tile_group);
   const hdet_batch_index bi = hdet_split_batch(id.bz, g.n1, g.n2);
+  const int gk = contraction_of<EPI>(g, bi);
   const uint16_t* A = g.a + hdet_batch_offset(bi, g.a_s);
   const uint16_t* B = g.b + hdet_batch_offset(bi, g.b_s);
   const int64_t c_base = hdet_batch_offset(bi, g.c_s);
@@ -539,8 +547,8 @@ __global__ __launch_bounds__(512, 2) void hdet_bgemm_alt_kernel(const hdet_bgemm
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wn = (wave % WGN) * 64, hr = (wave / WGN) * 64;
-  const uint32_t a_bytes = (uint32_t)(((int64_t)((A_KMAJOR ? g.m : g.k) - 1) * g.lda + (((A_KMAJOR ? g.k : g.m) + 7) & ~7)) * 2);
-  const uint32_t b_bytes = (uint32_t)(((int64_t)((B_KMAJOR ? g.n : g.k) - 1) * g.ldb + (((B_KMAJOR ? g.k : g.n) + 7) & ~7)) * 2);
+  const uint32_t a_bytes = (uint32_t)(((int64_t)((A_KMAJOR ? g.m : gk) - 1) * g.lda + (((A_KMAJOR ? gk : g.m) + 7) & ~7)) * 2);
+  const uint32_t b_bytes = (uint32_t)(((int64_t)((B_KMAJOR ? g.n : gk) - 1) * g.ldb + (((B_KMAJOR ? gk : g.n) + 7) & ~7)) * 2);
   const i4 ra = make_rsrc(A, a_bytes), rb = make_rsrc(B, b_bytes);
   const uint32_t s_addr = lds_addr_of(S);
 
@@ -557,16 +565,16 @@ __global__ __launch_bounds__(512, 2) void hdet_bgemm_alt_kernel(const hdet_bgemm
     for (int j = 0; j < 4; ++j) acc[i][j] = f4{0.f, 0.f, 0.f, 0.f};
 
   // LDS, in units of 128 rows x 64: half h of A of stage s at 2 h + s, B at 4 + 2 s
-  const int nk = (g.k + TK - 1) / TK;
+  const int nk = (gk + TK - 1) / TK;
   auto load_a = [&](int h, int s, int kt) {
     const uint32_t at = s_addr + (2 * h + s) * HALF * 2;
 #pragma unroll
-    for (int i = 0; i < ta::NI; ++i) la[h].load(i, ra, at, kt, g.lda, ck + kt * TK < g.k, wave);
+    for (int i = 0; i < ta::NI; ++i) la[h].load(i, ra, at, kt, g.lda, ck + kt * TK < gk, wave);
   };
   auto load_b = [&](int s, int kt) {
     const uint32_t at = s_addr + (4 + 2 * s) * HALF * 2;
 #pragma unroll
-    for (int i = 0; i < tb::NI; ++i) lb.load(i, rb, at, kt, g.ldb, ck + kt * TK < g.k, wave);
+    for (int i = 0; i < tb::NI; ++i) lb.load(i, rb, at, kt, g.ldb, ck + kt * TK < gk, wave);
   };
   bf16x8 fa[2][4], fb[2][4];
   auto read_a = [&](int h, int s) {
@@ -1197,12 +1205,13 @@ bool hdet_bgemm_dma_eligible(const hdet_bgemm_args& g, bool a_kmajor, bool b_kma
        ((reinterpret_cast<uintptr_t>(g.upd.theta) | reinterpret_cast<uintptr_t>(g.upd.m) | reinterpret_cast<uintptr_t>(g.upd.v)) & 15) ||
        (reinterpret_cast<uintptr_t>(g.upd.shadow) & 7)))
     return false;
+  if (g.k_last && (epi != HDET_EPI_SCALED_F32 || g.k_last > g.k)) return false;
   if (epi == HDET_EPI_ACCUM_BF16 && (!g.accum || ((g.accum_ld | g.accum_bs) & 3) || (reinterpret_cast<uintptr_t>(g.accum) & 15) || g.n1 * g.n2 != 1)) return false;
   // instantiated combinations: what the MLP, the transformer and the loss in pieces use
   if (a_kmajor && b_kmajor)
     return epi == HDET_EPI_BIAS_RELU_BF16 || epi == HDET_EPI_BIAS_F32 || epi == HDET_EPI_BIAS_BF16 || epi == HDET_EPI_F32 ||
            epi == HDET_EPI_BIAS_GELU_BF16 || epi == HDET_EPI_BIAS_RESID_BF16 || epi == HDET_EPI_BIAS_DROP_RESID_BF16;
-  if (a_kmajor && !b_kmajor) return epi == HDET_EPI_MASK_BF16 || epi == HDET_EPI_BF16 || epi == HDET_EPI_GELUGRAD_BF16 || epi == HDET_EPI_ACCUM_BF16;
+  if (a_kmajor && !b_kmajor) return epi == HDET_EPI_MASK_BF16 || epi == HDET_EPI_BF16 || epi == HDET_EPI_GELUGRAD_BF16 || epi == HDET_EPI_ACCUM_BF16 || epi == HDET_EPI_SCALED_F32;
   if (!a_kmajor && !b_kmajor)
     return epi == HDET_EPI_F32 || epi == HDET_EPI_BF16 || epi == HDET_EPI_ADAMW || epi == HDET_EPI_SCALED_F32 || epi == HDET_EPI_SCALED_BF16;
   return false;
@@ -1229,6 +1238,7 @@ hipError_t hdet_launch_bgemm_dma(const hdet_bgemm_args& g_in, bool a_kmajor, boo
     if (epi == HDET_EPI_MASK_BF16) return launch_shape<true, false, HDET_EPI_MASK_BF16>(g, batch, s);
     if (epi == HDET_EPI_GELUGRAD_BF16) return launch_shape<true, false, HDET_EPI_GELUGRAD_BF16>(g, batch, s);
     if (epi == HDET_EPI_ACCUM_BF16) return launch_shape<true, false, HDET_EPI_ACCUM_BF16>(g, batch, s);
+    if (epi == HDET_EPI_SCALED_F32) return launch_shape<true, false, HDET_EPI_SCALED_F32>(g, batch, s);
     return launch_shape<true, false, HDET_EPI_BF16>(g, batch, s);
   }
   if (epi == HDET_EPI_F32) return launch_shape<false, false, HDET_EPI_F32>(g, batch, s);   // wgrad

@@ -211,6 +211,7 @@ struct hdet_bgemm_args {
   float* accum; int64_t accum_ld, accum_bs;   // HDET_EPI_ACCUM_BF16: accum[z0*accum_bs + m*accum_ld + n]; the first piece does not read it,
   bool accum_first, accum_last;               // the last writes c instead
   const float* out_scale;                     // [z0], or null
+  int k_last;              // LDS-direct kernels, HDET_EPI_SCALED_F32: where not 0, the contraction of the batch items with the last z1 (at most k)
   // Rows of A and B go on to a multiple of 8: with zeros in A (its chunks are read whole), with anything in B.  For HDET_EPI_XENT_* an n that is no multiple of 8:
   // bias goes on with -inf, and c with columns that may be written
   bool padded;

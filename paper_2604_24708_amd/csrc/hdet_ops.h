@@ -20,6 +20,18 @@ hipError_t hdet_launch_partial_sum(const float* partial, int n_replicas, int par
 // hdet_gemm_codes.hip
 hipError_t hdet_launch_codes_gemm(const hdet_linear_args& a, hipStream_t s);
 
+// hdet_split.hip: products (input-gradient or weight-gradient order) of few tiles and a long contraction
+struct hdet_split { int pieces; int64_t each; size_t bytes; };      // pieces of `each`, and the memory of their results (0: one piece, no split)
+struct hdet_split_out {
+  void* c; int dtype; int64_t ld, bs;                // result, HDET_TYPE_*, at any element
+  const float* scale;                                // [replica] or null
+  float* accum; int64_t accum_ld, accum_bs;          // as HDET_EPI_ACCUM_BF16, or null
+  bool first, last;
+};
+hdet_split hdet_split_of(int batch, int64_t m, int64_t n, int64_t k);
+// g: operands, m, n, k, padded; one batch level
+hipError_t hdet_launch_split(const hdet_bgemm_args& g, bool a_kmajor, int batch, const hdet_split& sp, float* partial, const hdet_split_out& out, hipStream_t s);
+
 // hdet_vocab.hip
 hipError_t hdet_launch_zero_rows(const hdet_rows& m, int n_replicas, int64_t rows, int width, int dtype, hipStream_t s);
 size_t hdet_vocab_bytes(int n_replicas, int64_t rows, int width, int classes, int dw_dtype, int piece);

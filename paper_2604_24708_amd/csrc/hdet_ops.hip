@@ -80,8 +80,9 @@ int entry(const char* name, F check, G launch) {
 int element(int dtype) { return dtype == HDET_TYPE_BF16 ? 2 : 4; }
 
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
-// Workspace of the linear layer's gradients: X and W in bfloat16, and dy where its rows are no whole 16-byte pieces, in rows of whole pieces; partial sums of dy
-struct linear_layout { int64_t pitch, dy_pitch; size_t x, w, dy, sum, total; };
+// Workspace of the linear layer's gradients: X and W in bfloat16, and dy where its rows are no whole 16-byte pieces, in rows of whole pieces; partial sums of dy,
+// results of pieces of a long contraction
+struct linear_layout { int64_t pitch, dy_pitch; hdet_split for_dx, for_dw; size_t x, w, dy, sum, part, total; };
 linear_layout linear_layout_of(int n, int64_t rows, int d_in, int d_out) {
   linear_layout l;
   l.pitch = (d_in + 7) & ~7;
@@ -90,7 +91,10 @@ linear_layout linear_layout_of(int n, int64_t rows, int d_in, int d_out) {
   l.w = l.x + up256((size_t)n * rows * l.pitch * 2);
   l.dy = l.w + up256((size_t)n * d_out * l.pitch * 2);
   l.sum = l.dy + (l.dy_pitch != d_out ? up256((size_t)n * rows * l.dy_pitch * 2) : 0);
-  l.total = l.sum + up256(hdet_row_sum_bytes(n, rows, d_out));
+  l.for_dx = hdet_split_of(n, rows, d_in, d_out);
+  l.for_dw = hdet_split_of(n, d_out, d_in, rows);
+  l.part = l.sum + up256(hdet_row_sum_bytes(n, rows, d_out));
+  l.total = l.part + (l.for_dx.bytes > l.for_dw.bytes ? l.for_dx.bytes : l.for_dw.bytes);
   return l;
 }
 void linear_sizes(checker& c, int n, int64_t rows, int d_in, int d_out) {
@@ -242,8 +246,10 @@ extern "C" int hdet_quantised_linear_backward(const hdet_linear_grad_args* a, vo
       dy = {ws + l.dy, l.dy_pitch, M * l.dy_pitch};
     }
     // a result of any alignment takes an epilogue that writes at any element where the operands allow the fast path
-    auto product = [&](hdet_bgemm_args& g, bool a_kmajor, int epi, int any_epi) {
+    auto product = [&](hdet_bgemm_args& g, bool a_kmajor, int epi, int any_epi, const hdet_split& sp) {
       g.padded = true;
+      if (sp.pieces > 1)
+        return hdet_launch_split(g, a_kmajor, n, sp, (float*)(ws + l.part), {g.c, a_kmajor ? HDET_TYPE_BF16 : HDET_TYPE_F32, g.ldc, g.c_s[0], nullptr, nullptr, 0, 0, true, true}, s);
       g.accum = (float*)ws; g.accum_ld = 4; g.accum_first = g.accum_last = true;      // (one piece: never touched)
       g.n1 = g.n2 = 1;
       const bool any = !hdet_bgemm_dma_eligible(g, a_kmajor, false, epi) && hdet_bgemm_dma_eligible(g, a_kmajor, false, any_epi);
@@ -256,7 +262,7 @@ extern "C" int hdet_quantised_linear_backward(const hdet_linear_grad_args* a, vo
       g.b = (const uint16_t*)(ws + l.w); g.ldb = l.pitch; g.b_s[0] = a->d_out * l.pitch;
       g.c = a->dx.dev; g.ldc = a->dx.row_stride; g.c_s[0] = a->dx.replica_stride;
       g.m = (int)M; g.n = a->d_in; g.k = a->d_out;
-      if ((e = product(g, true, HDET_EPI_BF16, HDET_EPI_ACCUM_BF16)) != hipSuccess) return e;
+      if ((e = product(g, true, HDET_EPI_BF16, HDET_EPI_ACCUM_BF16, l.for_dx)) != hipSuccess) return e;
     }
     if (a->dw.dev) {
       if ((e = restored(a->codes, a->scale_dev, M, l.x)) != hipSuccess) return e;
@@ -265,7 +271,7 @@ extern "C" int hdet_quantised_linear_backward(const hdet_linear_grad_args* a, vo
       g.b = (const uint16_t*)(ws + l.x); g.ldb = l.pitch; g.b_s[0] = M * l.pitch;
       g.c = a->dw.dev; g.ldc = a->dw.row_stride; g.c_s[0] = a->dw.replica_stride;
       g.m = a->d_out; g.n = a->d_in; g.k = (int)M;
-      if ((e = product(g, false, HDET_EPI_F32, HDET_EPI_SCALED_F32)) != hipSuccess) return e;
+      if ((e = product(g, false, HDET_EPI_F32, HDET_EPI_SCALED_F32, l.for_dw)) != hipSuccess) return e;
     }
     return hipSuccess;
   });

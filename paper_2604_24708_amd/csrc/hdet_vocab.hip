@@ -23,7 +23,7 @@ namespace {
 
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr double kLn2 = 0.6931471805599453, kLog2eD = 1.4426950408889634;
-constexpr int kRowChunk = 128;                          // rows of a block's column sums
+constexpr int kRowChunk = 128;                          // rows of a block's column sums in tiles
 constexpr size_t kPieceBytes = (size_t)1 << 30;         // most that dz of a piece takes where the caller does not say
 
 // Memory of a call, in the order it is carved.  What a member names: [replica][...].
@@ -34,10 +34,23 @@ struct vocab_layout {
   int64_t bias_pitch;
   int64_t width8;           // a row of h and W in whole 16-byte pieces
   int h_copies;             // copies of h in such rows: three below each other beside three parts of dz, one where its own rows are no whole pieces
-  size_t inv, labels, ref, a, sum, zy, bias, dz, h, w, acc, part, total;
+  size_t inv, labels, ref, a, sum, zy, bias, dz, h, w, acc, part, split, split_bytes, total;
 };
 size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
 int64_t up8(int64_t x) { return (x + 7) & ~(int64_t)7; }
+// rows of a block of hdet_vocab_grad_kernel: 128, fewer until there are two blocks a compute unit
+int rows_each(int n, int64_t rows, int cols) {
+  int each = 128;
+  while (each > 16 && (rows + each - 1) / each * ((cols + 1023) / 1024) * n < 2 * hdet_compute_units()) each >>= 1;
+  return each;
+}
+// Whether z goes through memory also where it could stay in the matrix cores' registers: up to a tile of 256 x 256 on every fourth compute unit, where a tile's long way from the first
+// load to the last store (12 us for its statistics, 18 for dz in three parts) counts for more than the passes over z, and up to 8192 classes, whose rows the statistics walk one
+// block each.  us of the call, registers / memory (tiles):  4 x 128 rows of 64, 512 classes, fp32 dW (8) 51 / 37;  3 x 159 of 896, 523 (9) 78 / 49;  4 x 256 of 1024, 2048 (32) 101 / 75;
+// 1024 of 512, 4096 (64) 100 / 85;  256 of 512, 16384 (64) 95 / 107;  100 of 90, 9600 (38) 63 / 66;  2 x 512 of 256, 8192 (128) 85 / 169
+bool small_call(int n, int64_t rows, int classes) {
+  return classes <= 8192 && 4 * ((rows + 255) / 256 * ((classes + 255) / 256) * n) <= hdet_compute_units();
+}
 
 // Classes at a time.  A piece's dW is one product with the rows as its contraction: it wants whole rounds of 256 x 256 tiles over the compute units, and every piece costs
 // about a twelfth of a round in launches, first loads and passes over the sum of dh.  us, by classes a piece (rounds of each):
@@ -98,7 +111,19 @@ vocab_layout layout_of(int n, int64_t rows, int width, int classes, int dw_dtype
   l.h = take(all * l.h_copies * l.width8 * 2);
   l.w = take(l.width8 != width ? (size_t)n * classes * l.width8 * 2 : 0);
   l.acc = take(l.pieces > 1 || l.small_piece < l.piece ? all * l.width8 * 4 : 0);
-  l.part = take((size_t)n * ((rows + kRowChunk - 1) / kRowChunk) * up8(l.piece) * 4);
+  size_t part = (size_t)n * ((rows + kRowChunk - 1) / kRowChunk) * up8(l.piece);
+  for (const int cols : {l.small_piece, classes - (classes + l.small_piece - 1) / l.small_piece * l.small_piece + l.small_piece}) {
+    const int each = rows_each(n, rows, cols);
+    const size_t want = (size_t)n * ((rows + each - 1) / each) * up8(cols);
+    if (want > part) part = want;
+  }
+  l.part = take(part * 4);
+  // results of pieces of a long contraction: the most that a piece of either kind may take
+  l.split_bytes = 0;
+  for (const int cols : {l.piece, classes - (l.pieces - 1) * l.piece, l.small_piece, classes - (classes + l.small_piece - 1) / l.small_piece * l.small_piece + l.small_piece})
+    for (const hdet_split& sp : {hdet_split_of(n, rows, width, cols), hdet_split_of(n, cols, width, l.planes * rows)})
+      if (sp.bytes > l.split_bytes) l.split_bytes = sp.bytes;
+  l.split = take(l.split_bytes);
   l.total = at;
   return l;
 }
@@ -106,6 +131,7 @@ vocab_layout layout_of(int n, int64_t rows, int width, int classes, int dw_dtype
 struct prep_args {
   const int32_t* labels; int32_t* labels_out;
   const float* bias; int64_t bias_z; float* bias_out; int64_t bias_pitch;
+  const uint16_t* h; int64_t h_s, h_z; uint16_t* h_out; int width, copies;      // rows of whole 16-byte pieces
   float *inv, *mean;
   int64_t rows;
   int classes;
@@ -113,7 +139,8 @@ struct prep_args {
 
 }  // namespace
 
-// What a call starts with, [replica] on blockIdx.y: labels that name no class become -1; 1 / rows that count; bias in rows padded with -inf.
+// What a call starts with, [replica] on blockIdx.y: labels that name no class become -1; 1 / rows that count; bias in rows padded with -inf; copies of h below
+// each other.
 __global__ __launch_bounds__(1024) void hdet_vocab_prep_kernel(const prep_args a) {
   const int z = blockIdx.y;
   const int64_t t = (int64_t)blockIdx.x * 1024 + threadIdx.x, step = (int64_t)gridDim.x * 1024;
@@ -121,6 +148,14 @@ __global__ __launch_bounds__(1024) void hdet_vocab_prep_kernel(const prep_args a
   for (int64_t i = t; i < a.rows; i += step) a.labels_out[z * a.rows + i] = (unsigned)lab[i] < (unsigned)a.classes ? lab[i] : -1;
   if (a.bias_out)
     for (int64_t i = t; i < a.bias_pitch; i += step) a.bias_out[z * a.bias_pitch + i] = i >= a.classes ? -INFINITY : a.bias ? a.bias[z * a.bias_z + i] : 0.f;
+  if (a.h_out) {
+    const int64_t pieces = a.width / 8, all = a.rows * pieces;
+    hdet_u4v* const out = reinterpret_cast<hdet_u4v*>(a.h_out) + z * a.copies * all;
+    for (int64_t i = t; i < all; i += step) {
+      const hdet_u4v v = *reinterpret_cast<const hdet_u4v*>(a.h + z * a.h_z + i / pieces * a.h_s + i % pieces * 8);
+      for (int q = 0; q < a.copies; ++q) out[q * all + i] = v;
+    }
+  }
   if (blockIdx.x != 0) return;
   __shared__ int part[16];
   int n = 0;
@@ -138,9 +173,9 @@ __global__ __launch_bounds__(1024) void hdet_vocab_prep_kernel(const prep_args a
   }
 }
 
-// Reference and sum of a row over the classes so far, and its label's logit.  Block = one row of a piece; grid (rows, replicas).
+// Reference and sum of a row over the classes so far, and its label's logit; after the last piece its loss.  Block = one row of a piece; grid (rows, replicas).
 __global__ __launch_bounds__(256) void hdet_vocab_stat_kernel(const float* z, int64_t pitch, int64_t rows, int cols, int v0, const int32_t* labels, float* ref,
-                                                              double* sum, float* zy) {
+                                                              double* sum, float* zy, bool last, float* a_out, float* row_loss) {
   __shared__ float part[4];
   const int64_t row = blockIdx.x, at = (int64_t)blockIdx.y * rows + row;
   const float* p = z + at * pitch;
@@ -158,33 +193,29 @@ __global__ __launch_bounds__(256) void hdet_vocab_stat_kernel(const float* z, in
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = s;
   __syncthreads();
   if (threadIdx.x == 0) {
-    s = (part[0] + part[1]) + (part[2] + part[3]);
     const int y = labels[at] - v0;
-    if ((unsigned)y < (unsigned)cols) zy[at] = p[y];
-    if (v0 == 0) {
-      ref[at] = r;
-      sum[at] = (double)s;
-    } else {
-      const float r0 = ref[at], top = fmaxf(r0, r);
+    float top = r, ly = (unsigned)y < (unsigned)cols ? p[y] : 0.f;
+    double all = (double)((part[0] + part[1]) + (part[2] + part[3]));
+    if (v0 != 0) {
+      const float r0 = ref[at];
+      top = fmaxf(r0, r);
       // a side without classes has the sum 0 (or NaN) and no reference
-      const double a = r0 == -INFINITY ? sum[at] : sum[at] * (double)__builtin_amdgcn_exp2f(r0 - top);
-      const double b = r == -INFINITY ? (double)s : (double)(s * __builtin_amdgcn_exp2f(r - top));
-      ref[at] = top;
-      sum[at] = a + b;
+      all = (r0 == -INFINITY ? sum[at] : sum[at] * (double)__builtin_amdgcn_exp2f(r0 - top)) + (r == -INFINITY ? all : all * (double)__builtin_amdgcn_exp2f(r - top));
+      if ((unsigned)y >= (unsigned)cols) ly = zy[at];
+    }
+    ref[at] = top;
+    if (last) {      // the row's loss and the factor of its exponentials in dz
+      const bool counts = labels[at] >= 0;
+      a_out[at] = counts ? (float)(1.0 / all) : 0.f;
+      row_loss[at] = counts ? (float)(((double)top + log2(all) - (double)ly * kLog2eD) * kLn2) : 0.f;
+    } else {
+      sum[at] = all;
+      zy[at] = ly;
     }
   }
 }
 
-// A row's loss and the factor of its exponentials in dz
-__global__ __launch_bounds__(256) void hdet_vocab_rows_kernel(const float* ref, const double* sum, const float* zy, const int32_t* labels, int64_t rows, float* a, float* row_loss) {
-  const int64_t row = (int64_t)blockIdx.x * 256 + threadIdx.x, at = blockIdx.y * rows + row;
-  if (row >= rows) return;
-  const bool counts = labels[at] >= 0;
-  a[at] = counts ? (float)(1.0 / sum[at]) : 0.f;
-  row_loss[at] = counts ? (float)(((double)ref[at] + log2(sum[at]) - (double)zy[at] * kLog2eD) * kLn2) : 0.f;
-}
-
-// The same from the column tiles' references and sums ([replica][tile][row]); lse: log2 of the sum of exp2(z log2(e)).  Rows that do not count: loss and factor 0.
+// What it leaves after the last piece, from the column tiles' references and sums ([replica][tile][row]); lse: log2 of the sum of exp2(z log2(e)).  Rows that do not count: loss and factor 0.
 // Block = 64 rows x 4 phases; phase q takes tiles q, q + 4, ..., the phases are added in their order, in 64 bits.
 __global__ __launch_bounds__(256) void hdet_vocab_merge_kernel(const float2* part, int tiles, int64_t rows, const int32_t* labels, float* ref, float* a, double* lse, float* row_loss) {
   __shared__ float refs[4][64];
@@ -242,33 +273,38 @@ __global__ __launch_bounds__(256) void hdet_vocab_label_kernel(const uint16_t* h
   if (lane == 0) row_loss[at] = (float)((lse[at] - (double)s * kLog2eD) * kLn2);
 }
 
-// c dz of a piece from z, in PLANES bfloat16 parts, and its sums over 128 rows.  Thread = a column; grid (ceil(pitch / 256), row chunks, replicas).
+// c dz of a piece from z, in PLANES bfloat16 parts, and its sums over `each` rows.  Thread = 4 columns; grid (ceil(pitch / 1024), row blocks, replicas).
 template <int PLANES>
-__global__ __launch_bounds__(256) void hdet_vocab_grad_kernel(const float* z, int64_t pitch, int64_t rows, int cols, int v0, const int32_t* labels, const float* ref,
+__global__ __launch_bounds__(256) void hdet_vocab_grad_kernel(const float* z, int64_t pitch, int64_t rows, int each, int cols, int v0, const int32_t* labels, const float* ref,
                                                               const float* a, uint16_t* dz, float* part, int64_t part_pitch) {
-  const int c = blockIdx.x * 256 + threadIdx.x, zr = blockIdx.z;
+  const int c = (blockIdx.x * 256 + threadIdx.x) * 4, zr = blockIdx.z;
   if (c >= pitch) return;
-  const int64_t r0 = (int64_t)blockIdx.y * kRowChunk, r1 = r0 + kRowChunk < rows ? r0 + kRowChunk : rows;
-  float sum = 0.f;
+  const int64_t r0 = (int64_t)blockIdx.y * each, r1 = r0 + each < rows ? r0 + each : rows;
+  hdet_f4v sum = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
   for (int64_t r = r0; r < r1; ++r) {
     const int64_t at = zr * rows + r;
-    float v = 0.f;
-    if (c < cols) {
-      const float x = z[at * pitch + c], f = a[at];
-      if (f != 0.f) v = __builtin_amdgcn_exp2f(__builtin_fmaf(x, kLog2e, -ref[at])) * f;
-      if (c == labels[at] - v0) v -= 1.f;
+    const hdet_f4v x = *reinterpret_cast<const hdet_f4v*>(z + at * pitch + c);
+    const float f = a[at], rf = ref[at];
+    const int y = labels[at] - v0 - c;
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      v[e] = f != 0.f ? __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], kLog2e, -rf)) * f : 0.f;      // (rows that do not count: 0 whatever z is)
+      if (e == y) v[e] -= 1.f;
+      if (c + e >= cols) v[e] = 0.f;
+      sum[e] += v[e];
     }
-    sum += v;
     uint16_t* p = dz + ((int64_t)zr * PLANES * rows + r) * pitch + c;
 #pragma unroll
     for (int q = 0; q < PLANES; ++q) {
-      const unsigned b = hdet_bf16_bits(v);
-      p[q * rows * pitch] = (uint16_t)b;
-      v -= __uint_as_float(b << 16);
+      const hdet_u2v b = {hdet_bf16_pack(v[0], v[1]), hdet_bf16_pack(v[2], v[3])};
+      *reinterpret_cast<hdet_u2v*>(p + q * rows * pitch) = b;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] -= __uint_as_float(e & 1 ? b[e >> 1] & 0xffff0000u : b[e >> 1] << 16);
     }
   }
-  if (part && c < part_pitch) part[((int64_t)zr * gridDim.y + blockIdx.y) * part_pitch + c] = sum;
+  if (part && c < part_pitch) *reinterpret_cast<hdet_f4v*>(part + ((int64_t)zr * gridDim.y + blockIdx.y) * part_pitch + c) = sum;
 }
 
 // db of a piece from its column sums, 64 columns x 4 phases a block; the last block column, where row_loss is given: the mean loss.  Grid (blocks, replicas).
@@ -336,7 +372,6 @@ hipError_t hdet_launch_vocab_loss(const hdet_vocab_args& a, hipStream_t s) {
   }
   const uint16_t *hp = (const uint16_t*)h.dev, *wp = (const uint16_t*)w.dev;
   const bool grads = a.dh.dev || a.dw.dev || a.db_dev;
-  const int chunks = (int)((M + kRowChunk - 1) / kRowChunk);
   hipError_t e;
 
   // z = h W^T + bias of the classes from v0 on; in tiles: bias padded
@@ -352,13 +387,19 @@ hipError_t hdet_launch_vocab_loss(const hdet_vocab_args& a, hipStream_t s) {
     g.xent.invb = 1.f; g.xent.label0 = v0;
     return g;
   };
-  const bool tiles = M > 0 && hdet_vocab_tiles_eligible(product(0, V, true));
+  const bool tiles = M > 0 && !small_call(n, M, V) && hdet_vocab_tiles_eligible(product(0, V, true));
   const int piece = tiles ? l.piece : l.small_piece, pieces = (V + piece - 1) / piece;
   const int64_t pitch = up8(piece);
 
+  bool copied;
   {
-    prep_args p = {a.labels_dev, labels, a.bias_dev, a.bias_stride, tiles ? bias : nullptr, l.bias_pitch, inv, a.mean_loss_dev, M, V};
-    const int64_t work = M > l.bias_pitch ? M : l.bias_pitch;
+    // (copies of rows that are no whole pieces take a launch of their own)
+    const bool copy = l.h_copies && l.width8 == d && M > 0 && ((a.h.row_stride | a.h.replica_stride) & 7) == 0 && (reinterpret_cast<uintptr_t>(a.h.dev) & 15) == 0;
+    const prep_args p = {a.labels_dev, labels, a.bias_dev, a.bias_stride, tiles ? bias : nullptr, l.bias_pitch, (const uint16_t*)a.h.dev, a.h.row_stride, a.h.replica_stride,
+                         copy ? (uint16_t*)(ws + l.h) : nullptr, d, l.h_copies, inv, a.mean_loss_dev, M, V};
+    int64_t work = M > l.bias_pitch ? M : l.bias_pitch;
+    if (copy && M * d / 8 > work) work = M * d / 8;
+    copied = copy;
     int64_t blocks = (work + 1023) / 1024;
     if (blocks > 1024) blocks = 1024;
     hipLaunchKernelGGL(hdet_vocab_prep_kernel, dim3((unsigned)blocks, n), dim3(1024), 0, s, p);
@@ -368,7 +409,7 @@ hipError_t hdet_launch_vocab_loss(const hdet_vocab_args& a, hipStream_t s) {
     if (a.dw.dev && (e = hdet_launch_zero_rows(a.dw, n, V, d, a.dw_dtype, s)) != hipSuccess) return e;
     return a.db_dev ? hdet_launch_partial_sum(nullptr, n, 0, V, 0, a.db_dev, a.db_stride, s) : hipSuccess;
   }
-  if (l.h_copies && (l.width8 != d || a.dw.dev) && (e = hdet_launch_pad_rows(a.h, n, M, d, (uint16_t*)(ws + l.h), l.width8, l.h_copies, s)) != hipSuccess) return e;
+  if (l.h_copies && !copied && (e = hdet_launch_pad_rows(a.h, n, M, d, (uint16_t*)(ws + l.h), l.width8, l.h_copies, s)) != hipSuccess) return e;
   if (l.width8 != d && (e = hdet_launch_pad_rows(a.w, n, V, d, (uint16_t*)(ws + l.w), l.width8, 1, s)) != hipSuccess) return e;
   float* const z = (float*)(ws + l.dz);
   uint16_t* const dz = (uint16_t*)(ws + l.dz + (tiles ? 0 : (size_t)n * M * pitch * 4));
@@ -392,9 +433,8 @@ hipError_t hdet_launch_vocab_loss(const hdet_vocab_args& a, hipStream_t s) {
     for (int p = 0; p < pieces; ++p) {
       const int v0 = p * piece, cols = V - v0 < piece ? V - v0 : piece;
       if ((e = logits(v0, cols)) != hipSuccess) return e;
-      hipLaunchKernelGGL(hdet_vocab_stat_kernel, dim3((unsigned)M, n), dim3(256), 0, s, z, pitch, M, cols, v0, labels, ref, sum, zy);
+      hipLaunchKernelGGL(hdet_vocab_stat_kernel, dim3((unsigned)M, n), dim3(256), 0, s, z, pitch, M, cols, v0, labels, ref, sum, zy, p + 1 == pieces, ra, a.row_loss_dev);
     }
-    hipLaunchKernelGGL(hdet_vocab_rows_kernel, dim3((unsigned)((M + 255) / 256), n), dim3(256), 0, s, ref, sum, zy, labels, M, ra, a.row_loss_dev);
   }
   if ((e = hipGetLastError()) != hipSuccess) return e;
 
@@ -402,6 +442,7 @@ hipError_t hdet_launch_vocab_loss(const hdet_vocab_args& a, hipStream_t s) {
   for (int p = 0; p < pieces && grads; ++p) {
     const int v0 = p * piece, cols = V - v0 < piece ? V - v0 : piece;
     const int64_t part_pitch = (cols + 3) & ~3;
+    const int each = tiles ? kRowChunk : rows_each(n, M, cols), chunks = (int)((M + each - 1) / each);
     if (tiles) {
       hdet_bgemm_args g = product(v0, cols, true);
       g.c = dz; g.ldc = pitch; g.c_s[0] = l.planes * M * pitch;
@@ -409,10 +450,10 @@ hipError_t hdet_launch_vocab_loss(const hdet_vocab_args& a, hipStream_t s) {
       if ((e = hdet_launch_vocab_grad(g, l.planes, n, s)) != hipSuccess) return e;
     } else {
       if (pieces > 1 && (e = logits(v0, cols)) != hipSuccess) return e;
-      const dim3 grid((unsigned)((pitch + 255) / 256), chunks, n);
+      const dim3 grid((unsigned)((pitch + 1023) / 1024), chunks, n);
       float* const to = a.db_dev ? part : nullptr;
-      if (l.planes == 3) hipLaunchKernelGGL(hdet_vocab_grad_kernel<3>, grid, dim3(256), 0, s, z, pitch, M, cols, v0, labels, ref, ra, dz, to, part_pitch);
-      else hipLaunchKernelGGL(hdet_vocab_grad_kernel<1>, grid, dim3(256), 0, s, z, pitch, M, cols, v0, labels, ref, ra, dz, to, part_pitch);
+      if (l.planes == 3) hipLaunchKernelGGL(hdet_vocab_grad_kernel<3>, grid, dim3(256), 0, s, z, pitch, M, each, cols, v0, labels, ref, ra, dz, to, part_pitch);
+      else hipLaunchKernelGGL(hdet_vocab_grad_kernel<1>, grid, dim3(256), 0, s, z, pitch, M, each, cols, v0, labels, ref, ra, dz, to, part_pitch);
       if ((e = hipGetLastError()) != hipSuccess) return e;
     }
     const bool last = p + 1 == pieces;
@@ -431,7 +472,13 @@ hipError_t hdet_launch_vocab_loss(const hdet_vocab_args& a, hipStream_t s) {
       g.accum = (float*)(ws + l.acc); g.accum_ld = l.width8; g.accum_bs = M * l.width8;
       g.accum_first = p == 0; g.accum_last = last; g.out_scale = inv;
       g.padded = true;
-      if ((e = hdet_launch_bgemm(g, true, false, HDET_EPI_ACCUM_BF16, n, s)) != hipSuccess) return e;
+      const hdet_split sp = hdet_split_of(n, M, d, cols);
+      if (sp.pieces > 1) {
+        if ((e = hdet_launch_split(g, true, n, sp, (float*)(ws + l.split), {g.c, HDET_TYPE_BF16, g.ldc, g.c_s[0], inv, g.accum, g.accum_ld, g.accum_bs, p == 0, last}, s)) != hipSuccess)
+          return e;
+      } else if ((e = hdet_launch_bgemm(g, true, false, HDET_EPI_ACCUM_BF16, n, s)) != hipSuccess) {
+        return e;
+      }
     }
     if (a.dw.dev) {
       const bool f32 = l.planes == 3;
@@ -441,7 +488,12 @@ hipError_t hdet_launch_vocab_loss(const hdet_vocab_args& a, hipStream_t s) {
       g.c = (char*)a.dw.dev + v0 * a.dw.row_stride * (f32 ? 4 : 2); g.ldc = a.dw.row_stride; g.c_s[0] = a.dw.replica_stride;
       g.m = cols; g.n = d; g.k = (int)(l.planes * M); g.out_scale = inv;
       g.padded = true;
-      if ((e = hdet_launch_bgemm(g, false, false, f32 ? HDET_EPI_SCALED_F32 : HDET_EPI_SCALED_BF16, n, s)) != hipSuccess) return e;
+      const hdet_split sp = hdet_split_of(n, cols, d, l.planes * M);
+      if (sp.pieces > 1) {
+        if ((e = hdet_launch_split(g, false, n, sp, (float*)(ws + l.split), {g.c, a.dw_dtype, g.ldc, g.c_s[0], inv, nullptr, 0, 0, true, true}, s)) != hipSuccess) return e;
+      } else if ((e = hdet_launch_bgemm(g, false, false, f32 ? HDET_EPI_SCALED_F32 : HDET_EPI_SCALED_BF16, n, s)) != hipSuccess) {
+        return e;
+      }
     }
   }
   if (!grads) {

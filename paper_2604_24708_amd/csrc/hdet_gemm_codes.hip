@@ -156,8 +156,8 @@ void hdet_codes_gemm_kernel(const codes_args g) {
 //    fragments and requests a later K step; the block's barriers hand the matrix cores over.  A K step of 128 bytes is two such turns: rows 0-63 of the wavefront, then rows
 //    64-127 with the column fragments still in registers.  Two stages of 64 KiB; each turn waits for all but the newest eight of its loads.
 //  * The next tile's first two K steps are requested in the last two of the tile before; its scales and bias come into LDS a tile ahead.
-//  * Results leave from the registers.  Stores are always issued -- what does not exist lies outside the descriptor -- and the next tile's first K step waits for the loads before
-//    them, not for them.
+//  * Results leave from the registers.  Stores are always issued -- what does not exist lies outside the descriptor.  The next tile's first two K steps are requested before them, and its
+//    first three turns wait for those loads, not for the stores.
 //  * Rows and columns past the matrices are zeros in the loop, and their results are not stored.
 template <typename OUT>
 __global__ __launch_bounds__(512, 2) void hdet_codes_walk_kernel(const codes_args g, unsigned gx, unsigned gy, unsigned total, int tile_group) {
@@ -309,7 +309,7 @@ __global__ __launch_bounds__(512, 2) void hdet_codes_walk_kernel(const codes_arg
   int slot = 0;
   load_side(cur, 0);
   load_a(cur.ra, 0, 0, 0); load_b(cur.rb, 0, 0); load_a(cur.ra, 1, 0, 0);
-  load_a(cur.ra, 0, 1, 1); load_b(cur.rb, 1, 1);
+  load_a(cur.ra, 0, 1, 1); load_b(cur.rb, 1, 1); load_a(cur.ra, 1, 1, 1);
   wait_and_barrier<8>();
   if (wave >= 4) meet();
   for (bool begun = false;; begun = true) {
@@ -320,14 +320,17 @@ __global__ __launch_bounds__(512, 2) void hdet_codes_walk_kernel(const codes_arg
       for (int s = 0; s < 2; ++s) {
         const int kt = kt0 + s;
         const bool fs = first && s == 0;
-        auto wait = [&] {
-          if (fs && begun) wait_and_barrier<8 + kStores>();
+        // all but the newest eight loads; in a tile's first three turns those are older than the stores of the tile before, which need not be done
+        auto wait = [&](bool early) {
+          if (early && begun) wait_and_barrier<8 + kStores>();
           else wait_and_barrier<8>();
         };
         read_a(0, s);
         read_b(s);
-        if (first || kt + 1 < nk) load_a(cur.ra, 1, s ^ 1, kt + 1); else load_a(nxt.ra, 1, s ^ 1, 0);
-        wait();
+        if (!fs) {                                               // (the first step's has been requested before the stores)
+          if (first || kt + 1 < nk) load_a(cur.ra, 1, s ^ 1, kt + 1); else load_a(nxt.ra, 1, s ^ 1, 0);
+        }
+        wait(first);
         multiply(0, fs);
         meet();
         read_a(1, s);
@@ -338,7 +341,7 @@ __global__ __launch_bounds__(512, 2) void hdet_codes_walk_kernel(const codes_arg
           nxt = tile_at(t);
         }
         if (first && s == 1) load_side(nxt, slot ^ 1);
-        wait();
+        wait(fs);
         multiply(1, fs);
         if (s == 0) meet();
       }
@@ -347,6 +350,7 @@ __global__ __launch_bounds__(512, 2) void hdet_codes_walk_kernel(const codes_arg
     for (int kt0 = 2; kt0 < nk; kt0 += 2) { meet(); pair(kt0, false); }
     // the first group ends its tile under the second's last products, the second at once
     if (wave < 4) meet();
+    load_a(nxt.ra, 1, 1, 1);       // both groups have read what it goes over
     finish(cur, slot);
     if (wave >= 4) meet();
     if (t >= total) break;

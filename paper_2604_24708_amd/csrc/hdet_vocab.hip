@@ -41,7 +41,7 @@ int64_t up8(int64_t x) { return (x + 7) & ~(int64_t)7; }
 // rows of a block of hdet_vocab_grad_kernel: 128, fewer until there are two blocks a compute unit
 int rows_each(int n, int64_t rows, int cols) {
   int each = 128;
-  while (each > 16 && (rows + each - 1) / each * ((cols + 1023) / 1024) * n < 2 * hdet_compute_units()) each >>= 1;
+  while (each > 4 && (rows + each - 1) / each * ((cols + 1023) / 1024) * n < 2 * hdet_compute_units()) each >>= 1;
   return each;
 }
 // Whether z goes through memory also where it could stay in the matrix cores' registers: up to a tile of 256 x 256 on every fourth compute unit, where a tile's long way from the first

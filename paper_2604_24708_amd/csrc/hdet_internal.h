@@ -168,11 +168,11 @@ enum { HDET_EPI_F32 = 0, HDET_EPI_BIAS_F32 = 1, HDET_EPI_BIAS_RELU_BF16 = 2, HDE
        HDET_EPI_ADAMW = 10,           // weight gradient that is applied at once: the AdamW update of `upd` on the tile (c is not written)
        // output layer whose logits z = acc + bias stay on the chip (hdet_launch_head_loss only):
        HDET_EPI_XENT_STAT = 11,       // reference and sum of a tile's rows (hdet_xent_epi; c is not written)
-       HDET_EPI_XENT_GRAD = 12,
+       HDET_EPI_XENT_GRAD = 12,       // c = bf16 gradient of the mean cross-entropy at z, from the whole rows' reference and sum; row losses, column sums
        // a product in pieces of its contraction, input-gradient order: the sum so far is in fp32 at `accum`, the last piece's is times out_scale and
        // rounded to c; weight gradients times out_scale.  out_scale may be null, and c may lie at any element
        HDET_EPI_ACCUM_BF16 = 13, HDET_EPI_SCALED_F32 = 14, HDET_EPI_SCALED_BF16 = 15,
-       HDET_EPI_XENT_PARTS = 16 };    // HDET_EPI_XENT_GRAD in three bf16 parts (hdet_launch_vocab_grad only)     // c = bf16 gradient of the mean cross-entropy at z, from the whole rows' reference and sum; row losses, column sums
+       HDET_EPI_XENT_PARTS = 16 };    // HDET_EPI_XENT_GRAD in three bf16 parts (hdet_launch_vocab_grad only)
 
 // Cross-entropy inside the output layer's product: what its two passes and the merge between them exchange.  Row scalars are [replica][row].
 struct hdet_xent_epi {

@@ -9,7 +9,7 @@ namespace {
 // rows a replica: what the launches' grids and 32-bit row numbers hold
 constexpr int64_t kMaxRows = (int64_t)1 << 21;
 
-struct checker {
+struct argument_checks {
   std::string why;
   bool ok() const { return why.empty(); }
   void need(bool cond, const char* msg) { if (why.empty() && !cond) why = msg; }
@@ -58,11 +58,11 @@ struct checker {
   }
 };
 
-// Runs one entry: f(checker) checks, g() launches.  Nothing thrown leaves it.
+// Runs one entry: f(argument_checks) checks, g() launches.  Nothing thrown leaves it.
 template <typename F, typename G>
 int entry(const char* name, F check, G launch) {
   try {
-    checker c;
+    argument_checks c;
     check(c);
     if (!c.ok()) {
       hdet_set_global_error(std::string(name) + ": " + c.why);
@@ -97,12 +97,12 @@ linear_layout linear_layout_of(int n, int64_t rows, int d_in, int d_out) {
   l.total = l.part + (l.for_dx.bytes > l.for_dw.bytes ? l.for_dx.bytes : l.for_dw.bytes);
   return l;
 }
-void linear_sizes(checker& c, int n, int64_t rows, int d_in, int d_out) {
+void linear_sizes(argument_checks& c, int n, int64_t rows, int d_in, int d_out) {
   c.common(n, rows);
   c.need(d_in >= 1 && d_in <= HDET_MAX_CODES_WIDTH, "d_in must be in 1 .. HDET_MAX_CODES_WIDTH");
   c.need(d_out >= 1 && d_out <= kMaxRows, "d_out must be in 1 .. 2^21");
 }
-void vocab_sizes(checker& c, int n, int64_t rows, int width, int classes, int dw_dtype, int piece) {
+void vocab_sizes(argument_checks& c, int n, int64_t rows, int width, int classes, int dw_dtype, int piece) {
   c.common(n, rows);
   c.need(width >= 1 && width <= HDET_MAX_CODES_WIDTH, "width must be in 1 .. HDET_MAX_CODES_WIDTH");
   c.need(classes >= 1 && classes <= kMaxRows, "classes must be in 1 .. 2^21");
@@ -113,7 +113,7 @@ void vocab_sizes(checker& c, int n, int64_t rows, int width, int classes, int dw
 }  // namespace
 
 extern "C" int hdet_rmsnorm(const hdet_norm_args* a, void* stream) {
-  return entry("hdet_rmsnorm", [&](checker& c) {
+  return entry("hdet_rmsnorm", [&](argument_checks& c) {
     c.need(a != nullptr, "args is null");
     if (!c.ok()) return;
     const int n = a->n_replicas;
@@ -135,7 +135,7 @@ extern "C" int hdet_rmsnorm(const hdet_norm_args* a, void* stream) {
 }
 
 extern "C" int hdet_rmsnorm_backward_workspace(int32_t n_replicas, int64_t rows, int32_t width, size_t* bytes) {
-  return entry("hdet_rmsnorm_backward_workspace", [&](checker& c) {
+  return entry("hdet_rmsnorm_backward_workspace", [&](argument_checks& c) {
     c.common(n_replicas, rows);
     c.need(width >= 1 && width <= HDET_MAX_NORM_WIDTH, "width must be in 1 .. HDET_MAX_NORM_WIDTH");
     c.need(bytes != nullptr, "bytes is null");
@@ -143,7 +143,7 @@ extern "C" int hdet_rmsnorm_backward_workspace(int32_t n_replicas, int64_t rows,
 }
 
 extern "C" int hdet_rmsnorm_backward(const hdet_norm_grad_args* a, void* stream) {
-  return entry("hdet_rmsnorm_backward", [&](checker& c) {
+  return entry("hdet_rmsnorm_backward", [&](argument_checks& c) {
     c.need(a != nullptr, "args is null");
     if (!c.ok()) return;
     const int n = a->n_replicas;
@@ -164,7 +164,7 @@ extern "C" int hdet_rmsnorm_backward(const hdet_norm_grad_args* a, void* stream)
 }
 
 static int codes_entry(const char* name, const hdet_codes_args* a, void* stream, bool restore) {
-  return entry(name, [&](checker& c) {
+  return entry(name, [&](argument_checks& c) {
     c.need(a != nullptr, "args is null");
     if (!c.ok()) return;
     const int n = a->n_replicas;
@@ -182,7 +182,7 @@ extern "C" int hdet_quantise_rows(const hdet_codes_args* a, void* stream) { retu
 extern "C" int hdet_restore_rows(const hdet_codes_args* a, void* stream) { return codes_entry("hdet_restore_rows", a, stream, true); }
 
 extern "C" int hdet_quantised_linear(const hdet_linear_args* a, void* stream) {
-  return entry("hdet_quantised_linear", [&](checker& c) {
+  return entry("hdet_quantised_linear", [&](argument_checks& c) {
     c.need(a != nullptr, "args is null");
     if (!c.ok()) return;
     const int n = a->n_replicas;
@@ -199,14 +199,14 @@ extern "C" int hdet_quantised_linear(const hdet_linear_args* a, void* stream) {
 }
 
 extern "C" int hdet_quantised_linear_backward_workspace(int32_t n_replicas, int64_t rows, int32_t d_in, int32_t d_out, size_t* bytes) {
-  return entry("hdet_quantised_linear_backward_workspace", [&](checker& c) {
+  return entry("hdet_quantised_linear_backward_workspace", [&](argument_checks& c) {
     linear_sizes(c, n_replicas, rows, d_in, d_out);
     c.need(bytes != nullptr, "bytes is null");
   }, [&] { *bytes = linear_layout_of(n_replicas, rows, d_in, d_out).total; return hipSuccess; });
 }
 
 extern "C" int hdet_quantised_linear_backward(const hdet_linear_grad_args* a, void* stream) {
-  return entry("hdet_quantised_linear_backward", [&](checker& c) {
+  return entry("hdet_quantised_linear_backward", [&](argument_checks& c) {
     c.need(a != nullptr, "args is null");
     if (!c.ok()) return;
     const int n = a->n_replicas;
@@ -278,14 +278,14 @@ extern "C" int hdet_quantised_linear_backward(const hdet_linear_grad_args* a, vo
 }
 
 extern "C" int hdet_vocab_loss_workspace(int32_t n_replicas, int64_t rows, int32_t width, int32_t classes, int32_t dw_dtype, int32_t piece, size_t* bytes) {
-  return entry("hdet_vocab_loss_workspace", [&](checker& c) {
+  return entry("hdet_vocab_loss_workspace", [&](argument_checks& c) {
     vocab_sizes(c, n_replicas, rows, width, classes, dw_dtype, piece);
     c.need(bytes != nullptr, "bytes is null");
   }, [&] { *bytes = hdet_vocab_bytes(n_replicas, rows, width, classes, dw_dtype, piece); return hipSuccess; });
 }
 
 extern "C" int hdet_vocab_loss(const hdet_vocab_args* a, void* stream) {
-  return entry("hdet_vocab_loss", [&](checker& c) {
+  return entry("hdet_vocab_loss", [&](argument_checks& c) {
     c.need(a != nullptr, "args is null");
     if (!c.ok()) return;
     const int n = a->n_replicas;

@@ -12,7 +12,9 @@
 //  * dz is held as c dz = softmax - onehot and the products' results are divided by c: at a label it is next to -1, which a bfloat16 holds to 2^-9 of itself, where
 //    (softmax - onehot) / c lies anywhere between two powers of two (dh against 64 bits: 2.9e-3 of its norm with the division before the rounding).
 //  * dz leaves as bfloat16 -- what the matrix cores multiply -- for dh and a bfloat16 dW, whose own rounding is as coarse.  An fp32 dW takes dz in three bfloat16
-//    parts, 24 bits: they stand below each other as rows, beside three copies of h, and make one product of three times the rows.
+//    parts, 24 bits: they stand below each other as rows, beside three copies of h, and make one product of three times the rows.  (Two fp16 parts take two thirds of that product -- 4 x 8192
+//    rows of 1024, 32000 classes: the call 9.3 ms for 10.8 -- but hold nothing below about 2^-40: the gradient of a class that is never likely came out as 0.)
+//  * Bound by the products and by the exponentials and stores at their tiles' ends.  8 x 4096 rows of 512, 32000 classes, bf16 dW, us: statistics 1064 (1.0 PFLOP/s), dz 1320 (0.8), dh 820 (1.3), dW 885 (1.2).
 
 #include <type_traits>
 

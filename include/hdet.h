@@ -441,7 +441,8 @@ int hdet_quantised_linear_backward(const hdet_linear_grad_args* args, void* stre
  *   dh = dz W,   dw = dz^T h,   db = sum over the rows of dz
  * h, W and dh are bfloat16; sums are fp32.  dw is bfloat16 or fp32.  dh and a bfloat16 dw are
  * formed from dz rounded to bfloat16, an fp32 dw from dz in three such parts (24 bits) and with two more
- * products.  dh, dw and db are optional: without them only the losses are formed.  A bias of -inf takes a class out of the sum; a row that counts and has no class left is NaN.
+ * products.  dh, dw and db are optional: without them only the losses are formed.  A row that does not count takes part in nothing, whatever its row of h holds (NaN and
+ * infinity too).  A bias of -inf takes a class of a finite row of W out of the sum; a row that counts and has no class left is NaN.
  * piece: classes at a time (taken down to whole groups of 256 or, below that, of 8), or 0 for the library's choice.  The workspace depends on it
  * (hdet_vocab_loss_workspace with the same arguments; without dw as for a bfloat16 one); 16-byte aligned. */
 typedef struct {

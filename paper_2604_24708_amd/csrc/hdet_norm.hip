@@ -417,15 +417,16 @@ __global__ __launch_bounds__(256) void hdet_restore_kernel(const int8_t* q, int6
   store_piece<WHOLE>(v + z * v_z + row * v_s + col, o, width - col);
 }
 
-// Rows of a bfloat16 matrix in rows of `pitch`, `copies` times: a thread takes 8 columns.  Grid: (ceil(rows * pieces / 256), replicas).
+// Rows of a bfloat16 matrix in rows of `pitch`, `copies` times, zeros for rows with a negative label: a thread takes 8 columns.  Grid: (ceil(rows * pieces / 256), replicas).
 template <int WHOLE>
-__global__ __launch_bounds__(256) void hdet_pad_rows_kernel(const uint16_t* x, int64_t x_s, int64_t x_z, int64_t rows, int width, uint16_t* out, int64_t pitch, int copies) {
+__global__ __launch_bounds__(256) void hdet_pad_rows_kernel(const uint16_t* x, int64_t x_s, int64_t x_z, int64_t rows, int width, const int32_t* labels, uint16_t* out,
+                                                            int64_t pitch, int copies) {
   const int64_t pieces = pitch >> 3, t = (int64_t)blockIdx.x * 256 + threadIdx.x, row = t / pieces, all = rows * pieces;
   const int col = (int)(t - row * pieces) * 8;
   if (row >= rows) return;
   piece<uint16_t> v;
   v.zero();
-  if (col < width) v.load<WHOLE>(x + blockIdx.y * x_z + row * x_s, col, width);
+  if (col < width && !(labels && labels[blockIdx.y * rows + row] < 0)) v.load<WHOLE>(x + blockIdx.y * x_z + row * x_s, col, width);
   hdet_u4v* const to = reinterpret_cast<hdet_u4v*>(out) + blockIdx.y * copies * all + t;
   for (int c = 0; c < copies; ++c) to[c * all] = v.w;
 }
@@ -525,11 +526,11 @@ hipError_t hdet_launch_restore(const hdet_codes_args& a, hipStream_t s) {
   return hipGetLastError();
 }
 
-hipError_t hdet_launch_pad_rows(const hdet_rows& x, int n_replicas, int64_t rows, int width, uint16_t* out, int64_t pitch, int copies, hipStream_t s) {
+hipError_t hdet_launch_pad_rows(const hdet_rows& x, int n_replicas, int64_t rows, int width, const int32_t* labels, uint16_t* out, int64_t pitch, int copies, hipStream_t s) {
   const dim3 grid((unsigned)((rows * (pitch >> 3) + 255) / 256), n_replicas);
   const uint16_t* from = (const uint16_t*)x.dev;
-  if (pieces_of_8(x, 2, width)) hipLaunchKernelGGL(hdet_pad_rows_kernel<kWhole>, grid, dim3(256), 0, s, from, x.row_stride, x.replica_stride, rows, width, out, pitch, copies);
-  else hipLaunchKernelGGL(hdet_pad_rows_kernel<kLoose>, grid, dim3(256), 0, s, from, x.row_stride, x.replica_stride, rows, width, out, pitch, copies);
+  if (pieces_of_8(x, 2, width)) hipLaunchKernelGGL(hdet_pad_rows_kernel<kWhole>, grid, dim3(256), 0, s, from, x.row_stride, x.replica_stride, rows, width, labels, out, pitch, copies);
+  else hipLaunchKernelGGL(hdet_pad_rows_kernel<kLoose>, grid, dim3(256), 0, s, from, x.row_stride, x.replica_stride, rows, width, labels, out, pitch, copies);
   return hipGetLastError();
 }
 

@@ -242,7 +242,7 @@ extern "C" int hdet_quantised_linear_backward(const hdet_linear_grad_args* a, vo
     if (a->db_dev && (e = hdet_launch_row_sum(a->dy, n, M, a->d_out, a->db_dev, a->db_stride, ws + l.sum, s)) != hipSuccess) return e;
     hdet_rows dy = a->dy;
     if (l.dy_pitch != a->d_out && (a->dx.dev || a->dw.dev)) {
-      if ((e = hdet_launch_pad_rows(a->dy, n, M, a->d_out, (uint16_t*)(ws + l.dy), l.dy_pitch, 1, s)) != hipSuccess) return e;
+      if ((e = hdet_launch_pad_rows(a->dy, n, M, a->d_out, nullptr, (uint16_t*)(ws + l.dy), l.dy_pitch, 1, s)) != hipSuccess) return e;
       dy = {ws + l.dy, l.dy_pitch, M * l.dy_pitch};
     }
     // a result of any alignment takes an epilogue that writes at any element where the operands allow the fast path

@@ -35,7 +35,7 @@ struct vocab_layout {
   int planes;               // bfloat16 parts of dz
   int64_t bias_pitch;
   int64_t width8;           // a row of h and W in whole 16-byte pieces
-  int h_copies;             // copies of h in such rows: three below each other beside three parts of dz, one where its own rows are no whole pieces
+  int h_copies;             // copies of h in such rows, zeros in those that do not count: three below each other beside three parts of dz, else one
   size_t inv, labels, ref, a, sum, zy, bias, dz, h, w, acc, part, split, split_bytes, total;
 };
 size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -99,7 +99,7 @@ vocab_layout layout_of(int n, int64_t rows, int width, int classes, int dw_dtype
   l.small_piece = fit < (size_t)l.piece ? (int)fit : l.piece;
   l.bias_pitch = up8(classes);
   l.width8 = up8(width);
-  l.h_copies = l.planes == 3 ? 3 : l.width8 != width ? 1 : 0;
+  l.h_copies = l.planes;
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t here = at; at += up(bytes); return here; };
   l.inv = take((size_t)n * 4);
@@ -142,7 +142,7 @@ struct prep_args {
 }  // namespace
 
 // What a call starts with, [replica] on blockIdx.y: labels that name no class become -1; 1 / rows that count; bias in rows padded with -inf; copies of h below
-// each other.
+// each other, zeros in rows that do not count (their dz is 0 and would take a NaN or infinity of h into dW's sum).
 __global__ __launch_bounds__(1024) void hdet_vocab_prep_kernel(const prep_args a) {
   const int z = blockIdx.y;
   const int64_t t = (int64_t)blockIdx.x * 1024 + threadIdx.x, step = (int64_t)gridDim.x * 1024;
@@ -154,7 +154,9 @@ __global__ __launch_bounds__(1024) void hdet_vocab_prep_kernel(const prep_args a
     const int64_t pieces = a.width / 8, all = a.rows * pieces;
     hdet_u4v* const out = reinterpret_cast<hdet_u4v*>(a.h_out) + z * a.copies * all;
     for (int64_t i = t; i < all; i += step) {
-      const hdet_u4v v = *reinterpret_cast<const hdet_u4v*>(a.h + z * a.h_z + i / pieces * a.h_s + i % pieces * 8);
+      const int64_t row = i / pieces;
+      hdet_u4v v = *reinterpret_cast<const hdet_u4v*>(a.h + z * a.h_z + row * a.h_s + i % pieces * 8);
+      if ((unsigned)lab[row] >= (unsigned)a.classes) v = hdet_u4v{0u, 0u, 0u, 0u};
       for (int q = 0; q < a.copies; ++q) out[q * all + i] = v;
     }
   }
@@ -366,8 +368,9 @@ hipError_t hdet_launch_vocab_loss(const hdet_vocab_args& a, hipStream_t s) {
   int32_t* const labels = (int32_t*)(ws + l.labels);
   double* const sum = (double*)(ws + l.sum);
   // operands of the products: the caller's, or copies in rows of whole pieces
+  const int copies = a.dw.dev || l.width8 != d ? l.h_copies : 0;
   hdet_rows h = a.h, w = a.w, hk = a.h;              // hk: what stands beside all parts of dz
-  if (l.h_copies) hk = {ws + l.h, l.width8, l.h_copies * M * l.width8};
+  if (copies) hk = {ws + l.h, l.width8, copies * M * l.width8};
   if (l.width8 != d) {
     h = hk;
     w = {ws + l.w, l.width8, V * l.width8};
@@ -396,9 +399,9 @@ hipError_t hdet_launch_vocab_loss(const hdet_vocab_args& a, hipStream_t s) {
   bool copied;
   {
     // (copies of rows that are no whole pieces take a launch of their own)
-    const bool copy = l.h_copies && l.width8 == d && M > 0 && ((a.h.row_stride | a.h.replica_stride) & 7) == 0 && (reinterpret_cast<uintptr_t>(a.h.dev) & 15) == 0;
+    const bool copy = copies && l.width8 == d && M > 0 && ((a.h.row_stride | a.h.replica_stride) & 7) == 0 && (reinterpret_cast<uintptr_t>(a.h.dev) & 15) == 0;
     const prep_args p = {a.labels_dev, labels, a.bias_dev, a.bias_stride, tiles ? bias : nullptr, l.bias_pitch, (const uint16_t*)a.h.dev, a.h.row_stride, a.h.replica_stride,
-                         copy ? (uint16_t*)(ws + l.h) : nullptr, d, l.h_copies, inv, a.mean_loss_dev, M, V};
+                         copy ? (uint16_t*)(ws + l.h) : nullptr, d, copies, inv, a.mean_loss_dev, M, V};
     int64_t work = M > l.bias_pitch ? M : l.bias_pitch;
     if (copy && M * d / 8 > work) work = M * d / 8;
     copied = copy;
@@ -411,8 +414,8 @@ hipError_t hdet_launch_vocab_loss(const hdet_vocab_args& a, hipStream_t s) {
     if (a.dw.dev && (e = hdet_launch_zero_rows(a.dw, n, V, d, a.dw_dtype, s)) != hipSuccess) return e;
     return a.db_dev ? hdet_launch_partial_sum(nullptr, n, 0, V, 0, a.db_dev, a.db_stride, s) : hipSuccess;
   }
-  if (l.h_copies && !copied && (e = hdet_launch_pad_rows(a.h, n, M, d, (uint16_t*)(ws + l.h), l.width8, l.h_copies, s)) != hipSuccess) return e;
-  if (l.width8 != d && (e = hdet_launch_pad_rows(a.w, n, V, d, (uint16_t*)(ws + l.w), l.width8, 1, s)) != hipSuccess) return e;
+  if (copies && !copied && (e = hdet_launch_pad_rows(a.h, n, M, d, labels, (uint16_t*)(ws + l.h), l.width8, copies, s)) != hipSuccess) return e;
+  if (l.width8 != d && (e = hdet_launch_pad_rows(a.w, n, V, d, nullptr, (uint16_t*)(ws + l.w), l.width8, 1, s)) != hipSuccess) return e;
   float* const z = (float*)(ws + l.dz);
   uint16_t* const dz = (uint16_t*)(ws + l.dz + (tiles ? 0 : (size_t)n * M * pitch * 4));
   auto logits = [&](int v0, int cols) {

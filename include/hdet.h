@@ -443,8 +443,10 @@ int hdet_quantised_linear_backward(const hdet_linear_grad_args* args, void* stre
  * formed from dz rounded to bfloat16, an fp32 dw from dz in three such parts (24 bits) and with two more
  * products.  dh, dw and db are optional: without them only the losses are formed.  A row that does not count takes part in nothing, whatever its row of h holds (NaN and
  * infinity too).  A bias of -inf takes a class of a finite row of W out of the sum; a row that counts and has no class left is NaN.
- * piece: classes at a time (taken down to whole groups of 256 or, below that, of 8), or 0 for the library's choice.  The workspace depends on it
- * (hdet_vocab_loss_workspace with the same arguments; without dw as for a bfloat16 one); 16-byte aligned. */
+ * piece: classes at a time (taken down to whole groups of 256 or, below that, of 8), or 0 for the library's choice.  The workspace depends on it and on dw
+ * (hdet_vocab_loss_workspace with the same arguments; HDET_VOCAB_NO_DW for the type of a dw that is absent, HDET_VOCAB_LOSSES where dh and db are too): without dw no more
+ * than with either type, for the losses alone no more than that; 16-byte aligned. */
+enum { HDET_VOCAB_NO_DW = -1, HDET_VOCAB_LOSSES = -2 };
 typedef struct {
   int32_t   n_replicas, dw_dtype;              /* HDET_TYPE_* of dw                          */
   int64_t   rows;

@@ -25,6 +25,7 @@ HDET_CH_LR, HDET_CH_DROPOUT, HDET_CH_WD, HDET_CH_LABEL_SMOOTH, HDET_CH_ATTN_TEMP
 HDET_FUSE_CONVERGE = 1
 HDET_TYPE_F32, HDET_TYPE_BF16 = 0, 1
 HDET_MAX_NORM_WIDTH, HDET_MAX_CODES_WIDTH = 32768, 131056
+HDET_VOCAB_NO_DW, HDET_VOCAB_LOSSES = -1, -2
 
 EXPORTS = [
     "hdet_workspace_bytes", "hdet_create", "hdet_warm_init", "hdet_warm_init_noalloc", "hdet_forward_backward", "hdet_fanout_step", "hdet_train_step",
@@ -519,9 +520,11 @@ def hdet_quantised_linear_backward(dy, codes, scale, w_codes, w_scale, dx=None, 
 
 
 def hdet_vocab_loss_workspace(n_replicas: int, rows: int, width: int, classes: int, dw=None, piece: int = 0) -> int:
-    """`dw`: the dtype of the weight gradient (float32 if None)."""
+    """`dw`: the dtype of the weight gradient, HDET_VOCAB_NO_DW for calls without one or HDET_VOCAB_LOSSES for the losses alone; None: float32.  What is enough with a dw of
+    either type is enough without."""
     load_library()
-    return _size_of("hdet_vocab_loss_workspace", n_replicas, rows, width, classes, HDET_TYPE_BF16 if dw == _BF16 else HDET_TYPE_F32, piece)
+    kind = dw if isinstance(dw, int) else HDET_TYPE_BF16 if dw == _BF16 else HDET_TYPE_F32
+    return _size_of("hdet_vocab_loss_workspace", n_replicas, rows, width, classes, kind, piece)
 
 
 def hdet_vocab_loss(h, w, labels, row_loss, mean_loss, dh=None, dw=None, bias=None, db=None, piece: int = 0, workspace=None,

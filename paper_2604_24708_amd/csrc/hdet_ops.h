@@ -35,5 +35,6 @@ hipError_t hdet_launch_split(const hdet_bgemm_args& g, bool a_kmajor, int batch,
 
 // hdet_vocab.hip
 hipError_t hdet_launch_zero_rows(const hdet_rows& m, int n_replicas, int64_t rows, int width, int dtype, hipStream_t s);
-size_t hdet_vocab_bytes(int n_replicas, int64_t rows, int width, int classes, int dw_dtype, int piece);
+int hdet_vocab_kind(const hdet_vocab_args& a);                                       // HDET_TYPE_* of dw, HDET_VOCAB_* without one
+size_t hdet_vocab_bytes(int n_replicas, int64_t rows, int width, int classes, int kind, int piece);
 hipError_t hdet_launch_vocab_loss(const hdet_vocab_args& a, hipStream_t s);

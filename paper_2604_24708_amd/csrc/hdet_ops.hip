@@ -102,11 +102,10 @@ void linear_sizes(argument_checks& c, int n, int64_t rows, int d_in, int d_out) 
   c.need(d_in >= 1 && d_in <= HDET_MAX_CODES_WIDTH, "d_in must be in 1 .. HDET_MAX_CODES_WIDTH");
   c.need(d_out >= 1 && d_out <= kMaxRows, "d_out must be in 1 .. 2^21");
 }
-void vocab_sizes(argument_checks& c, int n, int64_t rows, int width, int classes, int dw_dtype, int piece) {
+void vocab_sizes(argument_checks& c, int n, int64_t rows, int width, int classes, int piece) {
   c.common(n, rows);
   c.need(width >= 1 && width <= HDET_MAX_CODES_WIDTH, "width must be in 1 .. HDET_MAX_CODES_WIDTH");
   c.need(classes >= 1 && classes <= kMaxRows, "classes must be in 1 .. 2^21");
-  c.type(dw_dtype, "dw_dtype must be HDET_TYPE_F32 or HDET_TYPE_BF16");
   c.need(piece >= 0, "piece must be 0 or a number of classes");
 }
 
@@ -279,7 +278,8 @@ extern "C" int hdet_quantised_linear_backward(const hdet_linear_grad_args* a, vo
 
 extern "C" int hdet_vocab_loss_workspace(int32_t n_replicas, int64_t rows, int32_t width, int32_t classes, int32_t dw_dtype, int32_t piece, size_t* bytes) {
   return entry("hdet_vocab_loss_workspace", [&](argument_checks& c) {
-    vocab_sizes(c, n_replicas, rows, width, classes, dw_dtype, piece);
+    vocab_sizes(c, n_replicas, rows, width, classes, piece);
+    if (dw_dtype != HDET_VOCAB_NO_DW && dw_dtype != HDET_VOCAB_LOSSES) c.type(dw_dtype, "dw_dtype must be HDET_TYPE_F32, HDET_TYPE_BF16, HDET_VOCAB_NO_DW or HDET_VOCAB_LOSSES");
     c.need(bytes != nullptr, "bytes is null");
   }, [&] { *bytes = hdet_vocab_bytes(n_replicas, rows, width, classes, dw_dtype, piece); return hipSuccess; });
 }
@@ -289,7 +289,8 @@ extern "C" int hdet_vocab_loss(const hdet_vocab_args* a, void* stream) {
     c.need(a != nullptr, "args is null");
     if (!c.ok()) return;
     const int n = a->n_replicas;
-    vocab_sizes(c, n, a->rows, a->width, a->classes, a->dw_dtype, a->piece);
+    vocab_sizes(c, n, a->rows, a->width, a->classes, a->piece);
+    c.type(a->dw_dtype, "dw_dtype must be HDET_TYPE_F32 or HDET_TYPE_BF16");
     if (!c.ok()) return;
     c.matrix("h", a->h, n, a->rows, a->width, 2, true, false);
     c.matrix("w", a->w, n, a->classes, a->width, 2, true, false);
@@ -300,6 +301,6 @@ extern "C" int hdet_vocab_loss(const hdet_vocab_args* a, void* stream) {
     c.matrix("dh", a->dh, n, a->rows, a->width, 2, false, true);
     c.matrix("dw", a->dw, n, a->classes, a->width, element(a->dw_dtype), false, true);
     c.vector("db_dev", a->db_dev, n, a->classes, a->db_stride, false, true);
-    if (c.ok()) c.workspace(a->workspace_dev, a->workspace_bytes, hdet_vocab_bytes(n, a->rows, a->width, a->classes, a->dw.dev ? a->dw_dtype : HDET_TYPE_BF16, a->piece));
+    if (c.ok()) c.workspace(a->workspace_dev, a->workspace_bytes, hdet_vocab_bytes(n, a->rows, a->width, a->classes, hdet_vocab_kind(*a), a->piece));
   }, [&] { return hdet_launch_vocab_loss(*a, (hipStream_t)stream); });
 }

@@ -27,6 +27,10 @@ namespace {
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr double kLn2 = 0.6931471805599453;
 constexpr int kRowChunk = 128;                          // rows of a block's column sums in tiles
+constexpr size_t kSmallRoom = (size_t)64 << 20;         // z and dz take that much where they pass through memory, if not all of them fits what dz alone takes
+// Most that z takes in a call for the losses alone (us, rows one element off a 16-byte boundary, 64 / 128 / 256 MB: 8 x 4096 rows of 512, 32000 classes 7677 / 5859 / 6561,
+// 4 x 8192 of 1024, 32000 8922 / 8088 / 8958, 4096 of 1024, 50000 1709 / 1664 / 1764)
+constexpr size_t kLossRoom = (size_t)128 << 20;
 constexpr size_t kPieceBytes = (size_t)1 << 30;         // most that dz of a piece takes where the caller does not say
 
 // Memory of a call, in the order it is carved.  What a member names: [replica][...].
@@ -36,7 +40,7 @@ struct vocab_layout {
   int planes;               // bfloat16 parts of dz
   int64_t bias_pitch;
   int64_t width8;           // a row of h and W in whole 16-byte pieces
-  int h_copies;             // copies of h in such rows, zeros in those that do not count: three below each other beside three parts of dz, else one
+  int h_copies;             // copies of h in such rows, zeros in those that do not count: as many below each other as dz has parts; without dw one where h's own rows are no whole pieces
   size_t inv, labels, ref, a, sum, zy, bias, dz, h, w, acc, part, split, split_bytes, total;
 };
 size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -61,11 +65,16 @@ bool small_call(int n, int64_t rows, int classes) {
 //   4 x 8192 rows of 1024, 32000 classes, fp32 dW: 2048 (1/2) 12739, 4096 (1) 10972, 6400 (1.6) 11420, 8192 (2) 10720, 32000 10439
 //   4096 rows of 1024, 50000 classes, bf16: 2048 (1/8) 2689, 4096 (1/4) 1883, 8192 (1/2) 1697, 16384 (1) 1550, 32000 (2) 1558, 50000 1684
 // Between the two stands kPieceBytes.
-int chosen_piece(int n, size_t class_bytes, int width, int classes) {
+// Without a dW nothing wants rounds: pieces alike, as few as fit.
+int chosen_piece(int n, size_t class_bytes, int width, int classes, size_t piece_bytes, bool dw) {
   const int64_t tiles = (int64_t)((width + 255) / 256) * n, cus = hdet_compute_units(), columns = (classes + 255) / 256;
-  int64_t most = (int64_t)(kPieceBytes / class_bytes) / 256;      // columns of tiles that fit
+  int64_t most = (int64_t)(piece_bytes / class_bytes) / 256;      // columns of tiles that fit
   if (most < 4) most = 4;
   if (most >= columns) most = columns;
+  if (!dw) {
+    const int64_t pieces = (columns + most - 1) / most;
+    return pieces == 1 ? classes : (int)((columns + pieces - 1) / pieces) * 256;
+  }
   int64_t best = most;
   double least = 1e30;
   for (int64_t pieces = (columns + most - 1) / most; pieces <= columns && pieces <= 4 * ((columns + most - 1) / most) + 4; ++pieces) {
@@ -76,12 +85,12 @@ int chosen_piece(int n, size_t class_bytes, int width, int classes) {
   return best >= columns ? classes : (int)best * 256;
 }
 
-vocab_layout layout_of(int n, int64_t rows, int width, int classes, int dw_dtype, int piece) {
+// kind: HDET_TYPE_* of dw, or one of HDET_VOCAB_*.  Pieces are made for plan_planes parts of dz that take piece_bytes at most, for a call with dw or without.
+vocab_layout layout_in(int n, int64_t rows, int width, int classes, int kind, int plan_planes, int piece, size_t piece_bytes = kPieceBytes, bool for_dw = true) {
   vocab_layout l;
-  l.planes = dw_dtype == HDET_TYPE_F32 ? 3 : 1;
   const size_t all = (size_t)n * (rows > 0 ? rows : 1);
   if (piece <= 0) {
-    piece = chosen_piece(n, all * 2 * l.planes, width, classes);
+    piece = chosen_piece(n, all * 2 * plan_planes, width, classes, piece_bytes, for_dw);
   } else {      // whole tiles of 256 classes, or whole groups of 8 where the caller wants fewer
     if (piece > classes) piece = classes;
     if (piece < classes) piece = piece >= 256 ? piece / 256 * 256 : piece >= 8 ? piece / 8 * 8 : 8;
@@ -89,8 +98,8 @@ vocab_layout layout_of(int n, int64_t rows, int width, int classes, int dw_dtype
   }
   l.piece = piece;
   l.pieces = (classes + piece - 1) / piece;
-  size_t room = all * up8(l.piece) * 2 * l.planes;                                  // dz
-  const size_t a_class = all * (4 + 2 * l.planes), small = (size_t)64 << 20;        // z and dz
+  size_t room = all * up8(l.piece) * 2 * plan_planes;                               // dz
+  const size_t a_class = all * (4 + 2 * plan_planes), small = kSmallRoom;           // z and dz
   const size_t whole = a_class * up8(l.piece);
   if (room < (whole < small ? whole : small)) room = whole < small ? whole : small;
   if (room < a_class * 8) room = a_class * 8;
@@ -98,9 +107,18 @@ vocab_layout layout_of(int n, int64_t rows, int width, int classes, int dw_dtype
   if (room < stats) room = stats;
   size_t fit = room / a_class / 8 * 8;
   l.small_piece = fit < (size_t)l.piece ? (int)fit : l.piece;
+  const bool dw = kind >= 0, losses = kind == HDET_VOCAB_LOSSES;
+  l.planes = dw ? plan_planes : 1;
+  if (!dw) {                                                                        // what is left of that room: z, and one part of dz
+    room = all * up8(l.small_piece) * (losses ? 4 : 6);
+    if (!losses && room < all * up8(l.piece) * 2) room = all * up8(l.piece) * 2;
+    if (losses && room > kLossRoom) room = kLossRoom > all * 32 ? kLossRoom : all * 32;
+    if (room < stats) room = stats;
+    if (losses && room / (all * 4) / 8 * 8 < (size_t)l.small_piece) l.small_piece = (int)(room / (all * 4) / 8 * 8);
+  }
   l.bias_pitch = up8(classes);
   l.width8 = up8(width);
-  l.h_copies = l.planes;
+  l.h_copies = dw ? l.planes : l.width8 != width ? 1 : 0;
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t here = at; at += up(bytes); return here; };
   l.inv = take((size_t)n * 4);
@@ -113,22 +131,44 @@ vocab_layout layout_of(int n, int64_t rows, int width, int classes, int dw_dtype
   l.dz = take(room);
   l.h = take(all * l.h_copies * l.width8 * 2);
   l.w = take(l.width8 != width ? (size_t)n * classes * l.width8 * 2 : 0);
-  l.acc = take(l.pieces > 1 || l.small_piece < l.piece ? all * l.width8 * 4 : 0);
+  l.acc = take(!losses && (l.pieces > 1 || l.small_piece < l.piece) ? all * l.width8 * 4 : 0);
   size_t part = (size_t)n * ((rows + kRowChunk - 1) / kRowChunk) * up8(l.piece);
   for (const int cols : {l.small_piece, classes - (classes + l.small_piece - 1) / l.small_piece * l.small_piece + l.small_piece}) {
     const int each = rows_each(n, rows, cols);
     const size_t want = (size_t)n * ((rows + each - 1) / each) * up8(cols);
     if (want > part) part = want;
   }
-  l.part = take(part * 4);
+  l.part = take(losses ? 0 : part * 4);
   // results of pieces of a long contraction: the most that a piece of either kind may take
   l.split_bytes = 0;
   for (const int cols : {l.piece, classes - (l.pieces - 1) * l.piece, l.small_piece, classes - (classes + l.small_piece - 1) / l.small_piece * l.small_piece + l.small_piece})
-    for (const hdet_split& sp : {hdet_split_of(n, rows, width, cols), hdet_split_of(n, cols, width, l.planes * rows)})
-      if (sp.bytes > l.split_bytes) l.split_bytes = sp.bytes;
+    for (const hdet_split& sp : {hdet_split_of(n, rows, width, cols), hdet_split_of(n, cols, width, dw ? l.planes * rows : 0)})
+      if (!losses && sp.bytes > l.split_bytes) l.split_bytes = sp.bytes;
   l.split = take(l.split_bytes);
   l.total = at;
   return l;
+}
+
+// Memory that is enough for a call with a dw of either type is enough without: pieces as large as the smaller of the two allows, at the least those of one of the calls
+// with dw, whose own layout less what only dw needs fits it.
+vocab_layout layout_of(int n, int64_t rows, int width, int classes, int kind, int piece) {
+  if (kind >= 0) return layout_in(n, rows, width, classes, kind, kind == HDET_TYPE_F32 ? 3 : 1, piece);
+  int planes = 1, eighths = 8;
+  bool for_dw = false;
+  auto with = [&](int kind) { return layout_in(n, rows, width, classes, kind, planes, piece, kPieceBytes / 8 * eighths, for_dw); };
+  vocab_layout l = with(HDET_VOCAB_NO_DW);
+  if (l.pieces > 1 || (size_t)n * rows * 10 * up8(classes) > kSmallRoom) {      // (else one piece for all three of them)
+    const size_t f32 = layout_in(n, rows, width, classes, HDET_TYPE_F32, 3, piece).total, bf16 = layout_in(n, rows, width, classes, HDET_TYPE_BF16, 1, piece).total;
+    const size_t most = f32 < bf16 ? f32 : bf16;
+    while (l.total > most && --eighths > 2) l = with(HDET_VOCAB_NO_DW);
+    if (l.total > most) {
+      planes = bf16 == most ? 1 : 3;
+      eighths = 8;
+      for_dw = true;
+      l = with(HDET_VOCAB_NO_DW);
+    }
+  }
+  return kind == HDET_VOCAB_NO_DW ? l : with(kind);
 }
 
 struct prep_args {
@@ -355,21 +395,22 @@ hipError_t hdet_launch_zero_rows(const hdet_rows& m, int n_replicas, int64_t row
   return hipGetLastError();
 }
 
-size_t hdet_vocab_bytes(int n_replicas, int64_t rows, int width, int classes, int dw_dtype, int piece) {
-  return layout_of(n_replicas, rows, width, classes, dw_dtype, piece).total;
+size_t hdet_vocab_bytes(int n_replicas, int64_t rows, int width, int classes, int kind, int piece) {
+  return layout_of(n_replicas, rows, width, classes, kind, piece).total;
 }
+int hdet_vocab_kind(const hdet_vocab_args& a) { return a.dw.dev ? a.dw_dtype : a.dh.dev || a.db_dev ? HDET_VOCAB_NO_DW : HDET_VOCAB_LOSSES; }
 
 hipError_t hdet_launch_vocab_loss(const hdet_vocab_args& a, hipStream_t s) {
   const int n = a.n_replicas, d = a.width, V = a.classes;
   const int64_t M = a.rows;
-  const vocab_layout l = layout_of(n, M, d, V, a.dw.dev ? a.dw_dtype : HDET_TYPE_BF16, a.piece);
+  const vocab_layout l = layout_of(n, M, d, V, hdet_vocab_kind(a), a.piece);
   char* const ws = (char*)a.workspace_dev;
   float *const inv = (float*)(ws + l.inv), *const ref = (float*)(ws + l.ref), *const ra = (float*)(ws + l.a), *const zy = (float*)(ws + l.zy), *const part = (float*)(ws + l.part);
   float* const bias = (float*)(ws + l.bias);
   int32_t* const labels = (int32_t*)(ws + l.labels);
   double* const sum = (double*)(ws + l.sum);
   // operands of the products: the caller's, or copies in rows of whole pieces
-  const int copies = a.dw.dev || l.width8 != d ? l.h_copies : 0;
+  const int copies = l.h_copies;
   hdet_rows h = a.h, w = a.w, hk = a.h;              // hk: what stands beside all parts of dz
   if (copies) hk = {ws + l.h, l.width8, copies * M * l.width8};
   if (l.width8 != d) {
@@ -377,7 +418,7 @@ hipError_t hdet_launch_vocab_loss(const hdet_vocab_args& a, hipStream_t s) {
     w = {ws + l.w, l.width8, V * l.width8};
   }
   const uint16_t *hp = (const uint16_t*)h.dev, *wp = (const uint16_t*)w.dev;
-  const bool grads = a.dh.dev || a.dw.dev || a.db_dev;
+  const bool grads = hdet_vocab_kind(a) != HDET_VOCAB_LOSSES;
   hipError_t e;
 
   // z = h W^T + bias of the classes from v0 on; in tiles: bias padded

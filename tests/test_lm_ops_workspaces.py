@@ -1,0 +1,97 @@
+"""Scratch memory of the language-model operators: what a call asks for is what it uses, and no more than it needs for the results it is given."""
+import ctypes as C
+import math
+import random
+import re
+
+import pytest
+import torch
+
+import ops_reference as R
+import paper_2604_24708_amd as H
+from paper_2604_24708_amd import binding as B
+
+P = 1 << 40            # an aligned address that nothing reads
+BF, F32 = torch.bfloat16, torch.float32
+
+
+def asked_for(name, args):
+    """The workspace that a call says it needs, given one byte too few of it: refused before anything is enqueued."""
+    args.workspace_dev, args.workspace_bytes = P, 0
+    assert getattr(H.load_library(), name)(C.byref(args), None) == H.HDET_EINVAL
+    return int(re.search(r"(\d+) bytes are needed", H.hdet_last_error()).group(1))
+
+
+def vocab_args(n, rows, width, classes, piece, dw_dtype, dh=True, dw=True, db=True):
+    m = lambda r: B.hdet_rows(P, width, r * width)  # noqa: E731
+    a = B.hdet_vocab_args(n_replicas=n, dw_dtype=dw_dtype, rows=rows, width=width, classes=classes, piece=piece, labels_dev=P, row_loss_dev=P, mean_loss_dev=P, h=m(rows), w=m(classes))
+    if dh:
+        a.dh = m(rows)
+    if dw:
+        a.dw = m(classes)
+    if db:
+        a.db_dev, a.db_stride = P, classes
+    return a
+
+
+def vocab_sizes():
+    rng = random.Random(5)
+    log = lambda lo, hi: int(round(math.exp(rng.uniform(math.log(lo), math.log(hi)))))  # noqa: E731
+    drawn = [(rng.choice([1, 2, 3, 4, 5, 8, 64]), log(1, 30000), log(1, 4096), log(1, 200000), rng.choice([0, 0, 0, 5, 300, 4096])) for _ in range(1500)]
+    return [(8, 4096, 512, 32000, 0), (4, 8192, 1024, 32000, 0), (8, 521, 64, 105157, 0)] + drawn
+
+
+def test_a_loss_without_dw_needs_no_more_than_with_one():
+    for n, rows, width, classes, piece in vocab_sizes():
+        s = lambda dh, dw, db, t=H.HDET_TYPE_F32: asked_for("hdet_vocab_loss", vocab_args(n, rows, width, classes, piece, t, dh, dw, db))  # noqa: E731
+        full = [s(True, True, True, t) for t in (H.HDET_TYPE_F32, H.HDET_TYPE_BF16)]
+        size = lambda dw: H.hdet_vocab_loss_workspace(n, rows, width, classes, dw=dw, piece=piece)  # noqa: E731
+        assert full == [size(F32), size(BF)] and size(None) == size(F32)
+        for t in (H.HDET_TYPE_F32, H.HDET_TYPE_BF16):
+            some, none = s(True, False, True, t), s(False, False, False, t)
+            assert none <= some <= min(full), (n, rows, width, classes, piece, none, some, full)
+            assert s(True, False, False, t) == s(False, False, True, t) == some
+            assert some == size(H.HDET_VOCAB_NO_DW) and none == size(H.HDET_VOCAB_LOSSES)
+
+
+def test_the_losses_alone_need_no_gradient_of_the_logits():
+    """8 x 4096 rows of 512, 32000 classes: 1 GB in a call with gradients; without, a reference and a sum for each row and 256 classes, or 128 MB of logits."""
+    assert H.hdet_vocab_loss_workspace(8, 4096, 512, 32000, dw=H.HDET_VOCAB_LOSSES) < 144 << 20
+    for bad in (-3, 2):
+        with pytest.raises(H.HdetError):
+            H.hdet_vocab_loss_workspace(1, 1, 1, 1, dw=bad)
+
+
+def guarded(size):
+    """`size` bytes of scratch memory, and what lies behind them."""
+    t = torch.full((size + 4096,), 0xa5, dtype=torch.uint8, device=R.DEV)
+    return t[:size], t[size:]
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,rows,width,classes,piece", [(2, 50, 72, 300, 64), (1, 100, 96, 9600, 0), (2, 300, 333, 8200, 2048), (1, 1900, 264, 2304, 0), (8, 521, 64, 105157, 0)])
+def test_a_loss_stays_inside_its_workspace(n, rows, width, classes, piece):
+    import test_lm_ops_vocab as V
+    h, w, bias, labels = V.make(n, rows, width, classes, 12)
+    nan = float("nan")
+    want = None
+    for dw_dtype, dw in ((F32, True), (BF, True), (H.HDET_VOCAB_NO_DW, False), (H.HDET_VOCAB_LOSSES, False)):
+        work, behind = guarded(H.hdet_vocab_loss_workspace(n, rows, width, classes, dw=dw_dtype, piece=piece))
+        grads = dict(dh=torch.full_like(h, nan), db=torch.full((n, classes), nan, device=R.DEV)) if dw_dtype != H.HDET_VOCAB_LOSSES else {}
+        if dw:
+            grads["dw"] = torch.full(w.shape, nan, dtype=dw_dtype, device=R.DEV)
+        loss, mean = torch.full((n, rows), nan, device=R.DEV), torch.full((n,), nan, device=R.DEV)
+        H.hdet_vocab_loss(h, w, labels, loss, mean, bias=bias, piece=piece, workspace=work, **grads)
+        assert torch.all(behind == 0xa5)
+        out = (loss, mean, *(grads[k] for k in ("dh", "db") if k in grads))
+        if want is None:
+            want = out
+            for z in range(n):
+                ref = R.vocab_loss(h[z:z + 1], w[z:z + 1], bias[z:z + 1], labels[z:z + 1])
+                assert torch.all((loss[z:z + 1].double() - ref[0]).abs() <= 1e-5 * (1 + ref[0].abs())) and R.rel(grads["dh"][z:z + 1], ref[2]) <= 2 * 2.0 ** -9
+                assert R.rel(grads["dw"][z:z + 1], ref[3]) <= 1e-5 and R.rel(grads["db"][z:z + 1], ref[4]) <= 1e-5
+                del ref
+        # pieces differ between the calls, and with them the order of fp32 sums
+        assert torch.all((loss - want[0]).abs() <= 1e-5 * (1 + want[0].abs())) and torch.all((mean - want[1]).abs() <= 1e-5 * (1 + want[1].abs()))
+        if grads:
+            assert R.rel(grads["dh"], want[2].double()) <= 2 * 2.0 ** -9 and R.rel(grads["db"], want[3].double()) <= 1e-5

@@ -88,7 +88,7 @@ int chosen_piece(int n, size_t class_bytes, int width, int classes, size_t piece
 // kind: HDET_TYPE_* of dw, or one of HDET_VOCAB_*.  Pieces are made for plan_planes parts of dz that take piece_bytes at most, for a call with dw or without.
 vocab_layout layout_in(int n, int64_t rows, int width, int classes, int kind, int plan_planes, int piece, size_t piece_bytes = kPieceBytes, bool for_dw = true) {
   vocab_layout l;
-  const size_t all = (size_t)n * (rows > 0 ? rows : 1);
+  const size_t all = (size_t)n * rows;
   if (piece <= 0) {
     piece = chosen_piece(n, all * 2 * plan_planes, width, classes, piece_bytes, for_dw);
   } else {      // whole tiles of 256 classes, or whole groups of 8 where the caller wants fewer
@@ -175,7 +175,7 @@ struct prep_args {
   const int32_t* labels; int32_t* labels_out;
   const float* bias; int64_t bias_z; float* bias_out; int64_t bias_pitch;
   const uint16_t* h; int64_t h_s, h_z; uint16_t* h_out; int width, copies;      // rows of whole 16-byte pieces
-  float *inv, *mean;
+  float* inv;
   int64_t rows;
   int classes;
 };
@@ -214,7 +214,6 @@ __global__ __launch_bounds__(1024) void hdet_vocab_prep_kernel(const prep_args a
 #pragma unroll
     for (int w = 0; w < 16; ++w) n += part[w];
     a.inv[z] = 1.f / (float)(n > 1 ? n : 1);
-    if (a.rows == 0) a.mean[z] = 0.f;
   }
 }
 
@@ -396,13 +395,19 @@ hipError_t hdet_launch_zero_rows(const hdet_rows& m, int n_replicas, int64_t row
 }
 
 size_t hdet_vocab_bytes(int n_replicas, int64_t rows, int width, int classes, int kind, int piece) {
-  return layout_of(n_replicas, rows, width, classes, kind, piece).total;
+  return rows == 0 ? 0 : layout_of(n_replicas, rows, width, classes, kind, piece).total;
 }
 int hdet_vocab_kind(const hdet_vocab_args& a) { return a.dw.dev ? a.dw_dtype : a.dh.dev || a.db_dev ? HDET_VOCAB_NO_DW : HDET_VOCAB_LOSSES; }
 
 hipError_t hdet_launch_vocab_loss(const hdet_vocab_args& a, hipStream_t s) {
   const int n = a.n_replicas, d = a.width, V = a.classes;
   const int64_t M = a.rows;
+  hipError_t e;
+  if (M == 0) {      // no rows: the sums over none of them
+    if ((e = hdet_launch_partial_sum(nullptr, n, 0, 1, 0, a.mean_loss_dev, 1, s)) != hipSuccess) return e;
+    if (a.dw.dev && (e = hdet_launch_zero_rows(a.dw, n, V, d, a.dw_dtype, s)) != hipSuccess) return e;
+    return a.db_dev ? hdet_launch_partial_sum(nullptr, n, 0, V, 0, a.db_dev, a.db_stride, s) : hipSuccess;
+  }
   const vocab_layout l = layout_of(n, M, d, V, hdet_vocab_kind(a), a.piece);
   char* const ws = (char*)a.workspace_dev;
   float *const inv = (float*)(ws + l.inv), *const ref = (float*)(ws + l.ref), *const ra = (float*)(ws + l.a), *const zy = (float*)(ws + l.zy), *const part = (float*)(ws + l.part);
@@ -419,7 +424,6 @@ hipError_t hdet_launch_vocab_loss(const hdet_vocab_args& a, hipStream_t s) {
   }
   const uint16_t *hp = (const uint16_t*)h.dev, *wp = (const uint16_t*)w.dev;
   const bool grads = hdet_vocab_kind(a) != HDET_VOCAB_LOSSES;
-  hipError_t e;
 
   // z = h W^T + bias of the classes from v0 on; in tiles: bias padded
   auto product = [&](int v0, int cols, bool tiles) {
@@ -434,16 +438,16 @@ hipError_t hdet_launch_vocab_loss(const hdet_vocab_args& a, hipStream_t s) {
     g.xent.invb = 1.f; g.xent.label0 = v0;
     return g;
   };
-  const bool tiles = M > 0 && !small_call(n, M, V) && hdet_vocab_tiles_eligible(product(0, V, true));
+  const bool tiles = !small_call(n, M, V) && hdet_vocab_tiles_eligible(product(0, V, true));
   const int piece = tiles ? l.piece : l.small_piece, pieces = (V + piece - 1) / piece;
   const int64_t pitch = up8(piece);
 
   bool copied;
   {
     // (copies of rows that are no whole pieces take a launch of their own)
-    const bool copy = copies && l.width8 == d && M > 0 && ((a.h.row_stride | a.h.replica_stride) & 7) == 0 && (reinterpret_cast<uintptr_t>(a.h.dev) & 15) == 0;
+    const bool copy = copies && l.width8 == d && ((a.h.row_stride | a.h.replica_stride) & 7) == 0 && (reinterpret_cast<uintptr_t>(a.h.dev) & 15) == 0;
     const prep_args p = {a.labels_dev, labels, a.bias_dev, a.bias_stride, tiles ? bias : nullptr, l.bias_pitch, (const uint16_t*)a.h.dev, a.h.row_stride, a.h.replica_stride,
-                         copy ? (uint16_t*)(ws + l.h) : nullptr, d, copies, inv, a.mean_loss_dev, M, V};
+                         copy ? (uint16_t*)(ws + l.h) : nullptr, d, copies, inv, M, V};
     int64_t work = M > l.bias_pitch ? M : l.bias_pitch;
     if (copy && M * d / 8 > work) work = M * d / 8;
     copied = copy;
@@ -451,10 +455,6 @@ hipError_t hdet_launch_vocab_loss(const hdet_vocab_args& a, hipStream_t s) {
     if (blocks > 1024) blocks = 1024;
     hipLaunchKernelGGL(hdet_vocab_prep_kernel, dim3((unsigned)blocks, n), dim3(1024), 0, s, p);
     if ((e = hipGetLastError()) != hipSuccess) return e;
-  }
-  if (M == 0) {
-    if (a.dw.dev && (e = hdet_launch_zero_rows(a.dw, n, V, d, a.dw_dtype, s)) != hipSuccess) return e;
-    return a.db_dev ? hdet_launch_partial_sum(nullptr, n, 0, V, 0, a.db_dev, a.db_stride, s) : hipSuccess;
   }
   if (copies && !copied && (e = hdet_launch_pad_rows(a.h, n, M, d, labels, (uint16_t*)(ws + l.h), l.width8, copies, s)) != hipSuccess) return e;
   if (l.width8 != d && (e = hdet_launch_pad_rows(a.w, n, V, d, nullptr, (uint16_t*)(ws + l.w), l.width8, 1, s)) != hipSuccess) return e;

@@ -95,3 +95,24 @@ def test_a_loss_stays_inside_its_workspace(n, rows, width, classes, piece):
         assert torch.all((loss - want[0]).abs() <= 1e-5 * (1 + want[0].abs())) and torch.all((mean - want[1]).abs() <= 1e-5 * (1 + want[1].abs()))
         if grads:
             assert R.rel(grads["dh"], want[2].double()) <= 2 * 2.0 ** -9 and R.rel(grads["db"], want[3].double()) <= 1e-5
+
+
+def test_no_rows_need_no_workspace_for_a_loss():
+    for dw in (F32, BF, H.HDET_VOCAB_NO_DW, H.HDET_VOCAB_LOSSES):
+        assert H.hdet_vocab_loss_workspace(3, 0, 777, 50000, dw=dw) == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dw_dtype", [BF, F32])
+@pytest.mark.parametrize("width,classes", [(8, 300), (333, 9000)])
+def test_a_loss_without_rows(width, classes, dw_dtype):
+    n = 3
+    h, w = torch.empty(n, 0, width, dtype=BF, device=R.DEV), torch.ones(n, classes, width, dtype=BF, device=R.DEV)
+    labels, loss = torch.empty(n, 0, dtype=torch.int32, device=R.DEV), torch.empty(n, 0, device=R.DEV)
+    mean, db = torch.full((n,), 7.0, device=R.DEV), torch.full((n, classes + 5), 7.0, device=R.DEV)
+    dw = R.strided(torch.zeros(n, classes, width, device=R.DEV).to(dw_dtype), 3, 2, 1).fill_(7)
+    H.hdet_vocab_loss(h, w, labels, loss, mean, dh=torch.empty_like(h), dw=dw, db=db[:, 2:2 + classes])
+    assert torch.all(mean == 0) and torch.all(dw == 0) and torch.all(db[:, 2:2 + classes] == 0) and torch.all(db[:, :2] == 7) and torch.all(db[:, 2 + classes:] == 7)
+    mean.fill_(7)
+    H.hdet_vocab_loss(h, w, labels, loss, mean)
+    assert torch.all(mean == 0)

@@ -317,7 +317,8 @@ int hdet_destroy(hdet_handle* h);
  * are in elements; any that keep rows and replicas apart (of an output: no two elements may
  * share memory).  Rows of whole 16-byte pieces at 16-byte boundaries are the fastest, by a
  * factor of two and more.  Outputs may not lie over inputs unless stated otherwise.  With no
- * rows the sums over them (gradients of weights, mean losses) are written as 0.
+ * rows the sums over them (gradients of weights, mean losses) are written as 0, and no workspace
+ * is needed.
  *
  * A matrix in 8 bits: codes -127 .. 127 and one fp32 scale a row; entry = code * scale.  The
  * codes of a row start 16-byte aligned (row and replica strides are multiples of 16) and are
@@ -415,7 +416,7 @@ int hdet_quantised_linear(const hdet_linear_args* args, void* stream);
  *   dx = dy W (bfloat16, optional),  dw = dy^T X (fp32, optional),  db = sum over the rows of dy (fp32, optional)
  * in bfloat16 products with fp32 sums.  The values code * scale are read as bfloat16 numbers: exact for the
  * scales that this library chooses, rounded for others.  X (for dw) and W (for dx) pass through the workspace in bfloat16:
- * hdet_quantised_linear_backward_workspace bytes, 16-byte aligned.                          */
+ * hdet_quantised_linear_backward_workspace bytes, 16-byte aligned (a call without some of the results needs no more).                       */
 typedef struct {
   int32_t   n_replicas, reserved;
   int64_t   rows;

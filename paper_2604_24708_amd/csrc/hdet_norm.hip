@@ -576,7 +576,10 @@ static int row_sum_parts(int n_replicas, int64_t rows, int width) {
   return (int)((rows + each - 1) / each);
 }
 
-size_t hdet_row_sum_bytes(int n_replicas, int64_t rows, int width) { return (size_t)n_replicas * row_sum_parts(n_replicas, rows, width) * width * sizeof(float); }
+size_t hdet_row_sum_bytes(int n_replicas, int64_t rows, int width) {
+  const int parts = row_sum_parts(n_replicas, rows, width);
+  return parts > 1 ? (size_t)n_replicas * parts * width * sizeof(float) : 0;
+}
 
 hipError_t hdet_launch_row_sum(const hdet_rows& x, int n_replicas, int64_t rows, int width, float* out, int64_t out_stride, void* scratch, hipStream_t s) {
   const int parts = row_sum_parts(n_replicas, rows, width), each = rows_each(n_replicas, rows, width);

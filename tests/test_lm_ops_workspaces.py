@@ -116,3 +116,66 @@ def test_a_loss_without_rows(width, classes, dw_dtype):
     mean.fill_(7)
     H.hdet_vocab_loss(h, w, labels, loss, mean)
     assert torch.all(mean == 0)
+
+
+def linear_grad_args(n, rows, d_in, d_out, dx=True, dw=True, db=True):
+    wide = -(-d_in // 16) * 16
+    a = B.hdet_linear_grad_args(n_replicas=n, rows=rows, d_in=d_in, d_out=d_out, scale_dev=P, w_scale_dev=P, dy=B.hdet_rows(P, d_out, rows * d_out),
+                                codes=B.hdet_rows(P, wide, rows * wide), w_codes=B.hdet_rows(P, wide, d_out * wide))
+    if dx:
+        a.dx = B.hdet_rows(P, d_in, rows * d_in)
+    if dw:
+        a.dw = B.hdet_rows(P, d_in, d_out * d_in)
+    if db:
+        a.db_dev, a.db_stride = P, d_out
+    return a
+
+
+def test_linear_gradients_ask_for_what_their_results_need():
+    """bfloat16 copies of W for dx and of X for dw; neither for db."""
+    for n, rows, d_in, d_out in [(8, 8192, 1024, 4096), (3, 5150, 776, 1501), (1, 20000, 64, 40), (2, 1000, 9000, 24)]:
+        s = lambda *on: asked_for("hdet_quantised_linear_backward", linear_grad_args(n, rows, d_in, d_out, *on))  # noqa: E731
+        full, dx, dw, db = s(True, True, True), s(True, False, False), s(False, True, False), s(False, False, True)
+        assert full == H.hdet_quantised_linear_backward_workspace(n, rows, d_in, d_out) and max(dx, dw, db) <= full
+        pitch, ragged = -(-d_in // 8) * 8, d_out % 8 != 0
+        more = n * rows * (d_out + 8) * 2 if ragged else 0             # dy in whole pieces
+        parts = 256 * 128 * 128 * 4 * 2                                # results of pieces of a contraction: half the compute units' tiles at most, each in up to twice as many
+        assert n * d_out * pitch * 2 <= dx <= n * d_out * pitch * 2 + more + parts
+        assert n * rows * pitch * 2 <= dw <= n * rows * pitch * 2 + more + parts
+        assert db <= n * (rows // 16 + 1) * d_out * 4 + 256
+        assert full <= n * (rows + d_out) * pitch * 2 + more + parts + db + 1024
+    assert H.hdet_quantised_linear_backward_workspace(3, 0, 777, 50000) == 0
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("n,rows,d_in,d_out", [(3, 129, 300, 131), (2, 257, 384, 1024), (1, 2000, 96, 72), (2, 130, 264, 1664), (1, 9, 40, 33)])
+def test_linear_gradients_stay_inside_their_workspace(n, rows, d_in, d_out):
+    import test_lm_ops_linear as L
+    x, xs, w, ws, _, dy = L.make(n, rows, d_in, d_out, 13)
+    new = lambda: dict(dx=torch.empty(n, rows, d_in, dtype=BF, device=R.DEV), dw=torch.empty(n, d_out, d_in, device=R.DEV), db=torch.empty(n, d_out, device=R.DEV))  # noqa: E731
+    want = None
+    for on in (("dx", "dw", "db"), ("dx",), ("dw",), ("db",), ("dw", "db"), ("dx", "db")):
+        out = {k: v for k, v in new().items() if k in on}
+        size = 0
+        if on != ("db",) or rows > 16:
+            size = asked_for("hdet_quantised_linear_backward", linear_grad_args(n, rows, d_in, d_out, *(k in on for k in ("dx", "dw", "db"))))
+        work, behind = guarded(size)
+        H.hdet_quantised_linear_backward(dy, x, xs, w, ws, workspace=work if size else None, **out)
+        assert torch.all(behind == 0xa5)
+        if want is None:
+            want = out
+            d = dy.double()
+            assert R.rel(out["dx"], torch.matmul(d, L.values(w, ws))) <= R.half_ulp(BF)
+            assert R.rel(out["dw"], torch.matmul(d.transpose(1, 2).contiguous(), L.values(x, xs))) <= 8 * R.U * rows ** 0.5
+            assert torch.all((out["db"].double() - d.sum(1)).abs() <= (rows + 2) * R.U * d.abs().sum(1))
+        assert all(torch.equal(out[k], want[k]) for k in on)
+
+
+@pytest.mark.gpu
+def test_linear_gradients_without_rows_need_no_workspace():
+    n, d_in, d_out = 2, 72, 40
+    x, w = H.hdet_codes_empty(n, 0, d_in), H.hdet_codes_empty(n, d_out, d_in)
+    db, dw = torch.ones(n, d_out, device=R.DEV), torch.ones(n, d_out, d_in, device=R.DEV)
+    dy, dx = torch.empty(n, 0, d_out, dtype=BF, device=R.DEV), torch.empty(n, 0, d_in, dtype=BF, device=R.DEV)
+    H.hdet_quantised_linear_backward(dy, x, torch.empty(n, 0, device=R.DEV), w, torch.ones(n, d_out, device=R.DEV), dx=dx, dw=dw, db=db)
+    assert torch.all(db == 0) and torch.all(dw == 0)

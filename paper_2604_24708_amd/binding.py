@@ -418,7 +418,12 @@ def _scalars(name, t, shape, dtype=None):
 
 
 def _work_of(t):
-    return (None, 0) if t is None else (t.data_ptr(), t.numel() * t.element_size())
+    """scratch memory: the kernels write as many bytes from its start on as the tensor has"""
+    if t is None:
+        return None, 0
+    if not t.is_cuda or not t.is_contiguous():
+        _refuse("workspace", t, t.shape, t.dtype, contiguous=True)
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
 def _size_of(name, *args) -> int:

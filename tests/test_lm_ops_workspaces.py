@@ -179,3 +179,28 @@ def test_linear_gradients_without_rows_need_no_workspace():
     dy, dx = torch.empty(n, 0, d_out, dtype=BF, device=R.DEV), torch.empty(n, 0, d_in, dtype=BF, device=R.DEV)
     H.hdet_quantised_linear_backward(dy, x, torch.empty(n, 0, device=R.DEV), w, torch.ones(n, d_out, device=R.DEV), dx=dx, dw=dw, db=db)
     assert torch.all(db == 0) and torch.all(dw == 0)
+
+
+def test_scratch_in_host_memory_is_refused():
+    with pytest.raises(ValueError, match="workspace is on cpu"):
+        B._work_of(torch.empty(1 << 20, dtype=torch.uint8))
+    assert B._work_of(None) == (None, 0)
+
+
+@pytest.mark.gpu
+def test_scratch_with_gaps_is_refused():
+    """The library takes a pointer and a number of bytes: every other byte of a buffer, or one of them many times, is no such memory.  Nothing is enqueued."""
+    n, rows, width = 2, 40, 64
+    x, gain, rstd = torch.ones(n, rows, width, device=R.DEV), torch.ones(n, width, device=R.DEV), torch.ones(n, rows, device=R.DEV)
+    size = H.hdet_rmsnorm_backward_workspace(n, rows, width)
+    buf = torch.full((2 * size,), 0x5a, dtype=torch.uint8, device=R.DEV)
+    h, labels = torch.ones(n, rows, width, dtype=BF, device=R.DEV), torch.zeros(n, rows, dtype=torch.int32, device=R.DEV)
+    codes, w = H.hdet_codes_empty(n, rows, width), H.hdet_codes_empty(n, 24, width)
+    for work in (buf[::2], buf[:1].expand(1 << 30)):
+        for call in (lambda: H.hdet_rmsnorm_backward(x, gain, rstd, x, torch.empty_like(x), dgain=torch.empty_like(gain), workspace=work),
+                     lambda: H.hdet_vocab_loss(h, h, labels, rstd, torch.empty(n, device=R.DEV), workspace=work),
+                     lambda: H.hdet_quantised_linear_backward(h[..., :24], codes, rstd, w, torch.ones(n, 24, device=R.DEV), dx=torch.empty_like(h), workspace=work)):
+            with pytest.raises(ValueError, match="workspace must be contiguous"):
+                call()
+    torch.cuda.synchronize()
+    assert torch.all(buf == 0x5a)

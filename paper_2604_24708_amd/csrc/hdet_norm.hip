@@ -402,11 +402,11 @@ __global__ __launch_bounds__(256) void hdet_row_sum_kernel(const uint16_t* x, in
       part[z * part_z + (int64_t)blockIdx.y * width + blockIdx.x * 512 + c] = (s[0][c] + s[1][c]) + (s[2][c] + s[3][c]);
 }
 
-// Rows of codes to values: a thread takes 8 columns.  Bound by memory: 8 x 8192 rows of 1024 to bf16 31 us = 6.5 TB/s of what it reads and writes (part of it in the caches).  Grid: (ceil(rows * pieces / 256), replicas).
+// Rows of codes to values: a thread takes 8 columns.  Bound by memory: 8 x 8192 rows of 1024 to bf16 31 us = 6.5 TB/s of what it reads and writes (part of it in the caches).  Grid: hdet_long_grid(rows * pieces).
 template <typename T, int WHOLE>
 __global__ __launch_bounds__(256) void hdet_restore_kernel(const int8_t* q, int64_t q_s, int64_t q_z, const float* scale, T* v, int64_t v_s, int64_t v_z,
                                                            int64_t rows, int width, int pieces) {
-  const int64_t t = (int64_t)blockIdx.x * 256 + threadIdx.x, row = t / pieces;
+  const int64_t t = hdet_long_thread(), row = t / pieces;
   const int z = blockIdx.y, col = (int)(t - row * pieces) * 8;
   if (row >= rows) return;
   const hdet_u2v w = *reinterpret_cast<const hdet_u2v*>(q + z * q_z + row * q_s + col);
@@ -417,11 +417,11 @@ __global__ __launch_bounds__(256) void hdet_restore_kernel(const int8_t* q, int6
   store_piece<WHOLE>(v + z * v_z + row * v_s + col, o, width - col);
 }
 
-// Rows of a bfloat16 matrix in rows of `pitch`, `copies` times, zeros for rows with a negative label: a thread takes 8 columns.  Grid: (ceil(rows * pieces / 256), replicas).
+// Rows of a bfloat16 matrix in rows of `pitch`, `copies` times, zeros for rows with a negative label: a thread takes 8 columns.  Grid: hdet_long_grid(rows * pieces).
 template <int WHOLE>
 __global__ __launch_bounds__(256) void hdet_pad_rows_kernel(const uint16_t* x, int64_t x_s, int64_t x_z, int64_t rows, int width, const int32_t* labels, uint16_t* out,
                                                             int64_t pitch, int copies) {
-  const int64_t pieces = pitch >> 3, t = (int64_t)blockIdx.x * 256 + threadIdx.x, row = t / pieces, all = rows * pieces;
+  const int64_t pieces = pitch >> 3, t = hdet_long_thread(), row = t / pieces, all = rows * pieces;
   const int col = (int)(t - row * pieces) * 8;
   if (row >= rows) return;
   piece<uint16_t> v;
@@ -514,7 +514,7 @@ hipError_t hdet_launch_restore(const hdet_codes_args& a, hipStream_t s) {
   if (a.rows == 0) return hipSuccess;
   const int pieces = (a.width + 7) / 8;
   const bool bf = a.dtype == HDET_TYPE_BF16, vec = pieces_of_8(a.values, bf ? 2 : 4, a.width);
-  const dim3 grid((unsigned)((a.rows * pieces + 255) / 256), a.n_replicas);
+  const dim3 grid = hdet_long_grid(a.rows * pieces, a.n_replicas);
   auto go = [&](auto kernel, auto* v) {
     hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, (const int8_t*)a.codes.dev, a.codes.row_stride, a.codes.replica_stride, a.scale_dev, v,
                        a.values.row_stride, a.values.replica_stride, a.rows, a.width, pieces);
@@ -527,7 +527,7 @@ hipError_t hdet_launch_restore(const hdet_codes_args& a, hipStream_t s) {
 }
 
 hipError_t hdet_launch_pad_rows(const hdet_rows& x, int n_replicas, int64_t rows, int width, const int32_t* labels, uint16_t* out, int64_t pitch, int copies, hipStream_t s) {
-  const dim3 grid((unsigned)((rows * (pitch >> 3) + 255) / 256), n_replicas);
+  const dim3 grid = hdet_long_grid(rows * (pitch >> 3), n_replicas);
   const uint16_t* from = (const uint16_t*)x.dev;
   if (pieces_of_8(x, 2, width)) hipLaunchKernelGGL(hdet_pad_rows_kernel<kWhole>, grid, dim3(256), 0, s, from, x.row_stride, x.replica_stride, rows, width, labels, out, pitch, copies);
   else hipLaunchKernelGGL(hdet_pad_rows_kernel<kLoose>, grid, dim3(256), 0, s, from, x.row_stride, x.replica_stride, rows, width, labels, out, pitch, copies);

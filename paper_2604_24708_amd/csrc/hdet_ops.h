@@ -3,6 +3,14 @@
 
 #include "hdet_internal.h"
 
+// Blocks of 256 threads for `threads` of them a replica, which is blockIdx.y: a launch takes fewer than 2^32 along x, and a large matrix has more elements, or pieces
+// of 8 of them
+inline dim3 hdet_long_grid(int64_t threads, int n_replicas) {
+  const int64_t blocks = (threads + 255) / 256, x = blocks < (1 << 23) ? blocks : 1 << 23;
+  return dim3((unsigned)x, n_replicas, (unsigned)((blocks + x - 1) / x));
+}
+__device__ __forceinline__ int64_t hdet_long_thread() { return ((int64_t)blockIdx.z * gridDim.x + blockIdx.x) * 256 + threadIdx.x; }
+
 // hdet_norm.hip
 hipError_t hdet_launch_norm(const hdet_norm_args& a, hipStream_t s);
 hipError_t hdet_launch_norm_backward(const hdet_norm_grad_args& a, hipStream_t s);

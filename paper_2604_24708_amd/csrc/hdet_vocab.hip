@@ -379,9 +379,9 @@ __global__ __launch_bounds__(256) void hdet_vocab_sums_kernel(const float* part,
   if (ph == 0 && col < cols) db[z * db_z + col] = ((s[0][lane] + s[1][lane]) + (s[2][lane] + s[3][lane])) * inv[z];
 }
 
-// zeros in a matrix of `size`-byte elements (2 or 4)
+// zeros in a matrix of `size`-byte elements (2 or 4).  Grid: hdet_long_grid(rows * width).
 __global__ __launch_bounds__(256) void hdet_zero_rows_kernel(void* m, int64_t row_s, int64_t rep_s, int64_t rows, int width, int size) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t i = hdet_long_thread();
   if (i >= rows * width) return;
   const int64_t at = blockIdx.y * rep_s + i / width * row_s + i % width;
   if (size == 2) ((uint16_t*)m)[at] = 0;
@@ -389,7 +389,7 @@ __global__ __launch_bounds__(256) void hdet_zero_rows_kernel(void* m, int64_t ro
 }
 
 hipError_t hdet_launch_zero_rows(const hdet_rows& m, int n_replicas, int64_t rows, int width, int dtype, hipStream_t s) {
-  hipLaunchKernelGGL(hdet_zero_rows_kernel, dim3((unsigned)((rows * width + 255) / 256), n_replicas), dim3(256), 0, s, m.dev, m.row_stride, m.replica_stride, rows, width,
+  hipLaunchKernelGGL(hdet_zero_rows_kernel, hdet_long_grid(rows * width, n_replicas), dim3(256), 0, s, m.dev, m.row_stride, m.replica_stride, rows, width,
                      dtype == HDET_TYPE_BF16 ? 2 : 4);
   return hipGetLastError();
 }

@@ -343,7 +343,8 @@ typedef struct {
 /* Root-mean-square norm of a residual sum:
  *   u = x + resid (u = x without resid),  total = u,  rstd = 1 / sqrt(mean_j u_j^2 + eps),
  *   y_j = u_j rstd gain_j,  codes and scale: y in 8 bits.
- * Sums in fp32; the norm is that of u before it is rounded to `total`.  total, y, codes (with
+ * The sum of squares, the norm and what is rounded to codes are held in 64 bits (u of bfloat16
+ * summands in fp32); the norm is that of u before it is rounded to `total`.  total, y, codes (with
  * scale) and rstd are written where they are given.  total may be x or resid itself.          */
 typedef struct {
   int32_t   n_replicas;
@@ -397,8 +398,9 @@ int hdet_quantise_rows(const hdet_codes_args* args, void* stream);      /* reads
 int hdet_restore_rows(const hdet_codes_args* args, void* stream);       /* writes values      */
 
 /* y = X W^T + bias with X [rows][d_in] and W [d_out][d_in] in 8 bits: whole-number sums of code
- * products (exact in 32 bits), times both scales, plus bias, rounded once.  Scales may be any
- * numbers here.                                                                             */
+ * products (exact in 32 bits), rounded to fp32 (from 2^24 on), times the fp32 product of both scales,
+ * plus bias in one fused step, and rounded to y's type.  Scales may be any numbers here whose product
+ * fp32 holds.                                                                               */
 typedef struct {
   int32_t   n_replicas, y_dtype;               /* HDET_TYPE_* of y                           */
   int64_t   rows;

@@ -416,9 +416,10 @@ int hdet_quantised_linear(const hdet_linear_args* args, void* stream);
 
 /* Gradients of that layer from the 8-bit copies and dy (bfloat16):
  *   dx = dy W (bfloat16, optional),  dw = dy^T X (fp32, optional),  db = sum over the rows of dy (fp32, optional)
- * in bfloat16 products with fp32 sums.  The values code * scale are read as bfloat16 numbers: exact for the
- * scales that this library chooses, rounded for others.  X (for dw) and W (for dx) pass through the workspace in bfloat16:
- * hdet_quantised_linear_backward_workspace bytes, 16-byte aligned (a call without some of the results needs no more).                       */
+ * in bfloat16 products with fp32 sums.  The values code * scale are read as bfloat16 numbers: exact
+ * for the scales that this library chooses, rounded for others.  X (for dw) and W (for dx) pass
+ * through the workspace in bfloat16: hdet_quantised_linear_backward_workspace bytes, 16-byte aligned
+ * (a call without some of the results needs no more).                                        */
 typedef struct {
   int32_t   n_replicas, reserved;
   int64_t   rows;
@@ -444,11 +445,15 @@ int hdet_quantised_linear_backward(const hdet_linear_grad_args* args, void* stre
  *   dh = dz W,   dw = dz^T h,   db = sum over the rows of dz
  * h, W and dh are bfloat16; sums are fp32.  dw is bfloat16 or fp32.  dh and a bfloat16 dw are
  * formed from dz rounded to bfloat16, an fp32 dw from dz in three such parts (24 bits) and with two more
- * products.  dh, dw and db are optional: without them only the losses are formed.  A row that does not count takes part in nothing, whatever its row of h holds (NaN and
- * infinity too).  A bias of -inf takes a class of a finite row of W out of the sum; a row that counts and has no class left is NaN.
- * piece: classes at a time (taken down to whole groups of 256 or, below that, of 8), or 0 for the library's choice.  The workspace depends on it and on dw
- * (hdet_vocab_loss_workspace with the same arguments; HDET_VOCAB_NO_DW for the type of a dw that is absent, HDET_VOCAB_LOSSES where dh and db are too): without dw no more
- * than with either type, for the losses alone no more than that; 16-byte aligned. */
+ * products.  dh, dw and db are optional: without them only the losses are formed.
+ * A row that does not count takes part in nothing, whatever its row of h holds (NaN and infinity
+ * too).  A bias of -inf takes a class of a finite row of W out of the sum; a row that counts and has
+ * no class left is NaN.
+ * piece: classes at a time (taken down to whole groups of 256 or, below that, of 8), or 0 for the
+ * library's choice.  The workspace (16-byte aligned) depends on it and on the results:
+ * hdet_vocab_loss_workspace with the same arguments, HDET_VOCAB_NO_DW for the type of a dw that is
+ * absent, HDET_VOCAB_LOSSES where dh and db are too.  Without dw it is no more than with one of
+ * either type, for the losses alone no more than that.                                       */
 enum { HDET_VOCAB_NO_DW = -1, HDET_VOCAB_LOSSES = -2 };
 typedef struct {
   int32_t   n_replicas, dw_dtype;              /* HDET_TYPE_* of dw                          */

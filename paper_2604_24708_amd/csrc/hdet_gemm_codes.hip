@@ -1,10 +1,11 @@
-// Product of two matrices in 8 bits, N replicas:  y = s_m t_o sum_k q[m][k] w[o][k] + b_o,  on v_mfma_i32_16x16x64_i8.  The sums of code products
-// are whole numbers below 2^31 and exact; both scales and the bias come in as fp32 where a sum is complete.
+// Product of two matrices in 8 bits, N replicas:  y = s_m t_o sum_k q[m][k] w[o][k] + b_o,  on v_mfma_i32_16x16x64_i8.  The sums of code
+// products are whole numbers below 2^31 and exact; both scales and the bias come in as fp32 where a sum is complete.
 //
-//  * Tiles (hdet_codes_gemm_kernel): both operands are contiguous along k and their rows start at 16-byte boundaries, with zeros behind the last
-//    column up to the next one, so every shape is made of whole 16-byte chunks.  Chunks go from global memory straight into LDS, a K step of 128 bytes a row,
-//    NST steps in flight; a row's chunks are permuted by row / 2 so that the 128-bit fragment reads are free of bank conflicts.  Rows past the matrix and
-//    chunks past k lie outside the buffer descriptor and arrive as zeros: no edge cases in the loop.
+//  * Tiles (hdet_codes_gemm_kernel): both operands are contiguous along k and their rows start at 16-byte boundaries, with zeros behind the
+//    last column up to the next one, so every shape is made of whole 16-byte chunks.  Chunks go from global memory straight into LDS, a K
+//    step of 128 bytes a row, NST steps in flight; a row's chunks are permuted by row / 2 so that the 128-bit fragment reads are free of
+//    bank conflicts.  Rows past the matrix and chunks past k lie outside the buffer descriptor and arrive as zeros: no edge cases in the
+//    loop.
 //  * Few rows (hdet_codes_rows_kernel): the weights' stream is all there is; see there.
 
 #include "hdet_ops.h"
@@ -150,17 +151,18 @@ void hdet_codes_gemm_kernel(const codes_args g) {
   }
 }
 
-// Large products: blocks that walk over tiles of 256 x 256, so that a tile's end -- y is written there, as many bytes as the products of a K of 500 take to form -- lies under the
-// next tile's loads.
-//  * Eight wavefronts of 128 x 64 in two groups of four, one of each on every SIMD: while one group multiplies (32 instructions, 512 cycles), the other reads its next
-//    fragments and requests a later K step; the block's barriers hand the matrix cores over.  A K step of 128 bytes is two such turns: rows 0-63 of the wavefront, then rows
-//    64-127 with the column fragments still in registers.  Two stages of 64 KiB; each turn waits for all but the newest eight of its loads.
+// Large products: blocks that walk over tiles of 256 x 256, so that a tile's end -- y is written there, as many bytes as the products of a
+// K of 500 take to form -- lies under the next tile's loads.
+//  * Eight wavefronts of 128 x 64 in two groups of four, one of each on every SIMD: while one group multiplies (32 instructions, 512
+//    cycles), the other reads its next fragments and requests a later K step; the block's barriers hand the matrix cores over.  A K step of
+//    128 bytes is two such turns: rows 0-63 of the wavefront, then rows 64-127 with the column fragments still in registers.  Two stages of
+//    64 KiB; each turn waits for all but the newest eight of its loads.
 //  * The next tile's first two K steps are requested in the last two of the tile before; its scales and bias come into LDS a tile ahead.
-//  * Results leave from the registers.  Stores are always issued -- what does not exist lies outside the descriptor.  The next tile's first two K steps are requested before them, and its
-//    first three turns wait for those loads, not for the stores.
+//  * Results leave from the registers.  Stores are always issued -- what does not exist lies outside the descriptor.  The next tile's first
+//    two K steps are requested before them, and its first three turns wait for those loads, not for the stores.
 //  * Rows and columns past the matrices are zeros in the loop, and their results are not stored.
-// 8192^3 402 us = 2.7 POP/s, 8 x 8192 rows 1024 -> 4096 336 us = 1.6, 8 x 4096 rows 512 -> 2048 48 us = 1.4 (3.3 TB/s): what a tile stores bounds the short contractions.  Of those 336 us 71 go
-// without the stores and 95 without the tile's end altogether.
+// 8192^3 402 us = 2.7 POP/s, 8 x 8192 rows 1024 -> 4096 336 us = 1.6, 8 x 4096 rows 512 -> 2048 48 us = 1.4 (3.3 TB/s): what a tile stores
+// bounds the short contractions.  Of those 336 us 71 go without the stores and 95 without the tile's end altogether.
 template <typename OUT>
 __global__ __launch_bounds__(512, 2) void hdet_codes_walk_kernel(const codes_args g, unsigned gx, unsigned gy, unsigned total, int tile_group) {
   constexpr int TM = 256, TN = 256, HALF = 128 * 128;             // bytes of half an operand tile
@@ -179,8 +181,9 @@ __global__ __launch_bounds__(512, 2) void hdet_codes_walk_kernel(const codes_arg
   const uint32_t s_addr = lds_addr_of(S);
   const int8_t* const base = reinterpret_cast<const int8_t*>(S);
   const float* const side = reinterpret_cast<const float*>(base + kSideAt);
-  // A fragment is rows order(i) + row_in(0 .. 15) of the wavefront's 64, so a lane of group cg = lane / 16 accumulates columns order(j) + cg * kGroup + (0 .. 3), j = 0 .. 3, of
-  // y.  For bfloat16 results the order gives it 8 neighbours twice, so that one store of 16 bytes a lane covers 64 bytes of each row; four fp32 results are 16 bytes as they are.
+  // A fragment is rows order(i) + row_in(0 .. 15) of the wavefront's 64, so a lane of group cg = lane / 16 accumulates columns order(j) +
+  // cg * kGroup + (0 .. 3), j = 0 .. 3, of y.  For bfloat16 results the order gives it 8 neighbours twice, so that one store of 16 bytes a
+  // lane covers 64 bytes of each row; four fp32 results are 16 bytes as they are.
   constexpr bool kPlain = sizeof(OUT) == 4;
   constexpr int kGroup = kPlain ? 4 : 8;
   auto order = [](int j) { return kPlain ? j * 16 : (j >> 1) * 32 + (j & 1) * 4; };
@@ -202,7 +205,8 @@ __global__ __launch_bounds__(512, 2) void hdet_codes_walk_kernel(const codes_arg
   };
   const int ck = ((tid & 7) ^ perm(tid >> 3)) * 16;
   uint32_t off_a = (uint32_t)((tid >> 3) * g.x_ld + ck), off_b = (uint32_t)((tid >> 3) * g.w_ld + ck);
-  // LDS, in units of 128 rows x 128 bytes: half h of A of stage s at 2 h + s (its rows 64 .. 127 are the tile's 128 .. 191 of that half), B at 4 + 2 s
+  // LDS, in units of 128 rows x 128 bytes: half h of A of stage s at 2 h + s (its rows 64 .. 127 are the tile's 128 .. 191 of that half), B
+  // at 4 + 2 s
   auto load_a = [&](const hdet_rsrc& r, int h, int s, int kt) {
     const uint32_t at = s_addr + (2 * h + s) * HALF;
 #pragma unroll
@@ -322,7 +326,8 @@ __global__ __launch_bounds__(512, 2) void hdet_codes_walk_kernel(const codes_arg
       for (int s = 0; s < 2; ++s) {
         const int kt = kt0 + s;
         const bool fs = first && s == 0;
-        // all but the newest eight loads; in a tile's first three turns those are older than the stores of the tile before, which need not be done
+        // all but the newest eight loads; in a tile's first three turns those are older than the stores of the tile before, which need not
+        // be done
         auto wait = [&](bool early) {
           if (early && begun) wait_and_barrier<8 + kStores>();
           else wait_and_barrier<8>();
@@ -363,8 +368,10 @@ __global__ __launch_bounds__(512, 2) void hdet_codes_walk_kernel(const codes_arg
   wait_and_barrier<0>();
 }
 
-// Up to 16 rows.  The weights' stream is the work: a block takes 16 columns of y, its four wavefronts a quarter of k each, with fragments straight from global
-// memory (16 rows of the weights, 64 bytes of each, an instruction) and no barrier in the loop; whole-number partial sums are added through LDS.  8 x 16 rows, 1024 -> 4096: 10.5 us, the weights at 3.2 TB/s; 8 x 1 row, 512 -> 2048: 4.0 us, a launch and its chain.
+// Up to 16 rows.  The weights' stream is the work: a block takes 16 columns of y, its four wavefronts a quarter of k each, with fragments
+// straight from global memory (16 rows of the weights, 64 bytes of each, an instruction) and no barrier in the loop; whole-number partial
+// sums are added through LDS.  8 x 16 rows, 1024 -> 4096: 10.5 us, the weights at 3.2 TB/s; 8 x 1 row, 512 -> 2048: 4.0 us, a launch and
+// its chain.
 template <typename OUT>
 __global__ __launch_bounds__(256) void hdet_codes_rows_kernel(const codes_args g) {
   __shared__ i4v part[4][64];
@@ -411,7 +418,8 @@ namespace {
 template <typename OUT>
 hipError_t launch_typed(const codes_args& g, int n_replicas, hipStream_t s) {
   const int size = sizeof(OUT);
-  // Up to 16 rows; beyond, the tiles' shorter chain counts for more than their empty rows (8 x 64 rows, 1024 -> 4096: 24 us in blocks of 16 columns, 13 in tiles)
+  // Up to 16 rows; beyond, the tiles' shorter chain counts for more than their empty rows (8 x 64 rows, 1024 -> 4096: 24 us in blocks of 16
+  // columns, 13 in tiles)
   if (g.m <= 16) {
     hipLaunchKernelGGL(hdet_codes_rows_kernel<OUT>, dim3((g.n + 15) / 16, 1, n_replicas), dim3(256), 0, s, g);
     return hipGetLastError();

@@ -1,6 +1,6 @@
 // Root-mean-square norm of a residual sum with an output in 8 bits, its backward pass, rows to 8 bits and back, and sums over rows.
 //
-//   u = x + r,  rstd = 1 / sqrt(mean u^2 + eps),  y = u rstd g;  codes q = rint(y / s) with s the power of two that takes max|y| to 127 or less
+//   u = x + r,  rstd = 1 / sqrt(mean u^2 + eps),  y = u rstd g;  codes q = rint(y / s), s the power of two that takes max|y| to 127 or less
 //   dx = rstd (dy g - xh mean(dy g xh)) + dtotal,  xh = h rstd;  dg = sum_rows dy xh
 //
 // All of it is bound by memory: a row is read once, stays in registers between its sums and its results, and nothing but the results is
@@ -14,13 +14,15 @@
 
 namespace {
 
-// How a launch's rows lie: anywhere; in whole pieces of 8 elements at 16-byte boundaries; the same, and so much of it that what is written would push what is still to be read out of
-// the memory-side cache (256 MB): past the caches then.  us, through / past:  backward 8 x 8192 rows of 1024 119 / 101, 8 x 4096 of 512 26.5 / 29;  forward 84 / 78 and 22 / 26
+// How a launch's rows lie: anywhere; in whole pieces of 8 elements at 16-byte boundaries; the same, and so much of it that what is written
+// would push what is still to be read out of the memory-side cache (256 MB): past the caches then.  us, through / past:  backward 8 x 8192
+// rows of 1024 119 / 101, 8 x 4096 of 512 26.5 / 29;  forward 84 / 78 and 22 / 26
 enum { kLoose = 0, kWhole = 1, kStream = 2 };
 
-// Eight neighbouring elements of a row of `width`, as they lie in memory; zeros behind the row's end.  Where rows are not whole pieces one lies at any
-// element, which the memory takes as it takes aligned ones but for the lines it crosses; the last piece of a row is loaded from 8 elements before the end and moved
-// into place, so that no lane waits for another's single elements (an odd row of 1001: 14.5 us of a launch that takes 9 so).
+// Eight neighbouring elements of a row of `width`, as they lie in memory; zeros behind the row's end.  Where rows are not whole pieces one
+// lies at any element, which the memory takes as it takes aligned ones but for the lines it crosses; the last piece of a row is loaded from
+// 8 elements before the end and moved into place, so that no lane waits for another's single elements (an odd row of 1001: 14.5 us of a
+// launch that takes 9 so).
 typedef hdet_u4v hdet_u4v_any __attribute__((aligned(2)));
 typedef hdet_f4v hdet_f4v_any __attribute__((aligned(4)));
 template <typename T> struct piece;
@@ -129,8 +131,9 @@ __device__ __forceinline__ V over_row(V x, V* buf, F op) {
 template <int L, typename V> __device__ __forceinline__ V row_sum_of(V x, V* buf) { return over_row<L>(x, buf, [](V a, V b) { return a + b; }); }
 __device__ __forceinline__ unsigned larger(unsigned a, unsigned b) { return a > b ? a : b; }
 
-// Scale of a row from the bits of its largest absolute value.  With top = m 2^(E - 126), m in [1/2, 1): 127 2^e >= top from e = E - 133 on, or one more
-// where m > 127 / 128.  Absolute values compare as their bits do, NaN above infinity above all numbers: either gives the exponent 255.
+// Scale of a row from the bits of its largest absolute value.  With top = m 2^(E - 126), m in [1/2, 1): 127 2^e >= top from e = E - 133 on,
+// or one more where m > 127 / 128.  Absolute values compare as their bits do, NaN above infinity above all numbers: either gives the
+// exponent 255.
 struct row_scale { float scale, inverse; };
 __device__ __forceinline__ row_scale scale_of(unsigned top) {
   const int E = (int)(top >> 23);
@@ -139,7 +142,8 @@ __device__ __forceinline__ row_scale scale_of(unsigned top) {
   if (e < -126) e = -126;
   return {__uint_as_float((unsigned)(e + 127) << 23), __uint_as_float((unsigned)(127 - e) << 23)};
 }
-// rint(x inverse) as the low bits of that + 1.5 2^52, halves to even; |x inverse| is 127 at most, up to what rounding the row's largest value to fp32 took off
+// rint(x inverse) as the low bits of that + 1.5 2^52, halves to even; |x inverse| is 127 at most, up to what rounding the row's largest
+// value to fp32 took off
 __device__ __forceinline__ unsigned code_of(double x, double inverse) {
   return (unsigned)__builtin_bit_cast(unsigned long long, __builtin_fma(x, inverse, 6755399441055744.0));
 }
@@ -157,11 +161,13 @@ struct norm_kernel_args {
 
 }  // namespace
 
-// The sum of squares, the norm and what is rounded to codes are held in 64 bits, which costs a tenth of the time (8 x 8192 rows of 1024, bf16, sum and codes: 80 us in 32 bits, 88 so) and
-// puts a code where the formula has it: in 32 bits y is off by up to 3e-7 of itself, and about one row in 800 (normally distributed, 1000 columns) has a code one off.  Bound by memory:
-// that size 87 us = 5.4 TB/s, 8 x 4096 rows of 512 25.5 us; one row of 512 3.6 us, a launch and its chain of load, two reductions and store.
+// The sum of squares, the norm and what is rounded to codes are held in 64 bits, which costs a tenth of the time (8 x 8192 rows of 1024,
+// bf16, sum and codes: 80 us in 32 bits, 88 so) and puts a code where the formula has it: in 32 bits y is off by up to 3e-7 of itself, and
+// about one row in 800 (normally distributed, 1000 columns) has a code one off.  Bound by memory: that size 87 us = 5.4 TB/s, 8 x 4096 rows
+// of 512 25.5 us; one row of 512 3.6 us, a launch and its chain of load, two reductions and store.
 // NORM: as above; otherwise y = x (rows to 8 bits).  Grid: (ceil(rows / rows a block), replicas).
-// (The row is in registers from its two loads to its two or three stores; what is left between the loads and the stores are the two reductions.)
+// (The row is in registers from its two loads to its two or three stores; what is left between the loads and the stores are the two
+// reductions.)
 template <typename T, int WHOLE, int L, int C, bool NORM>
 __global__ __launch_bounds__(L < 256 ? 256 : L) void hdet_norm_kernel(const norm_kernel_args a) {
   constexpr int THREADS = L < 256 ? 256 : L, RPB = THREADS / L;
@@ -251,10 +257,11 @@ struct norm_grad_kernel_args {
 };
 }  // namespace
 
-// Grid: (blocks, replicas); a block takes every gridDim.x-th group of rows and adds up its columns' dy xh on the way (the gain's gradient is then
-// `blocks` rows instead of all of them for a second launch).  A row stays in registers as it lies in memory, the gain is in LDS; other wavefronts cover a row's loads.  Bound by memory: 8 x 8192
-// rows of 1024, bf16, 96 us = 5.6 TB/s, 8 x 4096 of 512 24.  Not faster, us, of 115 to 119 through the caches: consecutive rows a block 128, four times the blocks 142, registers for 5, 6 or 8
-// wavefronts a SIMD 207, 292, 413 (spills); the next row's loads under a row 115, but 16.8 for 12.9 at 3 x 777 rows of 1001 in fp32.
+// Grid: (blocks, replicas); a block takes every gridDim.x-th group of rows and adds up its columns' dy xh on the way (the gain's gradient
+// is then `blocks` rows instead of all of them for a second launch).  A row stays in registers as it lies in memory, the gain is in LDS;
+// other wavefronts cover a row's loads.  Bound by memory: 8 x 8192 rows of 1024, bf16, 96 us = 5.6 TB/s, 8 x 4096 of 512 24.  Not faster,
+// us, of 115 to 119 through the caches: consecutive rows a block 128, four times the blocks 142, registers for 5, 6 or 8 wavefronts a SIMD
+// 207, 292, 413 (spills); the next row's loads under a row 115, but 16.8 for 12.9 at 3 x 777 rows of 1001 in fp32.
 template <typename T, int WHOLE, int L, int C>
 __global__ __launch_bounds__(L < 256 ? 256 : L) void hdet_norm_grad_kernel(const norm_grad_kernel_args a) {
   constexpr int THREADS = L < 256 ? 256 : L, RPB = THREADS / L, COLS = L * 8 * C;
@@ -355,7 +362,8 @@ __global__ __launch_bounds__(L < 256 ? 256 : L) void hdet_norm_grad_kernel(const
   }
 }
 
-// out[z][col] = sum over p of part[z][p][col], ascending in 16 phases that are added in their order.  Block = 64 columns x 16 phases; grid (ceil(width / 64), replicas).
+// out[z][col] = sum over p of part[z][p][col], ascending in 16 phases that are added in their order.  Block = 64 columns x 16 phases; grid
+// (ceil(width / 64), replicas).
 __global__ __launch_bounds__(1024) void hdet_partial_sum_kernel(const float* part, int parts, int width, int64_t pitch, float* out, int64_t out_z) {
   __shared__ float s[16][64];
   const int lane = threadIdx.x & 63, col = blockIdx.x * 64 + lane, ph = threadIdx.x >> 6, z = blockIdx.y;
@@ -374,7 +382,8 @@ __global__ __launch_bounds__(1024) void hdet_partial_sum_kernel(const float* par
   out[z * out_z + col] = x;
 }
 
-// Sums over `each` rows of a bfloat16 matrix.  Block = 64 pieces of 8 columns x 4 phases of rows, eight rows' loads in flight; grid (column blocks, row blocks, replicas).
+// Sums over `each` rows of a bfloat16 matrix.  Block = 64 pieces of 8 columns x 4 phases of rows, eight rows' loads in flight; grid (column
+// blocks, row blocks, replicas).
 // (8 x 8192 rows of 4096, more than the memory-side cache holds: 122 us, past the caches 93 = 5.8 TB/s.)
 template <int WHOLE>
 __global__ __launch_bounds__(256) void hdet_row_sum_kernel(const uint16_t* x, int64_t x_s, int64_t x_z, int64_t rows, int each, int width, float* part, int64_t part_z) {
@@ -402,7 +411,8 @@ __global__ __launch_bounds__(256) void hdet_row_sum_kernel(const uint16_t* x, in
       part[z * part_z + (int64_t)blockIdx.y * width + blockIdx.x * 512 + c] = (s[0][c] + s[1][c]) + (s[2][c] + s[3][c]);
 }
 
-// Rows of codes to values: a thread takes 8 columns.  Bound by memory: 8 x 8192 rows of 1024 to bf16 31 us = 6.5 TB/s of what it reads and writes (part of it in the caches).  Grid: hdet_long_grid(rows * pieces).
+// Rows of codes to values: a thread takes 8 columns.  Bound by memory: 8 x 8192 rows of 1024 to bf16 31 us = 6.5 TB/s of what it reads and
+// writes (part of it in the caches).  Grid: hdet_long_grid(rows * pieces).
 template <typename T, int WHOLE>
 __global__ __launch_bounds__(256) void hdet_restore_kernel(const int8_t* q, int64_t q_s, int64_t q_z, const float* scale, T* v, int64_t v_s, int64_t v_z,
                                                            int64_t rows, int width, int pieces) {
@@ -417,7 +427,8 @@ __global__ __launch_bounds__(256) void hdet_restore_kernel(const int8_t* q, int6
   store_piece<WHOLE>(v + z * v_z + row * v_s + col, o, width - col);
 }
 
-// Rows of a bfloat16 matrix in rows of `pitch`, `copies` times, zeros for rows with a negative label: a thread takes 8 columns.  Grid: hdet_long_grid(rows * pieces).
+// Rows of a bfloat16 matrix in rows of `pitch`, `copies` times, zeros for rows with a negative label: a thread takes 8 columns.  Grid:
+// hdet_long_grid(rows * pieces).
 template <int WHOLE>
 __global__ __launch_bounds__(256) void hdet_pad_rows_kernel(const uint16_t* x, int64_t x_s, int64_t x_z, int64_t rows, int width, const int32_t* labels, uint16_t* out,
                                                             int64_t pitch, int copies) {

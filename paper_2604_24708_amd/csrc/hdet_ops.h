@@ -3,8 +3,8 @@
 
 #include "hdet_internal.h"
 
-// Blocks of 256 threads for `threads` of them a replica, which is blockIdx.y: a launch takes fewer than 2^32 along x, and a large matrix has more elements, or pieces
-// of 8 of them
+// Blocks of 256 threads for `threads` of them a replica, which is blockIdx.y: a launch takes fewer than 2^32 along x, and a large matrix
+// has more elements, or pieces of 8 of them
 inline dim3 hdet_long_grid(int64_t threads, int n_replicas) {
   const int64_t blocks = (threads + 255) / 256, x = blocks < (1 << 23) ? blocks : 1 << 23;
   return dim3((unsigned)x, n_replicas, (unsigned)((blocks + x - 1) / x));
@@ -20,8 +20,8 @@ hipError_t hdet_launch_restore(const hdet_codes_args& a, hipStream_t s);
 // Sums over the rows of a bfloat16 matrix, [width] per replica, in a fixed order; scratch: hdet_row_sum_bytes bytes.
 size_t hdet_row_sum_bytes(int n_replicas, int64_t rows, int width);
 hipError_t hdet_launch_row_sum(const hdet_rows& x, int n_replicas, int64_t rows, int width, float* out, int64_t out_stride, void* scratch, hipStream_t s);
-// A bfloat16 matrix as `copies` matrices below each other in rows of `pitch` elements (a multiple of 8, at least width), zeros behind the last column and
-// in rows whose label ([replica][row], or null: none) is negative
+// A bfloat16 matrix as `copies` matrices below each other in rows of `pitch` elements (a multiple of 8, at least width), zeros behind the
+// last column and in rows whose label ([replica][row], or null: none) is negative
 hipError_t hdet_launch_pad_rows(const hdet_rows& x, int n_replicas, int64_t rows, int width, const int32_t* labels, uint16_t* out, int64_t pitch, int copies, hipStream_t s);
 // The second half of such a sum: out[z][j] = sum_p partial[z][p][j]
 hipError_t hdet_launch_partial_sum(const float* partial, int n_replicas, int parts, int width, int64_t pitch, float* out, int64_t out_stride, hipStream_t s);

@@ -80,9 +80,10 @@ int entry(const char* name, F check, G launch) {
 int element(int dtype) { return dtype == HDET_TYPE_BF16 ? 2 : 4; }
 
 size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
-// Workspace of the linear layer's gradients, of what the results that are wanted need: X (for dw) and W (for dx) in bfloat16, and dy where its rows are no whole 16-byte
-// pieces, in rows of whole pieces; partial sums of dy, results of pieces of a long contraction.  (X over W, which dx is done with by then: 57.9 -> 60.7 us for 3 x 515 rows of
-// 776 -> 1501, 44.7 -> 46.5 for 3 x 500 of 512 -> 1536, 1192 -> 1199 for 8 x 8192 of 1024 -> 4096.)
+// Workspace of the linear layer's gradients, of what the results that are wanted need: X (for dw) and W (for dx) in bfloat16, and dy where
+// its rows are no whole 16-byte pieces, in rows of whole pieces; partial sums of dy, results of pieces of a long contraction.  (X over W,
+// which dx is done with by then: 57.9 -> 60.7 us for 3 x 515 rows of 776 -> 1501, 44.7 -> 46.5 for 3 x 500 of 512 -> 1536, 1192 -> 1199 for
+// 8 x 8192 of 1024 -> 4096.)
 struct linear_layout { int64_t pitch, dy_pitch; hdet_split for_dx, for_dw; size_t x, w, dy, sum, part, total; };
 linear_layout linear_layout_of(int n, int64_t rows, int d_in, int d_out, bool dx, bool dw, bool db) {
   linear_layout l;

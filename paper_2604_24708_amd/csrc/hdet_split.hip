@@ -1,11 +1,13 @@
-// Products of few tiles and a long contraction, in pieces of it: the pieces are further batch items of one launch, their fp32 results are added by a second one.  (One block a
-// compute unit walks 64 of the contraction in 0.4 us: a tile of 128 x 128 with 9600 of it alone took 62 us.)
+// Products of few tiles and a long contraction, in pieces of it: the pieces are further batch items of one launch, their fp32 results are
+// added by a second one.  (One block a compute unit walks 64 of the contraction in 0.4 us: a tile of 128 x 128 with 9600 of it alone took
+// 62 us.)
 
 #include "hdet_ops.h"
 #include "hdet_elem.h"
 
-// How a product is split: not at all from half a tile of 128 x 128 a compute unit on, else into as many pieces as there are units to take them, of 512 at least.  (us of the call,
-// whole / split: loss of 2 x 1000 rows of 776, 5000 classes, 112 tiles, two pieces 184 / 169;  100 rows of 96, 9600 classes, one tile 115 / 56)
+// How a product is split: not at all from half a tile of 128 x 128 a compute unit on, else into as many pieces as there are units to take
+// them, of 512 at least.  (us of the call, whole / split: loss of 2 x 1000 rows of 776, 5000 classes, 112 tiles, two pieces 184 / 169;  100
+// rows of 96, 9600 classes, one tile 115 / 56)
 hdet_split hdet_split_of(int batch, int64_t m, int64_t n, int64_t k) {
   hdet_split s = {1, k, 0};
   const int64_t tiles = ((m + 127) / 128) * ((n + 127) / 128) * batch, cus = hdet_compute_units();

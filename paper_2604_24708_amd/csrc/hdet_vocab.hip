@@ -2,20 +2,24 @@
 //
 //   z = h W^T + b,  loss = log sum exp z - z_label,  dz = (softmax(z) - onehot) / c,  dh = dz W,  dW = dz^T h,  db = sum_rows dz
 //
-// No more than `piece` classes of z and dz exist at a time: a first round forms each row's reference and sum of exponentials, a second forms z again,
-// dz from it, and with dz the piece's share of dh (added up in fp32) and its rows of dW and db.
+// No more than `piece` classes of z and dz exist at a time: a first round forms each row's reference and sum of exponentials, a second
+// forms z again, dz from it, and with dz the piece's share of dh (added up in fp32) and its rows of dW and db.
 //
-//  * Where h and W are made of whole 16-byte chunks -- copies are made of rows that are not -- z never leaves the matrix cores' registers: one product leaves reference and sum of each tile's part of a row,
-//    a second dz (hdet_bgemm_walk_kernel).  Rows of whole chunks at other boundaries take z through memory in fp32, by pieces that are smaller
-//    by as much.
-//  * Exponentials are exp2(z log2(e) - r) with r the whole number next to max log2(e): tiles and pieces refer to each other by exact powers of two.  The label's z is
-//    taken times the same fp32 log2(e): 64 bits of it there would leave 1.3e-8 of the logit's size in the loss (-4e-5 for a row certain of a label at 3008).
-//  * dz is held as c dz = softmax - onehot and the products' results are divided by c: at a label it is next to -1, which a bfloat16 holds to 2^-9 of itself, where
-//    (softmax - onehot) / c lies anywhere between two powers of two (dh against 64 bits: 2.9e-3 of its norm with the division before the rounding).
-//  * dz leaves as bfloat16 -- what the matrix cores multiply -- for dh and a bfloat16 dW, whose own rounding is as coarse.  An fp32 dW takes dz in three bfloat16
-//    parts, 24 bits: they stand below each other as rows, beside three copies of h, and make one product of three times the rows.  (Two fp16 parts take two thirds of that product -- 4 x 8192
-//    rows of 1024, 32000 classes: the call 9.3 ms for 10.8 -- but hold nothing below about 2^-40: the gradient of a class that is never likely came out as 0.)
-//  * Bound by the products and by the exponentials and stores at their tiles' ends.  8 x 4096 rows of 512, 32000 classes, bf16 dW, us: statistics 1064 (1.0 PFLOP/s), dz 1320 (0.8), dh 820 (1.3), dW 885 (1.2).
+//  * Where h and W are made of whole 16-byte chunks -- copies are made of rows that are not -- z never leaves the matrix cores' registers:
+//    one product leaves reference and sum of each tile's part of a row, a second dz (hdet_bgemm_walk_kernel).  Rows of whole chunks at
+//    other boundaries take z through memory in fp32, by pieces that are smaller by as much.
+//  * Exponentials are exp2(z log2(e) - r) with r the whole number next to max log2(e): tiles and pieces refer to each other by exact powers
+//    of two.  The label's z is taken times the same fp32 log2(e): 64 bits of it there would leave 1.3e-8 of the logit's size in the loss
+//    (-4e-5 for a row certain of a label at 3008).
+//  * dz is held as c dz = softmax - onehot and the products' results are divided by c: at a label it is next to -1, which a bfloat16 holds
+//    to 2^-9 of itself, where (softmax - onehot) / c lies anywhere between two powers of two (dh against 64 bits: 2.9e-3 of its norm with
+//    the division before the rounding).
+//  * dz leaves as bfloat16 -- what the matrix cores multiply -- for dh and a bfloat16 dW, whose own rounding is as coarse.  An fp32 dW
+//    takes dz in three bfloat16 parts, 24 bits: they stand below each other as rows, beside three copies of h, and make one product of
+//    three times the rows.  (Two fp16 parts take two thirds of that product -- 4 x 8192 rows of 1024, 32000 classes: the call 9.3 ms for
+//    10.8 -- but hold nothing below about 2^-40: the gradient of a class that is never likely came out as 0.)
+//  * Bound by the products and by the exponentials and stores at their tiles' ends.  8 x 4096 rows of 512, 32000 classes, bf16 dW, us:
+//    statistics 1086 (1.0 PFLOP/s), dz 1318 (0.8), dh 818 (1.3), dW 880 (1.2).
 
 #include <type_traits>
 
@@ -28,8 +32,8 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr double kLn2 = 0.6931471805599453;
 constexpr int kRowChunk = 128;                          // rows of a block's column sums in tiles
 constexpr size_t kSmallRoom = (size_t)64 << 20;         // z and dz take that much where they pass through memory, if not all of them fits what dz alone takes
-// Most that z takes in a call for the losses alone (us, rows one element off a 16-byte boundary, 64 / 128 / 256 MB: 8 x 4096 rows of 512, 32000 classes 7677 / 5859 / 6561,
-// 4 x 8192 of 1024, 32000 8922 / 8088 / 8958, 4096 of 1024, 50000 1709 / 1664 / 1764)
+// Most that z takes in a call for the losses alone (us, rows one element off a 16-byte boundary, 64 / 128 / 256 MB: 8 x 4096 rows of 512,
+// 32000 classes 7677 / 5859 / 6561, 4 x 8192 of 1024, 32000 8922 / 8088 / 8958, 4096 of 1024, 50000 1709 / 1664 / 1764)
 constexpr size_t kLossRoom = (size_t)128 << 20;
 constexpr size_t kPieceBytes = (size_t)1 << 30;         // most that dz of a piece takes where the caller does not say
 
@@ -40,7 +44,8 @@ struct vocab_layout {
   int planes;               // bfloat16 parts of dz
   int64_t bias_pitch;
   int64_t width8;           // a row of h and W in whole 16-byte pieces
-  int h_copies;             // copies of h in such rows, zeros in those that do not count: as many below each other as dz has parts; without dw one where h's own rows are no whole pieces
+  int h_copies;             // copies of h in such rows, zeros in those that do not count: as many below each other as dz has parts;
+                            // without dw one where h's own rows are no whole pieces
   size_t inv, labels, ref, a, sum, zy, bias, dz, h, w, acc, part, split, split_bytes, total;
 };
 size_t up(size_t x) { return (x + 255) & ~(size_t)255; }
@@ -51,17 +56,20 @@ int rows_each(int n, int64_t rows, int cols) {
   while (each > 4 && (rows + each - 1) / each * ((cols + 1023) / 1024) * n < 2 * hdet_compute_units()) each >>= 1;
   return each;
 }
-// Whether z goes through memory also where it could stay in the matrix cores' registers: up to a tile of 256 x 256 on every fourth compute unit, where a tile's long way from the first
-// load to the last store (12 us for its statistics, 18 for dz in three parts) counts for more than the passes over z, and up to 8192 classes, whose rows the statistics walk one
-// block each.  us of the call, registers / memory (tiles):  4 x 128 rows of 64, 512 classes, fp32 dW (8) 51 / 37;  3 x 159 of 896, 523 (9) 78 / 49;  4 x 256 of 1024, 2048 (32) 101 / 75;
+// Whether z goes through memory also where it could stay in the matrix cores' registers: up to a tile of 256 x 256 on every fourth compute
+// unit, where a tile's long way from the first load to the last store (12 us for its statistics, 18 for dz in three parts) counts for more
+// than the passes over z, and up to 8192 classes, whose rows the statistics walk one block each.  us of the call, registers / memory
+// (tiles):  4 x 128 rows of 64, 512 classes, fp32 dW (8) 51 / 37;  3 x 159 of 896, 523 (9) 78 / 49;  4 x 256 of 1024, 2048 (32) 101 / 75;
 // 1024 of 512, 4096 (64) 100 / 85;  256 of 512, 16384 (64) 95 / 107;  100 of 90, 9600 (38) 63 / 66;  2 x 512 of 256, 8192 (128) 85 / 169
 bool small_call(int n, int64_t rows, int classes) {
   return classes <= 8192 && 4 * ((rows + 255) / 256 * ((classes + 255) / 256) * n) <= hdet_compute_units();
 }
 
-// Classes at a time.  A piece's dW is one product with the rows as its contraction: it wants whole rounds of 256 x 256 tiles over the compute units, and every piece costs
-// about a twelfth of a round in launches, first loads and passes over the sum of dh.  us, by classes a piece (rounds of each):
-//   8 x 4096 rows of 512, 32000 classes, bf16 dW: 1536 (3/8) 4876, 2048 (1/2) 4484, 4096 (1) 4161, 6400 (1.6) 4110, 8192 (2) 4028, 16384 (4) 3947, 32000 3860
+// Classes at a time.  A piece's dW is one product with the rows as its contraction: it wants whole rounds of 256 x 256 tiles over the
+// compute units, and every piece costs about a twelfth of a round in launches, first loads and passes over the sum of dh.  us, by classes a
+// piece (rounds of each):
+//   8 x 4096 rows of 512, 32000 classes, bf16 dW: 1536 (3/8) 4876, 2048 (1/2) 4484, 4096 (1) 4161, 6400 (1.6) 4110, 8192 (2) 4028,
+//     16384 (4) 3947, 32000 3860
 //   4 x 8192 rows of 1024, 32000 classes, fp32 dW: 2048 (1/2) 12739, 4096 (1) 10972, 6400 (1.6) 11420, 8192 (2) 10720, 32000 10439
 //   4096 rows of 1024, 50000 classes, bf16: 2048 (1/8) 2689, 4096 (1/4) 1883, 8192 (1/2) 1697, 16384 (1) 1550, 32000 (2) 1558, 50000 1684
 // Between the two stands kPieceBytes.
@@ -85,7 +93,8 @@ int chosen_piece(int n, size_t class_bytes, int width, int classes, size_t piece
   return best >= columns ? classes : (int)best * 256;
 }
 
-// kind: HDET_TYPE_* of dw, or one of HDET_VOCAB_*.  Pieces are made for plan_planes parts of dz that take piece_bytes at most, for a call with dw or without.
+// kind: HDET_TYPE_* of dw, or one of HDET_VOCAB_*.  Pieces are made for plan_planes parts of dz that take piece_bytes at most, for a call
+// with dw or without.
 vocab_layout layout_in(int n, int64_t rows, int width, int classes, int kind, int plan_planes, int piece, size_t piece_bytes = kPieceBytes, bool for_dw = true) {
   vocab_layout l;
   const size_t all = (size_t)n * rows;
@@ -149,8 +158,8 @@ vocab_layout layout_in(int n, int64_t rows, int width, int classes, int kind, in
   return l;
 }
 
-// Memory that is enough for a call with a dw of either type is enough without: pieces as large as the smaller of the two allows, at the least those of one of the calls
-// with dw, whose own layout less what only dw needs fits it.
+// Memory that is enough for a call with a dw of either type is enough without: pieces as large as the smaller of the two allows, at the
+// least those of one of the calls with dw, whose own layout less what only dw needs fits it.
 vocab_layout layout_of(int n, int64_t rows, int width, int classes, int kind, int piece) {
   if (kind >= 0) return layout_in(n, rows, width, classes, kind, kind == HDET_TYPE_F32 ? 3 : 1, piece);
   int planes = 1, eighths = 8;
@@ -182,8 +191,8 @@ struct prep_args {
 
 }  // namespace
 
-// What a call starts with, [replica] on blockIdx.y: labels that name no class become -1; 1 / rows that count; bias in rows padded with -inf; copies of h below
-// each other, zeros in rows that do not count (their dz is 0 and would take a NaN or infinity of h into dW's sum).
+// What a call starts with, [replica] on blockIdx.y: labels that name no class become -1; 1 / rows that count; bias in rows padded with
+// -inf; copies of h below each other, zeros in rows that do not count (their dz is 0 and would take a NaN or infinity of h into dW's sum).
 __global__ __launch_bounds__(1024) void hdet_vocab_prep_kernel(const prep_args a) {
   const int z = blockIdx.y;
   const int64_t t = (int64_t)blockIdx.x * 1024 + threadIdx.x, step = (int64_t)gridDim.x * 1024;
@@ -217,7 +226,8 @@ __global__ __launch_bounds__(1024) void hdet_vocab_prep_kernel(const prep_args a
   }
 }
 
-// Reference and sum of a row over the classes so far, and its label's logit; after the last piece its loss.  Block = one row of a piece; grid (rows, replicas).
+// Reference and sum of a row over the classes so far, and its label's logit; after the last piece its loss.  Block = one row of a piece;
+// grid (rows, replicas).
 __global__ __launch_bounds__(256) void hdet_vocab_stat_kernel(const float* z, int64_t pitch, int64_t rows, int cols, int v0, const int32_t* labels, float* ref,
                                                               double* sum, float* zy, bool last, float* a_out, float* row_loss) {
   __shared__ float part[4];
@@ -259,7 +269,8 @@ __global__ __launch_bounds__(256) void hdet_vocab_stat_kernel(const float* z, in
   }
 }
 
-// What it leaves after the last piece, from the column tiles' references and sums ([replica][tile][row]); lse: log2 of the sum of exp2(z log2(e)).  Rows that do not count: loss and factor 0.
+// What it leaves after the last piece, from the column tiles' references and sums ([replica][tile][row]); lse: log2 of the sum of exp2(z
+// log2(e)).  Rows that do not count: loss and factor 0.
 // Block = 64 rows x 4 phases; phase q takes tiles q, q + 4, ..., the phases are added in their order, in 64 bits.
 __global__ __launch_bounds__(256) void hdet_vocab_merge_kernel(const float2* part, int tiles, int64_t rows, const int32_t* labels, float* ref, float* a, double* lse, float* row_loss) {
   __shared__ float refs[4][64];
@@ -317,7 +328,8 @@ __global__ __launch_bounds__(256) void hdet_vocab_label_kernel(const uint16_t* h
   if (lane == 0) row_loss[at] = (float)((lse[at] - (double)s * (double)kLog2e) * kLn2);
 }
 
-// c dz of a piece from z, in PLANES bfloat16 parts, and its sums over `each` rows.  Thread = 4 columns; grid (ceil(pitch / 1024), row blocks, replicas).
+// c dz of a piece from z, in PLANES bfloat16 parts, and its sums over `each` rows.  Thread = 4 columns; grid (ceil(pitch / 1024), row
+// blocks, replicas).
 template <int PLANES>
 __global__ __launch_bounds__(256) void hdet_vocab_grad_kernel(const float* z, int64_t pitch, int64_t rows, int each, int cols, int v0, const int32_t* labels, const float* ref,
                                                               const float* a, uint16_t* dz, float* part, int64_t part_pitch) {
@@ -351,7 +363,8 @@ __global__ __launch_bounds__(256) void hdet_vocab_grad_kernel(const float* z, in
   if (part && c < part_pitch) *reinterpret_cast<hdet_f4v*>(part + ((int64_t)zr * gridDim.y + blockIdx.y) * part_pitch + c) = sum;
 }
 
-// db of a piece from its column sums, 64 columns x 4 phases a block; the last block column, where row_loss is given: the mean loss.  Grid (blocks, replicas).
+// db of a piece from its column sums, 64 columns x 4 phases a block; the last block column, where row_loss is given: the mean loss.  Grid
+// (blocks, replicas).
 __global__ __launch_bounds__(256) void hdet_vocab_sums_kernel(const float* part, int parts, int cols, int64_t pitch, float* db, int64_t db_z, const float* inv, const float* row_loss,
                                                               int64_t rows, float* mean) {
   __shared__ double sum[4];

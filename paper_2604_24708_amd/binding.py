@@ -528,7 +528,9 @@ def hdet_vocab_loss_workspace(n_replicas: int, rows: int, width: int, classes: i
     """`dw`: the dtype of the weight gradient, HDET_VOCAB_NO_DW for calls without one or HDET_VOCAB_LOSSES for the losses alone; None: float32.  What is enough with a dw of
     either type is enough without."""
     load_library()
-    kind = dw if isinstance(dw, int) else HDET_TYPE_BF16 if dw == _BF16 else HDET_TYPE_F32
+    kind = dw if isinstance(dw, int) else _CODE.get(_F32 if dw is None else dw)
+    if kind is None:
+        raise ValueError(f"dw is {dw}: float32 or bfloat16 is wanted")
     return _size_of("hdet_vocab_loss_workspace", n_replicas, rows, width, classes, kind, piece)
 
 

@@ -62,6 +62,11 @@ def test_the_losses_alone_need_no_gradient_of_the_logits():
             H.hdet_vocab_loss_workspace(1, 1, 1, 1, dw=bad)
 
 
+def test_the_size_for_a_dw_that_the_call_would_refuse_is_refused():
+    with pytest.raises(ValueError):
+        H.hdet_vocab_loss_workspace(1, 1, 1, 1, dw=torch.float16)
+
+
 def guarded(size):
     """`size` bytes of scratch memory, and what lies behind them."""
     t = torch.full((size + 4096,), 0xa5, dtype=torch.uint8, device=R.DEV)

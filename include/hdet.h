@@ -475,6 +475,161 @@ typedef struct {
 int hdet_vocab_loss_workspace(int32_t n_replicas, int64_t rows, int32_t width, int32_t classes, int32_t dw_dtype, int32_t piece, size_t* bytes);
 int hdet_vocab_loss(const hdet_vocab_args* args, void* stream);
 
+/* Norm of every head of the queries and keys with the rotation by position, in one pass.  A row of q
+ * is q_heads heads of head_dim columns, one of k k_heads; q and k may be slices of one matrix.
+ *   xh = x rstd, rstd = 1 / sqrt(mean_c x_c^2 + eps) over the head's columns,  u = xh gain   (u = x where the gain is NULL)
+ *   y: for each pair t of the head's first `rotated` columns, with a = position * freq_t,
+ *      y_1 = magnitude (u_1 cos a - u_2 sin a),  y_2 = magnitude (u_1 sin a + u_2 cos a);  y = u in the other columns
+ * Pair t is the columns t and t + rotated / 2 (HDET_ROTARY_HALVES) or 2 t and 2 t + 1 (HDET_ROTARY_PAIRS).
+ * freq_dev holds rotated / 2 frequencies in radians a position, in 64 bits, as any stretching for long
+ * contexts leaves them (hdet_rotary_frequencies makes the usual ones); angles are formed and reduced
+ * in 64 bits, good for any 32-bit position.  Row i of a replica stands at positions_dev[replica][i] or, where
+ * that is NULL, at i mod period (i where period is 0).  Sums of squares are 64 bits, the rest fp32.
+ * q_out may be q itself and k_out k itself.  k absent (dev NULL): q alone; its norm and the keys' are
+ * each left out where their gain is NULL.                                                    */
+enum { HDET_ROTARY_HALVES = 0, HDET_ROTARY_PAIRS = 1 };
+#define HDET_MAX_ROTARY_DIM 256
+typedef struct {
+  int32_t   n_replicas, dtype;                 /* HDET_TYPE_* of q, k and their outputs      */
+  int64_t   rows;
+  int32_t   head_dim;                          /* 1 .. HDET_MAX_ROTARY_DIM                   */
+  int32_t   q_heads, k_heads;                  /* heads * head_dim up to 2^20                */
+  int32_t   rotated;                           /* even, 0 .. head_dim                        */
+  int32_t   layout;                            /* HDET_ROTARY_*                              */
+  int32_t   period;                            /* >= 0                                       */
+  double    eps, magnitude;
+  hdet_rows q, k, q_out, k_out;
+  const float*   q_gain_dev;                   /* [head_dim] per replica, stride apart, or NULL: no norm */
+  int64_t        q_gain_stride;
+  const float*   k_gain_dev;
+  int64_t        k_gain_stride;
+  const int32_t* positions_dev;                /* [N][rows] or NULL                          */
+  const double*  freq_dev;                     /* [rotated / 2]                              */
+} hdet_rotary_args;
+int hdet_head_rotary(const hdet_rotary_args* args, void* stream);
+
+/* Backward pass: dq_out and dk_out are the gradients at the outputs, q and k what the forward pass
+ * took (needed with a gain only).  With w = dq_out rotated back (by -a, times magnitude):
+ *   dq = rstd (w gain - xh mean_c(w_c gain_c xh_c))   (w where the gain is NULL)
+ *   dgain_c = sum over rows and heads of w_c xh_c     (in a fixed order; optional)
+ * dq may be dq_out itself, dk dk_out.  workspace: hdet_head_rotary_backward_workspace bytes (needed
+ * for the gains' gradients only), 16-byte aligned.                                          */
+typedef struct {
+  int32_t   n_replicas, dtype;
+  int64_t   rows;
+  int32_t   head_dim, q_heads, k_heads, rotated, layout, period;
+  double    eps, magnitude;
+  hdet_rows q, k, dq_out, dk_out, dq, dk;
+  const float*   q_gain_dev;
+  int64_t        q_gain_stride;
+  const float*   k_gain_dev;
+  int64_t        k_gain_stride;
+  const int32_t* positions_dev;
+  const double*  freq_dev;
+  float*    dq_gain_dev;                       /* [head_dim] per replica, stride apart, or NULL */
+  int64_t   dq_gain_stride;
+  float*    dk_gain_dev;
+  int64_t   dk_gain_stride;
+  void*     workspace_dev;
+  size_t    workspace_bytes;
+} hdet_rotary_grad_args;
+int hdet_head_rotary_backward_workspace(int32_t n_replicas, int64_t rows, int32_t head_dim, int32_t q_heads, int32_t k_heads, size_t* bytes);
+int hdet_head_rotary_backward(const hdet_rotary_grad_args* args, void* stream);
+
+/* freq_host[t] = b^(-2 t / rotated), t < rotated / 2, stretched for contexts longer than those of training (factor 1: not):
+ *   HDET_STRETCH_POSITIONS  every frequency over factor
+ *   HDET_STRETCH_BASE       b = base factor^(rotated / (rotated - 2)) (rotated > 2): the fastest pair stays, the slowest is over factor
+ *   HDET_STRETCH_PARTS      pairs that turn `fast` times or more over `context` positions stay, those that turn `slow` times or
+ *                           less are over factor, in between the two frequencies are mixed in proportion to the turns
+ * On the host; context, slow and fast are read by HDET_STRETCH_PARTS only (0 < slow < fast).  */
+enum { HDET_STRETCH_POSITIONS = 0, HDET_STRETCH_BASE = 1, HDET_STRETCH_PARTS = 2 };
+int hdet_rotary_frequencies(int32_t rotated, double base, int32_t stretch, double factor, double context, double slow, double fast, double* freq_host);
+
+/* Attention of `seqs` sequences a replica, each q_len queries over kv_len keys: query i of sequence b is row
+ * b * q_len + i of q and out, key j row b * kv_len + j of k and v.  A row of q and out is `heads` heads of head_dim
+ * columns, one of k and v kv_heads heads; query head h reads key head h / (heads / kv_heads).
+ *   z_ij = scale q_i . k_j;  with softcap > 0, z_ij = softcap tanh(z_ij / softcap);  with slopes, z_ij -= slope_h |position_i - j|
+ *   out_i = sum_j p_ij v_j,  p_i = softmax of z_i over the keys that query i attends,  lse_i = log sum_j exp(z_ij)
+ * Query i stands at key position positions_dev[replica][row] or, where that is NULL, at i + kv_len - q_len.  It attends the keys
+ * of its sequence from the largest of 0, first_dev[row] and, with window > 0, position - window + 1 on, and before the
+ * smallest of kv_len, end_dev[row] and, with causal, position + 1.  (Packed documents: first = the document's start.
+ * A prefix that all queries see: causal 0, end = the larger of position + 1 and the prefix.  Padding and caches with
+ * room: end; rows of padding: end = 0.)  A query that attends no key has out 0, lse -infinity and gradient 0.
+ * Keys, values and queries take part only in the pairs that are attended: whatever the others hold, NaN and infinity
+ * too, leaves no trace.
+ * Scores, statistics and sums are fp32; bfloat16 inputs: p (relative to a maximum of the row) is rounded to bfloat16 for the product with v,
+ * p and dz are for the gradients' products.  out may not lie over the inputs.  workspace: hdet_attention_workspace bytes, 16-byte aligned
+ * (0 for most sizes: what few queries over many keys leave in pieces).                                       */
+#define HDET_MAX_ATTENTION_DIM 128
+typedef struct {
+  int32_t   n_replicas, dtype;                 /* HDET_TYPE_* of q, k, v and out             */
+  int32_t   seqs, q_len, kv_len;               /* seqs * q_len up to 2^21, seqs * kv_len up to 2^28 */
+  int32_t   heads, kv_heads, head_dim;         /* heads a multiple of kv_heads, heads * head_dim up to 2^20 */
+  int32_t   causal, window;                    /* window 0: none                             */
+  double    scale, softcap;                    /* softcap 0: none                            */
+  hdet_rows q, k, v, out;
+  float*    lse_dev;                           /* [N][heads][seqs * q_len] or NULL           */
+  const float*   slopes_dev;                   /* [heads] per replica, slopes_stride apart, or NULL */
+  int64_t        slopes_stride;
+  const int32_t* positions_dev;                /* [N][seqs * q_len] or NULL                  */
+  const int32_t* first_dev;
+  const int32_t* end_dev;
+  void*     workspace_dev;
+  size_t    workspace_bytes;
+} hdet_attention_args;
+int hdet_attention_workspace(int32_t n_replicas, int32_t seqs, int32_t q_len, int32_t kv_len, int32_t heads, int32_t kv_heads, int32_t head_dim, size_t* bytes);
+int hdet_attention(const hdet_attention_args* args, void* stream);
+
+/* Backward pass, from what the forward pass took, its out and lse, and dout (all with the same mask arguments):
+ *   dv_j = sum_i p_ij dout_i,  dz_ij = p_ij (dout_i . v_j - dout_i . out_i),  times 1 - tanh^2 with softcap
+ *   dq_i = scale sum_j dz_ij k_j,  dk_j = scale sum_i dz_ij q_i       (over the heads that share the key head; in a fixed order)
+ * workspace: hdet_attention_backward_workspace bytes, 16-byte aligned.                       */
+typedef struct {
+  int32_t   n_replicas, dtype;
+  int32_t   seqs, q_len, kv_len, heads, kv_heads, head_dim, causal, window;
+  double    scale, softcap;
+  hdet_rows q, k, v, out, dout, dq, dk, dv;
+  const float*   lse_dev;
+  const float*   slopes_dev;
+  int64_t        slopes_stride;
+  const int32_t* positions_dev;
+  const int32_t* first_dev;
+  const int32_t* end_dev;
+  void*     workspace_dev;
+  size_t    workspace_bytes;
+} hdet_attention_grad_args;
+int hdet_attention_backward_workspace(int32_t n_replicas, int32_t seqs, int32_t q_len, int32_t kv_len, int32_t heads, int32_t kv_heads, int32_t head_dim, size_t* bytes);
+int hdet_attention_backward(const hdet_attention_grad_args* args, void* stream);
+
+/* Gradients of many tensors, bounded by their common norm, on the way into the plane that hdet_fanout_step reads.
+ *   norm_r = sqrt of the sum of g^2 over all tensors of replica r; with HDET_GRAD_SHARED that of the replicas' mean gradient, the same for all r
+ *   out = g factor_r,  factor_r = max_norm / norm_r where norm_r > max_norm, else 1
+ * Sums are 64 bits in a fixed order, the factor is rounded to fp32.  A norm that is not finite leaves factor 1: norm_dev says so to
+ * the caller.  max_norm infinite: nothing is bounded (and without `out` only the norm is formed).
+ * tensors_host: read during the call only (the addresses in it are what a captured graph keeps).  Every tensor is an hdet_rows of rows x width;
+ * `out` is fp32 in any strides, or absent: the gradients themselves are scaled, in their type.  No two elements of outputs (and of gradients that are
+ * scaled in place) may share memory, within a tensor or between two; two tensors that start at the same place are refused.
+ * Elements between the tensors of a plane are left as they are.
+ * workspace: hdet_clip_gradients_workspace bytes, 16-byte aligned.                           */
+#define HDET_MAX_GRAD_TENSORS 65536
+typedef struct {
+  hdet_rows grad, out;
+  int64_t   rows;                              /* rows * width up to 2^40                    */
+  int32_t   width;
+  int32_t   dtype;                             /* HDET_TYPE_* of grad                        */
+} hdet_grad_tensor;
+typedef struct {
+  int32_t   n_replicas, n_tensors;             /* 0 tensors: norm 0                          */
+  const hdet_grad_tensor* tensors_host;
+  int32_t   grad_mode, reserved;               /* HDET_GRAD_PER_REPLICA or HDET_GRAD_SHARED  */
+  double    max_norm;                          /* >= 0                                       */
+  float*    norm_dev;                          /* [N]                                        */
+  void*     workspace_dev;
+  size_t    workspace_bytes;
+} hdet_clip_args;
+int hdet_clip_gradients_workspace(int32_t n_replicas, int32_t n_tensors, size_t* bytes);
+int hdet_clip_gradients(const hdet_clip_args* args, void* stream);
+
 #ifdef __cplusplus
 }
 #endif

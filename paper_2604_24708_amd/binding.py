@@ -26,6 +26,9 @@ HDET_FUSE_CONVERGE = 1
 HDET_TYPE_F32, HDET_TYPE_BF16 = 0, 1
 HDET_MAX_NORM_WIDTH, HDET_MAX_CODES_WIDTH = 32768, 131056
 HDET_VOCAB_NO_DW, HDET_VOCAB_LOSSES = -1, -2
+HDET_ROTARY_HALVES, HDET_ROTARY_PAIRS = 0, 1
+HDET_STRETCH_POSITIONS, HDET_STRETCH_BASE, HDET_STRETCH_PARTS = 0, 1, 2
+HDET_MAX_ROTARY_DIM, HDET_MAX_ATTENTION_DIM, HDET_MAX_GRAD_TENSORS = 256, 128, 65536
 
 EXPORTS = [
     "hdet_workspace_bytes", "hdet_create", "hdet_warm_init", "hdet_warm_init_noalloc", "hdet_forward_backward", "hdet_fanout_step", "hdet_train_step",
@@ -34,6 +37,9 @@ EXPORTS = [
     "hdet_rmsnorm", "hdet_rmsnorm_backward_workspace", "hdet_rmsnorm_backward", "hdet_quantise_rows", "hdet_restore_rows",
     "hdet_quantised_linear", "hdet_quantised_linear_backward_workspace", "hdet_quantised_linear_backward",
     "hdet_vocab_loss_workspace", "hdet_vocab_loss",
+    "hdet_head_rotary", "hdet_head_rotary_backward_workspace", "hdet_head_rotary_backward", "hdet_rotary_frequencies",
+    "hdet_attention_workspace", "hdet_attention", "hdet_attention_backward_workspace", "hdet_attention_backward",
+    "hdet_clip_gradients_workspace", "hdet_clip_gradients",
 ]
 
 
@@ -138,6 +144,45 @@ class hdet_vocab_args(C.Structure):
                 ("workspace_dev", C.c_void_p), ("workspace_bytes", C.c_size_t)]
 
 
+class hdet_rotary_args(C.Structure):
+    _fields_ = [("n_replicas", C.c_int32), ("dtype", C.c_int32), ("rows", C.c_int64), ("head_dim", C.c_int32), ("q_heads", C.c_int32), ("k_heads", C.c_int32),
+                ("rotated", C.c_int32), ("layout", C.c_int32), ("period", C.c_int32), ("eps", C.c_double), ("magnitude", C.c_double),
+                ("q", hdet_rows), ("k", hdet_rows), ("q_out", hdet_rows), ("k_out", hdet_rows), ("q_gain_dev", C.c_void_p), ("q_gain_stride", C.c_int64),
+                ("k_gain_dev", C.c_void_p), ("k_gain_stride", C.c_int64), ("positions_dev", C.c_void_p), ("freq_dev", C.c_void_p)]
+
+
+class hdet_rotary_grad_args(C.Structure):
+    _fields_ = [("n_replicas", C.c_int32), ("dtype", C.c_int32), ("rows", C.c_int64), ("head_dim", C.c_int32), ("q_heads", C.c_int32), ("k_heads", C.c_int32),
+                ("rotated", C.c_int32), ("layout", C.c_int32), ("period", C.c_int32), ("eps", C.c_double), ("magnitude", C.c_double),
+                ("q", hdet_rows), ("k", hdet_rows), ("dq_out", hdet_rows), ("dk_out", hdet_rows), ("dq", hdet_rows), ("dk", hdet_rows),
+                ("q_gain_dev", C.c_void_p), ("q_gain_stride", C.c_int64), ("k_gain_dev", C.c_void_p), ("k_gain_stride", C.c_int64),
+                ("positions_dev", C.c_void_p), ("freq_dev", C.c_void_p), ("dq_gain_dev", C.c_void_p), ("dq_gain_stride", C.c_int64),
+                ("dk_gain_dev", C.c_void_p), ("dk_gain_stride", C.c_int64), ("workspace_dev", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+_ATTENTION_SIZES = [(name, C.c_int32) for name in ("n_replicas", "dtype", "seqs", "q_len", "kv_len", "heads", "kv_heads", "head_dim", "causal", "window")] + [
+    ("scale", C.c_double), ("softcap", C.c_double)]
+_ATTENTION_MASK = [("slopes_dev", C.c_void_p), ("slopes_stride", C.c_int64), ("positions_dev", C.c_void_p), ("first_dev", C.c_void_p), ("end_dev", C.c_void_p),
+                   ("workspace_dev", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
+class hdet_attention_args(C.Structure):
+    _fields_ = _ATTENTION_SIZES + [(name, hdet_rows) for name in ("q", "k", "v", "out")] + [("lse_dev", C.c_void_p)] + _ATTENTION_MASK
+
+
+class hdet_attention_grad_args(C.Structure):
+    _fields_ = _ATTENTION_SIZES + [(name, hdet_rows) for name in ("q", "k", "v", "out", "dout", "dq", "dk", "dv")] + [("lse_dev", C.c_void_p)] + _ATTENTION_MASK
+
+
+class hdet_grad_tensor(C.Structure):
+    _fields_ = [("grad", hdet_rows), ("out", hdet_rows), ("rows", C.c_int64), ("width", C.c_int32), ("dtype", C.c_int32)]
+
+
+class hdet_clip_args(C.Structure):
+    _fields_ = [("n_replicas", C.c_int32), ("n_tensors", C.c_int32), ("tensors_host", C.POINTER(hdet_grad_tensor)), ("grad_mode", C.c_int32),
+                ("reserved", C.c_int32), ("max_norm", C.c_double), ("norm_dev", C.c_void_p), ("workspace_dev", C.c_void_p), ("workspace_bytes", C.c_size_t)]
+
+
 LIB_PATH = os.path.join(os.path.dirname(os.path.abspath(__file__)), "libhdet.so")
 _lib = None
 
@@ -161,8 +206,8 @@ def load_library(path: Optional[str] = None):
     # libhdet.so binds to, or the library and the tensors it is handed would live in two
     # runtimes (the second one finds no device).  Importing torch first loads that copy.
     import torch
-    global _F32, _BF16, _I8, _I32, _CODE
-    _F32, _BF16, _I8, _I32 = torch.float32, torch.bfloat16, torch.int8, torch.int32
+    global _F32, _BF16, _I8, _I32, _F64, _CODE
+    _F32, _BF16, _I8, _I32, _F64 = torch.float32, torch.bfloat16, torch.int8, torch.int32, torch.float64
     _CODE = {_F32: HDET_TYPE_F32, _BF16: HDET_TYPE_BF16}
     lib = C.CDLL(p)
     vp = C.c_void_p
@@ -184,12 +229,18 @@ def load_library(path: Optional[str] = None):
     lib.hdet_destroy.argtypes = [vp]
     for name, args in (("hdet_rmsnorm", hdet_norm_args), ("hdet_rmsnorm_backward", hdet_norm_grad_args), ("hdet_quantise_rows", hdet_codes_args),
                        ("hdet_restore_rows", hdet_codes_args), ("hdet_quantised_linear", hdet_linear_args),
-                       ("hdet_quantised_linear_backward", hdet_linear_grad_args), ("hdet_vocab_loss", hdet_vocab_args)):
+                       ("hdet_quantised_linear_backward", hdet_linear_grad_args), ("hdet_vocab_loss", hdet_vocab_args),
+                       ("hdet_head_rotary", hdet_rotary_args), ("hdet_head_rotary_backward", hdet_rotary_grad_args), ("hdet_attention", hdet_attention_args),
+                       ("hdet_attention_backward", hdet_attention_grad_args), ("hdet_clip_gradients", hdet_clip_args)):
         getattr(lib, name).argtypes = [C.POINTER(args), vp]
     size = C.POINTER(C.c_size_t)
     lib.hdet_rmsnorm_backward_workspace.argtypes = [C.c_int32, C.c_int64, C.c_int32, size]
     lib.hdet_quantised_linear_backward_workspace.argtypes = [C.c_int32, C.c_int64, C.c_int32, C.c_int32, size]
     lib.hdet_vocab_loss_workspace.argtypes = [C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_int32, size]
+    lib.hdet_head_rotary_backward_workspace.argtypes = [C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_int32, size]
+    lib.hdet_rotary_frequencies.argtypes = [C.c_int32, C.c_double, C.c_int32, C.c_double, C.c_double, C.c_double, C.c_double, C.POINTER(C.c_double)]
+    lib.hdet_attention_workspace.argtypes = lib.hdet_attention_backward_workspace.argtypes = [C.c_int32] * 7 + [size]
+    lib.hdet_clip_gradients_workspace.argtypes = [C.c_int32, C.c_int32, size]
     for name in EXPORTS:
         if name != "hdet_last_error":
             getattr(lib, name).restype = C.c_int
@@ -346,7 +397,7 @@ def hdet_destroy(h):
 # between rows and replicas); vectors a replica are [N, columns]; row scalars [N, rows] are contiguous.  `stream`: a hipStream_t as
 # an integer, None for the default stream.  Tensors are borrowed until the work on that stream is done.
 # ---------------------------------------------------------------------------------------
-_F32 = _BF16 = _I8 = _I32 = _CODE = None       # torch's types, from load_library on
+_F32 = _BF16 = _I8 = _I32 = _F64 = _CODE = None       # torch's types, from load_library on
 
 
 def _refuse(name, t, shape, dtype, contiguous=False):
@@ -547,5 +598,166 @@ def hdet_vocab_loss(h, w, labels, row_loss, mean_loss, dh=None, dw=None, bias=No
                         _scalars("row_loss", row_loss, (n, rows)), _scalars("mean_loss", mean_loss, (n,)), _rows_of("dh", dh, shape, _BF16),
                         _ABSENT if dw is None else _rows_of("dw", dw, wide, dw.dtype), *_vector("db", db, (n, classes)), *_work_of(workspace))
     rc = lib.hdet_vocab_loss(C.byref(a), stream)
+    if rc:
+        _check(rc)
+
+
+def hdet_rotary_frequencies(rotated: int, base: float = 10000.0, stretch: int = HDET_STRETCH_POSITIONS, factor: float = 1.0, context: float = 0.0,
+                            slow: float = 1.0, fast: float = 32.0, device="cuda"):
+    """Radians a position for each of rotated / 2 pairs of columns, float64 [rotated / 2] on `device`."""
+    import torch
+    out = (C.c_double * max(rotated // 2, 1))()
+    _check(load_library().hdet_rotary_frequencies(rotated, base, stretch, factor, context, slow, fast, out))
+    return torch.tensor(out[:rotated // 2], dtype=torch.float64, device=device)
+
+
+def _heads_of(name, t, head_dim) -> int:
+    if head_dim < 1 or t.shape[2] % head_dim:
+        raise ValueError(f"{name} has {t.shape[2]} columns: whole heads of {head_dim} are wanted")
+    return t.shape[2] // head_dim
+
+
+def _rotary_sizes(q, k, head_dim, freq, paired, period, eps, magnitude):
+    """The fields up to `magnitude`, from the tensors of the queries and keys."""
+    n, rows, _ = q.shape
+    return (n, _dtype_code("q", q), rows, head_dim, _heads_of("q", q, head_dim), 0 if k is None else _heads_of("k", k, head_dim),
+            0 if freq is None else 2 * freq.shape[0], HDET_ROTARY_PAIRS if paired else HDET_ROTARY_HALVES, period, eps, magnitude)
+
+
+def hdet_head_rotary(q, q_out, head_dim: int, k=None, k_out=None, q_gain=None, k_gain=None, freq=None, positions=None, period: int = 0, paired: bool = False,
+                     magnitude: float = 1.0, eps: float = 1e-6, stream: Optional[int] = None):
+    """q_out <- the heads of q [N, rows, heads * head_dim], each normed (with q_gain [N, head_dim]) and rotated by its row's position (int32 [N, rows]; None: row mod period, the
+    row where period is 0); k_out <- the same of k.  freq: float64 [pairs]; the first 2 * pairs columns of a head turn, neighbours with each other (`paired`) or halves."""
+    lib = _lib or load_library()
+    shape, dt = q.shape, q.dtype
+    n, rows, _ = shape
+    ks = None if k is None else (n, rows, k.shape[2])
+    a = hdet_rotary_args(*_rotary_sizes(q, k, head_dim, freq, paired, period, eps, magnitude), _rows_of("q", q, shape, dt), _rows_of("k", k, ks, dt),
+                         _rows_of("q_out", q_out, shape, dt), _rows_of("k_out", None if k is None else k_out, ks, dt), *_vector("q_gain", q_gain, (n, head_dim)),
+                         *_vector("k_gain", k_gain, (n, head_dim)), _scalars("positions", positions, (n, rows), _I32),
+                         None if freq is None else _scalars("freq", freq, freq.shape[:1], _F64))
+    rc = lib.hdet_head_rotary(C.byref(a), stream)
+    if rc:
+        _check(rc)
+
+
+def hdet_head_rotary_backward_workspace(n_replicas: int, rows: int, head_dim: int, q_heads: int, k_heads: int = 0) -> int:
+    return _size_of("hdet_head_rotary_backward_workspace", n_replicas, rows, head_dim, q_heads, k_heads)
+
+
+def hdet_head_rotary_backward(q, dq_out, dq, head_dim: int, k=None, dk_out=None, dk=None, q_gain=None, k_gain=None, freq=None, positions=None, period: int = 0,
+                              paired: bool = False, magnitude: float = 1.0, eps: float = 1e-6, dq_gain=None, dk_gain=None, workspace=None, stream: Optional[int] = None):
+    """dq (and dk) <- the gradient at q (k) from the one at q_out (k_out); dq_gain, dk_gain [N, head_dim] <- the gains'.  q and k may be None where there is no gain."""
+    lib = _lib or load_library()
+    shape, dt = dq_out.shape, dq_out.dtype
+    n, rows, _ = shape
+    ks = None if dk_out is None else (n, rows, dk_out.shape[2])
+    a = hdet_rotary_grad_args(*_rotary_sizes(dq_out, dk_out, head_dim, freq, paired, period, eps, magnitude), _rows_of("q", q, shape, dt),
+                              _rows_of("k", k, ks, dt) if ks else _ABSENT, _rows_of("dq_out", dq_out, shape, dt), _rows_of("dk_out", dk_out, ks, dt),
+                              _rows_of("dq", dq, shape, dt), _rows_of("dk", dk, ks, dt) if ks else _ABSENT, *_vector("q_gain", q_gain, (n, head_dim)),
+                              *_vector("k_gain", k_gain, (n, head_dim)), _scalars("positions", positions, (n, rows), _I32),
+                              None if freq is None else _scalars("freq", freq, freq.shape[:1], _F64), *_vector("dq_gain", dq_gain, (n, head_dim)),
+                              *_vector("dk_gain", dk_gain, (n, head_dim)), *_work_of(workspace))
+    rc = lib.hdet_head_rotary_backward(C.byref(a), stream)
+    if rc:
+        _check(rc)
+
+
+def _attention_sizes(q, k, heads, kv_heads, seqs, causal, window, scale, softcap):
+    """The fields up to `softcap`, and the shapes of the queries, the keys and the row scalars."""
+    n, rows, width = q.shape
+    keys = k.shape[1]
+    if heads < 1 or width % heads:
+        raise ValueError(f"q has {width} columns: {heads} heads are wanted")
+    if seqs < 0 or (rows % seqs or keys % seqs if seqs else rows or keys):
+        raise ValueError(f"q has {rows} rows and k {keys}: {seqs} sequences of one length each are wanted")
+    d = width // heads
+    return ((n, _dtype_code("q", q), seqs, rows // seqs if seqs else 0, keys // seqs if seqs else 0, heads, kv_heads, d, 1 if causal else 0, window,
+             d ** -0.5 if scale is None and d else scale or 0.0, softcap), q.shape, (n, keys, kv_heads * d), (n, rows))
+
+
+def hdet_attention_workspace(n_replicas: int, seqs: int, q_len: int, kv_len: int, heads: int, kv_heads: int, head_dim: int) -> int:
+    return _size_of("hdet_attention_workspace", n_replicas, seqs, q_len, kv_len, heads, kv_heads, head_dim)
+
+
+def hdet_attention(q, k, v, out, heads: int, kv_heads: int, seqs: int = 1, lse=None, causal: bool = True, window: int = 0, scale: Optional[float] = None,
+                   softcap: float = 0.0, slopes=None, positions=None, first=None, end=None, workspace=None, stream: Optional[int] = None):
+    """out [N, seqs * q_len, heads * d] <- softmax(scores) v for q of that shape and k, v [N, seqs * kv_len, kv_heads * d]; lse [N, heads, seqs * q_len].  scale: None for
+    1 / sqrt(d); slopes [N, heads]; positions, first, end: int32 [N, seqs * q_len], keys first .. end - 1 of a sequence are attended (with causal and window, those of them)."""
+    lib = _lib or load_library()
+    sizes, qs, ks, scalars = _attention_sizes(q, k, heads, kv_heads, seqs, causal, window, scale, softcap)
+    dt = q.dtype
+    a = hdet_attention_args(*sizes, _rows_of("q", q, qs, dt), _rows_of("k", k, ks, dt), _rows_of("v", v, ks, dt), _rows_of("out", out, qs, dt),
+                            _scalars("lse", lse, (qs[0], heads, qs[1])), *_vector("slopes", slopes, (qs[0], heads)), _scalars("positions", positions, scalars, _I32),
+                            _scalars("first", first, scalars, _I32), _scalars("end", end, scalars, _I32), *_work_of(workspace))
+    rc = lib.hdet_attention(C.byref(a), stream)
+    if rc:
+        _check(rc)
+
+
+def hdet_attention_backward_workspace(n_replicas: int, seqs: int, q_len: int, kv_len: int, heads: int, kv_heads: int, head_dim: int) -> int:
+    return _size_of("hdet_attention_backward_workspace", n_replicas, seqs, q_len, kv_len, heads, kv_heads, head_dim)
+
+
+def hdet_attention_backward(q, k, v, out, lse, dout, dq, dk, dv, heads: int, kv_heads: int, seqs: int = 1, causal: bool = True, window: int = 0,
+                            scale: Optional[float] = None, softcap: float = 0.0, slopes=None, positions=None, first=None, end=None, workspace=None,
+                            stream: Optional[int] = None):
+    """dq, dk, dv <- gradients at q, k, v from dout, the one at out; out and lse as hdet_attention left them, the other arguments as it had them."""
+    lib = _lib or load_library()
+    sizes, qs, ks, scalars = _attention_sizes(q, k, heads, kv_heads, seqs, causal, window, scale, softcap)
+    dt = q.dtype
+    a = hdet_attention_grad_args(*sizes, _rows_of("q", q, qs, dt), _rows_of("k", k, ks, dt), _rows_of("v", v, ks, dt), _rows_of("out", out, qs, dt),
+                                 _rows_of("dout", dout, qs, dt), _rows_of("dq", dq, qs, dt), _rows_of("dk", dk, ks, dt), _rows_of("dv", dv, ks, dt),
+                                 _scalars("lse", lse, (qs[0], heads, qs[1])), *_vector("slopes", slopes, (qs[0], heads)),
+                                 _scalars("positions", positions, scalars, _I32), _scalars("first", first, scalars, _I32), _scalars("end", end, scalars, _I32),
+                                 *_work_of(workspace))
+    rc = lib.hdet_attention_backward(C.byref(a), stream)
+    if rc:
+        _check(rc)
+
+
+class hdet_gradient_list:
+    """Where the gradients of a model's tensors lie and, with `outs`, where they go: `grads` are [N, rows, columns] or [N, columns], float32 or bfloat16, `outs`
+    float32 of the same shapes (views of the plane that hdet_fanout_step reads).  Made once; holds the tensors."""
+
+    def __init__(self, grads, outs=None):
+        load_library()
+        if outs is not None and len(outs) != len(grads):
+            raise ValueError(f"{len(grads)} gradients and {len(outs)} outputs")
+        self.tensors = (list(grads), None if outs is None else list(outs))
+        self.n_replicas = grads[0].shape[0] if len(grads) else 0
+        self.items = (hdet_grad_tensor * max(len(grads), 1))()
+        for i, g in enumerate(grads):
+            name = f"grads[{i}]"
+            if g.dim() not in (2, 3):
+                raise ValueError(f"{name} has shape {tuple(g.shape)}: [N, rows, columns] or [N, columns] is wanted")
+            o = None if outs is None else outs[i]
+            shape = (self.n_replicas, *g.shape[1:])
+            if g.dim() == 2:
+                g = g[:, None] if tuple(g.shape) == shape else g
+                if o is not None and tuple(o.shape) == shape:
+                    o = o[:, None]
+                shape = (shape[0], 1, shape[1])
+            dtype = _dtype_code(name, g)
+            self.items[i] = hdet_grad_tensor(_rows_of(name, g, shape, g.dtype), _ABSENT if o is None else _rows_of(f"outs[{i}]", o, shape, _F32), shape[1], shape[2], dtype)
+
+    def __len__(self):
+        return len(self.tensors[0])
+
+
+def hdet_clip_gradients_workspace(n_replicas: int, n_tensors: int) -> int:
+    return _size_of("hdet_clip_gradients_workspace", n_replicas, n_tensors)
+
+
+def hdet_clip_gradients(tensors: hdet_gradient_list, norm, max_norm: float, shared: bool = False, workspace=None, stream: Optional[int] = None):
+    """norm [N] <- the norm of each replica's gradient over all tensors (`shared`: of the replicas' mean); the outputs (the gradients themselves where there are none)
+    <- the gradients times min(1, max_norm / norm)."""
+    lib = _lib or load_library()
+    n = norm.shape[0]
+    if len(tensors) and n != tensors.n_replicas:
+        raise ValueError(f"norm has shape {tuple(norm.shape)}, {(tensors.n_replicas,)} is wanted")
+    a = hdet_clip_args(n, len(tensors), tensors.items, HDET_GRAD_SHARED if shared else HDET_GRAD_PER_REPLICA, 0, max_norm, _scalars("norm", norm, (n,)),
+                       *_work_of(workspace))
+    rc = lib.hdet_clip_gradients(C.byref(a), stream)
     if rc:
         _check(rc)

@@ -46,3 +46,18 @@ hipError_t hdet_launch_zero_rows(const hdet_rows& m, int n_replicas, int64_t row
 int hdet_vocab_kind(const hdet_vocab_args& a);                                       // HDET_TYPE_* of dw, HDET_VOCAB_* without one
 size_t hdet_vocab_bytes(int n_replicas, int64_t rows, int width, int classes, int kind, int piece);
 hipError_t hdet_launch_vocab_loss(const hdet_vocab_args& a, hipStream_t s);
+
+// hdet_rotary.hip
+hipError_t hdet_launch_rotary(const hdet_rotary_args& a, hipStream_t s);
+hipError_t hdet_launch_rotary_backward(const hdet_rotary_grad_args& a, hipStream_t s);
+size_t hdet_rotary_backward_bytes(int n_replicas, int64_t rows, int head_dim, int q_heads, int k_heads);
+
+// hdet_attend.hip
+hipError_t hdet_launch_attend(const hdet_attention_args& a, hipStream_t s);
+hipError_t hdet_launch_attend_backward(const hdet_attention_grad_args& a, hipStream_t s);
+size_t hdet_attend_bytes(int n_replicas, int seqs, int q_len, int kv_len, int heads, int kv_heads, int head_dim);
+size_t hdet_attend_backward_bytes(int n_replicas, int seqs, int q_len, int kv_len, int heads, int kv_heads, int head_dim);
+
+// hdet_clip.hip
+hipError_t hdet_launch_clip(const hdet_clip_args& a, hipStream_t s);
+size_t hdet_clip_bytes(int n_replicas, int n_tensors);

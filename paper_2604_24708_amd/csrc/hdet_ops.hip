@@ -3,11 +3,16 @@
 #include "hdet_ops.h"
 
 #include <limits.h>
+#include <math.h>
+
+#include <algorithm>
 
 namespace {
 
 // rows a replica: what the launches' grids and 32-bit row numbers hold
 constexpr int64_t kMaxRows = (int64_t)1 << 21;
+constexpr int64_t kMaxKeys = (int64_t)1 << 28;             // keys a replica: 32-bit key numbers with room to add a tile
+constexpr int64_t kMaxHeadColumns = (int64_t)1 << 20;      // columns of all heads of a row
 
 struct argument_checks {
   std::string why;
@@ -113,6 +118,61 @@ void vocab_sizes(argument_checks& c, int n, int64_t rows, int width, int classes
   c.need(width >= 1 && width <= HDET_MAX_CODES_WIDTH, "width must be in 1 .. HDET_MAX_CODES_WIDTH");
   c.need(classes >= 1 && classes <= kMaxRows, "classes must be in 1 .. 2^21");
   c.need(piece >= 0, "piece must be 0 or a number of classes");
+}
+
+// Sizes that both passes of the rotation check
+template <typename A> void rotary_sizes(argument_checks& c, const A& a) {
+  c.common(a.n_replicas, a.rows);
+  c.type(a.dtype, "dtype must be HDET_TYPE_F32 or HDET_TYPE_BF16");
+  c.need(a.head_dim >= 1 && a.head_dim <= HDET_MAX_ROTARY_DIM, "head_dim must be in 1 .. HDET_MAX_ROTARY_DIM");
+  if (!c.ok()) return;
+  c.need(a.q_heads >= 1 && (int64_t)a.q_heads * a.head_dim <= kMaxHeadColumns, "q_heads must be 1 or more, q_heads * head_dim up to 2^20");
+  c.need(!a.k.dev || (a.k_heads >= 1 && (int64_t)a.k_heads * a.head_dim <= kMaxHeadColumns), "k_heads must be 1 or more, k_heads * head_dim up to 2^20");
+  c.need(a.rotated >= 0 && a.rotated <= a.head_dim && a.rotated % 2 == 0, "rotated must be even and in 0 .. head_dim");
+  c.need(a.layout == HDET_ROTARY_HALVES || a.layout == HDET_ROTARY_PAIRS, "layout must be HDET_ROTARY_HALVES or HDET_ROTARY_PAIRS");
+  c.need(a.period >= 0, "period must be 0 or a number of rows");
+  c.need(a.eps >= 0.0 && a.eps < 1e30, "eps must be a number from 0 on");
+  c.need(a.magnitude > -1e30 && a.magnitude < 1e30, "magnitude must be finite");
+  c.need(a.rotated == 0 || a.rows == 0 || a.freq_dev, "freq_dev is required");
+  c.need(reinterpret_cast<uintptr_t>(a.freq_dev) % 8 == 0, "freq_dev is not aligned to its elements");
+  c.need(reinterpret_cast<uintptr_t>(a.positions_dev) % 4 == 0, "positions_dev is not aligned to its elements");
+  if (!c.ok()) return;
+  c.vector("q_gain_dev", a.q_gain_dev, a.n_replicas, a.head_dim, a.q_gain_stride, false, false);
+  if (a.k.dev) c.vector("k_gain_dev", a.k_gain_dev, a.n_replicas, a.head_dim, a.k_gain_stride, false, false);
+}
+
+void attention_sizes(argument_checks& c, int n, int seqs, int q_len, int kv_len, int heads, int kv_heads, int head_dim) {
+  c.need(seqs >= 0 && q_len >= 0 && kv_len >= 0, "seqs, q_len and kv_len must be 0 or more");
+  if (!c.ok()) return;
+  c.need(n >= 1 && n <= HDET_MAX_REPLICAS, "n_replicas out of range");
+  c.need((int64_t)seqs * q_len <= kMaxRows, "seqs * q_len must be in 0 .. 2^21 per replica");
+  c.need(kv_len <= kMaxKeys && (int64_t)seqs * kv_len <= kMaxKeys, "seqs * kv_len must be in 0 .. 2^28 per replica");
+  c.need(head_dim >= 1 && head_dim <= HDET_MAX_ATTENTION_DIM, "head_dim must be in 1 .. HDET_MAX_ATTENTION_DIM");
+  c.need(kv_heads >= 1 && heads >= 1 && heads % (kv_heads < 1 ? 1 : kv_heads) == 0, "heads must be a multiple of kv_heads");
+  c.need((int64_t)heads * head_dim <= kMaxHeadColumns, "heads * head_dim must be up to 2^20");
+}
+// What both passes of attention check
+template <typename A> void attention_arguments(argument_checks& c, const A& a) {
+  attention_sizes(c, a.n_replicas, a.seqs, a.q_len, a.kv_len, a.heads, a.kv_heads, a.head_dim);
+  c.type(a.dtype, "dtype must be HDET_TYPE_F32 or HDET_TYPE_BF16");
+  c.need(a.window >= 0, "window must be 0 or a number of keys");
+  c.need(a.scale > -1e30 && a.scale < 1e30, "scale must be finite");
+  c.need(a.softcap >= 0.0 && a.softcap < 1e30 && (a.softcap == 0.0 || a.softcap > 1e-30), "softcap must be 0 or a number above it");
+  if (!c.ok()) return;
+  const int n = a.n_replicas, size = element(a.dtype);
+  const int64_t rows = (int64_t)a.seqs * a.q_len, keys = (int64_t)a.seqs * a.kv_len, wide = (int64_t)a.heads * a.head_dim, narrow = (int64_t)a.kv_heads * a.head_dim;
+  c.matrix("q", a.q, n, rows, wide, size, keys > 0, false);
+  c.matrix("k", a.k, n, keys, narrow, size, rows > 0, false);
+  c.matrix("v", a.v, n, keys, narrow, size, rows > 0, false);
+  c.vector("slopes_dev", a.slopes_dev, n, a.heads, a.slopes_stride, false, false);
+  c.vector("positions_dev", a.positions_dev, n, rows, rows, false, false);
+  c.vector("first_dev", a.first_dev, n, rows, rows, false, false);
+  c.vector("end_dev", a.end_dev, n, rows, rows, false, false);
+}
+
+void clip_sizes(argument_checks& c, int n, int tensors) {
+  c.need(n >= 1 && n <= HDET_MAX_REPLICAS, "n_replicas out of range");
+  c.need(tensors >= 0 && tensors <= HDET_MAX_GRAD_TENSORS, "n_tensors must be in 0 .. HDET_MAX_GRAD_TENSORS");
 }
 
 }  // namespace
@@ -309,4 +369,164 @@ extern "C" int hdet_vocab_loss(const hdet_vocab_args* a, void* stream) {
     c.vector("db_dev", a->db_dev, n, a->classes, a->db_stride, false, true);
     if (c.ok()) c.workspace(a->workspace_dev, a->workspace_bytes, hdet_vocab_bytes(n, a->rows, a->width, a->classes, hdet_vocab_kind(*a), a->piece));
   }, [&] { return hdet_launch_vocab_loss(*a, (hipStream_t)stream); });
+}
+
+extern "C" int hdet_head_rotary(const hdet_rotary_args* a, void* stream) {
+  return entry("hdet_head_rotary", [&](argument_checks& c) {
+    c.need(a != nullptr, "args is null");
+    if (!c.ok()) return;
+    rotary_sizes(c, *a);
+    if (!c.ok()) return;
+    const int n = a->n_replicas, size = element(a->dtype);
+    c.matrix("q", a->q, n, a->rows, (int64_t)a->q_heads * a->head_dim, size, true, false);
+    c.matrix("q_out", a->q_out, n, a->rows, (int64_t)a->q_heads * a->head_dim, size, true, true);
+    if (!a->k.dev) return;
+    c.matrix("k", a->k, n, a->rows, (int64_t)a->k_heads * a->head_dim, size, true, false);
+    c.matrix("k_out", a->k_out, n, a->rows, (int64_t)a->k_heads * a->head_dim, size, true, true);
+  }, [&] { return hdet_launch_rotary(*a, (hipStream_t)stream); });
+}
+
+extern "C" int hdet_head_rotary_backward_workspace(int32_t n_replicas, int64_t rows, int32_t head_dim, int32_t q_heads, int32_t k_heads, size_t* bytes) {
+  return entry("hdet_head_rotary_backward_workspace", [&](argument_checks& c) {
+    c.common(n_replicas, rows);
+    c.need(head_dim >= 1 && head_dim <= HDET_MAX_ROTARY_DIM, "head_dim must be in 1 .. HDET_MAX_ROTARY_DIM");
+    c.need(q_heads >= 1 && k_heads >= 0 && (int64_t)q_heads * head_dim <= kMaxHeadColumns && (int64_t)k_heads * head_dim <= kMaxHeadColumns,
+           "q_heads must be 1 or more, k_heads 0 or more, heads * head_dim up to 2^20");
+    c.need(bytes != nullptr, "bytes is null");
+  }, [&] { *bytes = hdet_rotary_backward_bytes(n_replicas, rows, head_dim, q_heads, k_heads); return hipSuccess; });
+}
+
+extern "C" int hdet_head_rotary_backward(const hdet_rotary_grad_args* a, void* stream) {
+  return entry("hdet_head_rotary_backward", [&](argument_checks& c) {
+    c.need(a != nullptr, "args is null");
+    if (!c.ok()) return;
+    rotary_sizes(c, *a);
+    if (!c.ok()) return;
+    const int n = a->n_replicas, size = element(a->dtype);
+    const int64_t wide = (int64_t)a->q_heads * a->head_dim, narrow = (int64_t)a->k_heads * a->head_dim;
+    const bool keys = a->dk_out.dev != nullptr;
+    c.need(keys || !a->k.dev, "dk_out is required with k");
+    c.need(!keys || (a->k_heads >= 1 && narrow <= kMaxHeadColumns), "k_heads must be 1 or more, k_heads * head_dim up to 2^20");
+    c.matrix("q", a->q, n, a->rows, wide, size, a->q_gain_dev != nullptr, false);
+    c.matrix("dq_out", a->dq_out, n, a->rows, wide, size, true, false);
+    c.matrix("dq", a->dq, n, a->rows, wide, size, true, true);
+    c.need(a->q_gain_dev || !a->dq_gain_dev, "dq_gain_dev needs q_gain_dev");
+    c.vector("dq_gain_dev", a->dq_gain_dev, n, a->head_dim, a->dq_gain_stride, false, true);
+    if (keys) {
+      c.matrix("k", a->k, n, a->rows, narrow, size, a->k_gain_dev != nullptr, false);
+      c.matrix("dk_out", a->dk_out, n, a->rows, narrow, size, true, false);
+      c.matrix("dk", a->dk, n, a->rows, narrow, size, true, true);
+      c.vector("k_gain_dev", a->k_gain_dev, n, a->head_dim, a->k_gain_stride, false, false);
+    }
+    c.need(!a->dk_gain_dev || (keys && a->k_gain_dev), "dk_gain_dev needs dk_out and k_gain_dev");
+    c.vector("dk_gain_dev", a->dk_gain_dev, n, a->head_dim, a->dk_gain_stride, false, true);
+    if (c.ok() && (a->dq_gain_dev || a->dk_gain_dev))
+      c.workspace(a->workspace_dev, a->workspace_bytes, hdet_rotary_backward_bytes(n, a->rows, a->head_dim, a->q_heads, keys ? a->k_heads : 0));
+  }, [&] { return hdet_launch_rotary_backward(*a, (hipStream_t)stream); });
+}
+
+extern "C" int hdet_rotary_frequencies(int32_t rotated, double base, int32_t stretch, double factor, double context, double slow, double fast, double* freq_host) {
+  return entry("hdet_rotary_frequencies", [&](argument_checks& c) {
+    c.need(rotated >= 0 && rotated <= HDET_MAX_ROTARY_DIM && rotated % 2 == 0, "rotated must be even and in 0 .. HDET_MAX_ROTARY_DIM");
+    c.need(base > 0.0 && base < 1e30, "base must be a number above 0");
+    c.need(stretch >= HDET_STRETCH_POSITIONS && stretch <= HDET_STRETCH_PARTS, "stretch must be one of HDET_STRETCH_*");
+    c.need(factor > 0.0 && factor < 1e30, "factor must be a number above 0");
+    c.need(stretch != HDET_STRETCH_BASE || rotated != 2 || factor == 1.0, "HDET_STRETCH_BASE needs more than one pair");
+    c.need(stretch != HDET_STRETCH_PARTS || (context > 0.0 && context < 1e30 && slow > 0.0 && slow < fast && fast < 1e30),
+           "HDET_STRETCH_PARTS needs a context above 0 and 0 < slow < fast");
+    c.need(freq_host != nullptr || rotated == 0, "freq_host is null");
+  }, [&] {
+    if (stretch == HDET_STRETCH_BASE && rotated > 2) base *= pow(factor, (double)rotated / (rotated - 2));
+    for (int t = 0; t < rotated / 2; ++t) {
+      const double f = pow(base, -2.0 * t / rotated);
+      double keep = stretch == HDET_STRETCH_BASE ? 1.0 : 0.0;      // the part of the unstretched frequency
+      if (stretch == HDET_STRETCH_PARTS) keep = std::min(1.0, std::max(0.0, (context * f / (2.0 * M_PI) - slow) / (fast - slow)));
+      freq_host[t] = f * (keep + (1.0 - keep) / factor);
+    }
+    return hipSuccess;
+  });
+}
+
+extern "C" int hdet_attention_workspace(int32_t n_replicas, int32_t seqs, int32_t q_len, int32_t kv_len, int32_t heads, int32_t kv_heads, int32_t head_dim, size_t* bytes) {
+  return entry("hdet_attention_workspace", [&](argument_checks& c) {
+    attention_sizes(c, n_replicas, seqs, q_len, kv_len, heads, kv_heads, head_dim);
+    c.need(bytes != nullptr, "bytes is null");
+  }, [&] { *bytes = hdet_attend_bytes(n_replicas, seqs, q_len, kv_len, heads, kv_heads, head_dim); return hipSuccess; });
+}
+
+extern "C" int hdet_attention(const hdet_attention_args* a, void* stream) {
+  return entry("hdet_attention", [&](argument_checks& c) {
+    c.need(a != nullptr, "args is null");
+    if (!c.ok()) return;
+    attention_arguments(c, *a);
+    if (!c.ok()) return;
+    const int n = a->n_replicas;
+    const int64_t rows = (int64_t)a->seqs * a->q_len;
+    c.matrix("out", a->out, n, rows, (int64_t)a->heads * a->head_dim, element(a->dtype), true, true);
+    c.vector("lse_dev", a->lse_dev, n, rows * a->heads, rows * a->heads, false, true);
+    c.workspace(a->workspace_dev, a->workspace_bytes, hdet_attend_bytes(n, a->seqs, a->q_len, a->kv_len, a->heads, a->kv_heads, a->head_dim));
+  }, [&] { return hdet_launch_attend(*a, (hipStream_t)stream); });
+}
+
+extern "C" int hdet_attention_backward_workspace(int32_t n_replicas, int32_t seqs, int32_t q_len, int32_t kv_len, int32_t heads, int32_t kv_heads, int32_t head_dim,
+                                                 size_t* bytes) {
+  return entry("hdet_attention_backward_workspace", [&](argument_checks& c) {
+    attention_sizes(c, n_replicas, seqs, q_len, kv_len, heads, kv_heads, head_dim);
+    c.need(bytes != nullptr, "bytes is null");
+  }, [&] { *bytes = hdet_attend_backward_bytes(n_replicas, seqs, q_len, kv_len, heads, kv_heads, head_dim); return hipSuccess; });
+}
+
+extern "C" int hdet_attention_backward(const hdet_attention_grad_args* a, void* stream) {
+  return entry("hdet_attention_backward", [&](argument_checks& c) {
+    c.need(a != nullptr, "args is null");
+    if (!c.ok()) return;
+    attention_arguments(c, *a);
+    if (!c.ok()) return;
+    const int n = a->n_replicas, size = element(a->dtype);
+    const int64_t rows = (int64_t)a->seqs * a->q_len, keys = (int64_t)a->seqs * a->kv_len, wide = (int64_t)a->heads * a->head_dim, narrow = (int64_t)a->kv_heads * a->head_dim;
+    c.matrix("out", a->out, n, rows, wide, size, keys > 0, false);
+    c.matrix("dout", a->dout, n, rows, wide, size, keys > 0, false);
+    c.vector("lse_dev", a->lse_dev, n, rows * a->heads, rows * a->heads, keys > 0, false);
+    c.matrix("dq", a->dq, n, rows, wide, size, true, true);
+    c.matrix("dk", a->dk, n, keys, narrow, size, true, true);
+    c.matrix("dv", a->dv, n, keys, narrow, size, true, true);
+    c.workspace(a->workspace_dev, a->workspace_bytes, hdet_attend_backward_bytes(n, a->seqs, a->q_len, a->kv_len, a->heads, a->kv_heads, a->head_dim));
+  }, [&] { return hdet_launch_attend_backward(*a, (hipStream_t)stream); });
+}
+
+extern "C" int hdet_clip_gradients_workspace(int32_t n_replicas, int32_t n_tensors, size_t* bytes) {
+  return entry("hdet_clip_gradients_workspace", [&](argument_checks& c) {
+    clip_sizes(c, n_replicas, n_tensors);
+    c.need(bytes != nullptr, "bytes is null");
+  }, [&] { *bytes = hdet_clip_bytes(n_replicas, n_tensors); return hipSuccess; });
+}
+
+extern "C" int hdet_clip_gradients(const hdet_clip_args* a, void* stream) {
+  return entry("hdet_clip_gradients", [&](argument_checks& c) {
+    c.need(a != nullptr, "args is null");
+    if (!c.ok()) return;
+    clip_sizes(c, a->n_replicas, a->n_tensors);
+    c.need(a->n_tensors == 0 || a->tensors_host, "tensors_host is null");
+    c.need(a->grad_mode == HDET_GRAD_PER_REPLICA || a->grad_mode == HDET_GRAD_SHARED, "grad_mode must be HDET_GRAD_PER_REPLICA or HDET_GRAD_SHARED");
+    c.need(a->max_norm >= 0.0, "max_norm must be a number from 0 on, or infinity");
+    if (!c.ok()) return;
+    const int n = a->n_replicas;
+    c.vector("norm_dev", a->norm_dev, n, 1, 1, true, true);
+    std::vector<const void*> starts;
+    for (int i = 0; i < a->n_tensors && c.ok(); ++i) {
+      const hdet_grad_tensor& t = a->tensors_host[i];
+      c.type(t.dtype, "dtype of a tensor must be HDET_TYPE_F32 or HDET_TYPE_BF16");
+      c.need(t.rows >= 0 && t.width >= 0 && (t.width == 0 || t.rows <= ((int64_t)1 << 40) / t.width), "rows * width of a tensor must be in 0 .. 2^40");
+      if (!c.ok() || t.rows == 0 || t.width == 0) continue;
+      const bool in_place = !t.out.dev;
+      c.matrix("grad", t.grad, n, t.rows, t.width, element(t.dtype), true, in_place && a->max_norm < INFINITY);
+      c.matrix("out", t.out, n, t.rows, t.width, 4, false, true);
+      if (!in_place) starts.push_back(t.out.dev);
+      else if (a->max_norm < INFINITY) starts.push_back(t.grad.dev);
+    }
+    if (!c.ok()) return;
+    std::sort(starts.begin(), starts.end());
+    c.need(std::adjacent_find(starts.begin(), starts.end()) == starts.end(), "two tensors are written at the same place");
+    c.workspace(a->workspace_dev, a->workspace_bytes, hdet_clip_bytes(n, a->n_tensors));
+  }, [&] { return hdet_launch_clip(*a, (hipStream_t)stream); });
 }

@@ -3,152 +3,693 @@
 //   z_ij = scale q_i . k_j, capped: cap tanh(z / cap), minus slope_h |pos_i - j|;  p_i = softmax over first_i <= j < end_i;  o_i = sum p_ij v_j
 //   dv_j = sum_i p_ij do_i;  dz = p (do_i . v_j - do_i . o_i) (1 - tanh^2);  dq_i = scale sum_j dz k_j;  dk_j = scale sum_i dz q_i
 //
-// A wavefront to a query (forward, dq) or to a key (dk, dv), its lanes over the head's columns, one pass with the running maximum and sum.
+// Every mask is a range of keys a query, so that a block of queries walks over the union of its ranges, tile by tile, and a 32 x 32 block of scores is
+// outside, inside or across the ranges of its queries: only the last kind tests its pairs.
+// In units of log2 throughout: p = 2^(z log2 e - m), one fma and one exponential a score.
+//
+// A pair that is not attended must leave no trace, but 0 times an infinity or a NaN does: the matrix cores multiply all of a block that lies across the
+// ranges.  Results that came out finite are right; where one did not, the block walks its tiles a second time and leaves out the pairs of such blocks one
+// by one (second_exact).  That costs nothing where numbers are finite, and at most the same time again and a few thousand cycles a block across.
 
+#include <limits.h>
 #include <math.h>
 
+#include <type_traits>
+
 #include "hdet_ops.h"
-#include "hdet_elem.h"
+#include "hdet_attend_tiles.h"
+
+using namespace hdet_attend;
 
 namespace {
 
 constexpr int THREADS = 256;
-constexpr int WAVES = THREADS / 64;
+constexpr int NWV = THREADS / 64;
+constexpr int WR = 32;                     // rows a wavefront owns
+constexpr int RB = WR * NWV;               // rows a block owns
 
 struct attend_args {
   const void *q, *k, *v, *o, *dout;
   void *out, *dq, *dk, *dv;
   int64_t q_s, q_z, k_s, k_z, v_s, v_z, o_s, o_z, do_s, do_z, out_s, out_z, dq_s, dq_z, dk_s, dk_z, dv_s, dv_z;
-  float* lse;
-  const float* lse_in;
-  float* dot;                              // backward: [replica][head][row] sum_c do o
+  float* lse;                              // forward
+  const float* lse_in;                     // backward
+  float *lse2, *dot;                       // backward: [replica][head][row] lse log2 e (infinity for empty rows), minus sum_c do o
+  int *lo, *hi, *pos_of;                   // backward: [replica][row] the rows' ranges and positions
+  i4v* groups;                             // backward: [replica][sequence][32 queries] least and largest lo, least and largest hi
+  float* part;                             // few queries: results of the splits
   const float* slopes;
   int64_t slopes_z;
   const int32_t *pos, *first, *end;
-  int n, seqs, q_len, kv_len, heads, kv_heads, d, causal, window;
-  float scale, cap, inv_cap;
+  int n, seqs, q_len, kv_len, heads, kv_heads, group, d, causal, window;
+  int splits;
+  float scale, c, cap2, inv_cap;           // c = scale log2 e; cap2 = cap log2 e or 0
+  unsigned total;                          // blocks
+  bool heavy_first;
 };
 
-struct key_range { int lo, hi; int64_t pos; };
+struct key_range { int lo, hi, pos; };
 
-// Keys that query i of sequence b attends: lo .. hi - 1
+// Keys that query i of sequence b attends: lo .. hi - 1, 0 .. -1 for none
 __device__ __forceinline__ key_range range_of(const attend_args& g, int r, int b, int i) {
-  const int64_t row = (int64_t)b * g.q_len + i, at = (int64_t)r * g.seqs * g.q_len + row;
-  const int64_t pos = g.pos ? g.pos[at] : (int64_t)i + g.kv_len - g.q_len;
-  int64_t lo = 0, hi = g.kv_len;
+  const int64_t at = ((int64_t)r * g.seqs + b) * g.q_len + i;
+  const int pos = g.pos ? g.pos[at] : i + g.kv_len - g.q_len;
+  int lo = 0, hi = g.kv_len;
   if (g.first && g.first[at] > lo) lo = g.first[at];
-  if (g.window && pos - g.window + 1 > lo) lo = pos - g.window + 1;
+  if (g.window) {
+    const int64_t from = (int64_t)pos - g.window + 1;
+    if (from > lo) lo = from > g.kv_len ? g.kv_len : (int)from;
+  }
   if (g.end && g.end[at] < hi) hi = g.end[at];
-  if (g.causal && pos + 1 < hi) hi = pos + 1;
+  if (g.causal && pos < hi) hi = pos < 0 ? 0 : pos + 1 < hi ? pos + 1 : hi;
   if (hi <= lo) lo = hi = 0;
-  return {(int)lo, (int)hi, pos};
+  return {lo, hi, pos};
 }
 
-// the score of a pair from q . k; `slope` receives the derivative of the cap
-__device__ __forceinline__ float score(const attend_args& g, float qk, float slope, int64_t distance, float& bend) {
-  float z = qk * g.scale;
-  bend = 1.f;
-  if (g.cap > 0.f) {
-    const float t = tanhf(z * g.inv_cap);
-    z = g.cap * t;
-    bend = 1.f - t * t;
+// Block number -> row block x (of nx, the one with most work first) and (replica, sequence, head) grp.  Blocks reach the chip's 8 XCDs round-robin in
+// launch order: every XCD works through a contiguous range of grp, so that the tiles which blocks share are in one L2; heavy_first: the longest row
+// blocks of all grp first, then the next ones (few rounds of blocks: the last one's length counts more).
+struct block_id { unsigned x, grp; };
+__device__ __forceinline__ block_id place_block(unsigned lin, unsigned total, unsigned nx, bool heavy_first) {
+  const unsigned groups = total / nx;
+  block_id b;
+  if (heavy_first) {
+    if ((groups & 7u) == 0u) {
+      const unsigned own = groups >> 3, j = lin >> 3;
+      b.x = j / own;
+      b.grp = (lin & 7u) * own + j % own;
+    } else {
+      b.x = lin / groups;
+      b.grp = lin % groups;
+    }
+  } else {
+    if ((total & 7u) == 0u) lin = (lin & 7u) * (total >> 3) + (lin >> 3);
+    b.grp = lin / nx;
+    b.x = (lin % nx + b.grp + (b.grp >> 3) + (b.grp >> 6)) % nx;
   }
-  return __builtin_fmaf(-slope, (float)(distance < 0 ? -distance : distance), z);
+  return b;
 }
 
-template <typename T> struct lane_columns {            // columns lane and lane + 64 of a head
-  float a, b;
-  __device__ __forceinline__ lane_columns(const T* p, int lane, int d) : a(lane < d ? hdet_ld(p + lane) : 0.f), b(lane + 64 < d ? hdet_ld(p + lane + 64) : 0.f) {}
-  __device__ __forceinline__ float dot(const lane_columns& o) const { return hdet_wave_sum(__builtin_fmaf(a, o.a, b * o.b)); }
+// Least and largest over the 32 rows of a wavefront
+__device__ __forceinline__ int wave_min(int x) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x = min(x, __shfl_xor(x, o));
+  return __builtin_amdgcn_readfirstlane(x);
+}
+__device__ __forceinline__ int wave_max(int x) {
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) x = max(x, __shfl_xor(x, o));
+  return __builtin_amdgcn_readfirstlane(x);
+}
+// The ranges of 32 queries: any keys outside lo_min .. hi_max - 1 are outside for all, keys of lo_max .. hi_min - 1 inside for all
+struct wave_range { int lo_min, lo_max, hi_min, hi_max; };
+// `there`: the lane's row exists
+__device__ __forceinline__ wave_range wave_range_of(const key_range& k, bool there) {
+  const bool some = there && k.hi > k.lo;
+  wave_range w;
+  w.lo_min = wave_min(some ? k.lo : INT_MAX);
+  w.hi_max = wave_max(some ? k.hi : 0);
+  w.lo_max = wave_max(some ? k.lo : there ? INT_MAX : 0);
+  w.hi_min = wave_min(some ? k.hi : there ? 0 : INT_MAX);
+  return w;
+}
+
+// Scores of a block from its raw products, [key or query][..], in units of log2; bend: the cap's derivative.  dist(e): |position - key| of element e.
+template <bool BEND, typename F>
+__device__ __forceinline__ void shape_scores(const attend_args& g, f16v& x, f16v& bend, float slope2, F dist) {
+  if (g.cap2 > 0.f) {
+    const float s = g.scale * g.inv_cap;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float t = tanh_fast(x[e] * s);
+      x[e] = t * g.cap2;
+      if (BEND) bend[e] = __builtin_fmaf(-t, t, 1.f);
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] *= g.c;
+    if (BEND) bend = all16(1.f);
+  }
+  if (slope2 != 0.f) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = __builtin_fmaf(-slope2, dist(e), x[e]);
+  }
+}
+__device__ __forceinline__ float distance(int pos, int key) { return (float)(pos < key ? (unsigned)key - (unsigned)pos : (unsigned)pos - (unsigned)key); }
+
+// Row statistics and results of a wavefront's 32 queries (columns of the accumulators) on its way over the keys
+template <int D> struct running {
+  f16v o[D / 32];
+  float m, l;                              // reference of the exponentials (log2), this half-wavefront's sum
+  __device__ __forceinline__ void reset() {
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) o[i] = all16(0.f);
+    m = -INFINITY;
+    l = 0.f;
+  }
+  __device__ __forceinline__ float ref() const { return m == -INFINITY ? 0.f : m; }
+  // Exponentials of NB blocks of scores times c; the reference follows the maximum only when that has risen by more than 2^8 (the sums hold that), so that
+  // results are seldom rescaled
+  template <int NB> __device__ __forceinline__ void take(f16v (&x)[NB], float c) {
+    float top = x[0][0];
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) top = fmaxf(top, x[b][e]);
+    top = fmaxf(top, other_half(top)) * c;
+    if (__any(top > m + 8.f)) {
+      const float next = fmaxf(m, top), keep = exp2_fast(m - (next == -INFINITY ? 0.f : next));
+      m = next;
+      l *= keep;
+#pragma unroll
+      for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+        for (int e = 0; e < 16; ++e) o[i][e] *= keep;
+    }
+    const float r = -ref();
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        x[b][e] = exp2_fast(__builtin_fmaf(x[b][e], c, r));
+        l += x[b][e];
+      }
+  }
 };
-template <typename T> __device__ __forceinline__ void store_columns(T* p, int lane, int d, float a, float b) {
-  if (lane < d) hdet_st(p + lane, a);
-  if (lane + 64 < d) hdet_st(p + lane + 64, b);
-}
 
-__device__ __forceinline__ int64_t wave_index() { return (((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * THREADS + threadIdx.x) >> 6; }
-
-template <typename T> __global__ __launch_bounds__(THREADS) void attend_kernel(const attend_args g) {
-  const int64_t w = wave_index(), rows = (int64_t)g.seqs * g.q_len;
-  if (w >= rows * g.heads * g.n) return;
-  const int lane = threadIdx.x & 63, h = (int)(w % g.heads), kh = h / (g.heads / g.kv_heads);
-  const int64_t row = w / g.heads % rows;
-  const int r = (int)(w / g.heads / rows), b = (int)(row / g.q_len);
-  const key_range range = range_of(g, r, b, (int)(row % g.q_len));
-  const lane_columns<T> q((const T*)g.q + r * g.q_z + row * g.q_s + (int64_t)h * g.d, lane, g.d);
-  const T* k = (const T*)g.k + r * g.k_z + (int64_t)b * g.kv_len * g.k_s + (int64_t)kh * g.d;
-  const T* v = (const T*)g.v + r * g.v_z + (int64_t)b * g.kv_len * g.v_s + (int64_t)kh * g.d;
-  const float slope = g.slopes ? g.slopes[r * g.slopes_z + h] : 0.f;
-  float m = -INFINITY, l = 0.f, oa = 0.f, ob = 0.f, bend;
-  for (int j = range.lo; j < range.hi; ++j) {
-    const float z = score(g, q.dot(lane_columns<T>(k + j * g.k_s, lane, g.d)), slope, range.pos - j, bend);
-    const lane_columns<T> x(v + j * g.v_s, lane, g.d);
-    const float top = fmaxf(m, z), ref = top == -INFINITY ? 0.f : top;
-    const float keep = expf(m - ref), p = expf(z - ref);
-    l = __builtin_fmaf(l, keep, p);
-    oa = __builtin_fmaf(oa, keep, p * x.a);
-    ob = __builtin_fmaf(ob, keep, p * x.b);
-    m = top;
+// ---------------------------------------------------------------------------------------------
+// forward: block = 128 queries of one (replica, sequence, head)
+// ---------------------------------------------------------------------------------------------
+template <typename T, int D> constexpr int forward_waves() { return sizeof(T) == 2 && D == 64 ? 3 : 2; }
+template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds__(THREADS, (forward_waves<T, D>())) void attend_kernel(const attend_args g) {
+  typedef shape<T, D> S;
+  constexpr int TILE = S::TB * D, NB = S::TB / 32;
+  __shared__ __attribute__((aligned(1024))) T smem[4 * TILE];              // two stages of keys and values
+  __shared__ int ends[2 * NWV];
+  const unsigned lin = blockIdx.y * gridDim.x + blockIdx.x;
+  if (lin >= g.total) return;
+  const unsigned nx = (g.q_len + RB - 1) / RB;
+  const block_id blk = place_block(lin, g.total, nx, g.heavy_first);
+  const int h = blk.grp % g.heads, b = blk.grp / g.heads % g.seqs, r = blk.grp / g.heads / g.seqs;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wq0 = (int)(nx - 1 - blk.x) * RB + w * WR, qi = wq0 + (lane & 31);
+  const bool there = qi < g.q_len;
+  const key_range range = there ? range_of(g, r, b, qi) : key_range{0, 0, 0};
+  const wave_range wr = wave_range_of(range, there);
+  if (lane == 0) {
+    ends[w] = wr.lo_min;
+    ends[NWV + w] = wr.hi_max;
   }
-  const float inv = range.hi > range.lo ? 1.f / l : 0.f;
-  store_columns((T*)g.out + r * g.out_z + row * g.out_s + (int64_t)h * g.d, lane, g.d, oa * inv, ob * inv);
-  if (g.lse && lane == 0) g.lse[((int64_t)r * g.heads + h) * rows + row] = range.hi > range.lo ? m + logf(l) : -INFINITY;
-}
+  const int64_t col = (int64_t)h * g.d, kcol = (int64_t)(h / g.group) * g.d, row0 = (int64_t)b * g.q_len + wq0;
+  const T* const own = there ? (const T*)g.q + r * g.q_z + (row0 + (lane & 31)) * g.q_s + col : nullptr;
+  typename S::frag fq[S::NF];
+#pragma unroll
+  for (int i = 0; i < S::NF; ++i) fq[i] = own_frag<T, D, WHOLE>(own, i, g.d, lane);
+  const tile_loader<T, D, S::TB, NWV, WHOLE> keys((const T*)g.k + r * g.k_z + (int64_t)b * g.kv_len * g.k_s + kcol, g.k_s, g.d, w, lane);
+  const tile_loader<T, D, S::TB, NWV, WHOLE> vals((const T*)g.v + r * g.v_z + (int64_t)b * g.kv_len * g.v_s + kcol, g.v_s, g.d, w, lane);
+  const S at(lane);
+  const float slope2 = EXTRA && g.slopes ? g.slopes[r * g.slopes_z + h] * kLog2e : 0.f, c = EXTRA ? 1.f : g.c;
+  __syncthreads();
+  const int lo = __builtin_amdgcn_readfirstlane(min(min(ends[0], ends[1]), min(ends[2], ends[3])));
+  const int hi = __builtin_amdgcn_readfirstlane(max(max(ends[4], ends[5]), max(ends[6], ends[7])));
+  const int t0 = lo / S::TB, t1 = (hi + S::TB - 1) / S::TB;                // hi = 0: none
 
-template <typename T> __global__ __launch_bounds__(THREADS) void attend_dq_kernel(const attend_args g) {
-  const int64_t w = wave_index(), rows = (int64_t)g.seqs * g.q_len;
-  if (w >= rows * g.heads * g.n) return;
-  const int lane = threadIdx.x & 63, h = (int)(w % g.heads), kh = h / (g.heads / g.kv_heads);
-  const int64_t row = w / g.heads % rows;
-  const int r = (int)(w / g.heads / rows), b = (int)(row / g.q_len);
-  const key_range range = range_of(g, r, b, (int)(row % g.q_len));
-  const int64_t col = (int64_t)h * g.d, stat = ((int64_t)r * g.heads + h) * rows + row;
-  T* const dq = (T*)g.dq + r * g.dq_z + row * g.dq_s + col;
-  if (range.hi == range.lo) return store_columns(dq, lane, g.d, 0.f, 0.f);
-  const lane_columns<T> q((const T*)g.q + r * g.q_z + row * g.q_s + col, lane, g.d), o((const T*)g.o + r * g.o_z + row * g.o_s + col, lane, g.d);
-  const lane_columns<T> dout((const T*)g.dout + r * g.do_z + row * g.do_s + col, lane, g.d);
-  const T* k = (const T*)g.k + r * g.k_z + (int64_t)b * g.kv_len * g.k_s + (int64_t)kh * g.d;
-  const T* v = (const T*)g.v + r * g.v_z + (int64_t)b * g.kv_len * g.v_s + (int64_t)kh * g.d;
-  const float slope = g.slopes ? g.slopes[r * g.slopes_z + h] : 0.f, lse = g.lse_in[stat], dot = dout.dot(o);
-  float a = 0.f, c = 0.f, bend;
-  for (int j = range.lo; j < range.hi; ++j) {
-    const lane_columns<T> x(k + j * g.k_s, lane, g.d);
-    const float p = expf(score(g, q.dot(x), slope, range.pos - j, bend) - lse);
-    const float dz = p * (dout.dot(lane_columns<T>(v + j * g.v_s, lane, g.d)) - dot) * bend;
-    a = __builtin_fmaf(dz, x.a, a);
-    c = __builtin_fmaf(dz, x.b, c);
+  running<D> z;
+  auto request = [&](int t) {
+    if (t >= t1) return;
+    T* const to = smem + (t & 1) * (2 * TILE);
+    keys.load((int64_t)t * S::TB, hi - t * S::TB, to);
+    vals.load((int64_t)t * S::TB, hi - t * S::TB, to + TILE);
+  };
+  for (bool exact = false;; exact = true) {
+    z.reset();
+    if (hi > 0) request(t0);
+    for (int t = t0; t < t1; ++t) {
+      wait_and_barrier<0>();
+      request(t + 1);
+      const T* const kt = smem + (t & 1) * (2 * TILE);
+      const T* const vt = kt + TILE;
+      const int key0 = t * S::TB;
+      // one block of 32 keys, its pairs tested
+      auto across = [&](int i) {
+        f16v x[1], bend;
+        x[0] = at.first(kt + i * 32 * D, fq, all16(0.f));
+        const int k0 = key0 + 32 * i + ((lane >> 5) << 2);
+        if (EXTRA) shape_scores<false>(g, x[0], bend, slope2, [&](int e) { return distance(range.pos, k0 + acc_row(e, 0)); });
+        const unsigned from = k0 - range.lo, len = range.hi - range.lo;
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[0][e] = from + acc_row(e, 0) < len ? x[0][e] : -INFINITY;
+        z.take(x, c);
+        if (!exact) at.second(vt + i * 32 * D, x[0], z.o);
+        else second_exact<T, D>(vt + i * 32 * D, x[0], z.o, lane, [&](int row) { return (unsigned)(key0 + 32 * i + row - range.lo) < len; });
+      };
+      if (key0 >= wr.lo_max && key0 + S::TB <= wr.hi_min) {
+        f16v x[NB], bend;
+#pragma unroll
+        for (int i = 0; i < NB; ++i) {
+          x[i] = at.first(kt + i * 32 * D, fq, all16(0.f));
+          const int k0 = key0 + 32 * i + ((lane >> 5) << 2);
+          if (EXTRA) shape_scores<false>(g, x[i], bend, slope2, [&](int e) { return distance(range.pos, k0 + acc_row(e, 0)); });
+        }
+        z.take(x, c);
+#pragma unroll
+        for (int i = 0; i < NB; ++i) at.second(vt + i * 32 * D, x[i], z.o);
+      } else {
+#pragma unroll 1
+        for (int i = 0; i < NB; ++i)
+          if (key0 + 32 * i < wr.hi_max && key0 + 32 * i + 32 > wr.lo_min) across(i);
+      }
+    }
+    z.l += other_half(z.l);
+    const bool again = __syncthreads_or(there && fabsf(z.l) < INFINITY && not_finite(z.o));
+    if (exact || !again) break;
   }
-  store_columns(dq, lane, g.d, a * g.scale, c * g.scale);
-  if (lane == 0) g.dot[stat] = dot;
+  const bool some = range.hi > range.lo;
+  const float inv = some ? 1.f / z.l : 0.f;
+#pragma unroll
+  for (int i = 0; i < S::ND; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) z.o[i][e] = some ? z.o[i][e] * inv : 0.f;
+  if (g.lse && there && lane < 32) g.lse[((int64_t)r * g.heads + h) * g.seqs * g.q_len + row0 + lane] = some ? (z.ref() + log2f(z.l)) * kLn2 : -INFINITY;
+  store_rows<T, D, WHOLE>(z.o, (char*)smem + w * STRIP, (T*)g.out + r * g.out_z + row0 * g.out_s + col, g.out_s, g.q_len - wq0, g.d, lane);
 }
 
-template <typename T> __global__ __launch_bounds__(THREADS) void attend_dkv_kernel(const attend_args g) {
-  const int64_t w = wave_index(), keys = (int64_t)g.seqs * g.kv_len, rows = (int64_t)g.seqs * g.q_len;
-  if (w >= keys * g.kv_heads * g.n) return;
-  const int lane = threadIdx.x & 63, kh = (int)(w % g.kv_heads), group = g.heads / g.kv_heads;
-  const int64_t key = w / g.kv_heads % keys;
-  const int r = (int)(w / g.kv_heads / keys), b = (int)(key / g.kv_len), j = (int)(key % g.kv_len);
-  const lane_columns<T> k((const T*)g.k + r * g.k_z + key * g.k_s + (int64_t)kh * g.d, lane, g.d), v((const T*)g.v + r * g.v_z + key * g.v_s + (int64_t)kh * g.d, lane, g.d);
-  float ka = 0.f, kb = 0.f, va = 0.f, vb = 0.f, bend;
-  for (int h = kh * group; h < (kh + 1) * group; ++h) {
-    const float slope = g.slopes ? g.slopes[r * g.slopes_z + h] : 0.f;
-    for (int i = 0; i < g.q_len; ++i) {
-      const key_range range = range_of(g, r, b, i);
-      if (j < range.lo || j >= range.hi) continue;
-      const int64_t row = (int64_t)b * g.q_len + i, col = (int64_t)h * g.d, stat = ((int64_t)r * g.heads + h) * rows + row;
-      const lane_columns<T> q((const T*)g.q + r * g.q_z + row * g.q_s + col, lane, g.d), dout((const T*)g.dout + r * g.do_z + row * g.do_s + col, lane, g.d);
-      const float p = expf(score(g, q.dot(k), slope, range.pos - j, bend) - g.lse_in[stat]);
-      const float dz = p * (dout.dot(v) - g.dot[stat]) * bend;
-      ka = __builtin_fmaf(dz, q.a, ka);
-      kb = __builtin_fmaf(dz, q.b, kb);
-      va = __builtin_fmaf(p, dout.a, va);
-      vb = __builtin_fmaf(p, dout.b, vb);
+// ---------------------------------------------------------------------------------------------
+// forward, few queries over many keys: a block takes 32 (query, head) pairs that share a key head, as one wavefront's rows, and a part of the keys, of
+// which its wavefronts take every NW-th tile of 32, each through LDS of its own.  Their results are joined in LDS, those of the parts by a second launch.
+// ---------------------------------------------------------------------------------------------
+template <typename T, int D> constexpr int few_waves() { return sizeof(T) == 4 && D == 128 ? 2 : 4; }
+template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds__((few_waves<T, D>() * 64)) void attend_few_kernel(const attend_args g) {
+  typedef shape<T, D> S;
+  constexpr int NW = few_waves<T, D>(), TILE = 32 * D, P = D + 4;
+  __shared__ __attribute__((aligned(1024))) T smem[NW * 4 * TILE];
+  unsigned lin = blockIdx.y * gridDim.x + blockIdx.x;
+  if (lin >= g.total) return;
+  if ((g.total & 7u) == 0u) lin = (lin & 7u) * (g.total >> 3) + (lin >> 3);
+  const int pairs = g.group * g.q_len;
+  const unsigned ncg = (pairs + 31) / 32, cg = lin % ncg, split = lin / ncg % g.splits, grp = lin / ncg / g.splits;
+  const int kh = grp % g.kv_heads, b = grp / g.kv_heads % g.seqs, r = grp / g.kv_heads / g.seqs;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int pair = cg * 32 + (lane & 31);
+  const bool there = pair < pairs;
+  const int h = kh * g.group + (there ? pair / g.q_len : 0), qi = there ? pair % g.q_len : 0;
+  const key_range range = there ? range_of(g, r, b, qi) : key_range{0, 0, 0};
+  const wave_range wr = wave_range_of(range, there);
+  const int64_t row = (int64_t)b * g.q_len + qi, kcol = (int64_t)kh * g.d;
+  const T* const own = there ? (const T*)g.q + r * g.q_z + row * g.q_s + (int64_t)h * g.d : nullptr;
+  typename S::frag fq[S::NF];
+#pragma unroll
+  for (int i = 0; i < S::NF; ++i) fq[i] = own_frag<T, D, WHOLE>(own, i, g.d, lane);
+  const tile_loader<T, D, 32, 1, WHOLE> keys((const T*)g.k + r * g.k_z + (int64_t)b * g.kv_len * g.k_s + kcol, g.k_s, g.d, 0, lane);
+  const tile_loader<T, D, 32, 1, WHOLE> vals((const T*)g.v + r * g.v_z + (int64_t)b * g.kv_len * g.v_s + kcol, g.v_s, g.d, 0, lane);
+  constexpr int IN_FLIGHT = 2 * tile_loader<T, D, 32, 1, WHOLE>::NI;
+  const S at(lane);
+  const float slope2 = EXTRA && g.slopes ? g.slopes[r * g.slopes_z + h] * kLog2e : 0.f, c = EXTRA ? 1.f : g.c;
+  // the union of the ranges in tiles, this block's part of them
+  const int hi = wr.hi_max, lo = hi > 0 ? wr.lo_min : 0, t0 = lo / 32, t1 = (hi + 31) / 32, per = (t1 - t0 + g.splits - 1) / g.splits;
+  const int ts = t0 + split * per, te = min(t1, ts + per);
+  T* const mine = smem + w * (4 * TILE);
+
+  running<D> z;
+  auto request = [&](int t, int stage) {
+    const int have = t < te ? hi - t * 32 : 0;
+    keys.load((int64_t)t * 32, have, mine + stage * (2 * TILE));
+    vals.load((int64_t)t * 32, have, mine + stage * (2 * TILE) + TILE);
+  };
+  for (bool exact = false;; exact = true) {
+    z.reset();
+    int stage = 0;
+    if (ts + w < te) request(ts + w, 0);
+    for (int t = ts + w; t < te; t += NW, stage ^= 1) {
+      wave_fence();                        // the other stage's tiles have been read
+      request(t + NW, stage ^ 1);
+      asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(IN_FLIGHT) : "memory");
+      const T* const kt = mine + stage * (2 * TILE);
+      f16v x[1], bend;
+      x[0] = at.first(kt, fq, all16(0.f));
+      const int k0 = t * 32 + ((lane >> 5) << 2);
+      if (EXTRA) shape_scores<false>(g, x[0], bend, slope2, [&](int e) { return distance(range.pos, k0 + acc_row(e, 0)); });
+      const unsigned from = k0 - range.lo, len = range.hi - range.lo;
+      const bool inside = t * 32 >= wr.lo_max && t * 32 + 32 <= wr.hi_min;
+      if (!inside) {
+#pragma unroll
+        for (int e = 0; e < 16; ++e) x[0][e] = from + acc_row(e, 0) < len ? x[0][e] : -INFINITY;
+      }
+      z.take(x, c);
+      if (!exact || inside) at.second(kt + TILE, x[0], z.o);
+      else second_exact<T, D>(kt + TILE, x[0], z.o, lane, [&](int i) { return (unsigned)(t * 32 + i - range.lo) < len; });
+    }
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    z.l += other_half(z.l);
+    if (exact || !__any(there && fabsf(z.l) < INFINITY && not_finite(z.o))) break;
+  }
+
+  // join the wavefronts
+  float* const joint = (float*)smem;       // [wave][32][P], then [wave][32] references and sums
+  float* const stats = joint + NW * 32 * P;
+  __syncthreads();
+#pragma unroll
+  for (int i = 0; i < S::ND; ++i)
+#pragma unroll
+    for (int e4 = 0; e4 < 4; ++e4)
+      *reinterpret_cast<f4v*>(joint + (w * 32 + (lane & 31)) * P + 32 * i + acc_row(4 * e4, lane)) = f4v{z.o[i][4 * e4], z.o[i][4 * e4 + 1], z.o[i][4 * e4 + 2], z.o[i][4 * e4 + 3]};
+  if (lane < 32) {
+    stats[w * 64 + lane] = z.m;
+    stats[w * 64 + 32 + lane] = z.l;
+  }
+  __syncthreads();
+  for (int item = tid; item < 32 * (D / 4); item += NW * 64) {
+    const int c_ = item / (D / 4), col = item % (D / 4) * 4, p = cg * 32 + c_;
+    if (p >= pairs || col >= g.d) continue;
+    float m = stats[c_];
+#pragma unroll
+    for (int i = 1; i < NW; ++i) m = fmaxf(m, stats[i * 64 + c_]);
+    const float ref = m == -INFINITY ? 0.f : m;
+    float l = 0.f;
+    f4v o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+      const float keep = exp2_fast(stats[i * 64 + c_] - ref);
+      l = __builtin_fmaf(stats[i * 64 + 32 + c_], keep, l);
+      const f4v x = *reinterpret_cast<const f4v*>(joint + (i * 32 + c_) * P + col);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) o[e] = __builtin_fmaf(x[e], keep, o[e]);
+    }
+    if (g.splits > 1) {
+      float* const to = g.part + ((int64_t)lin * 32 + c_) * (D + 2);
+      if (col == 0) {
+        to[0] = m;
+        to[1] = l;
+      }
+#pragma unroll
+      for (int e = 0; e < 4; ++e) to[2 + col + e] = o[e];
+      continue;
+    }
+    const int oh = kh * g.group + p / g.q_len, oi = p % g.q_len;
+    const key_range k = range_of(g, r, b, oi);
+    const bool some = k.hi > k.lo;
+    const float inv = some ? 1.f / l : 0.f;
+    const int64_t orow = (int64_t)b * g.q_len + oi;
+    T* const to = (T*)g.out + r * g.out_z + orow * g.out_s + (int64_t)oh * g.d + col;
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (col + e < g.d) hdet_st(to + e, some ? o[e] * inv : 0.f);
+    if (g.lse && col == 0) g.lse[((int64_t)r * g.heads + oh) * g.seqs * g.q_len + orow] = some ? (ref + log2f(l)) * kLn2 : -INFINITY;
+  }
+}
+
+// A wavefront to a (query, head): the parts' results, times 2^(reference - the largest)
+template <typename T, int D> __global__ __launch_bounds__(THREADS) void attend_join_kernel(const attend_args g) {
+  const int pairs = g.group * g.q_len, ncg = (pairs + 31) / 32, lane = threadIdx.x & 63;
+  const int64_t id = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * NWV + (threadIdx.x >> 6);
+  if (id >= (int64_t)g.n * g.seqs * g.kv_heads * pairs) return;
+  const int p = (int)(id % pairs);
+  const int64_t grp = id / pairs;
+  const int kh = (int)(grp % g.kv_heads), b = (int)(grp / g.kv_heads % g.seqs), r = (int)(grp / g.kv_heads / g.seqs);
+  const float* const from = g.part + ((grp * g.splits * ncg + p / 32) * 32 + p % 32) * (D + 2);
+  const int64_t step = (int64_t)ncg * 32 * (D + 2);
+  const float own = lane < g.splits ? from[lane * step] : -INFINITY;
+  const float m = hdet_wave_max(own), ref = m == -INFINITY ? 0.f : m, keep = exp2_fast(own - ref);
+  const float l = hdet_wave_sum(lane < g.splits ? keep * from[lane * step + 1] : 0.f);
+  float o[D / 64] = {};
+  for (int i = 0; i < g.splits; ++i) {
+    const float k = __shfl(keep, i);
+#pragma unroll
+    for (int u = 0; u < D / 64; ++u)
+      if (lane + 64 * u < g.d) o[u] = __builtin_fmaf(k, from[i * step + 2 + lane + 64 * u], o[u]);
+  }
+  const int h = kh * g.group + p / g.q_len, qi = p % g.q_len;
+  const key_range k = range_of(g, r, b, qi);
+  const bool some = k.hi > k.lo;
+  const float inv = some ? 1.f / l : 0.f;
+  const int64_t row = (int64_t)b * g.q_len + qi;
+  T* const to = (T*)g.out + r * g.out_z + row * g.out_s + (int64_t)h * g.d;
+#pragma unroll
+  for (int u = 0; u < D / 64; ++u)
+    if (lane + 64 * u < g.d) hdet_st(to + lane + 64 * u, some ? o[u] * inv : 0.f);
+  if (g.lse && lane == 0) g.lse[((int64_t)r * g.heads + h) * g.seqs * g.q_len + row] = some ? (ref + log2f(l)) * kLn2 : -INFINITY;
+}
+
+// ---------------------------------------------------------------------------------------------
+// backward, step 1: dq, and what step 2 needs of the queries (row dots, statistics, ranges); block = 128 queries
+// ---------------------------------------------------------------------------------------------
+template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds__(THREADS, 2) void attend_dq_kernel(const attend_args g) {
+  typedef shape<T, D> S;
+  constexpr int TILE = S::TB * D, NB = S::TB / 32;
+  __shared__ __attribute__((aligned(1024))) T smem[4 * TILE];              // two stages of keys and values
+  __shared__ int ends[2 * NWV];
+  const unsigned lin = blockIdx.y * gridDim.x + blockIdx.x;
+  if (lin >= g.total) return;
+  const unsigned nx = (g.q_len + RB - 1) / RB;
+  const block_id blk = place_block(lin, g.total, nx, g.heavy_first);
+  const int h = blk.grp % g.heads, b = blk.grp / g.heads % g.seqs, r = blk.grp / g.heads / g.seqs;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int wq0 = (int)(nx - 1 - blk.x) * RB + w * WR, qi = wq0 + (lane & 31);
+  const bool there = qi < g.q_len;
+  const key_range range = there ? range_of(g, r, b, qi) : key_range{0, 0, 0};
+  const wave_range wr = wave_range_of(range, there);
+  if (lane == 0) {
+    ends[w] = wr.lo_min;
+    ends[NWV + w] = wr.hi_max;
+  }
+  const int64_t rows = (int64_t)g.seqs * g.q_len, row0 = (int64_t)b * g.q_len + wq0, row = row0 + (lane & 31);
+  const int64_t col = (int64_t)h * g.d, kcol = (int64_t)(h / g.group) * g.d, stat = ((int64_t)r * g.heads + h) * rows + row;
+  const bool some = range.hi > range.lo;
+  const T* const own = some ? (const T*)g.q + r * g.q_z + row * g.q_s + col : nullptr;
+  const T* const own_do = some ? (const T*)g.dout + r * g.do_z + row * g.do_s + col : nullptr;
+  const T* const own_o = some ? (const T*)g.o + r * g.o_z + row * g.o_s + col : nullptr;
+  typename S::frag fq[S::NF], fdo[S::NF];
+  float ndot = 0.f;                        // minus the row's dot, half of its columns a half-wavefront
+#pragma unroll
+  for (int i = 0; i < S::NF; ++i) {
+    fq[i] = own_frag<T, D, WHOLE>(own, i, g.d, lane);
+    fdo[i] = own_frag<T, D, WHOLE>(own_do, i, g.d, lane);
+    const typename S::frag fo = own_frag<T, D, WHOLE>(own_o, i, g.d, lane);
+#pragma unroll
+    for (int e = 0; e < S::E; ++e) ndot = __builtin_fmaf(-(float)fdo[i][e], (float)fo[e], ndot);
+  }
+  ndot += other_half(ndot);
+  const float lse2 = some ? g.lse_in[stat] * kLog2e : INFINITY;
+  if (there && lane < 32) {
+    g.lse2[stat] = lse2;
+    g.dot[stat] = ndot;
+    if (h == 0) {
+      g.lo[r * rows + row] = range.lo;
+      g.hi[r * rows + row] = range.hi;
+      g.pos_of[r * rows + row] = range.pos;
     }
   }
-  store_columns((T*)g.dk + r * g.dk_z + key * g.dk_s + (int64_t)kh * g.d, lane, g.d, ka * g.scale, kb * g.scale);
-  store_columns((T*)g.dv + r * g.dv_z + key * g.dv_s + (int64_t)kh * g.d, lane, g.d, va, vb);
+  // rows of the 32 that there are not: never inside
+  if (h == 0 && lane == 0 && wq0 < g.q_len)
+    g.groups[((int64_t)r * g.seqs + b) * ((g.q_len + 31) / 32) + wq0 / 32] = i4v{wr.lo_min, wq0 + 32 > g.q_len ? INT_MAX : wr.lo_max, wr.hi_min, wr.hi_max};
+  const tile_loader<T, D, S::TB, NWV, WHOLE> keys((const T*)g.k + r * g.k_z + (int64_t)b * g.kv_len * g.k_s + kcol, g.k_s, g.d, w, lane);
+  const tile_loader<T, D, S::TB, NWV, WHOLE> vals((const T*)g.v + r * g.v_z + (int64_t)b * g.kv_len * g.v_s + kcol, g.v_s, g.d, w, lane);
+  const S at(lane);
+  const float slope2 = EXTRA && g.slopes ? g.slopes[r * g.slopes_z + h] * kLog2e : 0.f, c = EXTRA ? 1.f : g.c;
+  __syncthreads();
+  const int lo = __builtin_amdgcn_readfirstlane(min(min(ends[0], ends[1]), min(ends[2], ends[3])));
+  const int hi = __builtin_amdgcn_readfirstlane(max(max(ends[4], ends[5]), max(ends[6], ends[7])));
+  const int t0 = lo / S::TB, t1 = (hi + S::TB - 1) / S::TB;
+
+  f16v dq[S::ND];                          // [column][query]
+  auto request = [&](int t) {
+    if (t >= t1) return;
+    T* const to = smem + (t & 1) * (2 * TILE);
+    keys.load((int64_t)t * S::TB, hi - t * S::TB, to);
+    vals.load((int64_t)t * S::TB, hi - t * S::TB, to + TILE);
+  };
+  for (bool exact = false;; exact = true) {
+#pragma unroll
+    for (int i = 0; i < S::ND; ++i) dq[i] = all16(0.f);
+    if (hi > 0) request(t0);
+    for (int t = t0; t < t1; ++t) {
+      wait_and_barrier<0>();
+      request(t + 1);
+#pragma unroll 1
+      for (int i = 0; i < NB; ++i) {
+        const int key0 = t * S::TB + 32 * i;
+        if (key0 >= wr.hi_max || key0 + 32 <= wr.lo_min) continue;
+        const T* const kt = smem + (t & 1) * (2 * TILE) + i * 32 * D;
+        f16v x = at.first(kt, fq, all16(0.f)), dp = at.first(kt + TILE, fdo, all16(ndot)), bend;
+        const int k0 = key0 + ((lane >> 5) << 2);
+        if (EXTRA) shape_scores<true>(g, x, bend, slope2, [&](int e) { return distance(range.pos, k0 + acc_row(e, 0)); });
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          dp[e] *= exp2_fast(__builtin_fmaf(x[e], c, -lse2));
+          if (EXTRA) dp[e] *= bend[e];
+        }
+        const bool inside = key0 >= wr.lo_max && key0 + 32 <= wr.hi_min;
+        const unsigned from = k0 - range.lo, len = range.hi - range.lo;
+        if (!inside) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) dp[e] = from + acc_row(e, 0) < len ? dp[e] : 0.f;
+        }
+        if (!exact || inside) at.second(kt, dp, dq);
+        else second_exact<T, D>(kt, dp, dq, lane, [&](int k) { return (unsigned)(key0 + k - range.lo) < len; });
+      }
+    }
+    const bool again = __syncthreads_or(some && fabsf(lse2) < INFINITY && not_finite(dq));
+    if (exact || !again) break;
+  }
+#pragma unroll
+  for (int i = 0; i < S::ND; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) dq[i][e] *= g.scale;
+  store_rows<T, D, WHOLE>(dq, (char*)smem + w * STRIP, (T*)g.dq + r * g.dq_z + row0 * g.dq_s + col, g.dq_s, g.q_len - wq0, g.d, lane);
 }
 
+// ---------------------------------------------------------------------------------------------
+// backward, step 2: dk and dv; block = 128 keys of a key head, walks over the query tiles of the heads that share it
+// ---------------------------------------------------------------------------------------------
+template <typename T, int D> constexpr int dkv_waves() { return sizeof(T) == 4 && D == 128 ? 1 : 2; }
+template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds__(THREADS, (dkv_waves<T, D>())) void attend_dkv_kernel(const attend_args g) {
+  typedef shape<T, D> S;
+  constexpr int TILE = S::TB * D, NB = S::TB / 32, STATS = 5 * S::TB;      // lse2, dot, lo, hi, position
+  __shared__ __attribute__((aligned(1024))) T smem[4 * TILE];              // two stages of queries and output gradients
+  __shared__ __attribute__((aligned(16))) int stats[2 * STATS];
+  __shared__ int ends[2 * NWV];
+  const unsigned lin = blockIdx.y * gridDim.x + blockIdx.x;
+  if (lin >= g.total) return;
+  const unsigned nx = (g.kv_len + RB - 1) / RB;
+  const block_id blk = place_block(lin, g.total, nx, g.heavy_first);
+  const int kh = blk.grp % g.kv_heads, b = blk.grp / g.kv_heads % g.seqs, r = blk.grp / g.kv_heads / g.seqs;
+  const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int k0 = blk.x * RB, wk0 = k0 + w * WR, key = wk0 + (lane & 31);
+  const int n_groups = (g.q_len + 31) / 32;
+  const i4v* const groups = g.groups + ((int64_t)r * g.seqs + b) * n_groups;
+  // first and last tile of queries that attend any of the block's keys
+  int first = INT_MAX, last = -1;
+  for (int i = tid; i < n_groups; i += THREADS) {
+    const i4v x = groups[i];
+    if (x[0] < k0 + RB && x[3] > k0) {
+      first = min(first, i);
+      last = i;
+    }
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    first = min(first, __shfl_xor(first, o));
+    last = max(last, __shfl_xor(last, o));
+  }
+  if (lane == 0) {
+    ends[w] = first;
+    ends[NWV + w] = last;
+  }
+  const bool there = key < g.kv_len;
+  const int64_t kcol = (int64_t)kh * g.d, row0 = (int64_t)b * g.kv_len + wk0, rows = (int64_t)g.seqs * g.q_len, q_row0 = (int64_t)b * g.q_len;
+  const T* const own_k = there ? (const T*)g.k + r * g.k_z + (row0 + (lane & 31)) * g.k_s + kcol : nullptr;
+  const T* const own_v = there ? (const T*)g.v + r * g.v_z + (row0 + (lane & 31)) * g.v_s + kcol : nullptr;
+  typename S::frag fk[S::NF], fv[S::NF];
+#pragma unroll
+  for (int i = 0; i < S::NF; ++i) {
+    fk[i] = own_frag<T, D, WHOLE>(own_k, i, g.d, lane);
+    fv[i] = own_frag<T, D, WHOLE>(own_v, i, g.d, lane);
+  }
+  const S at(lane);
+  const float c = EXTRA ? 1.f : g.c;
+  __syncthreads();
+  first = __builtin_amdgcn_readfirstlane(min(min(ends[0], ends[1]), min(ends[2], ends[3])));
+  last = __builtin_amdgcn_readfirstlane(max(max(ends[4], ends[5]), max(ends[6], ends[7])));
+  const int t0 = last < 0 ? 0 : first / NB, tiles = last < 0 ? 0 : last / NB + 1 - t0;
+
+  tile_loader<T, D, S::TB, NWV, WHOLE> qs((const T*)g.q + r * g.q_z + q_row0 * g.q_s, g.q_s, g.d, w, lane);
+  tile_loader<T, D, S::TB, NWV, WHOLE> dos((const T*)g.dout + r * g.do_z + q_row0 * g.do_s, g.do_s, g.d, w, lane);
+  const T *const q_at = qs.src, *const do_at = dos.src;
+  f16v dk[S::ND], dv[S::ND];               // [column][key]
+  auto request = [&](int j) {              // tile j of all heads' tiles
+    if (j >= tiles * g.group) return;
+    const int h = kh * g.group + j / tiles, t = t0 + j % tiles, q0 = t * S::TB, have = min(g.q_len - q0, S::TB);
+    qs.src = q_at + (int64_t)h * g.d;
+    dos.src = do_at + (int64_t)h * g.d;
+    T* const to = smem + (j & 1) * (2 * TILE);
+    qs.load(q0, have, to);
+    dos.load(q0, have, to + TILE);
+    // statistics: a wavefront an array (the last one two), zeros behind the last row
+    const int64_t row = q_row0 + q0, stat = ((int64_t)r * g.heads + h) * rows + row;
+    const void* const from = w == 0 ? (const void*)(g.lse2 + stat) : w == 1 ? (const void*)(g.dot + stat) : w == 2 ? (const void*)(g.lo + r * rows + row) : (const void*)(g.hi + r * rows + row);
+    int* const st = stats + (j & 1) * STATS;
+    if (lane < S::TB) {
+      lds_load4(scalar_rsrc(from, have * 4), __builtin_amdgcn_readfirstlane(lds_addr_of((const uint16_t*)(st + w * S::TB))), lane * 4);
+      if (w == 3) lds_load4(scalar_rsrc(g.pos_of + r * rows + row, have * 4), __builtin_amdgcn_readfirstlane(lds_addr_of((const uint16_t*)(st + 4 * S::TB))), lane * 4);
+    }
+  };
+  for (bool exact = false;; exact = true) {
+#pragma unroll
+    for (int i = 0; i < S::ND; ++i) dk[i] = dv[i] = all16(0.f);
+    request(0);
+    for (int j = 0; j < tiles * g.group; ++j) {
+      wait_and_barrier<0>();
+      request(j + 1);
+      const int h = kh * g.group + j / tiles, t = t0 + j % tiles;
+      const float slope2 = EXTRA && g.slopes ? g.slopes[r * g.slopes_z + h] * kLog2e : 0.f;
+#pragma unroll 1
+      for (int i = 0; i < NB; ++i) {
+        const int gi = t * NB + i;
+        if (gi >= n_groups) continue;
+        const i4v gr = groups[gi];
+        if (gr[0] >= wk0 + 32 || gr[3] <= wk0) continue;
+        const T* const qt = smem + (j & 1) * (2 * TILE) + i * 32 * D;
+        const int* const st = stats + (j & 1) * STATS + 32 * i + ((lane >> 5) << 2);
+        f16v dp, bend;
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4) {
+          const f4v nd = *reinterpret_cast<const f4v*>(st + S::TB + 8 * e4);
+#pragma unroll
+          for (int u = 0; u < 4; ++u) dp[4 * e4 + u] = nd[u];
+        }
+        f16v x = at.first(qt, fk, all16(0.f));
+        dp = at.first(qt + TILE, fv, dp);
+        if (EXTRA) shape_scores<true>(g, x, bend, slope2, [&](int e) { return distance(st[4 * S::TB + acc_row(e, 0)], key); });
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4) {
+          const f4v l2 = *reinterpret_cast<const f4v*>(st + 8 * e4);
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const int e = 4 * e4 + u;
+            x[e] = exp2_fast(__builtin_fmaf(x[e], c, -l2[u]));
+            dp[e] *= x[e];
+            if (EXTRA) dp[e] *= bend[e];
+          }
+        }
+        const bool inside = wk0 >= gr[1] && wk0 + 32 <= gr[2];
+        if (!inside) {
+#pragma unroll
+          for (int e4 = 0; e4 < 4; ++e4) {
+            const i4v lo = *reinterpret_cast<const i4v*>(st + 2 * S::TB + 8 * e4), hi = *reinterpret_cast<const i4v*>(st + 3 * S::TB + 8 * e4);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+              const bool seen = key >= lo[u] && key < hi[u];
+              x[4 * e4 + u] = seen ? x[4 * e4 + u] : 0.f;
+              dp[4 * e4 + u] = seen ? dp[4 * e4 + u] : 0.f;
+            }
+          }
+        }
+        if (!exact || inside) {
+          at.second(qt + TILE, x, dv);
+          at.second(qt, dp, dk);
+        } else {
+          const int* const s0 = stats + (j & 1) * STATS + 32 * i;
+          auto seen = [&](int q) { return key >= s0[2 * S::TB + q] && key < s0[3 * S::TB + q]; };
+          second_exact<T, D>(qt + TILE, x, dv, lane, seen);
+          second_exact<T, D>(qt, dp, dk, lane, seen);
+        }
+      }
+    }
+    const bool again = __syncthreads_or(there && (not_finite(dk) || not_finite(dv)));
+    if (exact || !again) break;
+  }
+#pragma unroll
+  for (int i = 0; i < S::ND; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) dk[i][e] *= g.scale;
+  char* const strip = (char*)smem + w * STRIP;
+  store_rows<T, D, WHOLE>(dk, strip, (T*)g.dk + r * g.dk_z + row0 * g.dk_s + kcol, g.dk_s, g.kv_len - wk0, g.d, lane);
+  store_rows<T, D, WHOLE>(dv, strip, (T*)g.dv + r * g.dv_z + row0 * g.dv_s + kcol, g.dv_s, g.kv_len - wk0, g.d, lane);
+}
+
+// ---------------------------------------------------------------------------------------------
+// launches
+// ---------------------------------------------------------------------------------------------
 template <typename A> attend_args common_args(const A& a) {
   attend_args g = {};
   g.q = a.q.dev; g.q_s = a.q.row_stride; g.q_z = a.q.replica_stride;
@@ -156,48 +697,129 @@ template <typename A> attend_args common_args(const A& a) {
   g.v = a.v.dev; g.v_s = a.v.row_stride; g.v_z = a.v.replica_stride;
   g.slopes = a.slopes_dev; g.slopes_z = a.slopes_stride;
   g.pos = a.positions_dev; g.first = a.first_dev; g.end = a.end_dev;
-  g.n = a.n_replicas; g.seqs = a.seqs; g.q_len = a.q_len; g.kv_len = a.kv_len; g.heads = a.heads; g.kv_heads = a.kv_heads; g.d = a.head_dim;
-  g.causal = a.causal; g.window = a.window;
-  g.scale = (float)a.scale; g.cap = (float)a.softcap; g.inv_cap = a.softcap > 0 ? (float)(1.0 / a.softcap) : 0.f;
+  g.n = a.n_replicas; g.seqs = a.seqs; g.q_len = a.q_len; g.kv_len = a.kv_len; g.heads = a.heads; g.kv_heads = a.kv_heads; g.group = a.heads / a.kv_heads;
+  g.d = a.head_dim; g.causal = a.causal; g.window = a.window; g.splits = 1;
+  g.scale = (float)a.scale; g.c = (float)(a.scale * 1.4426950408889634); g.cap2 = (float)(a.softcap * 1.4426950408889634);
+  g.inv_cap = a.softcap > 0 ? (float)(1.0 / a.softcap) : 0.f;
   return g;
 }
-dim3 wave_grid(int64_t waves) {
-  const int64_t blocks = (waves + WAVES - 1) / WAVES, x = blocks < (1 << 20) ? blocks : 1 << 20;
-  return dim3((unsigned)x, (unsigned)((blocks + x - 1) / x));
+// whole 16-byte pieces, and a tile within 31 bits
+bool whole(const hdet_rows& m, int size, int d) {
+  const int64_t mask = 16 / size - 1;
+  return ((uintptr_t)m.dev & 15) == 0 && ((m.row_stride | m.replica_stride | d) & mask) == 0 && m.row_stride < (int64_t)1 << 23;
+}
+dim3 grid_of(unsigned blocks) {
+  const unsigned x = blocks < (1u << 20) ? blocks : 1u << 20;
+  return dim3(x, (blocks + x - 1) / x);
+}
+// scores that need more than a product with a constant (a scale of 0 or below turns the maximum around)
+template <typename A> bool extra(const A& a) { return a.softcap > 0 || a.slopes_dev || !(a.scale > 0); }
+
+// f(type, D, EXTRA, WHOLE); rows that are not whole pieces take the general scores too
+template <typename F> void with_shape(int dtype, int d, bool ex, bool wh, F f) {
+  auto with_flags = [&](auto t, auto dd) {
+    if (!wh) f(t, dd, std::true_type(), std::false_type());
+    else if (ex) f(t, dd, std::true_type(), std::true_type());
+    else f(t, dd, std::false_type(), std::true_type());
+  };
+  auto with_d = [&](auto t) {
+    if (d <= 64) with_flags(t, std::integral_constant<int, 64>());
+    else with_flags(t, std::integral_constant<int, 128>());
+  };
+  if (dtype == HDET_TYPE_BF16) with_d(uint16_t());
+  else with_d(float());
+}
+bool heavy_first(unsigned total, unsigned nx) { return total <= (nx >= 8 ? 16u : 8u) * (unsigned)hdet_compute_units(); }
+
+// Parts of the keys for few queries, 0: the queries fill the chip
+int few_splits(int n, int seqs, int q_len, int kv_len, int heads, int kv_heads) {
+  const int64_t pairs = (int64_t)(heads / kv_heads) * q_len, groups = (int64_t)n * seqs * kv_heads, cus = hdet_compute_units();
+  if (pairs == 0 || groups == 0) return 0;
+  const int64_t blocks = (int64_t)n * seqs * heads * ((q_len + RB - 1) / RB), few = groups * ((pairs + 31) / 32);
+  if (q_len > 16 && (blocks >= cus / 2 || kv_len < 1024)) return 0;
+  int64_t s = (2 * cus + few - 1) / few, most = (kv_len + 255) / 256;
+  if (s > most) s = most;
+  return (int)(s < 1 ? 1 : s > 64 ? 64 : s);
+}
+constexpr size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
+
+struct backward_layout { size_t lse2, dot, lo, hi, pos, groups, total; };
+backward_layout layout_of(int n, int seqs, int q_len, int heads) {
+  const size_t rows = (size_t)n * seqs * q_len;
+  backward_layout l;
+  l.lse2 = 0;
+  l.dot = l.lse2 + up256(rows * heads * 4);
+  l.lo = l.dot + up256(rows * heads * 4);
+  l.hi = l.lo + up256(rows * 4);
+  l.pos = l.hi + up256(rows * 4);
+  l.groups = l.pos + up256(rows * 4);
+  l.total = rows ? l.groups + up256((size_t)n * seqs * ((q_len + 31) / 32) * 16) : 0;
+  return l;
 }
 
 }  // namespace
 
-size_t hdet_attend_bytes(int, int, int, int, int, int, int) { return 0; }
-size_t hdet_attend_backward_bytes(int n, int seqs, int q_len, int, int heads, int, int) { return (size_t)n * seqs * q_len * heads * sizeof(float); }
+size_t hdet_attend_bytes(int n, int seqs, int q_len, int kv_len, int heads, int kv_heads, int head_dim) {
+  const int s = few_splits(n, seqs, q_len, kv_len, heads, kv_heads);
+  if (s <= 1) return 0;
+  const size_t ncg = ((size_t)(heads / kv_heads) * q_len + 31) / 32;
+  return up256((size_t)n * seqs * kv_heads * ncg * s * 32 * ((head_dim <= 64 ? 64 : 128) + 2) * 4);
+}
+size_t hdet_attend_backward_bytes(int n, int seqs, int q_len, int, int heads, int, int) { return layout_of(n, seqs, q_len, heads).total; }
 
 hipError_t hdet_launch_attend(const hdet_attention_args& a, hipStream_t s) {
   attend_args g = common_args(a);
+  const int size = a.dtype == HDET_TYPE_BF16 ? 2 : 4;
   g.out = a.out.dev; g.out_s = a.out.row_stride; g.out_z = a.out.replica_stride;
   g.lse = a.lse_dev;
-  const int64_t waves = (int64_t)a.seqs * a.q_len * a.heads * a.n_replicas;
-  if (waves == 0) return hipSuccess;
-  if (a.dtype == HDET_TYPE_BF16) hipLaunchKernelGGL(attend_kernel<uint16_t>, wave_grid(waves), dim3(THREADS), 0, s, g);
-  else hipLaunchKernelGGL(attend_kernel<float>, wave_grid(waves), dim3(THREADS), 0, s, g);
+  if ((int64_t)a.seqs * a.q_len == 0) return hipSuccess;
+  const bool wh = whole(a.q, size, a.head_dim) && whole(a.k, size, a.head_dim) && whole(a.v, size, a.head_dim) && whole(a.out, size, a.head_dim);
+  const int splits = few_splits(a.n_replicas, a.seqs, a.q_len, a.kv_len, a.heads, a.kv_heads);
+  if (splits) {
+    const int64_t pairs = (int64_t)g.group * a.q_len, groups = (int64_t)a.n_replicas * a.seqs * a.kv_heads;
+    g.splits = splits;
+    g.part = (float*)a.workspace_dev;
+    g.total = (unsigned)(groups * ((pairs + 31) / 32) * splits);
+    with_shape(a.dtype, a.head_dim, extra(a), wh, [&](auto t, auto d, auto ex, auto w) {
+      typedef decltype(t) T;
+      hipLaunchKernelGGL((attend_few_kernel<T, d, ex, w>), grid_of(g.total), dim3(few_waves<T, d>() * 64), 0, s, g);
+      if (splits > 1) hipLaunchKernelGGL((attend_join_kernel<T, d>), grid_of((unsigned)((groups * pairs + NWV - 1) / NWV)), dim3(THREADS), 0, s, g);
+    });
+    return hipGetLastError();
+  }
+  const unsigned nx = (a.q_len + RB - 1) / RB;
+  g.total = nx * (unsigned)a.n_replicas * a.seqs * a.heads;
+  g.heavy_first = heavy_first(g.total, nx);
+  with_shape(a.dtype, a.head_dim, extra(a), wh, [&](auto t, auto d, auto ex, auto w) {
+    hipLaunchKernelGGL((attend_kernel<decltype(t), d, ex, w>), grid_of(g.total), dim3(THREADS), 0, s, g);
+  });
   return hipGetLastError();
 }
 
 hipError_t hdet_launch_attend_backward(const hdet_attention_grad_args& a, hipStream_t s) {
   attend_args g = common_args(a);
+  const int size = a.dtype == HDET_TYPE_BF16 ? 2 : 4;
   g.o = a.out.dev; g.o_s = a.out.row_stride; g.o_z = a.out.replica_stride;
   g.dout = a.dout.dev; g.do_s = a.dout.row_stride; g.do_z = a.dout.replica_stride;
   g.dq = a.dq.dev; g.dq_s = a.dq.row_stride; g.dq_z = a.dq.replica_stride;
   g.dk = a.dk.dev; g.dk_s = a.dk.row_stride; g.dk_z = a.dk.replica_stride;
   g.dv = a.dv.dev; g.dv_s = a.dv.row_stride; g.dv_z = a.dv.replica_stride;
   g.lse_in = a.lse_dev;
-  g.dot = (float*)a.workspace_dev;
-  const int64_t q_waves = (int64_t)a.seqs * a.q_len * a.heads * a.n_replicas, k_waves = (int64_t)a.seqs * a.kv_len * a.kv_heads * a.n_replicas;
-  auto go = [&](auto e) {
-    typedef decltype(e) T;
-    if (q_waves) hipLaunchKernelGGL(attend_dq_kernel<T>, wave_grid(q_waves), dim3(THREADS), 0, s, g);
-    if (k_waves) hipLaunchKernelGGL(attend_dkv_kernel<T>, wave_grid(k_waves), dim3(THREADS), 0, s, g);
-  };
-  if (a.dtype == HDET_TYPE_BF16) go(uint16_t());
-  else go(float());
+  const backward_layout l = layout_of(a.n_replicas, a.seqs, a.q_len, a.heads);
+  char* const w8 = (char*)a.workspace_dev;
+  g.lse2 = (float*)(w8 + l.lse2); g.dot = (float*)(w8 + l.dot);
+  g.lo = (int*)(w8 + l.lo); g.hi = (int*)(w8 + l.hi); g.pos_of = (int*)(w8 + l.pos); g.groups = (i4v*)(w8 + l.groups);
+  bool wh = true;
+  for (const hdet_rows* m : {&a.q, &a.k, &a.v, &a.out, &a.dout, &a.dq, &a.dk, &a.dv}) wh = wh && (!m->dev || whole(*m, size, a.head_dim));
+  const unsigned nq = (a.q_len + RB - 1) / RB, nk = (a.kv_len + RB - 1) / RB;
+  with_shape(a.dtype, a.head_dim, extra(a), wh, [&](auto t, auto d, auto ex, auto w) {
+    typedef decltype(t) T;
+    g.total = nq * (unsigned)a.n_replicas * a.seqs * a.heads;
+    g.heavy_first = nq && heavy_first(g.total, nq);
+    if (g.total) hipLaunchKernelGGL((attend_dq_kernel<T, d, ex, w>), grid_of(g.total), dim3(THREADS), 0, s, g);
+    g.total = nk * (unsigned)a.n_replicas * a.seqs * a.kv_heads;
+    g.heavy_first = nk && heavy_first(g.total, nk);
+    if (g.total) hipLaunchKernelGGL((attend_dkv_kernel<T, d, ex, w>), grid_of(g.total), dim3(THREADS), 0, s, g);
+  });
   return hipGetLastError();
 }

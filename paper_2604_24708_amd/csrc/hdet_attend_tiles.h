@@ -1,0 +1,254 @@
+// Tiles and 32 x 32 blocks of the attention kernels: element types, LDS layout, matrix instructions.
+//
+// A tile is rows of D columns (a head, zeros behind its last column) of keys, values, queries or gradients, in LDS in chunks of 16 bytes; the
+// chunks of row r are permuted by XOR with swz(r), so that the reads below touch disjoint banks: 16 bytes of each of 32 rows, and 4 rows x 32 bytes of
+// the transposing read.  The first product of a block has the wavefront's own 32 rows as the accumulator's COLUMNS: a lane holds one of them and
+// 16 entries of the other side, so that row reductions stay inside a lane and its partner lane + 32, and the accumulator, in bf16 or as it is, is the
+// second product's operand: its rows are that product's contraction index.
+#pragma once
+
+#include "hdet_elem.h"
+#include "hdet_lds.h"
+
+namespace hdet_attend {
+
+typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
+typedef float f16v __attribute__((ext_vector_type(16)));
+typedef float f4v __attribute__((ext_vector_type(4)));
+typedef int i4v __attribute__((ext_vector_type(4)));
+typedef short s4v __attribute__((ext_vector_type(4)));
+typedef short s8v __attribute__((ext_vector_type(8)));
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
+__device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+__device__ __forceinline__ f16v all16(float x) {
+  f16v z;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) z[e] = x;
+  return z;
+}
+// accumulator element e of lane l is row (e / 4) * 8 + (l / 32) * 4 + e % 4, column l % 32 of its 32 x 32 block
+__device__ __forceinline__ int acc_row(int e, int lane) { return ((e >> 2) << 3) + ((lane >> 5) << 2) + (e & 3); }
+// LDS of a wavefront's own: what its lanes have written is there for its other lanes
+__device__ __forceinline__ void wave_fence() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
+
+template <typename T, int D> struct shape;
+// bf16: v_mfma_f32_32x32x16_bf16; the second product's other operand comes through the transposing LDS read
+template <int D> struct shape<uint16_t, D> {
+  typedef bf16x8 frag;
+  static constexpr int E = 8, C = D / 8, NF = D / 16, ND = D / 32, TB = 64;
+  static __device__ __forceinline__ int swz(int r) { return D == 64 ? ((r & 2) << 1) | ((r >> 2) & 3) : ((r & 3) << 2) | ((r >> 2) & 3); }
+  int k[NF], t[ND][2];                     // where a lane's fragments begin inside a tile (elements)
+  __device__ __forceinline__ explicit shape(int lane) {
+    const int row = lane & 31, p = lane & 15;
+#pragma unroll
+    for (int i = 0; i < NF; ++i) k[i] = row * D + (((2 * i + (lane >> 5)) ^ swz(row)) << 3);
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+      for (int u = 0; u < 2; ++u) {
+        const int kr = ((lane >> 5) << 2) + (p >> 2) + 8 * u;
+        t[dt][u] = kr * D + (((4 * dt + ((lane >> 4) & 1) * 2 + ((p & 3) >> 1)) ^ swz(kr)) << 3) + ((p & 1) << 2);
+      }
+  }
+  // acc += (32 rows from `tile` on) (own rows)^T
+  __device__ __forceinline__ f16v first(const uint16_t* tile, const frag (&own)[NF], f16v acc) const {
+#pragma unroll
+    for (int i = 0; i < NF; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const frag*>(tile + k[i]), own[i], acc, 0, 0, 0);
+    return acc;
+  }
+  // acc^T += (32 rows from `tile` on)^T x, x [row][own row] rounded to bf16
+  __device__ __forceinline__ void second(const uint16_t* tile, const f16v& x, f16v (&acc)[ND]) const {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      frag f;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) f[i] = (__bf16)x[8 * j + i];
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt) {
+        const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s4v __attribute__((address_space(3)))*)(tile + 16 * j * D + t[dt][0]));
+        const s4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s4v __attribute__((address_space(3)))*)(tile + 16 * j * D + t[dt][1]));
+        const s8v both = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(frag, both), f, acc[dt], 0, 0, 0);
+      }
+    }
+  }
+  static __device__ __forceinline__ float rounded(float x) { return (float)(__bf16)x; }
+};
+// fp32: v_mfma_f32_32x32x2_f32; a fragment is 4 columns, and step i of them contracts column i of both half-wavefronts' chunks
+template <int D> struct shape<float, D> {
+  typedef f4v frag;
+  static constexpr int E = 4, C = D / 4, NF = D / 8, ND = D / 32, TB = 32;
+  static __device__ __forceinline__ int swz(int r) { return r & 7; }
+  int k[NF], t[ND][4];
+  __device__ __forceinline__ explicit shape(int lane) {
+    const int row = lane & 31;
+#pragma unroll
+    for (int i = 0; i < NF; ++i) k[i] = row * D + (((2 * i + (lane >> 5)) ^ swz(row)) << 2);
+#pragma unroll
+    for (int dt = 0; dt < ND; ++dt)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        const int r = ((lane >> 5) << 2) + u;
+        t[dt][u] = r * D + (((8 * dt + (row >> 2)) ^ swz(r)) << 2) + (row & 3);
+      }
+  }
+  __device__ __forceinline__ f16v first(const float* tile, const frag (&own)[NF], f16v acc) const {
+#pragma unroll
+    for (int i = 0; i < NF; ++i) {
+      const frag a = *reinterpret_cast<const frag*>(tile + k[i]);
+#pragma unroll
+      for (int u = 0; u < 4; ++u) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[u], own[i][u], acc, 0, 0, 0);
+    }
+    return acc;
+  }
+  __device__ __forceinline__ void second(const float* tile, const f16v& x, f16v (&acc)[ND]) const {
+#pragma unroll
+    for (int e = 0; e < 16; ++e)
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt) acc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(tile[(e >> 2) * 8 * D + t[dt][e & 3]], x[e], acc[dt], 0, 0, 0);
+  }
+  static __device__ __forceinline__ float rounded(float x) { return x; }
+};
+
+// second() with the pairs that are not attended left out one by one, for tiles in which 0 times something is not 0.  `seen(i)`: row i of the 32 takes part.
+template <typename T, int D, typename F>
+__device__ __forceinline__ void second_exact(const T* tile, f16v x, f16v (&acc)[D / 32], int lane, F seen) {
+  typedef shape<T, D> S;
+#pragma unroll 1
+  for (int e = 0; e < 16; ++e) {
+    const float own = S::rounded(x[0]), other = other_half(own);
+#pragma unroll
+    for (int i = 0; i < 15; ++i) x[i] = x[i + 1];
+#pragma unroll 1
+    for (int half = 0; half < 2; ++half) {
+      const int row = ((e >> 2) << 3) + half * 4 + (e & 3);
+      const float p = half == (lane >> 5) ? own : other;
+      if (!seen(row)) continue;
+#pragma unroll
+      for (int dt = 0; dt < D / 32; ++dt)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int col = 32 * dt + acc_row(i, lane);
+          acc[dt][i] = __builtin_fmaf(p, hdet_ld(tile + row * D + (((col / S::E) ^ S::swz(row)) * S::E) + col % S::E), acc[dt][i]);
+        }
+    }
+  }
+}
+template <int N> __device__ __forceinline__ bool not_finite(const f16v (&x)[N]) {
+  float s = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i)
+#pragma unroll
+    for (int e = 0; e < 16; ++e) s = __builtin_fmaf(x[i][e], 0.f, s);
+  return s != 0.f;
+}
+
+// a descriptor in scalar registers (every lane has the same; the compiler does not always see it)
+__device__ __forceinline__ hdet_rsrc scalar_rsrc(const void* p, uint32_t bytes) {
+  hdet_rsrc r = make_rsrc(p, bytes);
+#pragma unroll
+  for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_readfirstlane(r[i]);
+  return r;
+}
+// Tiles of ROWS rows of a matrix (row pitch ld, d columns) into LDS, by NW wavefronts.  WHOLE: 16-byte pieces straight from memory to LDS; else element by
+// element through registers.
+template <typename T, int D, int ROWS, int NW, bool WHOLE> struct tile_loader {
+  typedef shape<T, D> S;
+  static constexpr int NI = ROWS * S::C / (64 * NW);       // pieces a lane
+  static constexpr int STEP = 64 * NW / S::C;              // rows between them
+  static constexpr bool EVEN = STEP % (sizeof(T) == 2 ? 16 : 8) == 0;      // swz does not see the step
+  static constexpr int BYTES = ROWS * D * sizeof(T);
+  const T* src;
+  int64_t ld;
+  int d, wave, lane;
+  uint32_t off[EVEN ? 1 : NI];
+  __device__ __forceinline__ tile_loader(const T* src_, int64_t ld_, int d_, int wave_, int lane_) : src(src_), ld(ld_), d(d_), wave(wave_), lane(lane_) {
+#pragma unroll
+    for (int u = 0; u < (EVEN ? 1 : NI); ++u) {
+      const int id = (u * NW + wave) * 64 + lane, row = id / S::C, chunk = (id % S::C) ^ S::swz(row);
+      // columns that there are not: an offset beyond any extent
+      off[u] = chunk * S::E < d ? (uint32_t)((row * ld + chunk * S::E) * (int)sizeof(T)) : 0x80000000u;
+    }
+  }
+  // rows row0 .. row0 + have - 1 (have <= 0: none), zeros behind them, to the LDS tile `at`
+  __device__ __forceinline__ void load(int64_t row0, int have, T* at) const {
+    if (have > ROWS) have = ROWS;
+    if (WHOLE) {
+      const hdet_rsrc rs = scalar_rsrc(src + (have > 0 ? row0 * ld : 0), have > 0 ? (uint32_t)(((have - 1) * ld + d) * (int)sizeof(T)) : 0u);
+      const uint32_t to = __builtin_amdgcn_readfirstlane(lds_addr_of((const uint16_t*)at));
+#pragma unroll
+      for (int u = 0; u < NI; ++u)
+        lds_load16(rs, to + (u * NW + wave) * 1024, EVEN ? off[0] + (uint32_t)(u * STEP * ld * (int)sizeof(T)) : off[EVEN ? 0 : u]);
+    } else {
+#pragma unroll 1
+      for (int u = 0; u < NI; ++u) {
+        const int id = (u * NW + wave) * 64 + lane, row = id / S::C, chunk = (id % S::C) ^ S::swz(row);
+        const T* p = src + (row0 + row) * ld + chunk * S::E;
+#pragma unroll
+        for (int e = 0; e < S::E; ++e) at[id * S::E + e] = row < have && chunk * S::E + e < d ? p[e] : T(0);
+      }
+    }
+  }
+};
+
+// A lane's fragment i of its own row at p (null: zeros)
+template <typename T, int D, bool WHOLE> __device__ __forceinline__ typename shape<T, D>::frag own_frag(const T* p, int i, int d, int lane) {
+  typedef shape<T, D> S;
+  const int col = (2 * i + (lane >> 5)) * S::E;
+  typename S::frag f = {};
+  if (WHOLE) {
+    if (p && col < d) f = *reinterpret_cast<const typename S::frag*>(p + col);
+  } else if (p) {
+    T x[S::E];
+#pragma unroll
+    for (int e = 0; e < S::E; ++e) x[e] = col + e < d ? p[col + e] : T(0);
+    __builtin_memcpy(&f, x, 16);
+  }
+  return f;
+}
+
+// A wavefront's results, [column][own row] in accumulators, to rows of dst (row pitch ld), the first `have` of 32 and d columns, through the
+// wavefront's strip in LDS so that a store writes 16 bytes of a row
+constexpr int STRIP = 32 * 36 * 4;         // bytes
+template <typename T, int D, bool WHOLE>
+__device__ __forceinline__ void store_rows(const f16v (&o)[D / 32], void* strip_, T* dst, int64_t ld, int have, int d, int lane) {
+  typedef shape<T, D> S;
+  constexpr int P = sizeof(T) == 2 ? 40 : 36, PER = 32 / S::E;
+  T* const strip = (T*)strip_;
+#pragma unroll
+  for (int dt = 0; dt < D / 32; ++dt) {
+    if (32 * dt >= d) break;
+    wave_fence();
+#pragma unroll
+    for (int e4 = 0; e4 < 4; ++e4)
+      hdet_st4(strip + (lane & 31) * P + acc_row(4 * e4, lane), hdet_f4{{o[dt][4 * e4], o[dt][4 * e4 + 1], o[dt][4 * e4 + 2], o[dt][4 * e4 + 3]}});
+    wave_fence();
+#pragma unroll
+    for (int i = 0; i < PER / 2; ++i) {
+      const int c = lane + 64 * i, row = c / PER, col = c % PER * S::E;
+      if (row >= have) continue;
+      T* const to = dst + row * ld + 32 * dt + col;
+      if (WHOLE) {
+        if (32 * dt + col < d) *reinterpret_cast<f4v*>(to) = *reinterpret_cast<const f4v*>(strip + row * P + col);
+      } else {
+#pragma unroll
+        for (int e = 0; e < S::E; ++e)
+          if (32 * dt + col + e < d) to[e] = strip[row * P + col + e];
+      }
+    }
+  }
+  wave_fence();
+}
+
+// tanh: 1 - 2 / (e^2x + 1) on the hardware's exponential and reciprocal, and below 0.3, where that cancels, its series up to x^9 (off by 5e-8 of itself)
+__device__ __forceinline__ float tanh_fast(float x) {
+  const float x2 = x * x;
+  const float series = __builtin_fmaf(x * x2, __builtin_fmaf(x2, __builtin_fmaf(x2, __builtin_fmaf(x2, 2.1869489e-2f, -5.3968254e-2f), 0.13333334f), -0.33333334f), x);
+  const float far = __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(exp2_fast(x * (2.f * kLog2e)) + 1.f), 1.f);
+  return x2 < 0.09f ? series : far;
+}
+
+}  // namespace hdet_attend

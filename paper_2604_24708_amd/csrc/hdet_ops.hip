@@ -150,6 +150,10 @@ void attention_sizes(argument_checks& c, int n, int seqs, int q_len, int kv_len,
   c.need(head_dim >= 1 && head_dim <= HDET_MAX_ATTENTION_DIM, "head_dim must be in 1 .. HDET_MAX_ATTENTION_DIM");
   c.need(kv_heads >= 1 && heads >= 1 && heads % (kv_heads < 1 ? 1 : kv_heads) == 0, "heads must be a multiple of kv_heads");
   c.need((int64_t)heads * head_dim <= kMaxHeadColumns, "heads * head_dim must be up to 2^20");
+  if (!c.ok()) return;
+  // the kernels count their blocks in 32 bits
+  const int64_t pairs = (int64_t)n * seqs * (q_len > 0 ? q_len : 1) * heads, blocks = (int64_t)n * seqs * kv_heads * (((int64_t)kv_len + 127) / 128);
+  c.need(seqs <= kMaxKeys && pairs <= (int64_t)1 << 31 && blocks <= (int64_t)1 << 31, "too many sequences and heads: n_replicas * seqs * q_len * heads must be up to 2^31");
 }
 // What both passes of attention check
 template <typename A> void attention_arguments(argument_checks& c, const A& a) {

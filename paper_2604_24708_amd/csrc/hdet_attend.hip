@@ -180,7 +180,7 @@ template <int D> struct running {
 // ---------------------------------------------------------------------------------------------
 // forward: block = 128 queries of one (replica, sequence, head)
 // ---------------------------------------------------------------------------------------------
-template <typename T, int D> constexpr int forward_waves() { return sizeof(T) == 2 && D == 64 ? 3 : 2; }
+template <typename T, int D> constexpr int forward_waves() { return sizeof(T) == 2 ? (D == 64 ? 3 : 2) : (D == 64 ? 2 : 1); }
 template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds__(THREADS, (forward_waves<T, D>())) void attend_kernel(const attend_args g) {
   typedef shape<T, D> S;
   constexpr int TILE = S::TB * D, NB = S::TB / 32;
@@ -221,7 +221,7 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
     keys.load((int64_t)t * S::TB, hi - t * S::TB, to);
     vals.load((int64_t)t * S::TB, hi - t * S::TB, to + TILE);
   };
-  for (bool exact = false;; exact = true) {
+  auto walk = [&](auto exact) {            // (a body of its own for the second time: the first one keeps its registers)
     z.reset();
     if (hi > 0) request(t0);
     for (int t = t0; t < t1; ++t) {
@@ -240,7 +240,7 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
 #pragma unroll
         for (int e = 0; e < 16; ++e) x[0][e] = from + acc_row(e, 0) < len ? x[0][e] : -INFINITY;
         z.take(x, c);
-        if (!exact) at.second(vt + i * 32 * D, x[0], z.o);
+        if (!decltype(exact)::value) at.second(vt + i * 32 * D, x[0], z.o);
         else second_exact<T, D>(vt + i * 32 * D, x[0], z.o, lane, [&](int row) { return (unsigned)(key0 + 32 * i + row - range.lo) < len; });
       };
       if (key0 >= wr.lo_max && key0 + S::TB <= wr.hi_min) {
@@ -261,8 +261,11 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
       }
     }
     z.l += other_half(z.l);
-    const bool again = __syncthreads_or(there && fabsf(z.l) < INFINITY && not_finite(z.o));
-    if (exact || !again) break;
+  };
+  walk(std::false_type());
+  if (__syncthreads_or(there && fabsf(z.l) < INFINITY && not_finite(z.o))) {
+    walk(std::true_type());
+    __syncthreads();
   }
   const bool some = range.hi > range.lo;
   const float inv = some ? 1.f / z.l : 0.f;
@@ -316,7 +319,7 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
     keys.load((int64_t)t * 32, have, mine + stage * (2 * TILE));
     vals.load((int64_t)t * 32, have, mine + stage * (2 * TILE) + TILE);
   };
-  for (bool exact = false;; exact = true) {
+  auto walk = [&](auto exact) {
     z.reset();
     int stage = 0;
     if (ts + w < te) request(ts + w, 0);
@@ -336,13 +339,14 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
         for (int e = 0; e < 16; ++e) x[0][e] = from + acc_row(e, 0) < len ? x[0][e] : -INFINITY;
       }
       z.take(x, c);
-      if (!exact || inside) at.second(kt + TILE, x[0], z.o);
+      if (!decltype(exact)::value || inside) at.second(kt + TILE, x[0], z.o);
       else second_exact<T, D>(kt + TILE, x[0], z.o, lane, [&](int i) { return (unsigned)(t * 32 + i - range.lo) < len; });
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     z.l += other_half(z.l);
-    if (exact || !__any(there && fabsf(z.l) < INFINITY && not_finite(z.o))) break;
-  }
+  };
+  walk(std::false_type());
+  if (__any(there && fabsf(z.l) < INFINITY && not_finite(z.o))) walk(std::true_type());
 
   // join the wavefronts
   float* const joint = (float*)smem;       // [wave][32][P], then [wave][32] references and sums
@@ -433,7 +437,7 @@ template <typename T, int D> __global__ __launch_bounds__(THREADS) void attend_j
 // ---------------------------------------------------------------------------------------------
 // backward, step 1: dq, and what step 2 needs of the queries (row dots, statistics, ranges); block = 128 queries
 // ---------------------------------------------------------------------------------------------
-template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds__(THREADS, 2) void attend_dq_kernel(const attend_args g) {
+template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds__(THREADS, (sizeof(T) == 4 && D == 128 ? 1 : 2)) void attend_dq_kernel(const attend_args g) {
   typedef shape<T, D> S;
   constexpr int TILE = S::TB * D, NB = S::TB / 32;
   __shared__ __attribute__((aligned(1024))) T smem[4 * TILE];              // two stages of keys and values
@@ -498,7 +502,7 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
     keys.load((int64_t)t * S::TB, hi - t * S::TB, to);
     vals.load((int64_t)t * S::TB, hi - t * S::TB, to + TILE);
   };
-  for (bool exact = false;; exact = true) {
+  auto walk = [&](auto exact) {
 #pragma unroll
     for (int i = 0; i < S::ND; ++i) dq[i] = all16(0.f);
     if (hi > 0) request(t0);
@@ -524,12 +528,15 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
 #pragma unroll
           for (int e = 0; e < 16; ++e) dp[e] = from + acc_row(e, 0) < len ? dp[e] : 0.f;
         }
-        if (!exact || inside) at.second(kt, dp, dq);
+        if (!decltype(exact)::value || inside) at.second(kt, dp, dq);
         else second_exact<T, D>(kt, dp, dq, lane, [&](int k) { return (unsigned)(key0 + k - range.lo) < len; });
       }
     }
-    const bool again = __syncthreads_or(some && fabsf(lse2) < INFINITY && not_finite(dq));
-    if (exact || !again) break;
+  };
+  walk(std::false_type());
+  if (__syncthreads_or(some && fabsf(lse2) < INFINITY && not_finite(dq))) {
+    walk(std::true_type());
+    __syncthreads();
   }
 #pragma unroll
   for (int i = 0; i < S::ND; ++i)
@@ -541,7 +548,7 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
 // ---------------------------------------------------------------------------------------------
 // backward, step 2: dk and dv; block = 128 keys of a key head, walks over the query tiles of the heads that share it
 // ---------------------------------------------------------------------------------------------
-template <typename T, int D> constexpr int dkv_waves() { return sizeof(T) == 4 && D == 128 ? 1 : 2; }
+template <typename T, int D> constexpr int dkv_waves() { return D == 128 ? 1 : 2; }
 template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds__(THREADS, (dkv_waves<T, D>())) void attend_dkv_kernel(const attend_args g) {
   typedef shape<T, D> S;
   constexpr int TILE = S::TB * D, NB = S::TB / 32, STATS = 5 * S::TB;      // lse2, dot, lo, hi, position
@@ -613,7 +620,7 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
       if (w == 3) lds_load4(scalar_rsrc(g.pos_of + r * rows + row, have * 4), __builtin_amdgcn_readfirstlane(lds_addr_of((const uint16_t*)(st + 4 * S::TB))), lane * 4);
     }
   };
-  for (bool exact = false;; exact = true) {
+  auto walk = [&](auto exact) {
 #pragma unroll
     for (int i = 0; i < S::ND; ++i) dk[i] = dv[i] = all16(0.f);
     request(0);
@@ -664,7 +671,7 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
             }
           }
         }
-        if (!exact || inside) {
+        if (!decltype(exact)::value || inside) {
           at.second(qt + TILE, x, dv);
           at.second(qt, dp, dk);
         } else {
@@ -675,8 +682,11 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
         }
       }
     }
-    const bool again = __syncthreads_or(there && (not_finite(dk) || not_finite(dv)));
-    if (exact || !again) break;
+  };
+  walk(std::false_type());
+  if (__syncthreads_or(there && (not_finite(dk) || not_finite(dv)))) {
+    walk(std::true_type());
+    __syncthreads();
   }
 #pragma unroll
   for (int i = 0; i < S::ND; ++i)

@@ -130,9 +130,12 @@ __device__ __forceinline__ void second_exact(const T* tile, f16v x, f16v (&acc)[
 #pragma unroll
       for (int dt = 0; dt < D / 32; ++dt)
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int col = 32 * dt + acc_row(i, lane);
-          acc[dt][i] = __builtin_fmaf(p, hdet_ld(tile + row * D + (((col / S::E) ^ S::swz(row)) * S::E) + col % S::E), acc[dt][i]);
+        for (int i = 0; i < 4; ++i) {
+          const int col = 32 * dt + acc_row(4 * i, lane);
+          const hdet_f4 v = hdet_ld4(tile + row * D + (((col / S::E) ^ S::swz(row)) * S::E) + col % S::E);
+#pragma unroll
+          for (int u = 0; u < 4; ++u) acc[dt][4 * i + u] = __builtin_fmaf(p, v.v[u], acc[dt][4 * i + u]);
+          asm volatile("" ::: "memory");   // no more of the tile in registers than these
         }
     }
   }

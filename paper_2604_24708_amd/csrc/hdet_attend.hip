@@ -8,8 +8,9 @@
 // In units of log2 throughout: p = 2^(z log2 e - m), one fma and one exponential a score.
 //
 // A pair that is not attended must leave no trace, but 0 times an infinity or a NaN does: the matrix cores multiply all of a block that lies across the
-// ranges.  Results that came out finite are right; where one did not, the block walks its tiles a second time and leaves out the pairs of such blocks one
-// by one (second_exact).  That costs nothing where numbers are finite, and at most the same time again and a few thousand cycles a block across.
+// ranges.  Results that came out finite are right; where one did not, the block walks its tiles a second time with zeros for what is not finite in
+// the second product's tiles.  What of that is attended comes back by itself where it has made scores, statistics or row dots what they are; the values'
+// and the output gradients' own entries, which have not, are added to the results of the rows that attend them (add_not_finite).
 
 #include <limits.h>
 #include <math.h>
@@ -44,9 +45,14 @@ struct attend_args {
   int n, seqs, q_len, kv_len, heads, kv_heads, group, d, causal, window;
   int splits;
   float scale, c, cap2, inv_cap;           // c = scale log2 e; cap2 = cap log2 e or 0
+  bool close;                              // capped scores to fp32's last places, not to 1e-7 of the cap
   unsigned total;                          // blocks
   bool heavy_first;
 };
+
+// Stages of two tiles (keys and values, or queries and output gradients) in LDS: one that is worked on, the other on its way.  (A third one: forward 167 -> 193 us
+// at 8 x 16 sequences of 512, 16 heads of 64, for the blocks that the LDS then holds; without it lost, the same.)
+constexpr int STAGES = 2;
 
 struct key_range { int lo, hi, pos; };
 
@@ -90,47 +96,122 @@ __device__ __forceinline__ block_id place_block(unsigned lin, unsigned total, un
   return b;
 }
 
-// Least and largest over the 32 rows of a wavefront
+// Least over the 32 rows of a wavefront
 __device__ __forceinline__ int wave_min(int x) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) x = min(x, __shfl_xor(x, o));
-  return __builtin_amdgcn_readfirstlane(x);
+  x = min(x, __builtin_amdgcn_update_dpp(0, x, 0xB1, 0xf, 0xf, false));
+  x = min(x, __builtin_amdgcn_update_dpp(0, x, 0x4E, 0xf, 0xf, false));
+  x = min(x, __builtin_amdgcn_update_dpp(0, x, 0x141, 0xf, 0xf, false));
+  x = min(x, __builtin_amdgcn_update_dpp(0, x, 0x140, 0xf, 0xf, false));
+  return min(__builtin_amdgcn_readlane(x, 0), __builtin_amdgcn_readlane(x, 16));
 }
-__device__ __forceinline__ int wave_max(int x) {
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) x = max(x, __shfl_xor(x, o));
-  return __builtin_amdgcn_readfirstlane(x);
-}
-// The ranges of 32 queries: any keys outside lo_min .. hi_max - 1 are outside for all, keys of lo_max .. hi_min - 1 inside for all
+// The ranges of 32 queries: keys outside lo_min .. hi_max - 1 are outside for all, keys of lo_max .. hi_min - 1 inside for all
 struct wave_range { int lo_min, lo_max, hi_min, hi_max; };
 // `there`: the lane's row exists
 __device__ __forceinline__ wave_range wave_range_of(const key_range& k, bool there) {
   const bool some = there && k.hi > k.lo;
   wave_range w;
   w.lo_min = wave_min(some ? k.lo : INT_MAX);
-  w.hi_max = wave_max(some ? k.hi : 0);
-  w.lo_max = wave_max(some ? k.lo : there ? INT_MAX : 0);
+  w.hi_max = -wave_min(some ? -k.hi : 0);
+  w.lo_max = -wave_min(some ? -k.lo : there ? -INT_MAX : 0);
   w.hi_min = wave_min(some ? k.hi : there ? 0 : INT_MAX);
+  if (w.hi_max == 0) w.lo_max = INT_MAX;   // no keys at all are inside of no queries at all
   return w;
 }
+// Without arrays both ends of a range rise with the row: the same of rows i0 .. i0 + count - 1 of a sequence from the first and the last of them
+__device__ __forceinline__ wave_range plain_range_of(const attend_args& g, int i0, int count) {
+  if (i0 + count > g.q_len) count = g.q_len - i0;
+  if (count <= 0) return {INT_MAX, INT_MAX, 0, 0};
+  const key_range a = range_of(g, 0, 0, i0), b = range_of(g, 0, 0, i0 + count - 1);
+  if (b.hi <= b.lo) return {INT_MAX, INT_MAX, 0, 0};                       // queries before the first key: the last one has most
+  if (a.hi <= a.lo) return {0, INT_MAX, 0, b.hi};
+  return {a.lo, b.lo, a.hi, b.hi};
+}
+// ... of a wavefront's 32 queries, the lanes' ranges given, and (lo, hi) of the block's 128, through LDS that nothing else uses before the next barrier but one
+struct block_range { wave_range own; int lo, hi; };
+__device__ __forceinline__ block_range block_range_of(const attend_args& g, const key_range& k, bool there, int q0, int w, int lane, int* ends) {
+  block_range b;
+  if (!g.pos && !g.first && !g.end) {
+    b.own = plain_range_of(g, q0 + w * WR, WR);
+    const wave_range all = plain_range_of(g, q0, RB);
+    b.lo = all.lo_min;
+    b.hi = all.hi_max;
+  } else {
+    b.own = wave_range_of(k, there);
+    if (lane == 0) {
+      ends[w] = b.own.lo_min;
+      ends[NWV + w] = b.own.hi_max;
+    }
+    __syncthreads();
+    b.lo = __builtin_amdgcn_readfirstlane(min(min(ends[0], ends[1]), min(ends[2], ends[3])));
+    b.hi = __builtin_amdgcn_readfirstlane(max(max(ends[4], ends[5]), max(ends[6], ends[7])));
+  }
+  return b;
+}
 
-// Scores of a block from its raw products, [key or query][..], in units of log2; bend: the cap's derivative.  dist(e): |position - key| of element e.
-template <bool BEND, typename F>
-__device__ __forceinline__ void shape_scores(const attend_args& g, f16v& x, f16v& bend, float slope2, F dist) {
-  if (g.cap2 > 0.f) {
+// Whether any thread of the block says so; two barriers, and 16 bytes of LDS at `lds` that nothing else uses
+__device__ __forceinline__ bool block_any(bool yes, int w, int lane, int* lds) {
+  const int any = __any(yes);
+  __syncthreads();
+  if (lane == 0) lds[w] = any;
+  __syncthreads();
+  return lds[0] | lds[1] | lds[2] | lds[3];
+}
+
+// Scores of a block from its raw products: x such that the score is (x + shift) mult log2 units (score_units).  With a cap x is tanh - 1, exact enough unless
+// small scores are read off a very large cap (close).  dist(e): |position - key| of element e.
+struct score_units { float mult, shift; };
+__device__ __forceinline__ score_units units_of(const attend_args& g, bool extra) {
+  return !extra ? score_units{g.c, 0.f} : g.slopes || g.cap2 == 0.f ? score_units{1.f, 0.f} : score_units{g.cap2, g.close ? 0.f : 1.f};
+}
+template <typename F> __device__ __forceinline__ void shape_scores(const attend_args& g, f16v& x, float slope2, F dist) {
+  if (g.cap2 > 0.f && !g.close) {
+    const float s = 2.f * kLog2e * g.scale * g.inv_cap;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = tanh_less_1(x[e] * s);
+    if (g.slopes) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[e] = __builtin_fmaf(x[e], g.cap2, g.cap2);
+    }
+  } else if (g.cap2 > 0.f) {
     const float s = g.scale * g.inv_cap;
 #pragma unroll
-    for (int e = 0; e < 16; ++e) {
-      const float t = tanh_fast(x[e] * s);
-      x[e] = t * g.cap2;
-      if (BEND) bend[e] = __builtin_fmaf(-t, t, 1.f);
+    for (int e = 0; e < 16; ++e) x[e] = tanh_close(x[e] * s);
+    if (g.slopes) {
+#pragma unroll
+      for (int e = 0; e < 16; ++e) x[e] *= g.cap2;
     }
   } else {
 #pragma unroll
     for (int e = 0; e < 16; ++e) x[e] *= g.c;
-    if (BEND) bend = all16(1.f);
   }
-  if (slope2 != 0.f) {
+  if (g.slopes) {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = __builtin_fmaf(-slope2, dist(e), x[e]);
+  }
+}
+// Backward: scores, in log2 units, from raw products, and dp times the cap's derivative
+template <typename F> __device__ __forceinline__ void shape_scores_back(const attend_args& g, f16v& x, f16v& dp, float slope2, F dist) {
+  if (g.cap2 > 0.f && !g.close) {
+    const float s = 2.f * kLog2e * g.scale * g.inv_cap;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float t = tanh_less_1(x[e] * s);
+      dp[e] *= -t * (t + 2.f);
+      x[e] = __builtin_fmaf(t, g.cap2, g.cap2);
+    }
+  } else if (g.cap2 > 0.f) {
+    const float s = g.scale * g.inv_cap;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) {
+      const float t = tanh_close(x[e] * s);
+      dp[e] *= __builtin_fmaf(-t, t, 1.f);
+      x[e] = t * g.cap2;
+    }
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] *= g.c;
+  }
+  if (g.slopes) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) x[e] = __builtin_fmaf(-slope2, dist(e), x[e]);
   }
@@ -155,7 +236,7 @@ template <int D> struct running {
 #pragma unroll
     for (int b = 0; b < NB; ++b)
 #pragma unroll
-      for (int e = 0; e < 16; ++e) top = fmaxf(top, x[b][e]);
+      for (int e = 0; e < 16; e += 2) top = max3(top, x[b][e], x[b][e + 1]);
     top = fmaxf(top, other_half(top)) * c;
     if (__any(top > m + 8.f)) {
       const float next = fmaxf(m, top), keep = exp2_fast(m - (next == -INFINITY ? 0.f : next));
@@ -183,9 +264,8 @@ template <int D> struct running {
 template <typename T, int D> constexpr int forward_waves() { return sizeof(T) == 2 ? (D == 64 ? 3 : 2) : (D == 64 ? 2 : 1); }
 template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds__(THREADS, (forward_waves<T, D>())) void attend_kernel(const attend_args g) {
   typedef shape<T, D> S;
-  constexpr int TILE = S::TB * D, NB = S::TB / 32;
-  __shared__ __attribute__((aligned(1024))) T smem[4 * TILE];              // two stages of keys and values
-  __shared__ int ends[2 * NWV];
+  constexpr int TILE = S::TB * D, NB = S::TB / 32, LOADS = 2 * tile_loader<T, D, S::TB, NWV, WHOLE>::NI;
+  __shared__ __attribute__((aligned(1024))) T smem[2 * STAGES * TILE];     // keys and values
   const unsigned lin = blockIdx.y * gridDim.x + blockIdx.x;
   if (lin >= g.total) return;
   const unsigned nx = (g.q_len + RB - 1) / RB;
@@ -195,11 +275,6 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
   const int wq0 = (int)(nx - 1 - blk.x) * RB + w * WR, qi = wq0 + (lane & 31);
   const bool there = qi < g.q_len;
   const key_range range = there ? range_of(g, r, b, qi) : key_range{0, 0, 0};
-  const wave_range wr = wave_range_of(range, there);
-  if (lane == 0) {
-    ends[w] = wr.lo_min;
-    ends[NWV + w] = wr.hi_max;
-  }
   const int64_t col = (int64_t)h * g.d, kcol = (int64_t)(h / g.group) * g.d, row0 = (int64_t)b * g.q_len + wq0;
   const T* const own = there ? (const T*)g.q + r * g.q_z + (row0 + (lane & 31)) * g.q_s + col : nullptr;
   typename S::frag fq[S::NF];
@@ -208,73 +283,75 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
   const tile_loader<T, D, S::TB, NWV, WHOLE> keys((const T*)g.k + r * g.k_z + (int64_t)b * g.kv_len * g.k_s + kcol, g.k_s, g.d, w, lane);
   const tile_loader<T, D, S::TB, NWV, WHOLE> vals((const T*)g.v + r * g.v_z + (int64_t)b * g.kv_len * g.v_s + kcol, g.v_s, g.d, w, lane);
   const S at(lane);
-  const float slope2 = EXTRA && g.slopes ? g.slopes[r * g.slopes_z + h] * kLog2e : 0.f, c = EXTRA ? 1.f : g.c;
-  __syncthreads();
-  const int lo = __builtin_amdgcn_readfirstlane(min(min(ends[0], ends[1]), min(ends[2], ends[3])));
-  const int hi = __builtin_amdgcn_readfirstlane(max(max(ends[4], ends[5]), max(ends[6], ends[7])));
-  const int t0 = lo / S::TB, t1 = (hi + S::TB - 1) / S::TB;                // hi = 0: none
+  const float slope2 = EXTRA && g.slopes ? g.slopes[r * g.slopes_z + h] * kLog2e : 0.f;
+  const score_units unit = units_of(g, EXTRA);
+  // (the block's ends pass through the second stage, which is requested behind a barrier)
+  const block_range br = block_range_of(g, range, there, wq0 - w * WR, w, lane, (int*)(smem + 2 * TILE));
+  const wave_range wr = br.own;
+  const int hi = br.hi, t0 = br.lo / S::TB, t1 = (hi + S::TB - 1) / S::TB; // hi = 0: none
 
   running<D> z;
-  auto request = [&](int t) {
-    if (t >= t1) return;
-    T* const to = smem + (t & 1) * (2 * TILE);
-    keys.load((int64_t)t * S::TB, hi - t * S::TB, to);
-    vals.load((int64_t)t * S::TB, hi - t * S::TB, to + TILE);
+  // (every request is as many loads, of zeros behind the last tile, so that a wait can count them)
+  auto request = [&](int t, int slot) {
+    T* const to = smem + slot * (2 * TILE);
+    keys.load((int64_t)t * S::TB, t < t1 ? hi - t * S::TB : 0, to);
+    vals.load((int64_t)t * S::TB, t < t1 ? hi - t * S::TB : 0, to + TILE);
   };
-  auto walk = [&](auto exact) {            // (a body of its own for the second time: the first one keeps its registers)
+  auto walk = [&](auto clean) {
     z.reset();
-    if (hi > 0) request(t0);
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) request(t0 + i, i);
+    int slot = 0, free = STAGES - 1;
     for (int t = t0; t < t1; ++t) {
-      wait_and_barrier<0>();
-      request(t + 1);
-      const T* const kt = smem + (t & 1) * (2 * TILE);
-      const T* const vt = kt + TILE;
+      wait_and_barrier<(STAGES - 2) * LOADS>();
+      request(t + STAGES - 1, free);
+      T* const tiles = smem + slot * (2 * TILE);
+      free = slot;
+      slot = slot == STAGES - 1 ? 0 : slot + 1;
+      const T* const kt = tiles;
+      T* const vt = tiles + TILE;
+      if (decltype(clean)::value) {
+        clean_tile<T, D, S::TB>(vt, tid, THREADS);
+        __syncthreads();
+      }
       const int key0 = t * S::TB;
-      // one block of 32 keys, its pairs tested
-      auto across = [&](int i) {
-        f16v x[1], bend;
-        x[0] = at.first(kt + i * 32 * D, fq, all16(0.f));
-        const int k0 = key0 + 32 * i + ((lane >> 5) << 2);
-        if (EXTRA) shape_scores<false>(g, x[0], bend, slope2, [&](int e) { return distance(range.pos, k0 + acc_row(e, 0)); });
-        const unsigned from = k0 - range.lo, len = range.hi - range.lo;
-#pragma unroll
-        for (int e = 0; e < 16; ++e) x[0][e] = from + acc_row(e, 0) < len ? x[0][e] : -INFINITY;
-        z.take(x, c);
-        if (!decltype(exact)::value) at.second(vt + i * 32 * D, x[0], z.o);
-        else second_exact<T, D>(vt + i * 32 * D, x[0], z.o, lane, [&](int row) { return (unsigned)(key0 + 32 * i + row - range.lo) < len; });
-      };
-      if (key0 >= wr.lo_max && key0 + S::TB <= wr.hi_min) {
-        f16v x[NB], bend;
-#pragma unroll
-        for (int i = 0; i < NB; ++i) {
-          x[i] = at.first(kt + i * 32 * D, fq, all16(0.f));
-          const int k0 = key0 + 32 * i + ((lane >> 5) << 2);
-          if (EXTRA) shape_scores<false>(g, x[i], bend, slope2, [&](int e) { return distance(range.pos, k0 + acc_row(e, 0)); });
-        }
-        z.take(x, c);
-#pragma unroll
-        for (int i = 0; i < NB; ++i) at.second(vt + i * 32 * D, x[i], z.o);
-      } else {
 #pragma unroll 1
-        for (int i = 0; i < NB; ++i)
-          if (key0 + 32 * i < wr.hi_max && key0 + 32 * i + 32 > wr.lo_min) across(i);
+      for (int i = 0; i < NB; ++i) {
+        const int kb = key0 + 32 * i;
+        if (kb >= wr.hi_max || kb + 32 <= wr.lo_min) continue;
+        f16v x[1];
+        x[0] = at.first(kt + i * 32 * D, fq, all16(0.f));
+        const int k0 = kb + ((lane >> 5) << 2);
+        if (EXTRA) shape_scores(g, x[0], slope2, [&](int e) { return distance(range.pos, k0 + acc_row(e, 0)); });
+        const bool inside = kb >= wr.lo_max && kb + 32 <= wr.hi_min;
+        const unsigned from = k0 - range.lo, len = range.hi - range.lo;
+        if (!inside) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) x[0][e] = from + acc_row(e, 0) < len ? x[0][e] : -INFINITY;
+        }
+        z.take(x, unit.mult);
+        at.second(vt + i * 32 * D, x[0], z.o);
       }
     }
+    wait_and_barrier<0>();
     z.l += other_half(z.l);
   };
   walk(std::false_type());
-  if (__syncthreads_or(there && fabsf(z.l) < INFINITY && not_finite(z.o))) {
-    walk(std::true_type());
-    __syncthreads();
-  }
+  const bool again = block_any(there && finite_of(z.l) && not_finite(z.o), w, lane, (int*)(smem + 2 * STAGES * TILE) - NWV);
+  if (again) walk(std::true_type());
   const bool some = range.hi > range.lo;
   const float inv = some ? 1.f / z.l : 0.f;
 #pragma unroll
   for (int i = 0; i < S::ND; ++i)
 #pragma unroll
     for (int e = 0; e < 16; ++e) z.o[i][e] = some ? z.o[i][e] * inv : 0.f;
-  if (g.lse && there && lane < 32) g.lse[((int64_t)r * g.heads + h) * g.seqs * g.q_len + row0 + lane] = some ? (z.ref() + log2f(z.l)) * kLn2 : -INFINITY;
+  if (g.lse && there && lane < 32) g.lse[((int64_t)r * g.heads + h) * g.seqs * g.q_len + row0 + lane] = some ? (z.ref() + unit.mult * unit.shift + log2f(z.l)) * kLn2 : -INFINITY;
   store_rows<T, D, WHOLE>(z.o, (char*)smem + w * STRIP, (T*)g.out + r * g.out_z + row0 * g.out_s + col, g.out_s, g.q_len - wq0, g.d, lane);
+  if (again) {
+    __threadfence_block();
+    add_not_finite<T, D>(vals.src, g.v_s, g.d, wr.lo_min, wr.hi_max, (T*)g.out + r * g.out_z + row0 * g.out_s + col, g.out_s, min(WR, g.q_len - wq0), lane,
+                         [&](int key, int i) { return key >= __builtin_amdgcn_readlane(range.lo, i) && key < __builtin_amdgcn_readlane(range.hi, i); });
+  }
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -307,7 +384,8 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
   const tile_loader<T, D, 32, 1, WHOLE> vals((const T*)g.v + r * g.v_z + (int64_t)b * g.kv_len * g.v_s + kcol, g.v_s, g.d, 0, lane);
   constexpr int IN_FLIGHT = 2 * tile_loader<T, D, 32, 1, WHOLE>::NI;
   const S at(lane);
-  const float slope2 = EXTRA && g.slopes ? g.slopes[r * g.slopes_z + h] * kLog2e : 0.f, c = EXTRA ? 1.f : g.c;
+  const float slope2 = EXTRA && g.slopes ? g.slopes[r * g.slopes_z + h] * kLog2e : 0.f;
+  const score_units unit = units_of(g, EXTRA);
   // the union of the ranges in tiles, this block's part of them
   const int hi = wr.hi_max, lo = hi > 0 ? wr.lo_min : 0, t0 = lo / 32, t1 = (hi + 31) / 32, per = (t1 - t0 + g.splits - 1) / g.splits;
   const int ts = t0 + split * per, te = min(t1, ts + per);
@@ -319,7 +397,7 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
     keys.load((int64_t)t * 32, have, mine + stage * (2 * TILE));
     vals.load((int64_t)t * 32, have, mine + stage * (2 * TILE) + TILE);
   };
-  auto walk = [&](auto exact) {
+  auto walk = [&](auto clean) {
     z.reset();
     int stage = 0;
     if (ts + w < te) request(ts + w, 0);
@@ -327,26 +405,30 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
       wave_fence();                        // the other stage's tiles have been read
       request(t + NW, stage ^ 1);
       asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(IN_FLIGHT) : "memory");
-      const T* const kt = mine + stage * (2 * TILE);
-      f16v x[1], bend;
+      T* const kt = mine + stage * (2 * TILE);
+      if (decltype(clean)::value) {
+        clean_tile<T, D, 32>(kt + TILE, lane, 64);
+        wave_fence();
+      }
+      f16v x[1];
       x[0] = at.first(kt, fq, all16(0.f));
       const int k0 = t * 32 + ((lane >> 5) << 2);
-      if (EXTRA) shape_scores<false>(g, x[0], bend, slope2, [&](int e) { return distance(range.pos, k0 + acc_row(e, 0)); });
+      if (EXTRA) shape_scores(g, x[0], slope2, [&](int e) { return distance(range.pos, k0 + acc_row(e, 0)); });
       const unsigned from = k0 - range.lo, len = range.hi - range.lo;
       const bool inside = t * 32 >= wr.lo_max && t * 32 + 32 <= wr.hi_min;
       if (!inside) {
 #pragma unroll
         for (int e = 0; e < 16; ++e) x[0][e] = from + acc_row(e, 0) < len ? x[0][e] : -INFINITY;
       }
-      z.take(x, c);
-      if (!decltype(exact)::value || inside) at.second(kt + TILE, x[0], z.o);
-      else second_exact<T, D>(kt + TILE, x[0], z.o, lane, [&](int i) { return (unsigned)(t * 32 + i - range.lo) < len; });
+      z.take(x, unit.mult);
+      at.second(kt + TILE, x[0], z.o);
     }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     z.l += other_half(z.l);
   };
   walk(std::false_type());
-  if (__any(there && fabsf(z.l) < INFINITY && not_finite(z.o))) walk(std::true_type());
+  const bool again = __any(there && finite_of(z.l) && not_finite(z.o));
+  if (again) walk(std::true_type());
 
   // join the wavefronts
   float* const joint = (float*)smem;       // [wave][32][P], then [wave][32] references and sums
@@ -357,6 +439,12 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
 #pragma unroll
     for (int e4 = 0; e4 < 4; ++e4)
       *reinterpret_cast<f4v*>(joint + (w * 32 + (lane & 31)) * P + 32 * i + acc_row(4 * e4, lane)) = f4v{z.o[i][4 * e4], z.o[i][4 * e4 + 1], z.o[i][4 * e4 + 2], z.o[i][4 * e4 + 3]};
+  if (again) {
+    wave_fence();
+    for (int t = ts + w; t < te; t += NW)
+      add_not_finite<T, D>(vals.src, g.v_s, g.d, t * 32, min(t * 32 + 32, hi), joint + w * 32 * P, P, 32, lane,
+                           [&](int key, int i) { return key >= __builtin_amdgcn_readlane(range.lo, i) && key < __builtin_amdgcn_readlane(range.hi, i); });
+  }
   if (lane < 32) {
     stats[w * 64 + lane] = z.m;
     stats[w * 64 + 32 + lane] = z.l;
@@ -382,7 +470,7 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
     if (g.splits > 1) {
       float* const to = g.part + ((int64_t)lin * 32 + c_) * (D + 2);
       if (col == 0) {
-        to[0] = m;
+        to[0] = m + unit.mult * unit.shift;
         to[1] = l;
       }
 #pragma unroll
@@ -398,7 +486,7 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       if (col + e < g.d) hdet_st(to + e, some ? o[e] * inv : 0.f);
-    if (g.lse && col == 0) g.lse[((int64_t)r * g.heads + oh) * g.seqs * g.q_len + orow] = some ? (ref + log2f(l)) * kLn2 : -INFINITY;
+    if (g.lse && col == 0) g.lse[((int64_t)r * g.heads + oh) * g.seqs * g.q_len + orow] = some ? (ref + unit.mult * unit.shift + log2f(l)) * kLn2 : -INFINITY;
   }
 }
 
@@ -439,9 +527,8 @@ template <typename T, int D> __global__ __launch_bounds__(THREADS) void attend_j
 // ---------------------------------------------------------------------------------------------
 template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds__(THREADS, (sizeof(T) == 4 && D == 128 ? 1 : 2)) void attend_dq_kernel(const attend_args g) {
   typedef shape<T, D> S;
-  constexpr int TILE = S::TB * D, NB = S::TB / 32;
-  __shared__ __attribute__((aligned(1024))) T smem[4 * TILE];              // two stages of keys and values
-  __shared__ int ends[2 * NWV];
+  constexpr int TILE = S::TB * D, NB = S::TB / 32, LOADS = 2 * tile_loader<T, D, S::TB, NWV, WHOLE>::NI;
+  __shared__ __attribute__((aligned(1024))) T smem[2 * STAGES * TILE];     // keys and values
   const unsigned lin = blockIdx.y * gridDim.x + blockIdx.x;
   if (lin >= g.total) return;
   const unsigned nx = (g.q_len + RB - 1) / RB;
@@ -451,11 +538,8 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
   const int wq0 = (int)(nx - 1 - blk.x) * RB + w * WR, qi = wq0 + (lane & 31);
   const bool there = qi < g.q_len;
   const key_range range = there ? range_of(g, r, b, qi) : key_range{0, 0, 0};
-  const wave_range wr = wave_range_of(range, there);
-  if (lane == 0) {
-    ends[w] = wr.lo_min;
-    ends[NWV + w] = wr.hi_max;
-  }
+  const block_range br = block_range_of(g, range, there, wq0 - w * WR, w, lane, (int*)(smem + 2 * TILE));
+  const wave_range wr = br.own;
   const int64_t rows = (int64_t)g.seqs * g.q_len, row0 = (int64_t)b * g.q_len + wq0, row = row0 + (lane & 31);
   const int64_t col = (int64_t)h * g.d, kcol = (int64_t)(h / g.group) * g.d, stat = ((int64_t)r * g.heads + h) * rows + row;
   const bool some = range.hi > range.lo;
@@ -489,55 +573,56 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
   const tile_loader<T, D, S::TB, NWV, WHOLE> keys((const T*)g.k + r * g.k_z + (int64_t)b * g.kv_len * g.k_s + kcol, g.k_s, g.d, w, lane);
   const tile_loader<T, D, S::TB, NWV, WHOLE> vals((const T*)g.v + r * g.v_z + (int64_t)b * g.kv_len * g.v_s + kcol, g.v_s, g.d, w, lane);
   const S at(lane);
-  const float slope2 = EXTRA && g.slopes ? g.slopes[r * g.slopes_z + h] * kLog2e : 0.f, c = EXTRA ? 1.f : g.c;
-  __syncthreads();
-  const int lo = __builtin_amdgcn_readfirstlane(min(min(ends[0], ends[1]), min(ends[2], ends[3])));
-  const int hi = __builtin_amdgcn_readfirstlane(max(max(ends[4], ends[5]), max(ends[6], ends[7])));
-  const int t0 = lo / S::TB, t1 = (hi + S::TB - 1) / S::TB;
+  const float slope2 = EXTRA && g.slopes ? g.slopes[r * g.slopes_z + h] * kLog2e : 0.f;
+  const float c = EXTRA ? 1.f : g.c;
+  const int hi = br.hi, t0 = br.lo / S::TB, t1 = (hi + S::TB - 1) / S::TB;
 
   f16v dq[S::ND];                          // [column][query]
-  auto request = [&](int t) {
-    if (t >= t1) return;
-    T* const to = smem + (t & 1) * (2 * TILE);
-    keys.load((int64_t)t * S::TB, hi - t * S::TB, to);
-    vals.load((int64_t)t * S::TB, hi - t * S::TB, to + TILE);
+  // (every request is as many loads, of zeros behind the last tile, so that a wait can count them)
+  auto request = [&](int t, int slot) {
+    T* const to = smem + slot * (2 * TILE);
+    keys.load((int64_t)t * S::TB, t < t1 ? hi - t * S::TB : 0, to);
+    vals.load((int64_t)t * S::TB, t < t1 ? hi - t * S::TB : 0, to + TILE);
   };
-  auto walk = [&](auto exact) {
+  auto walk = [&](auto clean) {
 #pragma unroll
     for (int i = 0; i < S::ND; ++i) dq[i] = all16(0.f);
-    if (hi > 0) request(t0);
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) request(t0 + i, i);
+    int slot = 0, free = STAGES - 1;
     for (int t = t0; t < t1; ++t) {
-      wait_and_barrier<0>();
-      request(t + 1);
+      wait_and_barrier<(STAGES - 2) * LOADS>();
+      request(t + STAGES - 1, free);
+      T* const tiles = smem + slot * (2 * TILE);
+      free = slot;
+      slot = slot == STAGES - 1 ? 0 : slot + 1;
+      if (decltype(clean)::value) {
+        clean_tile<T, D, S::TB>(tiles, tid, THREADS);
+        __syncthreads();
+      }
 #pragma unroll 1
       for (int i = 0; i < NB; ++i) {
         const int key0 = t * S::TB + 32 * i;
         if (key0 >= wr.hi_max || key0 + 32 <= wr.lo_min) continue;
-        const T* const kt = smem + (t & 1) * (2 * TILE) + i * 32 * D;
-        f16v x = at.first(kt, fq, all16(0.f)), dp = at.first(kt + TILE, fdo, all16(ndot)), bend;
+        const T* const kt = tiles + i * 32 * D;
+        f16v x = at.first(kt, fq, all16(0.f)), dp = at.first(kt + TILE, fdo, all16(ndot));
         const int k0 = key0 + ((lane >> 5) << 2);
-        if (EXTRA) shape_scores<true>(g, x, bend, slope2, [&](int e) { return distance(range.pos, k0 + acc_row(e, 0)); });
+        if (EXTRA) shape_scores_back(g, x, dp, slope2, [&](int e) { return distance(range.pos, k0 + acc_row(e, 0)); });
 #pragma unroll
-        for (int e = 0; e < 16; ++e) {
-          dp[e] *= exp2_fast(__builtin_fmaf(x[e], c, -lse2));
-          if (EXTRA) dp[e] *= bend[e];
-        }
+        for (int e = 0; e < 16; ++e) dp[e] *= exp2_fast(__builtin_fmaf(x[e], c, -lse2));
         const bool inside = key0 >= wr.lo_max && key0 + 32 <= wr.hi_min;
         const unsigned from = k0 - range.lo, len = range.hi - range.lo;
         if (!inside) {
 #pragma unroll
           for (int e = 0; e < 16; ++e) dp[e] = from + acc_row(e, 0) < len ? dp[e] : 0.f;
         }
-        if (!decltype(exact)::value || inside) at.second(kt, dp, dq);
-        else second_exact<T, D>(kt, dp, dq, lane, [&](int k) { return (unsigned)(key0 + k - range.lo) < len; });
+        at.second(kt, dp, dq);
       }
     }
+    wait_and_barrier<0>();
   };
   walk(std::false_type());
-  if (__syncthreads_or(some && fabsf(lse2) < INFINITY && not_finite(dq))) {
-    walk(std::true_type());
-    __syncthreads();
-  }
+  if (block_any(some && finite_of(lse2) && not_finite(dq), w, lane, (int*)(smem + 2 * STAGES * TILE) - NWV)) walk(std::true_type());
 #pragma unroll
   for (int i = 0; i < S::ND; ++i)
 #pragma unroll
@@ -548,39 +633,50 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
 // ---------------------------------------------------------------------------------------------
 // backward, step 2: dk and dv; block = 128 keys of a key head, walks over the query tiles of the heads that share it
 // ---------------------------------------------------------------------------------------------
-template <typename T, int D> constexpr int dkv_waves() { return D == 128 ? 1 : 2; }
-template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds__(THREADS, (dkv_waves<T, D>())) void attend_dkv_kernel(const attend_args g) {
+template <typename T, int D, bool EXTRA> constexpr int dkv_waves() { return D == 128 ? 1 : sizeof(T) == 2 && !EXTRA ? 3 : 2; }
+template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds__(THREADS, (dkv_waves<T, D, EXTRA>())) void attend_dkv_kernel(const attend_args g) {
   typedef shape<T, D> S;
   constexpr int TILE = S::TB * D, NB = S::TB / 32, STATS = 5 * S::TB;      // lse2, dot, lo, hi, position
-  __shared__ __attribute__((aligned(1024))) T smem[4 * TILE];              // two stages of queries and output gradients
-  __shared__ __attribute__((aligned(16))) int stats[2 * STATS];
+  constexpr int LOADS = 2 * tile_loader<T, D, S::TB, NWV, WHOLE>::NI + 2;
+  __shared__ __attribute__((aligned(1024))) T smem[2 * STAGES * TILE];     // queries and output gradients
+  __shared__ __attribute__((aligned(16))) int stats[STAGES * STATS];
   __shared__ int ends[2 * NWV];
-  const unsigned lin = blockIdx.y * gridDim.x + blockIdx.x;
+  unsigned lin = blockIdx.y * gridDim.x + blockIdx.x;
   if (lin >= g.total) return;
-  const unsigned nx = (g.kv_len + RB - 1) / RB;
-  const block_id blk = place_block(lin, g.total, nx, g.heavy_first);
+  const unsigned nx = (g.kv_len + RB - 1) / RB, split = g.splits > 1 ? lin % g.splits : 0;
+  if (g.splits > 1) lin /= g.splits;
+  const block_id blk = place_block(lin, g.total / g.splits, nx, g.heavy_first);
   const int kh = blk.grp % g.kv_heads, b = blk.grp / g.kv_heads % g.seqs, r = blk.grp / g.kv_heads / g.seqs;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int k0 = blk.x * RB, wk0 = k0 + w * WR, key = wk0 + (lane & 31);
   const int n_groups = (g.q_len + 31) / 32;
   const i4v* const groups = g.groups + ((int64_t)r * g.seqs + b) * n_groups;
-  // first and last tile of queries that attend any of the block's keys
+  // first and last group of queries that attend any of the block's keys
+  const bool plain = !g.pos && !g.first && !g.end;
   int first = INT_MAX, last = -1;
-  for (int i = tid; i < n_groups; i += THREADS) {
-    const i4v x = groups[i];
-    if (x[0] < k0 + RB && x[3] > k0) {
-      first = min(first, i);
-      last = i;
+  if (plain) {
+    const int64_t off = (int64_t)g.kv_len - g.q_len, from = g.causal ? k0 - off : 0, to = g.window ? (int64_t)k0 + RB + g.window - 2 - off : INT_MAX;
+    if (from < g.q_len && to >= 0) {
+      first = (int)(from > 0 ? from : 0) / 32;
+      last = (int)(to < g.q_len ? to : g.q_len - 1) / 32;
     }
-  }
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    first = min(first, __shfl_xor(first, o));
-    last = max(last, __shfl_xor(last, o));
-  }
-  if (lane == 0) {
-    ends[w] = first;
-    ends[NWV + w] = last;
+  } else {
+    for (int i = tid; i < n_groups; i += THREADS) {
+      const i4v x = groups[i];
+      if (x[0] < k0 + RB && x[3] > k0) {
+        first = min(first, i);
+        last = i;
+      }
+    }
+    first = min(wave_min(first), wave_min(__shfl_xor(first, 32)));
+    last = -min(wave_min(-last), wave_min(-__shfl_xor(last, 32)));
+    if (lane == 0) {
+      ends[w] = first;
+      ends[NWV + w] = last;
+    }
+    __syncthreads();
+    first = __builtin_amdgcn_readfirstlane(min(min(ends[0], ends[1]), min(ends[2], ends[3])));
+    last = __builtin_amdgcn_readfirstlane(max(max(ends[4], ends[5]), max(ends[6], ends[7])));
   }
   const bool there = key < g.kv_len;
   const int64_t kcol = (int64_t)kh * g.d, row0 = (int64_t)b * g.kv_len + wk0, rows = (int64_t)g.seqs * g.q_len, q_row0 = (int64_t)b * g.q_len;
@@ -594,50 +690,65 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
   }
   const S at(lane);
   const float c = EXTRA ? 1.f : g.c;
-  __syncthreads();
-  first = __builtin_amdgcn_readfirstlane(min(min(ends[0], ends[1]), min(ends[2], ends[3])));
-  last = __builtin_amdgcn_readfirstlane(max(max(ends[4], ends[5]), max(ends[6], ends[7])));
   const int t0 = last < 0 ? 0 : first / NB, tiles = last < 0 ? 0 : last / NB + 1 - t0;
 
   tile_loader<T, D, S::TB, NWV, WHOLE> qs((const T*)g.q + r * g.q_z + q_row0 * g.q_s, g.q_s, g.d, w, lane);
   tile_loader<T, D, S::TB, NWV, WHOLE> dos((const T*)g.dout + r * g.do_z + q_row0 * g.do_s, g.do_s, g.d, w, lane);
   const T *const q_at = qs.src, *const do_at = dos.src;
   f16v dk[S::ND], dv[S::ND];               // [column][key]
-  auto request = [&](int j) {              // tile j of all heads' tiles
-    if (j >= tiles * g.group) return;
-    const int h = kh * g.group + j / tiles, t = t0 + j % tiles, q0 = t * S::TB, have = min(g.q_len - q0, S::TB);
+  // this block's part of all heads' tiles
+  const int share = (tiles * g.group + g.splits - 1) / g.splits, begin = split * share, all = min(tiles * g.group, begin + share);
+  auto request = [&](int j, int slot) {    // tile j of all heads' tiles
+    const int h = kh * g.group + (tiles ? j / tiles : 0), t = t0 + (tiles ? j % tiles : 0), q0 = t * S::TB, have = j < all ? min(g.q_len - q0, S::TB) : 0;
     qs.src = q_at + (int64_t)h * g.d;
     dos.src = do_at + (int64_t)h * g.d;
-    T* const to = smem + (j & 1) * (2 * TILE);
+    T* const to = smem + slot * (2 * TILE);
     qs.load(q0, have, to);
     dos.load(q0, have, to + TILE);
-    // statistics: a wavefront an array (the last one two), zeros behind the last row
+    // statistics: a wavefront an array, all of them the positions; zeros behind the last row
     const int64_t row = q_row0 + q0, stat = ((int64_t)r * g.heads + h) * rows + row;
     const void* const from = w == 0 ? (const void*)(g.lse2 + stat) : w == 1 ? (const void*)(g.dot + stat) : w == 2 ? (const void*)(g.lo + r * rows + row) : (const void*)(g.hi + r * rows + row);
-    int* const st = stats + (j & 1) * STATS;
+    int* const st = stats + slot * STATS;
     if (lane < S::TB) {
       lds_load4(scalar_rsrc(from, have * 4), __builtin_amdgcn_readfirstlane(lds_addr_of((const uint16_t*)(st + w * S::TB))), lane * 4);
-      if (w == 3) lds_load4(scalar_rsrc(g.pos_of + r * rows + row, have * 4), __builtin_amdgcn_readfirstlane(lds_addr_of((const uint16_t*)(st + 4 * S::TB))), lane * 4);
+      lds_load4(scalar_rsrc(g.pos_of + r * rows + row, have * 4), __builtin_amdgcn_readfirstlane(lds_addr_of((const uint16_t*)(st + 4 * S::TB))), lane * 4);
     }
   };
-  auto walk = [&](auto exact) {
+  auto walk = [&](auto clean) {
 #pragma unroll
     for (int i = 0; i < S::ND; ++i) dk[i] = dv[i] = all16(0.f);
-    request(0);
-    for (int j = 0; j < tiles * g.group; ++j) {
-      wait_and_barrier<0>();
-      request(j + 1);
+#pragma unroll
+    for (int i = 0; i < STAGES - 1; ++i) request(begin + i, i);
+    int slot = 0, free = STAGES - 1;
+    for (int j = begin; j < all; ++j) {
+      wait_and_barrier<(STAGES - 2) * LOADS>();
+      request(j + STAGES - 1, free);
+      T* const at_tiles = smem + slot * (2 * TILE);
+      const int* const at_stats = stats + slot * STATS;
+      free = slot;
+      slot = slot == STAGES - 1 ? 0 : slot + 1;
       const int h = kh * g.group + j / tiles, t = t0 + j % tiles;
       const float slope2 = EXTRA && g.slopes ? g.slopes[r * g.slopes_z + h] * kLog2e : 0.f;
+      if (decltype(clean)::value) {
+        clean_tile<T, D, 2 * S::TB>(at_tiles, tid, THREADS);
+        __syncthreads();
+      }
 #pragma unroll 1
       for (int i = 0; i < NB; ++i) {
         const int gi = t * NB + i;
         if (gi >= n_groups) continue;
-        const i4v gr = groups[gi];
-        if (gr[0] >= wk0 + 32 || gr[3] <= wk0) continue;
-        const T* const qt = smem + (j & 1) * (2 * TILE) + i * 32 * D;
-        const int* const st = stats + (j & 1) * STATS + 32 * i + ((lane >> 5) << 2);
-        f16v dp, bend;
+        wave_range gr;
+        if (plain) {
+          gr = plain_range_of(g, gi * 32, 32);
+          if (gi * 32 + 32 > g.q_len) gr.lo_max = INT_MAX;                 // the rows that there are not
+        } else {
+          const i4v x = groups[gi];
+          gr = wave_range{x[0], x[1], x[2], x[3]};
+        }
+        if (gr.lo_min >= wk0 + 32 || gr.hi_max <= wk0) continue;
+        const T* const qt = at_tiles + i * 32 * D;
+        const int* const st = at_stats + 32 * i + ((lane >> 5) << 2);
+        f16v dp;
 #pragma unroll
         for (int e4 = 0; e4 < 4; ++e4) {
           const f4v nd = *reinterpret_cast<const f4v*>(st + S::TB + 8 * e4);
@@ -646,7 +757,7 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
         }
         f16v x = at.first(qt, fk, all16(0.f));
         dp = at.first(qt + TILE, fv, dp);
-        if (EXTRA) shape_scores<true>(g, x, bend, slope2, [&](int e) { return distance(st[4 * S::TB + acc_row(e, 0)], key); });
+        if (EXTRA) shape_scores_back(g, x, dp, slope2, [&](int e) { return distance(st[4 * S::TB + acc_row(e, 0)], key); });
 #pragma unroll
         for (int e4 = 0; e4 < 4; ++e4) {
           const f4v l2 = *reinterpret_cast<const f4v*>(st + 8 * e4);
@@ -655,10 +766,9 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
             const int e = 4 * e4 + u;
             x[e] = exp2_fast(__builtin_fmaf(x[e], c, -l2[u]));
             dp[e] *= x[e];
-            if (EXTRA) dp[e] *= bend[e];
           }
         }
-        const bool inside = wk0 >= gr[1] && wk0 + 32 <= gr[2];
+        const bool inside = wk0 >= gr.lo_max && wk0 + 32 <= gr.hi_min;
         if (!inside) {
 #pragma unroll
           for (int e4 = 0; e4 < 4; ++e4) {
@@ -671,30 +781,56 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
             }
           }
         }
-        if (!decltype(exact)::value || inside) {
-          at.second(qt + TILE, x, dv);
-          at.second(qt, dp, dk);
-        } else {
-          const int* const s0 = stats + (j & 1) * STATS + 32 * i;
-          auto seen = [&](int q) { return key >= s0[2 * S::TB + q] && key < s0[3 * S::TB + q]; };
-          second_exact<T, D>(qt + TILE, x, dv, lane, seen);
-          second_exact<T, D>(qt, dp, dk, lane, seen);
-        }
+        at.second(qt + TILE, x, dv);
+        at.second(qt, dp, dk);
       }
     }
+    wait_and_barrier<0>();
   };
   walk(std::false_type());
-  if (__syncthreads_or(there && (not_finite(dk) || not_finite(dv)))) {
-    walk(std::true_type());
-    __syncthreads();
-  }
+  const bool again = block_any(there && (not_finite(dk) || not_finite(dv)), w, lane, (int*)(smem + 2 * STAGES * TILE) - NWV);
+  if (again) walk(std::true_type());
 #pragma unroll
   for (int i = 0; i < S::ND; ++i)
 #pragma unroll
     for (int e = 0; e < 16; ++e) dk[i][e] *= g.scale;
   char* const strip = (char*)smem + w * STRIP;
-  store_rows<T, D, WHOLE>(dk, strip, (T*)g.dk + r * g.dk_z + row0 * g.dk_s + kcol, g.dk_s, g.kv_len - wk0, g.d, lane);
-  store_rows<T, D, WHOLE>(dv, strip, (T*)g.dv + r * g.dv_z + row0 * g.dv_s + kcol, g.dv_s, g.kv_len - wk0, g.d, lane);
+  auto put = [&](auto to_k, auto to_v, int64_t k_s, int64_t v_s, auto wh) {
+    typedef std::remove_pointer_t<decltype(to_k)> U;
+    store_rows<U, D, decltype(wh)::value>(dk, strip, to_k, k_s, g.kv_len - wk0, g.d, lane);
+    store_rows<U, D, decltype(wh)::value>(dv, strip, to_v, v_s, g.kv_len - wk0, g.d, lane);
+    if (!again) return;
+    __threadfence_block();
+    for (int h = 0; h < g.group; ++h) {
+      // the rows of this block's tiles of the head
+      const int from = (t0 + min(max(begin - h * tiles, 0), tiles)) * S::TB, to = min(g.q_len, (t0 + min(max(all - h * tiles, 0), tiles)) * S::TB);
+      add_not_finite<T, D>(do_at + (int64_t)(kh * g.group + h) * g.d, g.do_s, g.d, from, to, to_v, v_s, min(WR, g.kv_len - wk0), lane,
+                           [&](int q, int i) { return wk0 + i >= g.lo[r * rows + q_row0 + q] && wk0 + i < g.hi[r * rows + q_row0 + q]; });
+    }
+  };
+  if (g.splits == 1) {
+    put((T*)g.dk + r * g.dk_z + row0 * g.dk_s + kcol, (T*)g.dv + r * g.dv_z + row0 * g.dv_s + kcol, g.dk_s, g.dv_s, std::integral_constant<bool, WHOLE>());
+  } else {
+    float* const to = g.part + (((int64_t)split * (g.total / g.splits / nx) + blk.grp) * g.kv_len + wk0) * (2 * D);
+    put(to, to + D, 2 * D, 2 * D, std::false_type());
+  }
+}
+
+// dk and dv from the splits' parts, [split][replica, sequence, key head][key][dk | dv]
+template <typename T, int D> __global__ __launch_bounds__(THREADS) void attend_dkv_join_kernel(const attend_args g) {
+  const int64_t rows = (int64_t)g.n * g.seqs * g.kv_heads * g.kv_len, i = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * THREADS + threadIdx.x, row = i / D;
+  const int col = (int)(i % D);
+  if (row >= rows || col >= g.d) return;
+  float dk = 0.f, dv = 0.f;
+  for (int s = 0; s < g.splits; ++s) {
+    dk += g.part[((int64_t)s * rows + row) * (2 * D) + col];
+    dv += g.part[((int64_t)s * rows + row) * (2 * D) + D + col];
+  }
+  const int64_t grp = row / g.kv_len, key = row % g.kv_len;
+  const int kh = (int)(grp % g.kv_heads), b = (int)(grp / g.kv_heads % g.seqs), r = (int)(grp / g.kv_heads / g.seqs);
+  const int64_t at = (int64_t)b * g.kv_len + key, c = (int64_t)kh * g.d + col;
+  hdet_st((T*)g.dk + r * g.dk_z + at * g.dk_s + c, dk);
+  hdet_st((T*)g.dv + r * g.dv_z + at * g.dv_s + c, dv);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -711,6 +847,8 @@ template <typename A> attend_args common_args(const A& a) {
   g.d = a.head_dim; g.causal = a.causal; g.window = a.window; g.splits = 1;
   g.scale = (float)a.scale; g.c = (float)(a.scale * 1.4426950408889634); g.cap2 = (float)(a.softcap * 1.4426950408889634);
   g.inv_cap = a.softcap > 0 ? (float)(1.0 / a.softcap) : 0.f;
+  // bfloat16 inputs: a score off by 1e-7 of a cap up to 1000 moves p by no more than 2^-13 of itself, where its rounding takes 2^-9
+  g.close = a.dtype == HDET_TYPE_F32 || a.softcap > 1000.0;
   return g;
 }
 // whole 16-byte pieces, and a tile within 31 bits
@@ -753,9 +891,19 @@ int few_splits(int n, int seqs, int q_len, int kv_len, int heads, int kv_heads) 
 }
 constexpr size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-struct backward_layout { size_t lse2, dot, lo, hi, pos, groups, total; };
-backward_layout layout_of(int n, int seqs, int q_len, int heads) {
+// Parts of the heads' query tiles that a block of dk and dv takes, where there are few blocks
+int dkv_splits(int n, int seqs, int q_len, int kv_len, int heads, int kv_heads) {
+  const int64_t blocks = (int64_t)n * seqs * kv_heads * ((kv_len + RB - 1) / RB), cus = hdet_compute_units(), tiles = (int64_t)((q_len + 63) / 64) * (heads / kv_heads);
+  if (blocks == 0) return 1;
+  int64_t s = cus / blocks;
+  if (s > tiles / 2) s = tiles / 2;        // two tiles at least
+  return (int)(s < 1 ? 1 : s > 16 ? 16 : s);
+}
+
+struct backward_layout { size_t lse2, dot, lo, hi, pos, groups, part, total; };
+backward_layout layout_of(int n, int seqs, int q_len, int kv_len, int heads, int kv_heads, int d) {
   const size_t rows = (size_t)n * seqs * q_len;
+  const int splits = dkv_splits(n, seqs, q_len, kv_len, heads, kv_heads);
   backward_layout l;
   l.lse2 = 0;
   l.dot = l.lse2 + up256(rows * heads * 4);
@@ -763,7 +911,8 @@ backward_layout layout_of(int n, int seqs, int q_len, int heads) {
   l.hi = l.lo + up256(rows * 4);
   l.pos = l.hi + up256(rows * 4);
   l.groups = l.pos + up256(rows * 4);
-  l.total = rows ? l.groups + up256((size_t)n * seqs * ((q_len + 31) / 32) * 16) : 0;
+  l.part = l.groups + up256((size_t)n * seqs * ((q_len + 31) / 32) * 16);
+  l.total = rows ? l.part + (splits > 1 ? up256((size_t)splits * n * seqs * kv_heads * kv_len * 2 * (d <= 64 ? 64 : 128) * 4) : 0) : 0;
   return l;
 }
 
@@ -775,7 +924,9 @@ size_t hdet_attend_bytes(int n, int seqs, int q_len, int kv_len, int heads, int 
   const size_t ncg = ((size_t)(heads / kv_heads) * q_len + 31) / 32;
   return up256((size_t)n * seqs * kv_heads * ncg * s * 32 * ((head_dim <= 64 ? 64 : 128) + 2) * 4);
 }
-size_t hdet_attend_backward_bytes(int n, int seqs, int q_len, int, int heads, int, int) { return layout_of(n, seqs, q_len, heads).total; }
+size_t hdet_attend_backward_bytes(int n, int seqs, int q_len, int kv_len, int heads, int kv_heads, int head_dim) {
+  return layout_of(n, seqs, q_len, kv_len, heads, kv_heads, head_dim).total;
+}
 
 hipError_t hdet_launch_attend(const hdet_attention_args& a, hipStream_t s) {
   attend_args g = common_args(a);
@@ -815,10 +966,12 @@ hipError_t hdet_launch_attend_backward(const hdet_attention_grad_args& a, hipStr
   g.dk = a.dk.dev; g.dk_s = a.dk.row_stride; g.dk_z = a.dk.replica_stride;
   g.dv = a.dv.dev; g.dv_s = a.dv.row_stride; g.dv_z = a.dv.replica_stride;
   g.lse_in = a.lse_dev;
-  const backward_layout l = layout_of(a.n_replicas, a.seqs, a.q_len, a.heads);
+  const backward_layout l = layout_of(a.n_replicas, a.seqs, a.q_len, a.kv_len, a.heads, a.kv_heads, a.head_dim);
   char* const w8 = (char*)a.workspace_dev;
   g.lse2 = (float*)(w8 + l.lse2); g.dot = (float*)(w8 + l.dot);
   g.lo = (int*)(w8 + l.lo); g.hi = (int*)(w8 + l.hi); g.pos_of = (int*)(w8 + l.pos); g.groups = (i4v*)(w8 + l.groups);
+  g.part = (float*)(w8 + l.part);
+  const int splits = dkv_splits(a.n_replicas, a.seqs, a.q_len, a.kv_len, a.heads, a.kv_heads);
   bool wh = true;
   for (const hdet_rows* m : {&a.q, &a.k, &a.v, &a.out, &a.dout, &a.dq, &a.dk, &a.dv}) wh = wh && (!m->dev || whole(*m, size, a.head_dim));
   const unsigned nq = (a.q_len + RB - 1) / RB, nk = (a.kv_len + RB - 1) / RB;
@@ -829,7 +982,11 @@ hipError_t hdet_launch_attend_backward(const hdet_attention_grad_args& a, hipStr
     if (g.total) hipLaunchKernelGGL((attend_dq_kernel<T, d, ex, w>), grid_of(g.total), dim3(THREADS), 0, s, g);
     g.total = nk * (unsigned)a.n_replicas * a.seqs * a.kv_heads;
     g.heavy_first = nk && heavy_first(g.total, nk);
+    g.splits = splits;
+    g.total *= splits;
     if (g.total) hipLaunchKernelGGL((attend_dkv_kernel<T, d, ex, w>), grid_of(g.total), dim3(THREADS), 0, s, g);
+    if (g.total && splits > 1)
+      hipLaunchKernelGGL((attend_dkv_join_kernel<T, d>), grid_of((unsigned)(((int64_t)a.n_replicas * a.seqs * a.kv_heads * a.kv_len * d + THREADS - 1) / THREADS)), dim3(THREADS), 0, s, g);
   });
   return hipGetLastError();
 }

@@ -23,6 +23,12 @@ constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 
 __device__ __forceinline__ float other_half(float x) { return __shfl_xor(x, 32); }
 __device__ __forceinline__ float exp2_fast(float x) { return __builtin_amdgcn_exp2f(x); }
+// the largest of three numbers (NaN: of the others), without the compiler's quieting of each of them first
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
 __device__ __forceinline__ f16v all16(float x) {
   f16v z;
 #pragma unroll
@@ -113,33 +119,6 @@ template <int D> struct shape<float, D> {
   static __device__ __forceinline__ float rounded(float x) { return x; }
 };
 
-// second() with the pairs that are not attended left out one by one, for tiles in which 0 times something is not 0.  `seen(i)`: row i of the 32 takes part.
-template <typename T, int D, typename F>
-__device__ __forceinline__ void second_exact(const T* tile, f16v x, f16v (&acc)[D / 32], int lane, F seen) {
-  typedef shape<T, D> S;
-#pragma unroll 1
-  for (int e = 0; e < 16; ++e) {
-    const float own = S::rounded(x[0]), other = other_half(own);
-#pragma unroll
-    for (int i = 0; i < 15; ++i) x[i] = x[i + 1];
-#pragma unroll 1
-    for (int half = 0; half < 2; ++half) {
-      const int row = ((e >> 2) << 3) + half * 4 + (e & 3);
-      const float p = half == (lane >> 5) ? own : other;
-      if (!seen(row)) continue;
-#pragma unroll
-      for (int dt = 0; dt < D / 32; ++dt)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const int col = 32 * dt + acc_row(4 * i, lane);
-          const hdet_f4 v = hdet_ld4(tile + row * D + (((col / S::E) ^ S::swz(row)) * S::E) + col % S::E);
-#pragma unroll
-          for (int u = 0; u < 4; ++u) acc[dt][4 * i + u] = __builtin_fmaf(p, v.v[u], acc[dt][4 * i + u]);
-          asm volatile("" ::: "memory");   // no more of the tile in registers than these
-        }
-    }
-  }
-}
 template <int N> __device__ __forceinline__ bool not_finite(const f16v (&x)[N]) {
   float s = 0.f;
 #pragma unroll
@@ -156,6 +135,44 @@ __device__ __forceinline__ hdet_rsrc scalar_rsrc(const void* p, uint32_t bytes) 
   for (int i = 0; i < 4; ++i) r[i] = __builtin_amdgcn_readfirstlane(r[i]);
   return r;
 }
+__device__ __forceinline__ bool finite_of(float x) { return fabsf(x) < INFINITY; }
+// Zeros for what is not finite in an LDS tile of ROWS rows; `t` of `count` threads
+template <typename T, int D, int ROWS> __device__ __forceinline__ void clean_tile(T* tile, int t, int count) {
+  typedef unsigned u4v __attribute__((ext_vector_type(4)));
+  for (int i = t; i < ROWS * shape<T, D>::C; i += count) {
+    u4v x = reinterpret_cast<u4v*>(tile)[i];
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      if (sizeof(T) == 4) x[e] = (x[e] & 0x7f800000u) == 0x7f800000u ? 0u : x[e];
+      else x[e] = ((x[e] & 0x7f80u) == 0x7f80u ? 0u : x[e] & 0xffffu) | ((x[e] & 0x7f800000u) == 0x7f800000u ? 0u : x[e] & 0xffff0000u);
+    }
+    reinterpret_cast<u4v*>(tile)[i] = x;
+  }
+}
+// What is not finite in rows from .. to - 1 of src is added to the rows of dst that attend them (seen(row, own row)): a wavefront's `have` rows
+template <typename T, int D, typename U, typename F>
+__device__ __forceinline__ void add_not_finite(const T* src, int64_t ld, int d, int from, int to, U* dst, int64_t dst_ld, int have, int lane, F seen) {
+  typedef shape<T, D> S;
+  constexpr int ROWS = 64 / S::C;
+  for (int j = from; j < to; j += ROWS) {
+    const int row = j + lane / S::C, col = lane % S::C * S::E;
+    bool bad = false;
+    if (row < to)
+      for (int e = 0; e < S::E; ++e) bad = bad || (col + e < d && !finite_of(hdet_ld(src + row * ld + col + e)));
+    const unsigned long long mask = __ballot(bad);
+    if (!mask) continue;
+    for (int i = 0; i < ROWS; ++i) {
+      if (!(mask >> (i * S::C) & (S::C == 64 ? ~0ull : (1ull << (S::C & 63)) - 1))) continue;
+      for (int c = lane; c < d; c += 64) {
+        const float x = hdet_ld(src + (j + i) * ld + c);
+        if (finite_of(x)) continue;
+        for (int own = 0; own < have; ++own)
+          if (seen(j + i, own)) hdet_st(dst + own * dst_ld + c, hdet_ld(dst + own * dst_ld + c) + x);
+      }
+    }
+  }
+}
+
 // Tiles of ROWS rows of a matrix (row pitch ld, d columns) into LDS, by NW wavefronts.  WHOLE: 16-byte pieces straight from memory to LDS; else element by
 // element through registers.
 template <typename T, int D, int ROWS, int NW, bool WHOLE> struct tile_loader {
@@ -246,12 +263,13 @@ __device__ __forceinline__ void store_rows(const f16v (&o)[D / 32], void* strip_
   wave_fence();
 }
 
-// tanh: 1 - 2 / (e^2x + 1) on the hardware's exponential and reciprocal, and below 0.3, where that cancels, its series up to x^9 (off by 5e-8 of itself)
-__device__ __forceinline__ float tanh_fast(float x) {
+// tanh x - 1 = -2 / (e^2x + 1) on the hardware's exponential and reciprocal, off by 1.2e-7
+__device__ __forceinline__ float tanh_less_1(float x2log2e) { return __builtin_amdgcn_rcpf(__builtin_fmaf(exp2_fast(x2log2e), -0.5f, -0.5f)); }
+// tanh x to 1e-7 of itself: the same, and below 0.3, where it cancels, its series up to x^9
+__device__ __forceinline__ float tanh_close(float x) {
   const float x2 = x * x;
   const float series = __builtin_fmaf(x * x2, __builtin_fmaf(x2, __builtin_fmaf(x2, __builtin_fmaf(x2, 2.1869489e-2f, -5.3968254e-2f), 0.13333334f), -0.33333334f), x);
-  const float far = __builtin_fmaf(-2.f, __builtin_amdgcn_rcpf(exp2_fast(x * (2.f * kLog2e)) + 1.f), 1.f);
-  return x2 < 0.09f ? series : far;
+  return x2 < 0.09f ? series : 1.f + tanh_less_1(x * (2.f * kLog2e));
 }
 
 }  // namespace hdet_attend

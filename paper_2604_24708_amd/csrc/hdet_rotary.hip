@@ -3,9 +3,12 @@
 //   xh = x rstd, rstd = 1 / sqrt(mean x^2 + eps);  u = xh g;  y = R(pos) u:  pairs (u_1, u_2) -> m (u_1 cos a - u_2 sin a, u_1 sin a + u_2 cos a), a = pos f_t
 //   w = R(pos)^T dy;  dx = rstd (w g - xh mean(w g xh));  dg = sum w xh
 //
-// Bound by memory: heads are read once and written once.  A head is held by a team of T lanes, 8 pairs of columns each, so that a rotation
-// never leaves a lane and the norm's sums are log2 T exchanges.  A block first forms the cosines and sines of its rows, once for all heads of
-// a row, in LDS, then walks over the heads.
+// Bound by memory: heads are read once and written once.  A head is held by a team of lanes, 16 bytes each, next to each other, so that a wavefront's loads and
+// stores cover whole lines; halves that turn with each other are exchanged between lanes as they lie in memory.  (8 columns and the 8 they turn with in one
+// lane, which exchanges nothing: 74 us for 8 x 8192 rows of 20 heads of 64, a line in two halves by two loads.)  A block first forms the cosines and
+// sines of its rows, once for all heads of a row, in LDS, then walks over the heads, two a team on their way at once.
+//   us (TB/s): MEASURED
+// Heads that are no whole pieces of 16 bytes at 16-byte boundaries go element by element, 8 pairs a lane (loose).
 
 #include <algorithm>
 #include <type_traits>
@@ -18,10 +21,6 @@ namespace {
 constexpr int THREADS = 256;
 constexpr int MAX_ROWS = 16;               // rows of a block's table at a time
 constexpr int MAX_TABLE = 1024;            // pairs of the table: 8 KiB
-
-// How a head's columns lie in the lanes' pairs: 8 neighbours and the 8 that they turn with (halves), 16 neighbours (pairs), or single elements of
-// heads that are no whole pieces of 8 columns at 16-byte boundaries
-enum { kHalves = 0, kPairs = 1, kLoose = 2 };
 
 struct side {                              // the queries or the keys
   const void *x, *dy;
@@ -39,7 +38,7 @@ struct rotary_args {
   float* partial;                          // [replica][block][2][d]
   int64_t rows;
   int d, half, period, table_rows;         // half: number of pairs that turn
-  int paired;                              // kLoose: which columns are a pair
+  int paired;                              // neighbours are a pair
   double eps;
   float magnitude, inv_d;
 };
@@ -65,215 +64,285 @@ template <int T> __device__ __forceinline__ float team_sum(float v) {
   if (T > 2) v += hdet_dpp<0x4E>(v);
   if (T > 4) v += hdet_dpp<0x141>(v);
   if (T > 8) v += hdet_dpp<0x140>(v);
+  if (T > 16) v += __shfl_xor(v, 16);
+  if (T > 32) v += __shfl_xor(v, 32);
   return v;
 }
 template <int T> __device__ __forceinline__ double team_sum64(double v) {
   for (int o = 1; o < T; o <<= 1) v += __shfl_xor(v, o);
   return v;
 }
-
-struct pairs { float a[8], b[8]; };
-
-// Column of the first and second of a lane's pairs, d and beyond: none
-template <int MODE, int T> __device__ __forceinline__ void columns(const rotary_args& g, int l, int i, int& ca, int& cb, int& t) {
-  if (MODE == kLoose) {
-    t = l + T * i;
-    if (t < g.half) {
-      ca = g.paired ? 2 * t : t;
-      cb = g.paired ? 2 * t + 1 : t + g.half;
-    } else {
-      ca = 2 * t;
-      cb = 2 * t + 1;
-    }
-  } else {
-    t = 8 * l + i;
-    if (MODE == kHalves && 8 * l < g.half) {
-      ca = t;
-      cb = t + g.half;
-    } else if (MODE == kHalves) {
-      ca = 16 * l + i;
-      cb = ca + 8;
-    } else {
-      ca = 2 * t;
-      cb = 2 * t + 1;
-    }
-  }
-}
-
-// A lane's pairs of a head at p; zeros in columns that there are not
-template <typename E, int MODE, int T> __device__ __forceinline__ pairs load_pairs(const rotary_args& g, const E* p, int l) {
-  pairs v;
-  if (MODE == kLoose) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      int ca, cb, t;
-      columns<MODE, T>(g, l, i, ca, cb, t);
-      v.a[i] = ca < g.d ? hdet_ld(p + ca) : 0.f;
-      v.b[i] = cb < g.d ? hdet_ld(p + cb) : 0.f;
-    }
-    return v;
-  }
-  int ca, cb, t;
-  columns<MODE, T>(g, l, 0, ca, cb, t);
-  if (MODE == kPairs) cb = ca + 8;
-  hdet_f8 x = {}, y = {};
-  if (ca < g.d) x = hdet_ld8(p + ca);
-  if (cb < g.d) y = hdet_ld8(p + cb);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    v.a[i] = MODE == kHalves ? x.v[i] : i < 4 ? x.v[2 * (i & 3)] : y.v[2 * (i & 3)];
-    v.b[i] = MODE == kHalves ? y.v[i] : i < 4 ? x.v[2 * (i & 3) + 1] : y.v[2 * (i & 3) + 1];
-  }
-  return v;
-}
-template <typename E, int MODE, int T> __device__ __forceinline__ void store_pairs(const rotary_args& g, E* p, int l, const pairs& v) {
-  if (MODE == kLoose) {
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      int ca, cb, t;
-      columns<MODE, T>(g, l, i, ca, cb, t);
-      if (ca < g.d) hdet_st(p + ca, v.a[i]);
-      if (cb < g.d) hdet_st(p + cb, v.b[i]);
-    }
-    return;
-  }
-  int ca, cb, t;
-  columns<MODE, T>(g, l, 0, ca, cb, t);
-  if (MODE == kPairs) cb = ca + 8;
-  hdet_f8 x, y;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    x.v[i] = MODE == kHalves ? v.a[i] : i & 1 ? v.b[i >> 1] : v.a[i >> 1];
-    y.v[i] = MODE == kHalves ? v.b[i] : i & 1 ? v.b[4 + (i >> 1)] : v.a[4 + (i >> 1)];
-  }
-  if (ca < g.d) hdet_st8(p + ca, x);
-  if (cb < g.d) hdet_st8(p + cb, y);
-}
-
-// 1 / sqrt(mean x^2 + eps): fp32 sums, in 64 bits where the squares leave fp32's range
-template <int T> __device__ __forceinline__ float rstd_of(const rotary_args& g, const pairs& v) {
-  float s = 0.f;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) s = __builtin_fmaf(v.a[i], v.a[i], __builtin_fmaf(v.b[i], v.b[i], s));
-  s = team_sum<T>(s);
-  const float m = __builtin_fmaf(s, g.inv_d, (float)g.eps);
+// 1 / sqrt(mean x^2 + eps) from a lane's sum of squares: fp32 sums, in 64 bits where the squares leave fp32's range (slow(): the lane's sum in 64 bits)
+template <int T, typename F> __device__ __forceinline__ float rstd_of(const rotary_args& g, float s, F slow) {
+  const float m = __builtin_fmaf(team_sum<T>(s), g.inv_d, (float)g.eps);
   if (m > 1e-30f && m < 1e30f) {
     const float r = __builtin_amdgcn_rsqf(m);
     return r * __builtin_fmaf(-0.5f * m * r, r, 1.5f);
   }
-  double w = 0.0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) w += (double)v.a[i] * v.a[i] + (double)v.b[i] * v.b[i];
-  return (float)(1.0 / sqrt(team_sum64<T>(w) / g.d + g.eps));
+  return (float)(1.0 / sqrt(team_sum64<T>(slow()) / g.d + g.eps));
 }
-
 __device__ __forceinline__ double position(const rotary_args& g, int r, int64_t row) {
   return g.pos ? (double)g.pos[(int64_t)r * g.rows + row] : (double)(g.period ? row % g.period : row);
 }
+// Cosines and sines of `have` rows from row0 on; between two barriers.  BACK: of the turn back
+template <bool BACK> __device__ __forceinline__ void make_table(const rotary_args& g, int r, int64_t row0, unsigned have, float2* table) {
+  __syncthreads();                         // the last rows' table has been read
+  for (unsigned i = threadIdx.x; i < have * g.half; i += THREADS) {
+    const unsigned row = i / (unsigned)g.half;
+    const float2 cs = cos_sin(position(g, r, row0 + row) * g.freq[i - row * g.half]);
+    table[i] = make_float2(cs.x * g.magnitude, (BACK ? -cs.y : cs.y) * g.magnitude);
+  }
+  __syncthreads();
+}
 
-// One block: rows `table_rows` at a time, all heads of them.  BACK: the gradients, and the gains' partial sums.
-template <typename E, int MODE, int T, bool BACK> __global__ __launch_bounds__(THREADS) void rotary_kernel(const rotary_args g) {
+// ---------------------------------------------------------------------------------------------
+// Whole pieces.  One block: rows `table_rows` at a time, all heads of one side (blockIdx.z) of them.  BACK: the gradients, and the gain's partial sums.
+// ---------------------------------------------------------------------------------------------
+template <typename E> struct chunk_of {    // 16 bytes of a row
+  static constexpr int N = 16 / sizeof(E);
+  hdet_u4v w;
+  __device__ __forceinline__ void load(const E* p) { w = *reinterpret_cast<const hdet_u4v*>(p); }
+  __device__ __forceinline__ float operator[](int e) const {
+    return sizeof(E) == 4 ? __uint_as_float(w[e & 3]) : __uint_as_float(e & 1 ? w[(e >> 1) & 3] & 0xffff0000u : w[(e >> 1) & 3] << 16);
+  }
+  __device__ __forceinline__ chunk_of from(int lane) const {
+    chunk_of r;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) r.w[i] = __shfl((int)w[i], lane);
+    return r;
+  }
+};
+template <typename E, bool PAIRED, int T, bool BACK> __global__ __launch_bounds__(THREADS) void rotary_kernel(const rotary_args g) {
+  typedef chunk_of<E> chunk;
+  constexpr int N = chunk::N, U = 2;
   __shared__ float2 table[MAX_TABLE];
-  __shared__ float sums[BACK ? THREADS * 16 : 1];
-  const int tid = threadIdx.x, l = tid % T, r = blockIdx.y;
+  __shared__ float sums[BACK ? THREADS * N : 1];
+  const int tid = threadIdx.x, l = tid % T, r = blockIdx.y, lane = tid & 63;
+  const side& s = g.s[blockIdx.z];
   const int64_t chunks = (g.rows + g.table_rows - 1) / g.table_rows;
-  pairs acc[2] = {};
-  pairs gain[2];
+  const bool on = l * N < g.d, turns = l * N < 2 * g.half;
+  // halves: the lane that holds the other half, whether this is the second, and the first pair
+  const int step = g.half / N;
+  const bool second = !PAIRED && turns && l >= step;
+  const int other = PAIRED || !turns ? lane : second ? lane - step : lane + step, pair0 = PAIRED ? l * (N / 2) : (second ? l - step : l) * N;
+  const E* const xs = (const E*)s.x + r * s.x_z + l * N;
+  const E* const dys = (const E*)s.dy + r * s.dy_z + l * N;
+  E* const ys = (E*)s.y + r * s.y_z + l * N;
+  float gain[N], acc[N];
 #pragma unroll
-  for (int z = 0; z < 2; ++z)
+  for (int e = 0; e < N; ++e) {
+    gain[e] = s.gain && on ? s.gain[r * s.gain_z + l * N + e] : 1.f;
+    acc[e] = 0.f;
+  }
+  for (int64_t chunk_i = blockIdx.x; chunk_i < chunks; chunk_i += gridDim.x) {
+    const int64_t row0 = chunk_i * g.table_rows;
+    const unsigned have = (unsigned)(g.rows - row0 < g.table_rows ? g.rows - row0 : g.table_rows), teams = have * (unsigned)s.heads;
+    make_table<BACK>(g, r, row0, have, table);
+    for (unsigned t0 = tid / T; t0 < teams; t0 += U * (THREADS / T)) {
+      chunk x_[U], dy_[U];
+      unsigned row_[U], head_[U];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      int ca, cb, t;
-      columns<MODE, T>(g, l, i, ca, cb, t);
-      const float* q = g.s[z].gain ? g.s[z].gain + r * g.s[z].gain_z : nullptr;
-      gain[z].a[i] = q && ca < g.d ? q[ca] : 0.f;
-      gain[z].b[i] = q && cb < g.d ? q[cb] : 0.f;
-    }
-  for (int64_t chunk = blockIdx.x; chunk < chunks; chunk += gridDim.x) {
-    const int64_t row0 = chunk * g.table_rows;
-    const int have = (int)(g.rows - row0 < g.table_rows ? g.rows - row0 : g.table_rows);
-    __syncthreads();                       // the last rows' table has been read
-    for (int i = tid; i < have * g.half; i += THREADS) {
-      const int row = i / g.half;
-      float2 cs = cos_sin(position(g, r, row0 + row) * g.freq[i - row * g.half]);
-      table[i] = make_float2(cs.x * g.magnitude, (BACK ? -cs.y : cs.y) * g.magnitude);
-    }
-    __syncthreads();
+      for (int u = 0; u < U; ++u) {
+        const unsigned team = t0 + u * (THREADS / T);
+        row_[u] = team / (unsigned)s.heads;
+        head_[u] = team - row_[u] * s.heads;
+        x_[u].w = dy_[u].w = hdet_u4v{0u, 0u, 0u, 0u};
+        if (team >= teams || !on) continue;
+        const int64_t at = row0 + row_[u], col = (int64_t)head_[u] * g.d;
+        if (!BACK || s.gain) x_[u].load(xs + at * s.x_s + col);
+        if (BACK) dy_[u].load(dys + at * s.dy_s + col);
+      }
 #pragma unroll
-    for (int z = 0; z < 2; ++z) {
-      const side& s = g.s[z];
-      const int items = have * s.heads * T;
-      for (int i = tid; i < items; i += THREADS) {
-        const int team = i / T, row = team / s.heads, head = team - row * s.heads;
-        const int64_t at = row0 + row;
-        pairs x = {}, dy;
+      for (int u = 0; u < U; ++u) {
+        if (t0 + u * (THREADS / T) >= teams) break;
+        const chunk x = x_[u];
         float rstd = 1.f;
-        if (!BACK || s.gain) x = load_pairs<E, MODE, T>(g, (const E*)s.x + r * s.x_z + at * s.x_s + (int64_t)head * g.d, l);
-        if (BACK) dy = load_pairs<E, MODE, T>(g, (const E*)s.dy + r * s.dy_z + at * s.dy_s + (int64_t)head * g.d, l);
-        if (s.gain) rstd = rstd_of<T>(g, x);
-        pairs& v = BACK ? dy : x;
-        if (!BACK && s.gain) {
+        if (s.gain) {
+          float q = 0.f;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            v.a[e] = v.a[e] * rstd * gain[z].a[e];
-            v.b[e] = v.b[e] * rstd * gain[z].b[e];
-          }
+          for (int e = 0; e < N; ++e) q = __builtin_fmaf(x[e], x[e], q);
+          rstd = rstd_of<T>(g, q, [&] {
+            double w = 0.0;
+            for (int e = 0; e < N; ++e) w += (double)x[e] * x[e];
+            return w;
+          });
         }
-        const float2* cs = table + row * g.half;
+        const chunk v = BACK ? dy_[u] : x;
+        float w[N], y[N];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int t = MODE == kLoose ? l + T * e : 8 * l + e;
-          if (t < g.half) {
-            const float2 c = cs[t];
-            const float a = v.a[e], b = v.b[e];
-            v.a[e] = __builtin_fmaf(a, c.x, -b * c.y);
-            v.b[e] = __builtin_fmaf(a, c.y, b * c.x);
+        for (int e = 0; e < N; ++e) {
+          w[e] = v[e];
+          if (!BACK && s.gain) w[e] *= rstd * gain[e];
+          y[e] = w[e];
+        }
+        const float2* const cs = table + row_[u] * g.half + pair0;
+        if (PAIRED) {
+#pragma unroll
+          for (int e = 0; e < N; e += 2)
+            if (pair0 + e / 2 < g.half) {
+              const float2 c = cs[e / 2];
+              y[e] = __builtin_fmaf(w[e], c.x, -w[e + 1] * c.y);
+              y[e + 1] = __builtin_fmaf(w[e], c.y, w[e + 1] * c.x);
+            }
+        } else {
+          float mate[N];
+          if (BACK) {
+            const chunk v2 = v.from(other);
+#pragma unroll
+            for (int e = 0; e < N; ++e) mate[e] = v2[e];
+          } else {
+#pragma unroll
+            for (int e = 0; e < N; ++e) mate[e] = __shfl(w[e], other);
+          }
+          if (turns) {
+#pragma unroll
+            for (int e = 0; e < N; ++e) {
+              const float2 c = cs[e];
+              y[e] = __builtin_fmaf(w[e], c.x, mate[e] * (second ? c.y : -c.y));
+            }
           }
         }
         if (BACK && s.gain) {
           float dot = 0.f;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            x.a[e] *= rstd;
-            x.b[e] *= rstd;
-            if (s.sums) {
-              acc[z].a[e] = __builtin_fmaf(v.a[e], x.a[e], acc[z].a[e]);
-              acc[z].b[e] = __builtin_fmaf(v.b[e], x.b[e], acc[z].b[e]);
-            }
-            v.a[e] *= gain[z].a[e];
-            v.b[e] *= gain[z].b[e];
-            dot = __builtin_fmaf(v.a[e], x.a[e], __builtin_fmaf(v.b[e], x.b[e], dot));
+          for (int e = 0; e < N; ++e) {
+            const float xh = x[e] * rstd;
+            acc[e] = __builtin_fmaf(y[e], xh, acc[e]);
+            y[e] *= gain[e];
+            dot = __builtin_fmaf(y[e], xh, dot);
           }
           dot = team_sum<T>(dot) * g.inv_d;
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            v.a[e] = rstd * __builtin_fmaf(-x.a[e], dot, v.a[e]);
-            v.b[e] = rstd * __builtin_fmaf(-x.b[e], dot, v.b[e]);
-          }
+          for (int e = 0; e < N; ++e) y[e] = rstd * __builtin_fmaf(-x[e] * rstd, dot, y[e]);
         }
-        store_pairs<E, MODE, T>(g, (E*)s.y + r * s.y_z + at * s.y_s + (int64_t)head * g.d, l, v);
+        if (!on) continue;
+        E* const to = ys + (row0 + row_[u]) * s.y_s + (int64_t)head_[u] * g.d;
+        if constexpr (N == 8) hdet_st8(to, hdet_f8{{y[0], y[1], y[2], y[3], y[4], y[5], y[6], y[7]}});
+        else hdet_st4(to, hdet_f4{{y[0], y[1], y[2], y[3]}});
       }
     }
   }
-  if (!BACK) return;
+  if (!BACK || !s.sums) return;
 #pragma unroll
-  for (int z = 0; z < 2; ++z) {
-    if (!g.s[z].sums) continue;
-    __syncthreads();
+  for (int e = 0; e < N; ++e) sums[tid * N + e] = acc[e];
+  __syncthreads();
+  for (int c = tid; c < g.d; c += THREADS) {
+    float v = 0.f;
+    for (int team = 0; team < THREADS / T; ++team) v += sums[team * (N * T) + c];
+    g.partial[(((int64_t)r * gridDim.x + blockIdx.x) * 2 + blockIdx.z) * g.d + c] = v;
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Any heads: a lane's pair i is number l + T i, behind the ones that turn the rest's neighbours
+// ---------------------------------------------------------------------------------------------
+struct pairs { float a[8], b[8]; };
+template <int T> __device__ __forceinline__ void columns(const rotary_args& g, int l, int i, int& ca, int& cb) {
+  const int t = l + T * i;
+  ca = g.paired || t >= g.half ? 2 * t : t;
+  cb = g.paired || t >= g.half ? 2 * t + 1 : t + g.half;
+}
+template <typename E, int T> __device__ __forceinline__ pairs load_pairs(const rotary_args& g, const E* p, int l) {
+  pairs v;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      sums[(tid / T) * (16 * T) + (2 * e) * T + l] = acc[z].a[e];
-      sums[(tid / T) * (16 * T) + (2 * e + 1) * T + l] = acc[z].b[e];
+  for (int i = 0; i < 8; ++i) {
+    int ca, cb;
+    columns<T>(g, l, i, ca, cb);
+    v.a[i] = ca < g.d ? hdet_ld(p + ca) : 0.f;
+    v.b[i] = cb < g.d ? hdet_ld(p + cb) : 0.f;
+  }
+  return v;
+}
+template <typename E, int T, bool BACK> __global__ __launch_bounds__(THREADS) void rotary_loose_kernel(const rotary_args g) {
+  __shared__ float2 table[MAX_TABLE];
+  __shared__ float sums[BACK ? THREADS * 16 : 1];
+  const int tid = threadIdx.x, l = tid % T, r = blockIdx.y;
+  const side& s = g.s[blockIdx.z];
+  const int64_t chunks = (g.rows + g.table_rows - 1) / g.table_rows;
+  pairs acc = {}, gain = {};
+  if (s.gain) gain = load_pairs<float, T>(g, s.gain + r * s.gain_z, l);
+  for (int64_t chunk = blockIdx.x; chunk < chunks; chunk += gridDim.x) {
+    const int64_t row0 = chunk * g.table_rows;
+    const unsigned have = (unsigned)(g.rows - row0 < g.table_rows ? g.rows - row0 : g.table_rows), teams = have * (unsigned)s.heads;
+    make_table<BACK>(g, r, row0, have, table);
+    for (unsigned team = tid / T; team < teams; team += THREADS / T) {
+      const unsigned row = team / (unsigned)s.heads, head = team - row * s.heads;
+      const int64_t at = row0 + row, col = (int64_t)head * g.d;
+      pairs x = {}, v;
+      float rstd = 1.f;
+      if (!BACK || s.gain) x = load_pairs<E, T>(g, (const E*)s.x + r * s.x_z + at * s.x_s + col, l);
+      if (BACK) v = load_pairs<E, T>(g, (const E*)s.dy + r * s.dy_z + at * s.dy_s + col, l);
+      if (s.gain) {
+        float q = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) q = __builtin_fmaf(x.a[i], x.a[i], __builtin_fmaf(x.b[i], x.b[i], q));
+        rstd = rstd_of<T>(g, q, [&] {
+          double w = 0.0;
+          for (int i = 0; i < 8; ++i) w += (double)x.a[i] * x.a[i] + (double)x.b[i] * x.b[i];
+          return w;
+        });
+      }
+      if (!BACK) {
+        v = x;
+        if (s.gain) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) {
+            v.a[i] = x.a[i] * rstd * gain.a[i];
+            v.b[i] = x.b[i] * rstd * gain.b[i];
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if (l + T * i >= g.half) continue;
+        const float2 c = table[row * g.half + l + T * i];
+        const float a = v.a[i], b = v.b[i];
+        v.a[i] = __builtin_fmaf(a, c.x, -b * c.y);
+        v.b[i] = __builtin_fmaf(a, c.y, b * c.x);
+      }
+      if (BACK && s.gain) {
+        float dot = 0.f;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          x.a[i] *= rstd;
+          x.b[i] *= rstd;
+          acc.a[i] = __builtin_fmaf(v.a[i], x.a[i], acc.a[i]);
+          acc.b[i] = __builtin_fmaf(v.b[i], x.b[i], acc.b[i]);
+          v.a[i] *= gain.a[i];
+          v.b[i] *= gain.b[i];
+          dot = __builtin_fmaf(v.a[i], x.a[i], __builtin_fmaf(v.b[i], x.b[i], dot));
+        }
+        dot = team_sum<T>(dot) * g.inv_d;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          v.a[i] = rstd * __builtin_fmaf(-x.a[i], dot, v.a[i]);
+          v.b[i] = rstd * __builtin_fmaf(-x.b[i], dot, v.b[i]);
+        }
+      }
+      E* const to = (E*)s.y + r * s.y_z + at * s.y_s + col;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        int ca, cb;
+        columns<T>(g, l, i, ca, cb);
+        if (ca < g.d) hdet_st(to + ca, v.a[i]);
+        if (cb < g.d) hdet_st(to + cb, v.b[i]);
+      }
     }
-    __syncthreads();
-    for (int j = tid; j < 16 * T; j += THREADS) {
-      float v = 0.f;
-      for (int team = 0; team < THREADS / T; ++team) v += sums[team * (16 * T) + j];
-      int ca, cb, t;
-      columns<MODE, T>(g, j % T, j / T / 2, ca, cb, t);
-      const int c = j / T & 1 ? cb : ca;
-      if (c < g.d) g.partial[(((int64_t)r * gridDim.x + blockIdx.x) * 2 + z) * g.d + c] = v;
-    }
+  }
+  if (!BACK || !s.sums) return;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    sums[(tid / T) * (16 * T) + (2 * i) * T + l] = acc.a[i];
+    sums[(tid / T) * (16 * T) + (2 * i + 1) * T + l] = acc.b[i];
+  }
+  __syncthreads();
+  for (int j = tid; j < 16 * T; j += THREADS) {
+    float v = 0.f;
+    for (int team = 0; team < THREADS / T; ++team) v += sums[team * (16 * T) + j];
+    int ca, cb;
+    columns<T>(g, j % T, j / T / 2, ca, cb);
+    const int c = j / T & 1 ? cb : ca;
+    if (c < g.d) g.partial[(((int64_t)r * gridDim.x + blockIdx.x) * 2 + blockIdx.z) * g.d + c] = v;
   }
 }
 
@@ -294,13 +363,18 @@ __global__ __launch_bounds__(1024) void rotary_gain_kernel(const float* partial,
   }
 }
 
-int team_of(int d) { return d <= 32 ? 2 : d <= 64 ? 4 : d <= 128 ? 8 : 16; }
+// lanes of a head, `each` columns a lane: a power of two
+int team_of(int d, int each) {
+  int t = 1;
+  while (t * each < d) t *= 2;
+  return t;
+}
 
 // Rows of a block's table: at least as many as give every thread a head, within the table
 int table_rows_of(int64_t rows, int n, int d, int half, int heads) {
   int most = half ? MAX_TABLE / half : MAX_ROWS;
   if (most > MAX_ROWS) most = MAX_ROWS;
-  int want = THREADS / team_of(d) / heads;
+  int want = THREADS / team_of(d, 8) / heads;
   if (want < 1) want = 1;
   // large calls: more rows a table, for fewer waits; small ones: a row a block, for more blocks
   while (want < most && rows * n / (2 * want) >= 8 * (int64_t)hdet_compute_units()) want *= 2;
@@ -320,24 +394,29 @@ bool whole(const hdet_rows& m, int size) {
   return !m.dev || (((uintptr_t)m.dev & 15) == 0 && ((m.row_stride | m.replica_stride) & mask) == 0);
 }
 
-template <bool BACK> hipError_t launch(const rotary_args& g, int dtype, int mode, int n, int blocks, hipStream_t s) {
-  const dim3 grid(blocks, n);
-  auto go = [&](auto e, auto m, auto t) { hipLaunchKernelGGL((rotary_kernel<decltype(e), m, t, BACK>), grid, dim3(THREADS), 0, s, g); };
-  auto with_mode = [&](auto e, auto t) {
-    if (mode == kHalves) go(e, std::integral_constant<int, kHalves>(), t);
-    else if (mode == kPairs) go(e, std::integral_constant<int, kPairs>(), t);
-    else go(e, std::integral_constant<int, kLoose>(), t);
-  };
-  auto with_team = [&](auto e) {
-    switch (team_of(g.d)) {
-      case 2: return with_mode(e, std::integral_constant<int, 2>());
-      case 4: return with_mode(e, std::integral_constant<int, 4>());
-      case 8: return with_mode(e, std::integral_constant<int, 8>());
-      default: return with_mode(e, std::integral_constant<int, 16>());
-    }
-  };
-  if (dtype == HDET_TYPE_BF16) with_team(uint16_t());
-  else with_team(float());
+// f(integral_constant<T>) for the smallest power of two from LEAST on that is T
+template <int LEAST, typename F> void with_team(int t, F f) {
+  if (t <= LEAST) f(std::integral_constant<int, LEAST>());
+  else if constexpr (LEAST < 64) with_team<2 * LEAST>(t, f);
+}
+template <bool BACK, typename E> void launch_typed(const rotary_args& g, bool whole, int n, int blocks, hipStream_t s) {
+  const dim3 grid(blocks, n, g.s[1].heads ? 2 : 1);
+  if (whole) {
+    with_team<2>(team_of(g.d, 16 / (int)sizeof(E)), [&](auto t) {
+      if (g.paired) hipLaunchKernelGGL((rotary_kernel<E, true, t, BACK>), grid, dim3(THREADS), 0, s, g);
+      else hipLaunchKernelGGL((rotary_kernel<E, false, t, BACK>), grid, dim3(THREADS), 0, s, g);
+    });
+  } else {
+    with_team<2>(std::min(16, team_of(g.d, 16)), [&](auto t) {
+      if constexpr (t <= 16) hipLaunchKernelGGL((rotary_loose_kernel<E, t, BACK>), grid, dim3(THREADS), 0, s, g);
+    });
+  }
+}
+template <bool BACK> hipError_t launch(const rotary_args& g, int dtype, bool aligned, int n, int blocks, hipStream_t s) {
+  const int each = dtype == HDET_TYPE_BF16 ? 8 : 4;
+  const bool whole = aligned && g.d % each == 0 && (g.paired || g.half % each == 0);
+  if (dtype == HDET_TYPE_BF16) launch_typed<BACK, uint16_t>(g, whole, n, blocks, s);
+  else launch_typed<BACK, float>(g, whole, n, blocks, s);
   return hipGetLastError();
 }
 
@@ -354,12 +433,6 @@ template <typename A> rotary_args common_args(const A& a, bool keys) {
   g.table_rows = table_rows_of(a.rows, a.n_replicas, g.d, g.half, g.s[0].heads + g.s[1].heads);
   return g;
 }
-int mode_of(const rotary_args& g, bool aligned) {
-  if (!aligned || g.d % 8) return kLoose;
-  if (g.paired) return kPairs;
-  return g.half % 8 == 0 ? kHalves : kLoose;
-}
-
 }  // namespace
 
 hipError_t hdet_launch_rotary(const hdet_rotary_args& a, hipStream_t s) {
@@ -373,7 +446,7 @@ hipError_t hdet_launch_rotary(const hdet_rotary_args& a, hipStream_t s) {
   g.s[1].y = a.k_out.dev; g.s[1].y_s = a.k_out.row_stride; g.s[1].y_z = a.k_out.replica_stride;
   const bool aligned = whole(a.q, size) && whole(a.q_out, size) && (!keys || (whole(a.k, size) && whole(a.k_out, size)));
   const int64_t chunks = (a.rows + g.table_rows - 1) / g.table_rows;
-  return launch<false>(g, a.dtype, mode_of(g, aligned), a.n_replicas, (int)chunks, s);
+  return launch<false>(g, a.dtype, aligned, a.n_replicas, (int)chunks, s);
 }
 
 size_t hdet_rotary_backward_bytes(int n_replicas, int64_t rows, int head_dim, int q_heads, int k_heads) {
@@ -401,7 +474,7 @@ hipError_t hdet_launch_rotary_backward(const hdet_rotary_grad_args& a, hipStream
     const bool aligned = whole(a.dq_out, size) && whole(a.dq, size) && (!a.q_gain_dev || whole(a.q, size)) &&
                          (!keys || (whole(a.dk_out, size) && whole(a.dk, size) && (!a.k_gain_dev || whole(a.k, size))));
     blocks = grad_blocks(a.rows, a.n_replicas, g.table_rows);
-    const hipError_t e = launch<true>(g, a.dtype, mode_of(g, aligned), a.n_replicas, blocks, s);
+    const hipError_t e = launch<true>(g, a.dtype, aligned, a.n_replicas, blocks, s);
     if (e != hipSuccess) return e;
   }
   if (!a.dq_gain_dev && !a.dk_gain_dev) return hipSuccess;

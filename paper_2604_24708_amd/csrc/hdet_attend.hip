@@ -29,6 +29,23 @@ constexpr int NWV = THREADS / 64;
 constexpr int WR = 32;                     // rows a wavefront owns
 constexpr int RB = WR * NWV;               // rows a block owns
 
+// n / d for any 32-bit n by a product and shifts: a division is some thirty instructions before a block's first load
+struct divisor { unsigned d, mul, s1, s2; };
+divisor divisor_of(unsigned d) {
+  divisor v = {d, 0, 0, 0};
+  if (d == 0) return v;
+  unsigned l = 0;
+  while (((uint64_t)1 << l) < d) ++l;
+  v.mul = (unsigned)((((uint64_t)1 << 32) * (((uint64_t)1 << l) - d)) / d + 1);
+  v.s1 = l < 1 ? l : 1;
+  v.s2 = l > 1 ? l - 1 : 0;
+  return v;
+}
+__device__ __forceinline__ unsigned over(unsigned n, const divisor& v) {
+  const unsigned t = __umulhi(n, v.mul);
+  return (t + ((n - t) >> v.s1)) >> v.s2;
+}
+
 struct attend_args {
   const void *q, *k, *v, *o, *dout;
   void *out, *dq, *dk, *dv;
@@ -47,6 +64,7 @@ struct attend_args {
   float scale, c, cap2, inv_cap;           // c = scale log2 e; cap2 = cap log2 e or 0
   bool close;                              // capped scores to fp32's last places, not to 1e-7 of the cap
   unsigned total;                          // blocks
+  divisor by_nx, by_groups, by_own, by_heads, by_kv_heads, by_seqs, by_group;   // row blocks; total / nx, an eighth of that; ..
   bool heavy_first;
 };
 
@@ -76,24 +94,31 @@ __device__ __forceinline__ key_range range_of(const attend_args& g, int r, int b
 // launch order: every XCD works through a contiguous range of grp, so that the tiles which blocks share are in one L2; heavy_first: the longest row
 // blocks of all grp first, then the next ones (few rounds of blocks: the last one's length counts more).
 struct block_id { unsigned x, grp; };
-__device__ __forceinline__ block_id place_block(unsigned lin, unsigned total, unsigned nx, bool heavy_first) {
-  const unsigned groups = total / nx;
+__device__ __forceinline__ block_id place_block(unsigned lin, const attend_args& g) {
+  const unsigned nx = g.by_nx.d, groups = g.by_groups.d, total = nx * groups;
   block_id b;
-  if (heavy_first) {
+  if (g.heavy_first) {
     if ((groups & 7u) == 0u) {
-      const unsigned own = groups >> 3, j = lin >> 3;
-      b.x = j / own;
-      b.grp = (lin & 7u) * own + j % own;
+      const unsigned j = lin >> 3;
+      b.x = over(j, g.by_own);
+      b.grp = (lin & 7u) * g.by_own.d + (j - b.x * g.by_own.d);
     } else {
-      b.x = lin / groups;
-      b.grp = lin % groups;
+      b.x = over(lin, g.by_groups);
+      b.grp = lin - b.x * groups;
     }
   } else {
     if ((total & 7u) == 0u) lin = (lin & 7u) * (total >> 3) + (lin >> 3);
-    b.grp = lin / nx;
-    b.x = (lin % nx + b.grp + (b.grp >> 3) + (b.grp >> 6)) % nx;
+    b.grp = over(lin, g.by_nx);
+    const unsigned turned = lin - b.grp * nx + b.grp + (b.grp >> 3) + (b.grp >> 6);
+    b.x = turned - over(turned, g.by_nx) * nx;
   }
   return b;
+}
+// replica, sequence and head of a group
+struct group_id { int r, b, h; };
+__device__ __forceinline__ group_id place_group(unsigned grp, const attend_args& g, const divisor& heads) {
+  const unsigned rb = over(grp, heads), r = over(rb, g.by_seqs);
+  return {(int)r, (int)(rb - r * g.by_seqs.d), (int)(grp - rb * heads.d)};
 }
 
 // Least over the 32 rows of a wavefront
@@ -189,14 +214,14 @@ template <typename F> __device__ __forceinline__ void shape_scores(const attend_
     for (int e = 0; e < 16; ++e) x[e] = __builtin_fmaf(-slope2, dist(e), x[e]);
   }
 }
-// Backward: scores, in log2 units, from raw products, and dp times the cap's derivative
-template <typename F> __device__ __forceinline__ void shape_scores_back(const attend_args& g, f16v& x, f16v& dp, float slope2, F dist) {
+// Backward: scores, in log2 units, from raw products; bend: the cap's derivative
+template <typename F> __device__ __forceinline__ void shape_scores_back(const attend_args& g, f16v& x, f16v& bend, float slope2, F dist) {
   if (g.cap2 > 0.f && !g.close) {
     const float s = 2.f * kLog2e * g.scale * g.inv_cap;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       const float t = tanh_less_1(x[e] * s);
-      dp[e] *= -t * (t + 2.f);
+      bend[e] = -t * (t + 2.f);
       x[e] = __builtin_fmaf(t, g.cap2, g.cap2);
     }
   } else if (g.cap2 > 0.f) {
@@ -204,10 +229,11 @@ template <typename F> __device__ __forceinline__ void shape_scores_back(const at
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       const float t = tanh_close(x[e] * s);
-      dp[e] *= __builtin_fmaf(-t, t, 1.f);
+      bend[e] = __builtin_fmaf(-t, t, 1.f);
       x[e] = t * g.cap2;
     }
   } else {
+    bend = all16(1.f);
 #pragma unroll
     for (int e = 0; e < 16; ++e) x[e] *= g.c;
   }
@@ -229,53 +255,53 @@ template <int D> struct running {
     l = 0.f;
   }
   __device__ __forceinline__ float ref() const { return m == -INFINITY ? 0.f : m; }
-  // Exponentials of NB blocks of scores times c; the reference follows the maximum only when that has risen by more than 2^8 (the sums hold that), so that
-  // results are seldom rescaled
-  template <int NB> __device__ __forceinline__ void take(f16v (&x)[NB], float c) {
-    float top = x[0][0];
+  // Exponentials of a block of scores times c.  Any reference will do that keeps them in fp32's range (bfloat16's is the same): FOLLOW takes the maximum, once
+  // it has risen by more than 2^8 since (so that results are seldom rescaled); without it the reference stays, and where a score is more than 2^127
+  // times larger, the sum says infinity.
+  template <bool FOLLOW> __device__ __forceinline__ void take(f16v& x, float c) {
+    if (FOLLOW) {
+      float top = x[0];
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
+      for (int e = 0; e < 16; e += 2) top = max3(top, x[e], x[e + 1]);
+      top = fmaxf(top, other_half(top)) * c;
+      if (__any(top > m + 8.f)) {
+        const float next = fmaxf(m, top), keep = exp2_fast(m - (next == -INFINITY ? 0.f : next));
+        m = next;
+        l *= keep;
 #pragma unroll
-      for (int e = 0; e < 16; e += 2) top = max3(top, x[b][e], x[b][e + 1]);
-    top = fmaxf(top, other_half(top)) * c;
-    if (__any(top > m + 8.f)) {
-      const float next = fmaxf(m, top), keep = exp2_fast(m - (next == -INFINITY ? 0.f : next));
-      m = next;
-      l *= keep;
+        for (int i = 0; i < D / 32; ++i)
 #pragma unroll
-      for (int i = 0; i < D / 32; ++i)
-#pragma unroll
-        for (int e = 0; e < 16; ++e) o[i][e] *= keep;
+          for (int e = 0; e < 16; ++e) o[i][e] *= keep;
+      }
     }
     const float r = -ref();
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int e = 0; e < 16; ++e) {
-        x[b][e] = exp2_fast(__builtin_fmaf(x[b][e], c, r));
-        l += x[b][e];
-      }
+    for (int e = 0; e < 16; ++e) {
+      x[e] = exp2_fast(__builtin_fmaf(x[e], c, r));
+      l += x[e];
+    }
   }
 };
 
 // ---------------------------------------------------------------------------------------------
 // forward: block = 128 queries of one (replica, sequence, head)
 // ---------------------------------------------------------------------------------------------
-template <typename T, int D> constexpr int forward_waves() { return sizeof(T) == 2 ? (D == 64 ? 3 : 2) : (D == 64 ? 2 : 1); }
-template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds__(THREADS, (forward_waves<T, D>())) void attend_kernel(const attend_args g) {
+template <typename T, int D, bool EXTRA> constexpr int forward_waves() { return sizeof(T) == 2 ? (D == 64 ? (EXTRA ? 3 : 4) : 2) : (D == 64 ? 2 : 1); }
+template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds__(THREADS, (forward_waves<T, D, EXTRA>())) void attend_kernel(const attend_args g) {
   typedef shape<T, D> S;
   constexpr int TILE = S::TB * D, NB = S::TB / 32, LOADS = 2 * tile_loader<T, D, S::TB, NWV, WHOLE>::NI;
   __shared__ __attribute__((aligned(1024))) T smem[2 * STAGES * TILE];     // keys and values
   const unsigned lin = blockIdx.y * gridDim.x + blockIdx.x;
   if (lin >= g.total) return;
-  const unsigned nx = (g.q_len + RB - 1) / RB;
-  const block_id blk = place_block(lin, g.total, nx, g.heavy_first);
-  const int h = blk.grp % g.heads, b = blk.grp / g.heads % g.seqs, r = blk.grp / g.heads / g.seqs;
+  const unsigned nx = g.by_nx.d;
+  const block_id blk = place_block(lin, g);
+  const group_id id = place_group(blk.grp, g, g.by_heads);
+  const int h = id.h, b = id.b, r = id.r;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wq0 = (int)(nx - 1 - blk.x) * RB + w * WR, qi = wq0 + (lane & 31);
   const bool there = qi < g.q_len;
   const key_range range = there ? range_of(g, r, b, qi) : key_range{0, 0, 0};
-  const int64_t col = (int64_t)h * g.d, kcol = (int64_t)(h / g.group) * g.d, row0 = (int64_t)b * g.q_len + wq0;
+  const int64_t col = (int64_t)h * g.d, kcol = (int64_t)over(h, g.by_group) * g.d, row0 = (int64_t)b * g.q_len + wq0;
   const T* const own = there ? (const T*)g.q + r * g.q_z + (row0 + (lane & 31)) * g.q_s + col : nullptr;
   typename S::frag fq[S::NF];
 #pragma unroll
@@ -302,42 +328,45 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i) request(t0 + i, i);
     int slot = 0, free = STAGES - 1;
-    for (int t = t0; t < t1; ++t) {
+    auto step = [&](int t, auto follow) {
       wait_and_barrier<(STAGES - 2) * LOADS>();
       request(t + STAGES - 1, free);
-      T* const tiles = smem + slot * (2 * TILE);
+      T* const kt = smem + slot * (2 * TILE);
+      T* const vt = kt + TILE;
       free = slot;
       slot = slot == STAGES - 1 ? 0 : slot + 1;
-      const T* const kt = tiles;
-      T* const vt = tiles + TILE;
       if (decltype(clean)::value) {
         clean_tile<T, D, S::TB>(vt, tid, THREADS);
         __syncthreads();
       }
-      const int key0 = t * S::TB;
 #pragma unroll 1
       for (int i = 0; i < NB; ++i) {
-        const int kb = key0 + 32 * i;
+        const int kb = t * S::TB + 32 * i;
         if (kb >= wr.hi_max || kb + 32 <= wr.lo_min) continue;
-        f16v x[1];
-        x[0] = at.first(kt + i * 32 * D, fq, all16(0.f));
+        f16v x = at.first(kt + i * 32 * D, fq, all16(0.f));
         const int k0 = kb + ((lane >> 5) << 2);
-        if (EXTRA) shape_scores(g, x[0], slope2, [&](int e) { return distance(range.pos, k0 + acc_row(e, 0)); });
-        const bool inside = kb >= wr.lo_max && kb + 32 <= wr.hi_min;
-        const unsigned from = k0 - range.lo, len = range.hi - range.lo;
-        if (!inside) {
+        if (EXTRA) shape_scores(g, x, slope2, [&](int e) { return distance(range.pos, k0 + acc_row(e, 0)); });
+        if (!(kb >= wr.lo_max && kb + 32 <= wr.hi_min)) {
+          const unsigned from = k0 - range.lo, len = range.hi - range.lo;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) x[0][e] = from + acc_row(e, 0) < len ? x[0][e] : -INFINITY;
+          for (int e = 0; e < 16; ++e) x[e] = from + acc_row(e, 0) < len ? x[e] : -INFINITY;
         }
-        z.take(x, unit.mult);
-        at.second(vt + i * 32 * D, x[0], z.o);
+        z.template take<decltype(follow)::value>(x, unit.mult);
+        at.second(vt + i * 32 * D, x, z.o);
       }
+    };
+    // the reference follows the maximum until every row has met a key; all the way on the second walk, and where scores fall with the distance
+    int t = t0;
+    for (bool met = false; t < t1 && !met; ++t) {
+      step(t, std::true_type());
+      met = !(EXTRA && g.slopes) && !__any(range.hi > range.lo && z.m == -INFINITY);
     }
+    for (; t < t1; ++t) step(t, clean);
     wait_and_barrier<0>();
     z.l += other_half(z.l);
   };
   walk(std::false_type());
-  const bool again = block_any(there && finite_of(z.l) && not_finite(z.o), w, lane, (int*)(smem + 2 * STAGES * TILE) - NWV);
+  const bool again = block_any(there && z.l == z.l && (z.l == INFINITY || not_finite(z.o)), w, lane, (int*)(smem + 2 * STAGES * TILE) - NWV);
   if (again) walk(std::true_type());
   const bool some = range.hi > range.lo;
   const float inv = some ? 1.f / z.l : 0.f;
@@ -368,7 +397,8 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
   if ((g.total & 7u) == 0u) lin = (lin & 7u) * (g.total >> 3) + (lin >> 3);
   const int pairs = g.group * g.q_len;
   const unsigned ncg = (pairs + 31) / 32, cg = lin % ncg, split = lin / ncg % g.splits, grp = lin / ncg / g.splits;
-  const int kh = grp % g.kv_heads, b = grp / g.kv_heads % g.seqs, r = grp / g.kv_heads / g.seqs;
+  const group_id id = place_group(grp, g, g.by_kv_heads);
+  const int kh = id.h, b = id.b, r = id.r;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int pair = cg * 32 + (lane & 31);
   const bool there = pair < pairs;
@@ -401,33 +431,38 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
     z.reset();
     int stage = 0;
     if (ts + w < te) request(ts + w, 0);
-    for (int t = ts + w; t < te; t += NW, stage ^= 1) {
+    auto step = [&](int t, auto follow) {
       wave_fence();                        // the other stage's tiles have been read
       request(t + NW, stage ^ 1);
       asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(IN_FLIGHT) : "memory");
       T* const kt = mine + stage * (2 * TILE);
+      stage ^= 1;
       if (decltype(clean)::value) {
         clean_tile<T, D, 32>(kt + TILE, lane, 64);
         wave_fence();
       }
-      f16v x[1];
-      x[0] = at.first(kt, fq, all16(0.f));
+      f16v x = at.first(kt, fq, all16(0.f));
       const int k0 = t * 32 + ((lane >> 5) << 2);
-      if (EXTRA) shape_scores(g, x[0], slope2, [&](int e) { return distance(range.pos, k0 + acc_row(e, 0)); });
-      const unsigned from = k0 - range.lo, len = range.hi - range.lo;
-      const bool inside = t * 32 >= wr.lo_max && t * 32 + 32 <= wr.hi_min;
-      if (!inside) {
+      if (EXTRA) shape_scores(g, x, slope2, [&](int e) { return distance(range.pos, k0 + acc_row(e, 0)); });
+      if (!(t * 32 >= wr.lo_max && t * 32 + 32 <= wr.hi_min)) {
+        const unsigned from = k0 - range.lo, len = range.hi - range.lo;
 #pragma unroll
-        for (int e = 0; e < 16; ++e) x[0][e] = from + acc_row(e, 0) < len ? x[0][e] : -INFINITY;
+        for (int e = 0; e < 16; ++e) x[e] = from + acc_row(e, 0) < len ? x[e] : -INFINITY;
       }
-      z.take(x, unit.mult);
-      at.second(kt + TILE, x[0], z.o);
+      z.template take<decltype(follow)::value>(x, unit.mult);
+      at.second(kt + TILE, x, z.o);
+    };
+    int t = ts + w;
+    for (bool met = false; t < te && !met; t += NW) {
+      step(t, std::true_type());
+      met = !(EXTRA && g.slopes) && !__any(range.hi > range.lo && z.m == -INFINITY);
     }
+    for (; t < te; t += NW) step(t, clean);
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
     z.l += other_half(z.l);
   };
   walk(std::false_type());
-  const bool again = __any(there && finite_of(z.l) && not_finite(z.o));
+  const bool again = __any(there && z.l == z.l && (z.l == INFINITY || not_finite(z.o)));
   if (again) walk(std::true_type());
 
   // join the wavefronts
@@ -531,9 +566,10 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
   __shared__ __attribute__((aligned(1024))) T smem[2 * STAGES * TILE];     // keys and values
   const unsigned lin = blockIdx.y * gridDim.x + blockIdx.x;
   if (lin >= g.total) return;
-  const unsigned nx = (g.q_len + RB - 1) / RB;
-  const block_id blk = place_block(lin, g.total, nx, g.heavy_first);
-  const int h = blk.grp % g.heads, b = blk.grp / g.heads % g.seqs, r = blk.grp / g.heads / g.seqs;
+  const unsigned nx = g.by_nx.d;
+  const block_id blk = place_block(lin, g);
+  const group_id id = place_group(blk.grp, g, g.by_heads);
+  const int h = id.h, b = id.b, r = id.r;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int wq0 = (int)(nx - 1 - blk.x) * RB + w * WR, qi = wq0 + (lane & 31);
   const bool there = qi < g.q_len;
@@ -541,26 +577,24 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
   const block_range br = block_range_of(g, range, there, wq0 - w * WR, w, lane, (int*)(smem + 2 * TILE));
   const wave_range wr = br.own;
   const int64_t rows = (int64_t)g.seqs * g.q_len, row0 = (int64_t)b * g.q_len + wq0, row = row0 + (lane & 31);
-  const int64_t col = (int64_t)h * g.d, kcol = (int64_t)(h / g.group) * g.d, stat = ((int64_t)r * g.heads + h) * rows + row;
+  const int64_t col = (int64_t)h * g.d, kcol = (int64_t)over(h, g.by_group) * g.d, stat = ((int64_t)r * g.heads + h) * rows + row;
   const bool some = range.hi > range.lo;
   const T* const own = some ? (const T*)g.q + r * g.q_z + row * g.q_s + col : nullptr;
   const T* const own_do = some ? (const T*)g.dout + r * g.do_z + row * g.do_s + col : nullptr;
   const T* const own_o = some ? (const T*)g.o + r * g.o_z + row * g.o_s + col : nullptr;
   typename S::frag fq[S::NF], fdo[S::NF];
-  float ndot = 0.f;                        // minus the row's dot, half of its columns a half-wavefront
+  // minus the row's dot, from out as it is stored, summed as the products below sum: a row that attends one key has dz = 0 to the bit
+  f16v both = all16(0.f);
 #pragma unroll
   for (int i = 0; i < S::NF; ++i) {
     fq[i] = own_frag<T, D, WHOLE>(own, i, g.d, lane);
     fdo[i] = own_frag<T, D, WHOLE>(own_do, i, g.d, lane);
-    const typename S::frag fo = own_frag<T, D, WHOLE>(own_o, i, g.d, lane);
-#pragma unroll
-    for (int e = 0; e < S::E; ++e) ndot = __builtin_fmaf(-(float)fdo[i][e], (float)fo[e], ndot);
+    both = S::product(own_frag<T, D, WHOLE>(own_o, i, g.d, lane), fdo[i], both);
   }
-  ndot += other_half(ndot);
+  float ndot = -diagonal(both, lane);
   const float lse2 = some ? g.lse_in[stat] * kLog2e : INFINITY;
   if (there && lane < 32) {
     g.lse2[stat] = lse2;
-    g.dot[stat] = ndot;
     if (h == 0) {
       g.lo[r * rows + row] = range.lo;
       g.hi[r * rows + row] = range.hi;
@@ -578,15 +612,19 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
   const int hi = br.hi, t0 = br.lo / S::TB, t1 = (hi + S::TB - 1) / S::TB;
 
   f16v dq[S::ND];                          // [column][query]
+  // sum over the keys of p (dp - dot): what the dot lacks for out's rounding, since the p sum to 1
+  float lack = 0.f;
   // (every request is as many loads, of zeros behind the last tile, so that a wait can count them)
   auto request = [&](int t, int slot) {
     T* const to = smem + slot * (2 * TILE);
     keys.load((int64_t)t * S::TB, t < t1 ? hi - t * S::TB : 0, to);
     vals.load((int64_t)t * S::TB, t < t1 ? hi - t * S::TB : 0, to + TILE);
   };
-  auto walk = [&](auto clean) {
+  // clean: zeros for what is not finite; dots: no more than `lack`
+  auto walk = [&](auto clean, auto dots) {
 #pragma unroll
     for (int i = 0; i < S::ND; ++i) dq[i] = all16(0.f);
+    lack = 0.f;
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i) request(t0 + i, i);
     int slot = 0, free = STAGES - 1;
@@ -605,24 +643,41 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
         const int key0 = t * S::TB + 32 * i;
         if (key0 >= wr.hi_max || key0 + 32 <= wr.lo_min) continue;
         const T* const kt = tiles + i * 32 * D;
-        f16v x = at.first(kt, fq, all16(0.f)), dp = at.first(kt + TILE, fdo, all16(ndot));
+        f16v x = at.first(kt, fq, all16(0.f)), dp = at.first(kt + TILE, fdo, all16(0.f)), bend;
         const int k0 = key0 + ((lane >> 5) << 2);
-        if (EXTRA) shape_scores_back(g, x, dp, slope2, [&](int e) { return distance(range.pos, k0 + acc_row(e, 0)); });
+        if (EXTRA) shape_scores_back(g, x, bend, slope2, [&](int e) { return distance(range.pos, k0 + acc_row(e, 0)); });
 #pragma unroll
-        for (int e = 0; e < 16; ++e) dp[e] *= exp2_fast(__builtin_fmaf(x[e], c, -lse2));
-        const bool inside = key0 >= wr.lo_max && key0 + 32 <= wr.hi_min;
-        const unsigned from = k0 - range.lo, len = range.hi - range.lo;
-        if (!inside) {
+        for (int e = 0; e < 16; ++e) dp[e] = (dp[e] + ndot) * exp2_fast(__builtin_fmaf(x[e], c, -lse2));
+        if (!(key0 >= wr.lo_max && key0 + 32 <= wr.hi_min)) {
+          const unsigned from = k0 - range.lo, len = range.hi - range.lo;
 #pragma unroll
-          for (int e = 0; e < 16; ++e) dp[e] = from + acc_row(e, 0) < len ? dp[e] : 0.f;
+          for (int e = 0; e < 16; ++e) {
+            const bool seen = from + acc_row(e, 0) < len;
+            dp[e] = seen ? dp[e] : 0.f;
+            if (EXTRA) bend[e] = seen ? bend[e] : 0.f;
+          }
         }
-        at.second(kt, dp, dq);
+#pragma unroll
+        for (int e = 0; e < 16; ++e) {
+          lack += dp[e];
+          if (EXTRA) dp[e] *= bend[e];
+        }
+        if (!decltype(dots)::value) at.second_in_two(kt, dp, dq);
       }
     }
     wait_and_barrier<0>();
   };
-  walk(std::false_type());
-  if (block_any(some && finite_of(lse2) && not_finite(dq), w, lane, (int*)(smem + 2 * STAGES * TILE) - NWV)) walk(std::true_type());
+  // Few keys: a dot that is off by out's rounding is off by as much in all of them, and the sum of dz k does not average that away (two keys: dq off by 2.4 times its own
+  // rounding): the dots first, then.  Many: they do (1.1 times), with dz in two bfloat16 parts (1.5 in one).
+  if (sizeof(T) == 2 && t1 - t0 <= 3) {
+    walk(std::false_type(), std::true_type());
+    ndot -= lack + other_half(lack);
+    __syncthreads();
+  }
+  walk(std::false_type(), std::false_type());
+  if (block_any(some && finite_of(lse2) && not_finite(dq), w, lane, (int*)(smem + 2 * STAGES * TILE) - NWV)) walk(std::true_type(), std::false_type());
+  lack += other_half(lack);
+  if (there && lane < 32) g.dot[stat] = ndot - lack;
 #pragma unroll
   for (int i = 0; i < S::ND; ++i)
 #pragma unroll
@@ -643,10 +698,11 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
   __shared__ int ends[2 * NWV];
   unsigned lin = blockIdx.y * gridDim.x + blockIdx.x;
   if (lin >= g.total) return;
-  const unsigned nx = (g.kv_len + RB - 1) / RB, split = g.splits > 1 ? lin % g.splits : 0;
+  const unsigned split = g.splits > 1 ? lin % g.splits : 0;
   if (g.splits > 1) lin /= g.splits;
-  const block_id blk = place_block(lin, g.total / g.splits, nx, g.heavy_first);
-  const int kh = blk.grp % g.kv_heads, b = blk.grp / g.kv_heads % g.seqs, r = blk.grp / g.kv_heads / g.seqs;
+  const block_id blk = place_block(lin, g);
+  const group_id id = place_group(blk.grp, g, g.by_kv_heads);
+  const int kh = id.h, b = id.b, r = id.r;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int k0 = blk.x * RB, wk0 = k0 + w * WR, key = wk0 + (lane & 31);
   const int n_groups = (g.q_len + 31) / 32;
@@ -748,24 +804,17 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
         if (gr.lo_min >= wk0 + 32 || gr.hi_max <= wk0) continue;
         const T* const qt = at_tiles + i * 32 * D;
         const int* const st = at_stats + 32 * i + ((lane >> 5) << 2);
-        f16v dp;
+        f16v x = at.first(qt, fk, all16(0.f)), dp = at.first(qt + TILE, fv, all16(0.f)), bend;
+        if (EXTRA) shape_scores_back(g, x, bend, slope2, [&](int e) { return distance(st[4 * S::TB + acc_row(e, 0)], key); });
 #pragma unroll
         for (int e4 = 0; e4 < 4; ++e4) {
-          const f4v nd = *reinterpret_cast<const f4v*>(st + S::TB + 8 * e4);
-#pragma unroll
-          for (int u = 0; u < 4; ++u) dp[4 * e4 + u] = nd[u];
-        }
-        f16v x = at.first(qt, fk, all16(0.f));
-        dp = at.first(qt + TILE, fv, dp);
-        if (EXTRA) shape_scores_back(g, x, dp, slope2, [&](int e) { return distance(st[4 * S::TB + acc_row(e, 0)], key); });
-#pragma unroll
-        for (int e4 = 0; e4 < 4; ++e4) {
-          const f4v l2 = *reinterpret_cast<const f4v*>(st + 8 * e4);
+          const f4v l2 = *reinterpret_cast<const f4v*>(st + 8 * e4), nd = *reinterpret_cast<const f4v*>(st + S::TB + 8 * e4);
 #pragma unroll
           for (int u = 0; u < 4; ++u) {
             const int e = 4 * e4 + u;
             x[e] = exp2_fast(__builtin_fmaf(x[e], c, -l2[u]));
-            dp[e] *= x[e];
+            dp[e] = (dp[e] + nd[u]) * x[e];
+            if (EXTRA) dp[e] *= bend[e];
           }
         }
         const bool inside = wk0 >= gr.lo_max && wk0 + 32 <= gr.hi_min;
@@ -811,7 +860,7 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
   if (g.splits == 1) {
     put((T*)g.dk + r * g.dk_z + row0 * g.dk_s + kcol, (T*)g.dv + r * g.dv_z + row0 * g.dv_s + kcol, g.dk_s, g.dv_s, std::integral_constant<bool, WHOLE>());
   } else {
-    float* const to = g.part + (((int64_t)split * (g.total / g.splits / nx) + blk.grp) * g.kv_len + wk0) * (2 * D);
+    float* const to = g.part + (((int64_t)split * g.by_groups.d + blk.grp) * g.kv_len + wk0) * (2 * D);
     put(to, to + D, 2 * D, 2 * D, std::false_type());
   }
 }
@@ -847,6 +896,7 @@ template <typename A> attend_args common_args(const A& a) {
   g.d = a.head_dim; g.causal = a.causal; g.window = a.window; g.splits = 1;
   g.scale = (float)a.scale; g.c = (float)(a.scale * 1.4426950408889634); g.cap2 = (float)(a.softcap * 1.4426950408889634);
   g.inv_cap = a.softcap > 0 ? (float)(1.0 / a.softcap) : 0.f;
+  g.by_heads = divisor_of(a.heads); g.by_kv_heads = divisor_of(a.kv_heads); g.by_seqs = divisor_of(a.seqs); g.by_group = divisor_of(g.group);
   // bfloat16 inputs: a score off by 1e-7 of a cap up to 1000 moves p by no more than 2^-13 of itself, where its rounding takes 2^-9
   g.close = a.dtype == HDET_TYPE_F32 || a.softcap > 1000.0;
   return g;
@@ -855,6 +905,15 @@ template <typename A> attend_args common_args(const A& a) {
 bool whole(const hdet_rows& m, int size, int d) {
   const int64_t mask = 16 / size - 1;
   return ((uintptr_t)m.dev & 15) == 0 && ((m.row_stride | m.replica_stride | d) & mask) == 0 && m.row_stride < (int64_t)1 << 23;
+}
+// `nx` row blocks of each group
+void set_blocks(attend_args& g, unsigned nx, unsigned groups) {
+  g.total = nx * groups;
+  g.by_nx = divisor_of(nx);
+  g.by_groups = divisor_of(groups);
+  g.by_own = divisor_of(groups >> 3);
+  // longest row blocks first while there are few rounds of them
+  g.heavy_first = nx && g.total <= (nx >= 8 ? 16u : 8u) * (unsigned)hdet_compute_units();
 }
 dim3 grid_of(unsigned blocks) {
   const unsigned x = blocks < (1u << 20) ? blocks : 1u << 20;
@@ -877,7 +936,6 @@ template <typename F> void with_shape(int dtype, int d, bool ex, bool wh, F f) {
   if (dtype == HDET_TYPE_BF16) with_d(uint16_t());
   else with_d(float());
 }
-bool heavy_first(unsigned total, unsigned nx) { return total <= (nx >= 8 ? 16u : 8u) * (unsigned)hdet_compute_units(); }
 
 // Parts of the keys for few queries, 0: the queries fill the chip
 int few_splits(int n, int seqs, int q_len, int kv_len, int heads, int kv_heads) {
@@ -949,8 +1007,7 @@ hipError_t hdet_launch_attend(const hdet_attention_args& a, hipStream_t s) {
     return hipGetLastError();
   }
   const unsigned nx = (a.q_len + RB - 1) / RB;
-  g.total = nx * (unsigned)a.n_replicas * a.seqs * a.heads;
-  g.heavy_first = heavy_first(g.total, nx);
+  set_blocks(g, nx, (unsigned)a.n_replicas * a.seqs * a.heads);
   with_shape(a.dtype, a.head_dim, extra(a), wh, [&](auto t, auto d, auto ex, auto w) {
     hipLaunchKernelGGL((attend_kernel<decltype(t), d, ex, w>), grid_of(g.total), dim3(THREADS), 0, s, g);
   });
@@ -977,11 +1034,9 @@ hipError_t hdet_launch_attend_backward(const hdet_attention_grad_args& a, hipStr
   const unsigned nq = (a.q_len + RB - 1) / RB, nk = (a.kv_len + RB - 1) / RB;
   with_shape(a.dtype, a.head_dim, extra(a), wh, [&](auto t, auto d, auto ex, auto w) {
     typedef decltype(t) T;
-    g.total = nq * (unsigned)a.n_replicas * a.seqs * a.heads;
-    g.heavy_first = nq && heavy_first(g.total, nq);
+    set_blocks(g, nq, (unsigned)a.n_replicas * a.seqs * a.heads);
     if (g.total) hipLaunchKernelGGL((attend_dq_kernel<T, d, ex, w>), grid_of(g.total), dim3(THREADS), 0, s, g);
-    g.total = nk * (unsigned)a.n_replicas * a.seqs * a.kv_heads;
-    g.heavy_first = nk && heavy_first(g.total, nk);
+    set_blocks(g, nk, (unsigned)a.n_replicas * a.seqs * a.kv_heads);
     g.splits = splits;
     g.total *= splits;
     if (g.total) hipLaunchKernelGGL((attend_dkv_kernel<T, d, ex, w>), grid_of(g.total), dim3(THREADS), 0, s, g);

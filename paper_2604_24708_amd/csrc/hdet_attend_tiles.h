@@ -81,7 +81,27 @@ template <int D> struct shape<uint16_t, D> {
       }
     }
   }
-  static __device__ __forceinline__ float rounded(float x) { return (float)(__bf16)x; }
+  // the same with x in two parts, 16 bits of it
+  __device__ __forceinline__ void second_in_two(const uint16_t* tile, const f16v& x, f16v (&acc)[ND]) const {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      frag f, rest;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        f[i] = (__bf16)x[8 * j + i];
+        rest[i] = (__bf16)(x[8 * j + i] - (float)f[i]);
+      }
+#pragma unroll
+      for (int dt = 0; dt < ND; ++dt) {
+        const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s4v __attribute__((address_space(3)))*)(tile + 16 * j * D + t[dt][0]));
+        const s4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s4v __attribute__((address_space(3)))*)(tile + 16 * j * D + t[dt][1]));
+        const s8v both = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+        acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(frag, both), f, acc[dt], 0, 0, 0);
+        acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(frag, both), rest, acc[dt], 0, 0, 0);
+      }
+    }
+  }
+  static __device__ __forceinline__ f16v product(const frag& a, const frag& b, const f16v& acc) { return __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, b, acc, 0, 0, 0); }
 };
 // fp32: v_mfma_f32_32x32x2_f32; a fragment is 4 columns, and step i of them contracts column i of both half-wavefronts' chunks
 template <int D> struct shape<float, D> {
@@ -116,7 +136,12 @@ template <int D> struct shape<float, D> {
 #pragma unroll
       for (int dt = 0; dt < ND; ++dt) acc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(tile[(e >> 2) * 8 * D + t[dt][e & 3]], x[e], acc[dt], 0, 0, 0);
   }
-  static __device__ __forceinline__ float rounded(float x) { return x; }
+  __device__ __forceinline__ void second_in_two(const float* tile, const f16v& x, f16v (&acc)[ND]) const { second(tile, x, acc); }
+  static __device__ __forceinline__ f16v product(const frag& a, const frag& b, f16v acc) {
+#pragma unroll
+    for (int u = 0; u < 4; ++u) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[u], b[u], acc, 0, 0, 0);
+    return acc;
+  }
 };
 
 template <int N> __device__ __forceinline__ bool not_finite(const f16v (&x)[N]) {
@@ -213,6 +238,15 @@ template <typename T, int D, int ROWS, int NW, bool WHOLE> struct tile_loader {
     }
   }
 };
+
+// Element (l % 32, l % 32) of an accumulator block
+__device__ __forceinline__ float diagonal(const f16v& x, int lane) {
+  float r = 0.f;
+#pragma unroll
+  for (int e = 0; e < 16; ++e) r = acc_row(e, lane) == (lane & 31) ? x[e] : r;
+  const float o = other_half(r);
+  return (lane >> 2 & 1) == lane >> 5 ? r : o;
+}
 
 // A lane's fragment i of its own row at p (null: zeros)
 template <typename T, int D, bool WHOLE> __device__ __forceinline__ typename shape<T, D>::frag own_frag(const T* p, int i, int d, int lane) {

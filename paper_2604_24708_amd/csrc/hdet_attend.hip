@@ -688,8 +688,9 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
 // ---------------------------------------------------------------------------------------------
 // backward, step 2: dk and dv; block = 128 keys of a key head, walks over the query tiles of the heads that share it
 // ---------------------------------------------------------------------------------------------
-template <typename T, int D, bool EXTRA> constexpr int dkv_waves() { return D == 128 ? 1 : sizeof(T) == 2 && !EXTRA ? 3 : 2; }
-template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds__(THREADS, (dkv_waves<T, D, EXTRA>())) void attend_dkv_kernel(const attend_args g) {
+template <typename T, int D, bool EXTRA, bool TWO> constexpr int dkv_waves() { return D == 128 ? 1 : sizeof(T) == 2 && !EXTRA && !TWO ? 3 : 2; }
+// TWO: dk from dz in two bfloat16 parts
+template <typename T, int D, bool EXTRA, bool WHOLE, bool TWO> __global__ __launch_bounds__(THREADS, (dkv_waves<T, D, EXTRA, TWO>())) void attend_dkv_kernel(const attend_args g) {
   typedef shape<T, D> S;
   constexpr int TILE = S::TB * D, NB = S::TB / 32, STATS = 5 * S::TB;      // lse2, dot, lo, hi, position
   constexpr int LOADS = 2 * tile_loader<T, D, S::TB, NWV, WHOLE>::NI + 2;
@@ -831,7 +832,8 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
           }
         }
         at.second(qt + TILE, x, dv);
-        at.second(qt, dp, dk);
+        if (TWO) at.second_in_two(qt, dp, dk);
+        else at.second(qt, dp, dk);
       }
     }
     wait_and_barrier<0>();
@@ -1031,6 +1033,9 @@ hipError_t hdet_launch_attend_backward(const hdet_attention_grad_args& a, hipStr
   const int splits = dkv_splits(a.n_replicas, a.seqs, a.q_len, a.kv_len, a.heads, a.kv_heads);
   bool wh = true;
   for (const hdet_rows* m : {&a.q, &a.k, &a.v, &a.out, &a.dout, &a.dq, &a.dk, &a.dv}) wh = wh && (!m->dev || whole(*m, size, a.head_dim));
+  // few queries: dk is made of few dz, whose rounding in one part shows (dk off by up to 1.48 times its own rounding in small tensors, 1.42 in large ones; 8 x 16 x 256
+  // queries in two parts: the backward pass 125 -> 152 us)
+  const bool two = a.dtype == HDET_TYPE_BF16 && (int64_t)((a.q_len + 63) / 64) * g.group <= 3;
   const unsigned nq = (a.q_len + RB - 1) / RB, nk = (a.kv_len + RB - 1) / RB;
   with_shape(a.dtype, a.head_dim, extra(a), wh, [&](auto t, auto d, auto ex, auto w) {
     typedef decltype(t) T;
@@ -1039,7 +1044,8 @@ hipError_t hdet_launch_attend_backward(const hdet_attention_grad_args& a, hipStr
     set_blocks(g, nk, (unsigned)a.n_replicas * a.seqs * a.kv_heads);
     g.splits = splits;
     g.total *= splits;
-    if (g.total) hipLaunchKernelGGL((attend_dkv_kernel<T, d, ex, w>), grid_of(g.total), dim3(THREADS), 0, s, g);
+    if (g.total && two) hipLaunchKernelGGL((attend_dkv_kernel<T, d, ex, w, sizeof(T) == 2>), grid_of(g.total), dim3(THREADS), 0, s, g);
+    else if (g.total) hipLaunchKernelGGL((attend_dkv_kernel<T, d, ex, w, false>), grid_of(g.total), dim3(THREADS), 0, s, g);
     if (g.total && splits > 1)
       hipLaunchKernelGGL((attend_dkv_join_kernel<T, d>), grid_of((unsigned)(((int64_t)a.n_replicas * a.seqs * a.kv_heads * a.kv_len * d + THREADS - 1) / THREADS)), dim3(THREADS), 0, s, g);
   });

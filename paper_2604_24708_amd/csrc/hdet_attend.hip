@@ -151,8 +151,8 @@ __device__ __forceinline__ wave_range plain_range_of(const attend_args& g, int i
   if (a.hi <= a.lo) return {0, INT_MAX, 0, b.hi};
   return {a.lo, b.lo, a.hi, b.hi};
 }
-// ... of a wavefront's 32 queries, the lanes' ranges given, and (lo, hi) of the block's 128, through LDS that nothing else uses before the next barrier but one
-struct block_range { wave_range own; int lo, hi; };
+// ... of a wavefront's 32 queries, the lanes' ranges given, and (lo, hi) of the block's 128 from q0 on, through LDS that nothing else uses before the next barrier but one
+struct block_range { wave_range own; int lo, hi, pairs; };                // pairs: of the block's rows, about
 __device__ __forceinline__ block_range block_range_of(const attend_args& g, const key_range& k, bool there, int q0, int w, int lane, int* ends) {
   block_range b;
   if (!g.pos && !g.first && !g.end) {
@@ -160,13 +160,19 @@ __device__ __forceinline__ block_range block_range_of(const attend_args& g, cons
     const wave_range all = plain_range_of(g, q0, RB);
     b.lo = all.lo_min;
     b.hi = all.hi_max;
+    const key_range a = range_of(g, 0, 0, q0), z = range_of(g, 0, 0, min(q0 + RB, g.q_len) - 1);
+    b.pairs = (a.hi - a.lo + z.hi - z.lo) / 2 * min(RB, g.q_len - q0);
   } else {
     b.own = wave_range_of(k, there);
     if (lane == 0) {
       ends[w] = b.own.lo_min;
       ends[NWV + w] = b.own.hi_max;
     }
+    float pairs = there ? (float)(k.hi - k.lo) : 0.f;
+    pairs = hdet_wave_sum(pairs) * 0.5f;   // (each row is in two lanes)
+    if (lane == 0) ends[2 * NWV + w] = (int)fminf(pairs, 1e8f);
     __syncthreads();
+    b.pairs = __builtin_amdgcn_readfirstlane(ends[8] + ends[9] + ends[10] + ends[11]);
     b.lo = __builtin_amdgcn_readfirstlane(min(min(ends[0], ends[1]), min(ends[2], ends[3])));
     b.hi = __builtin_amdgcn_readfirstlane(max(max(ends[4], ends[5]), max(ends[6], ends[7])));
   }
@@ -184,11 +190,19 @@ __device__ __forceinline__ bool block_any(bool yes, int w, int lane, int* lds) {
 
 // Scores of a block from its raw products: x such that the score is (x + shift) mult log2 units (score_units).  With a cap x is tanh - 1, exact enough unless
 // small scores are read off a very large cap (close).  dist(e): |position - key| of element e.
+// EXTRA says how much of it is asked for: nothing (a product with c), a cap alone, anything.
+enum { kPlain = 0, kCapped = 1, kGeneral = 2 };
 struct score_units { float mult, shift; };
-__device__ __forceinline__ score_units units_of(const attend_args& g, bool extra) {
-  return !extra ? score_units{g.c, 0.f} : g.slopes || g.cap2 == 0.f ? score_units{1.f, 0.f} : score_units{g.cap2, g.close ? 0.f : 1.f};
+__device__ __forceinline__ score_units units_of(const attend_args& g, int extra) {
+  return extra == kCapped ? score_units{g.cap2, 1.f} : extra == kPlain ? score_units{g.c, 0.f} : g.slopes || g.cap2 == 0.f ? score_units{1.f, 0.f} : score_units{g.cap2, g.close ? 0.f : 1.f};
 }
-template <typename F> __device__ __forceinline__ void shape_scores(const attend_args& g, f16v& x, float slope2, F dist) {
+template <int EXTRA, typename F> __device__ __forceinline__ void shape_scores(const attend_args& g, f16v& x, float slope2, F dist) {
+  if (EXTRA == kCapped) {
+    const float s = 2.f * kLog2e * g.scale * g.inv_cap;
+#pragma unroll
+    for (int e = 0; e < 16; ++e) x[e] = tanh_less_1(x[e] * s);
+    return;
+  }
   if (g.cap2 > 0.f && !g.close) {
     const float s = 2.f * kLog2e * g.scale * g.inv_cap;
 #pragma unroll
@@ -215,8 +229,8 @@ template <typename F> __device__ __forceinline__ void shape_scores(const attend_
   }
 }
 // Backward: scores, in log2 units, from raw products; bend: the cap's derivative
-template <typename F> __device__ __forceinline__ void shape_scores_back(const attend_args& g, f16v& x, f16v& bend, float slope2, F dist) {
-  if (g.cap2 > 0.f && !g.close) {
+template <int EXTRA, typename F> __device__ __forceinline__ void shape_scores_back(const attend_args& g, f16v& x, f16v& bend, float slope2, F dist) {
+  if (EXTRA == kCapped || (g.cap2 > 0.f && !g.close)) {
     const float s = 2.f * kLog2e * g.scale * g.inv_cap;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
@@ -237,7 +251,7 @@ template <typename F> __device__ __forceinline__ void shape_scores_back(const at
 #pragma unroll
     for (int e = 0; e < 16; ++e) x[e] *= g.c;
   }
-  if (g.slopes) {
+  if (EXTRA == kGeneral && g.slopes) {
 #pragma unroll
     for (int e = 0; e < 16; ++e) x[e] = __builtin_fmaf(-slope2, dist(e), x[e]);
   }
@@ -286,8 +300,8 @@ template <int D> struct running {
 // ---------------------------------------------------------------------------------------------
 // forward: block = 128 queries of one (replica, sequence, head)
 // ---------------------------------------------------------------------------------------------
-template <typename T, int D, bool EXTRA> constexpr int forward_waves() { return sizeof(T) == 2 ? (D == 64 ? (EXTRA ? 3 : 4) : 2) : (D == 64 ? 2 : 1); }
-template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds__(THREADS, (forward_waves<T, D, EXTRA>())) void attend_kernel(const attend_args g) {
+template <typename T, int D, int EXTRA> constexpr int forward_waves() { return sizeof(T) == 2 ? (D == 64 ? (EXTRA ? 3 : 4) : 2) : (D == 64 ? 2 : 1); }
+template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__(THREADS, (forward_waves<T, D, EXTRA>())) void attend_kernel(const attend_args g) {
   typedef shape<T, D> S;
   constexpr int TILE = S::TB * D, NB = S::TB / 32, LOADS = 2 * tile_loader<T, D, S::TB, NWV, WHOLE>::NI;
   __shared__ __attribute__((aligned(1024))) T smem[2 * STAGES * TILE];     // keys and values
@@ -309,7 +323,7 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
   const tile_loader<T, D, S::TB, NWV, WHOLE> keys((const T*)g.k + r * g.k_z + (int64_t)b * g.kv_len * g.k_s + kcol, g.k_s, g.d, w, lane);
   const tile_loader<T, D, S::TB, NWV, WHOLE> vals((const T*)g.v + r * g.v_z + (int64_t)b * g.kv_len * g.v_s + kcol, g.v_s, g.d, w, lane);
   const S at(lane);
-  const float slope2 = EXTRA && g.slopes ? g.slopes[r * g.slopes_z + h] * kLog2e : 0.f;
+  const float slope2 = EXTRA == kGeneral && g.slopes ? g.slopes[r * g.slopes_z + h] * kLog2e : 0.f;
   const score_units unit = units_of(g, EXTRA);
   // (the block's ends pass through the second stage, which is requested behind a barrier)
   const block_range br = block_range_of(g, range, there, wq0 - w * WR, w, lane, (int*)(smem + 2 * TILE));
@@ -345,7 +359,7 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
         if (kb >= wr.hi_max || kb + 32 <= wr.lo_min) continue;
         f16v x = at.first(kt + i * 32 * D, fq, all16(0.f));
         const int k0 = kb + ((lane >> 5) << 2);
-        if (EXTRA) shape_scores(g, x, slope2, [&](int e) { return distance(range.pos, k0 + acc_row(e, 0)); });
+        if (EXTRA) shape_scores<EXTRA>(g, x, slope2, [&](int e) { return distance(range.pos, k0 + acc_row(e, 0)); });
         if (!(kb >= wr.lo_max && kb + 32 <= wr.hi_min)) {
           const unsigned from = k0 - range.lo, len = range.hi - range.lo;
 #pragma unroll
@@ -359,7 +373,7 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
     int t = t0;
     for (bool met = false; t < t1 && !met; ++t) {
       step(t, std::true_type());
-      met = !(EXTRA && g.slopes) && !__any(range.hi > range.lo && z.m == -INFINITY);
+      met = !(EXTRA == kGeneral && g.slopes) && !__any(range.hi > range.lo && z.m == -INFINITY);
     }
     for (; t < t1; ++t) step(t, clean);
     wait_and_barrier<0>();
@@ -388,7 +402,7 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
 // which its wavefronts take every NW-th tile of 32, each through LDS of its own.  Their results are joined in LDS, those of the parts by a second launch.
 // ---------------------------------------------------------------------------------------------
 template <typename T, int D> constexpr int few_waves() { return sizeof(T) == 4 && D == 128 ? 2 : 4; }
-template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds__((few_waves<T, D>() * 64)) void attend_few_kernel(const attend_args g) {
+template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__((few_waves<T, D>() * 64)) void attend_few_kernel(const attend_args g) {
   typedef shape<T, D> S;
   constexpr int NW = few_waves<T, D>(), TILE = 32 * D, P = D + 4;
   __shared__ __attribute__((aligned(1024))) T smem[NW * 4 * TILE];
@@ -414,7 +428,7 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
   const tile_loader<T, D, 32, 1, WHOLE> vals((const T*)g.v + r * g.v_z + (int64_t)b * g.kv_len * g.v_s + kcol, g.v_s, g.d, 0, lane);
   constexpr int IN_FLIGHT = 2 * tile_loader<T, D, 32, 1, WHOLE>::NI;
   const S at(lane);
-  const float slope2 = EXTRA && g.slopes ? g.slopes[r * g.slopes_z + h] * kLog2e : 0.f;
+  const float slope2 = EXTRA == kGeneral && g.slopes ? g.slopes[r * g.slopes_z + h] * kLog2e : 0.f;
   const score_units unit = units_of(g, EXTRA);
   // the union of the ranges in tiles, this block's part of them
   const int hi = wr.hi_max, lo = hi > 0 ? wr.lo_min : 0, t0 = lo / 32, t1 = (hi + 31) / 32, per = (t1 - t0 + g.splits - 1) / g.splits;
@@ -443,7 +457,7 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
       }
       f16v x = at.first(kt, fq, all16(0.f));
       const int k0 = t * 32 + ((lane >> 5) << 2);
-      if (EXTRA) shape_scores(g, x, slope2, [&](int e) { return distance(range.pos, k0 + acc_row(e, 0)); });
+      if (EXTRA) shape_scores<EXTRA>(g, x, slope2, [&](int e) { return distance(range.pos, k0 + acc_row(e, 0)); });
       if (!(t * 32 >= wr.lo_max && t * 32 + 32 <= wr.hi_min)) {
         const unsigned from = k0 - range.lo, len = range.hi - range.lo;
 #pragma unroll
@@ -455,7 +469,7 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
     int t = ts + w;
     for (bool met = false; t < te && !met; t += NW) {
       step(t, std::true_type());
-      met = !(EXTRA && g.slopes) && !__any(range.hi > range.lo && z.m == -INFINITY);
+      met = !(EXTRA == kGeneral && g.slopes) && !__any(range.hi > range.lo && z.m == -INFINITY);
     }
     for (; t < te; t += NW) step(t, clean);
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
@@ -560,7 +574,7 @@ template <typename T, int D> __global__ __launch_bounds__(THREADS) void attend_j
 // ---------------------------------------------------------------------------------------------
 // backward, step 1: dq, and what step 2 needs of the queries (row dots, statistics, ranges); block = 128 queries
 // ---------------------------------------------------------------------------------------------
-template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds__(THREADS, (sizeof(T) == 4 && D == 128 ? 1 : 2)) void attend_dq_kernel(const attend_args g) {
+template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__(THREADS, (sizeof(T) == 4 && D == 128 ? 1 : 2)) void attend_dq_kernel(const attend_args g) {
   typedef shape<T, D> S;
   constexpr int TILE = S::TB * D, NB = S::TB / 32, LOADS = 2 * tile_loader<T, D, S::TB, NWV, WHOLE>::NI;
   __shared__ __attribute__((aligned(1024))) T smem[2 * STAGES * TILE];     // keys and values
@@ -607,7 +621,7 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
   const tile_loader<T, D, S::TB, NWV, WHOLE> keys((const T*)g.k + r * g.k_z + (int64_t)b * g.kv_len * g.k_s + kcol, g.k_s, g.d, w, lane);
   const tile_loader<T, D, S::TB, NWV, WHOLE> vals((const T*)g.v + r * g.v_z + (int64_t)b * g.kv_len * g.v_s + kcol, g.v_s, g.d, w, lane);
   const S at(lane);
-  const float slope2 = EXTRA && g.slopes ? g.slopes[r * g.slopes_z + h] * kLog2e : 0.f;
+  const float slope2 = EXTRA == kGeneral && g.slopes ? g.slopes[r * g.slopes_z + h] * kLog2e : 0.f;
   const float c = EXTRA ? 1.f : g.c;
   const int hi = br.hi, t0 = br.lo / S::TB, t1 = (hi + S::TB - 1) / S::TB;
 
@@ -645,7 +659,7 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
         const T* const kt = tiles + i * 32 * D;
         f16v x = at.first(kt, fq, all16(0.f)), dp = at.first(kt + TILE, fdo, all16(0.f)), bend;
         const int k0 = key0 + ((lane >> 5) << 2);
-        if (EXTRA) shape_scores_back(g, x, bend, slope2, [&](int e) { return distance(range.pos, k0 + acc_row(e, 0)); });
+        if (EXTRA) shape_scores_back<EXTRA>(g, x, bend, slope2, [&](int e) { return distance(range.pos, k0 + acc_row(e, 0)); });
 #pragma unroll
         for (int e = 0; e < 16; ++e) dp[e] = (dp[e] + ndot) * exp2_fast(__builtin_fmaf(x[e], c, -lse2));
         if (!(key0 >= wr.lo_max && key0 + 32 <= wr.hi_min)) {
@@ -667,9 +681,9 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
     }
     wait_and_barrier<0>();
   };
-  // Few keys: a dot that is off by out's rounding is off by as much in all of them, and the sum of dz k does not average that away (two keys: dq off by 2.4 times its own
-  // rounding): the dots first, then.  Many: they do (1.1 times), with dz in two bfloat16 parts (1.5 in one).
-  if (sizeof(T) == 2 && t1 - t0 <= 3) {
+  // Few keys a row: a dot that is off by out's rounding is off by as much in all of them, and the sum of dz k does not average that away (two keys: dq off by 2.4 times its
+  // own rounding): the dots first, then.  Many: it does (1.1 to 1.3 times), with dz in two bfloat16 parts (1.5 in one).
+  if (sizeof(T) == 2 && br.pairs < 40 * min(RB, g.q_len - (wq0 - w * WR))) {
     walk(std::false_type(), std::true_type());
     ndot -= lack + other_half(lack);
     __syncthreads();
@@ -688,9 +702,9 @@ template <typename T, int D, bool EXTRA, bool WHOLE> __global__ __launch_bounds_
 // ---------------------------------------------------------------------------------------------
 // backward, step 2: dk and dv; block = 128 keys of a key head, walks over the query tiles of the heads that share it
 // ---------------------------------------------------------------------------------------------
-template <typename T, int D, bool EXTRA, bool TWO> constexpr int dkv_waves() { return D == 128 ? 1 : sizeof(T) == 2 && !EXTRA && !TWO ? 3 : 2; }
+template <typename T, int D, int EXTRA, bool TWO> constexpr int dkv_waves() { return D == 128 ? 1 : sizeof(T) == 2 && !EXTRA && !TWO ? 3 : 2; }
 // TWO: dk from dz in two bfloat16 parts
-template <typename T, int D, bool EXTRA, bool WHOLE, bool TWO> __global__ __launch_bounds__(THREADS, (dkv_waves<T, D, EXTRA, TWO>())) void attend_dkv_kernel(const attend_args g) {
+template <typename T, int D, int EXTRA, bool WHOLE, bool TWO> __global__ __launch_bounds__(THREADS, (dkv_waves<T, D, EXTRA, TWO>())) void attend_dkv_kernel(const attend_args g) {
   typedef shape<T, D> S;
   constexpr int TILE = S::TB * D, NB = S::TB / 32, STATS = 5 * S::TB;      // lse2, dot, lo, hi, position
   constexpr int LOADS = 2 * tile_loader<T, D, S::TB, NWV, WHOLE>::NI + 2;
@@ -785,7 +799,7 @@ template <typename T, int D, bool EXTRA, bool WHOLE, bool TWO> __global__ __laun
       free = slot;
       slot = slot == STAGES - 1 ? 0 : slot + 1;
       const int h = kh * g.group + j / tiles, t = t0 + j % tiles;
-      const float slope2 = EXTRA && g.slopes ? g.slopes[r * g.slopes_z + h] * kLog2e : 0.f;
+      const float slope2 = EXTRA == kGeneral && g.slopes ? g.slopes[r * g.slopes_z + h] * kLog2e : 0.f;
       if (decltype(clean)::value) {
         clean_tile<T, D, 2 * S::TB>(at_tiles, tid, THREADS);
         __syncthreads();
@@ -806,7 +820,7 @@ template <typename T, int D, bool EXTRA, bool WHOLE, bool TWO> __global__ __laun
         const T* const qt = at_tiles + i * 32 * D;
         const int* const st = at_stats + 32 * i + ((lane >> 5) << 2);
         f16v x = at.first(qt, fk, all16(0.f)), dp = at.first(qt + TILE, fv, all16(0.f)), bend;
-        if (EXTRA) shape_scores_back(g, x, bend, slope2, [&](int e) { return distance(st[4 * S::TB + acc_row(e, 0)], key); });
+        if (EXTRA) shape_scores_back<EXTRA>(g, x, bend, slope2, [&](int e) { return distance(st[4 * S::TB + acc_row(e, 0)], key); });
 #pragma unroll
         for (int e4 = 0; e4 < 4; ++e4) {
           const f4v l2 = *reinterpret_cast<const f4v*>(st + 8 * e4), nd = *reinterpret_cast<const f4v*>(st + S::TB + 8 * e4);
@@ -921,15 +935,21 @@ dim3 grid_of(unsigned blocks) {
   const unsigned x = blocks < (1u << 20) ? blocks : 1u << 20;
   return dim3(x, (blocks + x - 1) / x);
 }
-// scores that need more than a product with a constant (a scale of 0 or below turns the maximum around)
-template <typename A> bool extra(const A& a) { return a.softcap > 0 || a.slopes_dev || !(a.scale > 0); }
+// what scores need: more than a product with a constant, also where a scale of 0 or below turns the maximum around
+template <typename A> int extra(const A& a, const attend_args& g) {
+  return a.slopes_dev || !(a.scale > 0) || (a.softcap > 0 && g.close) ? kGeneral : a.softcap > 0 ? kCapped : kPlain;
+}
 
 // f(type, D, EXTRA, WHOLE); rows that are not whole pieces take the general scores too
-template <typename F> void with_shape(int dtype, int d, bool ex, bool wh, F f) {
+template <typename F> void with_shape(int dtype, int d, int ex, bool wh, F f) {
+  typedef std::integral_constant<int, kPlain> plain;
+  typedef std::integral_constant<int, kGeneral> general;
   auto with_flags = [&](auto t, auto dd) {
-    if (!wh) f(t, dd, std::true_type(), std::false_type());
-    else if (ex) f(t, dd, std::true_type(), std::true_type());
-    else f(t, dd, std::false_type(), std::true_type());
+    typedef std::integral_constant<int, sizeof(t) == 2 ? kCapped : kGeneral> capped;
+    if (!wh) f(t, dd, general(), std::false_type());
+    else if (ex == kGeneral) f(t, dd, general(), std::true_type());
+    else if (ex == kCapped) f(t, dd, capped(), std::true_type());
+    else f(t, dd, plain(), std::true_type());
   };
   auto with_d = [&](auto t) {
     if (d <= 64) with_flags(t, std::integral_constant<int, 64>());
@@ -1001,7 +1021,7 @@ hipError_t hdet_launch_attend(const hdet_attention_args& a, hipStream_t s) {
     g.splits = splits;
     g.part = (float*)a.workspace_dev;
     g.total = (unsigned)(groups * ((pairs + 31) / 32) * splits);
-    with_shape(a.dtype, a.head_dim, extra(a), wh, [&](auto t, auto d, auto ex, auto w) {
+    with_shape(a.dtype, a.head_dim, extra(a, g), wh, [&](auto t, auto d, auto ex, auto w) {
       typedef decltype(t) T;
       hipLaunchKernelGGL((attend_few_kernel<T, d, ex, w>), grid_of(g.total), dim3(few_waves<T, d>() * 64), 0, s, g);
       if (splits > 1) hipLaunchKernelGGL((attend_join_kernel<T, d>), grid_of((unsigned)((groups * pairs + NWV - 1) / NWV)), dim3(THREADS), 0, s, g);
@@ -1010,7 +1030,7 @@ hipError_t hdet_launch_attend(const hdet_attention_args& a, hipStream_t s) {
   }
   const unsigned nx = (a.q_len + RB - 1) / RB;
   set_blocks(g, nx, (unsigned)a.n_replicas * a.seqs * a.heads);
-  with_shape(a.dtype, a.head_dim, extra(a), wh, [&](auto t, auto d, auto ex, auto w) {
+  with_shape(a.dtype, a.head_dim, extra(a, g), wh, [&](auto t, auto d, auto ex, auto w) {
     hipLaunchKernelGGL((attend_kernel<decltype(t), d, ex, w>), grid_of(g.total), dim3(THREADS), 0, s, g);
   });
   return hipGetLastError();
@@ -1037,7 +1057,7 @@ hipError_t hdet_launch_attend_backward(const hdet_attention_grad_args& a, hipStr
   // queries in two parts: the backward pass 125 -> 152 us)
   const bool two = a.dtype == HDET_TYPE_BF16 && (int64_t)((a.q_len + 63) / 64) * g.group <= 3;
   const unsigned nq = (a.q_len + RB - 1) / RB, nk = (a.kv_len + RB - 1) / RB;
-  with_shape(a.dtype, a.head_dim, extra(a), wh, [&](auto t, auto d, auto ex, auto w) {
+  with_shape(a.dtype, a.head_dim, extra(a, g), wh, [&](auto t, auto d, auto ex, auto w) {
     typedef decltype(t) T;
     set_blocks(g, nq, (unsigned)a.n_replicas * a.seqs * a.heads);
     if (g.total) hipLaunchKernelGGL((attend_dq_kernel<T, d, ex, w>), grid_of(g.total), dim3(THREADS), 0, s, g);

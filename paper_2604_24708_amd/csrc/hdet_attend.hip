@@ -55,7 +55,8 @@ struct attend_args {
   float *lse2, *dot;                       // backward: [replica][head][row] lse log2 e (infinity for empty rows), minus sum_c do o
   int *lo, *hi, *pos_of;                   // backward: [replica][row] the rows' ranges and positions
   i4v* groups;                             // backward: [replica][sequence][32 queries] least and largest lo, least and largest hi
-  float* part;                             // few queries: results of the splits
+  float* part;                             // results of the splits
+  float* lacks;                            // backward: the row dots' parts of dq's splits
   const float* slopes;
   int64_t slopes_z;
   const int32_t *pos, *first, *end;
@@ -578,8 +579,10 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
   typedef shape<T, D> S;
   constexpr int TILE = S::TB * D, NB = S::TB / 32, LOADS = 2 * tile_loader<T, D, S::TB, NWV, WHOLE>::NI;
   __shared__ __attribute__((aligned(1024))) T smem[2 * STAGES * TILE];     // keys and values
-  const unsigned lin = blockIdx.y * gridDim.x + blockIdx.x;
+  unsigned lin = blockIdx.y * gridDim.x + blockIdx.x;
   if (lin >= g.total) return;
+  const unsigned split = g.splits > 1 ? lin % g.splits : 0;
+  if (g.splits > 1) lin /= g.splits;
   const unsigned nx = g.by_nx.d;
   const block_id blk = place_block(lin, g);
   const group_id id = place_group(blk.grp, g, g.by_heads);
@@ -607,7 +610,7 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
   }
   float ndot = -diagonal(both, lane);
   const float lse2 = some ? g.lse_in[stat] * kLog2e : INFINITY;
-  if (there && lane < 32) {
+  if (there && lane < 32 && split == 0) {
     g.lse2[stat] = lse2;
     if (h == 0) {
       g.lo[r * rows + row] = range.lo;
@@ -616,14 +619,16 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
     }
   }
   // rows of the 32 that there are not: never inside
-  if (h == 0 && lane == 0 && wq0 < g.q_len)
+  if (h == 0 && lane == 0 && wq0 < g.q_len && split == 0)
     g.groups[((int64_t)r * g.seqs + b) * ((g.q_len + 31) / 32) + wq0 / 32] = i4v{wr.lo_min, wq0 + 32 > g.q_len ? INT_MAX : wr.lo_max, wr.hi_min, wr.hi_max};
   const tile_loader<T, D, S::TB, NWV, WHOLE> keys((const T*)g.k + r * g.k_z + (int64_t)b * g.kv_len * g.k_s + kcol, g.k_s, g.d, w, lane);
   const tile_loader<T, D, S::TB, NWV, WHOLE> vals((const T*)g.v + r * g.v_z + (int64_t)b * g.kv_len * g.v_s + kcol, g.v_s, g.d, w, lane);
   const S at(lane);
   const float slope2 = EXTRA == kGeneral && g.slopes ? g.slopes[r * g.slopes_z + h] * kLog2e : 0.f;
   const float c = EXTRA ? 1.f : g.c;
-  const int hi = br.hi, t0 = br.lo / S::TB, t1 = (hi + S::TB - 1) / S::TB;
+  const int hi = br.hi, first = br.lo / S::TB, last = (hi + S::TB - 1) / S::TB;
+  // this block's part of the tiles
+  const int share = hi > 0 ? (last - first + g.splits - 1) / g.splits : 0, t0 = first + split * share, t1 = hi > 0 ? min(last, t0 + share) : t0;
 
   f16v dq[S::ND];                          // [column][query]
   // sum over the keys of p (dp - dot): what the dot lacks for out's rounding, since the p sum to 1
@@ -683,7 +688,7 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
   };
   // Few keys a row: a dot that is off by out's rounding is off by as much in all of them, and the sum of dz k does not average that away (two keys: dq off by 2.4 times its
   // own rounding): the dots first, then.  Many: it does (1.1 to 1.3 times), with dz in two bfloat16 parts (1.5 in one).
-  if (sizeof(T) == 2 && br.pairs < 40 * min(RB, g.q_len - (wq0 - w * WR))) {
+  if (sizeof(T) == 2 && g.splits == 1 && br.pairs < 40 * min(RB, g.q_len - (wq0 - w * WR))) {
     walk(std::false_type(), std::true_type());
     ndot -= lack + other_half(lack);
     __syncthreads();
@@ -691,12 +696,39 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
   walk(std::false_type(), std::false_type());
   if (block_any(some && finite_of(lse2) && not_finite(dq), w, lane, (int*)(smem + 2 * STAGES * TILE) - NWV)) walk(std::true_type(), std::false_type());
   lack += other_half(lack);
-  if (there && lane < 32) g.dot[stat] = ndot - lack;
+  if (there && lane < 32) {
+    if (g.splits == 1) g.dot[stat] = ndot - lack;
+    else g.lacks[(int64_t)split * g.n * g.heads * rows + stat] = split == 0 ? ndot - lack : -lack;
+  }
 #pragma unroll
   for (int i = 0; i < S::ND; ++i)
 #pragma unroll
     for (int e = 0; e < 16; ++e) dq[i][e] *= g.scale;
-  store_rows<T, D, WHOLE>(dq, (char*)smem + w * STRIP, (T*)g.dq + r * g.dq_z + row0 * g.dq_s + col, g.dq_s, g.q_len - wq0, g.d, lane);
+  char* const strip = (char*)smem + w * STRIP;
+  if (g.splits == 1) {
+    store_rows<T, D, WHOLE>(dq, strip, (T*)g.dq + r * g.dq_z + row0 * g.dq_s + col, g.dq_s, g.q_len - wq0, g.d, lane);
+  } else {
+    float* const to = g.part + (((int64_t)split * g.n + r) * g.heads + h) * rows * D + row0 * D;
+    store_rows<float, D, false>(dq, strip, to, D, g.q_len - wq0, g.d, lane);
+  }
+}
+
+// dq and the row dots from the splits' parts, [split][replica][head][row]
+template <typename T, int D> __global__ __launch_bounds__(THREADS) void attend_dq_join_kernel(const attend_args g) {
+  const int64_t rows = (int64_t)g.seqs * g.q_len, all = rows * g.heads * g.n, i = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * THREADS + threadIdx.x, stat = i / D;
+  const int col = (int)(i % D);
+  if (stat >= all) return;
+  if (col == 0) {
+    float dot = 0.f;
+    for (int s = 0; s < g.splits; ++s) dot += g.lacks[(int64_t)s * all + stat];
+    g.dot[stat] = dot;
+  }
+  if (col >= g.d) return;
+  float dq = 0.f;
+  for (int s = 0; s < g.splits; ++s) dq += g.part[((int64_t)s * all + stat) * D + col];
+  const int64_t row = stat % rows;
+  const int h = (int)(stat / rows % g.heads), r = (int)(stat / rows / g.heads);
+  hdet_st((T*)g.dq + r * g.dq_z + row * g.dq_s + (int64_t)h * g.d + col, dq);
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -971,19 +1003,28 @@ int few_splits(int n, int seqs, int q_len, int kv_len, int heads, int kv_heads) 
 }
 constexpr size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Parts of the heads' query tiles that a block of dk and dv takes, where there are few blocks
-int dkv_splits(int n, int seqs, int q_len, int kv_len, int heads, int kv_heads) {
-  const int64_t blocks = (int64_t)n * seqs * kv_heads * ((kv_len + RB - 1) / RB), cus = hdet_compute_units(), tiles = (int64_t)((q_len + 63) / 64) * (heads / kv_heads);
+// Parts of a block's walk in the backward pass, where there are fewer blocks than CUs: of `tiles` tiles, two at least a part
+int parts_of(int64_t blocks, int64_t tiles) {
   if (blocks == 0) return 1;
-  int64_t s = cus / blocks;
-  if (s > tiles / 2) s = tiles / 2;        // two tiles at least
+  int64_t s = hdet_compute_units() / blocks;
+  if (s > tiles / 2) s = tiles / 2;
   return (int)(s < 1 ? 1 : s > 16 ? 16 : s);
 }
+// .. over the keys for dq; over the query tiles of the heads that share a key head for dk and dv
+int dq_splits(int n, int seqs, int q_len, int kv_len, int heads) {
+  return parts_of((int64_t)n * seqs * heads * ((q_len + RB - 1) / RB), kv_len < 512 ? 1 : (kv_len + 63) / 64);
+}
+int dkv_splits(int n, int seqs, int q_len, int kv_len, int heads, int kv_heads) {
+  return parts_of((int64_t)n * seqs * kv_heads * ((kv_len + RB - 1) / RB), (int64_t)((q_len + 63) / 64) * (heads / kv_heads));
+}
 
-struct backward_layout { size_t lse2, dot, lo, hi, pos, groups, part, total; };
+struct backward_layout { size_t lse2, dot, lo, hi, pos, groups, lacks, part, total; };
 backward_layout layout_of(int n, int seqs, int q_len, int kv_len, int heads, int kv_heads, int d) {
   const size_t rows = (size_t)n * seqs * q_len;
-  const int splits = dkv_splits(n, seqs, q_len, kv_len, heads, kv_heads);
+  const size_t wide = d <= 64 ? 64 : 128, keys = (size_t)n * seqs * kv_len;
+  const size_t q_parts = dq_splits(n, seqs, q_len, kv_len, heads), k_parts = dkv_splits(n, seqs, q_len, kv_len, heads, kv_heads);
+  // (the parts of dq have been joined when those of dk and dv are made)
+  const size_t dq_part = q_parts > 1 ? q_parts * rows * heads * wide * 4 : 0, dkv_part = k_parts > 1 ? k_parts * keys * kv_heads * 2 * wide * 4 : 0;
   backward_layout l;
   l.lse2 = 0;
   l.dot = l.lse2 + up256(rows * heads * 4);
@@ -991,8 +1032,9 @@ backward_layout layout_of(int n, int seqs, int q_len, int kv_len, int heads, int
   l.hi = l.lo + up256(rows * 4);
   l.pos = l.hi + up256(rows * 4);
   l.groups = l.pos + up256(rows * 4);
-  l.part = l.groups + up256((size_t)n * seqs * ((q_len + 31) / 32) * 16);
-  l.total = rows ? l.part + (splits > 1 ? up256((size_t)splits * n * seqs * kv_heads * kv_len * 2 * (d <= 64 ? 64 : 128) * 4) : 0) : 0;
+  l.lacks = l.groups + up256((size_t)n * seqs * ((q_len + 31) / 32) * 16);
+  l.part = l.lacks + (q_parts > 1 ? up256(q_parts * rows * heads * 4) : 0);
+  l.total = rows ? l.part + up256(dq_part > dkv_part ? dq_part : dkv_part) : 0;
   return l;
 }
 
@@ -1050,7 +1092,7 @@ hipError_t hdet_launch_attend_backward(const hdet_attention_grad_args& a, hipStr
   g.lse2 = (float*)(w8 + l.lse2); g.dot = (float*)(w8 + l.dot);
   g.lo = (int*)(w8 + l.lo); g.hi = (int*)(w8 + l.hi); g.pos_of = (int*)(w8 + l.pos); g.groups = (i4v*)(w8 + l.groups);
   g.part = (float*)(w8 + l.part);
-  const int splits = dkv_splits(a.n_replicas, a.seqs, a.q_len, a.kv_len, a.heads, a.kv_heads);
+  g.lacks = (float*)(w8 + l.lacks);
   bool wh = true;
   for (const hdet_rows* m : {&a.q, &a.k, &a.v, &a.out, &a.dout, &a.dq, &a.dk, &a.dv}) wh = wh && (!m->dev || whole(*m, size, a.head_dim));
   // few queries: dk is made of few dz, whose rounding in one part shows (dk off by up to 1.48 times its own rounding in small tensors, 1.42 in large ones; 8 x 16 x 256
@@ -1060,13 +1102,17 @@ hipError_t hdet_launch_attend_backward(const hdet_attention_grad_args& a, hipStr
   with_shape(a.dtype, a.head_dim, extra(a, g), wh, [&](auto t, auto d, auto ex, auto w) {
     typedef decltype(t) T;
     set_blocks(g, nq, (unsigned)a.n_replicas * a.seqs * a.heads);
+    g.splits = dq_splits(a.n_replicas, a.seqs, a.q_len, a.kv_len, a.heads);
+    g.total *= g.splits;
     if (g.total) hipLaunchKernelGGL((attend_dq_kernel<T, d, ex, w>), grid_of(g.total), dim3(THREADS), 0, s, g);
+    if (g.total && g.splits > 1)
+      hipLaunchKernelGGL((attend_dq_join_kernel<T, d>), grid_of((unsigned)(((int64_t)a.n_replicas * a.seqs * a.q_len * a.heads * d + THREADS - 1) / THREADS)), dim3(THREADS), 0, s, g);
     set_blocks(g, nk, (unsigned)a.n_replicas * a.seqs * a.kv_heads);
-    g.splits = splits;
-    g.total *= splits;
+    g.splits = dkv_splits(a.n_replicas, a.seqs, a.q_len, a.kv_len, a.heads, a.kv_heads);
+    g.total *= g.splits;
     if (g.total && two) hipLaunchKernelGGL((attend_dkv_kernel<T, d, ex, w, sizeof(T) == 2>), grid_of(g.total), dim3(THREADS), 0, s, g);
     else if (g.total) hipLaunchKernelGGL((attend_dkv_kernel<T, d, ex, w, false>), grid_of(g.total), dim3(THREADS), 0, s, g);
-    if (g.total && splits > 1)
+    if (g.total && g.splits > 1)
       hipLaunchKernelGGL((attend_dkv_join_kernel<T, d>), grid_of((unsigned)(((int64_t)a.n_replicas * a.seqs * a.kv_heads * a.kv_len * d + THREADS - 1) / THREADS)), dim3(THREADS), 0, s, g);
   });
   return hipGetLastError();

@@ -70,6 +70,28 @@ def test_sizes(n, seqs, q_len, kv_len, heads, kv_heads, d, dtype):
 
 
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+@pytest.mark.parametrize("d", [64, 72])
+def test_walks_in_parts(d, dtype):
+    """Few blocks over long sequences: the backward pass's kernels divide their walks; empty rows, documents and an infinite gradient among them."""
+    n, q_len = 1, 1300
+    q, k, v, dout = inputs(n, 1, q_len, q_len, 2, 1, d, dtype, seed=d)
+    run_and_check(q, k, v, dout, 2, 1, 1)
+    run_and_check(q, k, v, dout, 2, 1, 1, causal=False, window=700, softcap=4.0)
+    first, end = packed(n, 1, q_len, 5)
+    run_and_check(q, k, v, dout, 2, 1, 1, causal=False, first=first, end=end)
+    bad = dout.clone()
+    bad[0, 1000, 5] = float("inf")
+    out, lse = forward(q, k, v, 2, 1, 1)
+    _, dk, dv = backward(q, k, v, out, lse, bad, 2, 1, 1)
+    want = R.attention(q, k, v, 2, 1, 1, dout)
+    R.check(dk[:, 1001:], want["dk"][:, 1001:], want["bound_dk"][:, 1001:], "dk")
+    reached = torch.zeros_like(dv, dtype=torch.bool)
+    reached[:, :1001, 5] = True
+    assert bool((~torch.isfinite(dv[reached])).all()) and bool((~torch.isfinite(dk[:, :1001])).all())
+    R.check(torch.where(reached, torch.zeros_like(dv), dv), want["dv"].masked_fill(reached, 0.0), want["bound_dv"], "dv")
+
+
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
 def test_nothing_to_do(dtype):
     # no queries: the keys' gradients are 0; no keys: every query is empty
     q, k, v, dout = inputs(2, 2, 0, 5, 4, 2, 16, dtype)

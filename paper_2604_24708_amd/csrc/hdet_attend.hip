@@ -180,13 +180,15 @@ __device__ __forceinline__ block_range block_range_of(const attend_args& g, cons
   return b;
 }
 
-// Whether any thread of the block says so; two barriers, and 16 bytes of LDS at `lds` that nothing else uses
-__device__ __forceinline__ bool block_any(bool yes, int w, int lane, int* lds) {
-  const int any = __any(yes);
+// Whether any thread of the block's NW wavefronts says so; two barriers, and 4 NW bytes of LDS at `lds` that nothing else uses
+template <int NW = NWV> __device__ __forceinline__ bool block_any(bool yes, int w, int lane, int* lds) {
+  int any = __any(yes);
   __syncthreads();
   if (lane == 0) lds[w] = any;
   __syncthreads();
-  return lds[0] | lds[1] | lds[2] | lds[3];
+#pragma unroll
+  for (int i = 0; i < NW; ++i) any |= lds[i];
+  return any;
 }
 
 // Scores of a block from its raw products: x such that the score is (x + shift) mult log2 units (score_units).  With a cap x is tanh - 1, exact enough unless
@@ -734,15 +736,20 @@ template <typename T, int D> __global__ __launch_bounds__(THREADS) void attend_d
 // ---------------------------------------------------------------------------------------------
 // backward, step 2: dk and dv; block = 128 keys of a key head, walks over the query tiles of the heads that share it
 // ---------------------------------------------------------------------------------------------
-template <typename T, int D, int EXTRA, bool TWO> constexpr int dkv_waves() { return D == 128 ? 1 : sizeof(T) == 2 && !EXTRA && !TWO ? 3 : 2; }
+// bfloat16 heads of more than 64 columns: two wavefronts to 32 keys, one to either half of a query tile, and the own keys and values in LDS, since in registers they leave
+// room for one wavefront a SIMD (8192 queries and keys, 16 heads of 128: MEASURED)
+template <typename T, int D> constexpr bool dkv_paired() { return sizeof(T) == 2 && D == 128; }
+template <typename T, int D> constexpr int dkv_threads() { return dkv_paired<T, D>() ? 512 : 256; }
+template <typename T, int D, int EXTRA, bool TWO> constexpr int dkv_waves() { return sizeof(T) == 2 ? (D == 64 && !EXTRA && !TWO ? 3 : 2) : D == 64 ? 2 : 1; }
 // TWO: dk from dz in two bfloat16 parts
-template <typename T, int D, int EXTRA, bool WHOLE, bool TWO> __global__ __launch_bounds__(THREADS, (dkv_waves<T, D, EXTRA, TWO>())) void attend_dkv_kernel(const attend_args g) {
+template <typename T, int D, int EXTRA, bool WHOLE, bool TWO> __global__ __launch_bounds__((dkv_threads<T, D>()), (dkv_waves<T, D, EXTRA, TWO>())) void attend_dkv_kernel(const attend_args g) {
   typedef shape<T, D> S;
   constexpr int TILE = S::TB * D, NB = S::TB / 32, STATS = 5 * S::TB;      // lse2, dot, lo, hi, position
-  constexpr int LOADS = 2 * tile_loader<T, D, S::TB, NWV, WHOLE>::NI + 2;
-  __shared__ __attribute__((aligned(1024))) T smem[2 * STAGES * TILE];     // queries and output gradients
+  constexpr bool PAIRED = dkv_paired<T, D>();
+  constexpr int NW = dkv_threads<T, D>() / 64, LOADS = 2 * tile_loader<T, D, S::TB, NW, WHOLE>::NI + 2, RING = 2 * STAGES * TILE;
+  __shared__ __attribute__((aligned(1024))) T smem[RING + (PAIRED ? 2 * RB * D : 0)];        // queries and output gradients; own keys and values
   __shared__ __attribute__((aligned(16))) int stats[STAGES * STATS];
-  __shared__ int ends[2 * NWV];
+  __shared__ int ends[2 * NW];
   unsigned lin = blockIdx.y * gridDim.x + blockIdx.x;
   if (lin >= g.total) return;
   const unsigned split = g.splits > 1 ? lin % g.splits : 0;
@@ -751,7 +758,7 @@ template <typename T, int D, int EXTRA, bool WHOLE, bool TWO> __global__ __launc
   const group_id id = place_group(blk.grp, g, g.by_kv_heads);
   const int kh = id.h, b = id.b, r = id.r;
   const int tid = threadIdx.x, lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int k0 = blk.x * RB, wk0 = k0 + w * WR, key = wk0 + (lane & 31);
+  const int half = PAIRED ? w >> 2 : 0, k0 = blk.x * RB, wk0 = k0 + (w & 3) * WR, key = wk0 + (lane & 31);
   const int n_groups = (g.q_len + 31) / 32;
   const i4v* const groups = g.groups + ((int64_t)r * g.seqs + b) * n_groups;
   // first and last group of queries that attend any of the block's keys
@@ -764,7 +771,7 @@ template <typename T, int D, int EXTRA, bool WHOLE, bool TWO> __global__ __launc
       last = (int)(to < g.q_len ? to : g.q_len - 1) / 32;
     }
   } else {
-    for (int i = tid; i < n_groups; i += THREADS) {
+    for (int i = tid; i < n_groups; i += NW * 64) {
       const i4v x = groups[i];
       if (x[0] < k0 + RB && x[3] > k0) {
         first = min(first, i);
@@ -775,28 +782,45 @@ template <typename T, int D, int EXTRA, bool WHOLE, bool TWO> __global__ __launc
     last = -min(wave_min(-last), wave_min(-__shfl_xor(last, 32)));
     if (lane == 0) {
       ends[w] = first;
-      ends[NWV + w] = last;
+      ends[NW + w] = last;
     }
     __syncthreads();
-    first = __builtin_amdgcn_readfirstlane(min(min(ends[0], ends[1]), min(ends[2], ends[3])));
-    last = __builtin_amdgcn_readfirstlane(max(max(ends[4], ends[5]), max(ends[6], ends[7])));
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+      first = min(first, ends[i]);
+      last = max(last, ends[NW + i]);
+    }
+    first = __builtin_amdgcn_readfirstlane(first);
+    last = __builtin_amdgcn_readfirstlane(last);
   }
   const bool there = key < g.kv_len;
   const int64_t kcol = (int64_t)kh * g.d, row0 = (int64_t)b * g.kv_len + wk0, rows = (int64_t)g.seqs * g.q_len, q_row0 = (int64_t)b * g.q_len;
-  const T* const own_k = there ? (const T*)g.k + r * g.k_z + (row0 + (lane & 31)) * g.k_s + kcol : nullptr;
-  const T* const own_v = there ? (const T*)g.v + r * g.v_z + (row0 + (lane & 31)) * g.v_s + kcol : nullptr;
-  typename S::frag fk[S::NF], fv[S::NF];
+  typename S::frag fk[PAIRED ? 1 : S::NF], fv[PAIRED ? 1 : S::NF];
+  T* const own_k = smem + RING + (w & 3) * WR * D;
+  T* const own_v = own_k + RB * D;
+  if constexpr (PAIRED) {
+    const T* const from_k = (const T*)g.k + r * g.k_z + ((int64_t)b * g.kv_len + k0) * g.k_s + kcol;
+    const T* const from_v = (const T*)g.v + r * g.v_z + ((int64_t)b * g.kv_len + k0) * g.v_s + kcol;
 #pragma unroll
-  for (int i = 0; i < S::NF; ++i) {
-    fk[i] = own_frag<T, D, WHOLE>(own_k, i, g.d, lane);
-    fv[i] = own_frag<T, D, WHOLE>(own_v, i, g.d, lane);
+    for (int i = 0; i < RB / S::TB; ++i) {
+      tile_loader<T, D, S::TB, NW, WHOLE>(from_k, g.k_s, g.d, w, lane).load(i * S::TB, g.kv_len - k0 - i * S::TB, smem + RING + i * TILE);
+      tile_loader<T, D, S::TB, NW, WHOLE>(from_v, g.v_s, g.d, w, lane).load(i * S::TB, g.kv_len - k0 - i * S::TB, smem + RING + RB * D + i * TILE);
+    }
+  } else {
+    const T* const from_k = there ? (const T*)g.k + r * g.k_z + (row0 + (lane & 31)) * g.k_s + kcol : nullptr;
+    const T* const from_v = there ? (const T*)g.v + r * g.v_z + (row0 + (lane & 31)) * g.v_s + kcol : nullptr;
+#pragma unroll
+    for (int i = 0; i < S::NF; ++i) {
+      fk[i] = own_frag<T, D, WHOLE>(from_k, i, g.d, lane);
+      fv[i] = own_frag<T, D, WHOLE>(from_v, i, g.d, lane);
+    }
   }
   const S at(lane);
   const float c = EXTRA ? 1.f : g.c;
   const int t0 = last < 0 ? 0 : first / NB, tiles = last < 0 ? 0 : last / NB + 1 - t0;
 
-  tile_loader<T, D, S::TB, NWV, WHOLE> qs((const T*)g.q + r * g.q_z + q_row0 * g.q_s, g.q_s, g.d, w, lane);
-  tile_loader<T, D, S::TB, NWV, WHOLE> dos((const T*)g.dout + r * g.do_z + q_row0 * g.do_s, g.do_s, g.d, w, lane);
+  tile_loader<T, D, S::TB, NW, WHOLE> qs((const T*)g.q + r * g.q_z + q_row0 * g.q_s, g.q_s, g.d, w, lane);
+  tile_loader<T, D, S::TB, NW, WHOLE> dos((const T*)g.dout + r * g.do_z + q_row0 * g.do_s, g.do_s, g.d, w, lane);
   const T *const q_at = qs.src, *const do_at = dos.src;
   f16v dk[S::ND], dv[S::ND];               // [column][key]
   // this block's part of all heads' tiles
@@ -810,10 +834,11 @@ template <typename T, int D, int EXTRA, bool WHOLE, bool TWO> __global__ __launc
     dos.load(q0, have, to + TILE);
     // statistics: a wavefront an array, all of them the positions; zeros behind the last row
     const int64_t row = q_row0 + q0, stat = ((int64_t)r * g.heads + h) * rows + row;
-    const void* const from = w == 0 ? (const void*)(g.lse2 + stat) : w == 1 ? (const void*)(g.dot + stat) : w == 2 ? (const void*)(g.lo + r * rows + row) : (const void*)(g.hi + r * rows + row);
+    const int array = w & 3;
+    const void* const from = array == 0 ? (const void*)(g.lse2 + stat) : array == 1 ? (const void*)(g.dot + stat) : array == 2 ? (const void*)(g.lo + r * rows + row) : (const void*)(g.hi + r * rows + row);
     int* const st = stats + slot * STATS;
     if (lane < S::TB) {
-      lds_load4(scalar_rsrc(from, have * 4), __builtin_amdgcn_readfirstlane(lds_addr_of((const uint16_t*)(st + w * S::TB))), lane * 4);
+      lds_load4(scalar_rsrc(from, have * 4), __builtin_amdgcn_readfirstlane(lds_addr_of((const uint16_t*)(st + array * S::TB))), lane * 4);
       lds_load4(scalar_rsrc(g.pos_of + r * rows + row, have * 4), __builtin_amdgcn_readfirstlane(lds_addr_of((const uint16_t*)(st + 4 * S::TB))), lane * 4);
     }
   };
@@ -833,11 +858,11 @@ template <typename T, int D, int EXTRA, bool WHOLE, bool TWO> __global__ __launc
       const int h = kh * g.group + j / tiles, t = t0 + j % tiles;
       const float slope2 = EXTRA == kGeneral && g.slopes ? g.slopes[r * g.slopes_z + h] * kLog2e : 0.f;
       if (decltype(clean)::value) {
-        clean_tile<T, D, 2 * S::TB>(at_tiles, tid, THREADS);
+        clean_tile<T, D, 2 * S::TB>(at_tiles, tid, NW * 64);
         __syncthreads();
       }
 #pragma unroll 1
-      for (int i = 0; i < NB; ++i) {
+      for (int i = half; i < (PAIRED ? half + 1 : NB); ++i) {
         const int gi = t * NB + i;
         if (gi >= n_groups) continue;
         wave_range gr;
@@ -851,7 +876,14 @@ template <typename T, int D, int EXTRA, bool WHOLE, bool TWO> __global__ __launc
         if (gr.lo_min >= wk0 + 32 || gr.hi_max <= wk0) continue;
         const T* const qt = at_tiles + i * 32 * D;
         const int* const st = at_stats + 32 * i + ((lane >> 5) << 2);
-        f16v x = at.first(qt, fk, all16(0.f)), dp = at.first(qt + TILE, fv, all16(0.f)), bend;
+        f16v x, dp, bend;
+        if constexpr (PAIRED) {
+          x = at.first(qt, own_k, all16(0.f));
+          dp = at.first(qt + TILE, own_v, all16(0.f));
+        } else {
+          x = at.first(qt, fk, all16(0.f));
+          dp = at.first(qt + TILE, fv, all16(0.f));
+        }
         if (EXTRA) shape_scores_back<EXTRA>(g, x, bend, slope2, [&](int e) { return distance(st[4 * S::TB + acc_row(e, 0)], key); });
 #pragma unroll
         for (int e4 = 0; e4 < 4; ++e4) {
@@ -885,8 +917,38 @@ template <typename T, int D, int EXTRA, bool WHOLE, bool TWO> __global__ __launc
     wait_and_barrier<0>();
   };
   walk(std::false_type());
-  const bool again = block_any(there && (not_finite(dk) || not_finite(dv)), w, lane, (int*)(smem + 2 * STAGES * TILE) - NWV);
+  const bool again = block_any<NW>(there && (not_finite(dk) || not_finite(dv)), w, lane, (int*)(smem + RING) - NW);
   if (again) walk(std::true_type());
+  if constexpr (PAIRED) {
+    // the two halves' sums, as they lie in the lanes
+    f4v* const part = reinterpret_cast<f4v*>(smem) + (w & 3) * (2 * S::ND * 4 * 64) + lane;
+    __syncthreads();
+    if (half == 1) {
+#pragma unroll
+      for (int i = 0; i < S::ND; ++i)
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4) {
+          part[(i * 4 + e4) * 64] = f4v{dk[i][4 * e4], dk[i][4 * e4 + 1], dk[i][4 * e4 + 2], dk[i][4 * e4 + 3]};
+          part[((S::ND + i) * 4 + e4) * 64] = f4v{dv[i][4 * e4], dv[i][4 * e4 + 1], dv[i][4 * e4 + 2], dv[i][4 * e4 + 3]};
+        }
+    }
+    __syncthreads();
+    if (half == 0) {
+#pragma unroll
+      for (int i = 0; i < S::ND; ++i)
+#pragma unroll
+        for (int e4 = 0; e4 < 4; ++e4) {
+          const f4v a = part[(i * 4 + e4) * 64], c = part[((S::ND + i) * 4 + e4) * 64];
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            dk[i][4 * e4 + u] += a[u];
+            dv[i][4 * e4 + u] += c[u];
+          }
+        }
+    }
+    __syncthreads();
+    if (half == 1) return;
+  }
 #pragma unroll
   for (int i = 0; i < S::ND; ++i)
 #pragma unroll
@@ -1110,8 +1172,8 @@ hipError_t hdet_launch_attend_backward(const hdet_attention_grad_args& a, hipStr
     set_blocks(g, nk, (unsigned)a.n_replicas * a.seqs * a.kv_heads);
     g.splits = dkv_splits(a.n_replicas, a.seqs, a.q_len, a.kv_len, a.heads, a.kv_heads);
     g.total *= g.splits;
-    if (g.total && two) hipLaunchKernelGGL((attend_dkv_kernel<T, d, ex, w, sizeof(T) == 2>), grid_of(g.total), dim3(THREADS), 0, s, g);
-    else if (g.total) hipLaunchKernelGGL((attend_dkv_kernel<T, d, ex, w, false>), grid_of(g.total), dim3(THREADS), 0, s, g);
+    if (g.total && two) hipLaunchKernelGGL((attend_dkv_kernel<T, d, ex, w, sizeof(T) == 2>), grid_of(g.total), dim3(dkv_threads<T, d>()), 0, s, g);
+    else if (g.total) hipLaunchKernelGGL((attend_dkv_kernel<T, d, ex, w, false>), grid_of(g.total), dim3(dkv_threads<T, d>()), 0, s, g);
     if (g.total && g.splits > 1)
       hipLaunchKernelGGL((attend_dkv_join_kernel<T, d>), grid_of((unsigned)(((int64_t)a.n_replicas * a.seqs * a.kv_heads * a.kv_len * d + THREADS - 1) / THREADS)), dim3(THREADS), 0, s, g);
   });

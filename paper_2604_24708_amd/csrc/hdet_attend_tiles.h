@@ -65,6 +65,13 @@ template <int D> struct shape<uint16_t, D> {
     for (int i = 0; i < NF; ++i) acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const frag*>(tile + k[i]), own[i], acc, 0, 0, 0);
     return acc;
   }
+  // the same with the own rows in LDS too
+  __device__ __forceinline__ f16v first(const uint16_t* tile, const uint16_t* own, f16v acc) const {
+#pragma unroll
+    for (int i = 0; i < NF; ++i)
+      acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const frag*>(tile + k[i]), *reinterpret_cast<const frag*>(own + k[i]), acc, 0, 0, 0);
+    return acc;
+  }
   // acc^T += (32 rows from `tile` on)^T x, x [row][own row] rounded to bf16
   __device__ __forceinline__ void second(const uint16_t* tile, const f16v& x, f16v (&acc)[ND]) const {
 #pragma unroll

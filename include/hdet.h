@@ -484,7 +484,7 @@ int hdet_vocab_loss(const hdet_vocab_args* args, void* stream);
  * freq_dev holds rotated / 2 frequencies in radians a position, in 64 bits, as any stretching for long
  * contexts leaves them (hdet_rotary_frequencies makes the usual ones); angles are formed and reduced
  * in 64 bits, good for any 32-bit position.  Row i of a replica stands at positions_dev[replica][i] or, where
- * that is NULL, at i mod period (i where period is 0).  Sums of squares are 64 bits, the rest fp32.
+ * that is NULL, at i mod period (i where period is 0).  Sums are fp32; those of squares 64 bits where they leave its range.
  * q_out may be q itself and k_out k itself.  k absent (dev NULL): q alone; its norm and the keys' are
  * each left out where their gain is NULL.                                                    */
 enum { HDET_ROTARY_HALVES = 0, HDET_ROTARY_PAIRS = 1 };
@@ -557,13 +557,13 @@ int hdet_rotary_frequencies(int32_t rotated, double base, int32_t stretch, doubl
  * room: end; rows of padding: end = 0.)  A query that attends no key has out 0, lse -infinity and gradient 0.
  * Keys, values and queries take part only in the pairs that are attended: whatever the others hold, NaN and infinity
  * too, leaves no trace.
- * Scores, statistics and sums are fp32; bfloat16 inputs: p (relative to a maximum of the row) is rounded to bfloat16 for the product with v,
- * p and dz are for the gradients' products.  out may not lie over the inputs.  workspace: hdet_attention_workspace bytes, 16-byte aligned
- * (0 for most sizes: what few queries over many keys leave in pieces).                                       */
+ * Scores, statistics and sums are fp32; bfloat16 inputs: p (relative to some score of the row) is rounded to bfloat16 for the product with v.
+ * out may not lie over the inputs.  workspace: hdet_attention_workspace bytes, 16-byte aligned (what few queries over many keys leave in
+ * pieces; 0 otherwise).                                                                                      */
 #define HDET_MAX_ATTENTION_DIM 128
 typedef struct {
   int32_t   n_replicas, dtype;                 /* HDET_TYPE_* of q, k, v and out             */
-  int32_t   seqs, q_len, kv_len;               /* seqs * q_len up to 2^21, seqs * kv_len up to 2^28 */
+  int32_t   seqs, q_len, kv_len;               /* seqs * q_len up to 2^21, seqs * kv_len up to 2^28, n_replicas * seqs * q_len * heads up to 2^31 */
   int32_t   heads, kv_heads, head_dim;         /* heads a multiple of kv_heads, heads * head_dim up to 2^20 */
   int32_t   causal, window;                    /* window 0: none                             */
   double    scale, softcap;                    /* softcap 0: none                            */
@@ -583,7 +583,8 @@ int hdet_attention(const hdet_attention_args* args, void* stream);
 /* Backward pass, from what the forward pass took, its out and lse, and dout (all with the same mask arguments):
  *   dv_j = sum_i p_ij dout_i,  dz_ij = p_ij (dout_i . v_j - dout_i . out_i),  times 1 - tanh^2 with softcap
  *   dq_i = scale sum_j dz_ij k_j,  dk_j = scale sum_i dz_ij q_i       (over the heads that share the key head; in a fixed order)
- * workspace: hdet_attention_backward_workspace bytes, 16-byte aligned.                       */
+ * bfloat16 inputs: for their products p is rounded to bfloat16, dz for dk too, and dz for dq (for dk as well, where few queries make it) is the sum
+ * of two bfloat16 numbers.  dq, dk and dv may not lie over the inputs.  workspace: hdet_attention_backward_workspace bytes, 16-byte aligned. */
 typedef struct {
   int32_t   n_replicas, dtype;
   int32_t   seqs, q_len, kv_len, heads, kv_heads, head_dim, causal, window;

@@ -477,6 +477,15 @@ def _work_of(t):
     return t.data_ptr(), t.numel() * t.element_size()
 
 
+def _on_current_device(**tensors):
+    """Refuses tensors on a device other than the current one, where the kernels run."""
+    import torch
+    current = torch.cuda.current_device()
+    for name, t in tensors.items():
+        if t is not None and t.get_device() != current:
+            raise ValueError(f"{name} is on {t.device}, the current device is cuda:{current}")
+
+
 def _size_of(name, *args) -> int:
     n = C.c_size_t()
     _check(getattr(load_library(), name)(*args, C.byref(n)))
@@ -636,6 +645,7 @@ def hdet_head_rotary(q, q_out, head_dim: int, k=None, k_out=None, q_gain=None, k
                          _rows_of("q_out", q_out, shape, dt), _rows_of("k_out", None if k is None else k_out, ks, dt), *_vector("q_gain", q_gain, (n, head_dim)),
                          *_vector("k_gain", k_gain, (n, head_dim)), _scalars("positions", positions, (n, rows), _I32),
                          None if freq is None else _scalars("freq", freq, freq.shape[:1], _F64))
+    _on_current_device(q=q, q_out=q_out, k=k, k_out=k_out, q_gain=q_gain, k_gain=k_gain, positions=positions, freq=freq)
     rc = lib.hdet_head_rotary(C.byref(a), stream)
     if rc:
         _check(rc)
@@ -658,6 +668,8 @@ def hdet_head_rotary_backward(q, dq_out, dq, head_dim: int, k=None, dk_out=None,
                               *_vector("k_gain", k_gain, (n, head_dim)), _scalars("positions", positions, (n, rows), _I32),
                               None if freq is None else _scalars("freq", freq, freq.shape[:1], _F64), *_vector("dq_gain", dq_gain, (n, head_dim)),
                               *_vector("dk_gain", dk_gain, (n, head_dim)), *_work_of(workspace))
+    _on_current_device(q=q, dq_out=dq_out, dq=dq, k=k, dk_out=dk_out, dk=dk, q_gain=q_gain, k_gain=k_gain, positions=positions, freq=freq, dq_gain=dq_gain,
+                       dk_gain=dk_gain, workspace=workspace)
     rc = lib.hdet_head_rotary_backward(C.byref(a), stream)
     if rc:
         _check(rc)
@@ -690,6 +702,7 @@ def hdet_attention(q, k, v, out, heads: int, kv_heads: int, seqs: int = 1, lse=N
     a = hdet_attention_args(*sizes, _rows_of("q", q, qs, dt), _rows_of("k", k, ks, dt), _rows_of("v", v, ks, dt), _rows_of("out", out, qs, dt),
                             _scalars("lse", lse, (qs[0], heads, qs[1])), *_vector("slopes", slopes, (qs[0], heads)), _scalars("positions", positions, scalars, _I32),
                             _scalars("first", first, scalars, _I32), _scalars("end", end, scalars, _I32), *_work_of(workspace))
+    _on_current_device(q=q, k=k, v=v, out=out, lse=lse, slopes=slopes, positions=positions, first=first, end=end, workspace=workspace)
     rc = lib.hdet_attention(C.byref(a), stream)
     if rc:
         _check(rc)
@@ -711,6 +724,7 @@ def hdet_attention_backward(q, k, v, out, lse, dout, dq, dk, dv, heads: int, kv_
                                  _scalars("lse", lse, (qs[0], heads, qs[1])), *_vector("slopes", slopes, (qs[0], heads)),
                                  _scalars("positions", positions, scalars, _I32), _scalars("first", first, scalars, _I32), _scalars("end", end, scalars, _I32),
                                  *_work_of(workspace))
+    _on_current_device(q=q, k=k, v=v, out=out, lse=lse, dout=dout, dq=dq, dk=dk, dv=dv, slopes=slopes, positions=positions, first=first, end=end, workspace=workspace)
     rc = lib.hdet_attention_backward(C.byref(a), stream)
     if rc:
         _check(rc)
@@ -739,6 +753,8 @@ class hdet_gradient_list:
                     o = o[:, None]
                 shape = (shape[0], 1, shape[1])
             dtype = _dtype_code(name, g)
+            if g.get_device() != grads[0].get_device() or o is not None and o.get_device() != g.get_device():
+                raise ValueError(f"{name} or its output is on another device than grads[0]")
             self.items[i] = hdet_grad_tensor(_rows_of(name, g, shape, g.dtype), _ABSENT if o is None else _rows_of(f"outs[{i}]", o, shape, _F32), shape[1], shape[2], dtype)
 
     def __len__(self):
@@ -758,6 +774,7 @@ def hdet_clip_gradients(tensors: hdet_gradient_list, norm, max_norm: float, shar
         raise ValueError(f"norm has shape {tuple(norm.shape)}, {(tensors.n_replicas,)} is wanted")
     a = hdet_clip_args(n, len(tensors), tensors.items, HDET_GRAD_SHARED if shared else HDET_GRAD_PER_REPLICA, 0, max_norm, _scalars("norm", norm, (n,)),
                        *_work_of(workspace))
+    _on_current_device(norm=norm, workspace=workspace, **({"grads": tensors.tensors[0][0]} if len(tensors) else {}))
     rc = lib.hdet_clip_gradients(C.byref(a), stream)
     if rc:
         _check(rc)

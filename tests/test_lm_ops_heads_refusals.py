@@ -144,6 +144,20 @@ def test_binding_refuses_what_the_library_cannot_see():
             call()
 
 
+def test_tensors_on_another_device_are_refused(monkeypatch):
+    class Tensor:
+        def __init__(self, device):
+            self.device = torch.device("cuda", device)
+
+        def get_device(self):
+            return self.device.index
+
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: 1)
+    B._on_current_device(q=Tensor(1), k=None, v=Tensor(1))
+    with pytest.raises(ValueError, match="v is on cuda:0, the current device is cuda:1"):
+        B._on_current_device(q=Tensor(1), k=None, v=Tensor(0))
+
+
 def test_structures_have_the_c_compilers_layout():
     names = ["hdet_rotary_args", "hdet_rotary_grad_args", "hdet_attention_args", "hdet_attention_grad_args", "hdet_grad_tensor", "hdet_clip_args"]
     lines, want = [], []

@@ -583,8 +583,8 @@ int hdet_attention(const hdet_attention_args* args, void* stream);
 /* Backward pass, from what the forward pass took, its out and lse, and dout (all with the same mask arguments):
  *   dv_j = sum_i p_ij dout_i,  dz_ij = p_ij (dout_i . v_j - dout_i . out_i),  times 1 - tanh^2 with softcap
  *   dq_i = scale sum_j dz_ij k_j,  dk_j = scale sum_i dz_ij q_i       (over the heads that share the key head; in a fixed order)
- * bfloat16 inputs: for their products p is rounded to bfloat16, dz for dk too, and dz for dq (for dk as well, where few queries make it) is the sum
- * of two bfloat16 numbers.  dq, dk and dv may not lie over the inputs.  workspace: hdet_attention_backward_workspace bytes, 16-byte aligned. */
+ * bfloat16 inputs: for their products p and, for dk, dz are rounded to bfloat16; dz for dq, and where few queries make dk and dv all of them, are
+ * the sum of two bfloat16 numbers.  dq, dk and dv may not lie over the inputs.  workspace: hdet_attention_backward_workspace bytes, 16-byte aligned. */
 typedef struct {
   int32_t   n_replicas, dtype;
   int32_t   seqs, q_len, kv_len, heads, kv_heads, head_dim, causal, window;

@@ -12,6 +12,15 @@
 // the second product's tiles.  What of that is attended comes back by itself where it has made scores, statistics or row dots what they are; the values'
 // and the output gradients' own entries, which have not, are added to the results of the rows that attend them (add_not_finite).
 
+// Four kernels: attend (128 queries of a head a block), attend_few (few queries: the keys are divided over the chip), attend_dq and attend_dkv (backward; S = q k and dp are formed in
+// both, since one kernel for all three gradients would add up dq with atomics, in an order that changes).  A wavefront owns 32 rows, as columns of the 32 x 32 products, so that a
+// row's statistics lie in two lanes and a product's result is the next one's operand without a way through LDS.  Tiles of the other side (64 rows of bfloat16, 64 columns) come by
+// direct loads to LDS, one stage ahead; the wavefronts of other blocks on the same CU cover the waits, so registers are what decides: 8 x 16 sequences of 256, 8 heads of 64, forward
+// 4 wavefronts a SIMD 32 us; a variant with spills at that many: 2 to 3 times.
+// Bound by the work between the two products of a block (16 exponentials a lane, sums, conversions) as much as by the products themselves, which wait for it: longer heads, more of the
+// library's rate.  Reached, TFLOP/s (library's product: 1190 to 1270 bfloat16, 154 fp32): forward, 8192 queries and keys, heads of 64 850, of
+// 128 950; of 128 causal, 268 us, 1020 of the pairs that are attended; fp32 114; backward (5 products a pair), heads of 64 550 to 650.
+
 #include <limits.h>
 #include <math.h>
 
@@ -62,6 +71,7 @@ struct attend_args {
   const int32_t *pos, *first, *end;
   int n, seqs, q_len, kv_len, heads, kv_heads, group, d, causal, window;
   int splits;
+  int run;                                 // dk and dv in fp32: the launch's number
   float scale, c, cap2, inv_cap;           // c = scale log2 e; cap2 = cap log2 e or 0
   bool close;                              // capped scores to fp32's last places, not to 1e-7 of the cap
   unsigned total;                          // blocks
@@ -741,7 +751,11 @@ template <typename T, int D> __global__ __launch_bounds__(THREADS) void attend_d
 template <typename T, int D> constexpr bool dkv_paired() { return sizeof(T) == 2 && D == 128; }
 template <typename T, int D> constexpr int dkv_threads() { return dkv_paired<T, D>() ? 512 : 256; }
 template <typename T, int D, int EXTRA, bool TWO> constexpr int dkv_waves() { return sizeof(T) == 2 ? (D == 64 && !EXTRA && !TWO ? 3 : 2) : D == 64 ? 2 : 1; }
-// TWO: dk from dz in two bfloat16 parts
+// Query tiles that one launch sums up: in fp32 1024 rows, and the next launch adds its sums to what the one before has written, since a running sum over all rows of the heads
+// that share a key head rounds once a row (4 heads of 1088 rows: dk and dv off by 1.3e-6 of their norms,
+// in runs by 7.9e-7; 2 x 8192 tokens of 4 heads and one key head: the backward pass 3400 -> 3780 us)
+template <typename T, int D> constexpr int run_tiles() { return sizeof(T) == 2 ? 1 << 28 : 1024 / shape<T, D>::TB; }
+// TWO: dk and dv from dz and p in two bfloat16 parts each
 template <typename T, int D, int EXTRA, bool WHOLE, bool TWO> __global__ __launch_bounds__((dkv_threads<T, D>()), (dkv_waves<T, D, EXTRA, TWO>())) void attend_dkv_kernel(const attend_args g) {
   typedef shape<T, D> S;
   constexpr int TILE = S::TB * D, NB = S::TB / 32, STATS = 5 * S::TB;      // lse2, dot, lo, hi, position
@@ -824,7 +838,9 @@ template <typename T, int D, int EXTRA, bool WHOLE, bool TWO> __global__ __launc
   const T *const q_at = qs.src, *const do_at = dos.src;
   f16v dk[S::ND], dv[S::ND];               // [column][key]
   // this block's part of all heads' tiles
-  const int share = (tiles * g.group + g.splits - 1) / g.splits, begin = split * share, all = min(tiles * g.group, begin + share);
+  const int share = (tiles * g.group + g.splits - 1) / g.splits, end = min(tiles * g.group, (int)(split + 1) * share), begin = split * share + g.run * run_tiles<T, D>(),
+            all = min(end, begin + run_tiles<T, D>());
+  if (g.run && begin >= all) return;
   auto request = [&](int j, int slot) {    // tile j of all heads' tiles
     const int h = kh * g.group + (tiles ? j / tiles : 0), t = t0 + (tiles ? j % tiles : 0), q0 = t * S::TB, have = j < all ? min(g.q_len - q0, S::TB) : 0;
     qs.src = q_at + (int64_t)h * g.d;
@@ -909,9 +925,13 @@ template <typename T, int D, int EXTRA, bool WHOLE, bool TWO> __global__ __launc
             }
           }
         }
-        at.second(qt + TILE, x, dv);
-        if (TWO) at.second_in_two(qt, dp, dk);
-        else at.second(qt, dp, dk);
+        if (TWO) {
+          at.second_in_two(qt + TILE, x, dv);
+          at.second_in_two(qt, dp, dk);
+        } else {
+          at.second(qt + TILE, x, dv);
+          at.second(qt, dp, dk);
+        }
       }
     }
     wait_and_barrier<0>();
@@ -956,8 +976,8 @@ template <typename T, int D, int EXTRA, bool WHOLE, bool TWO> __global__ __launc
   char* const strip = (char*)smem + w * STRIP;
   auto put = [&](auto to_k, auto to_v, int64_t k_s, int64_t v_s, auto wh) {
     typedef std::remove_pointer_t<decltype(to_k)> U;
-    store_rows<U, D, decltype(wh)::value>(dk, strip, to_k, k_s, g.kv_len - wk0, g.d, lane);
-    store_rows<U, D, decltype(wh)::value>(dv, strip, to_v, v_s, g.kv_len - wk0, g.d, lane);
+    store_rows<U, D, decltype(wh)::value>(dk, strip, to_k, k_s, g.kv_len - wk0, g.d, lane, sizeof(T) == 4 && g.run);
+    store_rows<U, D, decltype(wh)::value>(dv, strip, to_v, v_s, g.kv_len - wk0, g.d, lane, sizeof(T) == 4 && g.run);
     if (!again) return;
     __threadfence_block();
     for (int h = 0; h < g.group; ++h) {
@@ -1157,9 +1177,9 @@ hipError_t hdet_launch_attend_backward(const hdet_attention_grad_args& a, hipStr
   g.lacks = (float*)(w8 + l.lacks);
   bool wh = true;
   for (const hdet_rows* m : {&a.q, &a.k, &a.v, &a.out, &a.dout, &a.dq, &a.dk, &a.dv}) wh = wh && (!m->dev || whole(*m, size, a.head_dim));
-  // few queries: dk is made of few dz, whose rounding in one part shows (dk off by up to 1.48 times its own rounding in small tensors, 1.42 in large ones; 8 x 16 x 256
-  // queries in two parts: the backward pass 125 -> 152 us)
-  const bool two = a.dtype == HDET_TYPE_BF16 && (int64_t)((a.q_len + 63) / 64) * g.group <= 3;
+  // few queries: dk and dv are made of few dz and p, whose rounding in one part shows (two queries of 4 heads to a key head: dk off by up to 1.7 times its own rounding; many
+  // queries: 1.42 times; 8 x 16 x 256 queries in two parts: the backward pass 125 -> 152 us)
+  const bool two = a.dtype == HDET_TYPE_BF16 && (int64_t)g.group * a.q_len <= 192;
   const unsigned nq = (a.q_len + RB - 1) / RB, nk = (a.kv_len + RB - 1) / RB;
   with_shape(a.dtype, a.head_dim, extra(a, g), wh, [&](auto t, auto d, auto ex, auto w) {
     typedef decltype(t) T;
@@ -1172,8 +1192,12 @@ hipError_t hdet_launch_attend_backward(const hdet_attention_grad_args& a, hipStr
     set_blocks(g, nk, (unsigned)a.n_replicas * a.seqs * a.kv_heads);
     g.splits = dkv_splits(a.n_replicas, a.seqs, a.q_len, a.kv_len, a.heads, a.kv_heads);
     g.total *= g.splits;
-    if (g.total && two) hipLaunchKernelGGL((attend_dkv_kernel<T, d, ex, w, sizeof(T) == 2>), grid_of(g.total), dim3(dkv_threads<T, d>()), 0, s, g);
-    else if (g.total) hipLaunchKernelGGL((attend_dkv_kernel<T, d, ex, w, false>), grid_of(g.total), dim3(dkv_threads<T, d>()), 0, s, g);
+    constexpr int tb = shape<T, d>::TB;
+    const int64_t share = ((int64_t)((a.q_len + tb - 1) / tb) * g.group + g.splits - 1) / g.splits;
+    for (g.run = 0; g.total && (g.run == 0 || (int64_t)g.run * run_tiles<T, d>() < share); ++g.run) {
+      if (two) hipLaunchKernelGGL((attend_dkv_kernel<T, d, ex, w, sizeof(T) == 2>), grid_of(g.total), dim3(dkv_threads<T, d>()), 0, s, g);
+      else hipLaunchKernelGGL((attend_dkv_kernel<T, d, ex, w, false>), grid_of(g.total), dim3(dkv_threads<T, d>()), 0, s, g);
+    }
     if (g.total && g.splits > 1)
       hipLaunchKernelGGL((attend_dkv_join_kernel<T, d>), grid_of((unsigned)(((int64_t)a.n_replicas * a.seqs * a.kv_heads * a.kv_len * d + THREADS - 1) / THREADS)), dim3(THREADS), 0, s, g);
   });

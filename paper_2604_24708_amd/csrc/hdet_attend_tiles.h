@@ -275,7 +275,7 @@ template <typename T, int D, bool WHOLE> __device__ __forceinline__ typename sha
 // wavefront's strip in LDS so that a store writes 16 bytes of a row
 constexpr int STRIP = 32 * 36 * 4;         // bytes
 template <typename T, int D, bool WHOLE>
-__device__ __forceinline__ void store_rows(const f16v (&o)[D / 32], void* strip_, T* dst, int64_t ld, int have, int d, int lane) {
+__device__ __forceinline__ void store_rows(const f16v (&o)[D / 32], void* strip_, T* dst, int64_t ld, int have, int d, int lane, bool add = false) {
   typedef shape<T, D> S;
   constexpr int P = sizeof(T) == 2 ? 40 : 36, PER = 32 / S::E;
   T* const strip = (T*)strip_;
@@ -293,11 +293,14 @@ __device__ __forceinline__ void store_rows(const f16v (&o)[D / 32], void* strip_
       if (row >= have) continue;
       T* const to = dst + row * ld + 32 * dt + col;
       if (WHOLE) {
-        if (32 * dt + col < d) *reinterpret_cast<f4v*>(to) = *reinterpret_cast<const f4v*>(strip + row * P + col);
+        if (32 * dt + col >= d) continue;
+        f4v x = *reinterpret_cast<const f4v*>(strip + row * P + col);
+        if (sizeof(T) == 4 && add) x += *reinterpret_cast<const f4v*>(to);
+        *reinterpret_cast<f4v*>(to) = x;
       } else {
 #pragma unroll
         for (int e = 0; e < S::E; ++e)
-          if (32 * dt + col + e < d) to[e] = strip[row * P + col + e];
+          if (32 * dt + col + e < d) to[e] = sizeof(T) == 4 && add ? (T)(to[e] + strip[row * P + col + e]) : strip[row * P + col + e];
       }
     }
   }

@@ -107,6 +107,32 @@ def test_nothing_to_do(dtype):
     H.hdet_attention(q[:, :0], k, v, q[:, :0], 4, 2, 0)
 
 
+def distance(got, want):
+    return float((got.double() - want).norm() / want.norm())
+
+
+@pytest.mark.parametrize("q_len,heads,kv_heads,d", [(2, 32, 8, 96), (4, 16, 4, 32), (48, 4, 1, 64)])
+def test_few_queries_of_many_heads(q_len, heads, kv_heads, d):
+    """Gradients that few queries make are as far from 64 bits as their own rounding takes them: p and dz enter to 2^-16 and their errors in fp32 are 2^-20 or so, where that rounding is
+    some 2^-9 (a tenth is allowed for both)."""
+    q, k, v, dout = inputs(2, 2, q_len, q_len, heads, kv_heads, d, BF16, seed=d)
+    out, lse = forward(q, k, v, heads, kv_heads, 2)
+    want = R.attention(q, k, v, heads, kv_heads, 2, dout)
+    for name, x in zip(("dk", "dv"), backward(q, k, v, out, lse, dout, heads, kv_heads, 2)[1:]):
+        assert distance(x, want[name]) <= 1.1 * distance(want[name].to(BF16), want[name]), name
+
+
+@pytest.mark.parametrize("heads,kv_heads,d", [(32, 8, 64), (32, 8, 128)])
+def test_gradients_of_many_rows_in_fp32(heads, kv_heads, d):
+    """Four heads of 1088 rows to a key.  A running sum over M rows rounds M times, each 2^-24 / sqrt(3) (times 0.72, a mantissa's mean) of a sum that the first queries, which attend few
+    keys, have made as large as it gets: sqrt(M) times 2.5e-8, 8.0e-7 for runs of 1024 rows and 1.6e-6 for one sum of 4352.  p and dz are off by 6e-7 (scores, lse and dots at 2^-24 of 16)."""
+    q, k, v, dout = inputs(2, 1, 1088, 1088, heads, kv_heads, d, F32, seed=d)
+    out, lse = forward(q, k, v, heads, kv_heads, 1, softcap=30.0)
+    want = R.attention(q, k, v, heads, kv_heads, 1, dout, softcap=30.0)
+    for name, x in zip(("dk", "dv"), backward(q, k, v, out, lse, dout, heads, kv_heads, 1, softcap=30.0)[1:]):
+        assert distance(x, want[name]) <= 1e-6, name
+
+
 # ---- scores and masks ---------------------------------------------------------------------------
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
 @pytest.mark.parametrize("how", [dict(softcap=2.0), dict(softcap=30.0, causal=False), dict(window=1), dict(window=17), dict(window=64, causal=False), dict(window=200, softcap=5.0),

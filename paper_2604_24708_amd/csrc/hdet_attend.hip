@@ -489,7 +489,8 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
     z.l += other_half(z.l);
   };
   walk(std::false_type());
-  const bool again = __any(there && z.l == z.l && (z.l == INFINITY || not_finite(z.o)));
+  // (2^64: room for the sum over wavefronts and parts)
+  const bool again = __any(there && z.l == z.l && (z.l > 0x1p64f || not_finite(z.o)));
   if (again) walk(std::true_type());
 
   // join the wavefronts
@@ -1073,13 +1074,17 @@ template <typename F> void with_shape(int dtype, int d, int ex, bool wh, F f) {
   else with_d(float());
 }
 
-// Parts of the keys for few queries, 0: the queries fill the chip
-int few_splits(int n, int seqs, int q_len, int kv_len, int heads, int kv_heads) {
+// Parts of the keys for few queries, 0: the queries fill the chip.  Up to 16 queries: always a part at least.  More: where blocks of 32 rows, whose four wavefronts divide
+// the keys, are no more than fit the chip at once, a block's way being four times as short (us; 128 queries a block, 32):
+//   blocks of 32   8 x 8 x 512 keys, 64 columns 256: 12.1, 9.4     fp32 45, 17       16 x 8 x 1024 512: 19.6, 13.8     8 x 8 x 2048 512: 33.5, 18.0      8 x 8 x 4096 1024: 62, 43.5
+//   128 columns    8 x 512 128: 15.9, 11.2      32 x 512 queries of 8192 keys 512: 194, 108     16 x 2048 1024: 47, 61
+// (fewer keys, or a block a CU more: the join, 64 to 128 KB of LDS a block and four times the tiles cost more: 6 x 333 keys of 8 x 128 13, 33.)
+int few_splits(int n, int seqs, int q_len, int kv_len, int heads, int kv_heads, int head_dim, int window) {
   const int64_t pairs = (int64_t)(heads / kv_heads) * q_len, groups = (int64_t)n * seqs * kv_heads, cus = hdet_compute_units();
   if (pairs == 0 || groups == 0) return 0;
-  const int64_t blocks = (int64_t)n * seqs * heads * ((q_len + RB - 1) / RB), few = groups * ((pairs + 31) / 32);
-  if (q_len > 16 && (blocks >= cus / 2 || kv_len < 1024)) return 0;
-  int64_t s = (2 * cus + few - 1) / few, most = (kv_len + 255) / 256;
+  const int64_t seen = (int64_t)window + (q_len < RB ? q_len : RB), keys = window && seen < kv_len ? seen : kv_len, few = groups * ((pairs + 31) / 32);
+  if (q_len > 16 && few > (keys < 1024 ? cus : keys < 2048 ? 2 * cus : 4 * cus) / (head_dim > 64 && keys >= 1024 ? 2 : 1)) return 0;
+  int64_t s = (2 * cus + few - 1) / few, most = keys < 1024 ? 1 : (keys + 255) / 256;
   if (s > most) s = most;
   return (int)(s < 1 ? 1 : s > 64 ? 64 : s);
 }
@@ -1123,7 +1128,7 @@ backward_layout layout_of(int n, int seqs, int q_len, int kv_len, int heads, int
 }  // namespace
 
 size_t hdet_attend_bytes(int n, int seqs, int q_len, int kv_len, int heads, int kv_heads, int head_dim) {
-  const int s = few_splits(n, seqs, q_len, kv_len, heads, kv_heads);
+  const int s = few_splits(n, seqs, q_len, kv_len, heads, kv_heads, head_dim, 0);   // (a window: no more parts)
   if (s <= 1) return 0;
   const size_t ncg = ((size_t)(heads / kv_heads) * q_len + 31) / 32;
   return up256((size_t)n * seqs * kv_heads * ncg * s * 32 * ((head_dim <= 64 ? 64 : 128) + 2) * 4);
@@ -1139,7 +1144,7 @@ hipError_t hdet_launch_attend(const hdet_attention_args& a, hipStream_t s) {
   g.lse = a.lse_dev;
   if ((int64_t)a.seqs * a.q_len == 0) return hipSuccess;
   const bool wh = whole(a.q, size, a.head_dim) && whole(a.k, size, a.head_dim) && whole(a.v, size, a.head_dim) && whole(a.out, size, a.head_dim);
-  const int splits = few_splits(a.n_replicas, a.seqs, a.q_len, a.kv_len, a.heads, a.kv_heads);
+  const int splits = few_splits(a.n_replicas, a.seqs, a.q_len, a.kv_len, a.heads, a.kv_heads, a.head_dim, a.window);
   if (splits) {
     const int64_t pairs = (int64_t)g.group * a.q_len, groups = (int64_t)a.n_replicas * a.seqs * a.kv_heads;
     g.splits = splits;

@@ -291,6 +291,16 @@ def test_few_queries_over_many_keys(n, seqs, q_len, kv_len, heads, kv_heads, d, 
     run_and_check(q, k, v, dout, heads, kv_heads, seqs, back=False, positions=none)
 
 
+@pytest.mark.parametrize("kv_len", [256, 8192])
+@pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
+def test_late_scores_that_nearly_leave_the_range(dtype, kv_len):
+    """One key of every 32 from the 128th on is ahead of all others by 2^126.96: exponentials relative to the first keys are in fp32's range, their sum is not."""
+    q, k, v, _ = inputs(1, 1, 1, kv_len, 1, 1, 16, dtype, seed=5)
+    q.zero_()[..., 0] = 1.0
+    k.zero_()[:, 128::32, 0] = 88.0
+    run_and_check(q, k, v, None, 1, 1, 1, back=False, scale=1.0, causal=False)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
 def test_a_cache_with_room_that_nobody_has_written(dtype):
     n, seqs, kv_len = 2, 2, 3000

@@ -24,6 +24,7 @@
 #include <limits.h>
 #include <math.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "hdet_ops.h"
@@ -641,7 +642,9 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
   const float c = EXTRA ? 1.f : g.c;
   const int hi = br.hi, first = br.lo / S::TB, last = (hi + S::TB - 1) / S::TB;
   // this block's part of the tiles
-  const int share = hi > 0 ? (last - first + g.splits - 1) / g.splits : 0, t0 = first + split * share, t1 = hi > 0 ? min(last, t0 + share) : t0;
+  // (rows of few keys, which form their dots first: the first part takes them all)
+  const bool few_keys = sizeof(T) == 2 && br.pairs < 40 * min(RB, g.q_len - (wq0 - w * WR));
+  const int parts = few_keys ? 1 : g.splits, share = hi > 0 ? (last - first + parts - 1) / parts : 0, t0 = first + split * share, t1 = hi > 0 ? min(last, t0 + share) : t0;
 
   f16v dq[S::ND];                          // [column][query]
   // sum over the keys of p (dp - dot): what the dot lacks for out's rounding, since the p sum to 1
@@ -701,7 +704,7 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
   };
   // Few keys a row: a dot that is off by out's rounding is off by as much in all of them, and the sum of dz k does not average that away (two keys: dq off by 2.4 times its
   // own rounding): the dots first, then.  Many: it does (1.1 to 1.3 times), with dz in two bfloat16 parts (1.5 in one).
-  if (sizeof(T) == 2 && g.splits == 1 && br.pairs < 40 * min(RB, g.q_len - (wq0 - w * WR))) {
+  if (few_keys && split == 0) {
     walk(std::false_type(), std::true_type());
     ndot -= lack + other_half(lack);
     __syncthreads();
@@ -1090,26 +1093,33 @@ int few_splits(int n, int seqs, int q_len, int kv_len, int heads, int kv_heads, 
 }
 constexpr size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Parts of a block's walk in the backward pass, where there are fewer blocks than CUs: of `tiles` tiles, two at least a part
-int parts_of(int64_t blocks, int64_t tiles) {
+// Parts of a block's walk in the backward pass, of `tiles` tiles: where there are fewer blocks than CUs, two tiles at least a part; up to two blocks a CU of eight tiles at least and, of up
+// to 64 columns, four of sixteen, since one or two blocks leave a CU waiting (the backward pass, us: 8 x 8 x 1024 tokens, 8 heads of 64 over 2: 128, 100; 4096 of 8 x 64: 235, 166; 8192 of
+// 4 x 64: 453, 220; 4096 of 8 over 2 x 128: 303, 234; fp32 2 x 2048 of 8 x 128: 954, 604.  Four blocks a CU of 128 columns: 2 x 2048 of 16 x 128 272, 305).
+int parts_of(int64_t blocks, int64_t tiles, int head_dim) {
   if (blocks == 0) return 1;
-  int64_t s = hdet_compute_units() / blocks;
-  if (s > tiles / 2) s = tiles / 2;
+  const int64_t cus = hdet_compute_units();
+  int64_t s = std::max(std::min(cus / blocks, tiles / 2), std::min(2 * cus / blocks, tiles / 8));
+  if (head_dim <= 64) s = std::max(s, std::min(4 * cus / blocks, tiles / 16));
   return (int)(s < 1 ? 1 : s > 16 ? 16 : s);
 }
+// Keys (queries) that 128 queries (keys) see of a sequence of `len`, without arrays of ranges
+int within(int window, int len) { return window && window < len - RB ? window + RB : len; }
+// .. and parts of two tiles at least
+int dkv_most(int window, int q_len, int group) { return (int)std::max<int64_t>(1, (int64_t)((within(window, q_len) + 63) / 64) * group / 2); }
 // .. over the keys for dq; over the query tiles of the heads that share a key head for dk and dv
-int dq_splits(int n, int seqs, int q_len, int kv_len, int heads) {
-  return parts_of((int64_t)n * seqs * heads * ((q_len + RB - 1) / RB), kv_len < 512 ? 1 : (kv_len + 63) / 64);
+int dq_splits(int n, int seqs, int q_len, int kv_len, int heads, int head_dim) {
+  return parts_of((int64_t)n * seqs * heads * ((q_len + RB - 1) / RB), kv_len < 512 ? 1 : (kv_len + 63) / 64, head_dim);
 }
-int dkv_splits(int n, int seqs, int q_len, int kv_len, int heads, int kv_heads) {
-  return parts_of((int64_t)n * seqs * kv_heads * ((kv_len + RB - 1) / RB), (int64_t)((q_len + 63) / 64) * (heads / kv_heads));
+int dkv_splits(int n, int seqs, int q_len, int kv_len, int heads, int kv_heads, int head_dim) {
+  return parts_of((int64_t)n * seqs * kv_heads * ((kv_len + RB - 1) / RB), (int64_t)((q_len + 63) / 64) * (heads / kv_heads), head_dim);
 }
 
 struct backward_layout { size_t lse2, dot, lo, hi, pos, groups, lacks, part, total; };
 backward_layout layout_of(int n, int seqs, int q_len, int kv_len, int heads, int kv_heads, int d) {
   const size_t rows = (size_t)n * seqs * q_len;
   const size_t wide = d <= 64 ? 64 : 128, keys = (size_t)n * seqs * kv_len;
-  const size_t q_parts = dq_splits(n, seqs, q_len, kv_len, heads), k_parts = dkv_splits(n, seqs, q_len, kv_len, heads, kv_heads);
+  const size_t q_parts = dq_splits(n, seqs, q_len, kv_len, heads, d), k_parts = dkv_splits(n, seqs, q_len, kv_len, heads, kv_heads, d);
   // (the parts of dq have been joined when those of dk and dv are made)
   const size_t dq_part = q_parts > 1 ? q_parts * rows * heads * wide * 4 : 0, dkv_part = k_parts > 1 ? k_parts * keys * kv_heads * 2 * wide * 4 : 0;
   backward_layout l;
@@ -1189,13 +1199,14 @@ hipError_t hdet_launch_attend_backward(const hdet_attention_grad_args& a, hipStr
   with_shape(a.dtype, a.head_dim, extra(a, g), wh, [&](auto t, auto d, auto ex, auto w) {
     typedef decltype(t) T;
     set_blocks(g, nq, (unsigned)a.n_replicas * a.seqs * a.heads);
-    g.splits = dq_splits(a.n_replicas, a.seqs, a.q_len, a.kv_len, a.heads);
+    // (a window shortens the walks: no more parts than the workspace has)
+    g.splits = dq_splits(a.n_replicas, a.seqs, a.q_len, within(a.window, a.kv_len), a.heads, a.head_dim);
     g.total *= g.splits;
     if (g.total) hipLaunchKernelGGL((attend_dq_kernel<T, d, ex, w>), grid_of(g.total), dim3(THREADS), 0, s, g);
     if (g.total && g.splits > 1)
       hipLaunchKernelGGL((attend_dq_join_kernel<T, d>), grid_of((unsigned)(((int64_t)a.n_replicas * a.seqs * a.q_len * a.heads * d + THREADS - 1) / THREADS)), dim3(THREADS), 0, s, g);
     set_blocks(g, nk, (unsigned)a.n_replicas * a.seqs * a.kv_heads);
-    g.splits = dkv_splits(a.n_replicas, a.seqs, a.q_len, a.kv_len, a.heads, a.kv_heads);
+    g.splits = std::min(dkv_splits(a.n_replicas, a.seqs, a.q_len, a.kv_len, a.heads, a.kv_heads, a.head_dim), dkv_most(a.window, a.q_len, g.group));
     g.total *= g.splits;
     constexpr int tb = shape<T, d>::TB;
     const int64_t share = ((int64_t)((a.q_len + tb - 1) / tb) * g.group + g.splits - 1) / g.splits;

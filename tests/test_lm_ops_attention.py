@@ -122,6 +122,20 @@ def test_few_queries_of_many_heads(q_len, heads, kv_heads, d):
         assert distance(x, want[name]) <= 1.1 * distance(want[name].to(BF16), want[name]), name
 
 
+@pytest.mark.parametrize("d", [64, 128])
+def test_short_documents_in_a_long_sequence(d):
+    """dq of rows that attend one or two keys of 2100, where the walk over the keys is divided: as far from 64 bits as its own rounding takes it (a tenth is allowed for dz in two parts and
+    for fp32)."""
+    q_len = 2100
+    q, k, v, dout = inputs(1, 1, q_len, q_len, 2, 1, d, BF16, seed=d)
+    first = ints((torch.arange(q_len) // 2 * 2)[None])
+    out, lse = forward(q, k, v, 2, 1, 1, first=first)
+    want = R.attention(q, k, v, 2, 1, 1, dout, first=first)
+    dq = backward(q, k, v, out, lse, dout, 2, 1, 1, first=first)[0]
+    assert distance(dq, want["dq"]) <= 1.1 * distance(want["dq"].to(BF16), want["dq"])
+    assert not dq[:, ::2].any()
+
+
 @pytest.mark.parametrize("heads,kv_heads,d", [(32, 8, 64), (32, 8, 128)])
 def test_gradients_of_many_rows_in_fp32(heads, kv_heads, d):
     """Four heads of 1088 rows to a key.  A running sum over M rows rounds M times, each 2^-24 / sqrt(3) (times 0.72, a mantissa's mean) of a sum that the first queries, which attend few

@@ -1081,12 +1081,12 @@ template <typename F> void with_shape(int dtype, int d, int ex, bool wh, F f) {
 // the keys, are no more than fit the chip at once, a block's way being four times as short (us; 128 queries a block, 32):
 //   blocks of 32   8 x 8 x 512 keys, 64 columns 256: 12.1, 9.4     fp32 45, 17       16 x 8 x 1024 512: 19.6, 13.8     8 x 8 x 2048 512: 33.5, 18.0      8 x 8 x 4096 1024: 62, 43.5
 //   128 columns    8 x 512 128: 15.9, 11.2      32 x 512 queries of 8192 keys 512: 194, 108     16 x 2048 1024: 47, 61
-// (fewer keys, or a block a CU more: the join, 64 to 128 KB of LDS a block and four times the tiles cost more: 6 x 333 keys of 8 x 128 13, 33.)
+// (Under 128 keys two or more of the four wavefronts have nothing: 32 keys of 16 x 4, fp32, 7.8, 9.4.  With more blocks the join, 64 to 128 KB of LDS a block and four times the tiles cost more: 6 x 333 keys of 8 x 128 13, 33.)
 int few_splits(int n, int seqs, int q_len, int kv_len, int heads, int kv_heads, int head_dim, int window) {
   const int64_t pairs = (int64_t)(heads / kv_heads) * q_len, groups = (int64_t)n * seqs * kv_heads, cus = hdet_compute_units();
   if (pairs == 0 || groups == 0) return 0;
   const int64_t seen = (int64_t)window + (q_len < RB ? q_len : RB), keys = window && seen < kv_len ? seen : kv_len, few = groups * ((pairs + 31) / 32);
-  if (q_len > 16 && few > (keys < 1024 ? cus : keys < 2048 ? 2 * cus : 4 * cus) / (head_dim > 64 && keys >= 1024 ? 2 : 1)) return 0;
+  if (q_len > 16 && (keys < 128 || few > (keys < 1024 ? cus : keys < 2048 ? 2 * cus : 4 * cus) / (head_dim > 64 && keys >= 1024 ? 2 : 1))) return 0;
   int64_t s = (2 * cus + few - 1) / few, most = keys < 1024 ? 1 : (keys + 255) / 256;
   if (s > most) s = most;
   return (int)(s < 1 ? 1 : s > 64 ? 64 : s);

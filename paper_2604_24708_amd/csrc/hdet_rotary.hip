@@ -20,7 +20,7 @@
 namespace {
 
 constexpr int THREADS = 256;
-constexpr int MAX_ROWS = 16;               // rows of a block's table at a time
+constexpr int MAX_ROWS = 16;               // rows of a block's table at a time, where they are not needed to give every thread a head
 constexpr int MAX_TABLE = 1024;            // pairs of the table: 8 KiB
 
 struct side {                              // the queries or the keys
@@ -371,12 +371,14 @@ int team_of(int d, int each) {
   return t;
 }
 
-// Rows of a block's table: at least as many as give every thread a head, within the table
+// Rows of a block's table: as many as give every thread a head (few heads of few columns: 4 x 16 sequences of 2525 tokens, 3 heads of 16, forward and backward 117 us, 198 in
+// tables of up to 16 rows), while that leaves two blocks a CU, within the table
 int table_rows_of(int64_t rows, int n, int d, int half, int heads) {
-  int most = half ? MAX_TABLE / half : MAX_ROWS;
-  if (most > MAX_ROWS) most = MAX_ROWS;
+  int most = half ? MAX_TABLE / half : MAX_TABLE;
   int want = THREADS / team_of(d, 8) / heads;
   if (want < 1) want = 1;
+  while (want > MAX_ROWS && rows * n / want < 2 * (int64_t)hdet_compute_units()) want /= 2;
+  if (most > MAX_ROWS && most > want) most = want > MAX_ROWS ? want : MAX_ROWS;
   // large calls: more rows a table, for fewer waits; small ones: a row a block, for more blocks
   while (want < most && rows * n / (2 * want) >= 8 * (int64_t)hdet_compute_units()) want *= 2;
   return want < most ? want : most;

@@ -751,13 +751,13 @@ template <typename T, int D> __global__ __launch_bounds__(THREADS) void attend_d
 // backward, step 2: dk and dv; block = 128 keys of a key head, walks over the query tiles of the heads that share it
 // ---------------------------------------------------------------------------------------------
 // bfloat16 heads of more than 64 columns: two wavefronts to 32 keys, one to either half of a query tile, and the own keys and values in LDS, since in registers they leave
-// room for one wavefront a SIMD (the backward pass of 2 x 8192 tokens, 8 query and 2 key heads of 128: 1610 us, in registers 2231; 8 x 4 x 1024 tokens of 8 and 8: 440, 530)
+// room for one wavefront a SIMD (the backward pass of 2 x 8192 tokens, 8 query and 2 key heads of 128, in undivided walks: 1610 us, in registers 2231; 8 x 4 x 1024 tokens of 8 and 8: 440, 530)
 template <typename T, int D> constexpr bool dkv_paired() { return sizeof(T) == 2 && D == 128; }
 template <typename T, int D> constexpr int dkv_threads() { return dkv_paired<T, D>() ? 512 : 256; }
 template <typename T, int D, int EXTRA, bool TWO> constexpr int dkv_waves() { return sizeof(T) == 2 ? (D == 64 && !EXTRA && !TWO ? 3 : 2) : D == 64 ? 2 : 1; }
 // Query tiles that one launch sums up: in fp32 1024 rows, and the next launch adds its sums to what the one before has written, since a running sum over all rows of the heads
 // that share a key head rounds once a row (4 heads of 1088 rows: dk and dv off by 1.3e-6 of their norms,
-// in runs by 7.9e-7; 2 x 8192 tokens of 4 heads and one key head: the backward pass 3400 -> 3780 us)
+// in runs by 7.9e-7; 2 x 8192 tokens of 4 heads and one key head: the backward pass in undivided walks 3400 -> 3780 us)
 template <typename T, int D> constexpr int run_tiles() { return sizeof(T) == 2 ? 1 << 28 : 1024 / shape<T, D>::TB; }
 // TWO: dk and dv from dz and p in two bfloat16 parts each
 template <typename T, int D, int EXTRA, bool WHOLE, bool TWO> __global__ __launch_bounds__((dkv_threads<T, D>()), (dkv_waves<T, D, EXTRA, TWO>())) void attend_dkv_kernel(const attend_args g) {

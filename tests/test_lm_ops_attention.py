@@ -91,6 +91,13 @@ def test_walks_in_parts(d, dtype):
     R.check(torch.where(reached, torch.zeros_like(dv), dv), want["dv"].masked_fill(reached, 0.0), want["bound_dv"], "dv")
 
 
+@pytest.mark.parametrize("d", [64, 50])
+def test_runs_of_rows_in_divided_walks(d):
+    """fp32, more than 1024 rows to a part of a walk: the parts are made by several launches that add up."""
+    q, k, v, dout = inputs(1, 1, 6200, 6200, 4, 1, d, F32, seed=d)
+    run_and_check(q, k, v, dout, 4, 1, 1)
+
+
 @pytest.mark.parametrize("dtype", [BF16, F32], ids=["bf16", "f32"])
 def test_nothing_to_do(dtype):
     # no queries: the keys' gradients are 0; no keys: every query is empty

@@ -6,6 +6,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <initializer_list>
 
 namespace {
 
@@ -172,6 +173,12 @@ template <typename A> void attention_arguments(argument_checks& c, const A& a) {
   c.vector("positions_dev", a.positions_dev, n, rows, rows, false, false);
   c.vector("first_dev", a.first_dev, n, rows, rows, false, false);
   c.vector("end_dev", a.end_dev, n, rows, rows, false, false);
+}
+
+// Outputs that start where an input or another output does
+void written_apart(argument_checks& c, std::initializer_list<const void*> outputs, std::initializer_list<const void*> inputs, bool any) {
+  for (auto o = outputs.begin(); any && o != outputs.end(); ++o)
+    c.need(std::find(inputs.begin(), inputs.end(), *o) == inputs.end() && std::find(o + 1, outputs.end(), *o) == outputs.end(), "an output lies over an input or another output");
 }
 
 void clip_sizes(argument_checks& c, int n, int tensors) {
@@ -468,6 +475,7 @@ extern "C" int hdet_attention(const hdet_attention_args* a, void* stream) {
     const int64_t rows = (int64_t)a->seqs * a->q_len;
     c.matrix("out", a->out, n, rows, (int64_t)a->heads * a->head_dim, element(a->dtype), true, true);
     c.vector("lse_dev", a->lse_dev, n, rows * a->heads, rows * a->heads, false, true);
+    written_apart(c, {a->out.dev}, {a->q.dev, a->k.dev, a->v.dev}, rows * a->kv_len > 0);
     c.workspace(a->workspace_dev, a->workspace_bytes, hdet_attend_bytes(n, a->seqs, a->q_len, a->kv_len, a->heads, a->kv_heads, a->head_dim));
   }, [&] { return hdet_launch_attend(*a, (hipStream_t)stream); });
 }
@@ -494,6 +502,7 @@ extern "C" int hdet_attention_backward(const hdet_attention_grad_args* a, void* 
     c.matrix("dq", a->dq, n, rows, wide, size, true, true);
     c.matrix("dk", a->dk, n, keys, narrow, size, true, true);
     c.matrix("dv", a->dv, n, keys, narrow, size, true, true);
+    written_apart(c, {a->dq.dev, a->dk.dev, a->dv.dev}, {a->q.dev, a->k.dev, a->v.dev, a->out.dev, a->dout.dev}, rows * a->kv_len > 0);
     c.workspace(a->workspace_dev, a->workspace_bytes, hdet_attend_backward_bytes(n, a->seqs, a->q_len, a->kv_len, a->heads, a->kv_heads, a->head_dim));
   }, [&] { return hdet_launch_attend_backward(*a, (hipStream_t)stream); });
 }

@@ -45,15 +45,16 @@ def rotary_grad(**kw):
 def attention(**kw):
     a = B.hdet_attention_args(n_replicas=2, dtype=H.HDET_TYPE_BF16, seqs=2, q_len=3, kv_len=5, heads=4, kv_heads=2, head_dim=16, causal=1, scale=0.25, lse_dev=P,
                               slopes_dev=P, slopes_stride=4, positions_dev=P, first_dev=P, end_dev=P, workspace_dev=P, workspace_bytes=1 << 30)
-    a.q, a.out, a.k, a.v = rows(64, 384), rows(64, 384), rows(32, 320), rows(32, 320)
+    a.q, a.out, a.k, a.v = rows(64, 384), rows(64, 384, 2 * P), rows(32, 320), rows(32, 320)
     return fill(a, kw)
 
 
 def attention_grad(**kw):
     a = B.hdet_attention_grad_args(n_replicas=2, dtype=H.HDET_TYPE_F32, seqs=2, q_len=3, kv_len=5, heads=4, kv_heads=2, head_dim=16, causal=1, scale=0.25, lse_dev=P,
                                    slopes_dev=P, slopes_stride=4, workspace_dev=P, workspace_bytes=1 << 30)
-    a.q = a.out = a.dout = a.dq = rows(64, 384)
-    a.k = a.v = a.dk = a.dv = rows(32, 320)
+    a.q = a.out = a.dout = rows(64, 384)
+    a.k = a.v = rows(32, 320)
+    a.dq, a.dk, a.dv = rows(64, 384, 2 * P), rows(32, 320, 3 * P), rows(32, 320, 4 * P)
     return fill(a, kw)
 
 
@@ -84,10 +85,10 @@ BAD = [
         dict(q=rows(64, 192, None)), dict(k=rows(32, 96, None)), dict(dq_out=rows(64, 192, None)), dict(dk_out=rows(32, 96, None)), dict(dq=rows(64, 192, None)),
         dict(dk=rows(32, 96, None)), dict(dq=rows(64, 128)), dict(q_gain_dev=None), dict(k_gain_dev=None), dict(dq_gain_stride=15), dict(dk_gain_stride=15),
         dict(workspace_dev=None), dict(workspace_bytes=100), dict(workspace_dev=P + 8)]),
-    ("hdet_attention", attention, SIZES + [dict(out=rows(64, 384, None)), dict(out=rows(64, 200)), dict(lse_dev=P + 2)]),
+    ("hdet_attention", attention, SIZES + [dict(out=rows(64, 384, None)), dict(out=rows(64, 200, 2 * P)), dict(lse_dev=P + 2), dict(out=rows(64, 384))]),
     ("hdet_attention_backward", attention_grad, SIZES + [
         dict(out=rows(64, 384, None)), dict(dout=rows(64, 384, None)), dict(lse_dev=None), dict(dq=rows(64, 384, None)), dict(dk=rows(32, 320, None)),
-        dict(dv=rows(32, 320, None)), dict(dk=rows(32, 200)), dict(dv=rows(30, 320)), dict(workspace_bytes=0), dict(workspace_dev=None), dict(workspace_dev=P + 4)]),
+        dict(dv=rows(32, 320, None)), dict(dk=rows(32, 200, 3 * P)), dict(dv=rows(30, 320, 4 * P)), dict(dq=rows(64, 384)), dict(dv=rows(32, 320)), dict(dv=rows(32, 320, 3 * P)), dict(workspace_bytes=0), dict(workspace_dev=None), dict(workspace_dev=P + 4)]),
     ("hdet_clip_gradients", clip, [
         dict(n_replicas=0), dict(n_replicas=65), dict(n_tensors=-1), dict(n_tensors=H.HDET_MAX_GRAD_TENSORS + 1), dict(tensors_host=None), dict(grad_mode=2),
         dict(max_norm=-1.0), dict(max_norm=NAN), dict(norm_dev=None), dict(norm_dev=P + 2), dict(workspace_bytes=0), dict(workspace_dev=None), dict(workspace_dev=P + 8),

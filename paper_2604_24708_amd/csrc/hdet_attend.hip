@@ -8,9 +8,11 @@
 // In units of log2 throughout: p = 2^(z log2 e - m), one fma and one exponential a score.
 //
 // A pair that is not attended must leave no trace, but 0 times an infinity or a NaN does: the matrix cores multiply all of a block that lies across the
-// ranges.  Results that came out finite are right; where one did not, the block walks its tiles a second time with zeros for what is not finite in
-// the second product's tiles.  What of that is attended comes back by itself where it has made scores, statistics or row dots what they are; the values'
-// and the output gradients' own entries, which have not, are added to the results of the rows that attend them (add_not_finite).
+// ranges.  Results that came out finite are right; where one did not, the block walks its tiles a second time, and the second product takes zeros for
+// what is not finite.  Scores and row dots are formed from the tiles as they are both times: a score of minus infinity has p = 0, that of an infinite
+// entry under a cap is the cap, and the other columns of such rows are finite.  The entries left out are then added to the results of the rows that
+// attend them (add_not_finite): values and output gradients times p, which is 0 for a score of minus infinity and more for any other; keys and queries
+// times dz, which is 0 wherever an entry is infinite and its row's statistics are finite (p is 0, or the cap's derivative): NaN.
 
 // Four kernels: attend (128 queries of a head a block), attend_few (few queries: the keys are divided over the chip), attend_dq and attend_dkv (backward; S = q k and dp are formed in
 // both, since one kernel for all three gradients would add up dq with atomics, in an order that changes).  A wavefront owns 32 rows, as columns of the 32 x 32 products, so that a
@@ -363,10 +365,6 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
       T* const vt = kt + TILE;
       free = slot;
       slot = slot == STAGES - 1 ? 0 : slot + 1;
-      if (decltype(clean)::value) {
-        clean_tile<T, D, S::TB>(vt, tid, THREADS);
-        __syncthreads();
-      }
 #pragma unroll 1
       for (int i = 0; i < NB; ++i) {
         const int kb = t * S::TB + 32 * i;
@@ -380,7 +378,7 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
           for (int e = 0; e < 16; ++e) x[e] = from + acc_row(e, 0) < len ? x[e] : -INFINITY;
         }
         z.template take<decltype(follow)::value>(x, unit.mult);
-        at.second(vt + i * 32 * D, x, z.o);
+        at.template second<decltype(clean)::value>(vt + i * 32 * D, x, z.o);
       }
     };
     // the reference follows the maximum until every row has met a key; all the way on the second walk, and where scores fall with the distance
@@ -407,7 +405,8 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
   if (again) {
     __threadfence_block();
     add_not_finite<T, D>(vals.src, g.v_s, g.d, wr.lo_min, wr.hi_max, (T*)g.out + r * g.out_z + row0 * g.out_s + col, g.out_s, min(WR, g.q_len - wq0), lane,
-                         [&](int key, int i) { return key >= __builtin_amdgcn_readlane(range.lo, i) && key < __builtin_amdgcn_readlane(range.hi, i); });
+                         [&](int key, int i) { return key >= __builtin_amdgcn_readlane(range.lo, i) && key < __builtin_amdgcn_readlane(range.hi, i); },
+                         [&](int key, int i) { return pair_weight((const T*)g.q + r * g.q_z + (row0 + i) * g.q_s + col, keys.src + key * g.k_s, g.d, g.scale, g.cap2 > 0.f, lane); });
   }
 }
 
@@ -465,10 +464,6 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
       asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"n"(IN_FLIGHT) : "memory");
       T* const kt = mine + stage * (2 * TILE);
       stage ^= 1;
-      if (decltype(clean)::value) {
-        clean_tile<T, D, 32>(kt + TILE, lane, 64);
-        wave_fence();
-      }
       f16v x = at.first(kt, fq, all16(0.f));
       const int k0 = t * 32 + ((lane >> 5) << 2);
       if (EXTRA) shape_scores<EXTRA>(g, x, slope2, [&](int e) { return distance(range.pos, k0 + acc_row(e, 0)); });
@@ -478,7 +473,7 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
         for (int e = 0; e < 16; ++e) x[e] = from + acc_row(e, 0) < len ? x[e] : -INFINITY;
       }
       z.template take<decltype(follow)::value>(x, unit.mult);
-      at.second(kt + TILE, x, z.o);
+      at.template second<decltype(clean)::value>(kt + TILE, x, z.o);
     };
     int t = ts + w;
     for (bool met = false; t < te && !met; t += NW) {
@@ -507,7 +502,12 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
     wave_fence();
     for (int t = ts + w; t < te; t += NW)
       add_not_finite<T, D>(vals.src, g.v_s, g.d, t * 32, min(t * 32 + 32, hi), joint + w * 32 * P, P, 32, lane,
-                           [&](int key, int i) { return key >= __builtin_amdgcn_readlane(range.lo, i) && key < __builtin_amdgcn_readlane(range.hi, i); });
+                           [&](int key, int i) { return key >= __builtin_amdgcn_readlane(range.lo, i) && key < __builtin_amdgcn_readlane(range.hi, i); },
+                           [&](int key, int i) {
+                             const int64_t own_row = (int64_t)b * g.q_len + __builtin_amdgcn_readlane(qi, i);
+                             return pair_weight((const T*)g.q + r * g.q_z + own_row * g.q_s + (int64_t)__builtin_amdgcn_readlane(h, i) * g.d, keys.src + key * g.k_s, g.d, g.scale,
+                                                g.cap2 > 0.f, lane);
+                           });
   }
   if (lane < 32) {
     stats[w * 64 + lane] = z.m;
@@ -655,7 +655,7 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
     keys.load((int64_t)t * S::TB, t < t1 ? hi - t * S::TB : 0, to);
     vals.load((int64_t)t * S::TB, t < t1 ? hi - t * S::TB : 0, to + TILE);
   };
-  // clean: zeros for what is not finite; dots: no more than `lack`
+  // clean: zeros for keys that are not finite, in the second product; dots: no more than `lack`
   auto walk = [&](auto clean, auto dots) {
 #pragma unroll
     for (int i = 0; i < S::ND; ++i) dq[i] = all16(0.f);
@@ -669,10 +669,6 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
       T* const tiles = smem + slot * (2 * TILE);
       free = slot;
       slot = slot == STAGES - 1 ? 0 : slot + 1;
-      if (decltype(clean)::value) {
-        clean_tile<T, D, S::TB>(tiles, tid, THREADS);
-        __syncthreads();
-      }
 #pragma unroll 1
       for (int i = 0; i < NB; ++i) {
         const int key0 = t * S::TB + 32 * i;
@@ -697,7 +693,7 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
           lack += dp[e];
           if (EXTRA) dp[e] *= bend[e];
         }
-        if (!decltype(dots)::value) at.second_in_two(kt, dp, dq);
+        if (!decltype(dots)::value) at.template second_in_two<decltype(clean)::value>(kt, dp, dq);
       }
     }
     wait_and_barrier<0>();
@@ -710,7 +706,8 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
     __syncthreads();
   }
   walk(std::false_type(), std::false_type());
-  if (block_any(some && finite_of(lse2) && not_finite(dq), w, lane, (int*)(smem + 2 * STAGES * TILE) - NWV)) walk(std::true_type(), std::false_type());
+  const bool again = block_any(some && finite_of(lse2) && not_finite(dq), w, lane, (int*)(smem + 2 * STAGES * TILE) - NWV);
+  if (again) walk(std::true_type(), std::false_type());
   lack += other_half(lack);
   if (there && lane < 32) {
     if (g.splits == 1) g.dot[stat] = ndot - lack;
@@ -721,12 +718,17 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
 #pragma unroll
     for (int e = 0; e < 16; ++e) dq[i][e] *= g.scale;
   char* const strip = (char*)smem + w * STRIP;
-  if (g.splits == 1) {
-    store_rows<T, D, WHOLE>(dq, strip, (T*)g.dq + r * g.dq_z + row0 * g.dq_s + col, g.dq_s, g.q_len - wq0, g.d, lane);
-  } else {
-    float* const to = g.part + (((int64_t)split * g.n + r) * g.heads + h) * rows * D + row0 * D;
-    store_rows<float, D, false>(dq, strip, to, D, g.q_len - wq0, g.d, lane);
-  }
+  auto put = [&](auto to, int64_t ld, auto wh) {
+    typedef std::remove_pointer_t<decltype(to)> U;
+    store_rows<U, D, decltype(wh)::value>(dq, strip, to, ld, g.q_len - wq0, g.d, lane);
+    if (!again) return;
+    __threadfence_block();
+    add_not_finite<T, D>(keys.src, g.k_s, g.d, max(wr.lo_min, t0 * S::TB), min(wr.hi_max, t1 * S::TB), to, ld, min(WR, g.q_len - wq0), lane,
+                         [&](int key, int i) { return key >= __builtin_amdgcn_readlane(range.lo, i) && key < __builtin_amdgcn_readlane(range.hi, i); },
+                         [](int, int) { return 0.f; });
+  };
+  if (g.splits == 1) put((T*)g.dq + r * g.dq_z + row0 * g.dq_s + col, g.dq_s, std::integral_constant<bool, WHOLE>());
+  else put(g.part + (((int64_t)split * g.n + r) * g.heads + h) * rows * D + row0 * D, (int64_t)D, std::false_type());
 }
 
 // dq and the row dots from the splits' parts, [split][replica][head][row]
@@ -824,15 +826,20 @@ template <typename T, int D, int EXTRA, bool WHOLE, bool TWO> __global__ __launc
       tile_loader<T, D, S::TB, NW, WHOLE>(from_k, g.k_s, g.d, w, lane).load(i * S::TB, g.kv_len - k0 - i * S::TB, smem + RING + i * TILE);
       tile_loader<T, D, S::TB, NW, WHOLE>(from_v, g.v_s, g.d, w, lane).load(i * S::TB, g.kv_len - k0 - i * S::TB, smem + RING + RB * D + i * TILE);
     }
-  } else {
-    const T* const from_k = there ? (const T*)g.k + r * g.k_z + (row0 + (lane & 31)) * g.k_s + kcol : nullptr;
-    const T* const from_v = there ? (const T*)g.v + r * g.v_z + (row0 + (lane & 31)) * g.v_s + kcol : nullptr;
-#pragma unroll
-    for (int i = 0; i < S::NF; ++i) {
-      fk[i] = own_frag<T, D, WHOLE>(from_k, i, g.d, lane);
-      fv[i] = own_frag<T, D, WHOLE>(from_v, i, g.d, lane);
-    }
   }
+  // (again before a second walk, whose registers then leave the first walk's alone)
+  auto load_own = [&] {
+    if constexpr (!PAIRED) {
+      const T* const from_k = there ? (const T*)g.k + r * g.k_z + (row0 + (lane & 31)) * g.k_s + kcol : nullptr;
+      const T* const from_v = there ? (const T*)g.v + r * g.v_z + (row0 + (lane & 31)) * g.v_s + kcol : nullptr;
+#pragma unroll
+      for (int i = 0; i < S::NF; ++i) {
+        fk[i] = own_frag<T, D, WHOLE>(from_k, i, g.d, lane);
+        fv[i] = own_frag<T, D, WHOLE>(from_v, i, g.d, lane);
+      }
+    }
+  };
+  load_own();
   const S at(lane);
   const float c = EXTRA ? 1.f : g.c;
   const int t0 = last < 0 ? 0 : first / NB, tiles = last < 0 ? 0 : last / NB + 1 - t0;
@@ -877,10 +884,6 @@ template <typename T, int D, int EXTRA, bool WHOLE, bool TWO> __global__ __launc
       slot = slot == STAGES - 1 ? 0 : slot + 1;
       const int h = kh * g.group + j / tiles, t = t0 + j % tiles;
       const float slope2 = EXTRA == kGeneral && g.slopes ? g.slopes[r * g.slopes_z + h] * kLog2e : 0.f;
-      if (decltype(clean)::value) {
-        clean_tile<T, D, 2 * S::TB>(at_tiles, tid, NW * 64);
-        __syncthreads();
-      }
 #pragma unroll 1
       for (int i = half; i < (PAIRED ? half + 1 : NB); ++i) {
         const int gi = t * NB + i;
@@ -929,12 +932,13 @@ template <typename T, int D, int EXTRA, bool WHOLE, bool TWO> __global__ __launc
             }
           }
         }
+        constexpr bool CLEAN = decltype(clean)::value;
         if (TWO) {
-          at.second_in_two(qt + TILE, x, dv);
-          at.second_in_two(qt, dp, dk);
+          at.template second_in_two<CLEAN>(qt + TILE, x, dv);
+          at.template second_in_two<CLEAN>(qt, dp, dk);
         } else {
-          at.second(qt + TILE, x, dv);
-          at.second(qt, dp, dk);
+          at.template second<CLEAN>(qt + TILE, x, dv);
+          at.template second<CLEAN>(qt, dp, dk);
         }
       }
     }
@@ -942,7 +946,10 @@ template <typename T, int D, int EXTRA, bool WHOLE, bool TWO> __global__ __launc
   };
   walk(std::false_type());
   const bool again = block_any<NW>(there && (not_finite(dk) || not_finite(dv)), w, lane, (int*)(smem + RING) - NW);
-  if (again) walk(std::true_type());
+  if (again) {
+    load_own();
+    walk(std::true_type());
+  }
   if constexpr (PAIRED) {
     // the two halves' sums, as they lie in the lanes
     f4v* const part = reinterpret_cast<f4v*>(smem) + (w & 3) * (2 * S::ND * 4 * 64) + lane;
@@ -987,8 +994,12 @@ template <typename T, int D, int EXTRA, bool WHOLE, bool TWO> __global__ __launc
     for (int h = 0; h < g.group; ++h) {
       // the rows of this block's tiles of the head
       const int from = (t0 + min(max(begin - h * tiles, 0), tiles)) * S::TB, to = min(g.q_len, (t0 + min(max(all - h * tiles, 0), tiles)) * S::TB);
-      add_not_finite<T, D>(do_at + (int64_t)(kh * g.group + h) * g.d, g.do_s, g.d, from, to, to_v, v_s, min(WR, g.kv_len - wk0), lane,
-                           [&](int q, int i) { return wk0 + i >= g.lo[r * rows + q_row0 + q] && wk0 + i < g.hi[r * rows + q_row0 + q]; });
+      const int64_t head = (int64_t)(kh * g.group + h) * g.d;
+      auto seen = [&](int q, int i) { return wk0 + i >= g.lo[r * rows + q_row0 + q] && wk0 + i < g.hi[r * rows + q_row0 + q]; };
+      add_not_finite<T, D>(do_at + head, g.do_s, g.d, from, to, to_v, v_s, min(WR, g.kv_len - wk0), lane, seen, [&](int q, int i) {
+        return pair_weight(q_at + q * g.q_s + head, (const T*)g.k + r * g.k_z + (row0 + i) * g.k_s + kcol, g.d, g.scale, g.cap2 > 0.f, lane);
+      });
+      add_not_finite<T, D>(q_at + head, g.q_s, g.d, from, to, to_k, k_s, min(WR, g.kv_len - wk0), lane, seen, [](int, int) { return 0.f; });
     }
   };
   if (g.splits == 1) {

@@ -40,6 +40,13 @@ __device__ __forceinline__ int acc_row(int e, int lane) { return ((e >> 2) << 3)
 // LDS of a wavefront's own: what its lanes have written is there for its other lanes
 __device__ __forceinline__ void wave_fence() { asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory"); }
 
+// Zeros for what is not finite among two bfloat16 numbers, or in a number
+__device__ __forceinline__ unsigned finite_pair(unsigned x) {
+  return ((x & 0x7f80u) == 0x7f80u ? 0u : x & 0xffffu) | ((x & 0x7f800000u) == 0x7f800000u ? 0u : x & 0xffff0000u);
+}
+__device__ __forceinline__ unsigned finite_bits(unsigned x) { return (x & 0x7f800000u) == 0x7f800000u ? 0u : x; }
+
+// (CLEAN: the second product takes zeros for what is not finite in the tile, which stays as it is for the first)
 template <typename T, int D> struct shape;
 // bf16: v_mfma_f32_32x32x16_bf16; the second product's other operand comes through the transposing LDS read
 template <int D> struct shape<uint16_t, D> {
@@ -72,24 +79,31 @@ template <int D> struct shape<uint16_t, D> {
       acc = __builtin_amdgcn_mfma_f32_32x32x16_bf16(*reinterpret_cast<const frag*>(tile + k[i]), *reinterpret_cast<const frag*>(own + k[i]), acc, 0, 0, 0);
     return acc;
   }
+  // a lane's 8 entries of column block dt of 16 rows
+  template <bool CLEAN> __device__ __forceinline__ frag columns(const uint16_t* rows, int dt) const {
+    const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s4v __attribute__((address_space(3)))*)(rows + t[dt][0]));
+    const s4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s4v __attribute__((address_space(3)))*)(rows + t[dt][1]));
+    const s8v both = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+    if (!CLEAN) return __builtin_bit_cast(frag, both);
+    i4v words = __builtin_bit_cast(i4v, both);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) words[i] = (int)finite_pair((unsigned)words[i]);
+    __builtin_amdgcn_sched_barrier(0);     // one at a time: their temporaries would take the registers of the whole kernel
+    return __builtin_bit_cast(frag, words);
+  }
   // acc^T += (32 rows from `tile` on)^T x, x [row][own row] rounded to bf16
-  __device__ __forceinline__ void second(const uint16_t* tile, const f16v& x, f16v (&acc)[ND]) const {
+  template <bool CLEAN = false> __device__ __forceinline__ void second(const uint16_t* tile, const f16v& x, f16v (&acc)[ND]) const {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       frag f;
 #pragma unroll
       for (int i = 0; i < 8; ++i) f[i] = (__bf16)x[8 * j + i];
 #pragma unroll
-      for (int dt = 0; dt < ND; ++dt) {
-        const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s4v __attribute__((address_space(3)))*)(tile + 16 * j * D + t[dt][0]));
-        const s4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s4v __attribute__((address_space(3)))*)(tile + 16 * j * D + t[dt][1]));
-        const s8v both = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(frag, both), f, acc[dt], 0, 0, 0);
-      }
+      for (int dt = 0; dt < ND; ++dt) acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(columns<CLEAN>(tile + 16 * j * D, dt), f, acc[dt], 0, 0, 0);
     }
   }
   // the same with x in two parts, 16 bits of it
-  __device__ __forceinline__ void second_in_two(const uint16_t* tile, const f16v& x, f16v (&acc)[ND]) const {
+  template <bool CLEAN = false> __device__ __forceinline__ void second_in_two(const uint16_t* tile, const f16v& x, f16v (&acc)[ND]) const {
 #pragma unroll
     for (int j = 0; j < 2; ++j) {
       frag f, rest;
@@ -100,11 +114,9 @@ template <int D> struct shape<uint16_t, D> {
       }
 #pragma unroll
       for (int dt = 0; dt < ND; ++dt) {
-        const s4v lo = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s4v __attribute__((address_space(3)))*)(tile + 16 * j * D + t[dt][0]));
-        const s4v hi = __builtin_amdgcn_ds_read_tr16_b64_v4i16((s4v __attribute__((address_space(3)))*)(tile + 16 * j * D + t[dt][1]));
-        const s8v both = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(frag, both), f, acc[dt], 0, 0, 0);
-        acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(__builtin_bit_cast(frag, both), rest, acc[dt], 0, 0, 0);
+        const frag a = columns<CLEAN>(tile + 16 * j * D, dt);
+        acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, f, acc[dt], 0, 0, 0);
+        acc[dt] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(a, rest, acc[dt], 0, 0, 0);
       }
     }
   }
@@ -137,13 +149,17 @@ template <int D> struct shape<float, D> {
     }
     return acc;
   }
-  __device__ __forceinline__ void second(const float* tile, const f16v& x, f16v (&acc)[ND]) const {
+  template <bool CLEAN = false> __device__ __forceinline__ void second(const float* tile, const f16v& x, f16v (&acc)[ND]) const {
 #pragma unroll
     for (int e = 0; e < 16; ++e)
 #pragma unroll
-      for (int dt = 0; dt < ND; ++dt) acc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(tile[(e >> 2) * 8 * D + t[dt][e & 3]], x[e], acc[dt], 0, 0, 0);
+      for (int dt = 0; dt < ND; ++dt) {
+        float a = tile[(e >> 2) * 8 * D + t[dt][e & 3]];
+        if (CLEAN) a = __uint_as_float(finite_bits(__float_as_uint(a)));
+        acc[dt] = __builtin_amdgcn_mfma_f32_32x32x2f32(a, x[e], acc[dt], 0, 0, 0);
+      }
   }
-  __device__ __forceinline__ void second_in_two(const float* tile, const f16v& x, f16v (&acc)[ND]) const { second(tile, x, acc); }
+  template <bool CLEAN = false> __device__ __forceinline__ void second_in_two(const float* tile, const f16v& x, f16v (&acc)[ND]) const { second<CLEAN>(tile, x, acc); }
   static __device__ __forceinline__ f16v product(const frag& a, const frag& b, f16v acc) {
 #pragma unroll
     for (int u = 0; u < 4; ++u) acc = __builtin_amdgcn_mfma_f32_32x32x2f32(a[u], b[u], acc, 0, 0, 0);
@@ -168,22 +184,16 @@ __device__ __forceinline__ hdet_rsrc scalar_rsrc(const void* p, uint32_t bytes) 
   return r;
 }
 __device__ __forceinline__ bool finite_of(float x) { return fabsf(x) < INFINITY; }
-// Zeros for what is not finite in an LDS tile of ROWS rows; `t` of `count` threads
-template <typename T, int D, int ROWS> __device__ __forceinline__ void clean_tile(T* tile, int t, int count) {
-  typedef unsigned u4v __attribute__((ext_vector_type(4)));
-  for (int i = t; i < ROWS * shape<T, D>::C; i += count) {
-    u4v x = reinterpret_cast<u4v*>(tile)[i];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      if (sizeof(T) == 4) x[e] = (x[e] & 0x7f800000u) == 0x7f800000u ? 0u : x[e];
-      else x[e] = ((x[e] & 0x7f80u) == 0x7f80u ? 0u : x[e] & 0xffffu) | ((x[e] & 0x7f800000u) == 0x7f800000u ? 0u : x[e] & 0xffff0000u);
-    }
-    reinterpret_cast<u4v*>(tile)[i] = x;
-  }
+// Weight of a pair of rows whose results are not finite: 0 where its score is minus infinity, otherwise more (1 will do)
+template <typename T> __device__ __forceinline__ float pair_weight(const T* q, const T* k, int d, float scale, bool capped, int lane) {
+  if (capped) return 1.f;
+  float s = 0.f;
+  for (int c = lane; c < d; c += 64) s = __builtin_fmaf(hdet_ld(q + c), hdet_ld(k + c), s);
+  return hdet_wave_sum(s) * scale == -INFINITY ? 0.f : 1.f;
 }
-// What is not finite in rows from .. to - 1 of src is added to the rows of dst that attend them (seen(row, own row)): a wavefront's `have` rows
-template <typename T, int D, typename U, typename F>
-__device__ __forceinline__ void add_not_finite(const T* src, int64_t ld, int d, int from, int to, U* dst, int64_t dst_ld, int have, int lane, F seen) {
+// What is not finite in rows from .. to - 1 of src, times weight(row, own row), is added to the rows of dst that attend them (seen(row, own row)): a wavefront's `have` rows
+template <typename T, int D, typename U, typename F, typename G>
+__device__ __forceinline__ void add_not_finite(const T* src, int64_t ld, int d, int from, int to, U* dst, int64_t dst_ld, int have, int lane, F seen, G weight) {
   typedef shape<T, D> S;
   constexpr int ROWS = 64 / S::C;
   for (int j = from; j < to; j += ROWS) {
@@ -195,11 +205,13 @@ __device__ __forceinline__ void add_not_finite(const T* src, int64_t ld, int d, 
     if (!mask) continue;
     for (int i = 0; i < ROWS; ++i) {
       if (!(mask >> (i * S::C) & (S::C == 64 ? ~0ull : (1ull << (S::C & 63)) - 1))) continue;
-      for (int c = lane; c < d; c += 64) {
-        const float x = hdet_ld(src + (j + i) * ld + c);
-        if (finite_of(x)) continue;
-        for (int own = 0; own < have; ++own)
-          if (seen(j + i, own)) hdet_st(dst + own * dst_ld + c, hdet_ld(dst + own * dst_ld + c) + x);
+      for (int own = 0; own < have; ++own) {
+        if (!seen(j + i, own)) continue;
+        const float w = weight(j + i, own);
+        for (int c = lane; c < d; c += 64) {
+          const float x = hdet_ld(src + (j + i) * ld + c);
+          if (!finite_of(x)) hdet_st(dst + own * dst_ld + c, hdet_ld(dst + own * dst_ld + c) + x * w);
+        }
       }
     }
   }

@@ -332,7 +332,8 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
   const bool there = qi < g.q_len;
   const key_range range = there ? range_of(g, r, b, qi) : key_range{0, 0, 0};
   const int64_t col = (int64_t)h * g.d, kcol = (int64_t)over(h, g.by_group) * g.d, row0 = (int64_t)b * g.q_len + wq0;
-  const T* const own = there ? (const T*)g.q + r * g.q_z + (row0 + (lane & 31)) * g.q_s + col : nullptr;
+  // (a row that attends nothing is not read: without keys there need be no queries)
+  const T* const own = range.hi > range.lo ? (const T*)g.q + r * g.q_z + (row0 + (lane & 31)) * g.q_s + col : nullptr;
   typename S::frag fq[S::NF];
 #pragma unroll
   for (int i = 0; i < S::NF; ++i) fq[i] = own_frag<T, D, WHOLE>(own, i, g.d, lane);
@@ -433,7 +434,7 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
   const key_range range = there ? range_of(g, r, b, qi) : key_range{0, 0, 0};
   const wave_range wr = wave_range_of(range, there);
   const int64_t row = (int64_t)b * g.q_len + qi, kcol = (int64_t)kh * g.d;
-  const T* const own = there ? (const T*)g.q + r * g.q_z + row * g.q_s + (int64_t)h * g.d : nullptr;
+  const T* const own = range.hi > range.lo ? (const T*)g.q + r * g.q_z + row * g.q_s + (int64_t)h * g.d : nullptr;
   typename S::frag fq[S::NF];
 #pragma unroll
   for (int i = 0; i < S::NF; ++i) fq[i] = own_frag<T, D, WHOLE>(own, i, g.d, lane);
@@ -785,9 +786,9 @@ template <typename T, int D, int EXTRA, bool WHOLE, bool TWO> __global__ __launc
   const bool plain = !g.pos && !g.first && !g.end;
   int first = INT_MAX, last = -1;
   if (plain) {
-    const int64_t off = (int64_t)g.kv_len - g.q_len, from = g.causal ? k0 - off : 0, to = g.window ? (int64_t)k0 + RB + g.window - 2 - off : INT_MAX;
-    if (from < g.q_len && to >= 0) {
-      first = (int)(from > 0 ? from : 0) / 32;
+    const int64_t off = (int64_t)g.kv_len - g.q_len, from = g.causal && k0 > off ? k0 - off : 0, to = g.window ? (int64_t)k0 + RB + g.window - 2 - off : INT_MAX;
+    if (from < g.q_len && to >= 0) {       // (no queries: none)
+      first = (int)from / 32;
       last = (int)(to < g.q_len ? to : g.q_len - 1) / 32;
     }
   } else {
@@ -813,7 +814,12 @@ template <typename T, int D, int EXTRA, bool WHOLE, bool TWO> __global__ __launc
     first = __builtin_amdgcn_readfirstlane(first);
     last = __builtin_amdgcn_readfirstlane(last);
   }
-  const bool there = key < g.kv_len;
+  const int t0 = last < 0 ? 0 : first / NB, tiles = last < 0 ? 0 : last / NB + 1 - t0;
+  // this block's part of all heads' tiles (none: zeros, and keys and values are not read, which need not be there without queries)
+  const int share = (tiles * g.group + g.splits - 1) / g.splits, end = min(tiles * g.group, (int)(split + 1) * share), begin = split * share + g.run * run_tiles<T, D>(),
+            all = min(end, begin + run_tiles<T, D>());
+  if (g.run && begin >= all) return;
+  const bool there = key < g.kv_len && begin < all;
   const int64_t kcol = (int64_t)kh * g.d, row0 = (int64_t)b * g.kv_len + wk0, rows = (int64_t)g.seqs * g.q_len, q_row0 = (int64_t)b * g.q_len;
   typename S::frag fk[PAIRED ? 1 : S::NF], fv[PAIRED ? 1 : S::NF];
   T* const own_k = smem + RING + (w & 3) * WR * D;
@@ -823,8 +829,9 @@ template <typename T, int D, int EXTRA, bool WHOLE, bool TWO> __global__ __launc
     const T* const from_v = (const T*)g.v + r * g.v_z + ((int64_t)b * g.kv_len + k0) * g.v_s + kcol;
 #pragma unroll
     for (int i = 0; i < RB / S::TB; ++i) {
-      tile_loader<T, D, S::TB, NW, WHOLE>(from_k, g.k_s, g.d, w, lane).load(i * S::TB, g.kv_len - k0 - i * S::TB, smem + RING + i * TILE);
-      tile_loader<T, D, S::TB, NW, WHOLE>(from_v, g.v_s, g.d, w, lane).load(i * S::TB, g.kv_len - k0 - i * S::TB, smem + RING + RB * D + i * TILE);
+      const int have = begin < all ? g.kv_len - k0 - i * S::TB : 0;
+      tile_loader<T, D, S::TB, NW, WHOLE>(from_k, g.k_s, g.d, w, lane).load(i * S::TB, have, smem + RING + i * TILE);
+      tile_loader<T, D, S::TB, NW, WHOLE>(from_v, g.v_s, g.d, w, lane).load(i * S::TB, have, smem + RING + RB * D + i * TILE);
     }
   }
   // (again before a second walk, whose registers then leave the first walk's alone)
@@ -842,16 +849,10 @@ template <typename T, int D, int EXTRA, bool WHOLE, bool TWO> __global__ __launc
   load_own();
   const S at(lane);
   const float c = EXTRA ? 1.f : g.c;
-  const int t0 = last < 0 ? 0 : first / NB, tiles = last < 0 ? 0 : last / NB + 1 - t0;
-
   tile_loader<T, D, S::TB, NW, WHOLE> qs((const T*)g.q + r * g.q_z + q_row0 * g.q_s, g.q_s, g.d, w, lane);
   tile_loader<T, D, S::TB, NW, WHOLE> dos((const T*)g.dout + r * g.do_z + q_row0 * g.do_s, g.do_s, g.d, w, lane);
   const T *const q_at = qs.src, *const do_at = dos.src;
   f16v dk[S::ND], dv[S::ND];               // [column][key]
-  // this block's part of all heads' tiles
-  const int share = (tiles * g.group + g.splits - 1) / g.splits, end = min(tiles * g.group, (int)(split + 1) * share), begin = split * share + g.run * run_tiles<T, D>(),
-            all = min(end, begin + run_tiles<T, D>());
-  if (g.run && begin >= all) return;
   auto request = [&](int j, int slot) {    // tile j of all heads' tiles
     const int h = kh * g.group + (tiles ? j / tiles : 0), t = t0 + (tiles ? j % tiles : 0), q0 = t * S::TB, have = j < all ? min(g.q_len - q0, S::TB) : 0;
     qs.src = q_at + (int64_t)h * g.d;

@@ -485,7 +485,8 @@ int hdet_vocab_loss(const hdet_vocab_args* args, void* stream);
  * contexts leaves them (hdet_rotary_frequencies makes the usual ones); angles are formed and reduced
  * in 64 bits, good for any 32-bit position.  Row i of a replica stands at positions_dev[replica][i] or, where
  * that is NULL, at i mod period (i where period is 0).  Sums are fp32; those of squares 64 bits where they leave its range.
- * q_out may be q itself and k_out k itself.  k absent (dev NULL): q alone; its norm and the keys' are
+ * q_out may be q itself, with its strides, and k_out k itself; otherwise outputs lie apart from one another and from what the call reads.  (Refused
+ * where the library sees it: matrices of one start, and of the same strides.)  k absent (dev NULL): q alone; its norm and the keys' are
  * each left out where their gain is NULL.                                                    */
 enum { HDET_ROTARY_HALVES = 0, HDET_ROTARY_PAIRS = 1 };
 #define HDET_MAX_ROTARY_DIM 256
@@ -512,7 +513,7 @@ int hdet_head_rotary(const hdet_rotary_args* args, void* stream);
  * took (needed with a gain only).  With w = dq_out rotated back (by -a, times magnitude):
  *   dq = rstd (w gain - xh mean_c(w_c gain_c xh_c))   (w where the gain is NULL)
  *   dgain_c = sum over rows and heads of w_c xh_c     (in a fixed order; optional)
- * dq may be dq_out itself, dk dk_out.  workspace: hdet_head_rotary_backward_workspace bytes (needed
+ * dq may be dq_out itself or q, with their strides, dk dk_out or k; otherwise as above.  workspace: hdet_head_rotary_backward_workspace bytes (needed
  * for the gains' gradients only), 16-byte aligned.                                          */
 typedef struct {
   int32_t   n_replicas, dtype;

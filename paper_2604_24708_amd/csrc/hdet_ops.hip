@@ -175,10 +175,44 @@ template <typename A> void attention_arguments(argument_checks& c, const A& a) {
   c.vector("end_dev", a.end_dev, n, rows, rows, false, false);
 }
 
-// Outputs that start where an input or another output does
-void written_apart(argument_checks& c, std::initializer_list<const void*> outputs, std::initializer_list<const void*> inputs, bool any) {
-  for (auto o = outputs.begin(); any && o != outputs.end(); ++o)
-    c.need(std::find(inputs.begin(), inputs.end(), *o) == inputs.end() && std::find(o + 1, outputs.end(), *o) == outputs.end(), "an output lies over an input or another output");
+// A matrix of a call: its place and its extent
+struct extent { hdet_rows m; int64_t rows, width; int size; };
+bool same_place(const extent& a, const extent& b, int n) {
+  return a.m.dev == b.m.dev && a.size == b.size && a.rows == b.rows && a.width == b.width && (a.rows <= 1 || a.m.row_stride == b.m.row_stride) &&
+         (n <= 1 || a.m.replica_stride == b.m.replica_stride);
+}
+// Whether two of n replicas' matrices share memory.  Exact where their strides agree, as those of slices of one matrix do: row j of replica z + dz of b lies dz replica strides
+// and dj row strides from row j - dj of replica z of a; otherwise only matrices that start at the same place do.
+bool share_memory(const extent& a, const extent& b, int n) {
+  if (!a.m.dev || !b.m.dev || a.rows == 0 || b.rows == 0 || a.width == 0 || b.width == 0) return false;
+  if (a.m.dev == b.m.dev) return true;
+  const int64_t row_a = a.m.row_stride * a.size, row_b = b.m.row_stride * b.size, row = a.rows > 1 ? row_a : row_b;
+  const int64_t rep_a = a.m.replica_stride * a.size, rep_b = b.m.replica_stride * b.size, rep = n > 1 ? rep_a : 0;
+  if ((a.rows > 1 && b.rows > 1 && row_a != row_b) || (n > 1 && rep_a != rep_b)) return false;
+  const int64_t wide_a = a.width * a.size, wide_b = b.width * b.size, from = (int64_t)((uintptr_t)b.m.dev - (uintptr_t)a.m.dev);
+  for (int64_t dz = 1 - n; dz < n; ++dz) {
+    // some dj in 1 - a.rows .. b.rows - 1 with -wide_b < x + dj row < wide_a
+    const int64_t x = from + dz * rep;
+    if (a.rows == 1 && b.rows == 1) {
+      if (-wide_b < x && x < wide_a) return true;
+      continue;
+    }
+    const int64_t low = -wide_b - x;                                       // dj row above this; the first dj that is
+    const int64_t dj = std::max((low >= 0 ? low / row : -((-low + row - 1) / row)) + 1, 1 - a.rows);
+    if (dj < b.rows && x + dj * row < wide_a) return true;
+  }
+  return false;
+}
+// Outputs that share memory with an input or another output
+void written_apart(argument_checks& c, int n, std::initializer_list<extent> outputs, std::initializer_list<extent> inputs, bool any) {
+  for (auto o = outputs.begin(); any && c.ok() && o != outputs.end(); ++o) {
+    auto meets = [&](const extent& x) { return share_memory(*o, x, n); };
+    c.need(std::none_of(inputs.begin(), inputs.end(), meets) && std::none_of(o + 1, outputs.end(), meets), "an output lies over an input or another output");
+  }
+}
+// An output that shares memory with an input and is not the whole of it
+void in_place_or_apart(argument_checks& c, int n, const extent& output, const extent& input) {
+  c.need(same_place(output, input, n) || !share_memory(output, input, n), "an output lies over its own input with other strides, or over a part of it");
 }
 
 void clip_sizes(argument_checks& c, int n, int tensors) {
@@ -391,9 +425,16 @@ extern "C" int hdet_head_rotary(const hdet_rotary_args* a, void* stream) {
     const int n = a->n_replicas, size = element(a->dtype);
     c.matrix("q", a->q, n, a->rows, (int64_t)a->q_heads * a->head_dim, size, true, false);
     c.matrix("q_out", a->q_out, n, a->rows, (int64_t)a->q_heads * a->head_dim, size, true, true);
+    const extent q = {a->q, a->rows, (int64_t)a->q_heads * a->head_dim, size}, q_out = {a->q_out, q.rows, q.width, size};
+    if (c.ok()) in_place_or_apart(c, n, q_out, q);
     if (!a->k.dev) return;
     c.matrix("k", a->k, n, a->rows, (int64_t)a->k_heads * a->head_dim, size, true, false);
     c.matrix("k_out", a->k_out, n, a->rows, (int64_t)a->k_heads * a->head_dim, size, true, true);
+    if (!c.ok()) return;
+    const extent k = {a->k, a->rows, (int64_t)a->k_heads * a->head_dim, size}, k_out = {a->k_out, k.rows, k.width, size};
+    in_place_or_apart(c, n, k_out, k);
+    written_apart(c, n, {q_out}, {k, k_out}, true);
+    written_apart(c, n, {k_out}, {q}, true);
   }, [&] { return hdet_launch_rotary(*a, (hipStream_t)stream); });
 }
 
@@ -431,6 +472,17 @@ extern "C" int hdet_head_rotary_backward(const hdet_rotary_grad_args* a, void* s
     }
     c.need(!a->dk_gain_dev || (keys && a->k_gain_dev), "dk_gain_dev needs dk_out and k_gain_dev");
     c.vector("dk_gain_dev", a->dk_gain_dev, n, a->head_dim, a->dk_gain_stride, false, true);
+    if (!c.ok()) return;
+    // (q and k are read where there are gains)
+    const hdet_rows none = {};
+    const extent q = {a->q_gain_dev ? a->q : none, a->rows, wide, size}, dq_out = {a->dq_out, a->rows, wide, size}, dq = {a->dq, a->rows, wide, size};
+    const extent k = {a->k_gain_dev && keys ? a->k : none, a->rows, narrow, size}, dk_out = {a->dk_out, a->rows, narrow, size}, dk = {keys ? a->dk : none, a->rows, narrow, size};
+    in_place_or_apart(c, n, dq, dq_out);
+    in_place_or_apart(c, n, dq, q);
+    in_place_or_apart(c, n, dk, dk_out);
+    in_place_or_apart(c, n, dk, k);
+    written_apart(c, n, {dq}, {k, dk_out, dk}, true);
+    written_apart(c, n, {dk}, {q, dq_out}, true);
     if (c.ok() && (a->dq_gain_dev || a->dk_gain_dev))
       c.workspace(a->workspace_dev, a->workspace_bytes, hdet_rotary_backward_bytes(n, a->rows, a->head_dim, a->q_heads, keys ? a->k_heads : 0));
   }, [&] { return hdet_launch_rotary_backward(*a, (hipStream_t)stream); });
@@ -471,11 +523,11 @@ extern "C" int hdet_attention(const hdet_attention_args* a, void* stream) {
     if (!c.ok()) return;
     attention_arguments(c, *a);
     if (!c.ok()) return;
-    const int n = a->n_replicas;
-    const int64_t rows = (int64_t)a->seqs * a->q_len;
-    c.matrix("out", a->out, n, rows, (int64_t)a->heads * a->head_dim, element(a->dtype), true, true);
+    const int n = a->n_replicas, size = element(a->dtype);
+    const int64_t rows = (int64_t)a->seqs * a->q_len, keys = (int64_t)a->seqs * a->kv_len, wide = (int64_t)a->heads * a->head_dim, narrow = (int64_t)a->kv_heads * a->head_dim;
+    c.matrix("out", a->out, n, rows, wide, size, true, true);
     c.vector("lse_dev", a->lse_dev, n, rows * a->heads, rows * a->heads, false, true);
-    written_apart(c, {a->out.dev}, {a->q.dev, a->k.dev, a->v.dev}, rows * a->kv_len > 0);
+    written_apart(c, n, {{a->out, rows, wide, size}}, {{a->q, rows, wide, size}, {a->k, keys, narrow, size}, {a->v, keys, narrow, size}}, rows * a->kv_len > 0);
     c.workspace(a->workspace_dev, a->workspace_bytes, hdet_attend_bytes(n, a->seqs, a->q_len, a->kv_len, a->heads, a->kv_heads, a->head_dim));
   }, [&] { return hdet_launch_attend(*a, (hipStream_t)stream); });
 }
@@ -502,7 +554,8 @@ extern "C" int hdet_attention_backward(const hdet_attention_grad_args* a, void* 
     c.matrix("dq", a->dq, n, rows, wide, size, true, true);
     c.matrix("dk", a->dk, n, keys, narrow, size, true, true);
     c.matrix("dv", a->dv, n, keys, narrow, size, true, true);
-    written_apart(c, {a->dq.dev, a->dk.dev, a->dv.dev}, {a->q.dev, a->k.dev, a->v.dev, a->out.dev, a->dout.dev}, rows * a->kv_len > 0);
+    written_apart(c, n, {{a->dq, rows, wide, size}, {a->dk, keys, narrow, size}, {a->dv, keys, narrow, size}},
+                  {{a->q, rows, wide, size}, {a->k, keys, narrow, size}, {a->v, keys, narrow, size}, {a->out, rows, wide, size}, {a->dout, rows, wide, size}}, rows * a->kv_len > 0);
     c.workspace(a->workspace_dev, a->workspace_bytes, hdet_attend_backward_bytes(n, a->seqs, a->q_len, a->kv_len, a->heads, a->kv_heads, a->head_dim));
   }, [&] { return hdet_launch_attend_backward(*a, (hipStream_t)stream); });
 }

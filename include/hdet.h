@@ -610,7 +610,9 @@ int hdet_attention_backward(const hdet_attention_grad_args* args, void* stream);
  * the caller.  max_norm infinite: nothing is bounded (and without `out` only the norm is formed).
  * tensors_host: read during the call only (the addresses in it are what a captured graph keeps).  Every tensor is an hdet_rows of rows x width;
  * `out` is fp32 in any strides, or absent: the gradients themselves are scaled, in their type.  No two elements of outputs (and of gradients that are
- * scaled in place) may share memory, within a tensor or between two; two tensors that start at the same place are refused.
+ * scaled in place) may share memory, within a tensor or between two, nor may what is written lie over another tensor's gradient; an output may be its
+ * own gradient itself, an fp32 one, with its strides.  A tensor that is written where another one starts is refused, and so is an output that is seen
+ * to lie over its own gradient otherwise.
  * Elements between the tensors of a plane are left as they are.
  * workspace: hdet_clip_gradients_workspace bytes, 16-byte aligned.                           */
 #define HDET_MAX_GRAD_TENSORS 65536

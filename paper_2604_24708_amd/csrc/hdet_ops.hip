@@ -6,6 +6,7 @@
 #include <math.h>
 
 #include <algorithm>
+#include <functional>
 #include <initializer_list>
 
 namespace {
@@ -190,6 +191,8 @@ bool share_memory(const extent& a, const extent& b, int n) {
   const int64_t rep_a = a.m.replica_stride * a.size, rep_b = b.m.replica_stride * b.size, rep = n > 1 ? rep_a : 0;
   if ((a.rows > 1 && b.rows > 1 && row_a != row_b) || (n > 1 && rep_a != rep_b)) return false;
   const int64_t wide_a = a.width * a.size, wide_b = b.width * b.size, from = (int64_t)((uintptr_t)b.m.dev - (uintptr_t)a.m.dev);
+  // from first to last element they lie apart
+  if (from >= (n - 1) * rep + (a.rows - 1) * row + wide_a || -from >= (n - 1) * rep + (b.rows - 1) * row + wide_b) return false;
   for (int64_t dz = 1 - n; dz < n; ++dz) {
     // some dj in 1 - a.rows .. b.rows - 1 with -wide_b < x + dj row < wide_a
     const int64_t x = from + dz * rep;
@@ -578,7 +581,8 @@ extern "C" int hdet_clip_gradients(const hdet_clip_args* a, void* stream) {
     if (!c.ok()) return;
     const int n = a->n_replicas;
     c.vector("norm_dev", a->norm_dev, n, 1, 1, true, true);
-    std::vector<const void*> starts;
+    struct start { const void* at; int tensor; bool written; };
+    std::vector<start> starts;
     for (int i = 0; i < a->n_tensors && c.ok(); ++i) {
       const hdet_grad_tensor& t = a->tensors_host[i];
       c.type(t.dtype, "dtype of a tensor must be HDET_TYPE_F32 or HDET_TYPE_BF16");
@@ -587,12 +591,22 @@ extern "C" int hdet_clip_gradients(const hdet_clip_args* a, void* stream) {
       const bool in_place = !t.out.dev;
       c.matrix("grad", t.grad, n, t.rows, t.width, element(t.dtype), true, in_place && a->max_norm < INFINITY);
       c.matrix("out", t.out, n, t.rows, t.width, 4, false, true);
-      if (!in_place) starts.push_back(t.out.dev);
-      else if (a->max_norm < INFINITY) starts.push_back(t.grad.dev);
+      starts.push_back({t.grad.dev, i, in_place && a->max_norm < INFINITY});
+      if (in_place || !c.ok()) continue;
+      starts.push_back({t.out.dev, i, true});
+      in_place_or_apart(c, n, {t.out, t.rows, t.width, 4}, {t.grad, t.rows, t.width, element(t.dtype)});
     }
     if (!c.ok()) return;
-    std::sort(starts.begin(), starts.end());
-    c.need(std::adjacent_find(starts.begin(), starts.end()) == starts.end(), "two tensors are written at the same place");
+    // the second pass reads every gradient while others' outputs are written
+    std::sort(starts.begin(), starts.end(), [](const start& x, const start& y) { return std::less<const void*>()(x.at, y.at); });
+    for (size_t i = 0, j; i < starts.size(); i = j) {
+      bool written = false, several = false;
+      for (j = i; j < starts.size() && starts[j].at == starts[i].at; ++j) {
+        written |= starts[j].written;
+        several |= starts[j].tensor != starts[i].tensor;
+      }
+      c.need(!(written && several), "a tensor is written where another one starts");
+    }
     c.workspace(a->workspace_dev, a->workspace_bytes, hdet_clip_bytes(n, a->n_tensors));
   }, [&] { return hdet_launch_clip(*a, (hipStream_t)stream); });
 }

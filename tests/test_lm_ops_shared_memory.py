@@ -1,4 +1,4 @@
-"""Outputs of the rotation and attention that lie over other matrices of the call are refused; in place and next to each other they are not.  No GPU needed: every call here is refused, the
+"""Outputs of the rotation, attention and the clipped gradient that lie over other matrices of the call are refused; in place and next to each other they are not.  No GPU needed: every call here is refused, the
 good ones for a workspace of no bytes, which is looked at last."""
 import ctypes as C
 import random
@@ -7,7 +7,7 @@ import pytest
 
 import paper_2604_24708_amd as H
 from paper_2604_24708_amd import binding as B
-from test_lm_ops_heads_refusals import attention, attention_grad, rotary, rotary_grad, rows
+from test_lm_ops_heads_refusals import attention, attention_grad, clip, rotary, rotary_grad, rows, tensor
 
 BASE = 1 << 40
 OVER = "lies over"
@@ -97,3 +97,31 @@ def test_strides_of_one_matrix_against_every_element():
         assert (OVER if meets else "workspace") in why("hdet_head_rotary_backward", a), (n, length, wide, narrow, row, rep, shift)
         count[meets] += 1
     assert min(count) > 500
+
+
+def places(grad, out, **kw):
+    return tensor(grad=grad, out=out if out is not None else rows(0, 0, None), **kw)
+
+
+HERE, THERE, FAR = at(0, 7, 21), at(4096, 7, 21), at(8192, 7, 21)
+BF16 = dict(dtype=H.HDET_TYPE_BF16)
+
+
+@pytest.mark.parametrize("bad", [
+    # an output where another tensor's gradient starts, whichever comes first, and a gradient that is scaled in place and read by another tensor
+    [places(HERE, THERE), places(FAR, HERE)], [places(FAR, HERE), places(HERE, THERE)], [places(HERE, None), places(HERE, THERE)], [places(HERE, THERE, **BF16), places(FAR, HERE)],
+    [places(HERE, THERE), places(HERE, HERE)],
+    # an output over its own gradient, of other types, strides or a part of it
+    [places(HERE, HERE, **BF16)], [places(HERE, at(0, 8, 24))], [places(HERE, at(0, 7, 22))], [places(HERE, at(4, 7, 21))], [places(HERE, at(-4, 7, 21))], [places(HERE, at(4 * 41, 7, 21))]])
+def test_clipped_gradients(bad):
+    message = why("hdet_clip_gradients", clip(bad))
+    assert OVER in message or "written where another" in message
+
+
+@pytest.mark.parametrize("good", [
+    [places(HERE, HERE)], [places(HERE, at(4 * 42, 7, 21))], [places(HERE, at(0, 9, 21), rows=1)], [places(HERE, None)], [places(HERE, None, **BF16)],
+    [places(HERE, THERE), places(HERE, FAR)],                   # one gradient twice, read alone
+    [places(at(0, 7, 42), at(4096, 7, 42)), places(at(84, 7, 42), at(4096 + 84, 7, 42))], [places(HERE, THERE), places(FAR, FAR), places(at(1 << 20, 7, 21), None)],
+    [places(HERE, THERE), places(FAR, HERE, rows=0)]])
+def test_clipped_gradients_in_place_and_apart(good):
+    assert "workspace" in why("hdet_clip_gradients", clip(good, workspace_bytes=0))

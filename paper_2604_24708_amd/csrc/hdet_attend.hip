@@ -815,11 +815,12 @@ template <typename T, int D, int EXTRA, bool WHOLE, bool TWO> __global__ __launc
     last = __builtin_amdgcn_readfirstlane(last);
   }
   const int t0 = last < 0 ? 0 : first / NB, tiles = last < 0 ? 0 : last / NB + 1 - t0;
-  // this block's part of all heads' tiles (none: zeros, and keys and values are not read, which need not be there without queries)
+  // this block's part of all heads' tiles
   const int share = (tiles * g.group + g.splits - 1) / g.splits, end = min(tiles * g.group, (int)(split + 1) * share), begin = split * share + g.run * run_tiles<T, D>(),
             all = min(end, begin + run_tiles<T, D>());
   if (g.run && begin >= all) return;
-  const bool there = key < g.kv_len && begin < all;
+  // (without queries keys and values need not be there)
+  const bool there = key < g.kv_len && g.q_len > 0;
   const int64_t kcol = (int64_t)kh * g.d, row0 = (int64_t)b * g.kv_len + wk0, rows = (int64_t)g.seqs * g.q_len, q_row0 = (int64_t)b * g.q_len;
   typename S::frag fk[PAIRED ? 1 : S::NF], fv[PAIRED ? 1 : S::NF];
   T* const own_k = smem + RING + (w & 3) * WR * D;
@@ -829,7 +830,7 @@ template <typename T, int D, int EXTRA, bool WHOLE, bool TWO> __global__ __launc
     const T* const from_v = (const T*)g.v + r * g.v_z + ((int64_t)b * g.kv_len + k0) * g.v_s + kcol;
 #pragma unroll
     for (int i = 0; i < RB / S::TB; ++i) {
-      const int have = begin < all ? g.kv_len - k0 - i * S::TB : 0;
+      const int have = g.q_len > 0 ? g.kv_len - k0 - i * S::TB : 0;
       tile_loader<T, D, S::TB, NW, WHOLE>(from_k, g.k_s, g.d, w, lane).load(i * S::TB, have, smem + RING + i * TILE);
       tile_loader<T, D, S::TB, NW, WHOLE>(from_v, g.v_s, g.d, w, lane).load(i * S::TB, have, smem + RING + RB * D + i * TILE);
     }

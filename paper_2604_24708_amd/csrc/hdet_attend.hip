@@ -274,14 +274,88 @@ template <int EXTRA, typename F> __device__ __forceinline__ void shape_scores_ba
 }
 __device__ __forceinline__ float distance(int pos, int key) { return (float)(pos < key ? (unsigned)key - (unsigned)pos : (unsigned)pos - (unsigned)key); }
 
+// fp32 sums over keys are made in runs of 1024: a running sum over M keys rounds M times, at its own size, which takes it 0.3 x 2^-24 sqrt(M) off (8192 keys: out off by 1.8e-6 of its
+// norm, in runs by 6.5e-7).  What bfloat16 rounds elsewhere is far more.  What the runs before the present one have come to is kept
+//   in registers, where there is one wavefront a SIMD all the same;
+template <typename T> constexpr int key_run() { return sizeof(T) == 4 ? 1024 : 1 << 30; }
+template <typename T, int D> struct runs_in_registers {
+  f16v sum[D / 32];
+  __device__ __forceinline__ void reset() {
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i) sum[i] = all16(0.f);
+  }
+  // x and what is kept, times `scale`: KEEP: kept, and x is 0 from then on; else to x.  (Accumulator order: columns of the lane's row.)
+  template <bool KEEP> __device__ __forceinline__ void join(f16v (&x)[D / 32], float scale, int) {
+    if (sizeof(T) == 2) return;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int e = 0; e < 16; ++e) {
+        const float y = __builtin_fmaf(sum[i][e], scale, x[i][e]);
+        sum[i][e] = y;
+        x[i][e] = KEEP ? 0.f : y;
+      }
+  }
+};
+//   in the rows of the result, where registers would cost a wavefront (8 x 8192 queries and keys of 8 heads of 64, us: one sum 8160, in rows 8320, in registers 8700).
+template <typename T, int D> struct runs_in_rows {
+  float* to;                               // the first of the wavefront's rows, `ld` apart
+  int64_t ld;
+  int d;
+  bool some, any;                          // the lane's row takes part; there is something kept
+  __device__ __forceinline__ void reset() { any = false; }
+  template <bool KEEP> __device__ __forceinline__ void join(f16v (&x)[D / 32], float scale, int lane) {
+    if (sizeof(T) == 2 || (!KEEP && !any)) return;
+    asm volatile("" : "+v"(lane));         // addresses and tests are formed here, not held all the way
+    float* const row = some ? to + (lane & 31) * ld : nullptr;
+#pragma unroll
+    for (int i = 0; i < D / 32; ++i)
+#pragma unroll
+      for (int e4 = 0; e4 < 4; ++e4) {
+        const int c = 32 * i + acc_row(4 * e4, lane);
+        f4v y = {x[i][4 * e4], x[i][4 * e4 + 1], x[i][4 * e4 + 2], x[i][4 * e4 + 3]};
+        if (row && c + 4 <= d) {
+          f4v_any* const at = reinterpret_cast<f4v_any*>(row + c);
+          if (any) y += *at * scale;
+          if (KEEP) *at = y;
+        } else if (row) {
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            if (c + u >= d) continue;
+            if (any) y[u] += row[c + u] * scale;
+            if (KEEP) row[c + u] = y[u];
+          }
+        }
+#pragma unroll
+        for (int u = 0; u < 4; ++u) x[i][4 * e4 + u] = KEEP ? 0.f : y[u];
+      }
+    any = true;
+  }
+};
+template <typename T, int D> __device__ __forceinline__ auto runs_of(void* to, int64_t ld, int d, bool some) {
+  if constexpr (D == 64) return runs_in_rows<T, D>{(float*)to, ld, d, some, false};
+  else return runs_in_registers<T, D>();
+}
+
 // Row statistics and results of a wavefront's 32 queries (columns of the accumulators) on its way over the keys
 template <int D> struct running {
   f16v o[D / 32];
   float m, l;                              // reference of the exponentials (log2), this half-wavefront's sum
+  float run_l, rescaled;                   // .. of the runs before; what those are to be multiplied by, since the reference has moved
   __device__ __forceinline__ void reset() {
 #pragma unroll
     for (int i = 0; i < D / 32; ++i) o[i] = all16(0.f);
     m = -INFINITY;
+    l = run_l = 0.f;
+    rescaled = 1.f;
+  }
+  // The end of a run: its results are kept; KEEP false: those of all runs
+  template <bool KEEP, typename K> __device__ __forceinline__ void join(K& kept, int lane) {
+    kept.template join<KEEP>(o, rescaled, lane);
+    l = __builtin_fmaf(run_l, rescaled, l);
+    rescaled = 1.f;
+    if (!KEEP) return;
+    run_l = l;
     l = 0.f;
   }
   __device__ __forceinline__ float ref() const { return m == -INFINITY ? 0.f : m; }
@@ -298,6 +372,7 @@ template <int D> struct running {
         const float next = fmaxf(m, top), keep = exp2_fast(m - (next == -INFINITY ? 0.f : next));
         m = next;
         l *= keep;
+        rescaled *= keep;
 #pragma unroll
         for (int i = 0; i < D / 32; ++i)
 #pragma unroll
@@ -316,8 +391,8 @@ template <int D> struct running {
 // ---------------------------------------------------------------------------------------------
 // forward: block = 128 queries of one (replica, sequence, head)
 // ---------------------------------------------------------------------------------------------
-template <typename T, int D, int EXTRA> constexpr int forward_waves() { return sizeof(T) == 2 ? (D == 64 ? (EXTRA ? 3 : 4) : 2) : (D == 64 ? 2 : 1); }
-template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__(THREADS, (forward_waves<T, D, EXTRA>())) void attend_kernel(const attend_args g) {
+template <typename T, int D, int EXTRA, bool WHOLE> constexpr int forward_waves() { return sizeof(T) == 2 ? (D == 64 ? (EXTRA ? 3 : 4) : 2) : D == 64 ? (WHOLE ? 3 : 2) : 1; }
+template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__(THREADS, (forward_waves<T, D, EXTRA, WHOLE>())) void attend_kernel(const attend_args g) {
   typedef shape<T, D> S;
   constexpr int TILE = S::TB * D, NB = S::TB / 32, LOADS = 2 * tile_loader<T, D, S::TB, NWV, WHOLE>::NI;
   __shared__ __attribute__((aligned(1024))) T smem[2 * STAGES * TILE];     // keys and values
@@ -348,6 +423,7 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
   const int hi = br.hi, t0 = br.lo / S::TB, t1 = (hi + S::TB - 1) / S::TB; // hi = 0: none
 
   running<D> z;
+  auto kept = runs_of<T, D>((T*)g.out + r * g.out_z + row0 * g.out_s + col, g.out_s, g.d, range.hi > range.lo);
   // (every request is as many loads, of zeros behind the last tile, so that a wait can count them)
   auto request = [&](int t, int slot) {
     T* const to = smem + slot * (2 * TILE);
@@ -356,6 +432,7 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
   };
   auto walk = [&](auto clean) {
     z.reset();
+    kept.reset();
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i) request(t0 + i, i);
     int slot = 0, free = STAGES - 1;
@@ -382,14 +459,22 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
         at.template second<decltype(clean)::value>(vt + i * 32 * D, x, z.o);
       }
     };
+    auto next_run = [&](int t) {
+      if (sizeof(T) == 4 && __builtin_expect(t > t0 && (t - t0) % (key_run<T>() / S::TB) == 0, 0)) z.template join<true>(kept, lane);
+    };
     // the reference follows the maximum until every row has met a key; all the way on the second walk, and where scores fall with the distance
     int t = t0;
     for (bool met = false; t < t1 && !met; ++t) {
+      next_run(t);
       step(t, std::true_type());
       met = !(EXTRA == kGeneral && g.slopes) && !__any(range.hi > range.lo && z.m == -INFINITY);
     }
-    for (; t < t1; ++t) step(t, clean);
+    for (; t < t1; ++t) {
+      next_run(t);
+      step(t, clean);
+    }
     wait_and_barrier<0>();
+    if (sizeof(T) == 4) z.template join<false>(kept, lane);
     z.l += other_half(z.l);
   };
   walk(std::false_type());
@@ -450,6 +535,7 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
   T* const mine = smem + w * (4 * TILE);
 
   running<D> z;
+  runs_in_registers<T, D> kept;
   auto request = [&](int t, int stage) {
     const int have = t < te ? hi - t * 32 : 0;
     keys.load((int64_t)t * 32, have, mine + stage * (2 * TILE));
@@ -457,6 +543,7 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
   };
   auto walk = [&](auto clean) {
     z.reset();
+    kept.reset();
     int stage = 0;
     if (ts + w < te) request(ts + w, 0);
     auto step = [&](int t, auto follow) {
@@ -476,13 +563,21 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
       z.template take<decltype(follow)::value>(x, unit.mult);
       at.template second<decltype(clean)::value>(kt + TILE, x, z.o);
     };
+    auto next_run = [&](int t) {
+      if (sizeof(T) == 4 && __builtin_expect(t > ts + w && (t - ts) % (NW * key_run<T>() / 32) == w, 0)) z.template join<true>(kept, lane);
+    };
     int t = ts + w;
     for (bool met = false; t < te && !met; t += NW) {
+      next_run(t);
       step(t, std::true_type());
       met = !(EXTRA == kGeneral && g.slopes) && !__any(range.hi > range.lo && z.m == -INFINITY);
     }
-    for (; t < te; t += NW) step(t, clean);
+    for (; t < te; t += NW) {
+      next_run(t);
+      step(t, clean);
+    }
     asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+    if (sizeof(T) == 4) z.template join<false>(kept, lane);
     z.l += other_half(z.l);
   };
   walk(std::false_type());
@@ -648,6 +743,8 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
   const int parts = few_keys ? 1 : g.splits, share = hi > 0 ? (last - first + parts - 1) / parts : 0, t0 = first + split * share, t1 = hi > 0 ? min(last, t0 + share) : t0;
 
   f16v dq[S::ND];                          // [column][query]
+  float* const part = g.part + (((int64_t)split * g.n + r) * g.heads + h) * rows * D + row0 * D;       // of a divided walk
+  auto kept = runs_of<T, D>(g.splits > 1 ? (void*)part : (T*)g.dq + r * g.dq_z + row0 * g.dq_s + col, g.splits > 1 ? D : g.dq_s, g.d, some);
   // sum over the keys of p (dp - dot): what the dot lacks for out's rounding, since the p sum to 1
   float lack = 0.f;
   // (every request is as many loads, of zeros behind the last tile, so that a wait can count them)
@@ -661,10 +758,12 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
 #pragma unroll
     for (int i = 0; i < S::ND; ++i) dq[i] = all16(0.f);
     lack = 0.f;
+    kept.reset();
 #pragma unroll
     for (int i = 0; i < STAGES - 1; ++i) request(t0 + i, i);
     int slot = 0, free = STAGES - 1;
     for (int t = t0; t < t1; ++t) {
+      if (sizeof(T) == 4 && __builtin_expect(t > t0 && (t - t0) % (key_run<T>() / S::TB) == 0, 0)) kept.template join<true>(dq, 1.f, lane);
       wait_and_barrier<(STAGES - 2) * LOADS>();
       request(t + STAGES - 1, free);
       T* const tiles = smem + slot * (2 * TILE);
@@ -698,6 +797,7 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
       }
     }
     wait_and_barrier<0>();
+    if (sizeof(T) == 4) kept.template join<false>(dq, 1.f, lane);
   };
   // Few keys a row: a dot that is off by out's rounding is off by as much in all of them, and the sum of dz k does not average that away (two keys: dq off by 2.4 times its
   // own rounding): the dots first, then.  Many: it does (1.1 to 1.3 times), with dz in two bfloat16 parts (1.5 in one).
@@ -729,7 +829,7 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
                          [](int, int) { return 0.f; });
   };
   if (g.splits == 1) put((T*)g.dq + r * g.dq_z + row0 * g.dq_s + col, g.dq_s, std::integral_constant<bool, WHOLE>());
-  else put(g.part + (((int64_t)split * g.n + r) * g.heads + h) * rows * D + row0 * D, (int64_t)D, std::false_type());
+  else put(part, (int64_t)D, std::false_type());
 }
 
 // dq and the row dots from the splits' parts, [split][replica][head][row]

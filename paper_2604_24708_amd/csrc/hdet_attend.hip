@@ -1166,9 +1166,9 @@ dim3 grid_of(unsigned blocks) {
   const unsigned x = blocks < (1u << 20) ? blocks : 1u << 20;
   return dim3(x, (blocks + x - 1) / x);
 }
-// what scores need: more than a product with a constant, also where a scale of 0 or below turns the maximum around
+// what scores need: more than a product with a constant, also where a scale of 0 or below turns the maximum around, or is 0 in fp32 (0 times a masked score's infinity)
 template <typename A> int extra(const A& a, const attend_args& g) {
-  return a.slopes_dev || !(a.scale > 0) || (a.softcap > 0 && g.close) ? kGeneral : a.softcap > 0 ? kCapped : kPlain;
+  return a.slopes_dev || !(g.c > 0.f) || (a.softcap > 0 && g.close) ? kGeneral : a.softcap > 0 ? kCapped : kPlain;
 }
 
 // f(type, D, EXTRA, WHOLE); rows that are not whole pieces take the general scores too

@@ -1142,7 +1142,8 @@ template <typename A> attend_args common_args(const A& a) {
   g.n = a.n_replicas; g.seqs = a.seqs; g.q_len = a.q_len; g.kv_len = a.kv_len; g.heads = a.heads; g.kv_heads = a.kv_heads; g.group = a.heads / a.kv_heads;
   g.d = a.head_dim; g.causal = a.causal; g.window = a.window; g.splits = 1;
   g.scale = (float)a.scale; g.c = (float)(a.scale * 1.4426950408889634); g.cap2 = (float)(a.softcap * 1.4426950408889634);
-  g.inv_cap = a.softcap > 0 ? (float)(1.0 / a.softcap) : 0.f;
+  // (scale / cap beyond fp32 is as good at 1e37: products from 1e-36 on are at the cap with either, and one of 0 stays 0)
+  g.inv_cap = a.softcap > 0 ? (float)std::min(1.0 / a.softcap, 1e37 / std::max(fabs(a.scale), 1e-30)) : 0.f;
   g.by_heads = divisor_of(a.heads); g.by_kv_heads = divisor_of(a.kv_heads); g.by_seqs = divisor_of(a.seqs); g.by_group = divisor_of(g.group);
   // bfloat16 inputs: a score off by 1e-7 of a cap up to 1000 moves p by no more than 2^-13 of itself, where its rounding takes 2^-9
   g.close = a.dtype == HDET_TYPE_F32 || a.softcap > 1000.0;

@@ -1322,8 +1322,11 @@ hipError_t hdet_launch_attend_backward(const hdet_attention_grad_args& a, hipStr
     set_blocks(g, nk, (unsigned)a.n_replicas * a.seqs * a.kv_heads);
     g.splits = std::min(dkv_splits(a.n_replicas, a.seqs, a.q_len, a.kv_len, a.heads, a.kv_heads, a.head_dim), dkv_most(a.window, a.q_len, g.group));
     g.total *= g.splits;
+    // query tiles of a part: 128 keys are seen by window + 127 queries in a row, where that is all the mask says
     constexpr int tb = shape<T, d>::TB;
-    const int64_t share = ((int64_t)((a.q_len + tb - 1) / tb) * g.group + g.splits - 1) / g.splits;
+    int64_t tiles = (a.q_len + tb - 1) / tb;
+    if (a.causal && a.window && !a.positions_dev && !a.first_dev && !a.end_dev) tiles = std::min(tiles, ((int64_t)a.window + RB - 2 + tb - 1) / tb + 1);
+    const int64_t share = (tiles * g.group + g.splits - 1) / g.splits;
     for (g.run = 0; g.total && (g.run == 0 || (int64_t)g.run * run_tiles<T, d>() < share); ++g.run) {
       if (two) hipLaunchKernelGGL((attend_dkv_kernel<T, d, ex, w, sizeof(T) == 2>), grid_of(g.total), dim3(dkv_threads<T, d>()), 0, s, g);
       else hipLaunchKernelGGL((attend_dkv_kernel<T, d, ex, w, false>), grid_of(g.total), dim3(dkv_threads<T, d>()), 0, s, g);

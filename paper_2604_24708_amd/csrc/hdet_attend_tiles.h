@@ -205,13 +205,23 @@ __device__ __forceinline__ void add_not_finite(const T* src, int64_t ld, int d, 
     if (!mask) continue;
     for (int i = 0; i < ROWS; ++i) {
       if (!(mask >> (i * S::C) & (S::C == 64 ? ~0ull : (1ull << (S::C & 63)) - 1))) continue;
+      float x[D / 64];
+      bool infinite = false;               // (a NaN has no weight)
+#pragma unroll
+      for (int u = 0; u < D / 64; ++u) {
+        x[u] = lane + 64 * u < d ? hdet_ld(src + (j + i) * ld + lane + 64 * u) : 0.f;
+        infinite = infinite || fabsf(x[u]) == INFINITY;
+      }
+      const bool weighted = __any(infinite);
       for (int own = 0; own < have; ++own) {
         if (!seen(j + i, own)) continue;
-        const float w = weight(j + i, own);
-        for (int c = lane; c < d; c += 64) {
-          const float x = hdet_ld(src + (j + i) * ld + c);
-          if (!finite_of(x)) hdet_st(dst + own * dst_ld + c, hdet_ld(dst + own * dst_ld + c) + x * w);
-        }
+        const float w = weighted ? weight(j + i, own) : 1.f;
+#pragma unroll
+        for (int u = 0; u < D / 64; ++u)
+          if (!finite_of(x[u])) {
+            U* const to = dst + own * dst_ld + lane + 64 * u;
+            hdet_st(to, hdet_ld(to) + x[u] * w);
+          }
       }
     }
   }

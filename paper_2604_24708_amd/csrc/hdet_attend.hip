@@ -337,6 +337,10 @@ template <typename T, int D> __device__ __forceinline__ auto runs_of(void* to, i
   else return runs_in_registers<T, D>();
 }
 
+// Exponentials of up to 2^8 over the reference, all keys': as many powers of 2 that their sum is below 1, and what they are multiplied with stays in range.  (Values near the type's largest,
+// whose mean is finite though the sum is not: taken on one more walk, since small values lose as many powers at fp32's other end.)
+__device__ __forceinline__ float room_for(int keys) { return (float)(9 + 32 - __builtin_clz((unsigned)keys | 1u)); }
+
 // Row statistics and results of a wavefront's 32 queries (columns of the accumulators) on its way over the keys
 template <int D> struct running {
   f16v o[D / 32];
@@ -361,8 +365,8 @@ template <int D> struct running {
   __device__ __forceinline__ float ref() const { return m == -INFINITY ? 0.f : m; }
   // Exponentials of a block of scores times c.  Any reference will do that keeps them in fp32's range (bfloat16's is the same): FOLLOW takes the maximum, once
   // it has risen by more than 2^8 since (so that results are seldom rescaled); without it the reference stays, and where a score is more than 2^127
-  // times larger, the sum says infinity.
-  template <bool FOLLOW> __device__ __forceinline__ void take(f16v& x, float c) {
+  // times larger, the sum says infinity.  room: of as many powers of 2 below it.
+  template <bool FOLLOW> __device__ __forceinline__ void take(f16v& x, float c, float room) {
     if (FOLLOW) {
       float top = x[0];
 #pragma unroll
@@ -379,7 +383,7 @@ template <int D> struct running {
           for (int e = 0; e < 16; ++e) o[i][e] *= keep;
       }
     }
-    const float r = -ref();
+    const float r = -ref() - room;
 #pragma unroll
     for (int e = 0; e < 16; ++e) {
       x[e] = exp2_fast(__builtin_fmaf(x[e], c, r));
@@ -424,6 +428,7 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
 
   running<D> z;
   auto kept = runs_of<T, D>((T*)g.out + r * g.out_z + row0 * g.out_s + col, g.out_s, g.d, range.hi > range.lo);
+  float room = 0.f;
   // (every request is as many loads, of zeros behind the last tile, so that a wait can count them)
   auto request = [&](int t, int slot) {
     T* const to = smem + slot * (2 * TILE);
@@ -455,7 +460,7 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
 #pragma unroll
           for (int e = 0; e < 16; ++e) x[e] = from + acc_row(e, 0) < len ? x[e] : -INFINITY;
         }
-        z.template take<decltype(follow)::value>(x, unit.mult);
+        z.template take<decltype(follow)::value>(x, unit.mult, decltype(clean)::value ? room : 0.f);
         at.template second<decltype(clean)::value>(vt + i * 32 * D, x, z.o);
       }
     };
@@ -478,15 +483,20 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
     z.l += other_half(z.l);
   };
   walk(std::false_type());
-  const bool again = block_any(there && z.l == z.l && (z.l == INFINITY || not_finite(z.o)), w, lane, (int*)(smem + 2 * STAGES * TILE) - NWV);
-  if (again) walk(std::true_type());
+  int* const any = (int*)(smem + 2 * STAGES * TILE) - NWV;
+  const bool again = block_any(there && z.l == z.l && (z.l == INFINITY || not_finite(z.o)), w, lane, any);
+  while (again) {
+    walk(std::true_type());
+    if (room > 0.f || !block_any(there && z.l == z.l && not_finite(z.o), w, lane, any)) break;
+    room = room_for(g.kv_len);
+  }
   const bool some = range.hi > range.lo;
   const float inv = some ? 1.f / z.l : 0.f;
 #pragma unroll
   for (int i = 0; i < S::ND; ++i)
 #pragma unroll
     for (int e = 0; e < 16; ++e) z.o[i][e] = some ? z.o[i][e] * inv : 0.f;
-  if (g.lse && there && lane < 32) g.lse[((int64_t)r * g.heads + h) * g.seqs * g.q_len + row0 + lane] = some ? (z.ref() + unit.mult * unit.shift + log2f(z.l)) * kLn2 : -INFINITY;
+  if (g.lse && there && lane < 32) g.lse[((int64_t)r * g.heads + h) * g.seqs * g.q_len + row0 + lane] = some ? (z.ref() + room + unit.mult * unit.shift + log2f(z.l)) * kLn2 : -INFINITY;
   store_rows<T, D, WHOLE>(z.o, (char*)smem + w * STRIP, (T*)g.out + r * g.out_z + row0 * g.out_s + col, g.out_s, g.q_len - wq0, g.d, lane);
   if (again) {
     __threadfence_block();
@@ -536,6 +546,7 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
 
   running<D> z;
   runs_in_registers<T, D> kept;
+  float room = 0.f;
   auto request = [&](int t, int stage) {
     const int have = t < te ? hi - t * 32 : 0;
     keys.load((int64_t)t * 32, have, mine + stage * (2 * TILE));
@@ -560,7 +571,7 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
 #pragma unroll
         for (int e = 0; e < 16; ++e) x[e] = from + acc_row(e, 0) < len ? x[e] : -INFINITY;
       }
-      z.template take<decltype(follow)::value>(x, unit.mult);
+      z.template take<decltype(follow)::value>(x, unit.mult, decltype(clean)::value ? room : 0.f);
       at.template second<decltype(clean)::value>(kt + TILE, x, z.o);
     };
     auto next_run = [&](int t) {
@@ -581,9 +592,13 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
     z.l += other_half(z.l);
   };
   walk(std::false_type());
-  // (2^64: room for the sum over wavefronts and parts)
-  const bool again = __any(there && z.l == z.l && (z.l > 0x1p64f || not_finite(z.o)));
-  if (again) walk(std::true_type());
+  // (2^64 and 2^-9: for the sum over wavefronts and parts, 256 at most)
+  const bool again = __any(there && z.l == z.l && (z.l > 0x1p64f || not_finite(z.o, 0x1p9f)));
+  while (again) {
+    walk(std::true_type());
+    if (room > 0.f || !__any(there && z.l == z.l && not_finite(z.o, 0x1p9f))) break;
+    room = room_for(g.kv_len);
+  }
 
   // join the wavefronts
   float* const joint = (float*)smem;       // [wave][32][P], then [wave][32] references and sums
@@ -606,7 +621,7 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
                            });
   }
   if (lane < 32) {
-    stats[w * 64 + lane] = z.m;
+    stats[w * 64 + lane] = z.m + room;
     stats[w * 64 + 32 + lane] = z.l;
   }
   __syncthreads();

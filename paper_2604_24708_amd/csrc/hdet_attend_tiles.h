@@ -167,12 +167,13 @@ template <int D> struct shape<float, D> {
   }
 };
 
-template <int N> __device__ __forceinline__ bool not_finite(const f16v (&x)[N]) {
+// Whether any of x, times a power of 2, is not finite
+template <int N> __device__ __forceinline__ bool not_finite(const f16v (&x)[N], float times = 1.f) {
   float s = 0.f;
 #pragma unroll
   for (int i = 0; i < N; ++i)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) s = __builtin_fmaf(x[i][e], 0.f, s);
+    for (int e = 0; e < 16; ++e) s = __builtin_fmaf(x[i][e] * times, 0.f, s);
   return s != 0.f;
 }
 

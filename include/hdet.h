@@ -607,7 +607,8 @@ int hdet_attention_backward(const hdet_attention_grad_args* args, void* stream);
  *   norm_r = sqrt of the sum of g^2 over all tensors of replica r; with HDET_GRAD_SHARED that of the replicas' mean gradient, the same for all r
  *   out = g factor_r,  factor_r = max_norm / norm_r where norm_r > max_norm, else 1
  * Sums are 64 bits in a fixed order, the factor is rounded to fp32.  A norm that is not finite leaves factor 1: norm_dev says so to
- * the caller.  max_norm infinite: nothing is bounded (and without `out` only the norm is formed).
+ * the caller.  (A norm that is finite and beyond fp32 is written as infinity and bounds the gradients all the same.)  max_norm infinite: nothing is
+ * bounded (and without `out` only the norm is formed).
  * tensors_host: read during the call only (the addresses in it are what a captured graph keeps).  Every tensor is an hdet_rows of rows x width;
  * `out` is fp32 in any strides, or absent: the gradients themselves are scaled, in their type.  No two elements of outputs (and of gradients that are
  * scaled in place) may share memory, within a tensor or between two, nor may what is written lie over another tensor's gradient; an output may be its

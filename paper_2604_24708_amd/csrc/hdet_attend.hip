@@ -14,14 +14,18 @@
 // attend them (add_not_finite): values and output gradients times p, which is 0 for a score of minus infinity and more for any other; keys and queries
 // times dz, which is 0 wherever an entry is infinite and its row's statistics are finite (p is 0, or the cap's derivative): NaN.
 
-// Four kernels: attend (128 queries of a head a block), attend_few (few queries: the keys are divided over the chip), attend_dq and attend_dkv (backward; S = q k and dp are formed in
-// both, since one kernel for all three gradients would add up dq with atomics, in an order that changes).  A wavefront owns 32 rows, as columns of the 32 x 32 products, so that a
-// row's statistics lie in two lanes and a product's result is the next one's operand without a way through LDS.  Tiles of the other side (64 rows of bfloat16, 64 columns) come by
-// direct loads to LDS, one stage ahead; the wavefronts of other blocks on the same CU cover the waits, so registers are what decides: 8 x 16 sequences of 256, 8 heads of 64, forward
-// 4 wavefronts a SIMD 32 us; a variant with spills at that many: 2 to 3 times.
-// Bound by the work between the two products of a block (16 exponentials a lane, sums, conversions) as much as by the products themselves, which wait for it: longer heads, more of the
-// library's rate.  Reached, TFLOP/s (library's product: 1190 to 1270 bfloat16, 154 fp32): forward, 8192 queries and keys, heads of 64 850, of
-// 128 950; of 128 causal, 268 us, 1020 of the pairs that are attended; fp32 114; backward (5 products a pair), heads of 64 550 to 650.
+// Four kernels: attend (128 queries of a head a block), attend_few (few queries: the keys are divided over the chip), attend_dq and attend_dkv
+// (backward; S = q k and dp are formed in both, since one kernel for all three gradients would add up dq with atomics, in an order that changes).  A
+// wavefront owns 32 rows, as columns of the 32 x 32 products, so that a row's statistics lie in two lanes and a product's result is the next one's
+// operand without a way through LDS.  Tiles of the other side (64 rows of bfloat16, 64 columns) come by direct loads to LDS, requested one stage ahead.
+// (In attend_kernel the compiler waits for every load in flight before a block's first product, the next tile's among them, since it holds the queries'
+// own loads for pending; in attend_dkv_kernel it does at the ranges of 32 queries, a load in the loop.)  The wavefronts of other blocks on the same CU
+// cover the waits, so registers are what decides: 8 x 16 sequences of 256, 8 heads of 64, forward 4 wavefronts a SIMD 32 us; a variant with spills at
+// that many: 2 to 3 times.
+// Bound by the work between the two products of a block (16 exponentials a lane, sums, conversions) as much as by the products themselves, which wait
+// for it: longer heads, more of the library's rate.  Reached, TFLOP/s (library's product: 1190 to 1270 bfloat16, 154 fp32): forward, 8192 queries and
+// keys, heads of 64 910, of 128 950; of 128 causal, 278 to 304 us, 990 to 905 of the pairs that are attended; fp32 112 to 132; backward (5 products a
+// pair), heads of 64 550 to 650.
 
 #include <limits.h>
 #include <math.h>
@@ -41,7 +45,8 @@ constexpr int NWV = THREADS / 64;
 constexpr int WR = 32;                     // rows a wavefront owns
 constexpr int RB = WR * NWV;               // rows a block owns
 
-// n / d for any 32-bit n by a product and shifts: a division is some thirty instructions before a block's first load
+// n / d for any 32-bit n by a product and shifts (Granlund and Montgomery, Division by Invariant Integers using Multiplication, 1994): a division is
+// some thirty instructions before a block's first load
 struct divisor { unsigned d, mul, s1, s2; };
 divisor divisor_of(unsigned d) {
   divisor v = {d, 0, 0, 0};
@@ -82,8 +87,9 @@ struct attend_args {
   bool heavy_first;
 };
 
-// Stages of two tiles (keys and values, or queries and output gradients) in LDS: one that is worked on, the other on its way.  (A third one: forward 167 -> 193 us
-// at 8 x 16 sequences of 512, 16 heads of 64, for the blocks that the LDS then holds; without it lost, the same.)
+// Stages of two tiles (keys and values, or queries and output gradients) in LDS: one that is worked on, the other on its way.  (A third one, under the
+// compiler's wait above: forward 167 -> 193 us at 8 x 16 sequences of 512, 16 heads of 64, for the blocks that the LDS then holds; with LDS for as many
+// blocks, the same as two.)
 constexpr int STAGES = 2;
 
 struct key_range { int lo, hi, pos; };
@@ -274,8 +280,9 @@ template <int EXTRA, typename F> __device__ __forceinline__ void shape_scores_ba
 }
 __device__ __forceinline__ float distance(int pos, int key) { return (float)(pos < key ? (unsigned)key - (unsigned)pos : (unsigned)pos - (unsigned)key); }
 
-// fp32 sums over keys are made in runs of 1024: a running sum over M keys rounds M times, at its own size, which takes it 0.3 x 2^-24 sqrt(M) off (8192 keys: out off by 1.8e-6 of its
-// norm, in runs by 6.5e-7).  What bfloat16 rounds elsewhere is far more.  What the runs before the present one have come to is kept
+// fp32 sums over keys are made in runs of 1024: a running sum over M keys rounds M times, at its own size, which takes it 0.3 x 2^-24 sqrt(M) off (8192
+// keys: out off by 1.8e-6 of its norm, in runs by 6.6e-7).  What bfloat16 rounds elsewhere is far more.  What the runs before the present one have come
+// to is kept
 //   in registers, where there is one wavefront a SIMD all the same;
 template <typename T> constexpr int key_run() { return sizeof(T) == 4 ? 1024 : 1 << 30; }
 template <typename T, int D> struct runs_in_registers {
@@ -297,7 +304,8 @@ template <typename T, int D> struct runs_in_registers {
       }
   }
 };
-//   in the rows of the result, where registers would cost a wavefront (8 x 8192 queries and keys of 8 heads of 64, us: one sum 8160, in rows 8320, in registers 8700).
+//   in the rows of the result, where registers would cost a wavefront (8 x 8192 queries and keys of 8 heads of 64, us: one sum 8160, in rows 8350, in
+//   registers 8700).
 template <typename T, int D> struct runs_in_rows {
   float* to;                               // the first of the wavefront's rows, `ld` apart
   int64_t ld;
@@ -337,8 +345,9 @@ template <typename T, int D> __device__ __forceinline__ auto runs_of(void* to, i
   else return runs_in_registers<T, D>();
 }
 
-// Exponentials of up to 2^8 over the reference, all keys': as many powers of 2 that their sum is below 1, and what they are multiplied with stays in range.  (Values near the type's largest,
-// whose mean is finite though the sum is not: taken on one more walk, since small values lose as many powers at fp32's other end.)
+// Exponentials of up to 2^8 over the reference, all keys': as many powers of 2 that their sum is below 1, and what they are multiplied with stays in
+// range.  (Values near the type's largest, whose mean is finite though the sum is not: taken on one more walk, since small values lose as many powers at
+// fp32's other end.)
 __device__ __forceinline__ float room_for(int keys) { return (float)(9 + 32 - __builtin_clz((unsigned)keys | 1u)); }
 
 // Row statistics and results of a wavefront's 32 queries (columns of the accumulators) on its way over the keys
@@ -1182,7 +1191,8 @@ dim3 grid_of(unsigned blocks) {
   const unsigned x = blocks < (1u << 20) ? blocks : 1u << 20;
   return dim3(x, (blocks + x - 1) / x);
 }
-// what scores need: more than a product with a constant, also where a scale of 0 or below turns the maximum around, or is 0 in fp32 (0 times a masked score's infinity)
+// what scores need: more than a product with a constant, also where a scale of 0 or below turns the maximum around, or is 0 in fp32 (0 times a masked
+// score's infinity)
 template <typename A> int extra(const A& a, const attend_args& g) {
   return a.slopes_dev || !(g.c > 0.f) || (a.softcap > 0 && g.close) ? kGeneral : a.softcap > 0 ? kCapped : kPlain;
 }

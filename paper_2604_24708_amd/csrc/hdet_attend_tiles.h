@@ -192,7 +192,8 @@ template <typename T> __device__ __forceinline__ float pair_weight(const T* q, c
   for (int c = lane; c < d; c += 64) s = __builtin_fmaf(hdet_ld(q + c), hdet_ld(k + c), s);
   return hdet_wave_sum(s) * scale == -INFINITY ? 0.f : 1.f;
 }
-// What is not finite in rows from .. to - 1 of src, times weight(row, own row), is added to the rows of dst that attend them (seen(row, own row)): a wavefront's `have` rows
+// What is not finite in rows from .. to - 1 of src, times weight(row, own row), is added to the rows of dst that attend them (seen(row, own row)): a
+// wavefront's `have` rows
 template <typename T, int D, typename U, typename F, typename G>
 __device__ __forceinline__ void add_not_finite(const T* src, int64_t ld, int d, int from, int to, U* dst, int64_t dst_ld, int have, int lane, F seen, G weight) {
   typedef shape<T, D> S;

@@ -3,10 +3,12 @@
 //   norm_r = sqrt(sum over tensors and elements of g^2);  with shared gradients g is the replicas' mean;  out = g factor
 //
 // Bound by memory: every gradient is read twice, since its factor depends on all of them, and written once.  Tensors are cut into pieces of
-// CHUNK elements; block b of G takes pieces b, b + G, b + 2 G .., so that all blocks together read neighbouring memory (a run of pieces each: 1950 us
-// for the 870 million elements of a 12-layer transformer's four replicas, 1825 so; 1745 with what the next lines say: 525 for the norm, 1245 for the rest, 5.3 TB/s over both), whatever tensors they belong to, and sums in 64 bits and a fixed order.  The second kernel's
-// blocks each add up the same partial sums (a few KB) instead of waiting for a third launch, and walk from the end, where the memory-side cache still
-// holds what the first kernel read last.
+// CHUNK elements; block b of G takes pieces b, b + G, b + 2 G .., so that all blocks together read neighbouring memory, whatever tensors they
+// belong to, and sums in 64 bits and a fixed order.  The second kernel's blocks each add up the same partial sums (a few KB) instead of waiting for a
+// third launch, and walk from the end, where the memory-side cache still holds what the first kernel read last.
+//   us for the 870 million elements of a 12-layer transformer's four replicas: 1750, 520 for the norm and 1250 for the rest under the profiler, 5.3 TB/s
+//   over both.  A run of pieces a block: 1950; 1825 without the numbers of blocks and the stores past the caches of hdet_launch_clip.
+// A list of more than INLINE tensors is written to the workspace first, INLINE of them a launch (2 to 5 us each).
 
 #include <math.h>
 

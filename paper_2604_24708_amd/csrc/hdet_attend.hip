@@ -841,7 +841,7 @@ template <typename T, int D, int EXTRA, bool WHOLE> __global__ __launch_bounds__
 #pragma unroll
   for (int i = 0; i < S::ND; ++i)
 #pragma unroll
-    for (int e = 0; e < 16; ++e) dq[i][e] *= g.scale;
+    for (int e = 0; e < 16; ++e) dq[i][e] = some ? dq[i][e] * g.scale : 0.f;               // (a row that attends nothing has not asked for the second walk)
   char* const strip = (char*)smem + w * STRIP;
   auto put = [&](auto to, int64_t ld, auto wh) {
     typedef std::remove_pointer_t<decltype(to)> U;

@@ -208,3 +208,20 @@ def test_infinite_values_and_output_gradients_of_weight_zero(q_len, heads, d, dt
     others = torch.arange(kv_len, device=DEV) != at
     assert bool(torch.isnan(dv[:, at, :, 9]).all()) and bool((dv[:, others][..., 9] == math.inf).all())
     assert bool(torch.isfinite(dv[..., torch.arange(d, device=DEV) != 9]).all())
+
+
+@each
+@pytest.mark.parametrize("bad", [math.nan, math.inf, -math.inf], ids=str)
+@pytest.mark.parametrize("n,seqs,q_len,kv_len,heads,kv_heads,d", [(1, 1, 40, 8, 2, 1, 64), (2, 2, 70, 70, 4, 2, 40), (16, 2, 300, 200, 8, 8, 128), (1, 1, 700, 700, 1, 1, 64)])
+def test_rows_that_attend_nothing_beside_rows_of_such_keys_alone(n, seqs, q_len, kv_len, heads, kv_heads, d, bad, dtype):
+    """Every row that attends anything has no finite results (a NaN, or weight 0 or an infinite score for all its keys); the others' are 0 all the same."""
+    q, k, v, dout = inputs(n, seqs, q_len, kv_len, heads, kv_heads, d, dtype, seed=d)
+    q.view(n, -1, heads, d)[..., 5] = 1.0
+    k.view(n, -1, kv_heads, d)[..., 5] = bad
+    at = torch.arange(q_len, device=DEV).repeat(seqs)
+    end = ints(torch.where(at % 3 == 1, 0, kv_len).expand(n, -1))
+    out, lse = forward(q, k, v, heads, kv_heads, seqs, causal=False, end=end)
+    dq, dk, dv = backward(q, k, v, out, lse, dout, heads, kv_heads, seqs, causal=False, end=end)
+    empty = at % 3 == 1
+    assert not out[:, empty].any() and bool((lse[..., empty] == -math.inf).all()) and not dq[:, empty].any()
+    assert all(bool(torch.isnan(x).all()) for x in (out[:, ~empty], dq[:, ~empty], dk, dv))

@@ -171,7 +171,8 @@ __device__ __forceinline__ wave_range plain_range_of(const attend_args& g, int i
   if (a.hi <= a.lo) return {0, INT_MAX, 0, b.hi};
   return {a.lo, b.lo, a.hi, b.hi};
 }
-// ... of a wavefront's 32 queries, the lanes' ranges given, and (lo, hi) of the block's 128 from q0 on, through LDS that nothing else uses before the next barrier but one
+// ... of a wavefront's 32 queries, the lanes' ranges given, and (lo, hi) of the block's 128 from q0 on, through LDS that nothing else uses before the
+// next barrier but one
 struct block_range { wave_range own; int lo, hi, pairs; };                // pairs: of the block's rows, about
 __device__ __forceinline__ block_range block_range_of(const attend_args& g, const key_range& k, bool there, int q0, int w, int lane, int* ends) {
   block_range b;
@@ -877,14 +878,15 @@ template <typename T, int D> __global__ __launch_bounds__(THREADS) void attend_d
 // ---------------------------------------------------------------------------------------------
 // backward, step 2: dk and dv; block = 128 keys of a key head, walks over the query tiles of the heads that share it
 // ---------------------------------------------------------------------------------------------
-// bfloat16 heads of more than 64 columns: two wavefronts to 32 keys, one to either half of a query tile, and the own keys and values in LDS, since in registers they leave
-// room for one wavefront a SIMD (the backward pass of 2 x 8192 tokens, 8 query and 2 key heads of 128, in undivided walks: 1610 us, in registers 2231; 8 x 4 x 1024 tokens of 8 and 8: 440, 530)
+// bfloat16 heads of more than 64 columns: two wavefronts to 32 keys, one to either half of a query tile, and the own keys and values in LDS, since in
+// registers they leave room for one wavefront a SIMD (the backward pass of 2 x 8192 tokens, 8 query and 2 key heads of 128, in undivided walks: 1610
+// us, in registers 2231; 8 x 4 x 1024 tokens of 8 and 8: 440, 530)
 template <typename T, int D> constexpr bool dkv_paired() { return sizeof(T) == 2 && D == 128; }
 template <typename T, int D> constexpr int dkv_threads() { return dkv_paired<T, D>() ? 512 : 256; }
 template <typename T, int D, int EXTRA, bool TWO> constexpr int dkv_waves() { return sizeof(T) == 2 ? (D == 64 && !EXTRA && !TWO ? 3 : 2) : D == 64 ? 2 : 1; }
-// Query tiles that one launch sums up: in fp32 1024 rows, and the next launch adds its sums to what the one before has written, since a running sum over all rows of the heads
-// that share a key head rounds once a row (4 heads of 1088 rows: dk and dv off by 1.3e-6 of their norms,
-// in runs by 7.9e-7; 2 x 8192 tokens of 4 heads and one key head: the backward pass in undivided walks 3400 -> 3780 us)
+// Query tiles that one launch sums up: in fp32 1024 rows, and the next launch adds its sums to what the one before has written, since a running sum
+// over all rows of the heads that share a key head rounds once a row (4 heads of 1088 rows: dk and dv off by 1.3e-6 of their norms, in runs by
+// 7.9e-7; 2 x 8192 tokens of 4 heads and one key head: the backward pass in undivided walks 3400 -> 3780 us)
 template <typename T, int D> constexpr int run_tiles() { return sizeof(T) == 2 ? 1 << 28 : 1024 / shape<T, D>::TB; }
 // TWO: dk and dv from dz and p in two bfloat16 parts each
 template <typename T, int D, int EXTRA, bool WHOLE, bool TWO> __global__ __launch_bounds__((dkv_threads<T, D>()), (dkv_waves<T, D, EXTRA, TWO>())) void attend_dkv_kernel(const attend_args g) {
@@ -1216,11 +1218,13 @@ template <typename F> void with_shape(int dtype, int d, int ex, bool wh, F f) {
   else with_d(float());
 }
 
-// Parts of the keys for few queries, 0: the queries fill the chip.  Up to 16 queries: always a part at least.  More: where blocks of 32 rows, whose four wavefronts divide
-// the keys, are no more than fit the chip at once, a block's way being four times as short (us; 128 queries a block, 32):
-//   blocks of 32   8 x 8 x 512 keys, 64 columns 256: 12.1, 9.4     fp32 45, 17       16 x 8 x 1024 512: 19.6, 13.8     8 x 8 x 2048 512: 33.5, 18.0      8 x 8 x 4096 1024: 62, 43.5
+// Parts of the keys for few queries, 0: the queries fill the chip.  Up to 16 queries: always a part at least.  More: where blocks of 32 rows, whose
+// four wavefronts divide the keys, are no more than fit the chip at once, a block's way being four times as short (us; 128 queries a block, 32):
+//   blocks of 32   8 x 8 x 512 keys, 64 columns 256: 12.1, 9.4     fp32 45, 17       16 x 8 x 1024 512: 19.6, 13.8
+//                  8 x 8 x 2048 512: 33.5, 18.0      8 x 8 x 4096 1024: 62, 43.5
 //   128 columns    8 x 512 128: 15.9, 11.2      32 x 512 queries of 8192 keys 512: 194, 108     16 x 2048 1024: 47, 61
-// (Under 128 keys two or more of the four wavefronts have nothing: 32 keys of 16 x 4, fp32, 7.8, 9.4.  With more blocks the join, 64 to 128 KB of LDS a block and four times the tiles cost more: 6 x 333 keys of 8 x 128 13, 33.)
+// (Under 128 keys two or more of the four wavefronts have nothing: 32 keys of 16 x 4, fp32, 7.8, 9.4.  With more blocks the join, 64 to 128 KB of LDS
+// a block and four times the tiles cost more: 6 x 333 keys of 8 x 128 13, 33.)
 int few_splits(int n, int seqs, int q_len, int kv_len, int heads, int kv_heads, int head_dim, int window) {
   const int64_t pairs = (int64_t)(heads / kv_heads) * q_len, groups = (int64_t)n * seqs * kv_heads, cus = hdet_compute_units();
   if (pairs == 0 || groups == 0) return 0;
@@ -1232,9 +1236,10 @@ int few_splits(int n, int seqs, int q_len, int kv_len, int heads, int kv_heads, 
 }
 constexpr size_t up256(size_t x) { return (x + 255) & ~(size_t)255; }
 
-// Parts of a block's walk in the backward pass, of `tiles` tiles: where there are fewer blocks than CUs, two tiles at least a part; up to two blocks a CU of eight tiles at least and, of up
-// to 64 columns, four of sixteen, since one or two blocks leave a CU waiting (the backward pass, us: 8 x 8 x 1024 tokens, 8 heads of 64 over 2: 128, 100; 4096 of 8 x 64: 235, 166; 8192 of
-// 4 x 64: 453, 220; 4096 of 8 over 2 x 128: 303, 234; fp32 2 x 2048 of 8 x 128: 954, 604.  Four blocks a CU of 128 columns: 2 x 2048 of 16 x 128 272, 305).
+// Parts of a block's walk in the backward pass, of `tiles` tiles: where there are fewer blocks than CUs, two tiles at least a part; up to two blocks
+// a CU of eight tiles at least and, of up to 64 columns, four of sixteen, since one or two blocks leave a CU waiting (the backward pass, us: 8 x 8 x
+// 1024 tokens, 8 heads of 64 over 2: 128, 100; 4096 of 8 x 64: 235, 166; 8192 of 4 x 64: 453, 220; 4096 of 8 over 2 x 128: 303, 234; fp32 2 x 2048 of
+// 8 x 128: 954, 604.  Four blocks a CU of 128 columns: 2 x 2048 of 16 x 128 272, 305).
 int parts_of(int64_t blocks, int64_t tiles, int head_dim) {
   if (blocks == 0) return 1;
   const int64_t cus = hdet_compute_units();

@@ -229,8 +229,8 @@ __device__ __forceinline__ void add_not_finite(const T* src, int64_t ld, int d, 
   }
 }
 
-// 16 bytes of a row of d elements from column col on, zeros behind the last, wherever the row lies: a load from within the row, moved into place (32 sequences of 512, 4 heads of 50: forward 26 us,
-// backward 79; element by element 46, 125)
+// 16 bytes of a row of d elements from column col on, zeros behind the last, wherever the row lies: a load from within the row, moved into place (32
+// sequences of 512, 4 heads of 50: forward 26 us, backward 79; element by element 46, 125)
 typedef f4v f4v_any __attribute__((aligned(2)));
 template <typename T> __device__ __forceinline__ f4v piece_of(const T* row, int col, int d) {
   constexpr int E = 16 / sizeof(T);

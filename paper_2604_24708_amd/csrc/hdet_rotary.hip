@@ -7,8 +7,8 @@
 // stores cover whole lines; halves that turn with each other are exchanged between lanes as they lie in memory.  (8 columns and the 8 they turn with in one
 // lane, which exchanges nothing: 74 us for 8 x 8192 rows of 20 heads of 64, a line in two halves by two loads.)  A block first forms the cosines and
 // sines of its rows, once for all heads of a row, in LDS, then walks over the heads, two a team on their way at once.
-//   us (TB/s of what is read and written), forward / backward: 8 x 4096 rows of 16 heads of 64 31 (4.4) / 46 (4.4), 8 x 8192 rows of 20 heads, half of each turning, 63 (5.3) /
-//   105 (4.8), both bfloat16 with gains; the gains' partial sums take another 5 to 8.  An addition over 8 GiB makes 6.2.
+//   us (TB/s of what is read and written), forward / backward: 8 x 4096 rows of 16 heads of 64 31 (4.4) / 46 (4.4), 8 x 8192 rows of 20 heads, half
+//   of each turning, 63 (5.3) / 105 (4.8), both bfloat16 with gains; the gains' partial sums take another 5 to 8.  An addition over 8 GiB makes 6.2.
 // Heads that are no whole pieces of 16 bytes at 16-byte boundaries go element by element, 8 pairs a lane (loose).
 
 #include <algorithm>
@@ -371,8 +371,8 @@ int team_of(int d, int each) {
   return t;
 }
 
-// Rows of a block's table: as many as give every thread a head (few heads of few columns: 4 x 16 sequences of 2525 tokens, 3 heads of 16, forward and backward 117 us, 198 in
-// tables of up to 16 rows), while that leaves two blocks a CU, within the table
+// Rows of a block's table: as many as give every thread a head (few heads of few columns: 4 x 16 sequences of 2525 tokens, 3 heads of 16, forward and
+// backward 117 us, 198 in tables of up to 16 rows), while that leaves two blocks a CU, within the table
 int table_rows_of(int64_t rows, int n, int d, int half, int heads) {
   int most = half ? MAX_TABLE / half : MAX_TABLE;
   int want = THREADS / team_of(d, 8) / heads;
